@@ -77,8 +77,10 @@ typedef enum estp_act { ESTP_ACT_RELU = 0, ESTP_ACT_GELU_TANH = 1 } estp_act;
 
 /* Library version, e.g. 200 for 0.2.0.  The version this header describes is
  * ESTP_VERSION; a library whose estp_version() differs has other signatures.
- * 0.2.0 added the vocab_argmax argument of estp_token_entropy. */
-#define ESTP_VERSION 200
+ * 0.2.0 added the vocab_argmax argument of estp_token_entropy; 0.3.0 the calls
+ * estp_token_loss(_backward), estp_tree_attention, estp_tree_importance and
+ * estp_cache_evict. */
+#define ESTP_VERSION 300
 ESTP_API int estp_version(void);
 
 /* Static text for a status code. */
@@ -320,6 +322,131 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
                          int act, const float* edges, const float* centres, float* theta, float* m, float* v,
                          int32_t step, float lambda3, float lr, float beta1, float beta2, float eps,
                          float weight_decay, float* loss, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * LM-head loss of given next tokens, and its gradient.
+ *
+ *   z_i = W x_i,  lse_i = log sum_v exp z_i[v],  loss_i = lse_i - z_i[t_i]
+ *
+ * the softmax cross entropy of token t_i (its negative log-probability, in
+ * nats) under the distribution whose entropy is estp_token_entropy's H_i.  The
+ * logits never reach memory: lse comes from the same pass over the vocabulary,
+ * which can also return H and the most probable token.
+ *
+ *   targets [n_tok]  int32; a token whose target is outside [0, V) (-100, say) is
+ *                    ignored: its loss is 0
+ *   loss [n_tok]     float32 output, at least 0
+ *   lse  [n_tok]     float32 output, natural log, of every token (ignored ones too):
+ *                    what estp_token_loss_backward takes
+ *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL
+ * Other arguments and requirements are those of estp_token_entropy.
+ *
+ * estp_token_loss_backward: with grad_i the gradient of the objective with
+ * respect to loss_i,
+ *
+ *   G_iv = grad_i (exp(z_i[v] - lse_i) - [v = t_i]),  dX = G W,  dW = G^T X
+ *
+ *   lse  [n_tok]     of estp_token_loss on the same X and W
+ *   grad [n_tok]     float32, or NULL (all 1)
+ *   dX [n_tok, d]    output (dtype), or NULL; rows of ignored tokens are 0
+ *   dW [V, d]        output (dtype), or NULL; 16-byte aligned both, not both NULL
+ * Rows of X, lse and grad of ignored tokens are not used (they may hold
+ * anything).  G is formed a piece of the vocabulary at a time, in dtype; sums
+ * are fp32 and each output element is rounded once.  Bitwise repeatable.
+ * n_tok > 4194304 returns ESTP_ERR_UNSUPPORTED.  The workspace holds one piece
+ * of G (about 256 MiB), the live rows of X and fp32 sums of dX.
+ * ------------------------------------------------------------------------ */
+ESTP_API size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
+ESTP_API int estp_token_loss(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,
+                    int dtype, float* loss, float* lse, float* H, int32_t* vocab_argmax, void* workspace,
+                    size_t workspace_bytes, void* stream);
+ESTP_API size_t estp_token_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
+ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse,
+                             const float* grad, int64_t n_tok, int32_t d, int32_t V, int dtype, void* dX, void* dW,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Attention of drafted tokens over a cache, with the weight each cached token
+ * receives.
+ *
+ * The cache holds, per sequence b and KV head, `cap` slots of K and V.
+ * Sequence b has lens[b] cached tokens in slots [0, lens[b]) and its
+ * T_b = cu_q[b+1] - cu_q[b] newly drafted ones (one token, a chain or a tree)
+ * in slots lens[b] + t, where their K and V have been written already.  Row t
+ * sees every cached slot and those drafted tokens j whose bit j is set in its
+ * mask (its ancestors and itself):
+ *
+ *   s_ij = scale q_i . k_j,  lse_i = log sum_j exp s_ij,  O_i = sum_j exp(s_ij - lse_i) v_j
+ *   acc[b][g][j] += sum over the sequence's rows i and the query heads of KV head g of exp(s_ij - lse_i)
+ *
+ * A row that sees nothing has O = 0 and lse = -inf and adds nothing.  A
+ * drafted token that a row does not see does not enter it, whatever its K and
+ * V hold.  The account acc keeps growing over calls: the decode-time
+ * counterpart of estp_attn_importance, whose N_b S_j (Hq / Hkv) is a prompt's
+ * starting account for each KV head, and what estp_cache_evict evicts by.
+ *
+ *   Q  [n_q, Hq, dh]        rows of all sequences, packed (dtype), 16-byte aligned
+ *   K, V [B, Hkv, cap, dh]  (dtype), 16-byte aligned
+ *   lens [B]                int32, device, 0 <= lens[b], lens[b] + T_b <= max_kv
+ *   cu_q [B+1]              int32, device, from 0; T_b in [0, max_q]; rows from cu_q[B] to
+ *                           n_q belong to no sequence: their outputs are left as they are
+ *   tree_mask [n_q]         int64, device, 8-byte aligned, or NULL: a chain (row t sees j <= t)
+ *   max_q, max_kv           host bounds of T_b (at most 64) and of lens[b] + T_b (at most cap)
+ *   O  [n_q, Hq, dh]        output (dtype), 16-byte aligned
+ *   lse [Hq, n_q]           float32 output, natural log, or NULL
+ *   acc [B, Hkv, cap]       float32, added to in place, or NULL
+ * Query head h reads KV head h / (Hq / Hkv).  dh in {32, 64, 128}.  Weights
+ * and sums are fp32; for ESTP_BF16 the weights are rounded to bf16 where the
+ * matrix cores multiply them by V.  Bitwise repeatable.
+ *
+ * estp_tree_importance: the account alone, from the rows' normalisers, with a
+ * weight for each row: 1 for the drafted rows that were accepted, 0 for the
+ * others (then call estp_tree_attention with acc = NULL).
+ *
+ *   acc[b][g][j] += sum_i row_weight_i sum_h exp(s_ij - lse_i)
+ *
+ *   lse [Hq, n_q]       float32, as estp_tree_attention returned it
+ *   row_weight [n_q]    float32, device, or NULL (all 1); a row of weight 0 is not used
+ * ------------------------------------------------------------------------ */
+ESTP_API size_t estp_tree_attention_workspace_size(int32_t B, int32_t max_q, int64_t n_q, int32_t Hq, int32_t Hkv,
+                                          int32_t max_kv, int32_t dh, int dtype);
+ESTP_API int estp_tree_attention(const void* Q, const void* K, const void* V, const int32_t* lens, const int32_t* cu_q,
+                        const int64_t* tree_mask, int32_t B, int32_t max_q, int64_t n_q, int32_t Hq, int32_t Hkv,
+                        int64_t cap, int32_t max_kv, int32_t dh, float scale, int dtype, void* O, float* lse,
+                        float* acc, void* workspace, size_t workspace_bytes, void* stream);
+ESTP_API int estp_tree_importance(const void* Q, const void* K, const float* lse, const int32_t* lens,
+                         const int32_t* cu_q, const int64_t* tree_mask, const float* row_weight, int32_t B,
+                         int32_t max_q, int64_t n_q, int32_t Hq, int32_t Hkv, int64_t cap, int32_t max_kv,
+                         int32_t dh, float scale, int dtype, float* acc, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Eviction from a cache by accumulated attention weight.
+ *
+ * Cuts every sequence longer than `keep` to its `keep` best slots, each KV head
+ * for itself.  Guarded slots come first: those whose position is below `sink`
+ * or among the last `recent` of the seen[b] positions so far; then the others
+ * by acc, largest first (NaN lowest), the lowest slot among equals.  Kept
+ * slots at or past `keep` move into the evicted slots below it, both in
+ * ascending order; kept slots below `keep` stay where they are.  So slots are
+ * in no order of position afterwards: pos says which token a slot holds.
+ *
+ *   K, V [B, Hkv, cap, dh]  updated in place (dtype), 16-byte aligned
+ *   acc, pos [B, Hkv, cap]  float32 weights and int32 positions of the slots below lens[b]
+ *   lens [B], seen [B]      int32, device: slots in use, and tokens seen so far
+ *   acc_out, pos_out        as acc, pos, or acc and pos themselves (in place): slots below
+ *                           lens_out[b] hold the moved values, slots from there to lens[b]
+ *                           0 and -1, and slots past lens[b] are left as they are
+ *   lens_out [B]            int32 output, min(lens[b], keep); may be lens itself
+ *   idx [B, Hkv, keep]      int32 output: the slot that slot i's content came from, -1 from
+ *                           lens_out[b] on
+ * Requires 1 <= keep <= cap, recent + sink <= keep, dh in {32, 64, 128}; B Hkv > 65535
+ * returns ESTP_ERR_UNSUPPORTED.  Exact: copies and whole numbers only.
+ * ------------------------------------------------------------------------ */
+ESTP_API size_t estp_cache_evict_workspace_size(int32_t B, int32_t Hkv, int32_t keep);
+ESTP_API int estp_cache_evict(void* K, void* V, const float* acc, const int32_t* pos, const int32_t* lens,
+                     const int32_t* seen, int32_t B, int32_t Hkv, int64_t cap, int32_t dh, int dtype, int32_t keep,
+                     int32_t recent, int32_t sink, float* acc_out, int32_t* pos_out, int32_t* lens_out, int32_t* idx,
+                     void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Analyses on the path's outputs.

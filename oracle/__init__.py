@@ -24,6 +24,8 @@ exactly to float64 and evaluates the paper's definitions:
   training step of the K-bin head: Eq. 8 loss, its gradients, AdamW (Section 5.1)
 * ``misalignment_counts`` - the entropy / semantics percentile split (Fig. 1b, Section 1)
 * ``sjf_padding``        - padding and completion time of static SJF batches (Section 5.4)
+* ``operators`` (module) - LM-head loss and gradients, attention of drafted tokens over a
+  cache, eviction, each with bounds on what 32-bit arithmetic can be off by
 
 ``oracle.bruteforce`` re-derives the same quantities with pure-Python loops
 for tiny shapes; the tests pin this module against it, against closed forms
@@ -51,3 +53,4 @@ from .estp_oracle import (  # noqa: F401
     sjf_padding,
     run_path,
 )
+from . import operators  # noqa: F401

@@ -11,6 +11,11 @@ Python face of libestp.so: the four calls of the ESTP path (arXiv 2608.15592)
 * ``combine_pool``    - Eq. 3-5, temperature softmax of the fused score and weighted pooling
 * ``predict``         - length head (Section 4.3, Eq. 7) and shortest-job-first order
 * ``head_train_step`` - one Eq. 6-8 / AdamW training step of the K-bin head
+* ``token_loss``, ``token_loss_backward`` - LM-head cross entropy of given next tokens and its gradients,
+  without the logits
+* ``tree_attention``  - attention of drafted tokens (one, a chain, a tree) over a cache, adding up the weight
+  each slot receives; ``tree_importance`` - that account for the accepted rows
+* ``cache_evict``     - the cache cut to its most attended slots, in place
 * ``misalignment``, ``sjf_padding`` - the Fig. 1b rank split and static SJF batch padding / JCT
 
 plus ``run_path`` chaining them.  All computation runs in the library's HIP
@@ -23,6 +28,7 @@ from ._lib import (  # noqa: F401
     attn_importance,
     attn_importance_from_lse,
     attn_importance_ex,
+    cache_evict,
     combine_pool,
     load,
     predict,
@@ -33,5 +39,9 @@ from ._lib import (  # noqa: F401
     token_entropy,
     token_entropy_noalloc,
     token_entropy_workspace_size,
+    token_loss,
+    token_loss_backward,
+    tree_attention,
+    tree_importance,
 )
 from .path import run_path  # noqa: F401

@@ -38,6 +38,10 @@ EXPORTS = (
     "estp_combine_pool_workspace_size", "estp_combine_pool",
     "estp_predict_workspace_size", "estp_predict",
     "estp_head_train_step_workspace_size", "estp_head_train_step",
+    "estp_token_loss_workspace_size", "estp_token_loss",
+    "estp_token_loss_backward_workspace_size", "estp_token_loss_backward",
+    "estp_tree_attention_workspace_size", "estp_tree_attention", "estp_tree_importance",
+    "estp_cache_evict_workspace_size", "estp_cache_evict",
     "estp_misalignment", "estp_sjf_padding",
 )
 
@@ -109,6 +113,27 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.estp_head_train_step.restype = _INT
     lib.estp_head_train_step.argtypes = [_P, _P, _I32, _I32, _I32, _I32, _INT, _P, _P, _P, _P, _P, _I32, _F, _F, _F,
                                          _F, _F, _F, _P, _P, _SZ, _P]
+    lib.estp_token_loss_workspace_size.restype = _SZ
+    lib.estp_token_loss_workspace_size.argtypes = [_I64, _I32, _I32, _INT]
+    lib.estp_token_loss.restype = _INT
+    lib.estp_token_loss.argtypes = [_P, _P, _P, _I64, _I32, _I32, _INT, _P, _P, _P, _P, _P, _SZ, _P]
+    lib.estp_token_loss_backward_workspace_size.restype = _SZ
+    lib.estp_token_loss_backward_workspace_size.argtypes = [_I64, _I32, _I32, _INT]
+    lib.estp_token_loss_backward.restype = _INT
+    lib.estp_token_loss_backward.argtypes = [_P, _P, _P, _P, _P, _I64, _I32, _I32, _INT, _P, _P, _P, _SZ, _P]
+    lib.estp_tree_attention_workspace_size.restype = _SZ
+    lib.estp_tree_attention_workspace_size.argtypes = [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _INT]
+    lib.estp_tree_attention.restype = _INT
+    lib.estp_tree_attention.argtypes = [_P, _P, _P, _P, _P, _P, _I32, _I32, _I64, _I32, _I32, _I64, _I32, _I32, _F,
+                                        _INT, _P, _P, _P, _P, _SZ, _P]
+    lib.estp_tree_importance.restype = _INT
+    lib.estp_tree_importance.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I64, _I32, _I32, _I64, _I32, _I32,
+                                         _F, _INT, _P, _P]
+    lib.estp_cache_evict_workspace_size.restype = _SZ
+    lib.estp_cache_evict_workspace_size.argtypes = [_I32, _I32, _I32]
+    lib.estp_cache_evict.restype = _INT
+    lib.estp_cache_evict.argtypes = [_P, _P, _P, _P, _P, _P, _I32, _I32, _I64, _I32, _INT, _I32, _I32, _I32, _P, _P,
+                                     _P, _P, _P, _SZ, _P]
     lib.estp_misalignment.restype = _INT
     lib.estp_misalignment.argtypes = [_P, _P, _P, _I32, _F, _F, _P, _P]
     lib.estp_sjf_padding.restype = _INT
@@ -466,6 +491,181 @@ def head_train_step(pooled: torch.Tensor, y: torch.Tensor, edges: torch.Tensor, 
                                         _ptr(workspace), wsb, st),
                "estp_head_train_step")
     return loss
+
+
+def _head_shapes(X, W, targets):
+    _need(X, "X", ndim=2)
+    _need(W, "W", device=X.device, dtype=X.dtype, ndim=2)
+    if W.shape[1] != X.shape[1]:
+        raise ValueError("X and W disagree on d")
+    _sized(targets, "targets", X.shape[0], device=X.device, dtype=torch.int32)
+    return X.shape[0], X.shape[1], W.shape[0]
+
+
+def token_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None,
+               vocab_argmax: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Softmax cross entropy (nats) of the given next tokens under the LM head: returns ``(loss [n_tok],
+    lse [n_tok])`` with loss[i] = lse[i] - (W @ X[i])[targets[i]].
+
+    Tokens whose target lies outside [0, V) are ignored (loss 0).  ``H`` and ``vocab_argmax`` (optional device
+    tensors) receive what ``token_entropy`` gives, from the same pass.
+    """
+    lib = load()
+    n_tok, d, V = _head_shapes(X, W, targets)
+    dt = _dtype_code(X)
+    for t, name, dtype in ((loss, "loss", torch.float32), (lse, "lse", torch.float32), (H, "H", torch.float32),
+                           (vocab_argmax, "vocab_argmax", torch.int32)):
+        if t is not None:
+            _sized(t, name, n_tok, device=X.device, dtype=dtype)
+    with _on(stream, X.device) as st:
+        if loss is None:
+            loss = torch.empty(n_tok, dtype=torch.float32, device=X.device)
+        if lse is None:
+            lse = torch.empty(n_tok, dtype=torch.float32, device=X.device)
+        workspace, wsb = _workspace(lib.estp_token_loss_workspace_size(n_tok, d, V, dt), X.device, workspace)
+        _check(lib.estp_token_loss(_ptr(X), _ptr(W), _ptr(targets), n_tok, d, V, dt, _ptr(loss), _ptr(lse), _ptr(H),
+                                   _ptr(vocab_argmax), _ptr(workspace), wsb, st), "estp_token_loss")
+    return loss, lse
+
+
+def token_loss_backward(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                        grad: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
+                        dW: Optional[torch.Tensor] = None, want_dX: bool = True, want_dW: bool = True,
+                        workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients ``(dX [n_tok, d] or None, dW [V, d] or None)`` of sum_i grad[i] loss[i], in the inputs' type.
+
+    ``lse`` is ``token_loss``'s; ``grad`` (float32 [n_tok], default all 1) the gradient with respect to the losses.
+    """
+    lib = load()
+    n_tok, d, V = _head_shapes(X, W, targets)
+    dt = _dtype_code(X)
+    _sized(lse, "lse", n_tok, device=X.device, dtype=torch.float32)
+    if grad is not None:
+        _sized(grad, "grad", n_tok, device=X.device, dtype=torch.float32)
+    with _on(stream, X.device) as st:
+        if dX is None and want_dX:
+            dX = torch.empty_like(X)
+        if dW is None and want_dW:
+            dW = torch.empty_like(W)
+        for t, name, like in ((dX, "dX", X), (dW, "dW", W)):
+            if t is not None:
+                _sized(t, name, like.numel(), device=X.device, dtype=X.dtype)
+        workspace, wsb = _workspace(lib.estp_token_loss_backward_workspace_size(n_tok, d, V, dt), X.device, workspace)
+        _check(lib.estp_token_loss_backward(_ptr(X), _ptr(W), _ptr(targets), _ptr(lse), _ptr(grad), n_tok, d, V, dt,
+                                            _ptr(dX), _ptr(dW), _ptr(workspace), wsb, st),
+               "estp_token_loss_backward")
+    return dX, dW
+
+
+def _tree_shapes(Q, K, lens, cu_q, tree_mask):
+    _need(Q, "Q", ndim=3)
+    _need(K, "K", device=Q.device, dtype=Q.dtype, ndim=4)
+    n_q, Hq, dh = Q.shape
+    B, Hkv, cap = K.shape[:3]
+    if K.shape[3] != dh:
+        raise ValueError("Q and K disagree on the head size")
+    _sized(lens, "lens", B, device=Q.device, dtype=torch.int32)
+    _sized(cu_q, "cu_q", B + 1, device=Q.device, dtype=torch.int32)
+    if tree_mask is not None:
+        _sized(tree_mask, "tree_mask", n_q, device=Q.device, dtype=torch.int64)
+    return B, n_q, Hq, Hkv, cap, dh
+
+
+def tree_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor,
+                   max_q: int, max_kv: int, tree_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                   O: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   acc: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of newly drafted tokens over a cache: returns ``(O [n_q, Hq, dh], lse [Hq, n_q])``.
+
+    Q [n_q, Hq, dh] packs the rows of all sequences (``cu_q`` int32 [B + 1]); K, V [B, Hkv, cap, dh] hold
+    ``lens[b]`` cached tokens and, in the slots after them, the drafted ones.  ``tree_mask`` (int64 [n_q]): bit j
+    lets a row see drafted token j of its sequence; without it a chain.  ``acc`` (float32 [B, Hkv, cap], optional)
+    is added each slot's attention weight over the sequence's rows and the KV head's query heads.
+    """
+    lib = load()
+    B, n_q, Hq, Hkv, cap, dh = _tree_shapes(Q, K, lens, cu_q, tree_mask)
+    _need(V, "V", device=Q.device, dtype=Q.dtype)
+    if V.shape != K.shape:
+        raise ValueError("V must have the shape of K")
+    if acc is not None:
+        _sized(acc, "acc", B * Hkv * cap, device=Q.device, dtype=torch.float32)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dh)
+    dt = _dtype_code(Q)
+    with _on(stream, Q.device) as st:
+        if O is None:
+            O = torch.empty_like(Q)
+        _sized(O, "O", Q.numel(), device=Q.device, dtype=Q.dtype)
+        if lse is None:
+            lse = torch.empty(Hq, n_q, dtype=torch.float32, device=Q.device)
+        _sized(lse, "lse", Hq * n_q, device=Q.device, dtype=torch.float32)
+        ws = lib.estp_tree_attention_workspace_size(B, int(max_q), n_q, Hq, Hkv, int(max_kv), dh, dt)
+        workspace, wsb = _workspace(ws, Q.device, workspace)
+        _check(lib.estp_tree_attention(_ptr(Q), _ptr(K), _ptr(V), _ptr(lens), _ptr(cu_q), _ptr(tree_mask), B,
+                                       int(max_q), n_q, Hq, Hkv, cap, int(max_kv), dh, float(scale), dt, _ptr(O),
+                                       _ptr(lse), _ptr(acc), _ptr(workspace), wsb, st), "estp_tree_attention")
+    return O, lse
+
+
+def tree_importance(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, lens: torch.Tensor, cu_q: torch.Tensor,
+                    max_q: int, max_kv: int, acc: torch.Tensor, tree_mask: Optional[torch.Tensor] = None,
+                    row_weight: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                    stream=None) -> torch.Tensor:
+    """Adds to ``acc`` [B, Hkv, cap] the attention weight each slot receives from the drafted rows, row i counting
+    ``row_weight[i]`` (float32 [n_q], default 1; 0 for rejected rows).  ``lse`` is ``tree_attention``'s."""
+    lib = load()
+    B, n_q, Hq, Hkv, cap, dh = _tree_shapes(Q, K, lens, cu_q, tree_mask)
+    _sized(lse, "lse", Hq * n_q, device=Q.device, dtype=torch.float32)
+    _sized(acc, "acc", B * Hkv * cap, device=Q.device, dtype=torch.float32)
+    if row_weight is not None:
+        _sized(row_weight, "row_weight", n_q, device=Q.device, dtype=torch.float32)
+    if scale is None:
+        scale = 1.0 / math.sqrt(dh)
+    with _on(stream, Q.device) as st:
+        _check(lib.estp_tree_importance(_ptr(Q), _ptr(K), _ptr(lse), _ptr(lens), _ptr(cu_q), _ptr(tree_mask),
+                                        _ptr(row_weight), B, int(max_q), n_q, Hq, Hkv, cap, int(max_kv), dh,
+                                        float(scale), _dtype_code(Q), _ptr(acc), st), "estp_tree_importance")
+    return acc
+
+
+def cache_evict(K: torch.Tensor, V: torch.Tensor, acc: torch.Tensor, pos: torch.Tensor, lens: torch.Tensor,
+                seen: torch.Tensor, keep: int, recent: int = 0, sink: int = 0,
+                acc_out: Optional[torch.Tensor] = None, pos_out: Optional[torch.Tensor] = None,
+                lens_out: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None, stream=None):
+    """Cuts the cache K, V [B, Hkv, cap, dh] (in place) to the ``keep`` most attended slots of every KV head:
+    returns ``(lens_out [B], idx [B, Hkv, keep])``, idx the slot each kept slot's content came from (-1: none).
+
+    The first ``sink`` and the last ``recent`` of a sequence's ``seen[b]`` positions stay in any case.  ``acc`` and
+    ``pos`` [B, Hkv, cap] (weights, int32 positions) are updated in place unless ``acc_out``, ``pos_out`` are given.
+    """
+    lib = load()
+    _need(K, "K", ndim=4)
+    B, Hkv, cap, dh = K.shape
+    _need(V, "V", device=K.device, dtype=K.dtype)
+    if V.shape != K.shape:
+        raise ValueError("V must have the shape of K")
+    acc_out = acc if acc_out is None else acc_out
+    pos_out = pos if pos_out is None else pos_out
+    for t, name, n, dtype in ((acc, "acc", B * Hkv * cap, torch.float32), (pos, "pos", B * Hkv * cap, torch.int32),
+                              (acc_out, "acc_out", B * Hkv * cap, torch.float32),
+                              (pos_out, "pos_out", B * Hkv * cap, torch.int32), (lens, "lens", B, torch.int32),
+                              (seen, "seen", B, torch.int32)):
+        _sized(t, name, n, device=K.device, dtype=dtype)
+    dt = _dtype_code(K)
+    with _on(stream, K.device) as st:
+        if lens_out is None:
+            lens_out = torch.empty(B, dtype=torch.int32, device=K.device)
+        _sized(lens_out, "lens_out", B, device=K.device, dtype=torch.int32)
+        if idx is None:
+            idx = torch.empty(B, Hkv, max(int(keep), 0), dtype=torch.int32, device=K.device)
+        _sized(idx, "idx", B * Hkv * max(int(keep), 0), device=K.device, dtype=torch.int32)
+        workspace, wsb = _workspace(lib.estp_cache_evict_workspace_size(B, Hkv, int(keep)), K.device, workspace)
+        _check(lib.estp_cache_evict(_ptr(K), _ptr(V), _ptr(acc), _ptr(pos), _ptr(lens), _ptr(seen), B, Hkv, cap, dh,
+                                    dt, int(keep), int(recent), int(sink), _ptr(acc_out), _ptr(pos_out),
+                                    _ptr(lens_out), _ptr(idx), _ptr(workspace), wsb, st), "estp_cache_evict")
+    return lens_out, idx
 
 
 def misalignment(H: torch.Tensor, S: torch.Tensor, cu_seqlens: torch.Tensor, frac_low: float = 0.4,

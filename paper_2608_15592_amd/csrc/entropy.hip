@@ -57,6 +57,7 @@
 
 #include "estp_common.h"
 #include "f32_paths.h"
+#include "lm_head.h"
 
 namespace estp {
 namespace detail {
@@ -111,6 +112,9 @@ __device__ __forceinline__ void arg_merge(float& av, int& ai, float bv, int bi) 
   ai = take ? bi : ai;
 }
 
+// Exponent of a weight, clamped to where exp2 is 0; a NaN stays one (a maximum would drop it).
+__device__ __forceinline__ float exp2_arg(float x) { return x < kExp2Floor ? kExp2Floor : x; }
+
 // Fold of a finished tile into one lane's running state of one token: the lane's 32 logits z(i, r) of
 // vocabulary rows 16 i + r past its first, live where 16 i + r < lim.
 //
@@ -163,6 +167,7 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
         mx = live ? fmaxf(mx, z(i, r)) : mx;
       }
     const float mnew = fmaxf(e.m, mx * kLog2e);
+    const float mref = fmaxf(mnew, -0x1p127f);  // finite for a lane with no live row yet
     const float dl = fmaxf(e.m - mnew, kExp2Floor);
     const float sc = fast_exp2(dl);
     float s = sc * e.s;
@@ -171,10 +176,9 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
     for (int i = 0; i < kNB; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        // dead rows enter as -inf: dd clamps to the floor and adds 0 * floor,
-        // also while mnew is still -inf (a lane with no live row yet)
+        // dead rows enter as -inf: dd clamps to the floor and adds 0 * floor
         const bool live = !ragged || i * 16 + r < lim;
-        const float dd = fmaxf(fmaf(live ? z(i, r) : -INFINITY, kLog2e, -mnew), kExp2Floor);
+        const float dd = exp2_arg(fmaf(live ? z(i, r) : -INFINITY, kLog2e, -mref));
         const float p = fast_exp2(dd);
         s += p;
         t = fmaf(p, dd, t);
@@ -553,6 +557,7 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_gemm_kernel(
             mx = live ? fmaxf(mx, acc[i][j][r]) : mx;
           }
         const float mnew = fmaxf(e.m, mx * kLog2e);
+        const float mref = fmaxf(mnew, -0x1p127f);  // finite for a lane with no live row yet
         const float dl = fmaxf(e.m - mnew, kExp2Floor);
         const float sc = fast_exp2(dl);
         float s = sc * e.s;
@@ -561,10 +566,9 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_gemm_kernel(
         for (int i = 0; i < kNB; ++i)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            // dead rows enter as -inf: dd clamps to the floor and adds 0 * floor,
-            // also while mnew is still -inf (a lane with no live row yet)
+            // dead rows enter as -inf: dd clamps to the floor and adds 0 * floor
             const bool live = !ragged || i * 16 + r < lim;
-            const float dd = fmaxf(fmaf(live ? acc[i][j][r] : -INFINITY, kLog2e, -mnew), kExp2Floor);
+            const float dd = exp2_arg(fmaf(live ? acc[i][j][r] : -INFINITY, kLog2e, -mref));
             const float p = fast_exp2(dd);
             s += p;
             t = fmaf(p, dd, t);
@@ -912,7 +916,8 @@ __global__ __launch_bounds__(256) void entropy_few_merge_kernel(const float* __r
                                                                 const float* __restrict__ part_zmax,
                                                                 const int* __restrict__ part_arg, int n_tok,
                                                                 int n_vsplit, float* __restrict__ H,
-                                                                int32_t* __restrict__ arg) {
+                                                                int32_t* __restrict__ arg,
+                                                                float* __restrict__ lse) {
   __shared__ float sh[5][kMaxVsplit][16];
   const int t = threadIdx.x & 15, vs = threadIdx.x >> 4, tok = blockIdx.x * 16 + t;
   if (tok < n_tok && vs < n_vsplit) {
@@ -945,8 +950,9 @@ __global__ __launch_bounds__(256) void entropy_few_merge_kernel(const float* __r
     a = ent2_merge(a, Ent2{sh[0][v][t], sh[1][v][t], sh[2][v][t]});
     arg_merge(zb, ib, sh[3][v][t], __float_as_int(sh[4][v][t]));
   }
-  H[tok] = kLn2 * (fast_log2(a.s) - a.t / a.s);
+  if (H) H[tok] = kLn2 * (fast_log2(a.s) - a.t / a.s);
   if (arg) arg[tok] = ib;
+  if (lse) lse[tok] = kLn2 * (a.m + fast_log2(a.s));
 }
 
 // Tokens per workgroup of entropy_few_kernel: 64 also for two blocks of them, which fill the chip (128 tokens
@@ -968,8 +974,8 @@ inline bool use_few(int64_t n_tok, int d, int n_vt) {
   return few < 0.85f * gemm;
 }
 
-// Merge the partial states of each token and write H in nats: H = ln2 * (log2 s - t / s).  With
-// `arg` non-null, also the vocabulary index of the largest logit over the slices (lowest index
+// Merge the partial states of each token and write H in nats: H = ln2 * (log2 s - t / s) (H may be null), and
+// with `lse` non-null the log-sum-exp in nats, ln2 * (m + log2 s).  With `arg` non-null, also the vocabulary index of the largest logit over the slices (lowest index
 // among equal maxima).  The tokens are first .. first + n, their states [n_slices, n].  kLanes
 // threads share a token: thread group q merges slices q, q + kLanes, ... in order, then the groups
 // merge in order (within a wave by lane exchange, then the four waves through LDS).  One thread per
@@ -983,7 +989,8 @@ __global__ __launch_bounds__(256) void entropy_merge_kernel(const float* __restr
                                                             const float* __restrict__ part_zmax,
                                                             const int* __restrict__ part_arg, int first, int n,
                                                             int n_slices, float* __restrict__ H,
-                                                            int32_t* __restrict__ arg) {
+                                                            int32_t* __restrict__ arg,
+                                                            float* __restrict__ lse) {
   static_assert(kLanes == 1 || kLanes == 16, "four groups per wave or none");
   constexpr int kToks = 256 / kLanes;
   const int t = threadIdx.x % kToks, q = threadIdx.x / kToks;
@@ -1028,8 +1035,9 @@ __global__ __launch_bounds__(256) void entropy_merge_kernel(const float* __restr
     }
   }
   if (tok >= n) return;
-  H[first + tok] = kLn2 * (fast_log2(a.s) - a.t / a.s);
+  if (H) H[first + tok] = kLn2 * (fast_log2(a.s) - a.t / a.s);
   if (arg) arg[first + tok] = ib;
+  if (lse) lse[first + tok] = kLn2 * (a.m + fast_log2(a.s));
 }
 
 }  // namespace detail
@@ -1049,12 +1057,11 @@ extern "C" size_t estp_token_entropy_workspace_size(int64_t n_tok, int32_t d, in
   return c.bytes();
 }
 
-namespace {
+namespace estp {
+namespace detail {
 
-// Host-side checks shared by both entry points; `fn` names the caller in the error message.
-int check_entropy_args(const char* fn, const void* X, const void* W, int64_t n_tok, int32_t d, int32_t V,
-                       int dtype, const float* H, const int32_t* vocab_argmax) {
-  ESTP_REQUIRE(X && W && H, ESTP_ERR_INVALID_ARG, "%s: X, W and H must be non-null", fn);
+int check_lm_head_args(const char* fn, const void* X, const void* W, int64_t n_tok, int32_t d, int32_t V, int dtype) {
+  ESTP_REQUIRE(X && W, ESTP_ERR_INVALID_ARG, "%s: X and W must be non-null", fn);
   ESTP_REQUIRE(n_tok >= 1 && n_tok <= INT32_MAX, ESTP_ERR_INVALID_ARG, "%s: n_tok must be in [1, 2^31), got %lld", fn,
                (long long)n_tok);
   ESTP_REQUIRE(V >= 1, ESTP_ERR_INVALID_ARG, "%s: V must be >= 1, got %d", fn, V);
@@ -1064,8 +1071,6 @@ int check_entropy_args(const char* fn, const void* X, const void* W, int64_t n_t
                "%s: d must be a multiple of 32 for the matrix-core path, got %d", fn, d);
   ESTP_REQUIRE(size_t(d) * 2 * kBV < (size_t(1) << 32), ESTP_ERR_UNSUPPORTED, "%s: d = %d too large", fn, d);
   ESTP_REQUIRE(aligned(X, 16) && aligned(W, 16), ESTP_ERR_INVALID_ARG, "%s: X and W must be 16-byte aligned", fn);
-  ESTP_REQUIRE(aligned(H, 4) && aligned(vocab_argmax, 4), ESTP_ERR_INVALID_ARG,
-               "%s: H and vocab_argmax must be 4-byte aligned", fn);
   const int n = int(n_tok);
   const int n_vt = (V + kBV - 1) / kBV;
   const size_t n_wg = dtype == ESTP_F32 ? entropy_f32_workgroups(n, choose_vsplit(n_vt))
@@ -1075,10 +1080,8 @@ int check_entropy_args(const char* fn, const void* X, const void* W, int64_t n_t
   return ESTP_OK;
 }
 
-// The kernels of one call on checked arguments; `workspace` holds
-// estp_token_entropy_workspace_size() bytes, 256-byte aligned.
 int launch_token_entropy(const void* X, const void* W, int n, int d, int V, int dtype, float* H,
-                         int32_t* vocab_argmax, void* workspace, hipStream_t s) {
+                         int32_t* vocab_argmax, float* lse, void* workspace, hipStream_t s) {
   const int n_vt = (V + kBV - 1) / kBV;
   const int n_tt = (n + kBT - 1) / kBT;
   const size_t cap = partial_capacity(n, n_vt);
@@ -1096,10 +1099,10 @@ int launch_token_entropy(const void* X, const void* W, int n, int d, int V, int 
     const int* pa_m = want_arg ? pa + off : nullptr;
     if (n_slices <= kMaxVsplit)
       entropy_merge_kernel<1><<<dim3((count + 255) / 256), dim3(256), 0, s>>>(
-          pm + off, ps + off, pt + off, pz + off, pa_m, first, count, n_slices, H, vocab_argmax);
+          pm + off, ps + off, pt + off, pz + off, pa_m, first, count, n_slices, H, vocab_argmax, lse);
     else
       entropy_merge_kernel<16><<<dim3((count + 15) / 16), dim3(256), 0, s>>>(
-          pm + off, ps + off, pt + off, pz + off, pa_m, first, count, n_slices, H, vocab_argmax);
+          pm + off, ps + off, pt + off, pz + off, pa_m, first, count, n_slices, H, vocab_argmax, lse);
   };
 
   if (dtype == ESTP_F32) {
@@ -1121,7 +1124,7 @@ int launch_token_entropy(const void* X, const void* W, int n, int d, int V, int 
       want_arg ? go(entropy_few_kernel<128, true, false>) : go(entropy_few_kernel<128, false, false>);
     ESTP_CHECK_LAUNCH("entropy_few_kernel");
     entropy_few_merge_kernel<<<dim3((n + 15) / 16), dim3(256), 0, s>>>(pm, ps, pt, pz, pa, n, n_vsplit, H,
-                                                                       vocab_argmax);
+                                                                       vocab_argmax, lse);
   } else {
     const SlicePlan pl = plan_slices(n, n_vt);
     const dim3 grid(unsigned(plan_workgroups(pl, n))), block(kWaves * 64);
@@ -1150,6 +1153,22 @@ int launch_token_entropy(const void* X, const void* W, int n, int d, int V, int 
   return ESTP_OK;
 }
 
+}  // namespace detail
+}  // namespace estp
+
+namespace {
+
+// Host-side checks shared by both entry points; `fn` names the caller in the error message.
+int check_entropy_args(const char* fn, const void* X, const void* W, int64_t n_tok, int32_t d, int32_t V,
+                       int dtype, const float* H, const int32_t* vocab_argmax) {
+  ESTP_REQUIRE(X && W && H, ESTP_ERR_INVALID_ARG, "%s: X, W and H must be non-null", fn);
+  const int st = check_lm_head_args(fn, X, W, n_tok, d, V, dtype);
+  if (st != ESTP_OK) return st;
+  ESTP_REQUIRE(aligned(H, 4) && aligned(vocab_argmax, 4), ESTP_ERR_INVALID_ARG,
+               "%s: H and vocab_argmax must be 4-byte aligned", fn);
+  return ESTP_OK;
+}
+
 }  // namespace
 
 extern "C" int estp_token_entropy(const void* X, const void* W, int64_t n_tok, int32_t d, int32_t V, int dtype,
@@ -1163,7 +1182,7 @@ extern "C" int estp_token_entropy(const void* X, const void* W, int64_t n_tok, i
                "estp_token_entropy: workspace of %zu bytes, %zu needed", workspace_bytes, need);
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "estp_token_entropy: workspace must be non-null and 256-byte aligned");
-  return launch_token_entropy(X, W, int(n_tok), d, V, dtype, H, vocab_argmax, workspace,
+  return launch_token_entropy(X, W, int(n_tok), d, V, dtype, H, vocab_argmax, nullptr, workspace,
                               static_cast<hipStream_t>(stream));
 }
 
@@ -1223,5 +1242,5 @@ extern "C" int estp_token_entropy_noalloc(const void* X, const void* W, int64_t 
                fn, (long long)n_tok, V, need, size_t(ESTP_NOALLOC_SCRATCH_BYTES));
   void* ws = scratch_of_current_device(fn);
   if (!ws) return ESTP_ERR_HIP;
-  return launch_token_entropy(X, W, int(n_tok), d, V, dtype, H, vocab_argmax, ws, static_cast<hipStream_t>(stream));
+  return launch_token_entropy(X, W, int(n_tok), d, V, dtype, H, vocab_argmax, nullptr, ws, static_cast<hipStream_t>(stream));
 }
