@@ -353,7 +353,7 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  * Rows of X, lse and grad of ignored tokens are not used (they may hold
  * anything).  G is formed a piece of the vocabulary at a time, in dtype; sums
  * are fp32 and each output element is rounded once.  Bitwise repeatable.
- * n_tok > 4194304 returns ESTP_ERR_UNSUPPORTED.  The workspace holds one piece
+ * n_tok > 4194304 or d > 1048576 returns ESTP_ERR_UNSUPPORTED.  The workspace holds one piece
  * of G (about 256 MiB), the live rows of X and fp32 sums of dX.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);

@@ -21,6 +21,7 @@
 
 #include "estp_common.h"
 #include "lm_head.h"
+#include "mfma_gemm.h"
 
 namespace estp {
 namespace detail {
@@ -123,16 +124,35 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(const uint4* __restric
   }
 }
 
-// dX of every token from the n_split partial sums of its slot, rounded once; 0 for ignored tokens.
+// Shares of a piece's vocabulary rows whose products add up to its part of dX: as many as give a workgroup each to
+// the chip, while the fp32 sums of all shares (n live rows each) fit into `room` floats.  The same on every piece
+// and for every kernel of a call.
+struct Shares {
+  int n;     // shares
+  int rows;  // vocabulary rows of a share, a multiple of 256
+};
+__device__ __forceinline__ Shares dx_shares(int n_live, int d, int Vc, int tile_toks, int wgs, size_t room) {
+  const int tiles = (n_live + tile_toks - 1) / tile_toks * ((d + 255) / 256);
+  int s = tiles > 0 ? max(1, wgs / tiles) : 1;
+  s = min(s, (Vc + 511) / 512);
+  const size_t each = size_t(max(1, n_live)) * d;
+  s = int(min(size_t(s), max(size_t(1), room / each)));
+  const int rows = ((Vc + s - 1) / s + 255) / 256 * 256;
+  return {(Vc + rows - 1) / rows, rows};
+}
+
+// dX of every token from the partial sums of its slot, rounded once; 0 for ignored tokens.
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ slot,
-                                                      int d, size_t split_stride, int n_split, T* __restrict__ dX) {
-  const int tok = blockIdx.x, s = slot[tok];
+                                                      const int* __restrict__ n_live, int d, int Vc, int tile_toks,
+                                                      int wgs, size_t room, T* __restrict__ dX) {
+  const int tok = blockIdx.x, s = slot[tok], n = n_live[0];
+  const Shares sh = dx_shares(n, d, Vc, tile_toks, wgs, room);
+  const size_t each = size_t(n) * d;
   for (int k = 4 * threadIdx.x; k < d; k += 1024) {
     f32x4_t v{0.f, 0.f, 0.f, 0.f};
     if (s >= 0)
-      for (int p = 0; p < n_split; ++p)
-        v += *reinterpret_cast<const f32x4_t*>(acc + size_t(p) * split_stride + size_t(s) * d + k);
+      for (int p = 0; p < sh.n; ++p) v += *reinterpret_cast<const f32x4_t*>(acc + p * each + size_t(s) * d + k);
     T* o = dX + size_t(tok) * d + k;
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
@@ -257,15 +277,16 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(const T* __restrict__ Xc
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_piece_kernel(const T* __restrict__ G, const T* __restrict__ W,
                                                             const int* __restrict__ n_live, int d, int V, int64_t v0,
-                                                            int Vc, int share, bool first, size_t split_stride,
+                                                            int Vc, int wgs, size_t room, bool first,
                                                             float* __restrict__ out) {
   const int n = n_live[0], m0 = blockIdx.y * kPT, n0 = blockIdx.x * kPT;
-  if (m0 >= n) return;
+  const Shares sh = dx_shares(n, d, Vc, kPT, wgs, room);
+  if (m0 >= n || int(blockIdx.z) >= sh.n) return;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
-  const int k0 = min(rows, int(blockIdx.z) * share), k1 = min(rows, k0 + share);
+  const int k0 = min(rows, int(blockIdx.z) * sh.rows), k1 = min(rows, k0 + sh.rows);
   float acc[8][8] = {};
   tile_product<T, T, true, false>(G, Vc, n, W + size_t(v0) * d, d, d, m0, n0, k0, k1, acc);
-  out += size_t(blockIdx.z) * split_stride;
+  out += size_t(blockIdx.z) * size_t(n) * d;
   const int rv = threadIdx.x >> 4, ct = threadIdx.x & 15;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -298,13 +319,184 @@ __global__ __launch_bounds__(256) void loss_dw_kernel(const T* __restrict__ G, c
     }
 }
 
+// ------------------------------------------------------------------ matrix-core products (bf16)
+
+// Stores of 8 and 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
+__device__ __forceinline__ void buf_store8(buf_rsrc_t r, uint32_t off, uint2 v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{v.x, v.y}, r, off, 0, 0);
+#endif
+}
+__device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, 0);
+#endif
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, bf16x2_t{__bf16(lo), __bf16(hi)});
+}
+
+// G of a piece: products of W's rows (M side) and the live tokens (N side), turned into G as they leave the matrix
+// cores.  A lane holds 8 consecutive vocabulary rows of a token: one 16-byte store.
+template <int kNBN, bool kOdd>
+__global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __restrict__ Xc,
+                                                                const __bf16* __restrict__ W,
+                                                                const int* __restrict__ n_live, int d, int V,
+                                                                int64_t v0, int Vc, const int32_t* __restrict__ tc,
+                                                                const float* __restrict__ lc,
+                                                                const float* __restrict__ gc, __bf16* __restrict__ G) {
+  using Run = gemm::Tiles<true, true, true, kNBN, kOdd>;
+  __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
+  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
+  const int n_m = (rows + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
+  const gemm::TileOrder order(n_m, n_n);
+  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 2u, rows};
+  const gemm::Operand B{reinterpret_cast<const char*>(Xc), uint32_t(d) * 2u, n};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+  Run::run(
+      lds, A, B, gemm::first_tile(blockIdx.x, gridDim.x), gridDim.x, n_m * n_n,
+      [&](int id) {
+        const gemm::TileAt t = order(id);
+        return gemm::Place{256 * t.m, Run::kBN * t.n, 0, d, 0};
+      },
+      [&](const gemm::Place& at, const f32x4_t(&acc)[8][kNBN]) {
+        const int m0 = at.m0, n0 = at.n0, lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
+        const int live = min(Run::kBN, n - n0);
+        const buf_rsrc_t out =
+            make_rsrc(reinterpret_cast<const char*>(G) + size_t(n0) * Vc * 2, uint32_t(live) * uint32_t(Vc) * 2u);
+        const int c0 = m0 + 128 * wm + 8 * fq;  // the lane's first column of G
+        const bool ragged = m0 + 256 > rows;
+#pragma unroll
+        for (int j = 0; j < kNBN; ++j) {
+          const int sl = 16 * kNBN * wn + 16 * j + fr, s = min(n0 + sl, n - 1);
+          const float l2 = lc[s] * kLog2e, g = gc[s];
+          const int rel = int(tc[s] - v0) - c0;  // the target is column rel of the lane's 128, 8 of every 32
+          float p[4][8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              p[i / 2][4 * (i % 2) + r] = g * fast_exp2(fmaf(acc[i][j][r], kLog2e, -l2));
+          if (__any(rel >= 0 && rel < 128 && (rel & 31) < 8)) {  // seldom: one tile in V / 256 holds a token's target
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[q][e] = rel == 32 * q + e ? p[q][e] - g : p[q][e];
+          }
+          if (ragged) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[q][e] = c0 + 32 * q + e < rows ? p[q][e] : 0.f;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            buf_store16(out, uint32_t(sl) * uint32_t(Vc) * 2u + uint32_t(c0 + 32 * q) * 2u,
+                        uint4{pack_bf16(p[q][0], p[q][1]), pack_bf16(p[q][2], p[q][3]), pack_bf16(p[q][4], p[q][5]),
+                              pack_bf16(p[q][6], p[q][7])});
+        }
+      });
+}
+
+// out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W (transposed reads), N
+// side: slots.
+template <int kNBN>
+__global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __restrict__ G,
+                                                              const __bf16* __restrict__ W,
+                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                              int Vc, size_t room, bool first,
+                                                              float* __restrict__ out) {
+  using Run = gemm::Tiles<false, true, false, kNBN, false>;
+  __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
+  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
+  const int n_m = (d + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
+  const gemm::TileOrder order(n_m, n_n);
+  const gemm::Divisor share_tiles(max(1, n_m * n_n));
+  const Shares sh = dx_shares(n, d, Vc, Run::kBN, gridDim.x, room);
+  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 2u, d};
+  const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 2u, n};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+  const int tiles = n_m * n_n;
+  Run::run(
+      lds, A, B, gemm::first_tile(blockIdx.x, gridDim.x), gridDim.x, tiles * sh.n,
+      [&](int id) {
+        const int share = int(share_tiles.div(uint32_t(id)));
+        const gemm::TileAt t = order(id - share * tiles);
+        return gemm::Place{256 * t.m, Run::kBN * t.n, min(rows, share * sh.rows), min(rows, (share + 1) * sh.rows),
+                           share};
+      },
+      [&](const gemm::Place& at, const f32x4_t(&acc)[8][kNBN]) {
+        const int m0 = at.m0, n0 = at.n0, lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
+        const int live = min(Run::kBN, n - n0);
+        float* sums = out + (size_t(at.tag) * n + n0) * d;
+        const buf_rsrc_t o = make_rsrc(sums, uint32_t(live) * uint32_t(d) * 4u);
+        const buf_rsrc_t was = make_rsrc(sums, first ? 0u : uint32_t(live) * uint32_t(d) * 4u);  // (empty: reads 0)
+#pragma unroll
+        for (int j = 0; j < kNBN; ++j) {
+          const uint32_t row = uint32_t(16 * kNBN * wn + 16 * j + fr) * uint32_t(d);
+          const int c0 = m0 + 128 * wm + 4 * fq;
+          f32x4_t v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            v[i] = buf_load4(was, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 4u : kPastEnd);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            buf_store16(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 4u : kPastEnd,
+                        __builtin_bit_cast(uint4, v[i] + acc[i][j]));
+        }
+      });
+}
+
+// dW of a piece: G^T Xc.  M side: columns k of Xc, N side: vocabulary rows; both transposed reads, the tokens are
+// the depth.
+__global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __restrict__ G,
+                                                              const __bf16* __restrict__ Xc,
+                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                              int Vc, __bf16* __restrict__ dW) {
+  using Run = gemm::Tiles<false, false, false, 8, false>;
+  __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
+  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
+  const int n_m = (d + 255) / 256, n_n = (rows + 255) / 256;
+  const gemm::TileOrder order(n_m, n_n);
+  const gemm::Operand A{reinterpret_cast<const char*>(Xc), uint32_t(d) * 2u, d};
+  const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 2u, Vc};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+  Run::run(
+      lds, A, B, gemm::first_tile(blockIdx.x, gridDim.x), gridDim.x, n_m * n_n,
+      [&](int id) {
+        const gemm::TileAt t = order(id);
+        return gemm::Place{256 * t.m, 256 * t.n, 0, n, 0};
+      },
+      [&](const gemm::Place& at, const f32x4_t(&acc)[8][8]) {
+        const int m0 = at.m0, n0 = at.n0, lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
+        const int live = min(256, rows - n0);
+        const buf_rsrc_t o = make_rsrc(dW + (size_t(v0) + n0) * d, uint32_t(live) * uint32_t(d) * 2u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t row = uint32_t(128 * wn + 16 * j + fr) * uint32_t(d);
+          const int c0 = m0 + 128 * wm + 4 * fq;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            buf_store8(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
+                       uint2{pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3])});
+        }
+      });
+}
+
 // ------------------------------------------------------------------ plan and workspace
 
-// How a backward call is cut.  Vc vocabulary rows a piece (a multiple of 256), the dX product of a piece in n_split
-// shares of them.
+// How a backward call is cut: Vc vocabulary rows a piece (a multiple of 256), n_split sums of dX in the workspace,
+// products of tile_toks tokens.
 struct LossPlan {
   int Vc;
   int n_split;
+  int tile_toks;
 };
 
 inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
@@ -315,8 +507,9 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
   LossPlan p;
   p.Vc = int(vc);
-  const int64_t tiles = (n_tok + kPT - 1) / kPT * ((d + kPT - 1) / kPT);
-  p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 512 / tiles), (vc + 511) / 512));
+  p.tile_toks = dtype == ESTP_F32 ? kPT : n_tok <= 128 ? 128 : 256;
+  const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
+  p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 511) / 512));
   return p;
 }
 
@@ -325,6 +518,7 @@ struct LossBuffers {
   int32_t* tc;
   float *lc, *gc, *acc;
   char *Xc, *G;
+  size_t room;   // floats of acc
   size_t bytes;
 };
 
@@ -340,7 +534,8 @@ inline LossBuffers carve_loss(const LossPlan& p, int64_t n_tok, int d, int dtype
   b.gc = c.take<float>(size_t(n_tok));
   b.Xc = c.take<char>(size_t(n_tok) * d * es);
   b.G = c.take<char>(size_t(n_tok) * p.Vc * es);
-  b.acc = c.take<float>(size_t(p.n_split) * size_t(n_tok) * d);
+  b.room = size_t(p.n_split) * size_t(n_tok) * d;
+  b.acc = c.take<float>(b.room);
   b.bytes = c.bytes();
   return b;
 }
@@ -350,6 +545,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
                          int n, int d, int V, int dtype, void* dX, void* dW, void* workspace, hipStream_t s) {
   const LossPlan p = plan_loss(n, d, V, dtype);
   const LossBuffers b = carve_loss(p, n, d, dtype, workspace);
+  constexpr int kWgs = 256;  // of the persistent kernels: one on each compute unit
   const T *Wt = static_cast<const T*>(W), *Xc = reinterpret_cast<const T*>(b.Xc);
   T* G = reinterpret_cast<T*>(b.G);
   loss_list_kernel<<<dim3(1), dim3(1024), 0, s>>>(targets, n, V, b.row, b.slot, b.n_live);
@@ -357,25 +553,43 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
                                                    int(size_t(d) * sizeof(T) / 16), targets, lse, grad,
                                                    reinterpret_cast<uint4*>(b.Xc), b.tc, b.lc, b.gc);
   ESTP_CHECK_LAUNCH("loss_gather_kernel");
-  const unsigned n_tt = unsigned((n + kPT - 1) / kPT), n_dt = unsigned((d + kPT - 1) / kPT);
-  const int share = (p.Vc / p.n_split + 255) / 256 * 256;
-  const size_t split_stride = size_t(n) * d;
+  const dim3 block(256);
   for (int64_t v0 = 0; v0 < V; v0 += p.Vc) {
-    const unsigned n_vt = unsigned((p.Vc + kPT - 1) / kPT);
-    loss_grad_kernel<T><<<dim3(n_vt, n_tt), dim3(256), 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
-    ESTP_CHECK_LAUNCH("loss_grad_kernel");
-    if (dX) {
-      loss_dx_piece_kernel<T><<<dim3(n_dt, n_tt, unsigned(p.n_split)), dim3(256), 0, s>>>(
-          G, Wt, b.n_live, d, V, v0, p.Vc, share, v0 == 0, split_stride, b.acc);
-      ESTP_CHECK_LAUNCH("loss_dx_piece_kernel");
-    }
-    if (dW) {
-      loss_dw_kernel<T><<<dim3(n_dt, n_vt), dim3(256), 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
-      ESTP_CHECK_LAUNCH("loss_dw_kernel");
+    if constexpr (sizeof(T) == 2) {
+      const dim3 grid(kWgs);
+      auto grad_kernel = p.tile_toks == 128 ? (d % 64 ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
+                                            : (d % 64 ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
+      grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      ESTP_CHECK_LAUNCH("loss_grad_mfma_kernel");
+      if (dX) {
+        auto dx_kernel = p.tile_toks == 128 ? loss_dx_mfma_kernel<4> : loss_dx_mfma_kernel<8>;
+        dx_kernel<<<grid, block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, b.room, v0 == 0, b.acc);
+        ESTP_CHECK_LAUNCH("loss_dx_mfma_kernel");
+      }
+      if (dW) {
+        loss_dw_mfma_kernel<<<grid, block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
+        ESTP_CHECK_LAUNCH("loss_dw_mfma_kernel");
+      }
+    } else {
+      const unsigned n_tt = unsigned((n + kPT - 1) / kPT), n_dt = unsigned((d + kPT - 1) / kPT);
+      const unsigned n_vt = unsigned((p.Vc + kPT - 1) / kPT);
+      loss_grad_kernel<T><<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      ESTP_CHECK_LAUNCH("loss_grad_kernel");
+      if (dX) {
+        const unsigned shares = unsigned(std::min<int64_t>(kWgs, (p.Vc + 511) / 512));
+        loss_dx_piece_kernel<T><<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs,
+                                                                           b.room, v0 == 0, b.acc);
+        ESTP_CHECK_LAUNCH("loss_dx_piece_kernel");
+      }
+      if (dW) {
+        loss_dw_kernel<T><<<dim3(n_dt, n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
+        ESTP_CHECK_LAUNCH("loss_dw_kernel");
+      }
     }
   }
   if (dX) {
-    loss_dx_kernel<T><<<dim3(n), dim3(256), 0, s>>>(b.acc, b.slot, d, split_stride, p.n_split, static_cast<T*>(dX));
+    loss_dx_kernel<T><<<dim3(n), block, 0, s>>>(b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room,
+                                                static_cast<T*>(dX));
     ESTP_CHECK_LAUNCH("loss_dx_kernel");
   }
   return ESTP_OK;
@@ -440,6 +654,7 @@ extern "C" int estp_token_loss_backward(const void* X, const void* W, const int3
   if (st != ESTP_OK) return st;
   ESTP_REQUIRE(n_tok <= (int64_t(1) << 22), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %lld, at most 4194304", fn,
                (long long)n_tok);
+  ESTP_REQUIRE(d <= (1 << 20), ESTP_ERR_UNSUPPORTED, "%s: d = %d, at most 1048576", fn, d);
   const size_t need = estp_token_loss_backward_workspace_size(n_tok, d, V, dtype);
   ESTP_REQUIRE(workspace_bytes >= need, ESTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn,
                workspace_bytes, need);
