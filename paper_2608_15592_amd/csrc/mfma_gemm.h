@@ -43,6 +43,27 @@ __device__ __forceinline__ s16x4_t read_tr(const char* p) {
 #endif
 }
 
+// lds_dma16_buf as one instruction that the compiler counts no wait for: before every transposing read it would wait
+// for all transfers in flight (vmcnt 0), which run() orders by itself.  There is no register result to wait for.
+// The resource is make_rsrc's, as the four words it is.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4_t rsrc_words(const void* base, uint32_t bytes) {
+  const uint64_t a = uint64_t(base);
+  return u32x4_t{uint32_t(a), uint32_t(a >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void dma16(u32x4_t r, uint32_t voffset, uint32_t soffset, char* dst_wave_base) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t m0 = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)(dst_wave_base)));
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, %3 offen lds"
+      :
+      : "s"(m0), "v"(voffset), "s"(r), "s"(soffset)
+      : "memory", "m0");
+#endif
+}
+
 // An operand in memory: element (row, k) at base + row * ld + 2 k (k contiguous) or base + k * ld + 2 row.
 struct Operand {
   const char* base;
@@ -160,7 +181,7 @@ struct Tiles {
     Place pf = at(first), nx = nx_id < total ? at(nx_id) : none;
     bool nx_used = false;
     struct Part {
-      buf_rsrc_t rsrc;
+      u32x4_t rsrc;
       uint32_t soff;
       char* dst;
       int depth;  // k the stage holds (kOdd)
@@ -173,11 +194,11 @@ struct Tiles {
       p.depth = left;
       if (contig) {
         const uint32_t bytes = uint32_t(min(rows, o.rows - r0)) * o.ld;
-        p.rsrc = make_rsrc(o.base + size_t(r0) * o.ld, left > 0 ? bytes : 0u);
+        p.rsrc = rsrc_words(o.base + size_t(r0) * o.ld, left > 0 ? bytes : 0u);
         p.soff = uint32_t(pf.k0) * 2u;
       } else {
         const uint32_t bytes = uint32_t(min(kDepth, left)) * o.ld - uint32_t(r0) * 2u;
-        p.rsrc = make_rsrc(o.base + size_t(pf.k0) * o.ld + size_t(r0) * 2, left > 0 ? bytes : 0u);
+        p.rsrc = rsrc_words(o.base + size_t(pf.k0) * o.ld + size_t(r0) * 2, left > 0 ? bytes : 0u);
         p.soff = 0;
       }
       return p;
@@ -203,11 +224,11 @@ struct Tiles {
     };
     auto dma_a = [&](const Part& p, int i) {
       const uint32_t o = kOdd && kAK && 8 * kc_a[i] >= p.depth ? kPastEnd : off_a[i];
-      lds_dma16_buf(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
+      dma16(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
     };
     auto dma_b = [&](const Part& p, int i) {
       const uint32_t o = kOdd && kBK && 8 * kc_b[i] >= p.depth ? kPastEnd : off_b[i];
-      lds_dma16_buf(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
+      dma16(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
     };
 
     // ---- fragment reads of the 32-deep step u of a stage
