@@ -14,6 +14,7 @@
 #pragma once
 
 #include "estp_common.h"
+#include "lds_ops.h"
 
 namespace estp {
 namespace detail {
@@ -25,44 +26,6 @@ constexpr int kDepth = 64;              // k of a stage
 constexpr int kSlots = 5;
 constexpr int kSlotBytes = 32768;
 constexpr int kNBM = 8;                 // 16-row blocks of a wave, M side
-
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef short s16x8_t __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f32x4_t mfma(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-// Lane s of a 16-lane group reads 4 elements at `p`; lane i gets element i % 4 of lanes i / 4, 4 + i / 4, 8 + i / 4
-// and 12 + i / 4.
-__device__ __forceinline__ s16x4_t read_tr(const char* p) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(p));
-#else
-  return s16x4_t{};
-#endif
-}
-
-// lds_dma16_buf as one instruction that the compiler counts no wait for: before every transposing read it would wait
-// for all transfers in flight (vmcnt 0), which run() orders by itself.  There is no register result to wait for.
-// The resource is make_rsrc's, as the four words it is.
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ u32x4_t rsrc_words(const void* base, uint32_t bytes) {
-  const uint64_t a = uint64_t(base);
-  return u32x4_t{uint32_t(a), uint32_t(a >> 32) & 0xffffu, bytes, 0x00020000u};
-}
-__device__ __forceinline__ void dma16(u32x4_t r, uint32_t voffset, uint32_t soffset, char* dst_wave_base) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const uint32_t m0 = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)(dst_wave_base)));
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds"
-      :
-      : "s"(m0), "v"(voffset), "s"(r), "s"(soffset)
-      : "memory", "m0");
-#endif
-}
 
 // An operand in memory: element (row, k) at base + row * ld + 2 k (k contiguous) or base + k * ld + 2 row.
 struct Operand {
@@ -247,9 +210,6 @@ struct Tiles {
         rb[u] = kBK ? rowb * 128 + ((4 * u + fq) ^ swz_k(false, rowb)) * 16
                     : k * (2 * kBN) + ((kNBN * wn) ^ g) * 32 + (fr & 3) * 8;
     }
-    auto join = [](s16x4_t lo, s16x4_t hi) {
-      return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
     s16x4_t half[2];  // first half of a transposed fragment until the second is read
     auto read = [&](Frags& f, int slot_a, int slot_b, int u, int q) {
       if (q < kReadsA) {
@@ -262,7 +222,7 @@ struct Tiles {
           if (q % 2 == 0)
             half[0] = read_tr(p);
           else
-            f.a[q / 2] = join(half[0], read_tr(p));
+            f.a[q / 2] = join_tr(half[0], read_tr(p));
         }
       } else {
         q -= kReadsA;
@@ -274,7 +234,7 @@ struct Tiles {
           if (q % 2 == 0)
             half[1] = read_tr(p);
           else
-            f.b[q / 2] = join(half[1], read_tr(p));
+            f.b[q / 2] = join_tr(half[1], read_tr(p));
         }
       }
     };
@@ -334,7 +294,7 @@ struct Tiles {
 #pragma unroll
             for (int j = 0; j < kNBN; ++j) {
               const int m = i * kNBN + j;
-              acc[i][j] = mfma(cur.a[i], cur.b[j], acc[i][j]);
+              acc[i][j] = mfma_bf16(cur.a[i], cur.b[j], acc[i][j]);
               if (u == 0 && m == kMfma / 8) pb = next_b();
               if (u == 0 && m == kMfma / 2) pa = next_a();
               if (m % kReadEvery == 0 && m / kReadEvery < kReads) {

@@ -23,6 +23,7 @@
 #include <cmath>
 
 #include "estp_common.h"
+#include "lds_ops.h"
 
 namespace estp {
 namespace detail {
@@ -32,7 +33,7 @@ constexpr int kTRows = 16;    // rows of a workgroup
 constexpr int kTKeys = 64;    // keys of a tile
 
 struct TreeShape {
-  int B, n_q, Hq, Hkv, cap, max_kv, n_split;
+  int B, max_q, n_q, Hq, Hkv, cap, max_kv, n_split, unit;  // n_split ranges of `unit` keys
 };
 
 // One sequence as the kernels see it: counts out of range (invalid input) never become an access out of range.
@@ -42,7 +43,7 @@ struct TreeSeq {
 __device__ __forceinline__ TreeSeq tree_seq(const TreeShape& sh, const int* lens, const int* cu_q, int b) {
   TreeSeq q;
   q.q0 = max(0, min(cu_q[b], sh.n_q));
-  q.T = max(0, min(min(cu_q[b + 1], sh.n_q) - q.q0, kMaxTree));
+  q.T = max(0, min(min(cu_q[b + 1], sh.n_q) - q.q0, sh.max_q));
   q.len = max(0, min(lens[b], sh.max_kv));
   q.keys = min(q.len + q.T, sh.max_kv);
   return q;
@@ -131,8 +132,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
   const TreeSeq q = tree_seq(sh, lens, cu_q, b);
   const int R = q.T * G;
   if (r0 >= R) return;
-  const int per = ((q.keys + sh.n_split - 1) / sh.n_split + kTKeys - 1) / kTKeys * kTKeys;
-  const int k0 = min(q.keys, split * per), k1 = min(q.keys, k0 + per);
+  const int k0 = min(int64_t(q.keys), int64_t(split) * sh.unit), k1 = min(q.keys, k0 + sh.unit);
   const int tid = threadIdx.x, rr = tid >> 4, c = tid & 15, r = r0 + rr;
   const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
   const T* Kb = K + size_t(bg) * sh.cap * DH;
@@ -191,35 +191,380 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
   for (int e = 0; e < NC; ++e) part_o[row * DH + c * NC + e] = o[e];
 }
 
-// Joins the ranges' partial results of each row: one wave per row.  Rows past the last sequence's are left as
-// they are.
+// Matrix-core kernel (bf16): one wave per workgroup, 16 NRT rows, `unit` keys in chunks of 32.
+//
+// S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of the chunk's two 16-key blocks, keys
+// 4 fq .. 4 fq + 3 each (fq = lane / 16).  These 8 weights are at once the lane's part of the second product's
+// operand, O^T = V^T P^T over 32 keys, if V's part holds the same keys for one of its columns: two transposing reads.
+// So scores never leave the registers.  The reference of a row's exponentials follows its maximum only when a score
+// passes it by 2^16 (sums and weights stay far from overflow): most chunks neither exchange maxima between lanes nor
+// rescale O.
+//
+// The chunks' K and V parts go straight from memory into a ring of five parts that this wave alone uses: no
+// barriers, only counts of its own transfers, two and a half chunks ahead.  Four such waves fill a compute unit's
+// LDS at a head size of 128, eight at 64.  16-byte pieces are swizzled so that the 16 rows of a K read and the 8 of
+// a transposing V read lie in distinct banks.
+template <int DH, int NRT, bool kScores>
+__global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
+    const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
+    const int* __restrict__ lens, const int* __restrict__ cu_q, const int64_t* __restrict__ mask, TreeShape sh,
+    int n_chunks, float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m,
+    float* __restrict__ part_l, float* __restrict__ part_o) {
+  constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
+  constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
+  constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
+  __shared__ __attribute__((aligned(16))) char lds[kSlots * kPart];
+  // row chunks of the same keys next to each other on one XCD
+  const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3, r0 = at % n_chunks * 16 * NRT, x = at / n_chunks * 8 + xcd;
+  if (x >= sh.n_split * sh.B * sh.Hkv) return;  // the grid is rounded up
+  const int bg = __builtin_amdgcn_readfirstlane(x / sh.n_split), split = x - bg * sh.n_split;
+  const int b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
+  TreeSeq q = tree_seq(sh, lens, cu_q, b);
+  q.len = __builtin_amdgcn_readfirstlane(q.len);
+  q.keys = __builtin_amdgcn_readfirstlane(q.keys);
+  const int R = q.T * G;
+  if (r0 >= R) return;
+  const int k0 = __builtin_amdgcn_readfirstlane(int(min(int64_t(q.keys), int64_t(split) * sh.unit)));
+  const int k1 = __builtin_amdgcn_readfirstlane(min(q.keys, k0 + sh.unit));
+  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4;
+
+  float m[NRT], l[NRT];
+  f32x4_t o[NRT][kND];
+#pragma unroll
+  for (int t = 0; t < NRT; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+#pragma unroll
+    for (int d = 0; d < kND; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+  if (k0 < k1) {
+    const char* Kb = reinterpret_cast<const char*>(K) + size_t(bg) * sh.cap * kRow;
+    const char* Vb = reinterpret_cast<const char*>(V) + size_t(bg) * sh.cap * kRow;
+    uint32_t off_k[kL], off_v[kL];
+#pragma unroll
+    for (int i = 0; i < kL; ++i) {
+      const int piece = 64 * i + lane, row = piece / kPieces, c = piece % kPieces;
+      off_k[i] = uint32_t(row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16);
+      off_v[i] = uint32_t(row * kRow + (c ^ (2 * (row / kWindow & (kPieces / 2 - 1)))) * 16);
+    }
+    auto read_k = [&](int at_slot, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
+      return *reinterpret_cast<const bf16x8_t*>(lds + at_slot * kPart + row * kRow +
+                                                ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
+    };
+    auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
+    int pf_key = k0, pf_slot = 0;
+    auto issue = [&](const char* base, const uint32_t (&off)[kL]) {  // past the range: an empty resource, no access
+      const int left = min(kC, q.keys - pf_key);
+      const u32x4_t r = rsrc_words(base + size_t(pf_key) * kRow, pf_key < k1 ? uint32_t(left) * kRow : 0u);
+#pragma unroll
+      for (int i = 0; i < kL; ++i) dma16(r, off[i], 0, lds + pf_slot * kPart + 1024 * i);
+      pf_slot = pf_slot + 1 == kSlots ? 0 : pf_slot + 1;
+    };
+    uint64_t bits[NRT];
+#pragma unroll
+    for (int t = 0; t < NRT; ++t) {
+      const int r = r0 + 16 * t + fr;
+      bits[t] = r < R ? tree_bits(mask, q.q0, r / G) : 0;
+    }
+    // the rows of Q come first, through the ring's last slot and laid out as a K part: a load of their own would
+    // wait for every transfer issued around it
+    {
+      const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
+                                    uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
+#pragma unroll
+      for (int i = 0; i < kL * NRT / 2 + (kL * NRT % 2); ++i) {
+        const int row = (64 * i + lane) / kPieces, r = r0 + row;
+        const uint32_t piece = off_k[i] - uint32_t(row * kRow);
+        dma16(rq, r < R ? (uint32_t(r / G) * uint32_t(sh.Hq) + uint32_t(g * G + r % G)) * kRow + piece : kPastEnd, 0,
+              lds + (kSlots - 1) * kPart + 1024 * i);
+      }
+    }
+    issue(Kb, off_k);
+    issue(Vb, off_v);
+    pf_key += kC;
+    issue(Kb, off_k);
+    issue(Vb, off_v);
+    pf_key += kC;
+    arrived<(kSlots - 1) * kL>();
+    bf16x8_t qf[NRT][kNK];
+#pragma unroll
+    for (int t = 0; t < NRT; ++t)
+#pragma unroll
+      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kSlots - 1, 16 * t + fr, c);
+    lds_read_done();
+    issue(Kb, off_k);
+    int slot = 0;
+    for (int k = k0; k < k1; k += kC) {
+      const bool edge = k + kC > q.len;  // holds drafted tokens, or ends the sequence
+      // ---- scores
+      arrived<(kSlots - 1) * kL>();
+      bf16x8_t kf[2][kNK];
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int c = 0; c < kNK; ++c) kf[a][c] = read_k(slot, 16 * a + fr, c);
+      lds_read_done();
+      issue(Vb, off_v);
+      pf_key += kC;
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
+      float p[NRT][8];
+      bf16x8_t pf[NRT];
+#pragma unroll
+      for (int t = 0; t < NRT; ++t) {
+        f32x4_t s[2];
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          s[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kNK; ++c) s[a] = mfma_bf16(kf[a][c], qf[t][c], s[a]);
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[t][e] = s[e / 4][e % 4] * c2;
+          if (edge) {
+            const int key = k + 16 * (e / 4) + 4 * fq + e % 4;
+            p[t][e] = key < q.keys && tree_sees(bits[t], key - q.len) ? p[t][e] : -INFINITY;
+          }
+          mx = fmaxf(mx, p[t][e]);
+        }
+        if (kScores && r0 + 16 * t + fr < R) {
+          float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
+          *reinterpret_cast<f32x4_t*>(w) = f32x4_t{p[t][0], p[t][1], p[t][2], p[t][3]};
+          *reinterpret_cast<f32x4_t*>(w + 16) = f32x4_t{p[t][4], p[t][5], p[t][6], p[t][7]};
+        }
+        if (__any(mx > m[t] + 16.f)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          mx = fmaxf(mx, m[t]);
+          const float f = fast_exp2(m[t] - (mx == -INFINITY ? 0.f : mx));
+          m[t] = mx;
+          l[t] *= f;
+#pragma unroll
+          for (int d = 0; d < kND; ++d) o[t][d] *= f;
+        }
+        const float ref = m[t] == -INFINITY ? 0.f : m[t];  // nothing seen yet: all weights are 0
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[t][e] = fast_exp2(p[t][e] - ref);
+          l[t] += p[t][e];
+          pf[t][e] = __bf16(p[t][e]);  // as the matrix cores take it; l keeps the unrounded sum
+        }
+      }
+      // ---- output
+      arrived<(kSlots - 1) * kL>();
+      const char* vs = lds + slot * kPart;
+      bf16x8_t vf[kND];
+#pragma unroll
+      for (int d = 0; d < kND; ++d) {
+        const int row = 4 * fq + (fr >> 2);  // and 16 further on: the swizzle is the same
+        const char* w = vs + row * kRow + (d ^ unit_of(row)) * 32 + (fr & 3) * 8;
+        vf[d] = join_tr(read_tr(w), read_tr(w + 16 * kRow));
+      }
+      lds_read_done();
+      if (edge) {
+        // A drafted token that a row does not see has weight 0 there, which a non-finite value must not meet: such
+        // values leave the product and are added, one by one, to the rows that see them.
+        bool bad = false;
+#pragma unroll
+        for (int d = 0; d < kND; ++d) {
+          s16x8_t v = __builtin_bit_cast(s16x8_t, vf[d]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool inf = (v[e] & 0x7f80) == 0x7f80;
+            bad |= inf;
+            v[e] = inf ? short(0) : v[e];
+          }
+          vf[d] = __builtin_bit_cast(bf16x8_t, v);
+        }
+        if (__any(bad)) {
+          for (int j = 0; j < kC && k + j < q.keys; ++j) {
+            const int from = fr + 16 * (j % 16 / 4), e = j / 16 * 4 + j % 4;
+#pragma unroll
+            for (int t = 0; t < NRT; ++t) {
+              float mine = 0.f;
+#pragma unroll
+              for (int z = 0; z < 8; ++z) mine = z == e ? p[t][z] : mine;
+              const float w = __shfl(mine, from, 64);
+              if (!tree_sees(bits[t], k + j - q.len)) continue;
+#pragma unroll
+              for (int d = 0; d < kND; ++d)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                  const int at_d = 16 * d + 4 * fq + z;
+                  const uint16_t v = *reinterpret_cast<const uint16_t*>(
+                      vs + j * kRow + ((at_d / 16) ^ unit_of(j)) * 32 + (at_d % 16) * 2);
+                  if ((v & 0x7f80) == 0x7f80) o[t][d][z] += w * bf16_to_f32(v);
+                }
+            }
+          }
+          lds_read_done();
+        }
+      }
+      issue(Kb, off_k);
+      slot = slot + 1 == kSlots ? 0 : slot + 1;
+#pragma unroll
+      for (int t = 0; t < NRT; ++t)
+#pragma unroll
+        for (int d = 0; d < kND; ++d) o[t][d] = mfma_bf16(vf[d], pf[t], o[t][d]);
+    }
+    wait_vm<0>();  // no transfer into LDS outlives the workgroup
+  }
+#pragma unroll
+  for (int t = 0; t < NRT; ++t) {
+    const int r = r0 + 16 * t + fr;
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
+    if (r >= R) continue;
+    const size_t row = size_t(split) * sh.n_q * sh.Hq + size_t(q.q0 + r / G) * sh.Hq + g * G + r % G;
+    if (fq == 0) {
+      part_m[row] = m[t];
+      part_l[row] = l[t];
+    }
+    if (k0 < k1)
+#pragma unroll
+      for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[t][d];
+  }
+}
+
+// Joins the ranges' partial results of each row, one workgroup per row: its four waves take every fourth range, a
+// lane DH / 64 (at least one) columns.  Rows past the last sequence's are left as they are.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void tree_join_kernel(const float* __restrict__ part_m,
                                                         const float* __restrict__ part_l,
                                                         const float* __restrict__ part_o,
                                                         const int* __restrict__ q_end, int n_split, int n_q, int Hq,
                                                         T* __restrict__ O, float* __restrict__ lse) {
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = int64_t(n_q) * Hq, row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (row >= rows || row / Hq >= q_end[0]) return;
+  constexpr int kE = DH >= 64 ? DH / 64 : 1;
+  __shared__ float top[4], sum[4], part[4][64 * kE];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t rows = int64_t(n_q) * Hq, row = blockIdx.x;
+  if (row / Hq >= q_end[0]) return;
   float M = -INFINITY;
-  for (int p = lane; p < n_split; p += 64) M = fmaxf(M, part_m[p * rows + row]);
+  for (int p = threadIdx.x; p < n_split; p += 256) M = fmaxf(M, part_m[p * rows + row]);
   M = wave_max(M);
+  if (lane == 0) top[wave] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
   const float ref = M == -INFINITY ? 0.f : M;
-  float l = 0.f, o[(DH + 63) / 64] = {};
-  for (int p = 0; p < n_split; ++p) {
-    const float f = fast_exp2(part_m[p * rows + row] - ref), lp = part_l[p * rows + row];
+  const bool mine = kE * lane < DH;
+  float l = 0.f, o[kE] = {};
+#pragma unroll 4
+  for (int p = wave; p < n_split; p += 4) {
+    const float lp = part_l[p * rows + row], f = fast_exp2(part_m[p * rows + row] - ref);
     if (lp == 0.f) continue;  // the range holds nothing the row sees
     l = fmaf(f, lp, l);
+    if (mine)
 #pragma unroll
-    for (int e = 0; e < (DH + 63) / 64; ++e)
-      if (64 * e + lane < DH) o[e] = fmaf(f, part_o[(p * rows + row) * DH + 64 * e + lane], o[e]);
+      for (int e = 0; e < kE; ++e) o[e] = fmaf(f, part_o[(p * rows + row) * DH + kE * lane + e], o[e]);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (lane == 0) sum[wave] = l;
 #pragma unroll
-  for (int e = 0; e < (DH + 63) / 64; ++e)
-    if (64 * e + lane < DH) store1(O + row * DH + 64 * e + lane, o[e] * inv);
-  if (lane == 0) lse[(row % Hq) * n_q + row / Hq] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
+  for (int e = 0; e < kE; ++e) part[wave][kE * lane + e] = o[e];
+  __syncthreads();
+  l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  if (threadIdx.x < DH) {
+    const int c = threadIdx.x;
+    store1(O + row * DH + c, ((part[0][c] + part[1][c]) + (part[2][c] + part[3][c])) * inv);
+  }
+  if (threadIdx.x == 0) lse[(row % Hq) * n_q + row / Hq] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
+}
+
+// acc[b][g][key] += sum over the rows of exp(s - lse), from the scores (base 2) the attention kernel has stored: a
+// thread per 4 keys.
+__global__ __launch_bounds__(256) void tree_weight_stored_kernel(const float* __restrict__ scores, int pitch,
+                                                                 const float* __restrict__ lse,
+                                                                 const int* __restrict__ lens,
+                                                                 const int* __restrict__ cu_q, TreeShape sh,
+                                                                 float* __restrict__ acc) {
+  const int bg = blockIdx.y, b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
+  const int R = q.T * G, k = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (k >= q.keys || R == 0) return;
+  f32x4_t sum{0.f, 0.f, 0.f, 0.f};
+  for (int r = 0; r < R; ++r) {
+    const float l = lse[size_t(g * G + r % G) * sh.n_q + q.q0 + r / G];
+    if (l == -INFINITY) continue;
+    const f32x4_t s = *reinterpret_cast<const f32x4_t*>(scores + (size_t(bg) * 16 + r) * pitch + k);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(fmaf(-l, kLog2e, s[e]));
+  }
+  float* a = acc + size_t(bg) * sh.cap + k;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (k + e < q.keys) a[e] += sum[e];
+}
+
+// The same with the scores formed again on the matrix cores (bf16): a wave per 64 keys, whose K stays in registers
+// while the rows pass, 16 at a time; sums over the rows of a product's columns join at the end.
+template <int DH>
+__global__ __launch_bounds__(64) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
+                                                              const uint16_t* __restrict__ K,
+                                                              const float* __restrict__ lse,
+                                                              const int* __restrict__ lens,
+                                                              const int* __restrict__ cu_q,
+                                                              const int64_t* __restrict__ mask,
+                                                              const float* __restrict__ row_weight, TreeShape sh,
+                                                              float c2, float* __restrict__ acc) {
+  constexpr int kNK = DH / 32;
+  const int bg = blockIdx.x % (sh.B * sh.Hkv), b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int k = blockIdx.x / (sh.B * sh.Hkv) * kTKeys;
+  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
+  const int R = q.T * G, lane = threadIdx.x, fr = lane & 15, fq = lane >> 4;
+  if (k >= q.keys || R == 0) return;
+  const bool edge = k + kTKeys > q.len;
+  bf16x8_t kf[4][kNK];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) {
+    const int key = min(k + 16 * a + fr, q.keys - 1);
+#pragma unroll
+    for (int c = 0; c < kNK; ++c)
+      kf[a][c] = *reinterpret_cast<const bf16x8_t*>(K + (size_t(bg) * sh.cap + key) * DH + 32 * c + 8 * fq);
+  }
+  f32x4_t sum[4];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) sum[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int r0 = 0; r0 < R; r0 += 16) {
+    const int r = r0 + fr;
+    const bool live = r < R;
+    const int tok = q.q0 + (live ? r / G : 0), h = g * G + (live ? r % G : 0);
+    const float w = !live ? 0.f : row_weight ? row_weight[tok] : 1.f;
+    if (!__any(w != 0.f)) continue;
+    const float l = lse[size_t(h) * sh.n_q + tok], l2 = l * kLog2e;
+    const uint64_t bits = tree_bits(mask, q.q0, live ? r / G : 0);
+    bf16x8_t qf[kNK];
+#pragma unroll
+    for (int c = 0; c < kNK; ++c)
+      qf[c] = *reinterpret_cast<const bf16x8_t*>(Q + (size_t(tok) * sh.Hq + h) * DH + 32 * c + 8 * fq);
+    const bool counts = w != 0.f && l != -INFINITY;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      f32x4_t s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
+#pragma unroll
+      for (int z = 0; z < 4; ++z) {
+        bool sees = counts;
+        if (edge) sees &= tree_sees(bits, k + 16 * a + 4 * fq + z - q.len);
+        sum[a][z] += sees ? w * fast_exp2(fmaf(s[z], c2, -l2)) : 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int z = 0; z < 4; ++z)
+#pragma unroll
+      for (int x = 1; x < 16; x <<= 1) sum[a][z] += __shfl_xor(sum[a][z], x, 64);
+  // lane (fr, fq) adds key 16 (fr / 4) + 4 fq + fr % 4
+  float v = 0.f;
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int z = 0; z < 4; ++z) v = fr == 4 * a + z ? sum[a][z] : v;
+  const int key = k + 16 * (fr >> 2) + 4 * fq + (fr & 3);
+  if (key < q.keys) acc[size_t(bg) * sh.cap + key] += v;
 }
 
 // acc[b][g][key] += sum over the rows of w exp(s - lse): one workgroup per 64 keys of a (sequence, KV head).
@@ -265,25 +610,40 @@ __global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ 
 
 // ------------------------------------------------------------------ plan and workspace
 
-// Ranges of the keys of one (sequence, KV head): enough workgroups for the chip, ranges of at least 128 keys.
-inline int plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv) {
-  const int64_t groups = int64_t(B) * Hkv * ((int64_t(max_q) * (Hq / Hkv) + kTRows - 1) / kTRows);
-  const int64_t most = (int64_t(max_kv) + 127) / 128;
-  return int(std::max<int64_t>(1, std::min<int64_t>(most, (1024 + groups - 1) / groups)));
+// How a call is cut: n_split ranges of `unit` keys of every (sequence, KV head), n_chunks of its rows.
+struct TreePlan {
+  int n_split, unit, n_chunks, row_tiles;
+  bool stored;  // the scores are kept for the account
+};
+inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
+  const int64_t rows = int64_t(max_q) * (Hq / Hkv), groups = int64_t(B) * Hkv;
+  TreePlan p;
+  p.row_tiles = dtype == ESTP_F32 || rows <= 16 ? 1 : 2;
+  p.n_chunks = int((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
+  // ranges of 256 keys, longer ones while there are many of them
+  int64_t unit = 256;
+  while (unit < max_kv && groups * p.n_chunks * ((max_kv + unit - 1) / unit) > 8192) unit *= 2;
+  p.unit = int(unit);
+  p.n_split = int((max_kv + unit - 1) / unit);
+  p.stored = dtype == ESTP_BF16 && p.n_chunks == 1 && p.row_tiles == 1 && rows * 4 <= dh;
+  return p;
 }
 
 struct TreeBuffers {
-  float *m, *l, *o, *lse;
+  float *m, *l, *o, *lse, *scores;
+  int pitch;
   size_t bytes;
 };
-inline TreeBuffers carve_tree(int n_split, int64_t n_q, int Hq, int dh, void* ws) {
+inline TreeBuffers carve_tree(const TreePlan& p, int B, int64_t n_q, int Hq, int Hkv, int max_kv, int dh, void* ws) {
   const size_t rows = size_t(n_q) * Hq;
   Carver c(ws);
   TreeBuffers t;
-  t.m = c.take<float>(n_split * rows);
-  t.l = c.take<float>(n_split * rows);
-  t.o = c.take<float>(n_split * rows * dh);
+  t.m = c.take<float>(p.n_split * rows);
+  t.l = c.take<float>(p.n_split * rows);
+  t.o = c.take<float>(p.n_split * rows * dh);
   t.lse = c.take<float>(rows);
+  t.pitch = (max_kv + 31) / 32 * 32;
+  t.scores = c.take<float>(p.stored ? size_t(B) * Hkv * 16 * t.pitch : 0);
   t.bytes = c.bytes();
   return t;
 }
@@ -307,10 +667,10 @@ int check_tree_args(const char* fn, const void* Q, const void* K, const int32_t*
                fn);
   ESTP_REQUIRE(dh == 32 || dh == 64 || dh == 128, ESTP_ERR_UNSUPPORTED, "%s: head_dim %d not in {32, 64, 128}", fn, dh);
   ESTP_REQUIRE(max_q <= kMaxTree, ESTP_ERR_UNSUPPORTED, "%s: max_q = %d, at most %d drafted tokens", fn, max_q, kMaxTree);
-  ESTP_REQUIRE(int64_t(max_q) * (Hq / Hkv) <= 65535, ESTP_ERR_UNSUPPORTED, "%s: %d query heads share a KV head", fn,
-               Hq / Hkv);
-  ESTP_REQUIRE(int64_t(B) * Hkv <= INT32_MAX / 4096 && n_q * Hq <= INT32_MAX / 64, ESTP_ERR_UNSUPPORTED,
-               "%s: B Hkv = %lld or n_q Hq = %lld too large", fn, (long long)B * Hkv, (long long)n_q * Hq);
+  ESTP_REQUIRE(int64_t(max_q) * (Hq / Hkv) <= 65535 && Hq <= 65536, ESTP_ERR_UNSUPPORTED,
+               "%s: %d query heads, %d sharing a KV head", fn, Hq, Hq / Hkv);
+  ESTP_REQUIRE(int64_t(B) * Hkv <= 65535 && n_q * Hq <= INT32_MAX / 64, ESTP_ERR_UNSUPPORTED,
+               "%s: B Hkv = %lld (at most 65535) or n_q Hq = %lld too large", fn, (long long)B * Hkv, (long long)n_q * Hq);
   const size_t tiles = size_t(max_kv + kTKeys - 1) / kTKeys;
   ESTP_REQUIRE(fits_launch(tiles * size_t(B) * Hkv, 256), ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv too large", fn);
   return ESTP_OK;
@@ -318,12 +678,22 @@ int check_tree_args(const char* fn, const void* Q, const void* K, const int32_t*
 
 template <typename T, int DH>
 int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* cu_q, const int64_t* mask,
-                const TreeShape& sh, int max_q, float scale, T* O, float* lse, const TreeBuffers& t, hipStream_t s) {
-  const unsigned chunks = unsigned((max_q * (sh.Hq / sh.Hkv) + kTRows - 1) / kTRows);
-  tree_attn_kernel<T, DH><<<dim3(unsigned(sh.n_split * sh.B * sh.Hkv), chunks), dim3(256), 0, s>>>(
-      Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
+                const TreeShape& sh, const TreePlan& p, bool scores, float scale, T* O, float* lse,
+                const TreeBuffers& t, hipStream_t s) {
+  const size_t groups = size_t(sh.n_split) * sh.B * sh.Hkv;
+  if constexpr (sizeof(T) == 2) {
+    const dim3 grid(unsigned((groups + 7) / 8 * 8 * p.n_chunks));
+    auto kernel = p.row_tiles == 2 ? tree_attn_mfma_kernel<DH, 2, false>
+                  : scores         ? tree_attn_mfma_kernel<DH, 1, true>
+                                   : tree_attn_mfma_kernel<DH, 1, false>;
+    kernel<<<grid, dim3(64), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, p.n_chunks, scale * kLog2e, t.scores, t.pitch, t.m,
+                                     t.l, t.o);
+  } else {
+    tree_attn_kernel<T, DH><<<dim3(unsigned(groups), unsigned(p.n_chunks)), dim3(256), 0, s>>>(
+        Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
+  }
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
-  tree_join_kernel<T, DH><<<dim3(unsigned((size_t(sh.n_q) * sh.Hq + 3) / 4)), dim3(256), 0, s>>>(
+  tree_join_kernel<T, DH><<<dim3(unsigned(size_t(sh.n_q) * sh.Hq)), dim3(256), 0, s>>>(
       t.m, t.l, t.o, cu_q + sh.B, sh.n_split, sh.n_q, sh.Hq, O, lse);
   ESTP_CHECK_LAUNCH("tree_join_kernel");
   return ESTP_OK;
@@ -332,8 +702,13 @@ template <typename T, int DH>
 int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, const int* cu_q, const int64_t* mask,
                   const float* row_weight, const TreeShape& sh, float scale, float* acc, hipStream_t s) {
   const unsigned tiles = unsigned((sh.max_kv + kTKeys - 1) / kTKeys);
-  tree_weight_kernel<T, DH><<<dim3(tiles * unsigned(sh.B * sh.Hkv)), dim3(256), 0, s>>>(
-      Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e, acc);
+  const dim3 grid(tiles * unsigned(sh.B * sh.Hkv));
+  if constexpr (sizeof(T) == 2)
+    tree_weight_mfma_kernel<DH><<<grid, dim3(64), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
+                                                          acc);
+  else
+    tree_weight_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
+                                                         acc);
   ESTP_CHECK_LAUNCH("tree_weight_kernel");
   return ESTP_OK;
 }
@@ -359,9 +734,8 @@ using namespace estp::detail;
 
 extern "C" size_t estp_tree_attention_workspace_size(int32_t B, int32_t max_q, int64_t n_q, int32_t Hq, int32_t Hkv,
                                                      int32_t max_kv, int32_t dh, int dtype) {
-  (void)dtype;
   if (B < 1 || max_q < 1 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_kv < 1 || dh < 1) return 0;
-  return carve_tree(plan_tree(B, max_q, max_kv, Hq, Hkv), n_q, Hq, dh, nullptr).bytes;
+  return carve_tree(plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype), B, n_q, Hq, Hkv, max_kv, dh, nullptr).bytes;
 }
 
 extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, const int32_t* lens,
@@ -381,16 +755,27 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
                workspace_bytes, need);
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
-  const TreeShape sh{B, int(n_q), Hq, Hkv, int(cap), max_kv, plan_tree(B, max_q, max_kv, Hq, Hkv)};
-  const TreeBuffers t = carve_tree(sh.n_split, n_q, Hq, dh, workspace);
+  const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
+  ESTP_REQUIRE(fits_launch(size_t(p.n_split) * B * Hkv * p.n_chunks + 8 * size_t(p.n_chunks), 256) &&
+                   fits_launch(size_t(n_q) * Hq, 256),
+               ESTP_ERR_UNSUPPORTED, "%s: more workgroups than one launch holds", fn);
+  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.n_split, p.unit};
+  const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   float* row_lse = lse ? lse : t.lse;
-  return tree_dispatch(dtype, dh, [&](auto element, auto size) {
+  const bool stored = acc && p.stored;
+  return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
     using T = decltype(element);
     constexpr int DH = decltype(size)::value;
     const int rc = launch_tree<T, DH>(static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V),
-                                      lens, cu_q, tree_mask, sh, max_q, scale, static_cast<T*>(O), row_lse, t, s);
+                                      lens, cu_q, tree_mask, sh, p, stored, scale, static_cast<T*>(O), row_lse, t, s);
     if (rc != ESTP_OK || !acc) return rc;
+    if (stored) {
+      tree_weight_stored_kernel<<<dim3(unsigned((max_kv + 1023) / 1024), unsigned(B * Hkv)), dim3(256), 0, s>>>(
+          t.scores, t.pitch, row_lse, lens, cu_q, sh, acc);
+      ESTP_CHECK_LAUNCH("tree_weight_stored_kernel");
+      return ESTP_OK;
+    }
     return launch_weight<T, DH>(static_cast<const T*>(Q), static_cast<const T*>(K), row_lse, lens, cu_q, tree_mask,
                                 nullptr, sh, scale, acc, s);
   });
@@ -407,8 +792,8 @@ extern "C" int estp_tree_importance(const void* Q, const void* K, const float* l
   ESTP_REQUIRE(lse && acc, ESTP_ERR_INVALID_ARG, "%s: lse and acc must be non-null", fn);
   ESTP_REQUIRE(aligned(tree_mask, 8) && aligned(lse, 4) && aligned(acc, 4) && aligned(row_weight, 4),
                ESTP_ERR_INVALID_ARG, "%s: tree_mask must be 8-byte, lse, row_weight and acc 4-byte aligned", fn);
-  const TreeShape sh{B, int(n_q), Hq, Hkv, int(cap), max_kv, 1};
-  return tree_dispatch(dtype, dh, [&](auto element, auto size) {
+  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, 1, max_kv};
+  return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
     using T = decltype(element);
     return launch_weight<T, decltype(size)::value>(static_cast<const T*>(Q), static_cast<const T*>(K), lse, lens, cu_q,
                                                    tree_mask, row_weight, sh, scale, acc,
