@@ -9,11 +9,12 @@
 // move at once in place.  The order of the slots carries no meaning, their
 // positions are in pos.
 //
-// evict_select_kernel, one workgroup per (sequence, KV head): the weights'
-// order-preserving 32-bit keys are cut to the threshold of the last one kept
-// by four histogram passes of 8 bits (LDS), then one pass in slot order counts
-// ties, holes and survivors and lists the moves.  evict_move_kernel copies the
-// listed rows.  Everything is exact: whole numbers and copies.
+// evict_select_kernel, one workgroup per (sequence, KV head), a thread per every 1024th slot: the weights'
+// order-preserving 32-bit keys stay in registers (caches of up to 65536 slots; longer ones are read again on each
+// pass).  Four histogram passes of 8 bits in LDS find the key of the last one kept.  Places in slot order (of ties,
+// holes and survivors) come from ballots: a count per 64 slots, one prefix over all counts.  The survivors' rows move
+// in the same kernel where its workgroups fill the chip or there is little to move, else in evict_move_kernel.
+// Everything is exact: whole numbers and copies.
 #include <algorithm>
 
 #include "estp_common.h"
@@ -32,146 +33,269 @@ __device__ __forceinline__ uint32_t weight_key(float v) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// Exclusive prefix of `v` over the workgroup (every thread calls), and its total.
-struct Scan {
-  int before, total;
-};
-__device__ __forceinline__ Scan block_scan(int v, int* sh) {
+// Exclusive prefix of a thread's pair of counts over the workgroup (every thread calls), in the halves of 64 bits.
+__device__ __forceinline__ uint64_t block_prefix(uint64_t v, uint64_t* sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
+  uint64_t x = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o, 64);
+    const uint64_t y = __shfl_up(x, o, 64);
     if (lane >= o) x += y;
   }
-  __syncthreads();  // the previous scan's totals are read
   if (lane == 63) sh[wave] = x;
   __syncthreads();
-  Scan r{x - v, 0};
+  uint64_t before = x - v;
 #pragma unroll
-  for (int w = 0; w < kEWaves; ++w) {
-    r.before += w < wave ? sh[w] : 0;
-    r.total += sh[w];
-  }
-  return r;
+  for (int w = 0; w < kEWaves; ++w) before += w < wave ? sh[w] : 0;
+  return before;
 }
 
-__global__ __launch_bounds__(kEThreads) void evict_select_kernel(
-    const float* __restrict__ acc, const int* __restrict__ pos, const int* __restrict__ lens,
-    const int* __restrict__ seen, int Hkv, int cap, int keep, int recent, int sink, float* acc_out, int* pos_out,
-    int* __restrict__ idx, int2* __restrict__ moves, int* __restrict__ n_moves) {
-  __shared__ int hist[256], sh[kEWaves], found[2];
-  const int bg = blockIdx.x, b = bg / Hkv, tid = threadIdx.x;
-  const size_t base = size_t(bg) * cap;
-  const int n = max(0, min(lens[b], cap));
-  acc += base;
-  pos += base;
-  acc_out += base;
-  pos_out += base;
-  idx += size_t(bg) * keep;
-  moves += size_t(bg) * keep;
+// One row of the slots' 1024: the thread's slot of round i is 1024 i + tid.
+struct EvictArgs {
+  const float* acc;
+  const int *pos, *lens, *seen;
+  int Hkv, cap, keep, recent, sink;
+  float* acc_out;
+  int *pos_out, *idx;
+  int2* moves;
+  int* n_moves;
+  uint4 *K, *V;  // rows moved here, or null: by evict_move_kernel
+  int row16;
+  int* lens_out;  // written here when the rows are
+};
+
+__device__ __forceinline__ void move_rows(uint4* K, uint4* V, size_t base, int row16, const int2* moves, int n,
+                                          int64_t first, int64_t step) {
+  for (int64_t i = first; i < int64_t(n) * row16; i += step) {
+    const int2 e = moves[i / row16];
+    const int c = int(i % row16);
+    const uint4 k = K[(base + e.x) * row16 + c], v = V[(base + e.x) * row16 + c];
+    K[(base + e.y) * row16 + c] = k;
+    V[(base + e.y) * row16 + c] = v;
+  }
+}
+
+// kE rounds of 1024 slots in registers; kE = 0: any number, read from memory on every pass.
+template <int kE>
+__global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
+  constexpr int kHists = 4;  // copies of the histogram: equal weights meet on fewer threads
+  constexpr int kSpan = kE > 0 ? kE : 64;  // rounds whose counts one prefix covers
+  __shared__ int hist[kHists][256];
+  __shared__ uint32_t found[2];
+  __shared__ int n_guarded_sh;
+  __shared__ uint64_t wave_sum_sh[kEWaves], counts[kSpan * kEWaves], carry;
+  const int bg = blockIdx.x, b = bg / g.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const size_t base = size_t(bg) * g.cap;
+  const int n = max(0, min(g.lens[b], g.cap)), keep = g.keep;
+  const float* acc = g.acc + base;
+  const int* pos = g.pos + base;
+  float* acc_out = g.acc_out + base;
+  int* pos_out = g.pos_out + base;
+  int* idx = g.idx + size_t(bg) * keep;
+  int2* moves = g.moves + size_t(bg) * keep;
+  const bool copy = acc_out != acc || pos_out != pos;
+  if (g.K && tid == 0 && bg % g.Hkv == 0) g.lens_out[b] = min(n, keep);
   if (n <= keep) {  // everything stays
     for (int i = tid; i < keep; i += kEThreads) idx[i] = i < n ? i : -1;
-    for (int i = tid; i < n; i += kEThreads) {
-      acc_out[i] = acc[i];
-      pos_out[i] = pos[i];
-    }
-    if (tid == 0) n_moves[bg] = 0;
+    if (copy)
+      for (int i = tid; i < n; i += kEThreads) {
+        acc_out[i] = acc[i];
+        pos_out[i] = pos[i];
+      }
+    if (tid == 0) g.n_moves[bg] = 0;
     return;
   }
-  const int64_t first_recent = int64_t(seen[b]) - recent;
-  auto guarded = [&](int i) { return pos[i] < sink || pos[i] >= first_recent; };
-  // guarded slots: all stay if they fit, else the best of them do and nothing else
+  const int64_t first_recent = int64_t(g.seen[b]) - g.recent;
+  auto is_guarded = [&](int i) { return pos[i] < g.sink || pos[i] >= first_recent; };
+  const int rounds = kE > 0 ? kE : (n + kEThreads - 1) / kEThreads;
+
+  uint32_t key[kE > 0 ? kE : 1];
+  uint64_t guard = 0;
+  if (tid == 0) n_guarded_sh = 0;
+  for (int i = tid; i < kHists * 256; i += kEThreads) (&hist[0][0])[i] = 0;
+  __syncthreads();
   int mine = 0;
-  for (int i = tid; i < n; i += kEThreads) mine += guarded(i);
-  const int n_guarded = block_scan(mine, sh).total;
+  if constexpr (kE > 0) {
+#pragma unroll
+    for (int r = 0; r < kE; ++r) {
+      const int i = r * kEThreads + tid;
+      key[r] = i < n ? weight_key(acc[i]) : 0;
+      const bool gd = i < n && is_guarded(i);
+      guard |= uint64_t(gd) << r;
+      mine += gd;
+    }
+  } else {
+    for (int i = tid; i < n; i += kEThreads) mine += is_guarded(i);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
+  if (lane == 0 && mine) atomicAdd(&n_guarded_sh, mine);
+  __syncthreads();
+  // guarded slots: all stay if they fit, else the best of them do and nothing else
+  const int n_guarded = n_guarded_sh;
   const bool among = n_guarded >= keep;  // whether the choice is among the guarded slots
-  int need = among ? keep : keep - n_guarded;
+  uint32_t need = uint32_t(among ? keep : keep - n_guarded);
+  // Round r's slot of this thread: its key, and whether it is in the choice.
+  auto at = [&](int r, uint32_t* k, bool* in, bool* gd) {
+    const int i = r * kEThreads + tid;
+    *in = i < n;
+    if constexpr (kE > 0) {
+      *k = key[r];
+      *gd = (guard >> r) & 1;
+    } else {
+      *k = *in ? weight_key(acc[i]) : 0;
+      *gd = *in && is_guarded(i);
+    }
+  };
+  auto each_round = [&](auto&& f) {
+    if constexpr (kE > 0) {
+#pragma unroll
+      for (int r = 0; r < kE; ++r) f(r);
+    } else {
+      for (int r = 0; r < rounds; ++r) f(r);
+    }
+  };
   // the key of the need-th best candidate, 8 bits at a time; `need` becomes how many of its equals stay
   uint32_t prefix = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kEThreads) hist[i] = 0;
+    each_round([&](int r) {
+      uint32_t k;
+      bool in, gd;
+      at(r, &k, &in, &gd);
+      if (in && gd == among && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
+        atomicAdd(&hist[wave % kHists][(k >> shift) & 255], 1);
+    });
     __syncthreads();
-    for (int i = tid; i < n; i += kEThreads) {
-      const uint32_t k = weight_key(acc[i]);
-      if (guarded(i) == among && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
-        atomicAdd(&hist[(k >> shift) & 255], 1);
+    if (wave == 0) {  // lane j: bins 255 - 4 j down to 252 - 4 j; the first lane whose running count reaches `need`
+      uint32_t c[4], sum = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        c[q] = 0;
+#pragma unroll
+        for (int h = 0; h < kHists; ++h) {
+          c[q] += uint32_t(hist[h][255 - 4 * lane - q]);
+          hist[h][255 - 4 * lane - q] = 0;
+        }
+        sum += c[q];
+      }
+      uint32_t x = sum;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t y = __shfl_up(x, o, 64);
+        if (lane >= o) x += y;
+      }
+      const uint64_t reached = __ballot(x >= need);
+      if (reached && lane == __builtin_ctzll(reached)) {
+        uint32_t above = x - sum;
+        int q = 0;
+        while (q < 3 && above + c[q] < need) above += c[q++];
+        found[0] = uint32_t(255 - 4 * lane - q);
+        found[1] = need - above;
+      }
     }
     __syncthreads();
-    if (tid == 0) {
-      int above = 0, d = 255;
-      while (d > 0 && above + hist[d] < need) above += hist[d--];
-      found[0] = d;
-      found[1] = need - above;
-    }
-    __syncthreads();
-    prefix |= uint32_t(found[0]) << shift;
+    prefix |= found[0] << shift;
     need = found[1];
   }
-  // in slot order: which slots stay, and the moves
-  int ties = 0, holes = 0, late = 0;
-  for (int at = 0; at < n; at += kEThreads) {
-    const int i = at + tid;
-    const bool in = i < n;
-    const bool gd = in && guarded(i);
-    const uint32_t k = in ? weight_key(acc[i]) : 0;
-    const bool tie = in && gd == among && k == prefix;
-    const Scan st = block_scan(tie, sh);
-    const bool stays = in && ((gd && !among) || (gd == among && k > prefix) || (tie && ties + st.before < need));
-    ties += st.total;
-    const Scan sl = block_scan(stays && i >= keep, sh);
-    const Scan so = block_scan(in && !stays && i < keep, sh);
-    if (in && i < keep) {
-      if (stays)
-        idx[i] = i;
-      else
-        moves[holes + so.before].y = i;
-    } else if (stays) {
-      moves[late + sl.before].x = i;
+
+  // Places in slot order: pass 0 counts ties and sees which of them stay, pass 1 counts holes (low half) and
+  // survivors (high half) and lists them.  Per span of rounds: a count for every 64 slots, one prefix, the lanes' own.
+  uint64_t stays = 0;  // kE > 0: a bit a round
+  int ties_before = 0;
+  uint64_t moved_before = 0;
+  auto span = [&](int r0, auto&& flags) {  // flags(r, &low, &high): exclusive counts before the thread's slot
+    const int nr = min(kSpan, rounds - r0);
+    for (int r = r0; r < r0 + nr; ++r) {
+      bool lo, hi;
+      flags(r, &lo, &hi);
+      const uint64_t bl = __ballot(lo), bh = __ballot(hi);
+      if (lane == 0) counts[(r - r0) * kEWaves + wave] = uint64_t(__popcll(bl)) | uint64_t(__popcll(bh)) << 32;
     }
-    holes += so.total;
-    late += sl.total;
+    __syncthreads();
+    const uint64_t c = tid < nr * kEWaves ? counts[tid] : 0;
+    const uint64_t before = block_prefix(c, wave_sum_sh);
+    if (tid < nr * kEWaves) counts[tid] = before;
+    if (tid == nr * kEWaves - 1) carry = before + c;
+    __syncthreads();
+  };
+  auto below = [&](bool x) { return uint32_t(__popcll(__ballot(x) & ((uint64_t(1) << lane) - 1))); };
+  auto stays_at = [&](int r, uint32_t tie_rank, bool* in_out) {
+    uint32_t k;
+    bool in, gd;
+    at(r, &k, &in, &gd);
+    *in_out = in;
+    return in && ((gd && !among) || (gd == among && (k > prefix || (k == prefix && tie_rank < need))));
+  };
+  auto is_tie = [&](int r) {
+    uint32_t k;
+    bool in, gd;
+    at(r, &k, &in, &gd);
+    return in && gd == among && k == prefix;
+  };
+  for (int r0 = 0; r0 < rounds; r0 += kSpan) {
+    const int r1 = min(rounds, r0 + kSpan);
+    span(r0, [&](int r, bool* lo, bool* hi) {
+      *lo = is_tie(r);
+      *hi = false;
+    });
+    uint64_t bits = 0;  // of this span: stays
+    for (int r = r0; r < r1; ++r) {
+      const uint32_t rank = uint32_t(ties_before) + uint32_t(counts[(r - r0) * kEWaves + wave]) + below(is_tie(r));
+      bool in;
+      bits |= uint64_t(stays_at(r, rank, &in)) << (r - r0);
+    }
+    ties_before += int(uint32_t(carry));
+    stays = bits;
+    __syncthreads();  // counts and carry are read
+    span(r0, [&](int r, bool* lo, bool* hi) {
+      const int i = r * kEThreads + tid;
+      const bool st = (stays >> (r - r0)) & 1;
+      *lo = i < n && i < keep && !st;
+      *hi = st && i >= keep;
+    });
+    for (int r = r0; r < r1; ++r) {
+      const int i = r * kEThreads + tid;
+      const bool st = (stays >> (r - r0)) & 1, hole = i < n && i < keep && !st, late = st && i >= keep;
+      const uint64_t c = moved_before + counts[(r - r0) * kEWaves + wave];
+      const uint32_t h = uint32_t(c) + below(hole), l = uint32_t(c >> 32) + below(late);
+      if (hole) moves[h].y = i;
+      if (late) moves[l].x = i;
+      if (st && i < keep) {
+        idx[i] = i;
+        if (copy) {
+          acc_out[i] = acc[i];
+          pos_out[i] = pos[i];
+        }
+      }
+    }
+    moved_before += carry;
+    __syncthreads();  // counts and carry are read, and the moves of this span written
   }
-  __syncthreads();  // the list is complete (holes == late), and acc and pos are read no more but where they stay
+  const int holes = int(uint32_t(moved_before));  // as many as survivors
   for (int m = tid; m < holes; m += kEThreads) {
     const int2 e = moves[m];
     idx[e.y] = e.x;
     acc_out[e.y] = acc[e.x];
     pos_out[e.y] = pos[e.x];
   }
-  if (acc_out != acc || pos_out != pos) {
-    __syncthreads();  // idx is complete
-    for (int i = tid; i < keep; i += kEThreads) {
-      if (idx[i] != i) continue;
-      acc_out[i] = acc[i];
-      pos_out[i] = pos[i];
-    }
-  }
   __syncthreads();  // freed slots are cleared after the moves have read them
   for (int i = keep + tid; i < n; i += kEThreads) {
     acc_out[i] = 0.f;
     pos_out[i] = -1;
   }
-  if (tid == 0) n_moves[bg] = holes;
+  if (tid == 0) g.n_moves[bg] = holes;
+  if (g.K) move_rows(g.K, g.V, base, g.row16, moves, holes, tid, kEThreads);
 }
 
-// Rows of 16-byte pieces: destination moves[m].y, source moves[m].x, of K and of V.  Also writes lens_out, which may
-// be lens: by now evict_select_kernel has read it.
+// The listed rows of K and V.  Also writes lens_out, which may be lens: by now evict_select_kernel has read it.
 __global__ __launch_bounds__(256) void evict_move_kernel(uint4* __restrict__ K, uint4* __restrict__ V, int cap,
                                                          int row16, const int2* __restrict__ moves, int keep,
                                                          const int* __restrict__ n_moves, const int* lens, int Hkv,
                                                          int* lens_out) {
   const int bg = blockIdx.y, n = n_moves[bg];
   if (blockIdx.x == 0 && threadIdx.x == 0 && bg % Hkv == 0) lens_out[bg / Hkv] = min(max(lens[bg / Hkv], 0), keep);
-  const size_t base = size_t(bg) * cap;
-  moves += size_t(bg) * keep;
-  const int64_t total = int64_t(n) * row16;
-  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-    const int2 e = moves[i / row16];
-    const int c = int(i % row16);
-    K[(base + e.y) * row16 + c] = K[(base + e.x) * row16 + c];
-    V[(base + e.y) * row16 + c] = V[(base + e.x) * row16 + c];
-  }
+  move_rows(K, V, size_t(bg) * cap, row16, moves + size_t(bg) * keep, n, int64_t(blockIdx.x) * 256 + threadIdx.x,
+            int64_t(gridDim.x) * 256);
 }
 
 struct EvictBuffers {
@@ -231,12 +355,21 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   const int groups = B * Hkv;
   const EvictBuffers e = carve_evict(size_t(groups), keep, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  evict_select_kernel<<<dim3(unsigned(groups)), dim3(kEThreads), 0, s>>>(acc, pos, lens, seen, Hkv, int(cap), keep,
-                                                                         recent, sink, acc_out, pos_out, idx, e.moves,
-                                                                         e.n_moves);
-  ESTP_CHECK_LAUNCH("evict_select_kernel");
   const int row16 = dh * (dtype == ESTP_F32 ? 4 : 2) / 16;
-  const int64_t most = std::min<int64_t>(keep, cap - keep) * row16;
+  const int64_t most = std::min<int64_t>(keep, cap - keep) * row16;  // 16-byte pieces that can move, of K or V
+  // Rows move in the selecting kernel where its workgroups fill the chip, or where there are few (16 KB; a kernel of
+  // their own costs its launch).  Not in place of lens, which workgroups of the same sequence still read.
+  const bool here = (groups >= 192 || most <= 1024) && lens_out != lens;
+  EvictArgs g{acc, pos, lens, seen, Hkv, int(cap), keep, recent, sink, acc_out, pos_out, idx, e.moves, e.n_moves,
+              here ? static_cast<uint4*>(K) : nullptr, static_cast<uint4*>(V), row16, lens_out};
+  auto select = cap <= kEThreads        ? evict_select_kernel<1>
+                : cap <= 4 * kEThreads  ? evict_select_kernel<4>
+                : cap <= 16 * kEThreads ? evict_select_kernel<16>
+                : cap <= 64 * kEThreads ? evict_select_kernel<64>
+                                        : evict_select_kernel<0>;
+  select<<<dim3(unsigned(groups)), dim3(kEThreads), 0, s>>>(g);
+  ESTP_CHECK_LAUNCH("evict_select_kernel");
+  if (here) return ESTP_OK;
   const int64_t wgs = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, std::max(1, 4096 / groups)));
   evict_move_kernel<<<dim3(unsigned(wgs), unsigned(groups)), dim3(256), 0, s>>>(
       static_cast<uint4*>(K), static_cast<uint4*>(V), int(cap), row16, e.moves, keep, e.n_moves, lens, Hkv, lens_out);

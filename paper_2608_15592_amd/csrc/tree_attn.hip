@@ -213,6 +213,7 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
   constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
   constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
   constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
+  constexpr int kQSlot = NRT == 4 ? kSlots - 2 : kSlots - 1;
   __shared__ __attribute__((aligned(16))) char lds[kSlots * kPart];
   // row chunks of the same keys next to each other on one XCD
   const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3, r0 = at % n_chunks * 16 * NRT, x = at / n_chunks * 8 + xcd;
@@ -266,32 +267,33 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
       const int r = r0 + 16 * t + fr;
       bits[t] = r < R ? tree_bits(mask, q.q0, r / G) : 0;
     }
-    // the rows of Q come first, through the ring's last slot and laid out as a K part: a load of their own would
-    // wait for every transfer issued around it
+    // the rows of Q come first, through the ring's last slot (the last two) and laid out as K parts: a load of their
+    // own would wait for every transfer issued around it
     {
       const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
                                     uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
 #pragma unroll
-      for (int i = 0; i < kL * NRT / 2 + (kL * NRT % 2); ++i) {
+      for (int i = 0; i < kL * NRT / 2; ++i) {
         const int row = (64 * i + lane) / kPieces, r = r0 + row;
-        const uint32_t piece = off_k[i] - uint32_t(row * kRow);
+        const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (row / kWindow & (kPieces - 1))) * 16u;
         dma16(rq, r < R ? (uint32_t(r / G) * uint32_t(sh.Hq) + uint32_t(g * G + r % G)) * kRow + piece : kPastEnd, 0,
-              lds + (kSlots - 1) * kPart + 1024 * i);
+              lds + kQSlot * kPart + 1024 * i);
       }
     }
     issue(Kb, off_k);
     issue(Vb, off_v);
     pf_key += kC;
     issue(Kb, off_k);
-    issue(Vb, off_v);
-    pf_key += kC;
-    arrived<(kSlots - 1) * kL>();
+    if (NRT < 4) issue(Vb, off_v);
+    arrived<(NRT < 4 ? 4 : 3) * kL>();
     bf16x8_t qf[NRT][kNK];
 #pragma unroll
     for (int t = 0; t < NRT; ++t)
 #pragma unroll
-      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kSlots - 1, 16 * t + fr, c);
+      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kQSlot, 16 * t + fr, c);
     lds_read_done();
+    if (NRT == 4) issue(Vb, off_v);
+    pf_key += kC;
     issue(Kb, off_k);
     int slot = 0;
     for (int k = k0; k < k1; k += kC) {
@@ -427,48 +429,77 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
   }
 }
 
-// Joins the ranges' partial results of each row, one workgroup per row: its four waves take every fourth range, a
-// lane DH / 64 (at least one) columns.  Rows past the last sequence's are left as they are.
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void tree_join_kernel(const float* __restrict__ part_m,
-                                                        const float* __restrict__ part_l,
-                                                        const float* __restrict__ part_o,
-                                                        const int* __restrict__ q_end, int n_split, int n_q, int Hq,
-                                                        T* __restrict__ O, float* __restrict__ lse) {
+// Joins the ranges' partial results of each row.  kWaves waves share a row and take every kWaves-th range; a lane
+// fetches the state of one range, 64 at a time, and DH / 64 (at least one) columns of those ranges that hold
+// something.  Rows past the last sequence's are left as they are.
+template <typename T, int DH, int kWaves>
+__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_kernel(
+    const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
+    const int* __restrict__ q_end, int n_split, int n_q, int Hq, T* __restrict__ O, float* __restrict__ lse) {
   constexpr int kE = DH >= 64 ? DH / 64 : 1;
-  __shared__ float top[4], sum[4], part[4][64 * kE];
+  typedef float vec_t __attribute__((ext_vector_type(kE)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows = int64_t(n_q) * Hq, row = blockIdx.x;
-  if (row / Hq >= q_end[0]) return;
-  float M = -INFINITY;
-  for (int p = threadIdx.x; p < n_split; p += 256) M = fmaxf(M, part_m[p * rows + row]);
-  M = wave_max(M);
-  if (lane == 0) top[wave] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  const float ref = M == -INFINITY ? 0.f : M;
+  const int64_t rows = int64_t(n_q) * Hq, row = kWaves == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
+  const int first = kWaves == 1 ? 0 : wave;
+  if (row >= rows || row / Hq >= q_end[0]) return;
   const bool mine = kE * lane < DH;
-  float l = 0.f, o[kE] = {};
-#pragma unroll 4
-  for (int p = wave; p < n_split; p += 4) {
-    const float lp = part_l[p * rows + row], f = fast_exp2(part_m[p * rows + row] - ref);
-    if (lp == 0.f) continue;  // the range holds nothing the row sees
-    l = fmaf(f, lp, l);
-    if (mine)
+  float M = -INFINITY, l = 0.f;
+  vec_t o = 0.f;
+  for (int p0 = first; p0 < n_split; p0 += 64 * kWaves) {
+    const int p = p0 + kWaves * lane;
+    const float lp = p < n_split ? part_l[p * rows + row] : 0.f;
+    const float mp = lp == 0.f ? -INFINITY : part_m[p * rows + row];  // 0: the range holds nothing the row sees
+    const float top = fmaxf(M, wave_max(mp));
+    const float ref = top == -INFINITY ? 0.f : top, down = fast_exp2(M - ref);
+    const float f = lp == 0.f ? 0.f : fast_exp2(mp - ref);
+    M = top;
+    l = l * down + wave_sum(f * lp);
+    o *= down;
+    uint64_t left = __ballot(lp != 0.f);
+    while (left) {
+      vec_t v[4];
+      float w[4];
 #pragma unroll
-      for (int e = 0; e < kE; ++e) o[e] = fmaf(f, part_o[(p * rows + row) * DH + kE * lane + e], o[e]);
+      for (int u = 0; u < 4; ++u) {  // four ranges' columns in flight
+        const int j = left ? __builtin_ctzll(left) : -1;
+        left &= left - 1;
+        w[u] = j < 0 ? 0.f : __shfl(f, j, 64);
+        v[u] = 0.f;
+        if (j >= 0 && mine)
+          v[u] = *reinterpret_cast<const vec_t*>(part_o + (size_t(p0 + kWaves * j) * rows + row) * DH + kE * lane);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o += w[u] * v[u];
+    }
   }
-  if (lane == 0) sum[wave] = l;
+  if constexpr (kWaves > 1) {
+    __shared__ float sh_m[kWaves], sh_l[kWaves], sh_o[kWaves][64 * kE];
+    if (lane == 0) {
+      sh_m[wave] = M;
+      sh_l[wave] = l;
+    }
 #pragma unroll
-  for (int e = 0; e < kE; ++e) part[wave][kE * lane + e] = o[e];
-  __syncthreads();
-  l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int e = 0; e < kE; ++e) sh_o[wave][kE * lane + e] = o[e];
+    __syncthreads();
+    if (wave != 0) return;
+    M = -INFINITY;
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sh_m[w]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    l = 0.f;
+    o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = fast_exp2(sh_m[w] - ref);
+      l = fmaf(f, sh_l[w], l);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) o[e] = fmaf(f, sh_o[w][kE * lane + e], o[e]);
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  if (threadIdx.x < DH) {
-    const int c = threadIdx.x;
-    store1(O + row * DH + c, ((part[0][c] + part[1][c]) + (part[2][c] + part[3][c])) * inv);
-  }
-  if (threadIdx.x == 0) lse[(row % Hq) * n_q + row / Hq] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
+  if (mine)
+#pragma unroll
+    for (int e = 0; e < kE; ++e) store1(O + row * DH + kE * lane + e, o[e] * inv);
+  if (lane == 0) lse[(row % Hq) * n_q + row / Hq] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
 }
 
 // acc[b][g][key] += sum over the rows of exp(s - lse), from the scores (base 2) the attention kernel has stored: a
@@ -525,29 +556,41 @@ __global__ __launch_bounds__(64) void tree_weight_mfma_kernel(const uint16_t* __
   f32x4_t sum[4];
 #pragma unroll
   for (int a = 0; a < 4; ++a) sum[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  for (int r0 = 0; r0 < R; r0 += 16) {
+  struct Rows {  // 16 rows: the lane's operand of them, and row fr's weight, normaliser and mask
+    bf16x8_t q[kNK];
+    float w, l;
+    uint64_t bits;
+  };
+  auto fetch = [&](int r0) {
+    Rows x;
     const int r = r0 + fr;
     const bool live = r < R;
     const int tok = q.q0 + (live ? r / G : 0), h = g * G + (live ? r % G : 0);
-    const float w = !live ? 0.f : row_weight ? row_weight[tok] : 1.f;
-    if (!__any(w != 0.f)) continue;
-    const float l = lse[size_t(h) * sh.n_q + tok], l2 = l * kLog2e;
-    const uint64_t bits = tree_bits(mask, q.q0, live ? r / G : 0);
-    bf16x8_t qf[kNK];
+    x.w = !live ? 0.f : row_weight ? row_weight[tok] : 1.f;
+    x.l = lse[size_t(h) * sh.n_q + tok];
+    x.bits = tree_bits(mask, q.q0, live ? r / G : 0);
 #pragma unroll
     for (int c = 0; c < kNK; ++c)
-      qf[c] = *reinterpret_cast<const bf16x8_t*>(Q + (size_t(tok) * sh.Hq + h) * DH + 32 * c + 8 * fq);
-    const bool counts = w != 0.f && l != -INFINITY;
+      x.q[c] = *reinterpret_cast<const bf16x8_t*>(Q + (size_t(tok) * sh.Hq + h) * DH + 32 * c + 8 * fq);
+    return x;
+  };
+  Rows next = fetch(0);
+  for (int r0 = 0; r0 < R; r0 += 16) {
+    const Rows now = next;
+    if (r0 + 16 < R) next = fetch(r0 + 16);  // in flight behind the products
+    const bool counts = now.w != 0.f && now.l != -INFINITY;
+    if (!__any(counts)) continue;
+    const float l2 = now.l * kLog2e;
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
       f32x4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
+      for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], now.q[c], s);
 #pragma unroll
       for (int z = 0; z < 4; ++z) {
         bool sees = counts;
-        if (edge) sees &= tree_sees(bits, k + 16 * a + 4 * fq + z - q.len);
-        sum[a][z] += sees ? w * fast_exp2(fmaf(s[z], c2, -l2)) : 0.f;
+        if (edge) sees &= tree_sees(now.bits, k + 16 * a + 4 * fq + z - q.len);
+        sum[a][z] += sees ? now.w * fast_exp2(fmaf(s[z], c2, -l2)) : 0.f;
       }
     }
   }
@@ -618,7 +661,7 @@ struct TreePlan {
 inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
   const int64_t rows = int64_t(max_q) * (Hq / Hkv), groups = int64_t(B) * Hkv;
   TreePlan p;
-  p.row_tiles = dtype == ESTP_F32 || rows <= 16 ? 1 : 2;
+  p.row_tiles = dtype == ESTP_F32 || rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   p.n_chunks = int((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
   // ranges of 256 keys, longer ones while there are many of them
   int64_t unit = 256;
@@ -683,8 +726,9 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
   const size_t groups = size_t(sh.n_split) * sh.B * sh.Hkv;
   if constexpr (sizeof(T) == 2) {
     const dim3 grid(unsigned((groups + 7) / 8 * 8 * p.n_chunks));
-    auto kernel = p.row_tiles == 2 ? tree_attn_mfma_kernel<DH, 2, false>
-                  : scores         ? tree_attn_mfma_kernel<DH, 1, true>
+    auto kernel = p.row_tiles == 4   ? tree_attn_mfma_kernel<DH, 4, false>
+                  : p.row_tiles == 2 ? tree_attn_mfma_kernel<DH, 2, false>
+                  : scores          ? tree_attn_mfma_kernel<DH, 1, true>
                                    : tree_attn_mfma_kernel<DH, 1, false>;
     kernel<<<grid, dim3(64), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, p.n_chunks, scale * kLog2e, t.scores, t.pitch, t.m,
                                      t.l, t.o);
@@ -693,8 +737,16 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
         Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
   }
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
-  tree_join_kernel<T, DH><<<dim3(unsigned(size_t(sh.n_q) * sh.Hq)), dim3(256), 0, s>>>(
-      t.m, t.l, t.o, cu_q + sh.B, sh.n_split, sh.n_q, sh.Hq, O, lse);
+  const size_t rows = size_t(sh.n_q) * sh.Hq;
+  auto join = [&](auto kernel, size_t wgs, int threads) {
+    kernel<<<dim3(unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, cu_q + sh.B, sh.n_split, sh.n_q, sh.Hq, O, lse);
+  };
+  if (sh.n_split <= 16)
+    join(tree_join_kernel<T, DH, 1>, (rows + 3) / 4, 256);
+  else if (sh.n_split <= 64)
+    join(tree_join_kernel<T, DH, 4>, rows, 256);
+  else
+    join(tree_join_kernel<T, DH, 16>, rows, 1024);
   ESTP_CHECK_LAUNCH("tree_join_kernel");
   return ESTP_OK;
 }
@@ -757,7 +809,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
                "%s: workspace must be non-null and 256-byte aligned", fn);
   const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
   ESTP_REQUIRE(fits_launch(size_t(p.n_split) * B * Hkv * p.n_chunks + 8 * size_t(p.n_chunks), 256) &&
-                   fits_launch(size_t(n_q) * Hq, 256),
+                   fits_launch(size_t(n_q) * Hq, 1024),
                ESTP_ERR_UNSUPPORTED, "%s: more workgroups than one launch holds", fn);
   const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.n_split, p.unit};
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
