@@ -13,12 +13,12 @@
 //
 // A row that sees nothing has lse -inf and O 0, and adds nothing.
 //
-// The keys of a (sequence, KV head) are cut into n_split ranges, each the work
-// of one workgroup per 16 rows, in one pass with the running maximum and sum of
-// the softmax (base 2); tree_join_kernel joins the ranges' partial results.
-// tree_weight_kernel then forms the scores again, per 64 keys over all rows,
-// since the weights need the rows' normalisers.  No atomics: bitwise
-// reproducible.
+// An item is one (sequence, KV head) and up to 16, 32 rows of it; its keys come in chunks.  All chunks of all items
+// form one line, cut into equal shares, one for each workgroup of a grid that fills the chip once: lengths may differ
+// as they like, and no workgroup is empty.  A share's piece of an item is a segment, worked off in one pass with the
+// running maximum and sum of the softmax (base 2); tree_join_kernel joins an item's segments.  The account takes the
+// rows' normalisers, so it comes last: from scores that the first kernel kept where the rows are few, else from
+// scores formed again.  No atomics: bitwise reproducible.
 #include <algorithm>
 #include <cmath>
 
@@ -33,7 +33,8 @@ constexpr int kTRows = 16;    // rows of a workgroup
 constexpr int kTKeys = 64;    // keys of a tile
 
 struct TreeShape {
-  int B, max_q, n_q, Hq, Hkv, cap, max_kv, n_split, unit;  // n_split ranges of `unit` keys
+  int B, max_q, n_q, Hq, Hkv, cap, max_kv;
+  int item_rows, items;  // rows of an item; items of a (sequence, KV head) at most
 };
 
 // One sequence as the kernels see it: counts out of range (invalid input) never become an access out of range.
@@ -55,6 +56,111 @@ __device__ __forceinline__ uint64_t tree_bits(const int64_t* mask, int q0, int t
 // Whether a row with mask `bits` sees the key `rel` places past the cached ones.
 __device__ __forceinline__ bool tree_sees(uint64_t bits, int rel) {
   return rel < 0 || (rel < kMaxTree && ((bits >> (rel & 63)) & 1));
+}
+
+// ------------------------------------------------------------------ the line of chunks
+
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
+  return uint32_t(__builtin_amdgcn_readlane(int(v), lane));
+}
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t y = __shfl_up(v, o, 64);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+// 64 sequences, one a lane: counts, and how many chunks of kChunk keys their items have in all.
+template <int kChunk>
+struct TreeBatch {
+  int b0, q0, T, len, keys;
+  uint32_t w, upto;  // chunks of the lane's sequence; of the batch's up to and with it
+  __device__ __forceinline__ void fetch(const TreeShape& sh, const int* lens, const int* cu_q, int first) {
+    b0 = first;
+    const int b = first + int(threadIdx.x & 63);
+    TreeSeq q{0, 0, 0, 0};
+    if (b < sh.B) q = tree_seq(sh, lens, cu_q, b);
+    q0 = q.q0;
+    T = q.T;
+    len = q.len;
+    keys = q.keys;
+    w = uint32_t(sh.Hkv) * items(sh, q.T) * chunks(q.keys);
+    upto = wave_prefix(w);
+  }
+  __device__ static __forceinline__ uint32_t items(const TreeShape& sh, int T) {  // of a KV head
+    return uint32_t(T * (sh.Hq / sh.Hkv) + sh.item_rows - 1) / uint32_t(sh.item_rows);
+  }
+  __device__ static __forceinline__ uint32_t chunks(int keys) { return uint32_t(keys + kChunk - 1) / kChunk; }
+  __device__ __forceinline__ uint32_t all() const { return lane_of(upto, 63); }
+};
+// Chunks of one share: at least 128 keys, so that joins stay few.
+template <int kChunk>
+__device__ __forceinline__ uint32_t tree_share(uint32_t total, int wgs) {
+  return max(uint32_t(128 / kChunk), (total + uint32_t(wgs) - 1) / uint32_t(wgs));
+}
+template <int kChunk>
+__device__ __forceinline__ uint32_t tree_total(const TreeShape& sh, const int* lens, const int* cu_q,
+                                               TreeBatch<kChunk>& first) {
+  first.fetch(sh, lens, cu_q, 0);
+  uint32_t total = first.all();
+  for (int b0 = 64; b0 < sh.B; b0 += 64) {
+    TreeBatch<kChunk> t;
+    t.fetch(sh, lens, cu_q, b0);
+    total += t.all();
+  }
+  return total;
+}
+// A segment: rows r0 .. of KV head g of sequence b, keys [k0, k1), its partial result's place.
+struct TreeSegment {
+  int b, g, r0, q0, T, len, keys, k0, k1, slot;
+};
+// Calls f with the segments of this workgroup's share in turn; all values are uniform.
+template <int kChunk, typename F>
+__device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, const int* cu_q, int wg, int wgs,
+                                          F&& f) {
+  TreeBatch<kChunk> t;
+  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  if (uint64_t(wg) * share >= total) return;
+  uint32_t at = uint32_t(wg) * share;
+  const uint32_t end = min(total, at + share);
+  uint32_t off = 0;  // of the batch, then of the sequence
+  while (off + t.all() <= at) {
+    off += t.all();
+    t.fetch(sh, lens, cu_q, t.b0 + 64);
+  }
+  int j = __builtin_ctzll(__ballot(off + t.upto > at));
+  off += lane_of(t.upto, j) - lane_of(t.w, j);
+  while (true) {
+    TreeSegment s;
+    s.b = t.b0 + j;
+    s.q0 = int(lane_of(uint32_t(t.q0), j));
+    s.T = int(lane_of(uint32_t(t.T), j));
+    s.len = int(lane_of(uint32_t(t.len), j));
+    s.keys = int(lane_of(uint32_t(t.keys), j));
+    const uint32_t n = TreeBatch<kChunk>::chunks(s.keys), items = TreeBatch<kChunk>::items(sh, s.T);
+    const uint32_t item = (at - off) / n, c0 = at - off - item * n, c1 = min(n, c0 + (end - at));
+    s.g = __builtin_amdgcn_readfirstlane(int(item / items));
+    const int part = __builtin_amdgcn_readfirstlane(int(item % items));
+    s.r0 = part * sh.item_rows;
+    s.k0 = __builtin_amdgcn_readfirstlane(int(c0) * kChunk);
+    s.k1 = __builtin_amdgcn_readfirstlane(min(s.keys, int(c1) * kChunk));
+    s.slot = wg + (s.b * sh.Hkv + s.g) * sh.items + part;  // grows from segment to segment
+    f(s);
+    at += c1 - c0;
+    if (at >= end) return;
+    if (at - off >= lane_of(t.w, j)) {
+      off += lane_of(t.w, j);
+      do {
+        if (++j == 64) {
+          t.fetch(sh, lens, cu_q, t.b0 + 64);
+          j = 0;
+        }
+      } while (lane_of(t.w, j) == 0);
+    }
+  }
 }
 
 template <typename T>
@@ -90,13 +196,13 @@ __device__ __forceinline__ void stage_rows(const T* src, int n, int live, float*
 }
 // the 16 query rows from r0 of a KV head's T G rows
 template <typename T, int DH, int P>
-__device__ __forceinline__ void stage_queries(const T* Q, const TreeShape& sh, const TreeSeq& q, int g, int r0, int R,
+__device__ __forceinline__ void stage_queries(const T* Q, const TreeShape& sh, const TreeSegment& q, int R,
                                               float* lds) {
   const int G = sh.Hq / sh.Hkv;
   for (int i = threadIdx.x; i < kTRows * (DH / 4); i += 256) {
-    const int r = r0 + i / (DH / 4), c = 4 * (i % (DH / 4));
+    const int r = q.r0 + i / (DH / 4), c = 4 * (i % (DH / 4));
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < R) load4<T>(Q + (size_t(q.q0 + r / G) * sh.Hq + g * G + r % G) * DH + c, v);
+    if (r < R) load4<T>(Q + (size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * DH + c, v);
     *reinterpret_cast<f32x4_t*>(lds + (i / (DH / 4)) * P + c) = f32x4_t{v[0], v[1], v[2], v[3]};
   }
 }
@@ -116,7 +222,7 @@ __device__ __forceinline__ void scores4(const float* qs, const float* ks, int rr
   }
 }
 
-// Vector-unit kernel.  Thread (rr, c) = (tid / 16, tid % 16) forms row rr's scores of keys c, 16 + c, 32 + c,
+// Vector-unit kernel (fp32).  Thread (rr, c) = (tid / 16, tid % 16) forms row rr's scores of keys c, 16 + c, 32 + c,
 // 48 + c of a tile and its output columns c DH / 16 ...
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q, const T* __restrict__ K,
@@ -127,71 +233,69 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
                                                         float* __restrict__ part_o) {
   constexpr int P = DH + 4, PP = kTKeys + 4, NC = DH / 16;
   __shared__ __attribute__((aligned(16))) float qs[kTRows * P], ks[kTKeys * P], vs[kTKeys * P], ps[kTRows * PP];
-  const int split = blockIdx.x % sh.n_split, bg = blockIdx.x / sh.n_split, b = bg / sh.Hkv, g = bg % sh.Hkv;
-  const int G = sh.Hq / sh.Hkv, r0 = blockIdx.y * kTRows;
-  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
-  const int R = q.T * G;
-  if (r0 >= R) return;
-  const int k0 = min(int64_t(q.keys), int64_t(split) * sh.unit), k1 = min(q.keys, k0 + sh.unit);
-  const int tid = threadIdx.x, rr = tid >> 4, c = tid & 15, r = r0 + rr;
-  const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
-  const T* Kb = K + size_t(bg) * sh.cap * DH;
-  const T* Vb = V + size_t(bg) * sh.cap * DH;
-  stage_queries<T, DH, P>(Q, sh, q, g, r0, R, qs);
-  float m = -INFINITY, l = 0.f, o[NC];
+  const int G = sh.Hq / sh.Hkv, tid = threadIdx.x, rr = tid >> 4, c = tid & 15;
+  tree_walk<kTKeys>(sh, lens, cu_q, blockIdx.x, gridDim.x, [&](const TreeSegment& q) {
+    const int R = q.T * G, r = q.r0 + rr;
+    const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
+    const size_t rows = size_t(q.b * sh.Hkv + q.g) * sh.cap;
+    const T *Kb = K + rows * DH, *Vb = V + rows * DH;
+    __syncthreads();  // the last segment's rows are read
+    stage_queries<T, DH, P>(Q, sh, q, R, qs);
+    float m = -INFINITY, l = 0.f, o[NC];
 #pragma unroll
-  for (int e = 0; e < NC; ++e) o[e] = 0.f;
-  for (int k = k0; k < k1; k += kTKeys) {
-    __syncthreads();
-    stage_rows<T, DH, P>(Kb + size_t(k) * DH, kTKeys, k1 - k, ks);
-    stage_rows<T, DH, P>(Vb + size_t(k) * DH, kTKeys, k1 - k, vs);
-    __syncthreads();
-    float s[4], mx = m;
-    scores4<DH, P>(qs, ks, rr, c, s);
+    for (int e = 0; e < NC; ++e) o[e] = 0.f;
+    for (int k = q.k0; k < q.k1; k += kTKeys) {
+      __syncthreads();
+      stage_rows<T, DH, P>(Kb + size_t(k) * DH, kTKeys, q.k1 - k, ks);
+      stage_rows<T, DH, P>(Vb + size_t(k) * DH, kTKeys, q.k1 - k, vs);
+      __syncthreads();
+      float s[4], mx = m;
+      scores4<DH, P>(qs, ks, rr, c, s);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int key = k + 16 * j + c;
-      s[j] = key < k1 && tree_sees(bits, key - q.len) ? s[j] * c2 : -INFINITY;
-      mx = fmaxf(mx, s[j]);
+      for (int j = 0; j < 4; ++j) {
+        const int key = k + 16 * j + c;
+        s[j] = key < q.k1 && tree_sees(bits, key - q.len) ? s[j] * c2 : -INFINITY;
+        mx = fmaxf(mx, s[j]);
+      }
+#pragma unroll
+      for (int x = 1; x < 16; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+      const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: all weights are 0
+      const float f = fast_exp2(m - ref);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = fast_exp2(s[j] - ref);
+        ps[rr * PP + 16 * j + c] = p;
+        sum += p;
+      }
+#pragma unroll
+      for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x, 64);
+      l = l * f + sum;
+      m = mx;
+#pragma unroll
+      for (int e = 0; e < NC; ++e) o[e] *= f;
+      __syncthreads();
+      const int n = min(kTKeys, q.k1 - k), rel = k - q.len;
+      for (int j = 0; j < n; ++j) {
+        // a drafted token the row does not see adds nothing, whatever its values are
+        if (rel + j >= 0 && !tree_sees(bits, rel + j)) continue;
+        const float p = ps[rr * PP + j];
+#pragma unroll
+        for (int e = 0; e < NC; ++e) o[e] = fmaf(p, vs[j * P + c * NC + e], o[e]);
+      }
+    }
+    if (r >= R) return;
+    const size_t row = size_t(q.slot) * kTRows + rr;
+    if (c == 0) {
+      part_m[row] = m;
+      part_l[row] = l;
     }
 #pragma unroll
-    for (int x = 1; x < 16; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: all weights are 0
-    const float f = fast_exp2(m - ref);
-    float sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float p = fast_exp2(s[j] - ref);
-      ps[rr * PP + 16 * j + c] = p;
-      sum += p;
-    }
-#pragma unroll
-    for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x, 64);
-    l = l * f + sum;
-    m = mx;
-#pragma unroll
-    for (int e = 0; e < NC; ++e) o[e] *= f;
-    __syncthreads();
-    const int n = min(kTKeys, k1 - k), rel = k - q.len;
-    for (int j = 0; j < n; ++j) {
-      // a drafted token the row does not see adds nothing, whatever its values are
-      if (rel + j >= 0 && !tree_sees(bits, rel + j)) continue;
-      const float p = ps[rr * PP + j];
-#pragma unroll
-      for (int e = 0; e < NC; ++e) o[e] = fmaf(p, vs[j * P + c * NC + e], o[e]);
-    }
-  }
-  if (r >= R) return;
-  const size_t row = size_t(split) * sh.n_q * sh.Hq + size_t(q.q0 + r / G) * sh.Hq + g * G + r % G;
-  if (c == 0) {
-    part_m[row] = m;
-    part_l[row] = l;
-  }
-#pragma unroll
-  for (int e = 0; e < NC; ++e) part_o[row * DH + c * NC + e] = o[e];
+    for (int e = 0; e < NC; ++e) part_o[row * DH + c * NC + e] = o[e];
+  });
 }
 
-// Matrix-core kernel (bf16): one wave per workgroup, 16 NRT rows, `unit` keys in chunks of 32.
+// Matrix-core kernel (bf16): one wave per workgroup, items of 16 NRT rows, chunks of 32 keys.
 //
 // S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of the chunk's two 16-key blocks, keys
 // 4 fq .. 4 fq + 3 each (fq = lane / 16).  These 8 weights are at once the lane's part of the second product's
@@ -208,27 +312,29 @@ template <int DH, int NRT, bool kScores>
 __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     const int* __restrict__ lens, const int* __restrict__ cu_q, const int64_t* __restrict__ mask, TreeShape sh,
-    int n_chunks, float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m,
-    float* __restrict__ part_l, float* __restrict__ part_o) {
+    float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m, float* __restrict__ part_l,
+    float* __restrict__ part_o) {
   constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
   constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
   constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
-  constexpr int kQSlot = NRT == 4 ? kSlots - 2 : kSlots - 1;
   __shared__ __attribute__((aligned(16))) char lds[kSlots * kPart];
-  // row chunks of the same keys next to each other on one XCD
-  const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3, r0 = at % n_chunks * 16 * NRT, x = at / n_chunks * 8 + xcd;
-  if (x >= sh.n_split * sh.B * sh.Hkv) return;  // the grid is rounded up
-  const int bg = __builtin_amdgcn_readfirstlane(x / sh.n_split), split = x - bg * sh.n_split;
-  const int b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
-  TreeSeq q = tree_seq(sh, lens, cu_q, b);
-  q.len = __builtin_amdgcn_readfirstlane(q.len);
-  q.keys = __builtin_amdgcn_readfirstlane(q.keys);
-  const int R = q.T * G;
-  if (r0 >= R) return;
-  const int k0 = __builtin_amdgcn_readfirstlane(int(min(int64_t(q.keys), int64_t(split) * sh.unit)));
-  const int k1 = __builtin_amdgcn_readfirstlane(min(q.keys, k0 + sh.unit));
-  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4;
-
+  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4, G = sh.Hq / sh.Hkv;
+  uint32_t off_k[kL], off_v[kL];
+#pragma unroll
+  for (int i = 0; i < kL; ++i) {
+    const int piece = 64 * i + lane, row = piece / kPieces, c = piece % kPieces;
+    off_k[i] = uint32_t(row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16);
+    off_v[i] = uint32_t(row * kRow + (c ^ (2 * (row / kWindow & (kPieces / 2 - 1)))) * 16);
+  }
+  auto read_k = [&](int at_slot, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
+    return *reinterpret_cast<const bf16x8_t*>(lds + at_slot * kPart + row * kRow +
+                                              ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
+  };
+  auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
+  // neighbouring shares, whose items have keys in common, on one XCD (the grid is a multiple of 8)
+  const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  tree_walk<kC>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
+  const int bg = q.b * sh.Hkv + q.g, g = q.g, r0 = q.r0, k0 = q.k0, k1 = q.k1, R = q.T * G;
   float m[NRT], l[NRT];
   f32x4_t o[NRT][kND];
 #pragma unroll
@@ -238,21 +344,9 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
 #pragma unroll
     for (int d = 0; d < kND; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  if (k0 < k1) {
+  {
     const char* Kb = reinterpret_cast<const char*>(K) + size_t(bg) * sh.cap * kRow;
     const char* Vb = reinterpret_cast<const char*>(V) + size_t(bg) * sh.cap * kRow;
-    uint32_t off_k[kL], off_v[kL];
-#pragma unroll
-    for (int i = 0; i < kL; ++i) {
-      const int piece = 64 * i + lane, row = piece / kPieces, c = piece % kPieces;
-      off_k[i] = uint32_t(row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16);
-      off_v[i] = uint32_t(row * kRow + (c ^ (2 * (row / kWindow & (kPieces / 2 - 1)))) * 16);
-    }
-    auto read_k = [&](int at_slot, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
-      return *reinterpret_cast<const bf16x8_t*>(lds + at_slot * kPart + row * kRow +
-                                                ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
-    };
-    auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
     int pf_key = k0, pf_slot = 0;
     auto issue = [&](const char* base, const uint32_t (&off)[kL]) {  // past the range: an empty resource, no access
       const int left = min(kC, q.keys - pf_key);
@@ -267,8 +361,8 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
       const int r = r0 + 16 * t + fr;
       bits[t] = r < R ? tree_bits(mask, q.q0, r / G) : 0;
     }
-    // the rows of Q come first, through the ring's last slot (the last two) and laid out as K parts: a load of their
-    // own would wait for every transfer issued around it
+    // the rows of Q come first, through the ring's last slot and laid out as a K part: a load of their own would
+    // wait for every transfer issued around it
     {
       const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
                                     uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
@@ -277,23 +371,22 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
         const int row = (64 * i + lane) / kPieces, r = r0 + row;
         const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (row / kWindow & (kPieces - 1))) * 16u;
         dma16(rq, r < R ? (uint32_t(r / G) * uint32_t(sh.Hq) + uint32_t(g * G + r % G)) * kRow + piece : kPastEnd, 0,
-              lds + kQSlot * kPart + 1024 * i);
+              lds + (kSlots - 1) * kPart + 1024 * i);
       }
     }
     issue(Kb, off_k);
     issue(Vb, off_v);
     pf_key += kC;
     issue(Kb, off_k);
-    if (NRT < 4) issue(Vb, off_v);
-    arrived<(NRT < 4 ? 4 : 3) * kL>();
+    issue(Vb, off_v);
+    pf_key += kC;
+    arrived<(kSlots - 1) * kL>();
     bf16x8_t qf[NRT][kNK];
 #pragma unroll
     for (int t = 0; t < NRT; ++t)
 #pragma unroll
-      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kQSlot, 16 * t + fr, c);
+      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kSlots - 1, 16 * t + fr, c);
     lds_read_done();
-    if (NRT == 4) issue(Vb, off_v);
-    pf_key += kC;
     issue(Kb, off_k);
     int slot = 0;
     for (int k = k0; k < k1; k += kC) {
@@ -410,7 +503,7 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
 #pragma unroll
         for (int d = 0; d < kND; ++d) o[t][d] = mfma_bf16(vf[d], pf[t], o[t][d]);
     }
-    wait_vm<0>();  // no transfer into LDS outlives the workgroup
+    arrived<0>();  // no transfer into LDS outlives the segment
   }
 #pragma unroll
   for (int t = 0; t < NRT; ++t) {
@@ -418,37 +511,60 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
     l[t] += __shfl_xor(l[t], 16, 64);
     l[t] += __shfl_xor(l[t], 32, 64);
     if (r >= R) continue;
-    const size_t row = size_t(split) * sh.n_q * sh.Hq + size_t(q.q0 + r / G) * sh.Hq + g * G + r % G;
+    const size_t row = size_t(q.slot) * (16 * NRT) + 16 * t + fr;
     if (fq == 0) {
       part_m[row] = m[t];
       part_l[row] = l[t];
     }
-    if (k0 < k1)
 #pragma unroll
-      for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[t][d];
+    for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[t][d];
   }
+  });
 }
 
-// Joins the ranges' partial results of each row.  kWaves waves share a row and take every kWaves-th range; a lane
-// fetches the state of one range, 64 at a time, and DH / 64 (at least one) columns of those ranges that hold
+// Joins the partial results of each row's segments.  kWaves waves share a row and take every kWaves-th segment; a
+// lane fetches the state of one segment, 64 at a time, and DH / 64 (at least one) columns of those that hold
 // something.  Rows past the last sequence's are left as they are.
-template <typename T, int DH, int kWaves>
+template <typename T, int DH, int kWaves, int kChunk>
 __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_kernel(
     const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
-    const int* __restrict__ q_end, int n_split, int n_q, int Hq, T* __restrict__ O, float* __restrict__ lse) {
+    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
+    float* __restrict__ lse) {
   constexpr int kE = DH >= 64 ? DH / 64 : 1;
   typedef float vec_t __attribute__((ext_vector_type(kE)));
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows = int64_t(n_q) * Hq, row = kWaves == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
+  const int64_t rows = int64_t(sh.n_q) * sh.Hq, row = kWaves == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
   const int first = kWaves == 1 ? 0 : wave;
-  if (row >= rows || row / Hq >= q_end[0]) return;
+  const int tok = int(row / sh.Hq), h = int(row % sh.Hq), G = sh.Hq / sh.Hkv;
+  if (row >= rows || tok >= cu_q[sh.B]) return;
+  // the row's sequence, item and segments
+  TreeBatch<kChunk> t;
+  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  uint32_t off = 0;
+  uint64_t here;
+  while (!(here = __ballot(tok >= t.q0 && tok < t.q0 + t.T)) && t.b0 + 64 < sh.B) {
+    off += t.all();
+    t.fetch(sh, lens, cu_q, t.b0 + 64);
+  }
+  if (!here) return;  // counts out of range (invalid input)
+  const int j = __builtin_ctzll(here);
+  off += lane_of(t.upto, j) - lane_of(t.w, j);
+  const int r = (tok - int(lane_of(uint32_t(t.q0), j))) * G + h % G, part = r / sh.item_rows, g = h / G;
+  const uint32_t n = TreeBatch<kChunk>::chunks(int(lane_of(uint32_t(t.keys), j)));
+  const uint32_t items = TreeBatch<kChunk>::items(sh, int(lane_of(uint32_t(t.T), j)));
+  off += (uint32_t(g) * items + uint32_t(part)) * n;
+  const uint32_t wg0 = off / share;
+  const int n_seg = n > 0 ? int((off + n - 1) / share - wg0) + 1 : 0;
+  const size_t row0 = (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) * sh.item_rows +
+                      (r - part * sh.item_rows);
   const bool mine = kE * lane < DH;
   float M = -INFINITY, l = 0.f;
   vec_t o = 0.f;
-  for (int p0 = first; p0 < n_split; p0 += 64 * kWaves) {
+  for (int p0 = first; p0 < n_seg; p0 += 64 * kWaves) {
     const int p = p0 + kWaves * lane;
-    const float lp = p < n_split ? part_l[p * rows + row] : 0.f;
-    const float mp = lp == 0.f ? -INFINITY : part_m[p * rows + row];  // 0: the range holds nothing the row sees
+    const size_t at = row0 + size_t(p) * sh.item_rows;
+    const float lp = p < n_seg ? part_l[at] : 0.f;
+    const float mp = lp == 0.f ? -INFINITY : part_m[at];  // 0: the segment holds nothing the row sees
     const float top = fmaxf(M, wave_max(mp));
     const float ref = top == -INFINITY ? 0.f : top, down = fast_exp2(M - ref);
     const float f = lp == 0.f ? 0.f : fast_exp2(mp - ref);
@@ -460,13 +576,13 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
       vec_t v[4];
       float w[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {  // four ranges' columns in flight
-        const int j = left ? __builtin_ctzll(left) : -1;
+      for (int u = 0; u < 4; ++u) {  // four segments' columns in flight
+        const int x = left ? __builtin_ctzll(left) : -1;
         left &= left - 1;
-        w[u] = j < 0 ? 0.f : __shfl(f, j, 64);
+        w[u] = x < 0 ? 0.f : __shfl(f, x, 64);
         v[u] = 0.f;
-        if (j >= 0 && mine)
-          v[u] = *reinterpret_cast<const vec_t*>(part_o + (size_t(p0 + kWaves * j) * rows + row) * DH + kE * lane);
+        if (x >= 0 && mine)
+          v[u] = *reinterpret_cast<const vec_t*>(part_o + (row0 + size_t(p0 + kWaves * x) * sh.item_rows) * DH + kE * lane);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) o += w[u] * v[u];
@@ -499,7 +615,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
   if (mine)
 #pragma unroll
     for (int e = 0; e < kE; ++e) store1(O + row * DH + kE * lane + e, o[e] * inv);
-  if (lane == 0) lse[(row % Hq) * n_q + row / Hq] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
+  if (lane == 0) lse[size_t(h) * sh.n_q + tok] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
 }
 
 // acc[b][g][key] += sum over the rows of exp(s - lse), from the scores (base 2) the attention kernel has stored: a
@@ -630,7 +746,11 @@ __global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ 
   float sum = 0.f;
   for (int r0 = 0; r0 < R; r0 += kTRows) {
     __syncthreads();
-    stage_queries<T, DH, P>(Q, sh, q, g, r0, R, qs);
+    TreeSegment seg{};
+    seg.g = g;
+    seg.r0 = r0;
+    seg.q0 = q.q0;
+    stage_queries<T, DH, P>(Q, sh, seg, R, qs);
     __syncthreads();
     const int r = r0 + rr;
     const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
@@ -653,22 +773,23 @@ __global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ 
 
 // ------------------------------------------------------------------ plan and workspace
 
-// How a call is cut: n_split ranges of `unit` keys of every (sequence, KV head), n_chunks of its rows.
+// How a call is cut: items of item_rows rows, at most `items` of them a (sequence, KV head), their chunks shared by
+// `wgs` workgroups.
 struct TreePlan {
-  int n_split, unit, n_chunks, row_tiles;
+  int item_rows, items, wgs;
   bool stored;  // the scores are kept for the account
 };
 inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
-  const int64_t rows = int64_t(max_q) * (Hq / Hkv), groups = int64_t(B) * Hkv;
+  const int64_t rows = int64_t(max_q) * (Hq / Hkv);
   TreePlan p;
-  p.row_tiles = dtype == ESTP_F32 || rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  p.n_chunks = int((rows + 16 * p.row_tiles - 1) / (16 * p.row_tiles));
-  // ranges of 256 keys, longer ones while there are many of them
-  int64_t unit = 256;
-  while (unit < max_kv && groups * p.n_chunks * ((max_kv + unit - 1) / unit) > 8192) unit *= 2;
-  p.unit = int(unit);
-  p.n_split = int((max_kv + unit - 1) / unit);
-  p.stored = dtype == ESTP_BF16 && p.n_chunks == 1 && p.row_tiles == 1 && rows * 4 <= dh;
+  p.item_rows = dtype == ESTP_F32 || rows <= 16 ? 16 : 32;
+  p.items = int((rows + p.item_rows - 1) / p.item_rows);
+  // one grid fills the chip: what 160 KB of LDS hold of the rings (fp32: two workgroups of 4 waves) on 256 units
+  const int64_t fill = dtype == ESTP_F32 ? 512 : 1024 * (128 / dh);
+  const int64_t shares = (int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) + 3) / 4;  // at most
+  p.wgs = int((std::min(fill, shares) + 7) / 8 * 8);
+  // Scores: 8 bytes a row and key, written and read, against 2 dh for forming them again.
+  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.item_rows == 16 && rows * 4 <= dh;
   return p;
 }
 
@@ -678,13 +799,14 @@ struct TreeBuffers {
   size_t bytes;
 };
 inline TreeBuffers carve_tree(const TreePlan& p, int B, int64_t n_q, int Hq, int Hkv, int max_kv, int dh, void* ws) {
-  const size_t rows = size_t(n_q) * Hq;
+  // a segment more than the last for every workgroup and for every item
+  const size_t rows = (size_t(p.wgs) + size_t(B) * Hkv * p.items) * p.item_rows;
   Carver c(ws);
   TreeBuffers t;
-  t.m = c.take<float>(p.n_split * rows);
-  t.l = c.take<float>(p.n_split * rows);
-  t.o = c.take<float>(p.n_split * rows * dh);
-  t.lse = c.take<float>(rows);
+  t.m = c.take<float>(rows);
+  t.l = c.take<float>(rows);
+  t.o = c.take<float>(rows * dh);
+  t.lse = c.take<float>(size_t(n_q) * Hq);
   t.pitch = (max_kv + 31) / 32 * 32;
   t.scores = c.take<float>(p.stored ? size_t(B) * Hkv * 16 * t.pitch : 0);
   t.bytes = c.bytes();
@@ -723,30 +845,29 @@ template <typename T, int DH>
 int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* cu_q, const int64_t* mask,
                 const TreeShape& sh, const TreePlan& p, bool scores, float scale, T* O, float* lse,
                 const TreeBuffers& t, hipStream_t s) {
-  const size_t groups = size_t(sh.n_split) * sh.B * sh.Hkv;
+  const dim3 grid{unsigned(p.wgs)};
+  constexpr int kChunk = sizeof(T) == 2 ? 32 : kTKeys;
   if constexpr (sizeof(T) == 2) {
-    const dim3 grid(unsigned((groups + 7) / 8 * 8 * p.n_chunks));
-    auto kernel = p.row_tiles == 4   ? tree_attn_mfma_kernel<DH, 4, false>
-                  : p.row_tiles == 2 ? tree_attn_mfma_kernel<DH, 2, false>
+    auto kernel = p.item_rows == 32 ? tree_attn_mfma_kernel<DH, 2, false>
                   : scores          ? tree_attn_mfma_kernel<DH, 1, true>
-                                   : tree_attn_mfma_kernel<DH, 1, false>;
-    kernel<<<grid, dim3(64), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, p.n_chunks, scale * kLog2e, t.scores, t.pitch, t.m,
-                                     t.l, t.o);
+                                    : tree_attn_mfma_kernel<DH, 1, false>;
+    kernel<<<grid, dim3(64), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
   } else {
-    tree_attn_kernel<T, DH><<<dim3(unsigned(groups), unsigned(p.n_chunks)), dim3(256), 0, s>>>(
-        Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
+    tree_attn_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
   }
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
   const size_t rows = size_t(sh.n_q) * sh.Hq;
   auto join = [&](auto kernel, size_t wgs, int threads) {
-    kernel<<<dim3(unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, cu_q + sh.B, sh.n_split, sh.n_q, sh.Hq, O, lse);
+    kernel<<<dim3(unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
   };
-  if (sh.n_split <= 16)
-    join(tree_join_kernel<T, DH, 1>, (rows + 3) / 4, 256);
-  else if (sh.n_split <= 64)
-    join(tree_join_kernel<T, DH, 4>, rows, 256);
+  // segments of an item, about: waves of a row
+  const int64_t segs = std::min<int64_t>(int64_t(p.wgs) / (int64_t(sh.B) * sh.Hkv * p.items), sh.max_kv / 128) + 2;
+  if (segs <= 16)
+    join(tree_join_kernel<T, DH, 1, kChunk>, (rows + 3) / 4, 256);
+  else if (segs <= 64)
+    join(tree_join_kernel<T, DH, 4, kChunk>, rows, 256);
   else
-    join(tree_join_kernel<T, DH, 16>, rows, 1024);
+    join(tree_join_kernel<T, DH, 16, kChunk>, rows, 1024);
   ESTP_CHECK_LAUNCH("tree_join_kernel");
   return ESTP_OK;
 }
@@ -808,10 +929,10 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
   const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
-  ESTP_REQUIRE(fits_launch(size_t(p.n_split) * B * Hkv * p.n_chunks + 8 * size_t(p.n_chunks), 256) &&
-                   fits_launch(size_t(n_q) * Hq, 1024),
-               ESTP_ERR_UNSUPPORTED, "%s: more workgroups than one launch holds", fn);
-  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.n_split, p.unit};
+  ESTP_REQUIRE(fits_launch(size_t(n_q) * Hq, 1024) &&
+                   int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX,
+               ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
+  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.item_rows, p.items};
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   float* row_lse = lse ? lse : t.lse;
@@ -844,7 +965,7 @@ extern "C" int estp_tree_importance(const void* Q, const void* K, const float* l
   ESTP_REQUIRE(lse && acc, ESTP_ERR_INVALID_ARG, "%s: lse and acc must be non-null", fn);
   ESTP_REQUIRE(aligned(tree_mask, 8) && aligned(lse, 4) && aligned(acc, 4) && aligned(row_weight, 4),
                ESTP_ERR_INVALID_ARG, "%s: tree_mask must be 8-byte, lse, row_weight and acc 4-byte aligned", fn);
-  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, 1, max_kv};
+  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, 16, 1};
   return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
     using T = decltype(element);
     return launch_weight<T, decltype(size)::value>(static_cast<const T*>(Q), static_cast<const T*>(K), lse, lens, cu_q,
