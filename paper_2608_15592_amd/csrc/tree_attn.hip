@@ -643,87 +643,116 @@ __global__ __launch_bounds__(256) void tree_weight_stored_kernel(const float* __
     if (k + e < q.keys) a[e] += sum[e];
 }
 
-// The same with the scores formed again on the matrix cores (bf16): a wave per 64 keys, whose K stays in registers
-// while the rows pass, 16 at a time; sums over the rows of a product's columns join at the end.
+// The same with the scores formed again on the matrix cores (bf16).  An item's rows wait in LDS, 128 at a time, with
+// their weights, normalisers and masks; a workgroup's share of 32-key tiles goes to its four waves in turn, a tile's
+// K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's columns are rows: their
+// sums join at the end of a tile, each exchange halving the values a lane still holds.
+constexpr int kWRows = 128;  // rows in LDS
+constexpr int kWKeys = 32;   // keys of a tile
+constexpr int kWWgs = 1024;  // workgroups: four on a compute unit
 template <int DH>
-__global__ __launch_bounds__(64) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
-                                                              const uint16_t* __restrict__ K,
-                                                              const float* __restrict__ lse,
-                                                              const int* __restrict__ lens,
-                                                              const int* __restrict__ cu_q,
-                                                              const int64_t* __restrict__ mask,
-                                                              const float* __restrict__ row_weight, TreeShape sh,
-                                                              float c2, float* __restrict__ acc) {
-  constexpr int kNK = DH / 32;
-  const int bg = blockIdx.x % (sh.B * sh.Hkv), b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
-  const int k = blockIdx.x / (sh.B * sh.Hkv) * kTKeys;
-  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
-  const int R = q.T * G, lane = threadIdx.x, fr = lane & 15, fq = lane >> 4;
-  if (k >= q.keys || R == 0) return;
-  const bool edge = k + kTKeys > q.len;
-  bf16x8_t kf[4][kNK];
-#pragma unroll
-  for (int a = 0; a < 4; ++a) {
-    const int key = min(k + 16 * a + fr, q.keys - 1);
-#pragma unroll
-    for (int c = 0; c < kNK; ++c)
-      kf[a][c] = *reinterpret_cast<const bf16x8_t*>(K + (size_t(bg) * sh.cap + key) * DH + 32 * c + 8 * fq);
-  }
-  f32x4_t sum[4];
-#pragma unroll
-  for (int a = 0; a < 4; ++a) sum[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  struct Rows {  // 16 rows: the lane's operand of them, and row fr's weight, normaliser and mask
-    bf16x8_t q[kNK];
-    float w, l;
+__global__ __launch_bounds__(256, 4) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
+                                                                  const uint16_t* __restrict__ K,
+                                                                  const float* __restrict__ lse,
+                                                                  const int* __restrict__ lens,
+                                                                  const int* __restrict__ cu_q,
+                                                                  const int64_t* __restrict__ mask,
+                                                                  const float* __restrict__ row_weight, TreeShape sh,
+                                                                  float c2, float* __restrict__ acc) {
+  constexpr int kNK = DH / 32, kRow = DH * 2, kPieces = DH / 8, kWindow = 16 / kPieces;
+  struct RowInfo {  // of weight 0: not used
+    float w, l2;
     uint64_t bits;
   };
-  auto fetch = [&](int r0) {
-    Rows x;
-    const int r = r0 + fr;
-    const bool live = r < R;
-    const int tok = q.q0 + (live ? r / G : 0), h = g * G + (live ? r % G : 0);
-    x.w = !live ? 0.f : row_weight ? row_weight[tok] : 1.f;
-    x.l = lse[size_t(h) * sh.n_q + tok];
-    x.bits = tree_bits(mask, q.q0, live ? r / G : 0);
+  __shared__ __attribute__((aligned(16))) char qs[kWRows * kRow];
+  __shared__ __attribute__((aligned(16))) RowInfo info[kWRows];
+  const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.Hq / sh.Hkv;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  tree_walk<kWKeys>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
+    const int R = q.T * G;
+    const size_t at = size_t(q.b * sh.Hkv + q.g) * sh.cap;
+    auto load_k = [&](bf16x8_t(&kf)[2][kNK], int k) {
 #pragma unroll
-    for (int c = 0; c < kNK; ++c)
-      x.q[c] = *reinterpret_cast<const bf16x8_t*>(Q + (size_t(tok) * sh.Hq + h) * DH + 32 * c + 8 * fq);
-    return x;
-  };
-  Rows next = fetch(0);
-  for (int r0 = 0; r0 < R; r0 += 16) {
-    const Rows now = next;
-    if (r0 + 16 < R) next = fetch(r0 + 16);  // in flight behind the products
-    const bool counts = now.w != 0.f && now.l != -INFINITY;
-    if (!__any(counts)) continue;
-    const float l2 = now.l * kLog2e;
+      for (int a = 0; a < 2; ++a) {
+        const size_t key = at + size_t(min(k + 16 * a + fr, q.keys - 1));
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      f32x4_t s{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], now.q[c], s);
-#pragma unroll
-      for (int z = 0; z < 4; ++z) {
-        bool sees = counts;
-        if (edge) sees &= tree_sees(now.bits, k + 16 * a + 4 * fq + z - q.len);
-        sum[a][z] += sees ? now.w * fast_exp2(fmaf(s[z], c2, -l2)) : 0.f;
+        for (int c = 0; c < kNK; ++c)
+          kf[a][c] = *reinterpret_cast<const bf16x8_t*>(K + key * DH + 32 * c + 8 * fq);
       }
+    };
+    for (int r0 = 0; r0 < R; r0 += kWRows) {
+    const int n_rows = min(kWRows, R - r0);
+    __syncthreads();  // the last rows are read
+    for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
+      const int row = i / kPieces, c = i % kPieces, r = r0 + row;
+      uint4 v{0, 0, 0, 0};
+      if (row < n_rows)
+        v = reinterpret_cast<const uint4*>(Q)[(size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * kPieces + c];
+      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) = v;
     }
-  }
+    if (tid < kWRows) {
+      RowInfo x{0.f, 0.f, 0};
+      if (tid < n_rows) {
+        const int r = r0 + tid, tok = q.q0 + r / G;
+        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r % G) * sh.n_q + tok];
+        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, tree_bits(mask, q.q0, r / G)};
+      }
+      info[tid] = x;
+    }
+    bf16x8_t kf[2][kNK], kn[2][kNK];
+    const int first = q.k0 + kWKeys * wave;
+    if (first < q.k1) load_k(kf, first);
+    __syncthreads();
+    for (int k = first; k < q.k1; k += 4 * kWKeys) {
+      const bool edge = k + kWKeys > q.len;
+      const int key = k + 16 * ((fr >> 2) & 1) + 4 * fq + (fr & 3);  // whose sum ends up in this lane (fr < 8)
+      const bool mine = fr < 8 && key < q.keys;
+      float was = 0.f;
+      if (mine) was = acc[at + key];
+      if (k + 4 * kWKeys < q.k1) load_k(kn, k + 4 * kWKeys);
+      float sum[8];
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+      for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+      for (int r = 0; r < n_rows; r += 16) {
+        const RowInfo x = info[r + fr];
+        if (!__any(x.w != 0.f)) continue;
+        bf16x8_t qf[kNK];
 #pragma unroll
-    for (int z = 0; z < 4; ++z)
+        for (int c = 0; c < kNK; ++c)
+          qf[c] = *reinterpret_cast<const bf16x8_t*>(qs + (r + fr) * kRow +
+                                                     ((4 * c + fq) ^ ((r + fr) / kWindow & (kPieces - 1))) * 16);
 #pragma unroll
-      for (int x = 1; x < 16; x <<= 1) sum[a][z] += __shfl_xor(sum[a][z], x, 64);
-  // lane (fr, fq) adds key 16 (fr / 4) + 4 fq + fr % 4
-  float v = 0.f;
+        for (int a = 0; a < 2; ++a) {
+          f32x4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+          for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
 #pragma unroll
-    for (int z = 0; z < 4; ++z) v = fr == 4 * a + z ? sum[a][z] : v;
-  const int key = k + 16 * (fr >> 2) + 4 * fq + (fr & 3);
-  if (key < q.keys) acc[size_t(bg) * sh.cap + key] += v;
+          for (int z = 0; z < 4; ++z) {
+            bool sees = x.w != 0.f;
+            if (edge) sees &= tree_sees(x.bits, k + 16 * a + 4 * fq + z - q.len);
+            sum[4 * a + z] += sees ? x.w * fast_exp2(fmaf(s[z], c2, -x.l2)) : 0.f;
+          }
+        }
+      }
+#pragma unroll
+      for (int half = 4; half >= 1; half >>= 1) {
+        const bool upper = (fr & half) != 0;
+#pragma unroll
+        for (int e = 0; e < half; ++e) {
+          const float keep = upper ? sum[e + half] : sum[e], give = upper ? sum[e] : sum[e + half];
+          sum[e] = keep + __shfl_xor(give, half, 64);
+        }
+      }
+      sum[0] += __shfl_xor(sum[0], 8, 64);
+      if (mine) acc[at + key] = was + sum[0];
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int c = 0; c < kNK; ++c) kf[a][c] = kn[a][c];
+    }
+    }
+  });
 }
 
 // acc[b][g][key] += sum over the rows of w exp(s - lse): one workgroup per 64 keys of a (sequence, KV head).
@@ -873,15 +902,18 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
 }
 template <typename T, int DH>
 int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, const int* cu_q, const int64_t* mask,
-                  const float* row_weight, const TreeShape& sh, float scale, float* acc, hipStream_t s) {
+                  const float* row_weight, TreeShape sh, float scale, float* acc, hipStream_t s) {
   const unsigned tiles = unsigned((sh.max_kv + kTKeys - 1) / kTKeys);
-  const dim3 grid(tiles * unsigned(sh.B * sh.Hkv));
-  if constexpr (sizeof(T) == 2)
-    tree_weight_mfma_kernel<DH><<<grid, dim3(64), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
-                                                          acc);
-  else
-    tree_weight_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
-                                                         acc);
+  const unsigned wgs = tiles * unsigned(sh.B * sh.Hkv);
+  if constexpr (sizeof(T) == 2) {
+    sh.item_rows = INT32_MAX / 2;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
+    const dim3 grid(std::min(unsigned(kWWgs), (wgs + 7) / 8 * 8));  // (a share is 128 keys or more)
+    tree_weight_mfma_kernel<DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
+                                                           acc);
+  } else {
+    tree_weight_kernel<T, DH><<<dim3(wgs), dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh,
+                                                              scale * kLog2e, acc);
+  }
   ESTP_CHECK_LAUNCH("tree_weight_kernel");
   return ESTP_OK;
 }
