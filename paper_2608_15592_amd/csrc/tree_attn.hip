@@ -649,9 +649,8 @@ __global__ __launch_bounds__(256) void tree_weight_stored_kernel(const float* __
 // sums join at the end of a tile, each exchange halving the values a lane still holds.
 constexpr int kWRows = 128;  // rows in LDS
 constexpr int kWKeys = 32;   // keys of a tile
-constexpr int kWWgs = 1024;  // workgroups: four on a compute unit
 template <int DH>
-__global__ __launch_bounds__(256, 4) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
+__global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
                                                                   const uint16_t* __restrict__ K,
                                                                   const float* __restrict__ lse,
                                                                   const int* __restrict__ lens,
@@ -663,9 +662,13 @@ __global__ __launch_bounds__(256, 4) void tree_weight_mfma_kernel(const uint16_t
   struct RowInfo {  // of weight 0: not used
     float w, l2;
     uint64_t bits;
+    int r;
   };
   __shared__ __attribute__((aligned(16))) char qs[kWRows * kRow];
   __shared__ __attribute__((aligned(16))) RowInfo info[kWRows];
+  __shared__ int live[2];
+  RowInfo mine{0.f, 0.f, 0, -1};
+  int place = 0;
   const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.Hq / sh.Hkv;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
@@ -682,41 +685,49 @@ __global__ __launch_bounds__(256, 4) void tree_weight_mfma_kernel(const uint16_t
       }
     };
     for (int r0 = 0; r0 < R; r0 += kWRows) {
-    const int n_rows = min(kWRows, R - r0);
-    __syncthreads();  // the last rows are read
-    for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
-      const int row = i / kPieces, c = i % kPieces, r = r0 + row;
-      uint4 v{0, 0, 0, 0};
-      if (row < n_rows)
-        v = reinterpret_cast<const uint4*>(Q)[(size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * kPieces + c];
-      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) = v;
-    }
-    if (tid < kWRows) {
-      RowInfo x{0.f, 0.f, 0};
-      if (tid < n_rows) {
-        const int r = r0 + tid, tok = q.q0 + r / G;
-        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r % G) * sh.n_q + tok];
-        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, tree_bits(mask, q.q0, r / G)};
-      }
-      info[tid] = x;
-    }
     bf16x8_t kf[2][kNK], kn[2][kNK];
     const int first = q.k0 + kWKeys * wave;
     if (first < q.k1) load_k(kf, first);
+    int n_rows = min(kWRows, R - r0);
+    __syncthreads();  // the last rows are read
+    // the rows that count, next to each other (of a tree often few: the accepted ones); the rest of the last 16 zero
+    if (tid < kWRows) {
+      RowInfo x{0.f, 0.f, 0, 0};
+      if (tid < n_rows) {
+        const int r = r0 + tid, tok = q.q0 + r / G;
+        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r % G) * sh.n_q + tok];
+        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, tree_bits(mask, q.q0, r / G), r};
+      }
+      const uint64_t counts = __ballot(x.w != 0.f);
+      if (lane == 0) live[wave] = int(__popcll(counts));
+      info[tid] = RowInfo{0.f, 0.f, 0, -1};
+      mine = x;
+      place = int(__popcll(counts & ((uint64_t(1) << lane) - 1)));
+    }
+    __syncthreads();
+    if (tid < kWRows && mine.w != 0.f) info[place + (wave == 1 ? live[0] : 0)] = mine;
+    n_rows = live[0] + live[1];
+    __syncthreads();
+    for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
+      const int row = i / kPieces, c = i % kPieces, r = info[row].r;
+      uint4 v{0, 0, 0, 0};
+      if (r >= 0)
+        v = reinterpret_cast<const uint4*>(Q)[(size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * kPieces + c];
+      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) = v;
+    }
     __syncthreads();
     for (int k = first; k < q.k1; k += 4 * kWKeys) {
       const bool edge = k + kWKeys > q.len;
       const int key = k + 16 * ((fr >> 2) & 1) + 4 * fq + (fr & 3);  // whose sum ends up in this lane (fr < 8)
-      const bool mine = fr < 8 && key < q.keys;
+      const bool writes = fr < 8 && key < q.keys && n_rows > 0;
       float was = 0.f;
-      if (mine) was = acc[at + key];
+      if (writes) was = acc[at + key];
       if (k + 4 * kWKeys < q.k1) load_k(kn, k + 4 * kWKeys);
       float sum[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] = 0.f;
       for (int r = 0; r < n_rows; r += 16) {
         const RowInfo x = info[r + fr];
-        if (!__any(x.w != 0.f)) continue;
         bf16x8_t qf[kNK];
 #pragma unroll
         for (int c = 0; c < kNK; ++c)
@@ -745,7 +756,7 @@ __global__ __launch_bounds__(256, 4) void tree_weight_mfma_kernel(const uint16_t
         }
       }
       sum[0] += __shfl_xor(sum[0], 8, 64);
-      if (mine) acc[at + key] = was + sum[0];
+      if (writes) acc[at + key] = was + sum[0];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -907,7 +918,7 @@ int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, con
   const unsigned wgs = tiles * unsigned(sh.B * sh.Hkv);
   if constexpr (sizeof(T) == 2) {
     sh.item_rows = INT32_MAX / 2;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
-    const dim3 grid(std::min(unsigned(kWWgs), (wgs + 7) / 8 * 8));  // (a share is 128 keys or more)
+    const dim3 grid(std::min(DH == 128 ? 768u : 1024u, (wgs + 7) / 8 * 8));  // (a share is 128 keys or more)
     tree_weight_mfma_kernel<DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
                                                            acc);
   } else {
