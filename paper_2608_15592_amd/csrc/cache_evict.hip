@@ -22,6 +22,7 @@
 namespace estp {
 namespace detail {
 
+typedef uint32_t piece_t __attribute__((ext_vector_type(4)));  // 16 bytes of a row
 constexpr int kEThreads = 1024;
 constexpr int kEWaves = kEThreads / 64;
 
@@ -59,19 +60,43 @@ struct EvictArgs {
   int *pos_out, *idx;
   int2* moves;
   int* n_moves;
-  uint4 *K, *V;  // rows moved here, or null: by evict_move_kernel
+  piece_t *K, *V;  // rows moved here, or null: by evict_move_kernel
   int row16;
   int* lens_out;  // written here when the rows are
 };
 
-__device__ __forceinline__ void move_rows(uint4* K, uint4* V, size_t base, int row16, const int2* moves, int n,
-                                          int64_t first, int64_t step) {
-  for (int64_t i = first; i < int64_t(n) * row16; i += step) {
-    const int2 e = moves[i / row16];
-    const int c = int(i % row16);
-    const uint4 k = K[(base + e.x) * row16 + c], v = V[(base + e.x) * row16 + c];
-    K[(base + e.y) * row16 + c] = k;
-    V[(base + e.y) * row16 + c] = v;
+// Pieces first, first + step, ... of the listed rows, four at a time: their places, then their loads, are in flight
+// together.  row16 is a power of two.
+__device__ __forceinline__ void move_rows(piece_t* __restrict__ K, piece_t* __restrict__ V, size_t base, int row16,
+                                          const int2* __restrict__ moves, int n, int64_t first, int64_t step) {
+  constexpr int kAhead = 4;
+  const int shift = __builtin_ctz(unsigned(row16));
+  const int64_t total = int64_t(n) << shift;
+  for (int64_t i = first; i < total; i += kAhead * step) {
+    int from[kAhead], to[kAhead];
+    piece_t k[kAhead], v[kAhead];
+    int c[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t at = min(i + u * step, total - 1);
+      const int2 e = moves[at >> shift];
+      from[u] = e.x;
+      to[u] = e.y;
+      c[u] = int(at) & (row16 - 1);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const size_t p = ((base + from[u]) << shift) + c[u];
+      k[u] = K[p];
+      v[u] = V[p];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (i + u * step < total) {
+        const size_t p = ((base + to[u]) << shift) + c[u];
+        K[p] = k[u];
+        V[p] = v[u];
+      }
   }
 }
 
@@ -288,7 +313,7 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
 }
 
 // The listed rows of K and V.  Also writes lens_out, which may be lens: by now evict_select_kernel has read it.
-__global__ __launch_bounds__(256) void evict_move_kernel(uint4* __restrict__ K, uint4* __restrict__ V, int cap,
+__global__ __launch_bounds__(256) void evict_move_kernel(piece_t* __restrict__ K, piece_t* __restrict__ V, int cap,
                                                          int row16, const int2* __restrict__ moves, int keep,
                                                          const int* __restrict__ n_moves, const int* lens, int Hkv,
                                                          int* lens_out) {
@@ -357,11 +382,12 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int row16 = dh * (dtype == ESTP_F32 ? 4 : 2) / 16;
   const int64_t most = std::min<int64_t>(keep, cap - keep) * row16;  // 16-byte pieces that can move, of K or V
-  // Rows move in the selecting kernel where its workgroups fill the chip, or where there are few (16 KB; a kernel of
-  // their own costs its launch).  Not in place of lens, which workgroups of the same sequence still read.
-  const bool here = (groups >= 192 || most <= 1024) && lens_out != lens;
+  // Rows move in the selecting kernel where there are few: a kernel of their own costs its launch, but spreads the
+  // rows of the longest sequences over the chip.  Not in place of lens, which workgroups of the same sequence still
+  // read.
+  const bool here = most <= 1024 && lens_out != lens;
   EvictArgs g{acc, pos, lens, seen, Hkv, int(cap), keep, recent, sink, acc_out, pos_out, idx, e.moves, e.n_moves,
-              here ? static_cast<uint4*>(K) : nullptr, static_cast<uint4*>(V), row16, lens_out};
+              here ? static_cast<piece_t*>(K) : nullptr, static_cast<piece_t*>(V), row16, lens_out};
   auto select = cap <= kEThreads        ? evict_select_kernel<1>
                 : cap <= 4 * kEThreads  ? evict_select_kernel<4>
                 : cap <= 16 * kEThreads ? evict_select_kernel<16>
@@ -372,7 +398,7 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   if (here) return ESTP_OK;
   const int64_t wgs = std::max<int64_t>(1, std::min<int64_t>((most + 255) / 256, std::max(1, 4096 / groups)));
   evict_move_kernel<<<dim3(unsigned(wgs), unsigned(groups)), dim3(256), 0, s>>>(
-      static_cast<uint4*>(K), static_cast<uint4*>(V), int(cap), row16, e.moves, keep, e.n_moves, lens, Hkv, lens_out);
+      static_cast<piece_t*>(K), static_cast<piece_t*>(V), int(cap), row16, e.moves, keep, e.n_moves, lens, Hkv, lens_out);
   ESTP_CHECK_LAUNCH("evict_move_kernel");
   return ESTP_OK;
 }
