@@ -215,6 +215,15 @@ def _sized(t: torch.Tensor, name: str, n: int, device=None, dtype=None):
         raise ValueError(f"{name} must hold {n} elements, got {t.numel()}")
 
 
+def _all_sized(index: int, device, *wanted):
+    """``_sized`` of (tensor, name, elements, dtype) in turn.  The common case, a tensor that is as wanted on device
+    ``index``, takes four short calls (0.3 us a tensor; each of ``_sized``'s comparisons of devices takes as long)."""
+    for t, name, n, dtype in wanted:
+        if t.get_device() == index and t.dtype is dtype and t.numel() == n and t.is_contiguous():
+            continue
+        _sized(t, name, n, device=device, dtype=dtype)
+
+
 def _workspace(nbytes: int, device, workspace: Optional[torch.Tensor]):
     if workspace is not None:
         _need(workspace, "workspace", device=device)
@@ -565,10 +574,10 @@ def _tree_shapes(Q, K, lens, cu_q, tree_mask):
     B, Hkv, cap = K.shape[:3]
     if K.shape[3] != dh:
         raise ValueError("Q and K disagree on the head size")
-    _sized(lens, "lens", B, device=Q.device, dtype=torch.int32)
-    _sized(cu_q, "cu_q", B + 1, device=Q.device, dtype=torch.int32)
+    dev = Q.device
+    _all_sized(dev.index, dev, (lens, "lens", B, torch.int32), (cu_q, "cu_q", B + 1, torch.int32))
     if tree_mask is not None:
-        _sized(tree_mask, "tree_mask", n_q, device=Q.device, dtype=torch.int64)
+        _all_sized(dev.index, dev, (tree_mask, "tree_mask", n_q, torch.int64))
     return B, n_q, Hq, Hkv, cap, dh
 
 
@@ -588,18 +597,21 @@ def tree_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, lens: torc
     _need(V, "V", device=Q.device, dtype=Q.dtype)
     if V.shape != K.shape:
         raise ValueError("V must have the shape of K")
+    dev = Q.device
     if acc is not None:
-        _sized(acc, "acc", B * Hkv * cap, device=Q.device, dtype=torch.float32)
+        _all_sized(dev.index, dev, (acc, "acc", B * Hkv * cap, torch.float32))
     if scale is None:
         scale = 1.0 / math.sqrt(dh)
     dt = _dtype_code(Q)
-    with _on(stream, Q.device) as st:
+    with _on(stream, dev) as st:
         if O is None:
             O = torch.empty_like(Q)
-        _sized(O, "O", Q.numel(), device=Q.device, dtype=Q.dtype)
+        else:
+            _all_sized(dev.index, dev, (O, "O", Q.numel(), Q.dtype))
         if lse is None:
-            lse = torch.empty(Hq, n_q, dtype=torch.float32, device=Q.device)
-        _sized(lse, "lse", Hq * n_q, device=Q.device, dtype=torch.float32)
+            lse = torch.empty(Hq, n_q, dtype=torch.float32, device=dev)
+        else:
+            _all_sized(dev.index, dev, (lse, "lse", Hq * n_q, torch.float32))
         ws = lib.estp_tree_attention_workspace_size(B, int(max_q), n_q, Hq, Hkv, int(max_kv), dh, dt)
         workspace, wsb = _workspace(ws, Q.device, workspace)
         _check(lib.estp_tree_attention(_ptr(Q), _ptr(K), _ptr(V), _ptr(lens), _ptr(cu_q), _ptr(tree_mask), B,
@@ -616,10 +628,10 @@ def tree_importance(Q: torch.Tensor, K: torch.Tensor, lse: torch.Tensor, lens: t
     ``row_weight[i]`` (float32 [n_q], default 1; 0 for rejected rows).  ``lse`` is ``tree_attention``'s."""
     lib = load()
     B, n_q, Hq, Hkv, cap, dh = _tree_shapes(Q, K, lens, cu_q, tree_mask)
-    _sized(lse, "lse", Hq * n_q, device=Q.device, dtype=torch.float32)
-    _sized(acc, "acc", B * Hkv * cap, device=Q.device, dtype=torch.float32)
+    dev = Q.device
+    _all_sized(dev.index, dev, (lse, "lse", Hq * n_q, torch.float32), (acc, "acc", B * Hkv * cap, torch.float32))
     if row_weight is not None:
-        _sized(row_weight, "row_weight", n_q, device=Q.device, dtype=torch.float32)
+        _all_sized(dev.index, dev, (row_weight, "row_weight", n_q, torch.float32))
     if scale is None:
         scale = 1.0 / math.sqrt(dh)
     with _on(stream, Q.device) as st:
@@ -648,22 +660,22 @@ def cache_evict(K: torch.Tensor, V: torch.Tensor, acc: torch.Tensor, pos: torch.
         raise ValueError("V must have the shape of K")
     acc_out = acc if acc_out is None else acc_out
     pos_out = pos if pos_out is None else pos_out
-    for t, name, n, dtype in ((acc, "acc", B * Hkv * cap, torch.float32), (pos, "pos", B * Hkv * cap, torch.int32),
-                              (acc_out, "acc_out", B * Hkv * cap, torch.float32),
-                              (pos_out, "pos_out", B * Hkv * cap, torch.int32), (lens, "lens", B, torch.int32),
-                              (seen, "seen", B, torch.int32)):
-        _sized(t, name, n, device=K.device, dtype=dtype)
+    keep, slots, f32, i32, dev = int(keep), B * Hkv * cap, torch.float32, torch.int32, K.device
+    _all_sized(dev.index, dev, (acc, "acc", slots, f32), (pos, "pos", slots, i32), (acc_out, "acc_out", slots, f32),
+               (pos_out, "pos_out", slots, i32), (lens, "lens", B, i32), (seen, "seen", B, i32))
     dt = _dtype_code(K)
-    with _on(stream, K.device) as st:
+    with _on(stream, dev) as st:
         if lens_out is None:
-            lens_out = torch.empty(B, dtype=torch.int32, device=K.device)
-        _sized(lens_out, "lens_out", B, device=K.device, dtype=torch.int32)
+            lens_out = torch.empty(B, dtype=i32, device=dev)
+        else:
+            _all_sized(dev.index, dev, (lens_out, "lens_out", B, i32))
         if idx is None:
-            idx = torch.empty(B, Hkv, max(int(keep), 0), dtype=torch.int32, device=K.device)
-        _sized(idx, "idx", B * Hkv * max(int(keep), 0), device=K.device, dtype=torch.int32)
-        workspace, wsb = _workspace(lib.estp_cache_evict_workspace_size(B, Hkv, int(keep)), K.device, workspace)
+            idx = torch.empty(B, Hkv, max(keep, 0), dtype=i32, device=dev)
+        else:
+            _all_sized(dev.index, dev, (idx, "idx", B * Hkv * max(keep, 0), i32))
+        workspace, wsb = _workspace(lib.estp_cache_evict_workspace_size(B, Hkv, keep), dev, workspace)
         _check(lib.estp_cache_evict(_ptr(K), _ptr(V), _ptr(acc), _ptr(pos), _ptr(lens), _ptr(seen), B, Hkv, cap, dh,
-                                    dt, int(keep), int(recent), int(sink), _ptr(acc_out), _ptr(pos_out),
+                                    dt, keep, int(recent), int(sink), _ptr(acc_out), _ptr(pos_out),
                                     _ptr(lens_out), _ptr(idx), _ptr(workspace), wsb, st), "estp_cache_evict")
     return lens_out, idx
 

@@ -9,15 +9,16 @@
 // move at once in place.  The order of the slots carries no meaning, their
 // positions are in pos.
 //
-// evict_select_kernel, one workgroup per (sequence, KV head), a thread per every 1024th slot: the weights'
-// order-preserving 32-bit keys stay in registers (caches of up to 65536 slots; longer ones are read again on each
-// pass).  Four histogram passes of 8 bits in LDS find the key of the last one kept.  Places in slot order (of ties,
-// holes and survivors) come from ballots: a count per 64 slots, one prefix over all counts.  The survivors' rows move
-// in the same kernel where its workgroups fill the chip or there is little to move, else in evict_move_kernel.
-// Everything is exact: whole numbers and copies.
+// evict_select_kernel, one workgroup per (sequence, KV head), a thread per every 1024th slot: weights and positions
+// stay in registers (caches of up to 16384 slots; longer ones are read again on each pass).  Four histogram passes of
+// 8 bits in LDS find the key of the last one kept; places in slot order (of ties, holes and survivors) come from
+// ballots, a count per 64 slots, one prefix over all counts.  Latency bounds it: so every wave searches the histogram
+// and forms the prefix for itself, which leaves one barrier a pass and a prefix.  The survivors' rows move in the same
+// kernel where they are few, else in evict_move_kernel.  Everything is exact: whole numbers and copies.
 #include <algorithm>
 
 #include "estp_common.h"
+#include "lds_ops.h"
 
 namespace estp {
 namespace detail {
@@ -25,6 +26,7 @@ namespace detail {
 typedef uint32_t piece_t __attribute__((ext_vector_type(4)));  // 16 bytes of a row
 constexpr int kEThreads = 1024;
 constexpr int kEWaves = kEThreads / 64;
+constexpr int kMovesHere = 256;  // rows that evict_select_kernel moves itself, at most
 
 // Weights as whole numbers in the same order: NaN lowest, -0 as +0.
 __device__ __forceinline__ uint32_t weight_key(float v) {
@@ -32,23 +34,6 @@ __device__ __forceinline__ uint32_t weight_key(float v) {
   if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
   if ((u & 0x7fffffffu) == 0) return 0x80000000u;
   return (u >> 31) ? ~u : u | 0x80000000u;
-}
-
-// Exclusive prefix of a thread's pair of counts over the workgroup (every thread calls), in the halves of 64 bits.
-__device__ __forceinline__ uint64_t block_prefix(uint64_t v, uint64_t* sh) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint64_t x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint64_t y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) sh[wave] = x;
-  __syncthreads();
-  uint64_t before = x - v;
-#pragma unroll
-  for (int w = 0; w < kEWaves; ++w) before += w < wave ? sh[w] : 0;
-  return before;
 }
 
 // One row of the slots' 1024: the thread's slot of round i is 1024 i + tid.
@@ -68,7 +53,7 @@ struct EvictArgs {
 // Pieces first, first + step, ... of the listed rows, four at a time: their places, then their loads, are in flight
 // together.  row16 is a power of two.
 __device__ __forceinline__ void move_rows(piece_t* __restrict__ K, piece_t* __restrict__ V, size_t base, int row16,
-                                          const int2* __restrict__ moves, int n, int64_t first, int64_t step) {
+                                          const int2* moves, int n, int64_t first, int64_t step) {
   constexpr int kAhead = 4;
   const int shift = __builtin_ctz(unsigned(row16));
   const int64_t total = int64_t(n) << shift;
@@ -103,15 +88,17 @@ __device__ __forceinline__ void move_rows(piece_t* __restrict__ K, piece_t* __re
 // kE rounds of 1024 slots in registers; kE = 0: any number, read from memory on every pass.
 template <int kE>
 __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
-  constexpr int kHists = 4;  // copies of the histogram: equal weights meet on fewer threads
-  constexpr int kSpan = kE > 0 ? kE : 64;  // rounds whose counts one prefix covers
-  __shared__ int hist[kHists][256];
-  __shared__ uint32_t found[2];
-  __shared__ int n_guarded_sh;
-  __shared__ uint64_t wave_sum_sh[kEWaves], counts[kSpan * kEWaves], carry;
-  const int bg = blockIdx.x, b = bg / g.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kHists = 2;               // copies of the histogram: equal weights meet on fewer threads
+  constexpr int kSpan = kE > 0 ? kE : 32;  // rounds whose counts one prefix covers
+  constexpr int kPer = (kSpan * kEWaves + 63) / 64;  // counts of a lane
+  constexpr bool kHeld = kE > 0;           // weights and positions stay in registers, holes in LDS
+  __shared__ __attribute__((aligned(16))) uint32_t hist[4][kHists][256];  // of the four digits
+  __shared__ uint32_t n_guarded_sh, counts[2][64 * kPer];
+  __shared__ int hole_sh[kHeld ? kE * (kEThreads / 2) : 1];  // at most half of the slots
+  __shared__ int2 moves_sh[kMovesHere];
+  const int bg = blockIdx.x, b = bg / g.Hkv, tid = threadIdx.x, lane = tid & 63, keep = g.keep;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t base = size_t(bg) * g.cap;
-  const int n = max(0, min(g.lens[b], g.cap)), keep = g.keep;
   const float* acc = g.acc + base;
   const int* pos = g.pos + base;
   float* acc_out = g.acc_out + base;
@@ -119,6 +106,22 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
   int* idx = g.idx + size_t(bg) * keep;
   int2* moves = g.moves + size_t(bg) * keep;
   const bool copy = acc_out != acc || pos_out != pos;
+  // the whole capacity's weights and positions, on their way while the length is
+  float a[kHeld ? kE : 1];
+  int ps[kHeld ? kE : 1];
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int r = 0; r < kE; ++r) {
+      const int i = min(r * kEThreads + tid, g.cap - 1);
+      a[r] = acc[i];
+      ps[r] = pos[i];
+    }
+  }
+  const int n = max(0, min(g.lens[b], g.cap));
+  const int64_t first_recent = int64_t(g.seen[b]) - g.recent;
+  for (int i = tid; i < 4 * kHists * 256; i += kEThreads) (&hist[0][0][0])[i] = 0;
+  for (int i = tid; i < 2 * 64 * kPer; i += kEThreads) (&counts[0][0])[i] = 0;
+  if (tid == 0) n_guarded_sh = 0;
   if (g.K && tid == 0 && bg % g.Hkv == 0) g.lens_out[b] = min(n, keep);
   if (n <= keep) {  // everything stays
     for (int i = tid; i < keep; i += kEThreads) idx[i] = i < n ? i : -1;
@@ -130,186 +133,196 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
     if (tid == 0) g.n_moves[bg] = 0;
     return;
   }
-  const int64_t first_recent = int64_t(g.seen[b]) - g.recent;
-  auto is_guarded = [&](int i) { return pos[i] < g.sink || pos[i] >= first_recent; };
   const int rounds = kE > 0 ? kE : (n + kEThreads - 1) / kEThreads;
-
-  uint32_t key[kE > 0 ? kE : 1];
-  uint64_t guard = 0;
-  if (tid == 0) n_guarded_sh = 0;
-  for (int i = tid; i < kHists * 256; i += kEThreads) (&hist[0][0])[i] = 0;
-  __syncthreads();
-  int mine = 0;
-  if constexpr (kE > 0) {
-#pragma unroll
-    for (int r = 0; r < kE; ++r) {
-      const int i = r * kEThreads + tid;
-      key[r] = i < n ? weight_key(acc[i]) : 0;
-      const bool gd = i < n && is_guarded(i);
-      guard |= uint64_t(gd) << r;
-      mine += gd;
-    }
-  } else {
-    for (int i = tid; i < n; i += kEThreads) mine += is_guarded(i);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
-  if (lane == 0 && mine) atomicAdd(&n_guarded_sh, mine);
-  __syncthreads();
-  // guarded slots: all stay if they fit, else the best of them do and nothing else
-  const int n_guarded = n_guarded_sh;
-  const bool among = n_guarded >= keep;  // whether the choice is among the guarded slots
-  uint32_t need = uint32_t(among ? keep : keep - n_guarded);
-  // Round r's slot of this thread: its key, and whether it is in the choice.
-  auto at = [&](int r, uint32_t* k, bool* in, bool* gd) {
-    const int i = r * kEThreads + tid;
-    *in = i < n;
-    if constexpr (kE > 0) {
-      *k = key[r];
-      *gd = (guard >> r) & 1;
-    } else {
-      *k = *in ? weight_key(acc[i]) : 0;
-      *gd = *in && is_guarded(i);
-    }
+  auto is_guarded = [&](int p) { return p < g.sink || p >= first_recent; };
+  auto weight = [&](int r) {
+    if constexpr (kHeld)
+      return a[r];
+    else
+      return acc[r * kEThreads + tid];
   };
-  auto each_round = [&](auto&& f) {
+  auto position = [&](int r) {
+    if constexpr (kHeld)
+      return ps[r];
+    else
+      return pos[r * kEThreads + tid];
+  };
+  // Round r's slot of this thread: its key, whether it is there, and whether it is guarded.
+  auto at = [&](int r, uint32_t* k, bool* in, bool* gd) {
+    *in = r * kEThreads + tid < n;
+    *k = *in ? weight_key(weight(r)) : 0;
+    *gd = *in && is_guarded(position(r));
+  };
+  auto rounds_from = [&](int r0, int r1, auto&& f) {
     if constexpr (kE > 0) {
 #pragma unroll
       for (int r = 0; r < kE; ++r) f(r);
     } else {
-      for (int r = 0; r < rounds; ++r) f(r);
+#pragma unroll 4
+      for (int r = r0; r < r1; ++r) f(r);
     }
   };
+  __syncthreads();
+  uint32_t in_wave = 0;
+  rounds_from(0, rounds, [&](int r) {
+    in_wave += uint32_t(__popcll(__ballot(r * kEThreads + tid < n && is_guarded(position(r)))));
+  });
+  if (lane == 0 && in_wave) atomicAdd(&n_guarded_sh, in_wave);
+  __syncthreads();
+  // guarded slots: all stay if they fit, else the best of them do and nothing else
+  const int n_guarded = int(n_guarded_sh);
+  const bool among = n_guarded >= keep;  // whether the choice is among the guarded slots
+  uint32_t need = uint32_t(among ? keep : keep - n_guarded);
   // the key of the need-th best candidate, 8 bits at a time; `need` becomes how many of its equals stay
   uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    each_round([&](int r) {
-      uint32_t k;
-      bool in, gd;
-      at(r, &k, &in, &gd);
-      if (in && gd == among && (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))))
-        atomicAdd(&hist[wave % kHists][(k >> shift) & 255], 1);
+#pragma unroll
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
+    rounds_from(0, rounds, [&](int r) {
+      if (r * kEThreads + tid >= n) return;
+      const uint32_t k = weight_key(weight(r));
+      if ((pass == 0 || (k >> (shift + 8)) == (prefix >> (shift + 8))) && is_guarded(position(r)) == among)
+        atomicAdd(&hist[pass][wave % kHists][255 - ((k >> shift) & 255)], 1u);
     });
     __syncthreads();
-    if (wave == 0) {  // lane j: bins 255 - 4 j down to 252 - 4 j; the first lane whose running count reaches `need`
-      uint32_t c[4], sum = 0;
+    // descending digits: lane j has the counts of 255 - 4 j down to 252 - 4 j; where the running count reaches `need`
+    u32x4_t c = *reinterpret_cast<const u32x4_t*>(&hist[pass][0][4 * lane]);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        c[q] = 0;
+    for (int h = 1; h < kHists; ++h) c += *reinterpret_cast<const u32x4_t*>(&hist[pass][h][4 * lane]);
+    const uint32_t sum = (c[0] + c[1]) + (c[2] + c[3]), upto = wave_prefix(sum);
+    const uint64_t reached = __ballot(upto >= need);
+    const int j = reached ? __builtin_ctzll(reached) : 63;
+    uint32_t above = lane_of(upto, j) - lane_of(sum, j), digit = uint32_t(255 - 4 * j);
 #pragma unroll
-        for (int h = 0; h < kHists; ++h) {
-          c[q] += uint32_t(hist[h][255 - 4 * lane - q]);
-          hist[h][255 - 4 * lane - q] = 0;
-        }
-        sum += c[q];
-      }
-      uint32_t x = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t y = __shfl_up(x, o, 64);
-        if (lane >= o) x += y;
-      }
-      const uint64_t reached = __ballot(x >= need);
-      if (reached && lane == __builtin_ctzll(reached)) {
-        uint32_t above = x - sum;
-        int q = 0;
-        while (q < 3 && above + c[q] < need) above += c[q++];
-        found[0] = uint32_t(255 - 4 * lane - q);
-        found[1] = need - above;
+    for (int z = 0; z < 3; ++z) {
+      const uint32_t cz = lane_of(c[z], j);
+      if (digit == uint32_t(255 - 4 * j - z) && above + cz < need) {
+        above += cz;
+        --digit;
       }
     }
-    __syncthreads();
-    prefix |= found[0] << shift;
-    need = found[1];
+    prefix |= digit << shift;
+    need -= above;
   }
 
-  // Places in slot order: pass 0 counts ties and sees which of them stay, pass 1 counts holes (low half) and
-  // survivors (high half) and lists them.  Per span of rounds: a count for every 64 slots, one prefix, the lanes' own.
-  uint64_t stays = 0;  // kE > 0: a bit a round
-  int ties_before = 0;
-  uint64_t moved_before = 0;
-  auto span = [&](int r0, auto&& flags) {  // flags(r, &low, &high): exclusive counts before the thread's slot
-    const int nr = min(kSpan, rounds - r0);
-    for (int r = r0; r < r0 + nr; ++r) {
-      bool lo, hi;
-      flags(r, &lo, &hi);
-      const uint64_t bl = __ballot(lo), bh = __ballot(hi);
-      if (lane == 0) counts[(r - r0) * kEWaves + wave] = uint64_t(__popcll(bl)) | uint64_t(__popcll(bh)) << 32;
-    }
-    __syncthreads();
-    const uint64_t c = tid < nr * kEWaves ? counts[tid] : 0;
-    const uint64_t before = block_prefix(c, wave_sum_sh);
-    if (tid < nr * kEWaves) counts[tid] = before;
-    if (tid == nr * kEWaves - 1) carry = before + c;
-    __syncthreads();
-  };
+  // Places in slot order, over spans of rounds: first the ties are counted, to see which of them stay, then holes (low
+  // half) and survivors (high half).  A count for every 64 slots, one prefix over all counts, the lanes' own.
+  uint32_t ties_before = 0, holes_before = 0, late_before = 0;
   auto below = [&](bool x) { return uint32_t(__popcll(__ballot(x) & ((uint64_t(1) << lane) - 1))); };
-  auto stays_at = [&](int r, uint32_t tie_rank, bool* in_out) {
-    uint32_t k;
-    bool in, gd;
-    at(r, &k, &in, &gd);
-    *in_out = in;
-    return in && ((gd && !among) || (gd == among && (k > prefix || (k == prefix && tie_rank < need))));
+  // Exclusive prefix of a count array, which every wave forms for itself: lane j holds counts kPer j .. of it.
+  struct Prefix {
+    uint32_t v[kPer], total;
+    __device__ __forceinline__ uint32_t of(int i) const {  // i uniform
+      uint32_t x = 0;
+#pragma unroll
+      for (int q = 0; q < kPer; ++q) x = i % kPer == q ? lane_of(v[q], i / kPer) : x;
+      return x;
+    }
   };
-  auto is_tie = [&](int r) {
-    uint32_t k;
-    bool in, gd;
-    at(r, &k, &in, &gd);
-    return in && gd == among && k == prefix;
+  auto prefix_of = [&](const uint32_t* counted) {
+    Prefix p;
+    uint32_t c[kPer], sum = 0;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      c[q] = counted[kPer * lane + q];
+      sum += c[q];
+    }
+    const uint32_t upto = wave_prefix(sum);
+    uint32_t run = upto - sum;
+#pragma unroll
+    for (int q = 0; q < kPer; ++q) {
+      p.v[q] = run;
+      run += c[q];
+    }
+    p.total = lane_of(upto, 63);
+    return p;
   };
   for (int r0 = 0; r0 < rounds; r0 += kSpan) {
     const int r1 = min(rounds, r0 + kSpan);
-    span(r0, [&](int r, bool* lo, bool* hi) {
-      *lo = is_tie(r);
-      *hi = false;
+    uint32_t tie = 0, stays = 0;  // a bit a round
+    rounds_from(r0, r1, [&](int r) {
+      uint32_t k;
+      bool in, gd;
+      at(r, &k, &in, &gd);
+      const bool t = in && gd == among && k == prefix;
+      tie |= uint32_t(t) << (r - r0);
+      stays |= uint32_t(in && ((gd && !among) || (gd == among && k > prefix))) << (r - r0);
+      const uint64_t m = __ballot(t);
+      if (lane == 0) counts[0][(r - r0) * kEWaves + wave] = uint32_t(__popcll(m));
     });
-    uint64_t bits = 0;  // of this span: stays
-    for (int r = r0; r < r1; ++r) {
-      const uint32_t rank = uint32_t(ties_before) + uint32_t(counts[(r - r0) * kEWaves + wave]) + below(is_tie(r));
-      bool in;
-      bits |= uint64_t(stays_at(r, rank, &in)) << (r - r0);
+    __syncthreads();
+    {
+      const Prefix p = prefix_of(counts[0]);
+      rounds_from(r0, r1, [&](int r) {
+        const bool t = (tie >> (r - r0)) & 1;
+        const uint32_t rank = ties_before + p.of((r - r0) * kEWaves + wave) + below(t);
+        if (t && rank < need) stays |= uint32_t(1) << (r - r0);
+      });
+      ties_before += p.total;
     }
-    ties_before += int(uint32_t(carry));
-    stays = bits;
-    __syncthreads();  // counts and carry are read
-    span(r0, [&](int r, bool* lo, bool* hi) {
+    // holes in the low half, survivors in the high one: at most 16384 each a span
+    rounds_from(r0, r1, [&](int r) {
       const int i = r * kEThreads + tid;
       const bool st = (stays >> (r - r0)) & 1;
-      *lo = i < n && i < keep && !st;
-      *hi = st && i >= keep;
+      const uint64_t h = __ballot(i < n && i < keep && !st), l = __ballot(st && i >= keep);
+      if (lane == 0) counts[1][(r - r0) * kEWaves + wave] = uint32_t(__popcll(h)) | uint32_t(__popcll(l)) << 16;
     });
-    for (int r = r0; r < r1; ++r) {
+    __syncthreads();
+    const Prefix p = prefix_of(counts[1]);
+    rounds_from(r0, r1, [&](int r) {  // holes are listed, kept slots below `keep` copied
       const int i = r * kEThreads + tid;
-      const bool st = (stays >> (r - r0)) & 1, hole = i < n && i < keep && !st, late = st && i >= keep;
-      const uint64_t c = moved_before + counts[(r - r0) * kEWaves + wave];
-      const uint32_t h = uint32_t(c) + below(hole), l = uint32_t(c >> 32) + below(late);
-      if (hole) moves[h].y = i;
-      if (late) moves[l].x = i;
+      const bool st = (stays >> (r - r0)) & 1, hole = i < n && i < keep && !st;
+      const uint32_t h = holes_before + (p.of((r - r0) * kEWaves + wave) & 0xffff) + below(hole);
+      if (hole) {
+        if constexpr (kHeld)
+          hole_sh[h] = i;
+        else
+          moves[h].y = i;
+      }
       if (st && i < keep) {
         idx[i] = i;
         if (copy) {
-          acc_out[i] = acc[i];
-          pos_out[i] = pos[i];
+          acc_out[i] = weight(r);
+          pos_out[i] = position(r);
         }
       }
+    });
+    __syncthreads();  // every hole that this span's survivors fill is listed: all holes lie before all survivors
+    rounds_from(r0, r1, [&](int r) {
+      const int i = r * kEThreads + tid;
+      const bool late = ((stays >> (r - r0)) & 1) && i >= keep;
+      const uint32_t l = late_before + (p.of((r - r0) * kEWaves + wave) >> 16) + below(late);
+      if (i < n && i >= keep) {
+        if (late) {
+          int to;
+          if constexpr (kHeld)
+            to = hole_sh[l];
+          else
+            to = moves[l].y;
+          idx[to] = i;
+          acc_out[to] = weight(r);
+          pos_out[to] = position(r);
+          if (g.K)
+            moves_sh[l] = int2{i, to};
+          else
+            moves[l] = int2{i, to};
+        }
+        acc_out[i] = 0.f;  // a freed slot
+        pos_out[i] = -1;
+      }
+    });
+    holes_before += p.total & 0xffff;
+    late_before += p.total >> 16;
+    if (kE == 0) {  // the next span may be shorter: no counts of this one's stay
+      __syncthreads();
+      for (int i = tid; i < 2 * 64 * kPer; i += kEThreads) (&counts[0][0])[i] = 0;
+      __syncthreads();
     }
-    moved_before += carry;
-    __syncthreads();  // counts and carry are read, and the moves of this span written
   }
-  const int holes = int(uint32_t(moved_before));  // as many as survivors
-  for (int m = tid; m < holes; m += kEThreads) {
-    const int2 e = moves[m];
-    idx[e.y] = e.x;
-    acc_out[e.y] = acc[e.x];
-    pos_out[e.y] = pos[e.x];
-  }
-  __syncthreads();  // freed slots are cleared after the moves have read them
-  for (int i = keep + tid; i < n; i += kEThreads) {
-    acc_out[i] = 0.f;
-    pos_out[i] = -1;
-  }
+  if (g.K) __syncthreads();
+  const int holes = int(holes_before);  // as many as survivors
   if (tid == 0) g.n_moves[bg] = holes;
-  if (g.K) move_rows(g.K, g.V, base, g.row16, moves, holes, tid, kEThreads);
+  if (g.K) move_rows(g.K, g.V, base, g.row16, moves_sh, holes, tid, kEThreads);
 }
 
 // The listed rows of K and V.  Also writes lens_out, which may be lens: by now evict_select_kernel has read it.
@@ -385,14 +398,13 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   // Rows move in the selecting kernel where there are few: a kernel of their own costs its launch, but spreads the
   // rows of the longest sequences over the chip.  Not in place of lens, which workgroups of the same sequence still
   // read.
-  const bool here = most <= 1024 && lens_out != lens;
+  const bool here = std::min<int64_t>(keep, cap - keep) <= kMovesHere && most <= 2048 && lens_out != lens;
   EvictArgs g{acc, pos, lens, seen, Hkv, int(cap), keep, recent, sink, acc_out, pos_out, idx, e.moves, e.n_moves,
               here ? static_cast<piece_t*>(K) : nullptr, static_cast<piece_t*>(V), row16, lens_out};
   auto select = cap <= kEThreads        ? evict_select_kernel<1>
                 : cap <= 4 * kEThreads  ? evict_select_kernel<4>
                 : cap <= 16 * kEThreads ? evict_select_kernel<16>
-                : cap <= 64 * kEThreads ? evict_select_kernel<64>
-                                        : evict_select_kernel<0>;
+                                                    : evict_select_kernel<0>;
   select<<<dim3(unsigned(groups)), dim3(kEThreads), 0, s>>>(g);
   ESTP_CHECK_LAUNCH("evict_select_kernel");
   if (here) return ESTP_OK;

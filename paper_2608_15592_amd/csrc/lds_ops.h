@@ -49,6 +49,22 @@ __device__ __forceinline__ bf16x8_t join_tr(s16x4_t lo, s16x4_t hi) {
   return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// Inclusive prefix sum over the wave, without LDS: shifts within rows of 16 lanes, then the rows' last lanes.
+__device__ __forceinline__ uint32_t wave_prefix(uint32_t x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x111, 0xf, 0xf, false));  // row_shr 1, 2, 4, 8
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x112, 0xf, 0xf, false));
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x114, 0xf, 0xf, false));
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x118, 0xf, 0xf, false));
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x142, 0xa, 0xf, false));  // row_bcast 15 into rows 1 and 3
+  x += uint32_t(__builtin_amdgcn_update_dpp(0, int(x), 0x143, 0xc, 0xf, false));  // row_bcast 31 into rows 2 and 3
+#endif
+  return x;
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
+  return uint32_t(__builtin_amdgcn_readlane(int(v), lane));
+}
+
 // At most N of this wave's vector-memory operations still in flight; LDS reads after it stay after it.
 template <int N>
 __device__ __forceinline__ void arrived() {

@@ -60,19 +60,6 @@ __device__ __forceinline__ bool tree_sees(uint64_t bits, int rel) {
 
 // ------------------------------------------------------------------ the line of chunks
 
-__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
-  return uint32_t(__builtin_amdgcn_readlane(int(v), lane));
-}
-__device__ __forceinline__ uint32_t wave_prefix(uint32_t v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t y = __shfl_up(v, o, 64);
-    if (lane >= o) v += y;
-  }
-  return v;
-}
-
 // 64 sequences, one a lane: counts, and how many chunks of kChunk keys their items have in all.
 template <int kChunk>
 struct TreeBatch {
