@@ -9,8 +9,8 @@
 // move at once in place.  The order of the slots carries no meaning, their
 // positions are in pos.
 //
-// evict_select_kernel, one workgroup per (sequence, KV head), a thread per every 1024th slot: weights and positions
-// stay in registers (caches of up to 16384 slots; longer ones are read again on each pass).  Four histogram passes of
+// evict_select_kernel, one workgroup per (sequence, KV head), a thread per every 1024th slot: the weights' keys
+// stay in registers (caches of up to 65536 slots; longer ones are read again on each pass).  Four histogram passes of
 // 8 bits in LDS find the key of the last one kept; places in slot order (of ties, holes and survivors) come from
 // ballots, a count per 64 slots, one prefix over all counts.  Latency bounds it: so every wave searches the histogram
 // and forms the prefix for itself, which leaves one barrier a pass and a prefix.  The survivors' rows move in the same
@@ -91,7 +91,8 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
   constexpr int kHists = 2;               // copies of the histogram: equal weights meet on fewer threads
   constexpr int kSpan = kE > 0 ? kE : 32;  // rounds whose counts one prefix covers
   constexpr int kPer = (kSpan * kEWaves + 63) / 64;  // counts of a lane
-  constexpr bool kHeld = kE > 0;           // weights and positions stay in registers, holes in LDS
+  constexpr bool kHeld = kE > 0;           // keys stay in registers, holes in LDS
+  constexpr bool kRaw = kE > 0 && kE <= 4;  // weights and positions too
   __shared__ __attribute__((aligned(16))) uint32_t hist[4][kHists][256];  // of the four digits
   __shared__ uint32_t n_guarded_sh, counts[2][64 * kPer];
   __shared__ int hole_sh[kHeld ? kE * (kEThreads / 2) : 1];  // at most half of the slots
@@ -107,9 +108,9 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
   int2* moves = g.moves + size_t(bg) * keep;
   const bool copy = acc_out != acc || pos_out != pos;
   // the whole capacity's weights and positions, on their way while the length is
-  float a[kHeld ? kE : 1];
-  int ps[kHeld ? kE : 1];
-  if constexpr (kHeld) {
+  float a[kRaw ? kE : 1];
+  int ps[kRaw ? kE : 1];
+  if constexpr (kRaw) {
 #pragma unroll
     for (int r = 0; r < kE; ++r) {
       const int i = min(r * kEThreads + tid, g.cap - 1);
@@ -136,53 +137,93 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
   const int rounds = kE > 0 ? kE : (n + kEThreads - 1) / kEThreads;
   auto is_guarded = [&](int p) { return p < g.sink || p >= first_recent; };
   auto weight = [&](int r) {
-    if constexpr (kHeld)
+    if constexpr (kRaw)
       return a[r];
     else
       return acc[r * kEThreads + tid];
   };
   auto position = [&](int r) {
-    if constexpr (kHeld)
+    if constexpr (kRaw)
       return ps[r];
     else
       return pos[r * kEThreads + tid];
   };
-  // Round r's slot of this thread: its key, whether it is there, and whether it is guarded.
-  auto at = [&](int r, uint32_t* k, bool* in, bool* gd) {
-    *in = r * kEThreads + tid < n;
-    *k = *in ? weight_key(weight(r)) : 0;
-    *gd = *in && is_guarded(position(r));
-  };
   auto rounds_from = [&](int r0, int r1, auto&& f) {
     if constexpr (kE > 0) {
 #pragma unroll
-      for (int r = 0; r < kE; ++r) f(r);
+      for (int r = 0; r < kE; ++r)
+        if (r * kEThreads < n) f(r);
     } else {
 #pragma unroll 4
       for (int r = r0; r < r1; ++r) f(r);
     }
   };
+  auto rounds_in_memory = [&](int r0, int r1, auto&& f) {  // what needs no keys
+    if constexpr (kRaw) {
+      rounds_from(r0, r1, f);
+    } else {
+#pragma unroll 2
+      for (int r = r0; r < min(r1, (n + kEThreads - 1) / kEThreads); ++r) f(r);
+    }
+  };
+  // choice[r]: one more than the key of round r's slot, 0 where there is none or it is not in the choice
+  uint32_t choice[kHeld ? kE : 1];
+  uint64_t guard = 0;  // a bit a round
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int r = 0; r < kE; ++r) {
+      const bool in = r * kEThreads + tid < n;
+      choice[r] = 0;
+      if (in) choice[r] = 1 + weight_key(weight(r));
+      guard |= uint64_t(in && is_guarded(position(r))) << r;
+    }
+  }
+  auto guarded = [&](int r) {
+    if constexpr (kHeld)
+      return ((guard >> r) & 1) != 0;
+    else
+      return r * kEThreads + tid < n && is_guarded(position(r));
+  };
   __syncthreads();
   uint32_t in_wave = 0;
-  rounds_from(0, rounds, [&](int r) {
-    in_wave += uint32_t(__popcll(__ballot(r * kEThreads + tid < n && is_guarded(position(r)))));
-  });
+  rounds_from(0, rounds, [&](int r) { in_wave += uint32_t(__popcll(__ballot(guarded(r)))); });
   if (lane == 0 && in_wave) atomicAdd(&n_guarded_sh, in_wave);
   __syncthreads();
   // guarded slots: all stay if they fit, else the best of them do and nothing else
   const int n_guarded = int(n_guarded_sh);
   const bool among = n_guarded >= keep;  // whether the choice is among the guarded slots
   uint32_t need = uint32_t(among ? keep : keep - n_guarded);
-  // the key of the need-th best candidate, 8 bits at a time; `need` becomes how many of its equals stay
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int r = 0; r < kE; ++r) choice[r] = guarded(r) == among ? choice[r] : 0;
+  }
+  auto chosen_by = [&](int r) {
+    if constexpr (kHeld) {
+      return choice[r];
+    } else {
+      const bool in = r * kEThreads + tid < n;
+      return in && guarded(r) == among ? 1 + weight_key(weight(r)) : 0u;
+    }
+  };
+  // the number of the need-th best in the choice, 8 bits at a time; `need` becomes how many of its equals stay.  (At
+  // least `need` are in the choice: what is not, 0, is never reached.)
   uint32_t prefix = 0;
 #pragma unroll
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
     rounds_from(0, rounds, [&](int r) {
-      if (r * kEThreads + tid >= n) return;
-      const uint32_t k = weight_key(weight(r));
-      if ((pass == 0 || (k >> (shift + 8)) == (prefix >> (shift + 8))) && is_guarded(position(r)) == among)
+      uint32_t k;
+      if constexpr (kHeld) {
+        k = choice[r];
+      } else {  // (the position is read where the digits before this one fit)
+        if (r * kEThreads + tid >= n) return;
+        k = 1 + weight_key(weight(r));
+      }
+      if (pass == 0 || (k >> (shift + 8)) == (prefix >> (shift + 8))) {
+        if constexpr (!kHeld)
+          if (guarded(r) != among) return;
         atomicAdd(&hist[pass][wave % kHists][255 - ((k >> shift) & 255)], 1u);
+      }
     });
     __syncthreads();
     // descending digits: lane j has the counts of 255 - 4 j down to 252 - 4 j; where the running count reaches `need`
@@ -209,18 +250,16 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
   // half) and survivors (high half).  A count for every 64 slots, one prefix over all counts, the lanes' own.
   uint32_t ties_before = 0, holes_before = 0, late_before = 0;
   auto below = [&](bool x) { return uint32_t(__popcll(__ballot(x) & ((uint64_t(1) << lane) - 1))); };
-  // Exclusive prefix of a count array, which every wave forms for itself: lane j holds counts kPer j .. of it.
+  // Exclusive prefix of a count array (16 a round), which every wave forms for itself: lane j holds counts kPer j ..,
+  // of which the wave needs one.
   struct Prefix {
-    uint32_t v[kPer], total;
-    __device__ __forceinline__ uint32_t of(int i) const {  // i uniform
-      uint32_t x = 0;
-#pragma unroll
-      for (int q = 0; q < kPer; ++q) x = i % kPer == q ? lane_of(v[q], i / kPer) : x;
-      return x;
+    uint32_t mine, total;
+    int shift_lane;
+    __device__ __forceinline__ uint32_t of(int round) const {
+      return lane_of(mine, round * (kEWaves / kPer) + shift_lane);
     }
   };
   auto prefix_of = [&](const uint32_t* counted) {
-    Prefix p;
     uint32_t c[kPer], sum = 0;
 #pragma unroll
     for (int q = 0; q < kPer; ++q) {
@@ -229,39 +268,37 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
     }
     const uint32_t upto = wave_prefix(sum);
     uint32_t run = upto - sum;
+    Prefix p{0, lane_of(upto, 63), wave / kPer};
 #pragma unroll
     for (int q = 0; q < kPer; ++q) {
-      p.v[q] = run;
+      p.mine = wave % kPer == q ? run : p.mine;
       run += c[q];
     }
-    p.total = lane_of(upto, 63);
     return p;
   };
   for (int r0 = 0; r0 < rounds; r0 += kSpan) {
     const int r1 = min(rounds, r0 + kSpan);
-    uint32_t tie = 0, stays = 0;  // a bit a round
+    uint64_t tie = 0, stays = 0;  // a bit a round
     rounds_from(r0, r1, [&](int r) {
-      uint32_t k;
-      bool in, gd;
-      at(r, &k, &in, &gd);
-      const bool t = in && gd == among && k == prefix;
-      tie |= uint32_t(t) << (r - r0);
-      stays |= uint32_t(in && ((gd && !among) || (gd == among && k > prefix))) << (r - r0);
+      const uint32_t k = chosen_by(r);
+      const bool t = k == prefix;
+      tie |= uint64_t(t) << (r - r0);
+      stays |= uint64_t(k > prefix || (!among && guarded(r))) << (r - r0);
       const uint64_t m = __ballot(t);
       if (lane == 0) counts[0][(r - r0) * kEWaves + wave] = uint32_t(__popcll(m));
     });
     __syncthreads();
     {
       const Prefix p = prefix_of(counts[0]);
-      rounds_from(r0, r1, [&](int r) {
+      rounds_in_memory(r0, r1, [&](int r) {
         const bool t = (tie >> (r - r0)) & 1;
-        const uint32_t rank = ties_before + p.of((r - r0) * kEWaves + wave) + below(t);
-        if (t && rank < need) stays |= uint32_t(1) << (r - r0);
+        const uint32_t rank = ties_before + p.of(r - r0) + below(t);
+        if (t && rank < need) stays |= uint64_t(1) << (r - r0);
       });
       ties_before += p.total;
     }
-    // holes in the low half, survivors in the high one: at most 16384 each a span
-    rounds_from(r0, r1, [&](int r) {
+    // holes in the low half, survivors in the high one: at most 32768 each a span
+    rounds_in_memory(r0, r1, [&](int r) {
       const int i = r * kEThreads + tid;
       const bool st = (stays >> (r - r0)) & 1;
       const uint64_t h = __ballot(i < n && i < keep && !st), l = __ballot(st && i >= keep);
@@ -269,10 +306,10 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
     });
     __syncthreads();
     const Prefix p = prefix_of(counts[1]);
-    rounds_from(r0, r1, [&](int r) {  // holes are listed, kept slots below `keep` copied
+    rounds_in_memory(r0, r1, [&](int r) {  // holes are listed, kept slots below `keep` copied
       const int i = r * kEThreads + tid;
       const bool st = (stays >> (r - r0)) & 1, hole = i < n && i < keep && !st;
-      const uint32_t h = holes_before + (p.of((r - r0) * kEWaves + wave) & 0xffff) + below(hole);
+      const uint32_t h = holes_before + (p.of(r - r0) & 0xffff) + below(hole);
       if (hole) {
         if constexpr (kHeld)
           hole_sh[h] = i;
@@ -288,10 +325,10 @@ __global__ __launch_bounds__(kEThreads) void evict_select_kernel(EvictArgs g) {
       }
     });
     __syncthreads();  // every hole that this span's survivors fill is listed: all holes lie before all survivors
-    rounds_from(r0, r1, [&](int r) {
+    rounds_in_memory(r0, r1, [&](int r) {
       const int i = r * kEThreads + tid;
       const bool late = ((stays >> (r - r0)) & 1) && i >= keep;
-      const uint32_t l = late_before + (p.of((r - r0) * kEWaves + wave) >> 16) + below(late);
+      const uint32_t l = late_before + (p.of(r - r0) >> 16) + below(late);
       if (i < n && i >= keep) {
         if (late) {
           int to;
@@ -404,7 +441,9 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   auto select = cap <= kEThreads        ? evict_select_kernel<1>
                 : cap <= 4 * kEThreads  ? evict_select_kernel<4>
                 : cap <= 16 * kEThreads ? evict_select_kernel<16>
-                                                    : evict_select_kernel<0>;
+                : cap <= 32 * kEThreads ? evict_select_kernel<32>
+                : cap <= 64 * kEThreads ? evict_select_kernel<64>
+                                        : evict_select_kernel<0>;
   select<<<dim3(unsigned(groups)), dim3(kEThreads), 0, s>>>(g);
   ESTP_CHECK_LAUNCH("evict_select_kernel");
   if (here) return ESTP_OK;
