@@ -28,17 +28,6 @@ namespace detail {
 
 // ------------------------------------------------------------------ elementwise parts
 
-template <typename T>
-__device__ __forceinline__ float to_f32(T v);
-template <>
-__device__ __forceinline__ float to_f32<float>(float v) {
-  return v;
-}
-template <>
-__device__ __forceinline__ float to_f32<__bf16>(__bf16 v) {
-  return float(v);
-}
-
 // sum over 8 consecutive elements of a[k] b[k]
 __device__ __forceinline__ float dot8(const __bf16* a, const __bf16* b, float s) {
   const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(a), y = *reinterpret_cast<const bf16x8_t*>(b);
@@ -129,15 +118,15 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(const uint4* __restric
 // and for every kernel of a call.
 struct Shares {
   int n;     // shares
-  int rows;  // vocabulary rows of a share, a multiple of 256
+  int rows;  // vocabulary rows of a share, a multiple of 64
 };
 __device__ __forceinline__ Shares dx_shares(int n_live, int d, int Vc, int tile_toks, int wgs, size_t room) {
   const int tiles = (n_live + tile_toks - 1) / tile_toks * ((d + 255) / 256);
   int s = tiles > 0 ? max(1, wgs / tiles) : 1;
-  s = min(s, (Vc + 511) / 512);
+  s = min(s, (Vc + 63) / 64);
   const size_t each = size_t(max(1, n_live)) * d;
   s = int(min(size_t(s), max(size_t(1), room / each)));
-  const int rows = ((Vc + s - 1) / s + 255) / 256 * 256;
+  const int rows = ((Vc + s - 1) / s + 63) / 64 * 64;
   return {(Vc + rows - 1) / rows, rows};
 }
 
@@ -159,164 +148,285 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
   }
 }
 
-// ------------------------------------------------------------------ vector-unit products
+// ------------------------------------------------------------------ matrix-core products (fp32)
 //
-// C[m][n] = sum_k A(m, k) B(n, k) over 128 x 128 tiles, 8 x 8 of them a thread, 16 deep stages held k-major in
-// LDS (double-buffered, the next stage loaded into registers meanwhile).  An operand lies in memory with k
-// contiguous (A[m * ld + k]) or with its rows contiguous (A[k * ld + m]).
-constexpr int kPT = 128, kPK = 16, kPPitch = 132;
+// C[m][n] = sum_k A(m, k) B(n, k) over 128 x 128 tiles on v_mfma_f32_32x32x2_f32 (without packed instructions the
+// vector units reach half its rate), 4 waves of 64 x 64.  Operands lie in memory with k contiguous or strided and
+// reach LDS as they lie, 32 k a stage, two stages of 32 KB, so two workgroups share a compute unit.  A lane of a step
+// gives row lane % 32 at one of two k; any order of the k will do if both sides keep it: of 8 k, step i takes k = i and
+// 4 + i, so that a lane's four values are one 16-byte read where k is contiguous.
+constexpr int kFT = 128, kFK = 32, kFPart = kFT * kFK * 4;
+constexpr int kFLds = 4 * kFPart;
 
-// 128 rows x 16 k of one operand: two groups of 4 elements a thread.
-template <typename T, bool kKContig>
-struct PieceLoad {
-  float v[2][4];
-  // element (r, k) for r < rows, k < depth; elsewhere 0
-  __device__ __forceinline__ void load(const T* p, size_t ld, int rows, int depth, int tid) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int q = tid + 256 * i;
-      const int r = kKContig ? q >> 2 : 4 * (q & 31), k = kKContig ? 4 * (q & 3) : q >> 5;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int rr = kKContig ? r : r + j, kk = kKContig ? k + j : k;
-        v[i][j] = rr < rows && kk < depth ? to_f32<T>(p[kKContig ? size_t(rr) * ld + kk : size_t(kk) * ld + rr]) : 0.f;
-      }
+template <bool kAK, bool kBK>
+struct F32Tile {
+  // byte offset in the source of what lane `lane` of transfer i of 4 brings; *kc: its first k where k is contiguous
+  template <bool kK>
+  __device__ static __forceinline__ uint32_t source(int i, int wave, int lane, uint32_t ld, int* kc) {
+    const int at = 64 * (4 * i + wave) + lane;
+    if (kK) {
+      const int row = at / 8, c = (at % 8) ^ (row & 7);
+      *kc = 4 * c;
+      return uint32_t(row) * ld + uint32_t(c) * 16u;
     }
+    *kc = 0;
+    return uint32_t(at / 32) * ld + uint32_t(at % 32) * 16u;
   }
-  __device__ __forceinline__ void store(float (*lds)[kPPitch], int tid) const {
+  // rows 32 block + lane % 32 at k = 8 g + 4 (lane / 32) .. + 3 of a part in LDS
+  template <bool kK>
+  __device__ static __forceinline__ f32x4_t read(const char* part, int row, int g, int half) {
+    if (kK) return *reinterpret_cast<const f32x4_t*>(part + row * 128 + ((2 * g + half) ^ (row & 7)) * 16);
+    f32x4_t v;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int q = tid + 256 * i;
-      const int r = kKContig ? q >> 2 : 4 * (q & 31), k = kKContig ? 4 * (q & 3) : q >> 5;
+    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(part + (8 * g + 4 * half + i) * 512 + row * 4);
+    return v;
+  }
+  // acc[i][j] = the product over k in [k0, k1) of rows m0 + 64 wm + 32 i, columns n0 + 64 wn + 32 j (mfma32_f32's layout)
+  __device__ static __forceinline__ void run(char* lds, const gemm::Operand& A, const gemm::Operand& B, int m0, int n0,
+                                             int k0, int k1, f32x16_t (&acc)[2][2]) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave & 1, wn = wave >> 1, half = lane >> 5, row = lane & 31;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) lds[kKContig ? k + j : k][kKContig ? r : r + j] = v[i][j];
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    if (k0 >= k1) return;
+    uint32_t off_a[4], off_b[4];
+    int kc_a[4], kc_b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      off_a[i] = source<kAK>(i, wave, lane, A.ld, &kc_a[i]);
+      off_b[i] = source<kBK>(i, wave, lane, B.ld, &kc_b[i]);
+    }
+    auto part = [&](const gemm::Operand& o, bool contig, int r0, int k, const uint32_t (&off)[4], const int (&kc)[4],
+                    char* dst) {
+      const int left = k1 - k;
+      const u32x4_t r = contig ? rsrc_words(o.base + size_t(r0) * o.ld, uint32_t(min(kFT, o.rows - r0)) * o.ld)
+                               : rsrc_words(o.base + size_t(k) * o.ld + size_t(r0) * 4,
+                                            uint32_t(min(kFK, left)) * o.ld - uint32_t(r0) * 4u);
+      const uint32_t soff = contig ? uint32_t(k) * 4u : 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        dma16(r, contig && kc[i] >= left ? kPastEnd : off[i], soff, dst + 1024 * (4 * i + wave));
+    };
+    auto stage = [&](int k, int buf) {
+      part(A, kAK, m0, k, off_a, kc_a, lds + (2 * buf) * kFPart);
+      part(B, kBK, n0, k, off_b, kc_b, lds + (2 * buf + 1) * kFPart);
+    };
+    lds_barrier();  // the last tile's stages are read
+    stage(k0, 0);
+    int buf = 0;
+    for (int k = k0; k < k1; k += kFK, buf ^= 1) {
+      arrived<0>();
+      lds_barrier();  // every wave's transfers of the stage have landed, and its reads of the other are done
+      if (k + kFK < k1) stage(k + kFK, buf ^ 1);
+      const char *pa = lds + 2 * buf * kFPart, *pb = pa + kFPart;
+#pragma unroll
+      for (int g = 0; g < kFK / 8; ++g) {
+        f32x4_t a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          a[i] = read<kAK>(pa, 64 * wm + 32 * i + row, g, half);
+          b[i] = read<kBK>(pb, 64 * wn + 32 * i + row, g, half);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(a[i][q], b[j][q], acc[i][j]);
+      }
     }
   }
 };
 
-// acc[i][j] += the product of the tile at rows m0, columns n0 over k in [k0, k1): rows 4 rv .. + 3 and 64 + 4 rv .. + 3,
-// columns 4 ct .. + 3 and 64 + 4 ct .. + 3 with rv = tid / 16, ct = tid % 16.
-template <typename TA, typename TB, bool kAK, bool kBK>
-__device__ __forceinline__ void tile_product(const TA* A, size_t lda, int M, const TB* B, size_t ldb, int N, int m0,
-                                             int n0, int k0, int k1, float (&acc)[8][8]) {
-  __shared__ __attribute__((aligned(16))) float as[2][kPK][kPPitch];
-  __shared__ __attribute__((aligned(16))) float bs[2][kPK][kPPitch];
-  const int tid = threadIdx.x, rv = tid >> 4, ct = tid & 15;
-  PieceLoad<TA, kAK> la;
-  PieceLoad<TB, kBK> lb;
-  auto load = [&](int k) {
-    la.load(A + (kAK ? size_t(m0) * lda + k : size_t(k) * lda + m0), lda, M - m0, k1 - k, tid);
-    lb.load(B + (kBK ? size_t(n0) * ldb + k : size_t(k) * ldb + n0), ldb, N - n0, k1 - k, tid);
-  };
-  if (k0 >= k1) return;
-  load(k0);
-  la.store(as[0], tid);
-  lb.store(bs[0], tid);
-  __syncthreads();
-  int buf = 0;
-  for (int k = k0; k < k1; k += kPK, buf ^= 1) {
-    const bool more = k + kPK < k1;
-    if (more) load(k + kPK);
+// What a lane of F32Tile's products holds: columns n0 + 64 wn + 32 j + lane % 32, and of each 32 rows
+// m0 + 64 wm + 32 i the four runs of four from 8 q + 4 (lane / 32).
+struct F32Lane {
+  int m, n;
+  __device__ __forceinline__ F32Lane(int m0, int n0) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    m = m0 + 64 * (wave & 1) + 4 * (lane >> 5);
+    n = n0 + 64 * (wave >> 1) + (lane & 31);
+  }
+};
+
+// Running (maximum, sum) in base 2 of every token's logits over a slice of the vocabulary tiles: slice s of n_slices
+// takes tiles s, s + n_slices, ...; the two row halves of a tile have states of their own.  Partial states
+// [2 n_slices, n_tok].
+__global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __restrict__ X, const float* __restrict__ W,
+                                                              int n_tok, int d, int V, int n_slices,
+                                                              float* __restrict__ part_m, float* __restrict__ part_s) {
+  __shared__ __attribute__((aligned(16))) char lds[kFLds];
+  const int slice = blockIdx.x % n_slices, n0 = blockIdx.x / n_slices * kFT;
+  const gemm::Operand A{reinterpret_cast<const char*>(W), uint32_t(d) * 4u, V};
+  const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 4u, n_tok};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  for (int64_t m0 = int64_t(slice) * kFT; m0 < V; m0 += int64_t(n_slices) * kFT) {
+    f32x16_t acc[2][2];
+    F32Tile<true, true>::run(lds, A, B, int(m0), n0, 0, d, acc);
+    const F32Lane at(int(m0), n0);
 #pragma unroll
-    for (int q = 0; q < kPK; ++q) {
-      float a[8], b[8];
+    for (int j = 0; j < 2; ++j) {
+      float mx = m[j];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4_t x = *reinterpret_cast<const f32x4_t*>(&as[buf][q][64 * h + 4 * rv]);
-        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&bs[buf][q][64 * h + 4 * ct]);
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a[4 * h + j] = x[j];
-          b[4 * h + j] = y[j];
+        for (int r = 0; r < 16; ++r) {
+          const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
+          mx = fmaxf(mx, live ? acc[i][j][r] * kLog2e : -INFINITY);
         }
-      }
+      const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
+      float sum = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        for (int r = 0; r < 16; ++r) {
+          const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
+          sum += live ? fast_exp2(fmaf(acc[i][j][r], kLog2e, -ref)) : 0.f;
+        }
+      m[j] = mx;
+      l[j] = sum;
     }
-    if (more) {
-      la.store(as[buf ^ 1], tid);
-      lb.store(bs[buf ^ 1], tid);
+  }
+  const F32Lane at(0, n0);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float mo = __shfl_xor(m[j], 32, 64), lo = __shfl_xor(l[j], 32, 64), M = fmaxf(m[j], mo);
+    const float ref = fmaxf(M, -0x1p127f);
+    const float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor)) + lo * fast_exp2(fmaxf(mo - ref, kExp2Floor));
+    const int tok = at.n + 32 * j;
+    if ((threadIdx.x & 32) == 0 && tok < n_tok) {
+      const size_t o = size_t(2 * slice + ((threadIdx.x >> 6) & 1)) * n_tok + tok;
+      part_m[o] = M;
+      part_s[o] = s;
     }
-    __syncthreads();
   }
 }
-__device__ __forceinline__ int tile_at(int group, int i) { return (i < 4 ? 4 * group + i : 64 + 4 * group + i - 4); }
 
-// G[slot][v] of vocabulary rows v0 .. v0 + Vc (columns past V: 0), pitch Vc.
-template <typename T>
-__global__ __launch_bounds__(256) void loss_grad_kernel(const T* __restrict__ Xc, const T* __restrict__ W,
-                                                        const int* __restrict__ n_live, int d, int V, int64_t v0,
-                                                        int Vc, const int32_t* __restrict__ tc,
-                                                        const float* __restrict__ lc, const float* __restrict__ gc,
-                                                        T* __restrict__ G) {
-  const int n = n_live[0], m0 = blockIdx.y * kPT, c0 = blockIdx.x * kPT;
-  if (m0 >= n) return;
+// lse of every token from its n partial states: 16 lanes a token take every 16th.
+__global__ __launch_bounds__(256) void loss_lse_merge_kernel(const float* __restrict__ part_m,
+                                                             const float* __restrict__ part_s, int n_tok, int n,
+                                                             float* __restrict__ lse) {
+  __shared__ float sh_m[16][17], sh_s[16][17];
+  const int t = threadIdx.x & 15, q = threadIdx.x >> 4, tok = blockIdx.x * 16 + t;
+  float M = -INFINITY, s = 0.f;
+  if (tok < n_tok)
+#pragma unroll 4
+    for (int p = q; p < n; p += 16) {
+      const float m = part_m[size_t(p) * n_tok + tok], l = part_s[size_t(p) * n_tok + tok];
+      const float top = fmaxf(M, m), ref = fmaxf(top, -0x1p127f);
+      s = s * fast_exp2(fmaxf(M - ref, kExp2Floor)) + l * fast_exp2(fmaxf(m - ref, kExp2Floor));
+      M = top;
+    }
+  sh_m[q][t] = M;
+  sh_s[q][t] = s;
+  __syncthreads();
+  if (q != 0 || tok >= n_tok) return;
+  for (int p = 1; p < 16; ++p) M = fmaxf(M, sh_m[p][t]);
+  const float ref = fmaxf(M, -0x1p127f);
+  s = 0.f;
+  for (int p = 0; p < 16; ++p) s += sh_s[p][t] * fast_exp2(fmaxf(sh_m[p][t] - ref, kExp2Floor));
+  lse[tok] = kLn2 * (M + fast_log2(s));
+}
+
+// G[slot][v] of vocabulary rows v0 .. v0 + Vc (columns past V: 0), pitch Vc.  M side: vocabulary rows.
+__global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __restrict__ Xc,
+                                                               const float* __restrict__ W,
+                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                               int Vc, const int32_t* __restrict__ tc,
+                                                               const float* __restrict__ lc,
+                                                               const float* __restrict__ gc, float* __restrict__ G) {
+  __shared__ __attribute__((aligned(16))) char lds[kFLds];
+  const int n = n_live[0], n0 = blockIdx.y * kFT, m0 = blockIdx.x * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
-  float acc[8][8] = {};
-  tile_product<T, T, true, true>(Xc, d, n, W + size_t(v0) * d, d, rows, m0, c0, 0, d, acc);
-  const int rv = threadIdx.x >> 4, ct = threadIdx.x & 15;
+  if (n0 >= n || m0 >= rows) return;
+  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, rows};
+  const gemm::Operand B{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, n};
+  f32x16_t acc[2][2];
+  F32Tile<true, true>::run(lds, A, B, m0, n0, 0, d, acc);
+  const F32Lane at(m0, n0);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int s = m0 + tile_at(rv, i);
+  for (int j = 0; j < 2; ++j) {
+    const int s = at.n + 32 * j;
     if (s >= n) continue;
     const int t = int(tc[s] - v0);
-    const float l2 = lc[s] * kLog2e, g = gc[s];
+    const float l = lc[s], g = gc[s];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int c = c0 + tile_at(ct, j);
-      if (c >= Vc) continue;
-      const float p = fast_exp2(fmaf(acc[i][j], kLog2e, -l2)) - (c == t ? 1.f : 0.f);
-      G[size_t(s) * Vc + c] = T(c < rows ? g * p : 0.f);
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int v = at.m + 32 * i + 8 * q;
+        f32x4_t out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          // (z - lse first: near 0 for the weights that matter, so its product is exact to its own rounding)
+          const float p = fast_exp2((acc[i][j][4 * q + e] - l) * kLog2e) - (v + e == t ? 1.f : 0.f);
+          out[e] = v + e < rows ? g * p : 0.f;
+        }
+        *reinterpret_cast<f32x4_t*>(G + size_t(s) * Vc + v) = out;
+      }
   }
 }
 
-// out[s][k] (+)= sum over the blockIdx.z-th share of the piece's vocabulary rows of G[s][v] W[v0 + v][k]
-template <typename T>
-__global__ __launch_bounds__(256) void loss_dx_piece_kernel(const T* __restrict__ G, const T* __restrict__ W,
-                                                            const int* __restrict__ n_live, int d, int V, int64_t v0,
-                                                            int Vc, int wgs, size_t room, bool first,
-                                                            float* __restrict__ out) {
-  const int n = n_live[0], m0 = blockIdx.y * kPT, n0 = blockIdx.x * kPT;
-  const Shares sh = dx_shares(n, d, Vc, kPT, wgs, room);
-  if (m0 >= n || int(blockIdx.z) >= sh.n) return;
+// out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W.
+__global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __restrict__ G, const float* __restrict__ W,
+                                                             const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                             int Vc, int wgs, size_t room, bool first,
+                                                             float* __restrict__ out) {
+  __shared__ __attribute__((aligned(16))) char lds[kFLds];
+  const int n = n_live[0], n0 = blockIdx.y * kFT, m0 = blockIdx.x * kFT;
+  const Shares sh = dx_shares(n, d, Vc, kFT, wgs, room);
+  if (n0 >= n || int(blockIdx.z) >= sh.n) return;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
-  const int k0 = min(rows, int(blockIdx.z) * sh.rows), k1 = min(rows, k0 + sh.rows);
-  float acc[8][8] = {};
-  tile_product<T, T, true, false>(G, Vc, n, W + size_t(v0) * d, d, d, m0, n0, k0, k1, acc);
+  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, d};
+  const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, n};
+  f32x16_t acc[2][2];
+  F32Tile<false, true>::run(lds, A, B, m0, n0, min(rows, int(blockIdx.z) * sh.rows),
+                            min(rows, (int(blockIdx.z) + 1) * sh.rows), acc);
   out += size_t(blockIdx.z) * size_t(n) * d;
-  const int rv = threadIdx.x >> 4, ct = threadIdx.x & 15;
+  const F32Lane at(m0, n0);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int s = m0 + tile_at(rv, i), k = n0 + tile_at(ct, j);
-      if (s >= n || k >= d) continue;
-      float* o = out + size_t(s) * d + k;
-      *o = first ? acc[i][j] : *o + acc[i][j];
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int s = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
+        if (s >= n || k >= d) continue;
+        f32x4_t* o = reinterpret_cast<f32x4_t*>(out + size_t(s) * d + k);
+        f32x4_t v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        if (!first) v += *o;
+        *o = v;
+      }
 }
 
-// dW[v0 + v][k] = sum over the live tokens of G[s][v] Xc[s][k]
-template <typename T>
-__global__ __launch_bounds__(256) void loss_dw_kernel(const T* __restrict__ G, const T* __restrict__ Xc,
-                                                      const int* __restrict__ n_live, int d, int V, int64_t v0, int Vc,
-                                                      T* __restrict__ dW) {
-  const int n = n_live[0], m0 = blockIdx.y * kPT, n0 = blockIdx.x * kPT;
+// dW[v0 + v][k] = sum over the live tokens of G[s][v] Xc[s][k].  M side: columns k of Xc, N side: vocabulary rows.
+__global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __restrict__ G, const float* __restrict__ Xc,
+                                                             const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                             int Vc, float* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) char lds[kFLds];
+  const int n = n_live[0], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
-  if (m0 >= rows) return;
-  float acc[8][8] = {};
-  tile_product<T, T, false, false>(G, Vc, rows, Xc, d, d, m0, n0, 0, n, acc);
-  const int rv = threadIdx.x >> 4, ct = threadIdx.x & 15;
+  if (n0 >= rows) return;
+  const gemm::Operand A{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, d};
+  const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, Vc};
+  f32x16_t acc[2][2];
+  F32Tile<false, false>::run(lds, A, B, m0, n0, 0, n, acc);
+  const F32Lane at(m0, n0);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int v = m0 + tile_at(rv, i), k = n0 + tile_at(ct, j);
-      if (v < rows && k < d) dW[(size_t(v0) + v) * d + k] = T(acc[i][j]);
-    }
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int v = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
+        if (v >= rows || k >= d) continue;
+        *reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v) * d + k) =
+            f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+      }
 }
 
 // ------------------------------------------------------------------ matrix-core products (bf16)
@@ -507,9 +617,9 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
   LossPlan p;
   p.Vc = int(vc);
-  p.tile_toks = dtype == ESTP_F32 ? kPT : n_tok <= 128 ? 128 : 256;
+  p.tile_toks = dtype == ESTP_F32 ? kFT : n_tok <= 128 ? 128 : 256;
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
-  p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 511) / 512));
+  p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
 }
 
@@ -571,19 +681,19 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dw_mfma_kernel");
       }
     } else {
-      const unsigned n_tt = unsigned((n + kPT - 1) / kPT), n_dt = unsigned((d + kPT - 1) / kPT);
-      const unsigned n_vt = unsigned((p.Vc + kPT - 1) / kPT);
-      loss_grad_kernel<T><<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
-      ESTP_CHECK_LAUNCH("loss_grad_kernel");
+      const unsigned n_tt = unsigned((n + kFT - 1) / kFT), n_dt = unsigned((d + kFT - 1) / kFT);
+      const unsigned n_vt = unsigned((p.Vc + kFT - 1) / kFT);
+      loss_grad_f32_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      ESTP_CHECK_LAUNCH("loss_grad_f32_kernel");
       if (dX) {
-        const unsigned shares = unsigned(std::min<int64_t>(kWgs, (p.Vc + 511) / 512));
-        loss_dx_piece_kernel<T><<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs,
-                                                                           b.room, v0 == 0, b.acc);
-        ESTP_CHECK_LAUNCH("loss_dx_piece_kernel");
+        const unsigned shares = unsigned(std::min<int64_t>(kWgs, (p.Vc + 63) / 64));
+        loss_dx_f32_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room,
+                                                                      v0 == 0, b.acc);
+        ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
-        loss_dw_kernel<T><<<dim3(n_dt, n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
-        ESTP_CHECK_LAUNCH("loss_dw_kernel");
+        loss_dw_f32_kernel<<<dim3(n_dt, n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
+        ESTP_CHECK_LAUNCH("loss_dw_f32_kernel");
       }
     }
   }
@@ -601,8 +711,22 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
 using namespace estp;
 using namespace estp::detail;
 
+namespace {
+
+// Slices of the vocabulary tiles of a fp32 call: two workgroups for every compute unit, at least 4 slices.
+int loss_f32_slices(int64_t n_tok, int V) {
+  const int64_t n_vt = (int64_t(V) + kFT - 1) / kFT, n_tt = (n_tok + kFT - 1) / kFT;
+  return int(std::min<int64_t>(n_vt, std::max<int64_t>(4, 512 / n_tt)));
+}
+
+}  // namespace
+
 extern "C" size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
-  return estp_token_entropy_workspace_size(n_tok, d, V, dtype);
+  const size_t entropy = estp_token_entropy_workspace_size(n_tok, d, V, dtype);
+  if (entropy == 0 || dtype != ESTP_F32) return entropy;
+  Carver c(nullptr);
+  for (int i = 0; i < 2; ++i) c.take<float>(2 * size_t(loss_f32_slices(n_tok, V)) * size_t(n_tok));
+  return std::max(entropy, c.bytes());
 }
 
 extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d,
@@ -622,8 +746,23 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
                "%s: workspace must be non-null and 256-byte aligned", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
-  const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
-  if (rc != ESTP_OK) return rc;
+  if (dtype == ESTP_F32 && !H && !vocab_argmax) {
+    // maximum and sum alone, on the fp32 matrix cores (the entropy kernel of fp32 inputs runs on the vector units)
+    const int slices = loss_f32_slices(n_tok, V);
+    Carver c(workspace);
+    float* pm = c.take<float>(2 * size_t(slices) * size_t(n_tok));
+    float* ps = c.take<float>(2 * size_t(slices) * size_t(n_tok));
+    const size_t wgs = size_t((n_tok + kFT - 1) / kFT) * size_t(slices);
+    ESTP_REQUIRE(fits_launch(wgs, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
+    loss_lse_f32_kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X),
+                                                                  static_cast<const float*>(W), n, d, V, slices, pm, ps);
+    ESTP_CHECK_LAUNCH("loss_lse_f32_kernel");
+    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, 2 * slices, lse);
+    ESTP_CHECK_LAUNCH("loss_lse_merge_kernel");
+  } else {
+    const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
+    if (rc != ESTP_OK) return rc;
+  }
   const dim3 grid(unsigned((n_tok + 3) / 4)), block(256);
   if (dtype == ESTP_F32)
     loss_pick_kernel<float><<<grid, block, 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), targets,
