@@ -150,16 +150,28 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
 
 // ------------------------------------------------------------------ matrix-core products (fp32)
 //
-// C[m][n] = sum_k A(m, k) B(n, k) over 128 x 128 tiles on v_mfma_f32_32x32x2_f32 (without packed instructions the
-// vector units reach half its rate), 4 waves of 64 x 64.  Operands lie in memory with k contiguous or strided and
-// reach LDS as they lie, 32 k a stage, two stages of 32 KB, so two workgroups share a compute unit.  A lane of a step
+// C[m][n] = sum_k A(m, k) B(n, k) over 128 x kTN tiles on v_mfma_f32_32x32x2_f32 (without packed instructions the
+// vector units reach half its rate), 4 waves of 64 x 64, or of 32 x kTN for the 64 and 32 columns of few tokens.  Operands lie in memory with k contiguous or strided and
+// reach LDS as they lie, 32 k a stage, two stages of at most 32 KB, so two or more workgroups share a compute unit.  A lane of a step
 // gives row lane % 32 at one of two k; any order of the k will do if both sides keep it: of 8 k, step i takes k = i and
 // 4 + i, so that a lane's four values are one 16-byte read where k is contiguous.
 constexpr int kFT = 128, kFK = 32, kFPart = kFT * kFK * 4;
-constexpr int kFLds = 4 * kFPart;
 
-template <bool kAK, bool kBK>
+template <bool kAK, bool kBK, int kTN>
 struct F32Tile {
+  static_assert(kTN == kFT || kBK, "few columns: k contiguous");
+  static constexpr int kWM = kTN == kFT ? 2 : 4;            // waves along the rows
+  static constexpr int kMI = kFT / 32 / kWM, kNJ = kTN == kFT ? 2 : kTN / 32;  // 32 x 32 blocks of a wave
+  static constexpr int kPartB = kTN * kFK * 4, kStage = kFPart + kPartB, kLds = 2 * kStage, kLB = kTN / 32;
+  using Acc = f32x16_t[kMI][kNJ];
+  // What a lane holds: columns n + 32 j, and of each 32 rows from m + 32 i the four runs of four at 8 q.
+  struct At {
+    int m, n, wm;
+  };
+  __device__ static __forceinline__ At place(int m0, int n0) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % kWM;
+    return {m0 + 32 * kMI * wm + 4 * (lane >> 5), n0 + 32 * kNJ * (wave / kWM) + (lane & 31), wm};
+  }
   // byte offset in the source of what lane `lane` of transfer i of 4 brings; *kc: its first k where k is contiguous
   template <bool kK>
   __device__ static __forceinline__ uint32_t source(int i, int wave, int lane, uint32_t ld, int* kc) {
@@ -181,39 +193,40 @@ struct F32Tile {
     for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(part + (8 * g + 4 * half + i) * 512 + row * 4);
     return v;
   }
-  // acc[i][j] = the product over k in [k0, k1) of rows m0 + 64 wm + 32 i, columns n0 + 64 wn + 32 j (mfma32_f32's layout)
+  // acc[i][j] = the product over k in [k0, k1) of the wave's 32 x 32 blocks (mfma32_f32's layout)
   __device__ static __forceinline__ void run(char* lds, const gemm::Operand& A, const gemm::Operand& B, int m0, int n0,
-                                             int k0, int k1, f32x16_t (&acc)[2][2]) {
+                                             int k0, int k1, Acc& acc) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave & 1, wn = wave >> 1, half = lane >> 5, row = lane & 31;
+    const int wm = wave % kWM, wn = wave / kWM, half = lane >> 5, row = lane & 31;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kMI; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j = 0; j < kNJ; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
     if (k0 >= k1) return;
-    uint32_t off_a[4], off_b[4];
-    int kc_a[4], kc_b[4];
+    uint32_t off_a[4], off_b[kLB];
+    int kc_a[4], kc_b[kLB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      off_a[i] = source<kAK>(i, wave, lane, A.ld, &kc_a[i]);
-      off_b[i] = source<kBK>(i, wave, lane, B.ld, &kc_b[i]);
-    }
-    auto part = [&](const gemm::Operand& o, bool contig, int r0, int k, const uint32_t (&off)[4], const int (&kc)[4],
-                    char* dst) {
+    for (int i = 0; i < 4; ++i) off_a[i] = source<kAK>(i, wave, lane, A.ld, &kc_a[i]);
+#pragma unroll
+    for (int i = 0; i < kLB; ++i) off_b[i] = source<kBK>(i, wave, lane, B.ld, &kc_b[i]);
+    auto part = [&](auto contig, auto n_parts, const gemm::Operand& o, int r0, int rows, int k, const uint32_t* off,
+                    const int* kc, char* dst) {
+      constexpr bool kContig = decltype(contig)::value;
       const int left = k1 - k;
-      const u32x4_t r = contig ? rsrc_words(o.base + size_t(r0) * o.ld, uint32_t(min(kFT, o.rows - r0)) * o.ld)
-                               : rsrc_words(o.base + size_t(k) * o.ld + size_t(r0) * 4,
-                                            uint32_t(min(kFK, left)) * o.ld - uint32_t(r0) * 4u);
-      const uint32_t soff = contig ? uint32_t(k) * 4u : 0u;
+      const u32x4_t r = kContig ? rsrc_words(o.base + size_t(r0) * o.ld, uint32_t(min(rows, o.rows - r0)) * o.ld)
+                                : rsrc_words(o.base + size_t(k) * o.ld + size_t(r0) * 4,
+                                             uint32_t(min(kFK, left)) * o.ld - uint32_t(r0) * 4u);
+      const uint32_t soff = kContig ? uint32_t(k) * 4u : 0u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        dma16(r, contig && kc[i] >= left ? kPastEnd : off[i], soff, dst + 1024 * (4 * i + wave));
+      for (int i = 0; i < decltype(n_parts)::value; ++i)
+        dma16(r, kContig && kc[i] >= left ? kPastEnd : off[i], soff, dst + 1024 * (4 * i + wave));
     };
     auto stage = [&](int k, int buf) {
-      part(A, kAK, m0, k, off_a, kc_a, lds + (2 * buf) * kFPart);
-      part(B, kBK, n0, k, off_b, kc_b, lds + (2 * buf + 1) * kFPart);
+      part(std::bool_constant<kAK>{}, std::integral_constant<int, 4>{}, A, m0, kFT, k, off_a, kc_a, lds + buf * kStage);
+      part(std::bool_constant<kBK>{}, std::integral_constant<int, kLB>{}, B, n0, kTN, k, off_b, kc_b,
+           lds + buf * kStage + kFPart);
     };
     lds_barrier();  // the last tile's stages are read
     stage(k0, 0);
@@ -222,57 +235,52 @@ struct F32Tile {
       arrived<0>();
       lds_barrier();  // every wave's transfers of the stage have landed, and its reads of the other are done
       if (k + kFK < k1) stage(k + kFK, buf ^ 1);
-      const char *pa = lds + 2 * buf * kFPart, *pb = pa + kFPart;
+      const char *pa = lds + buf * kStage, *pb = pa + kFPart;
 #pragma unroll
       for (int g = 0; g < kFK / 8; ++g) {
-        f32x4_t a[2], b[2];
+        f32x4_t a[kMI], b[kNJ];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          a[i] = read<kAK>(pa, 64 * wm + 32 * i + row, g, half);
-          b[i] = read<kBK>(pb, 64 * wn + 32 * i + row, g, half);
-        }
+        for (int i = 0; i < kMI; ++i) a[i] = read<kAK>(pa, 32 * (kMI * wm + i) + row, g, half);
+#pragma unroll
+        for (int j = 0; j < kNJ; ++j) b[j] = read<kBK>(pb, 32 * (kNJ * wn + j) + row, g, half);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < kMI; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(a[i][q], b[j][q], acc[i][j]);
+            for (int j = 0; j < kNJ; ++j) acc[i][j] = mfma32_f32(a[i][q], b[j][q], acc[i][j]);
       }
     }
   }
 };
 
-// What a lane of F32Tile's products holds: columns n0 + 64 wn + 32 j + lane % 32, and of each 32 rows
-// m0 + 64 wm + 32 i the four runs of four from 8 q + 4 (lane / 32).
-struct F32Lane {
-  int m, n;
-  __device__ __forceinline__ F32Lane(int m0, int n0) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    m = m0 + 64 * (wave & 1) + 4 * (lane >> 5);
-    n = n0 + 64 * (wave >> 1) + (lane & 31);
-  }
-};
-
 // Running (maximum, sum) in base 2 of every token's logits over a slice of the vocabulary tiles: slice s of n_slices
-// takes tiles s, s + n_slices, ...; the two row halves of a tile have states of their own.  Partial states
-// [2 n_slices, n_tok].
+// takes tiles s, s + n_slices, ...; each wave's rows of a tile have a state of their own.  Partial states
+// [kWM n_slices, n_tok].
+template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __restrict__ X, const float* __restrict__ W,
                                                               int n_tok, int d, int V, int n_slices,
                                                               float* __restrict__ part_m, float* __restrict__ part_s) {
-  __shared__ __attribute__((aligned(16))) char lds[kFLds];
-  const int slice = blockIdx.x % n_slices, n0 = blockIdx.x / n_slices * kFT;
+  using Run = F32Tile<true, true, kTN>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const int slice = blockIdx.x % n_slices, n0 = blockIdx.x / n_slices * kTN;
   const gemm::Operand A{reinterpret_cast<const char*>(W), uint32_t(d) * 4u, V};
   const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 4u, n_tok};
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-  for (int64_t m0 = int64_t(slice) * kFT; m0 < V; m0 += int64_t(n_slices) * kFT) {
-    f32x16_t acc[2][2];
-    F32Tile<true, true>::run(lds, A, B, int(m0), n0, 0, d, acc);
-    const F32Lane at(int(m0), n0);
+  float m[Run::kNJ], l[Run::kNJ];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < Run::kNJ; ++j) {
+    m[j] = -INFINITY;
+    l[j] = 0.f;
+  }
+  for (int64_t m0 = int64_t(slice) * kFT; m0 < V; m0 += int64_t(n_slices) * kFT) {
+    typename Run::Acc acc;
+    Run::run(lds, A, B, int(m0), n0, 0, d, acc);
+    const auto at = Run::place(int(m0), n0);
+#pragma unroll
+    for (int j = 0; j < Run::kNJ; ++j) {
       float mx = m[j];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
@@ -281,7 +289,7 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
       const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
       float sum = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
@@ -291,15 +299,15 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
       l[j] = sum;
     }
   }
-  const F32Lane at(0, n0);
+  const auto at = Run::place(0, n0);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < Run::kNJ; ++j) {
     const float mo = __shfl_xor(m[j], 32, 64), lo = __shfl_xor(l[j], 32, 64), M = fmaxf(m[j], mo);
     const float ref = fmaxf(M, -0x1p127f);
     const float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor)) + lo * fast_exp2(fmaxf(mo - ref, kExp2Floor));
     const int tok = at.n + 32 * j;
     if ((threadIdx.x & 32) == 0 && tok < n_tok) {
-      const size_t o = size_t(2 * slice + ((threadIdx.x >> 6) & 1)) * n_tok + tok;
+      const size_t o = size_t(Run::kWM * slice + at.wm) * n_tok + tok;
       part_m[o] = M;
       part_s[o] = s;
     }
@@ -333,29 +341,31 @@ __global__ __launch_bounds__(256) void loss_lse_merge_kernel(const float* __rest
 }
 
 // G[slot][v] of vocabulary rows v0 .. v0 + Vc (columns past V: 0), pitch Vc.  M side: vocabulary rows.
+template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __restrict__ Xc,
                                                                const float* __restrict__ W,
                                                                const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                                int Vc, const int32_t* __restrict__ tc,
                                                                const float* __restrict__ lc,
                                                                const float* __restrict__ gc, float* __restrict__ G) {
-  __shared__ __attribute__((aligned(16))) char lds[kFLds];
-  const int n = n_live[0], n0 = blockIdx.y * kFT, m0 = blockIdx.x * kFT;
+  using Run = F32Tile<true, true, kTN>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const int n = n_live[0], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   if (n0 >= n || m0 >= rows) return;
   const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, rows};
   const gemm::Operand B{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, n};
-  f32x16_t acc[2][2];
-  F32Tile<true, true>::run(lds, A, B, m0, n0, 0, d, acc);
-  const F32Lane at(m0, n0);
+  typename Run::Acc acc;
+  Run::run(lds, A, B, m0, n0, 0, d, acc);
+  const auto at = Run::place(m0, n0);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < Run::kNJ; ++j) {
     const int s = at.n + 32 * j;
     if (s >= n) continue;
     const int t = int(tc[s] - v0);
     const float l = lc[s], g = gc[s];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int v = at.m + 32 * i + 8 * q;
@@ -372,26 +382,28 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
 }
 
 // out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W.
+template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __restrict__ G, const float* __restrict__ W,
                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                              int Vc, int wgs, size_t room, bool first,
                                                              float* __restrict__ out) {
-  __shared__ __attribute__((aligned(16))) char lds[kFLds];
-  const int n = n_live[0], n0 = blockIdx.y * kFT, m0 = blockIdx.x * kFT;
-  const Shares sh = dx_shares(n, d, Vc, kFT, wgs, room);
+  using Run = F32Tile<false, true, kTN>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const int n = n_live[0], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
+  const Shares sh = dx_shares(n, d, Vc, kTN, wgs, room);
   if (n0 >= n || int(blockIdx.z) >= sh.n) return;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, d};
   const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, n};
-  f32x16_t acc[2][2];
-  F32Tile<false, true>::run(lds, A, B, m0, n0, min(rows, int(blockIdx.z) * sh.rows),
+  typename Run::Acc acc;
+  Run::run(lds, A, B, m0, n0, min(rows, int(blockIdx.z) * sh.rows),
                             min(rows, (int(blockIdx.z) + 1) * sh.rows), acc);
   out += size_t(blockIdx.z) * size_t(n) * d;
-  const F32Lane at(m0, n0);
+  const auto at = Run::place(m0, n0);
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < Run::kNJ; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int s = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
@@ -407,15 +419,16 @@ __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __rest
 __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __restrict__ G, const float* __restrict__ Xc,
                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                              int Vc, float* __restrict__ dW) {
-  __shared__ __attribute__((aligned(16))) char lds[kFLds];
+  using Run = F32Tile<false, false, kFT>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
   const int n = n_live[0], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   if (n0 >= rows) return;
   const gemm::Operand A{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, d};
   const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, Vc};
-  f32x16_t acc[2][2];
-  F32Tile<false, false>::run(lds, A, B, m0, n0, 0, n, acc);
-  const F32Lane at(m0, n0);
+  Run::Acc acc;
+  Run::run(lds, A, B, m0, n0, 0, n, acc);
+  const auto at = Run::place(m0, n0);
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -609,6 +622,9 @@ struct LossPlan {
   int tile_toks;
 };
 
+// Tokens of a fp32 tile.
+inline int f32_tile_toks(int64_t n_tok) { return n_tok <= 32 ? 32 : n_tok <= 64 ? 64 : kFT; }
+
 inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   const size_t es = dtype == ESTP_F32 ? 4 : 2;
   const int64_t tok_pad = (n_tok + 255) / 256 * 256;
@@ -617,7 +633,7 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
   LossPlan p;
   p.Vc = int(vc);
-  p.tile_toks = dtype == ESTP_F32 ? kFT : n_tok <= 128 ? 128 : 256;
+  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : n_tok <= 128 ? 128 : 256;
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -681,13 +697,19 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dw_mfma_kernel");
       }
     } else {
-      const unsigned n_tt = unsigned((n + kFT - 1) / kFT), n_dt = unsigned((d + kFT - 1) / kFT);
+      const unsigned n_tt = unsigned((n + p.tile_toks - 1) / p.tile_toks), n_dt = unsigned((d + kFT - 1) / kFT);
       const unsigned n_vt = unsigned((p.Vc + kFT - 1) / kFT);
-      loss_grad_f32_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      auto grad_kernel = p.tile_toks == 32   ? loss_grad_f32_kernel<32>
+                         : p.tile_toks == 64 ? loss_grad_f32_kernel<64>
+                                             : loss_grad_f32_kernel<kFT>;
+      grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
       ESTP_CHECK_LAUNCH("loss_grad_f32_kernel");
       if (dX) {
         const unsigned shares = unsigned(std::min<int64_t>(kWgs, (p.Vc + 63) / 64));
-        loss_dx_f32_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room,
+        auto dx_kernel = p.tile_toks == 32   ? loss_dx_f32_kernel<32>
+                         : p.tile_toks == 64 ? loss_dx_f32_kernel<64>
+                                             : loss_dx_f32_kernel<kFT>;
+        dx_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room,
                                                                       v0 == 0, b.acc);
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
@@ -713,10 +735,13 @@ using namespace estp::detail;
 
 namespace {
 
-// Slices of the vocabulary tiles of a fp32 call: two workgroups for every compute unit, at least 4 slices.
+// Slices of the vocabulary tiles of a fp32 call: two workgroups for every compute unit (four of the smaller ones), at least 4 slices.
 int loss_f32_slices(int64_t n_tok, int V) {
-  const int64_t n_vt = (int64_t(V) + kFT - 1) / kFT, n_tt = (n_tok + kFT - 1) / kFT;
-  return int(std::min<int64_t>(n_vt, std::max<int64_t>(4, 512 / n_tt)));
+  const int64_t n_vt = (int64_t(V) + kFT - 1) / kFT, tile = f32_tile_toks(n_tok), n_tt = (n_tok + tile - 1) / tile;
+  return int(std::min<int64_t>(n_vt, std::max<int64_t>(4, (tile < kFT ? 1024 : 512) / n_tt)));
+}
+size_t loss_f32_states(int64_t n_tok, int V) {  // of a token
+  return size_t(f32_tile_toks(n_tok) < kFT ? 4 : 2) * size_t(loss_f32_slices(n_tok, V));
 }
 
 }  // namespace
@@ -725,7 +750,7 @@ extern "C" size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32
   const size_t entropy = estp_token_entropy_workspace_size(n_tok, d, V, dtype);
   if (entropy == 0 || dtype != ESTP_F32) return entropy;
   Carver c(nullptr);
-  for (int i = 0; i < 2; ++i) c.take<float>(2 * size_t(loss_f32_slices(n_tok, V)) * size_t(n_tok));
+  for (int i = 0; i < 2; ++i) c.take<float>(loss_f32_states(n_tok, V) * size_t(n_tok));
   return std::max(entropy, c.bytes());
 }
 
@@ -750,14 +775,17 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
     // maximum and sum alone, on the fp32 matrix cores (the entropy kernel of fp32 inputs runs on the vector units)
     const int slices = loss_f32_slices(n_tok, V);
     Carver c(workspace);
-    float* pm = c.take<float>(2 * size_t(slices) * size_t(n_tok));
-    float* ps = c.take<float>(2 * size_t(slices) * size_t(n_tok));
-    const size_t wgs = size_t((n_tok + kFT - 1) / kFT) * size_t(slices);
+    const size_t states = loss_f32_states(n_tok, V);
+    float* pm = c.take<float>(states * size_t(n_tok));
+    float* ps = c.take<float>(states * size_t(n_tok));
+    const int tile = f32_tile_toks(n_tok);
+    const size_t wgs = size_t((n_tok + tile - 1) / tile) * size_t(slices);
     ESTP_REQUIRE(fits_launch(wgs, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
-    loss_lse_f32_kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X),
-                                                                  static_cast<const float*>(W), n, d, V, slices, pm, ps);
+    auto kernel = tile == 32 ? loss_lse_f32_kernel<32> : tile == 64 ? loss_lse_f32_kernel<64> : loss_lse_f32_kernel<kFT>;
+    kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), n, d, V,
+                                                     slices, pm, ps);
     ESTP_CHECK_LAUNCH("loss_lse_f32_kernel");
-    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, 2 * slices, lse);
+    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, int(states), lse);
     ESTP_CHECK_LAUNCH("loss_lse_merge_kernel");
   } else {
     const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
