@@ -13,6 +13,8 @@
 // stage, transfers issued two and a half stages ahead and across tile boundaries.
 #pragma once
 
+#include <type_traits>
+
 #include "estp_common.h"
 #include "lds_ops.h"
 
@@ -79,10 +81,13 @@ __device__ __forceinline__ int fresh_lane() {
 // First tile id of a workgroup; it goes on in steps of the grid (a multiple of 8).
 __device__ __forceinline__ int first_tile(int wg, int grid) { return (wg & 7) * (grid >> 3) + (wg >> 3); }
 
-// kAK, kBK: k contiguous (else strided).  kPairA (k-contiguous A): block i of a wave holds rows
-// 32 (i / 2) + 4 (i % 2) + 8 (m / 4) + m % 4, so that the results of a block pair in a lane are 8 consecutive m.
-// kNBN: 16-row blocks of a wave, N side.  kOdd: the depth may be an odd multiple of 32 (both k contiguous).
-template <bool kAK, bool kBK, bool kPairA, int kNBN, bool kOdd>
+// kAK, kBK: k contiguous (else strided).  kPairA: block i of a wave holds rows 32 (i / 2) + 4 (i % 2) + 8 (m / 4) + m % 4,
+// so that the results of a block pair in a lane are 8 consecutive m (a strided A then has 2-way bank conflicts, which
+// its reads have room for).
+// kNBN: 16-row blocks of a wave, N side.  kOdd: the depth may be an odd multiple of 32 (both k contiguous).  kStores:
+// vector-memory operations that done() leaves in flight at least (it ends with so many stores, always): the stage after
+// it need not wait for them.
+template <bool kAK, bool kBK, bool kPairA, int kNBN, bool kOdd, int kStores>
 struct Tiles {
   static constexpr int kBN = 32 * kNBN;
   static constexpr int kLA = 8;              // transfers of a wave per part
@@ -203,7 +208,8 @@ struct Tiles {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
         ra[u] = kAK ? row * 128 + ((4 * u + fq) ^ swz_k(kPairA, row)) * 16
-                    : k * (2 * kBM) + ((8 * wm) ^ g) * 32 + (fr & 3) * 8;
+                    : kPairA ? k * (2 * kBM) + ((8 * wm + ((fr >> 1) & 1)) ^ g) * 32 + (fr & 1) * 16
+                             : k * (2 * kBM) + ((8 * wm) ^ g) * 32 + (fr & 3) * 8;
       const int rowb = 16 * kNBN * wn + fr;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -218,7 +224,9 @@ struct Tiles {
           f.a[q] = *reinterpret_cast<const bf16x8_t*>(s + ra[u] +
                                                       (kPairA ? 4096 * (q / 2) + 512 * (q % 2) : 2048 * q));
         } else {
-          const char* p = s + (ra[0] ^ (uint32_t(q / 2) << 5)) + (32 * u + 4 * (q % 2)) * (2 * kBM);
+          const int i = q / 2;  // block
+          const char* p = s + (kPairA ? (ra[0] ^ (uint32_t(i / 2) << 6)) + 8 * (i % 2) : ra[0] ^ (uint32_t(i) << 5)) +
+                          (32 * u + 4 * (q % 2)) * (2 * kBM);
           if (q % 2 == 0)
             half[0] = read_tr(p);
           else
@@ -272,7 +280,7 @@ struct Tiles {
       // at least one stage, also of an empty depth.  The compiler must not know that: of a loop that surely runs it
       // keeps the sums in other registers than the products' own, and spills (145 registers of the dW kernel; 10 so).
       const int nk = __builtin_amdgcn_readfirstlane(max(1, (p.k1 - p.k0 + kDepth - 1) / kDepth));
-      for (int ks = 0; ks < nk; ++ks) {
+      auto stage = [&](auto behind) {  // behind: operations issued after the next stage's parts that may stay in flight
         const int sb = sa + 1 == kSlots ? 0 : sa + 1;
         const int sa_next = sb + 1 == kSlots ? 0 : sb + 1;
         const int sb_next = sa_next + 1 == kSlots ? 0 : sa_next + 1;
@@ -286,7 +294,7 @@ struct Tiles {
             // this wave's reads of the stage are done, and the next stage has landed (only its successor's A
             // part may be in flight): after the barrier nobody reads this stage's slots again
             __builtin_amdgcn_sched_barrier(0);
-            wait_vm<kLA>();
+            wait_vm<decltype(behind)::value>();
             lds_barrier();
           }
 #pragma unroll
@@ -314,7 +322,13 @@ struct Tiles {
             }
         }
         sa = sa_next;
-      }
+      };
+      // (the first stage of a tile leaves the last tile's stores behind as well)
+      if (id == first)
+        stage(std::integral_constant<int, kLA>{});
+      else
+        stage(std::integral_constant<int, kLA + kStores>{});
+      for (int ks = 1; ks < nk; ++ks) stage(std::integral_constant<int, kLA>{});
       done(p, acc);
       // the next tile's first fragments, again: done() has the registers to itself
       const int sb = sa + 1 == kSlots ? 0 : sa + 1;

@@ -444,13 +444,7 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
 
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
-// Stores of 8 and 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
-__device__ __forceinline__ void buf_store8(buf_rsrc_t r, uint32_t off, uint2 v) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{v.x, v.y}, r, off, 0, 0);
-#endif
-}
+// Stores of 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
 __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -471,7 +465,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
                                                                 int64_t v0, int Vc, const int32_t* __restrict__ tc,
                                                                 const float* __restrict__ lc,
                                                                 const float* __restrict__ gc, __bf16* __restrict__ G) {
-  using Run = gemm::Tiles<true, true, true, kNBN, kOdd>;
+  using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 4 * kNBN>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
   const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
@@ -533,7 +527,7 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                               int Vc, size_t room, bool first,
                                                               float* __restrict__ out) {
-  using Run = gemm::Tiles<false, true, false, kNBN, false>;
+  using Run = gemm::Tiles<false, true, false, kNBN, false, 8 * kNBN < 48 ? 8 * kNBN : 48>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
   const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
@@ -581,7 +575,7 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
                                                               const __bf16* __restrict__ Xc,
                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                               int Vc, __bf16* __restrict__ dW) {
-  using Run = gemm::Tiles<false, false, false, 8, false>;
+  using Run = gemm::Tiles<false, false, true, 8, false, 32>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
   const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
@@ -603,11 +597,13 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const uint32_t row = uint32_t(128 * wn + 16 * j + fr) * uint32_t(d);
-          const int c0 = m0 + 128 * wm + 4 * fq;
+          const int c0 = m0 + 128 * wm + 8 * fq;  // 8 columns of every 32: d is a multiple of 32, all 8 are live or none
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            buf_store8(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
-                       uint2{pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3])});
+          for (int i = 0; i < 8; i += 2)
+            buf_store16(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
+                        uint4{pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]),
+                              pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]),
+                              pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3])});
         }
       });
 }
