@@ -338,8 +338,8 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  *   loss [n_tok]     float32 output, at least 0
  *   lse  [n_tok]     float32 output, natural log, of every token (ignored ones too):
  *                    what estp_token_loss_backward takes
- *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL (for fp32 inputs lse comes
- *                    from other sums with them than without: its last bits differ)
+ *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL (lse can come from
+ *                    other sums with them than without: its last bits then differ)
  * Other arguments and requirements are those of estp_token_entropy.
  *
  * estp_token_loss_backward: with grad_i the gradient of the objective with

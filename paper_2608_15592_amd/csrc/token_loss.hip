@@ -456,6 +456,87 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, bf16x2_t{__bf16(lo), __bf16(hi)});
 }
 
+// Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
+// takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
+// first tile's maximum is the reference; later tiles add to the sum with one FMA, exponential and addition a logit,
+// and move the reference only where a sum would pass 2^64.  Partial states [2 n_slices, n_tok], a wave's 128 rows each.
+template <int kNBN, bool kOdd>
+__global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __restrict__ X,
+                                                               const __bf16* __restrict__ W, int n_tok, int d, int V,
+                                                               int n_tt, int n_slices, float* __restrict__ part_m,
+                                                               float* __restrict__ part_s) {
+  using Run = gemm::Tiles<true, true, false, kNBN, kOdd, 0>;
+  __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
+  // token tiles of a slice, which stream the same rows of W, next to each other on one XCD
+  const int wg = gemm::first_tile(blockIdx.x, gridDim.x), tt = wg % n_tt, slice = wg / n_tt;
+  if (slice >= n_slices) return;
+  const gemm::Operand A{reinterpret_cast<const char*>(W), uint32_t(d) * 2u, V};
+  const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 2u, n_tok};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+  const int n_vt = (V + 255) / 256, n_mine = (n_vt - slice + n_slices - 1) / n_slices;
+  float m[kNBN], l[kNBN];
+#pragma unroll
+  for (int j = 0; j < kNBN; ++j) {
+    m[j] = -INFINITY;
+    l[j] = 0.f;
+  }
+  Run::run(
+      lds, A, B, 0, 1, n_mine,
+      [&](int i) { return gemm::Place{256 * (slice + i * n_slices), Run::kBN * tt, 0, d, i}; },
+      [&](const gemm::Place& at, const f32x4_t(&acc)[8][kNBN]) {
+        const int fq = gemm::fresh_lane() >> 4;
+        const int lim = V - (at.m0 + 128 * wm + 4 * fq);  // live rows: 16 i + r < lim
+        const bool ragged = at.m0 + 256 > V;
+#pragma unroll
+        for (int j = 0; j < kNBN; ++j) {
+          bool exact = ragged || at.tag == 0;
+          if (!exact) {
+            float s = l[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s += fast_exp2(fmaf(acc[i][j][r], kLog2e, -m[j]));
+            exact = !(s <= 0x1p64f);  // (a NaN takes the exact path and stays one)
+            l[j] = exact ? l[j] : s;
+          }
+          if (exact) {
+            float mx = m[j];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * kLog2e : -INFINITY);
+            const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
+            float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                s += 16 * i + r < lim ? fast_exp2(fmaf(acc[i][j][r], kLog2e, -ref)) : 0.f;
+            m[j] = mx;
+            l[j] = s;
+          }
+        }
+      });
+  // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same tokens
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int j = 0; j < kNBN; ++j) {
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1) {
+      const float mo = __shfl_xor(m[j], o, 64), lo = __shfl_xor(l[j], o, 64), M = fmaxf(m[j], mo);
+      const float ref = fmaxf(M, -0x1p127f);
+      l[j] = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor)) + lo * fast_exp2(fmaxf(mo - ref, kExp2Floor));
+      m[j] = M;
+    }
+    const int tok = Run::kBN * tt + 16 * kNBN * wn + 16 * j + (lane & 15);
+    if (lane < 16 && tok < n_tok) {
+      const size_t o = size_t(2 * slice + wm) * n_tok + tok;
+      part_m[o] = m[j];
+      part_s[o] = l[j];
+    }
+  }
+}
+
 // G of a piece: products of W's rows (M side) and the live tokens (N side), turned into G as they leave the matrix
 // cores.  A lane holds 8 consecutive vocabulary rows of a token: one 16-byte store.
 template <int kNBN, bool kOdd>
@@ -731,22 +812,32 @@ using namespace estp::detail;
 
 namespace {
 
-// Slices of the vocabulary tiles of a fp32 call: two workgroups for every compute unit (four of the smaller ones), at least 4 slices.
-int loss_f32_slices(int64_t n_tok, int V) {
-  const int64_t n_vt = (int64_t(V) + kFT - 1) / kFT, tile = f32_tile_toks(n_tok), n_tt = (n_tok + tile - 1) / tile;
-  return int(std::min<int64_t>(n_vt, std::max<int64_t>(4, (tile < kFT ? 1024 : 512) / n_tt)));
+// How a call that wants no more than lse is cut: tiles of `tile` tokens, the vocabulary tiles in `slices`, `states`
+// partial states a token.
+struct LsePlan {
+  int tile, slices, states;
+};
+// bf16: a workgroup on every compute unit.  fp32: two workgroups for every compute unit (four of the smaller ones).
+LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
+  LsePlan p;
+  const bool f32 = dtype == ESTP_F32;
+  p.tile = f32 ? f32_tile_toks(n_tok) : n_tok <= 128 ? 128 : 256;
+  const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows, n_tt = (n_tok + p.tile - 1) / p.tile;
+  const int64_t fill = f32 ? std::max<int64_t>(4, (p.tile < kFT ? 1024 : 512) / n_tt) : std::max<int64_t>(1, 256 / n_tt);
+  p.slices = int(std::min(n_vt, fill));
+  p.states = p.slices * (f32 && p.tile < kFT ? 4 : 2);
+  return p;
 }
-size_t loss_f32_states(int64_t n_tok, int V) {  // of a token
-  return size_t(f32_tile_toks(n_tok) < kFT ? 4 : 2) * size_t(loss_f32_slices(n_tok, V));
-}
+// bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.
+bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 2048; }
 
 }  // namespace
 
 extern "C" size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   const size_t entropy = estp_token_entropy_workspace_size(n_tok, d, V, dtype);
-  if (entropy == 0 || dtype != ESTP_F32) return entropy;
+  if (entropy == 0 || !own_lse(n_tok, dtype)) return entropy;
   Carver c(nullptr);
-  for (int i = 0; i < 2; ++i) c.take<float>(loss_f32_states(n_tok, V) * size_t(n_tok));
+  for (int i = 0; i < 2; ++i) c.take<float>(size_t(plan_lse(n_tok, V, dtype).states) * size_t(n_tok));
   return std::max(entropy, c.bytes());
 }
 
@@ -767,21 +858,31 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
                "%s: workspace must be non-null and 256-byte aligned", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
-  if (dtype == ESTP_F32 && !H && !vocab_argmax) {
-    // maximum and sum alone, on the fp32 matrix cores (the entropy kernel of fp32 inputs runs on the vector units)
-    const int slices = loss_f32_slices(n_tok, V);
+  if (own_lse(n_tok, dtype) && !H && !vocab_argmax) {
+    // maximum and sum alone.  The entropy kernels' sums keep one order for any number of tokens, which leaves part of
+    // the chip idle for few of them (1021 tokens, d 2048: 735 us, here 435), and run on the vector units for fp32.
+    const LsePlan p = plan_lse(n_tok, V, dtype);
     Carver c(workspace);
-    const size_t states = loss_f32_states(n_tok, V);
-    float* pm = c.take<float>(states * size_t(n_tok));
-    float* ps = c.take<float>(states * size_t(n_tok));
-    const int tile = f32_tile_toks(n_tok);
-    const size_t wgs = size_t((n_tok + tile - 1) / tile) * size_t(slices);
-    ESTP_REQUIRE(fits_launch(wgs, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
-    auto kernel = tile == 32 ? loss_lse_f32_kernel<32> : tile == 64 ? loss_lse_f32_kernel<64> : loss_lse_f32_kernel<kFT>;
-    kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), n, d, V,
-                                                     slices, pm, ps);
-    ESTP_CHECK_LAUNCH("loss_lse_f32_kernel");
-    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, int(states), lse);
+    float* pm = c.take<float>(size_t(p.states) * size_t(n_tok));
+    float* ps = c.take<float>(size_t(p.states) * size_t(n_tok));
+    const int n_tt = int((n_tok + p.tile - 1) / p.tile);
+    const size_t wgs = size_t(n_tt) * size_t(p.slices);
+    ESTP_REQUIRE(fits_launch(wgs + 7, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
+    if (dtype == ESTP_F32) {
+      auto kernel = p.tile == 32   ? loss_lse_f32_kernel<32>
+                    : p.tile == 64 ? loss_lse_f32_kernel<64>
+                                   : loss_lse_f32_kernel<kFT>;
+      kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), n, d,
+                                                       V, p.slices, pm, ps);
+    } else {
+      auto kernel = p.tile == 128 ? (d % 64 ? loss_lse_mfma_kernel<4, true> : loss_lse_mfma_kernel<4, false>)
+                                  : (d % 64 ? loss_lse_mfma_kernel<8, true> : loss_lse_mfma_kernel<8, false>);
+      kernel<<<dim3(unsigned((wgs + 7) / 8 * 8)), dim3(256), 0, s>>>(static_cast<const __bf16*>(X),
+                                                                     static_cast<const __bf16*>(W), n, d, V, n_tt,
+                                                                     p.slices, pm, ps);
+    }
+    ESTP_CHECK_LAUNCH("loss_lse_kernel");
+    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, p.states, lse);
     ESTP_CHECK_LAUNCH("loss_lse_merge_kernel");
   } else {
     const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
