@@ -568,11 +568,21 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
             make_rsrc(reinterpret_cast<const char*>(G) + size_t(n0) * Vc * 2, uint32_t(live) * uint32_t(Vc) * 2u);
         const int c0 = m0 + 128 * wm + 8 * fq;  // the lane's first column of G
         const bool ragged = m0 + 256 > rows;
+        float lse_of[kNBN], g_of[kNBN];  // of the lane's tokens, all on their way before the first is needed
+        int t_of[kNBN];
 #pragma unroll
         for (int j = 0; j < kNBN; ++j) {
-          const int sl = 16 * kNBN * wn + 16 * j + fr, s = min(n0 + sl, n - 1);
-          const float l2 = lc[s] * kLog2e, g = gc[s];
-          const int rel = int(tc[s] - v0) - c0;  // the target is column rel of the lane's 128, 8 of every 32
+          const int s = min(n0 + 16 * kNBN * wn + 16 * j + fr, n - 1);
+          lse_of[j] = lc[s];
+          g_of[j] = gc[s];
+          t_of[j] = tc[s];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < kNBN; ++j) {
+          const int sl = 16 * kNBN * wn + 16 * j + fr;
+          const float l2 = lse_of[j] * kLog2e, g = g_of[j];
+          const int rel = int(t_of[j] - v0) - c0;  // the target is column rel of the lane's 128, 8 of every 32
           float p[4][8];
 #pragma unroll
           for (int i = 0; i < 8; ++i)
