@@ -381,38 +381,40 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
   }
 }
 
-// out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W.
+// out[share][slot][k] (+)= G W_piece over the share's vocabulary rows, shares blockIdx.z, + gridDim.z, ...  M side:
+// columns k of W.
 template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __restrict__ G, const float* __restrict__ W,
                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                              int Vc, int wgs, size_t room, bool first,
-                                                             float* __restrict__ out) {
+                                                             float* __restrict__ sums) {
   using Run = F32Tile<false, true, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
   const int n = n_live[0], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
   const Shares sh = dx_shares(n, d, Vc, kTN, wgs, room);
-  if (n0 >= n || int(blockIdx.z) >= sh.n) return;
+  if (n0 >= n) return;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, d};
   const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, n};
-  typename Run::Acc acc;
-  Run::run(lds, A, B, m0, n0, min(rows, int(blockIdx.z) * sh.rows),
-                            min(rows, (int(blockIdx.z) + 1) * sh.rows), acc);
-  out += size_t(blockIdx.z) * size_t(n) * d;
-  const auto at = Run::place(m0, n0);
+  for (int share = blockIdx.z; share < sh.n; share += gridDim.z) {
+    typename Run::Acc acc;
+    Run::run(lds, A, B, m0, n0, min(rows, share * sh.rows), min(rows, (share + 1) * sh.rows), acc);
+    float* out = sums + size_t(share) * size_t(n) * d;
+    const auto at = Run::place(m0, n0);
 #pragma unroll
-  for (int j = 0; j < Run::kNJ; ++j)
+    for (int j = 0; j < Run::kNJ; ++j)
 #pragma unroll
-    for (int i = 0; i < Run::kMI; ++i)
+      for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int s = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
-        if (s >= n || k >= d) continue;
-        f32x4_t* o = reinterpret_cast<f32x4_t*>(out + size_t(s) * d + k);
-        f32x4_t v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-        if (!first) v += *o;
-        *o = v;
-      }
+        for (int q = 0; q < 4; ++q) {
+          const int s = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
+          if (s >= n || k >= d) continue;
+          f32x4_t* o = reinterpret_cast<f32x4_t*>(out + size_t(s) * d + k);
+          f32x4_t v{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+          if (!first) v += *o;
+          *o = v;
+        }
+  }
 }
 
 // dW[v0 + v][k] = sum over the live tokens of G[s][v] Xc[s][k].  M side: columns k of Xc, N side: vocabulary rows.
@@ -792,12 +794,14 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
       grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
       ESTP_CHECK_LAUNCH("loss_grad_f32_kernel");
       if (dX) {
-        const unsigned shares = unsigned(std::min<int64_t>(kWgs, (p.Vc + 63) / 64));
+        // (a workgroup for every share there could be, up to a million in all: past that, a loop over the shares)
+        const int64_t most = std::max<int64_t>(1, (int64_t(1) << 20) / (int64_t(n_dt) * n_tt));
+        const unsigned shares = unsigned(std::min({int64_t(kWgs), int64_t((p.Vc + 63) / 64), most}));
         auto dx_kernel = p.tile_toks == 32   ? loss_dx_f32_kernel<32>
                          : p.tile_toks == 64 ? loss_dx_f32_kernel<64>
                                              : loss_dx_f32_kernel<kFT>;
-        dx_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room,
-                                                                      v0 == 0, b.acc);
+        dx_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room, v0 == 0,
+                                                             b.acc);
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
@@ -866,6 +870,8 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
                workspace_bytes, need);
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
+  ESTP_REQUIRE(fits_launch(size_t(n_tok + 3) / 4, 256), ESTP_ERR_UNSUPPORTED,
+               "%s: n_tok = %lld needs more workgroups than one launch holds", fn, (long long)n_tok);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
   if (own_lse(n_tok, dtype) && !H && !vocab_argmax) {
@@ -929,6 +935,8 @@ extern "C" int estp_token_loss_backward(const void* X, const void* W, const int3
   ESTP_REQUIRE(n_tok <= (int64_t(1) << 22), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %lld, at most 4194304", fn,
                (long long)n_tok);
   ESTP_REQUIRE(d <= (1 << 20), ESTP_ERR_UNSUPPORTED, "%s: d = %d, at most 1048576", fn, d);
+  ESTP_REQUIRE(n_tok * d <= (int64_t(1) << 36), ESTP_ERR_UNSUPPORTED, "%s: n_tok d = %lld, at most 2^36", fn,
+               (long long)n_tok * d);
   const size_t need = estp_token_loss_backward_workspace_size(n_tok, d, V, dtype);
   ESTP_REQUIRE(workspace_bytes >= need, ESTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn,
                workspace_bytes, need);

@@ -281,3 +281,21 @@ def test_a_nan_weight_row_reaches_every_loss(dtype, n):
         Wd[row, 5] = float("nan")
         loss, lse = estp.token_loss(dev(X), Wd, dev(t))
         assert torch.isnan(loss).all() and torch.isnan(lse).all(), row
+
+
+def test_few_live_tokens_among_very_many():
+    # fp32, 600 001 tokens of which 90 are live: more shares of the vocabulary than workgroups for them
+    n, d, V = 600_001, 256, 8192
+    X, W, t, g = _inputs(15, 90, d, V, "f32")
+    at = np.sort(np.random.default_rng(15).choice(n, 90, replace=False))
+    Xd = torch.full((n, d), float("nan"), device="cuda")
+    td = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    lse, gd = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    place = torch.from_numpy(at).cuda()
+    Xd[place], td[place], gd[place] = dev(X), dev(t), dev(g)
+    lse[place] = estp.token_loss(dev(X), dev(W), dev(t))[1]
+    dX, dW = estp.token_loss_backward(Xd, dev(W), td, lse, gd)
+    rX, rW, bX, bW = OP.token_loss_grads(X, W, t, g, "f32")
+    assert (np.abs(_wide(dX[place]) - rX) <= bX).all() and (np.abs(_wide(dW) - rW) <= bW).all()
+    dX[place] = 0
+    assert not dX.any()
