@@ -93,7 +93,8 @@ ESTP_API const char* estp_last_error(void);
  * on by ESTP_DEBUG_CHECKS=1 in the environment (read once).  Every call that
  * takes cu_seqlens then copies it back and checks it before any kernel runs
  * (cu_seqlens[0] = 0, cu_seqlens[B] = n_tok, every prompt length in
- * [1, max_seqlen]; ESTP_ERR_INVALID_ARG otherwise), and every call that
+ * [1, max_seqlen]; ESTP_ERR_INVALID_ARG otherwise), so do the calls on a cache
+ * with lens and cu_q (what they require of both), and every call that
  * builds a work list of live blocks or chunks on the device compares it with
  * its definition before the kernels that use it run (ESTP_ERR_HIP on a
  * mismatch).  The checks synchronise the stream: for testing, not for use
@@ -354,8 +355,9 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  * Rows of X, lse and grad of ignored tokens are not used (they may hold
  * anything).  G is formed a piece of the vocabulary at a time, in dtype; sums
  * are fp32 and each output element is rounded once.  Bitwise repeatable.
- * n_tok > 4194304 or d > 1048576 returns ESTP_ERR_UNSUPPORTED.  The workspace holds one piece
- * of G (about 256 MiB), the live rows of X and fp32 sums of dX.
+ * n_tok > 4194304, d > 1048576 or n_tok d > 2^36 returns ESTP_ERR_UNSUPPORTED.  The workspace
+ * holds one piece of G (about 256 MiB, more past 8192 tokens of fp32 or 16384 of bf16), the live
+ * rows of X and fp32 sums of dX.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
 ESTP_API int estp_token_loss(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,
@@ -392,7 +394,8 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  *   cu_q [B+1]              int32, device, from 0; T_b in [0, max_q]; rows from cu_q[B] to
  *                           n_q belong to no sequence: their outputs are left as they are
  *   tree_mask [n_q]         int64, device, 8-byte aligned, or NULL: a chain (row t sees j <= t)
- *   max_q, max_kv           host bounds of T_b (at most 64) and of lens[b] + T_b (at most cap)
+ *   max_q, max_kv           host bounds of T_b (at most 64 and n_q) and of lens[b] + T_b (at most
+ *                           cap); n_q is at most B max_q
  *   O  [n_q, Hq, dh]        output (dtype), 16-byte aligned
  *   lse [Hq, n_q]           float32 output, natural log, or NULL
  *   acc [B, Hkv, cap]       float32, added to in place, or NULL

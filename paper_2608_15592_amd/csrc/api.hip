@@ -42,15 +42,22 @@ bool debug_checks_enabled() {
   return on;
 }
 
-int debug_check_cu(const char* fn, const int32_t* cu_dev, int32_t B, int64_t n_tok, int32_t max_seqlen,
-                   hipStream_t s, std::vector<int>* cu_out) {
-  std::vector<int> cu(size_t(B) + 1);
-  hipError_t e = hipMemcpyAsync(cu.data(), cu_dev, cu.size() * sizeof(int), hipMemcpyDeviceToHost, s);
+int debug_copy(const char* fn, const char* what, const int32_t* dev, size_t n, hipStream_t s, std::vector<int>* out) {
+  out->resize(n);
+  hipError_t e = hipMemcpyAsync(out->data(), dev, n * sizeof(int), hipMemcpyDeviceToHost, s);
   if (e == hipSuccess) e = hipStreamSynchronize(s);
   if (e != hipSuccess) {
-    set_error("%s: debug check: copying cu_seqlens back: %s", fn, hipGetErrorString(e));
+    set_error("%s: debug check: copying %s back: %s", fn, what, hipGetErrorString(e));
     return ESTP_ERR_HIP;
   }
+  return ESTP_OK;
+}
+
+int debug_check_cu(const char* fn, const int32_t* cu_dev, int32_t B, int64_t n_tok, int32_t max_seqlen,
+                   hipStream_t s, std::vector<int>* cu_out) {
+  std::vector<int> cu;
+  const int st = debug_copy(fn, "cu_seqlens", cu_dev, size_t(B) + 1, s, &cu);
+  if (st != ESTP_OK) return st;
   ESTP_REQUIRE(cu[0] == 0, ESTP_ERR_INVALID_ARG, "%s: debug check: cu_seqlens[0] = %d, must be 0", fn, cu[0]);
   for (int32_t b = 0; b < B; ++b) {
     const int64_t N = int64_t(cu[b + 1]) - cu[b];

@@ -16,6 +16,7 @@
 // and forms the prefix for itself, which leaves one barrier a pass and a prefix.  The survivors' rows move in the same
 // kernel where they are few, else in evict_move_kernel.  Everything is exact: whole numbers and copies.
 #include <algorithm>
+#include <vector>
 
 #include "estp_common.h"
 #include "lds_ops.h"
@@ -430,6 +431,14 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   const int groups = B * Hkv;
   const EvictBuffers e = carve_evict(size_t(groups), keep, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (debug_checks_enabled()) {
+    std::vector<int> l;
+    const int st = debug_copy(fn, "lens", lens, size_t(B), s, &l);
+    if (st != ESTP_OK) return st;
+    for (int b = 0; b < B; ++b)
+      ESTP_REQUIRE(l[b] >= 0 && l[b] <= cap, ESTP_ERR_INVALID_ARG,
+                   "%s: debug check: sequence %d has %d slots in use, cap = %lld", fn, b, l[b], (long long)cap);
+  }
   const int row16 = dh * (dtype == ESTP_F32 ? 4 : 2) / 16;
   const int64_t most = std::min<int64_t>(keep, cap - keep) * row16;  // 16-byte pieces that can move, of K or V
   // Rows move in the selecting kernel where there are few: a kernel of their own costs its launch, but spreads the

@@ -182,10 +182,13 @@ void clear_error();
 
 // Debug mode: ESTP_DEBUG_CHECKS=1 in the environment (read once per process).  Calls that take
 // cu_seqlens copy it back and check it before any kernel runs (cu[0] = 0, cu[B] = n_tok, every
-// prompt length in [1, max_seqlen]); calls that build a work list on the device copy it back
-// and compare it with its definition before the kernels that consume it are launched.  Both
-// synchronise the stream, so the mode is for testing, not for graph capture.
+// prompt length in [1, max_seqlen]), so do the calls on a cache with lens and cu_q; calls that
+// build a work list on the device copy it back and compare it with its definition before the
+// kernels that consume it are launched.  All synchronise the stream, so the mode is for testing,
+// not for graph capture.
 bool debug_checks_enabled();
+// *out = the n integers at dev, named `what` in an error
+int debug_copy(const char* fn, const char* what, const int32_t* dev, size_t n, hipStream_t s, std::vector<int>* out);
 // n_tok < 0: the call does not state n_tok, cu_seqlens[B] is not compared.
 int debug_check_cu(const char* fn, const int32_t* cu_dev, int32_t B, int64_t n_tok, int32_t max_seqlen,
                    hipStream_t s, std::vector<int>* cu_out);

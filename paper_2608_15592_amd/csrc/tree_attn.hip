@@ -21,6 +21,7 @@
 // scores formed again.  No atomics: bitwise reproducible.
 #include <algorithm>
 #include <cmath>
+#include <vector>
 
 #include "estp_common.h"
 #include "lds_ops.h"
@@ -44,7 +45,7 @@ struct TreeSeq {
 __device__ __forceinline__ TreeSeq tree_seq(const TreeShape& sh, const int* lens, const int* cu_q, int b) {
   TreeSeq q;
   q.q0 = max(0, min(cu_q[b], sh.n_q));
-  q.T = max(0, min(min(cu_q[b + 1], sh.n_q) - q.q0, sh.max_q));
+  q.T = max(0, min(max(0, min(cu_q[b + 1], sh.n_q)) - q.q0, sh.max_q));
   q.len = max(0, min(lens[b], sh.max_kv));
   q.keys = min(q.len + q.T, sh.max_kv);
   return q;
@@ -868,6 +869,29 @@ int check_tree_args(const char* fn, const void* Q, const void* K, const int32_t*
   return ESTP_OK;
 }
 
+// ESTP_DEBUG_CHECKS=1: lens and cu_q against what the header asks of them, before any kernel reads them
+int debug_check_tree(const char* fn, const int32_t* lens, const int32_t* cu_q, int B, int max_q, int64_t n_q, int max_kv,
+                     hipStream_t s) {
+  if (!debug_checks_enabled()) return ESTP_OK;
+  std::vector<int> l, cu;
+  int st = debug_copy(fn, "lens", lens, size_t(B), s, &l);
+  if (st == ESTP_OK) st = debug_copy(fn, "cu_q", cu_q, size_t(B) + 1, s, &cu);
+  if (st != ESTP_OK) return st;
+  ESTP_REQUIRE(cu[0] == 0, ESTP_ERR_INVALID_ARG, "%s: debug check: cu_q[0] = %d, must be 0", fn, cu[0]);
+  for (int b = 0; b < B; ++b) {
+    const int64_t T = int64_t(cu[b + 1]) - cu[b];
+    ESTP_REQUIRE(T >= 0 && T <= max_q, ESTP_ERR_INVALID_ARG,
+                 "%s: debug check: sequence %d has %lld drafted tokens, must be in [0, max_q = %d]", fn, b, (long long)T,
+                 max_q);
+    ESTP_REQUIRE(l[b] >= 0 && l[b] + T <= max_kv, ESTP_ERR_INVALID_ARG,
+                 "%s: debug check: sequence %d has %d cached and %lld drafted tokens, max_kv = %d", fn, b, l[b],
+                 (long long)T, max_kv);
+  }
+  ESTP_REQUIRE(cu[B] <= n_q, ESTP_ERR_INVALID_ARG, "%s: debug check: cu_q[B] = %d, n_q = %lld", fn, cu[B],
+               (long long)n_q);
+  return ESTP_OK;
+}
+
 template <typename T, int DH>
 int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* cu_q, const int64_t* mask,
                 const TreeShape& sh, const TreePlan& p, bool scores, float scale, T* O, float* lse,
@@ -937,7 +961,9 @@ using namespace estp::detail;
 
 extern "C" size_t estp_tree_attention_workspace_size(int32_t B, int32_t max_q, int64_t n_q, int32_t Hq, int32_t Hkv,
                                                      int32_t max_kv, int32_t dh, int dtype) {
-  if (B < 1 || max_q < 1 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_kv < 1 || dh < 1) return 0;
+  if (B < 1 || max_q < 1 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_kv < 1 || dh < 1 ||
+      max_kv > INT32_MAX - 256)
+    return 0;
   return carve_tree(plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype), B, n_q, Hq, Hkv, max_kv, dh, nullptr).bytes;
 }
 
@@ -965,6 +991,8 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.item_rows, p.items};
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, s);
+  if (checked != ESTP_OK) return checked;
   float* row_lse = lse ? lse : t.lse;
   const bool stored = acc && p.stored;
   return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
@@ -996,6 +1024,8 @@ extern "C" int estp_tree_importance(const void* Q, const void* K, const float* l
   ESTP_REQUIRE(aligned(tree_mask, 8) && aligned(lse, 4) && aligned(acc, 4) && aligned(row_weight, 4),
                ESTP_ERR_INVALID_ARG, "%s: tree_mask must be 8-byte, lse, row_weight and acc 4-byte aligned", fn);
   const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, 16, 1};
+  const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, static_cast<hipStream_t>(stream));
+  if (checked != ESTP_OK) return checked;
   return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
     using T = decltype(element);
     return launch_weight<T, decltype(size)::value>(static_cast<const T*>(Q), static_cast<const T*>(K), lse, lens, cu_q,

@@ -78,6 +78,22 @@ def test_eviction_is_exact(lens, Hkv, dh, cap, keep, recent, sink, values, in_pl
     _check(*_case(len(lens) + cap, lens, Hkv, dh, cap, dtype, values), keep, recent, sink, in_place)
 
 
+LONG = [
+    # lens, Hkv, dh, cap, keep, recent, sink: slots held in registers up to 16384, 32768 and 65536 of a cache
+    ([16000, 16384, 4096, 4097], 1, 32, 16384, 4096, 64, 4),
+    ([20000, 5000, 32768], 2, 32, 32768, 5000, 64, 4),
+    ([32769, 65536, 40000], 2, 32, 65536, 32768, 64, 4),
+    ([65000], 1, 32, 65001, 64000, 3000, 4),
+    ([65536, 65537, 131000], 1, 32, 131073, 100, 64, 4),
+]
+
+
+@pytest.mark.parametrize("lens,Hkv,dh,cap,keep,recent,sink", LONG)
+@pytest.mark.parametrize("values", ["heavy", "ties", "odd"])
+def test_eviction_from_long_caches(lens, Hkv, dh, cap, keep, recent, sink, values):
+    _check(*_case(len(lens) + cap, lens, Hkv, dh, cap, "bf16", values), keep, recent, sink, values != "ties")
+
+
 def test_more_guarded_slots_than_kept():
     # positions that repeat guard more slots than the budget: the best of them stay
     K, V, acc, pos, lens, seen = _case(2, [500, 30], 2, 64, 500, "bf16", "ties")

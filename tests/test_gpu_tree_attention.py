@@ -196,6 +196,90 @@ def test_counts_out_of_range_stay_in_bounds(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_far_below_zero_stay_in_bounds(dtype):
+    c = Case(8, [50, 40, 60], [2, 3, 1], 4, 2, 32, dtype, cap=64)
+    acc = torch.cat([dev(c.acc).view(-1), torch.full((1000,), 3.0, device="cuda")])
+    cu = torch.tensor([0, 6, -(1 << 31), 6], dtype=torch.int32, device="cuda")
+    estp.tree_attention(dev(c.Q), dev(c.K), dev(c.V), dev(c.lens), cu, 3, 64, tree_mask=c.mask(), acc=acc[:c.acc.size])
+    torch.cuda.synchronize()
+    assert (acc[c.acc.size:] == 3).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tree", [True, False])
+def test_many_sequences_of_any_length(dtype, tree):
+    # more sequences than lanes, some without rows, some with several items of rows, few chunks and many
+    g = np.random.default_rng(20)
+    lens = g.integers(0, 120, 150)
+    T = g.integers(0, 4, 150)
+    lens[[3, 70, 140]], T[[3, 70, 140]] = [2500, 900, 1700], [40, 0, 17]
+    T[60:68] = 0
+    c = Case(21, lens.tolist(), T.tolist(), 8, 2, 32, dtype, tree)
+    acc = dev(c.acc)
+    O, lse = c.attend(acc=acc)
+    c.check(O, lse, acc)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_a_long_tree_of_many_heads(dtype, dh):
+    # 64 tokens of 16 heads on one KV head: many items that share the keys, rows in several batches of the account
+    c = Case(22, [3000, 9], [64, 50], 16, 1, dh, dtype)
+    acc = dev(c.acc)
+    O, lse = c.attend(acc=acc)
+    c.check(O, lse, acc)
+
+
+def test_two_captured_graphs_on_one_workspace():
+    cs = [Case(23, [300, 40], [3, 9], 8, 2, 64, "bf16"), Case(24, [900], [1], 8, 2, 64, "bf16")]
+    lib = estp.load()
+    need = max(lib.estp_tree_attention_workspace_size(len(c.lens), c.max_q, len(c.Q), 8, 2, c.max_kv, 64, 0) for c in cs)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for c in cs:
+        t = [dev(a) for a in (c.Q, c.K, c.V, c.lens, c.cu)]
+        out = {"O": torch.empty_like(t[0]), "lse": torch.empty(8, len(c.Q), device="cuda"), "acc": dev(c.acc)}
+        mask = c.mask()
+        call = lambda: estp.tree_attention(*t, c.max_q, c.max_kv, tree_mask=mask, workspace=ws, **out)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.current_stream().wait_stream(side)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call()
+        graphs.append((graph, c, out, t, mask))
+    for rep in range(3):
+        for graph, c, out, t, mask in graphs:
+            out["acc"].copy_(dev(c.acc))
+            out["O"].fill_(float("nan"))
+            graph.replay()
+        torch.cuda.synchronize()
+        for graph, c, out, t, mask in graphs:
+            c.check(out["O"], out["lse"], out["acc"])
+
+
+def test_two_calls_at_once():
+    # two streams, a workspace each: neither call disturbs the other
+    cs = [Case(25, [4000, 40], [3, 9], 8, 2, 128, "bf16"), Case(26, [6000], [20], 8, 2, 128, "bf16")]
+    want = [c.attend() for c in cs]
+    torch.cuda.synchronize()
+    args = [([dev(a) for a in (c.Q, c.K, c.V, c.lens, c.cu)], c.mask()) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, c in enumerate(cs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(estp.tree_attention(*args[i][0], c.max_q, c.max_kv, tree_mask=args[i][1]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for O, lse in got[i]:
+            assert torch.equal(O, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_cache(dtype):
     n = 131_072
     c = Case(9, [n], [2], 4, 1, 128, dtype)
