@@ -21,6 +21,7 @@
 // scores formed again.  No atomics: bitwise reproducible.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 #include <vector>
 
 #include "estp_common.h"
@@ -32,11 +33,23 @@ namespace detail {
 constexpr int kMaxTree = 64;  // drafted tokens of a sequence: the bits of a mask
 constexpr int kTRows = 16;    // rows of a workgroup
 constexpr int kTKeys = 64;    // keys of a tile
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
 struct TreeShape {
   int B, max_q, n_q, Hq, Hkv, cap, max_kv;
-  int item_rows, items;  // rows of an item; items of a (sequence, KV head) at most
+  int item_shift, items;  // 2^item_shift rows of an item; items of a (sequence, KV head) at most
+  int G;                  // Hq / Hkv, at most 32768
+  uint32_t over_G;        // ceil(2^31 / G)
+  __device__ __forceinline__ int item_rows() const { return 1 << item_shift; }
+  // r / G for a row number (below 65536): r (G over_G - 2^31) stays below 2^31
+  __device__ __forceinline__ int token(int r) const { return int(__umulhi(uint32_t(2 * r), over_G)); }
 };
+inline TreeShape tree_shape(int B, int max_q, int64_t n_q, int Hq, int Hkv, int64_t cap, int max_kv, int item_shift,
+                            int items) {
+  const int G = Hq / Hkv;
+  return {B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, item_shift, items, G,
+          uint32_t(((uint64_t(1) << 31) + uint64_t(G) - 1) / uint64_t(G))};
+}
 
 // One sequence as the kernels see it: counts out of range (invalid input) never become an access out of range.
 struct TreeSeq {
@@ -79,15 +92,16 @@ struct TreeBatch {
     upto = wave_prefix(w);
   }
   __device__ static __forceinline__ uint32_t items(const TreeShape& sh, int T) {  // of a KV head
-    return uint32_t(T * (sh.Hq / sh.Hkv) + sh.item_rows - 1) / uint32_t(sh.item_rows);
+    return uint32_t(T * sh.G + sh.item_rows() - 1) >> sh.item_shift;
   }
   __device__ static __forceinline__ uint32_t chunks(int keys) { return uint32_t(keys + kChunk - 1) / kChunk; }
   __device__ __forceinline__ uint32_t all() const { return lane_of(upto, 63); }
 };
 // Chunks of one share: at least 128 keys, so that joins stay few.
-template <int kChunk>
+template <int kChunk, int kRound = 1>
 __device__ __forceinline__ uint32_t tree_share(uint32_t total, int wgs) {
-  return max(uint32_t(128 / kChunk), (total + uint32_t(wgs) - 1) / uint32_t(wgs));
+  const uint32_t share = max(uint32_t(128 / kChunk), (total + uint32_t(wgs) - 1) / uint32_t(wgs));
+  return (share + kRound - 1) / kRound * kRound;
 }
 template <int kChunk>
 __device__ __forceinline__ uint32_t tree_total(const TreeShape& sh, const int* lens, const int* cu_q,
@@ -105,12 +119,22 @@ __device__ __forceinline__ uint32_t tree_total(const TreeShape& sh, const int* l
 struct TreeSegment {
   int b, g, r0, q0, T, len, keys, k0, k1, slot;
 };
-// Calls f with the segments of this workgroup's share in turn; all values are uniform.
-template <int kChunk, typename F>
+// The mask of drafted token t of the segment's sequence, without the bits of tokens that the sequence has not.
+__device__ __forceinline__ uint64_t tree_bits(const int64_t* mask, const TreeSegment& q, int t) {
+  const int n = q.keys - q.len;
+  return tree_bits(mask, q.q0, t) & (n >= 64 ? ~uint64_t(0) : (uint64_t(1) << n) - 1);
+}
+// Which of the four keys from `rel` places past the cached ones on a row with such a mask sees: a bit each.
+__device__ __forceinline__ uint32_t tree_sees4(uint64_t bits, int rel) {
+  const uint64_t drafted = rel < 64 ? bits >> (rel & 63) : 0, both = ~(~bits << (-rel & 63));
+  return uint32_t(rel >= 0 ? drafted : rel > -4 ? both : ~uint64_t(0)) & 15u;
+}
+// Calls f with the segments of this workgroup's share, a multiple of kRound chunks, in turn; all values are uniform.
+template <int kChunk, int kRound = 1, typename F>
 __device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, const int* cu_q, int wg, int wgs,
                                           F&& f) {
   TreeBatch<kChunk> t;
-  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk, kRound>(total, wgs);
   if (uint64_t(wg) * share >= total) return;
   uint32_t at = uint32_t(wg) * share;
   const uint32_t end = min(total, at + share);
@@ -132,7 +156,7 @@ __device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, 
     const uint32_t item = (at - off) / n, c0 = at - off - item * n, c1 = min(n, c0 + (end - at));
     s.g = __builtin_amdgcn_readfirstlane(int(item / items));
     const int part = __builtin_amdgcn_readfirstlane(int(item % items));
-    s.r0 = part * sh.item_rows;
+    s.r0 = part << sh.item_shift;
     s.k0 = __builtin_amdgcn_readfirstlane(int(c0) * kChunk);
     s.k1 = __builtin_amdgcn_readfirstlane(min(s.keys, int(c1) * kChunk));
     s.slot = wg + (s.b * sh.Hkv + s.g) * sh.items + part;  // grows from segment to segment
@@ -297,7 +321,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
 // LDS at a head size of 128, eight at 64.  16-byte pieces are swizzled so that the 16 rows of a K read and the 8 of
 // a transposing V read lie in distinct banks.
 template <int DH, int NRT, bool kScores>
-__global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
+__global__ __launch_bounds__(64, 2) void tree_attn_mfma_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     const int* __restrict__ lens, const int* __restrict__ cu_q, const int64_t* __restrict__ mask, TreeShape sh,
     float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m, float* __restrict__ part_l,
@@ -305,8 +329,8 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
   constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
   constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
   constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
-  __shared__ __attribute__((aligned(16))) char lds[kSlots * kPart];
-  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4, G = sh.Hq / sh.Hkv;
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // kSlots * kPart = 320 DH bytes
+  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4, G = sh.G;
   uint32_t off_k[kL], off_v[kL];
 #pragma unroll
   for (int i = 0; i < kL; ++i) {
@@ -347,7 +371,7 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
 #pragma unroll
     for (int t = 0; t < NRT; ++t) {
       const int r = r0 + 16 * t + fr;
-      bits[t] = r < R ? tree_bits(mask, q.q0, r / G) : 0;
+      bits[t] = r < R ? tree_bits(mask, q, sh.token(r)) : 0;
     }
     // the rows of Q come first, through the ring's last slot and laid out as a K part: a load of their own would
     // wait for every transfer issued around it
@@ -358,7 +382,8 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
       for (int i = 0; i < kL * NRT / 2; ++i) {
         const int row = (64 * i + lane) / kPieces, r = r0 + row;
         const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (row / kWindow & (kPieces - 1))) * 16u;
-        dma16(rq, r < R ? (uint32_t(r / G) * uint32_t(sh.Hq) + uint32_t(g * G + r % G)) * kRow + piece : kPastEnd, 0,
+        const uint32_t tok = uint32_t(sh.token(r)), head = uint32_t(g * G + r) - tok * uint32_t(G);
+        dma16(rq, r < R ? (tok * uint32_t(sh.Hq) + head) * kRow + piece : kPastEnd, 0,
               lds + (kSlots - 1) * kPart + 1024 * i);
       }
     }
@@ -401,20 +426,22 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
 #pragma unroll
           for (int c = 0; c < kNK; ++c) s[a] = mfma_bf16(kf[a][c], qf[t][c], s[a]);
         }
+        if (edge) {
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const uint32_t sees = tree_sees4(bits[t], k + 16 * a + 4 * fq - q.len);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) s[a][z] = (sees >> z) & 1 ? s[a][z] : -INFINITY;
+          }
+        }
         float mx = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[t][e] = s[e / 4][e % 4] * c2;
-          if (edge) {
-            const int key = k + 16 * (e / 4) + 4 * fq + e % 4;
-            p[t][e] = key < q.keys && tree_sees(bits[t], key - q.len) ? p[t][e] : -INFINITY;
-          }
-          mx = fmaxf(mx, p[t][e]);
-        }
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
+        mx *= c2;
         if (kScores && r0 + 16 * t + fr < R) {
           float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
-          *reinterpret_cast<f32x4_t*>(w) = f32x4_t{p[t][0], p[t][1], p[t][2], p[t][3]};
-          *reinterpret_cast<f32x4_t*>(w + 16) = f32x4_t{p[t][4], p[t][5], p[t][6], p[t][7]};
+          *reinterpret_cast<f32x4_t*>(w) = s[0] * c2;
+          *reinterpret_cast<f32x4_t*>(w + 16) = s[1] * c2;
         }
         if (__any(mx > m[t] + 16.f)) {
           mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -429,7 +456,7 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
         const float ref = m[t] == -INFINITY ? 0.f : m[t];  // nothing seen yet: all weights are 0
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          p[t][e] = fast_exp2(p[t][e] - ref);
+          p[t][e] = fast_exp2(fmaf(s[e / 4][e % 4], c2, -ref));
           l[t] += p[t][e];
           pf[t][e] = __bf16(p[t][e]);  // as the matrix cores take it; l keeps the unrounded sum
         }
@@ -448,19 +475,22 @@ __global__ __launch_bounds__(64) void tree_attn_mfma_kernel(
       if (edge) {
         // A drafted token that a row does not see has weight 0 there, which a non-finite value must not meet: such
         // values leave the product and are added, one by one, to the rows that see them.
-        bool bad = false;
+        u16x2_t top{0, 0};  // the largest exponent
 #pragma unroll
         for (int d = 0; d < kND; ++d) {
-          s16x8_t v = __builtin_bit_cast(s16x8_t, vf[d]);
+          const u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool inf = (v[e] & 0x7f80) == 0x7f80;
-            bad |= inf;
-            v[e] = inf ? short(0) : v[e];
-          }
-          vf[d] = __builtin_bit_cast(bf16x8_t, v);
+          for (int e = 0; e < 4; ++e)
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, v[e] & 0x7f807f80u));
         }
-        if (__any(bad)) {
+        if (__any(top[0] == 0x7f80 || top[1] == 0x7f80)) {
+#pragma unroll
+          for (int d = 0; d < kND; ++d) {
+            s16x8_t v = __builtin_bit_cast(s16x8_t, vf[d]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = (v[e] & 0x7f80) == 0x7f80 ? short(0) : v[e];
+            vf[d] = __builtin_bit_cast(bf16x8_t, v);
+          }
           for (int j = 0; j < kC && k + j < q.keys; ++j) {
             const int from = fr + 16 * (j % 16 / 4), e = j / 16 * 4 + j % 4;
 #pragma unroll
@@ -523,7 +553,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t rows = int64_t(sh.n_q) * sh.Hq, row = kWaves == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
   const int first = kWaves == 1 ? 0 : wave;
-  const int tok = int(row / sh.Hq), h = int(row % sh.Hq), G = sh.Hq / sh.Hkv;
+  const int tok = int(row / sh.Hq), h = int(row % sh.Hq), G = sh.G;
   if (row >= rows || tok >= cu_q[sh.B]) return;
   // the row's sequence, item and segments
   TreeBatch<kChunk> t;
@@ -537,20 +567,20 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
   if (!here) return;  // counts out of range (invalid input)
   const int j = __builtin_ctzll(here);
   off += lane_of(t.upto, j) - lane_of(t.w, j);
-  const int r = (tok - int(lane_of(uint32_t(t.q0), j))) * G + h % G, part = r / sh.item_rows, g = h / G;
+  const int r = (tok - int(lane_of(uint32_t(t.q0), j))) * G + h - sh.token(h) * G, part = r >> sh.item_shift, g = sh.token(h);
   const uint32_t n = TreeBatch<kChunk>::chunks(int(lane_of(uint32_t(t.keys), j)));
   const uint32_t items = TreeBatch<kChunk>::items(sh, int(lane_of(uint32_t(t.T), j)));
   off += (uint32_t(g) * items + uint32_t(part)) * n;
   const uint32_t wg0 = off / share;
   const int n_seg = n > 0 ? int((off + n - 1) / share - wg0) + 1 : 0;
-  const size_t row0 = (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) * sh.item_rows +
-                      (r - part * sh.item_rows);
+  const size_t row0 = (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) * sh.item_rows() +
+                      (r & (sh.item_rows() - 1));
   const bool mine = kE * lane < DH;
   float M = -INFINITY, l = 0.f;
   vec_t o = 0.f;
   for (int p0 = first; p0 < n_seg; p0 += 64 * kWaves) {
     const int p = p0 + kWaves * lane;
-    const size_t at = row0 + size_t(p) * sh.item_rows;
+    const size_t at = row0 + (size_t(p) << sh.item_shift);
     const float lp = p < n_seg ? part_l[at] : 0.f;
     const float mp = lp == 0.f ? -INFINITY : part_m[at];  // 0: the segment holds nothing the row sees
     const float top = fmaxf(M, wave_max(mp));
@@ -570,7 +600,7 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
         w[u] = x < 0 ? 0.f : __shfl(f, x, 64);
         v[u] = 0.f;
         if (x >= 0 && mine)
-          v[u] = *reinterpret_cast<const vec_t*>(part_o + (row0 + size_t(p0 + kWaves * x) * sh.item_rows) * DH + kE * lane);
+          v[u] = *reinterpret_cast<const vec_t*>(part_o + (row0 + (size_t(p0 + kWaves * x) << sh.item_shift)) * DH + kE * lane);
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) o += w[u] * v[u];
@@ -650,17 +680,17 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
   struct RowInfo {  // of weight 0: not used
     float w, l2;
     uint64_t bits;
-    int r;
+    int r;  // row of Q
   };
   __shared__ __attribute__((aligned(16))) char qs[kWRows * kRow];
   __shared__ __attribute__((aligned(16))) RowInfo info[kWRows];
   __shared__ int live[2];
-  RowInfo mine{0.f, 0.f, 0, -1};
+  RowInfo mine{0.f, 0.f, 0, 0};
   int place = 0;
-  const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.Hq / sh.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.G;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  tree_walk<kWKeys>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
+  tree_walk<kWKeys, 4>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
     const int R = q.T * G;
     const size_t at = size_t(q.b * sh.Hkv + q.g) * sh.cap;
     auto load_k = [&](bf16x8_t(&kf)[2][kNK], int k) {
@@ -678,17 +708,19 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
     if (first < q.k1) load_k(kf, first);
     int n_rows = min(kWRows, R - r0);
     __syncthreads();  // the last rows are read
-    // the rows that count, next to each other (of a tree often few: the accepted ones); the rest of the last 16 zero
+    // the rows that count, next to each other (of a tree often few: the accepted ones); the rest of the last 16 are the
+    // last of them again, with weight 0 and an infinite normaliser
     if (tid < kWRows) {
       RowInfo x{0.f, 0.f, 0, 0};
       if (tid < n_rows) {
-        const int r = r0 + tid, tok = q.q0 + r / G;
-        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r % G) * sh.n_q + tok];
-        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, tree_bits(mask, q.q0, r / G), r};
+        const int r = r0 + tid, t = sh.token(r), tok = q.q0 + t;
+        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r - t * G) * sh.n_q + tok];
+        const uint64_t bits = tree_bits(mask, q, t);
+        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, bits, tok * sh.Hq + q.g * G + r - t * G};
       }
       const uint64_t counts = __ballot(x.w != 0.f);
       if (lane == 0) live[wave] = int(__popcll(counts));
-      info[tid] = RowInfo{0.f, 0.f, 0, -1};
+      info[tid] = RowInfo{0.f, INFINITY, 0, 0};
       mine = x;
       place = int(__popcll(counts & ((uint64_t(1) << lane) - 1)));
     }
@@ -697,11 +729,9 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
     n_rows = live[0] + live[1];
     __syncthreads();
     for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
-      const int row = i / kPieces, c = i % kPieces, r = info[row].r;
-      uint4 v{0, 0, 0, 0};
-      if (r >= 0)
-        v = reinterpret_cast<const uint4*>(Q)[(size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * kPieces + c];
-      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) = v;
+      const int row = i / kPieces, c = i % kPieces, r = info[min(row, n_rows - 1)].r;
+      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) =
+          reinterpret_cast<const uint4*>(Q)[size_t(r) * kPieces + c];
     }
     __syncthreads();
     for (int k = first; k < q.k1; k += 4 * kWKeys) {
@@ -714,26 +744,38 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
       float sum[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-      for (int r = 0; r < n_rows; r += 16) {
-        const RowInfo x = info[r + fr];
-        bf16x8_t qf[kNK];
+      auto add_rows = [&](auto at_edge) {
+        for (int r = 0; r < n_rows; r += 16) {
+          const float w = info[r + fr].w, l2 = info[r + fr].l2;
+          const uint64_t bits = decltype(at_edge)::value ? info[r + fr].bits : 0;
+          bf16x8_t qf[kNK];
 #pragma unroll
-        for (int c = 0; c < kNK; ++c)
-          qf[c] = *reinterpret_cast<const bf16x8_t*>(qs + (r + fr) * kRow +
-                                                     ((4 * c + fq) ^ ((r + fr) / kWindow & (kPieces - 1))) * 16);
+          for (int c = 0; c < kNK; ++c)
+            qf[c] = *reinterpret_cast<const bf16x8_t*>(qs + (r + fr) * kRow +
+                                                       ((4 * c + fq) ^ ((r + fr) / kWindow & (kPieces - 1))) * 16);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          f32x4_t s{0.f, 0.f, 0.f, 0.f};
+          for (int a = 0; a < 2; ++a) {
+            const uint32_t sees = decltype(at_edge)::value ? tree_sees4(bits, k + 16 * a + 4 * fq - q.len) : 15u;
+            f32x4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
+            for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
 #pragma unroll
-          for (int z = 0; z < 4; ++z) {
-            bool sees = x.w != 0.f;
-            if (edge) sees &= tree_sees(x.bits, k + 16 * a + 4 * fq + z - q.len);
-            sum[4 * a + z] += sees ? x.w * fast_exp2(fmaf(s[z], c2, -x.l2)) : 0.f;
+            for (int z = 0; z < 4; ++z) {
+              // (cached keys are seen by every row; one behind the last adds 0 exp2(score - infinity), NaN only where
+              // the last row's is)
+              const float p = fast_exp2(fmaf(s[z], c2, -l2));
+              if constexpr (decltype(at_edge)::value)
+                sum[4 * a + z] = (sees >> z) & 1 ? fmaf(w, p, sum[4 * a + z]) : sum[4 * a + z];
+              else
+                sum[4 * a + z] = fmaf(w, p, sum[4 * a + z]);
+            }
           }
         }
-      }
+      };
+      if (edge)
+        add_rows(std::true_type{});
+      else
+        add_rows(std::false_type{});
 #pragma unroll
       for (int half = 4; half >= 1; half >>= 1) {
         const bool upper = (fr & half) != 0;
@@ -804,20 +846,20 @@ __global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ 
 // How a call is cut: items of item_rows rows, at most `items` of them a (sequence, KV head), their chunks shared by
 // `wgs` workgroups.
 struct TreePlan {
-  int item_rows, items, wgs;
+  int item_shift, items, wgs;
   bool stored;  // the scores are kept for the account
 };
 inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
   const int64_t rows = int64_t(max_q) * (Hq / Hkv);
   TreePlan p;
-  p.item_rows = dtype == ESTP_F32 || rows <= 16 ? 16 : 32;
-  p.items = int((rows + p.item_rows - 1) / p.item_rows);
+  p.item_shift = dtype == ESTP_F32 || rows <= 16 ? 4 : 5;
+  p.items = int((rows + (1 << p.item_shift) - 1) >> p.item_shift);
   // one grid fills the chip: what 160 KB of LDS hold of the rings (fp32: two workgroups of 4 waves) on 256 units
   const int64_t fill = dtype == ESTP_F32 ? 512 : 1024 * (128 / dh);
   const int64_t shares = (int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) + 3) / 4;  // at most
   p.wgs = int((std::min(fill, shares) + 7) / 8 * 8);
   // Scores: 8 bytes a row and key, written and read, against 2 dh for forming them again.
-  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.item_rows == 16 && rows * 4 <= dh;
+  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.item_shift == 4 && rows * 4 <= dh;
   return p;
 }
 
@@ -828,7 +870,7 @@ struct TreeBuffers {
 };
 inline TreeBuffers carve_tree(const TreePlan& p, int B, int64_t n_q, int Hq, int Hkv, int max_kv, int dh, void* ws) {
   // a segment more than the last for every workgroup and for every item
-  const size_t rows = (size_t(p.wgs) + size_t(B) * Hkv * p.items) * p.item_rows;
+  const size_t rows = (size_t(p.wgs) + size_t(B) * Hkv * p.items) << p.item_shift;
   Carver c(ws);
   TreeBuffers t;
   t.m = c.take<float>(rows);
@@ -860,7 +902,7 @@ int check_tree_args(const char* fn, const void* Q, const void* K, const int32_t*
                fn);
   ESTP_REQUIRE(dh == 32 || dh == 64 || dh == 128, ESTP_ERR_UNSUPPORTED, "%s: head_dim %d not in {32, 64, 128}", fn, dh);
   ESTP_REQUIRE(max_q <= kMaxTree, ESTP_ERR_UNSUPPORTED, "%s: max_q = %d, at most %d drafted tokens", fn, max_q, kMaxTree);
-  ESTP_REQUIRE(int64_t(max_q) * (Hq / Hkv) <= 65535 && Hq <= 65536, ESTP_ERR_UNSUPPORTED,
+  ESTP_REQUIRE(int64_t(max_q) * (Hq / Hkv) <= 65535 && Hq / Hkv <= 32768 && Hq <= 65535, ESTP_ERR_UNSUPPORTED,
                "%s: %d query heads, %d sharing a KV head", fn, Hq, Hq / Hkv);
   ESTP_REQUIRE(int64_t(B) * Hkv <= 65535 && n_q * Hq <= INT32_MAX / 64, ESTP_ERR_UNSUPPORTED,
                "%s: B Hkv = %lld (at most 65535) or n_q Hq = %lld too large", fn, (long long)B * Hkv, (long long)n_q * Hq);
@@ -899,10 +941,10 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
   const dim3 grid{unsigned(p.wgs)};
   constexpr int kChunk = sizeof(T) == 2 ? 32 : kTKeys;
   if constexpr (sizeof(T) == 2) {
-    auto kernel = p.item_rows == 32 ? tree_attn_mfma_kernel<DH, 2, false>
+    auto kernel = p.item_shift == 5 ? tree_attn_mfma_kernel<DH, 2, false>
                   : scores          ? tree_attn_mfma_kernel<DH, 1, true>
                                     : tree_attn_mfma_kernel<DH, 1, false>;
-    kernel<<<grid, dim3(64), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
+    kernel<<<grid, dim3(64), 320 * DH, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
   } else {
     tree_attn_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
   }
@@ -928,7 +970,7 @@ int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, con
   const unsigned tiles = unsigned((sh.max_kv + kTKeys - 1) / kTKeys);
   const unsigned wgs = tiles * unsigned(sh.B * sh.Hkv);
   if constexpr (sizeof(T) == 2) {
-    sh.item_rows = INT32_MAX / 2;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
+    sh.item_shift = 16;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
     const dim3 grid(std::min(DH == 128 ? 768u : 1024u, (wgs + 7) / 8 * 8));  // (a share is 128 keys or more)
     tree_weight_mfma_kernel<DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
                                                            acc);
@@ -988,7 +1030,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   ESTP_REQUIRE(fits_launch(size_t(n_q) * Hq, 1024) &&
                    int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
-  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, p.item_rows, p.items};
+  const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, p.item_shift, p.items);
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, s);
@@ -1023,7 +1065,7 @@ extern "C" int estp_tree_importance(const void* Q, const void* K, const float* l
   ESTP_REQUIRE(lse && acc, ESTP_ERR_INVALID_ARG, "%s: lse and acc must be non-null", fn);
   ESTP_REQUIRE(aligned(tree_mask, 8) && aligned(lse, 4) && aligned(acc, 4) && aligned(row_weight, 4),
                ESTP_ERR_INVALID_ARG, "%s: tree_mask must be 8-byte, lse, row_weight and acc 4-byte aligned", fn);
-  const TreeShape sh{B, max_q, int(n_q), Hq, Hkv, int(cap), max_kv, 16, 1};
+  const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, 4, 1);
   const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, static_cast<hipStream_t>(stream));
   if (checked != ESTP_OK) return checked;
   return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
