@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
   });
 }
 
-// Matrix-core kernel (bf16): one wave per workgroup, items of 16 NRT rows, chunks of 32 keys.
+// Matrix-core kernel (bf16): items of 16 rows a wave, chunks of 32 keys.
 //
 // S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of the chunk's two 16-key blocks, keys
 // 4 fq .. 4 fq + 3 each (fq = lane / 16).  These 8 weights are at once the lane's part of the second product's
@@ -316,12 +316,13 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
 // passes it by 2^16 (sums and weights stay far from overflow): most chunks neither exchange maxima between lanes nor
 // rescale O.
 //
-// The chunks' K and V parts go straight from memory into a ring of five parts that this wave alone uses: no
-// barriers, only counts of its own transfers, two and a half chunks ahead.  Four such waves fill a compute unit's
-// LDS at a head size of 128, eight at 64.  16-byte pieces are swizzled so that the 16 rows of a K read and the 8 of
-// a transposing V read lie in distinct banks.
-template <int DH, int NRT, bool kScores>
-__global__ __launch_bounds__(64, 2) void tree_attn_mfma_kernel(
+// The chunks' K and V parts go straight from memory into a ring of five parts.  Up to 16 rows: one wave that uses the
+// ring alone, without barriers, and counts its own transfers, two and a half chunks ahead; memory bounds it.  More
+// rows: kW waves of 16 rows each share the ring, so that the keys are fetched once for all of them, and there are more
+// waves on a compute unit to hide one another's waits.  16-byte pieces are swizzled so that the 16 rows of a K read
+// and the 8 of a transposing V read lie in distinct banks.
+template <int DH, int kW, bool kScores>
+__global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
     const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     const int* __restrict__ lens, const int* __restrict__ cu_q, const int64_t* __restrict__ mask, TreeShape sh,
     float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m, float* __restrict__ part_l,
@@ -329,63 +330,52 @@ __global__ __launch_bounds__(64, 2) void tree_attn_mfma_kernel(
   constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
   constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
   constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // kSlots * kPart = 320 DH bytes
-  const int lane = threadIdx.x, fr = lane & 15, fq = lane >> 4, G = sh.G;
-  uint32_t off_k[kL], off_v[kL];
+  constexpr int kLw = kL / kW;           // transfers of a wave for a part
+  static_assert(kL % kW == 0, "waves share a part's transfers equally");
+  // The ring, and 16 rows of Q for each of several waves: tree_lds(DH, kW) bytes.  (Dynamic: of a size it knows, the
+  // compiler takes one wave a SIMD for granted at a head size of 128, and copies sums between two register files.)
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4, G = sh.G;
+  const int wave = kW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t off_k[kLw], off_v[kLw];
 #pragma unroll
-  for (int i = 0; i < kL; ++i) {
-    const int piece = 64 * i + lane, row = piece / kPieces, c = piece % kPieces;
+  for (int i = 0; i < kLw; ++i) {
+    const int piece = 64 * (kW * i + wave) + lane, row = piece / kPieces, c = piece % kPieces;
     off_k[i] = uint32_t(row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16);
     off_v[i] = uint32_t(row * kRow + (c ^ (2 * (row / kWindow & (kPieces / 2 - 1)))) * 16);
   }
-  auto read_k = [&](int at_slot, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
-    return *reinterpret_cast<const bf16x8_t*>(lds + at_slot * kPart + row * kRow +
+  auto read_k = [&](const char* part, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
+    return *reinterpret_cast<const bf16x8_t*>(part + row * kRow +
                                               ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
   };
   auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
   // neighbouring shares, whose items have keys in common, on one XCD (the grid is a multiple of 8)
   const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   tree_walk<kC>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
-  const int bg = q.b * sh.Hkv + q.g, g = q.g, r0 = q.r0, k0 = q.k0, k1 = q.k1, R = q.T * G;
-  float m[NRT], l[NRT];
-  f32x4_t o[NRT][kND];
-#pragma unroll
-  for (int t = 0; t < NRT; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-#pragma unroll
-    for (int d = 0; d < kND; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  {
+    const int bg = q.b * sh.Hkv + q.g, r0 = q.r0 + 16 * wave, R = q.T * G, r = r0 + fr;
     const char* Kb = reinterpret_cast<const char*>(K) + size_t(bg) * sh.cap * kRow;
     const char* Vb = reinterpret_cast<const char*>(V) + size_t(bg) * sh.cap * kRow;
-    int pf_key = k0, pf_slot = 0;
-    auto issue = [&](const char* base, const uint32_t (&off)[kL]) {  // past the range: an empty resource, no access
+    int pf_key = q.k0, pf_slot = 0;
+    auto issue = [&](const char* base, const uint32_t (&off)[kLw]) {  // past the range: an empty resource, no access
       const int left = min(kC, q.keys - pf_key);
-      const u32x4_t r = rsrc_words(base + size_t(pf_key) * kRow, pf_key < k1 ? uint32_t(left) * kRow : 0u);
+      const u32x4_t rsrc = rsrc_words(base + size_t(pf_key) * kRow, pf_key < q.k1 ? uint32_t(left) * kRow : 0u);
 #pragma unroll
-      for (int i = 0; i < kL; ++i) dma16(r, off[i], 0, lds + pf_slot * kPart + 1024 * i);
+      for (int i = 0; i < kLw; ++i) dma16(rsrc, off[i], 0, lds + pf_slot * kPart + 1024 * (kW * i + wave));
       pf_slot = pf_slot + 1 == kSlots ? 0 : pf_slot + 1;
     };
-    uint64_t bits[NRT];
+    const uint64_t bits = r < R ? tree_bits(mask, q, sh.token(r)) : 0;
+    if (kW > 1) lds_barrier();  // every wave's reads of the last segment are done
+    // the wave's rows of Q come first, laid out as a K part, through the ring's last slot or places of their own: a
+    // load into registers would wait for every transfer issued around it
+    char* const own = lds + (kW == 1 ? (kSlots - 1) * kPart : kSlots * kPart + wave * (16 * kRow));
+    const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
+                                  uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
 #pragma unroll
-    for (int t = 0; t < NRT; ++t) {
-      const int r = r0 + 16 * t + fr;
-      bits[t] = r < R ? tree_bits(mask, q, sh.token(r)) : 0;
-    }
-    // the rows of Q come first, through the ring's last slot and laid out as a K part: a load of their own would
-    // wait for every transfer issued around it
-    {
-      const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
-                                    uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
-#pragma unroll
-      for (int i = 0; i < kL * NRT / 2; ++i) {
-        const int row = (64 * i + lane) / kPieces, r = r0 + row;
-        const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (row / kWindow & (kPieces - 1))) * 16u;
-        const uint32_t tok = uint32_t(sh.token(r)), head = uint32_t(g * G + r) - tok * uint32_t(G);
-        dma16(rq, r < R ? (tok * uint32_t(sh.Hq) + head) * kRow + piece : kPastEnd, 0,
-              lds + (kSlots - 1) * kPart + 1024 * i);
-      }
+    for (int i = 0; i < kL / 2; ++i) {
+      const int at = (64 * i + lane) / kPieces, row = r0 + at;
+      const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (at / kWindow & (kPieces - 1))) * 16u;
+      const uint32_t tok = uint32_t(sh.token(row)), head = uint32_t(q.g * G + row) - tok * uint32_t(G);
+      dma16(rq, row < R ? (tok * uint32_t(sh.Hq) + head) * kRow + piece : kPastEnd, 0, own + 1024 * i);
     }
     issue(Kb, off_k);
     issue(Vb, off_v);
@@ -393,76 +383,89 @@ __global__ __launch_bounds__(64, 2) void tree_attn_mfma_kernel(
     issue(Kb, off_k);
     issue(Vb, off_v);
     pf_key += kC;
-    arrived<(kSlots - 1) * kL>();
-    bf16x8_t qf[NRT][kNK];
+    arrived<4 * kLw>();
+    bf16x8_t qf[kNK];
 #pragma unroll
-    for (int t = 0; t < NRT; ++t)
-#pragma unroll
-      for (int c = 0; c < kNK; ++c) qf[t][c] = read_k(kSlots - 1, 16 * t + fr, c);
+    for (int c = 0; c < kNK; ++c) qf[c] = read_k(own, fr, c);
     lds_read_done();
-    issue(Kb, off_k);
+    if (kW == 1) issue(Kb, off_k);
+    float m = -INFINITY, l = 0.f;
+    f32x4_t o[kND];
+#pragma unroll
+    for (int d = 0; d < kND; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     int slot = 0;
-    for (int k = k0; k < k1; k += kC) {
+    // A part may be read when it has landed, its slot be filled again when it is read.  One wave: four parts stay in
+    // flight, the fifth follows the read.  Several: a barrier says that every wave's transfers of the part have landed
+    // and that every wave has read the part before it, whose slot the next transfers take.
+    auto part_landed = [&]() {
+      arrived<(kW == 1 ? 4 : 3) * kLw>();
+      if (kW > 1) lds_barrier();
+    };
+    for (int k = q.k0; k < q.k1; k += kC) {
       const bool edge = k + kC > q.len;  // holds drafted tokens, or ends the sequence
       // ---- scores
-      arrived<(kSlots - 1) * kL>();
+      part_landed();
+      if (kW > 1) issue(Kb, off_k);
       bf16x8_t kf[2][kNK];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int c = 0; c < kNK; ++c) kf[a][c] = read_k(slot, 16 * a + fr, c);
+        for (int c = 0; c < kNK; ++c) kf[a][c] = read_k(lds + slot * kPart, 16 * a + fr, c);
       lds_read_done();
-      issue(Vb, off_v);
-      pf_key += kC;
+      if (kW == 1) {
+        issue(Vb, off_v);
+        pf_key += kC;
+      }
       slot = slot + 1 == kSlots ? 0 : slot + 1;
-      float p[NRT][8];
-      bf16x8_t pf[NRT];
+      f32x4_t s[2];
 #pragma unroll
-      for (int t = 0; t < NRT; ++t) {
-        f32x4_t s[2];
+      for (int a = 0; a < 2; ++a) {
+        s[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kNK; ++c) s[a] = mfma_bf16(kf[a][c], qf[c], s[a]);
+      }
+      if (edge) {
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-          s[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          const uint32_t sees = tree_sees4(bits, k + 16 * a + 4 * fq - q.len);
 #pragma unroll
-          for (int c = 0; c < kNK; ++c) s[a] = mfma_bf16(kf[a][c], qf[t][c], s[a]);
-        }
-        if (edge) {
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const uint32_t sees = tree_sees4(bits[t], k + 16 * a + 4 * fq - q.len);
-#pragma unroll
-            for (int z = 0; z < 4; ++z) s[a][z] = (sees >> z) & 1 ? s[a][z] : -INFINITY;
-          }
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
-        mx *= c2;
-        if (kScores && r0 + 16 * t + fr < R) {
-          float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
-          *reinterpret_cast<f32x4_t*>(w) = s[0] * c2;
-          *reinterpret_cast<f32x4_t*>(w + 16) = s[1] * c2;
-        }
-        if (__any(mx > m[t] + 16.f)) {
-          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-          mx = fmaxf(mx, m[t]);
-          const float f = fast_exp2(m[t] - (mx == -INFINITY ? 0.f : mx));
-          m[t] = mx;
-          l[t] *= f;
-#pragma unroll
-          for (int d = 0; d < kND; ++d) o[t][d] *= f;
-        }
-        const float ref = m[t] == -INFINITY ? 0.f : m[t];  // nothing seen yet: all weights are 0
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[t][e] = fast_exp2(fmaf(s[e / 4][e % 4], c2, -ref));
-          l[t] += p[t][e];
-          pf[t][e] = __bf16(p[t][e]);  // as the matrix cores take it; l keeps the unrounded sum
+          for (int z = 0; z < 4; ++z) s[a][z] = (sees >> z) & 1 ? s[a][z] : -INFINITY;
         }
       }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
+      mx *= c2;
+      if (kScores && r < R) {
+        float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
+        *reinterpret_cast<f32x4_t*>(w) = s[0] * c2;
+        *reinterpret_cast<f32x4_t*>(w + 16) = s[1] * c2;
+      }
+      if (__any(mx > m + 16.f)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        mx = fmaxf(mx, m);
+        const float f = fast_exp2(m - (mx == -INFINITY ? 0.f : mx));
+        m = mx;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < kND; ++d) o[d] *= f;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: all weights are 0
+      float p[8];
+      bf16x8_t pf;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = fast_exp2(fmaf(s[e / 4][e % 4], c2, -ref));
+        l += p[e];
+        pf[e] = __bf16(p[e]);  // as the matrix cores take it; l keeps the unrounded sum
+      }
       // ---- output
-      arrived<(kSlots - 1) * kL>();
+      part_landed();
+      if (kW > 1) {
+        issue(Vb, off_v);
+        pf_key += kC;
+      }
       const char* vs = lds + slot * kPart;
       bf16x8_t vf[kND];
 #pragma unroll
@@ -493,50 +496,40 @@ __global__ __launch_bounds__(64, 2) void tree_attn_mfma_kernel(
           }
           for (int j = 0; j < kC && k + j < q.keys; ++j) {
             const int from = fr + 16 * (j % 16 / 4), e = j / 16 * 4 + j % 4;
+            float mine = 0.f;
 #pragma unroll
-            for (int t = 0; t < NRT; ++t) {
-              float mine = 0.f;
+            for (int z = 0; z < 8; ++z) mine = z == e ? p[z] : mine;
+            const float w = __shfl(mine, from, 64);
+            if (!tree_sees(bits, k + j - q.len)) continue;
 #pragma unroll
-              for (int z = 0; z < 8; ++z) mine = z == e ? p[t][z] : mine;
-              const float w = __shfl(mine, from, 64);
-              if (!tree_sees(bits[t], k + j - q.len)) continue;
+            for (int d = 0; d < kND; ++d)
 #pragma unroll
-              for (int d = 0; d < kND; ++d)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                  const int at_d = 16 * d + 4 * fq + z;
-                  const uint16_t v = *reinterpret_cast<const uint16_t*>(
-                      vs + j * kRow + ((at_d / 16) ^ unit_of(j)) * 32 + (at_d % 16) * 2);
-                  if ((v & 0x7f80) == 0x7f80) o[t][d][z] += w * bf16_to_f32(v);
-                }
-            }
+              for (int z = 0; z < 4; ++z) {
+                const int at_d = 16 * d + 4 * fq + z;
+                const uint16_t v = *reinterpret_cast<const uint16_t*>(
+                    vs + j * kRow + ((at_d / 16) ^ unit_of(j)) * 32 + (at_d % 16) * 2);
+                if ((v & 0x7f80) == 0x7f80) o[d][z] += w * bf16_to_f32(v);
+              }
           }
           lds_read_done();
         }
       }
-      issue(Kb, off_k);
+      if (kW == 1) issue(Kb, off_k);
       slot = slot + 1 == kSlots ? 0 : slot + 1;
 #pragma unroll
-      for (int t = 0; t < NRT; ++t)
-#pragma unroll
-        for (int d = 0; d < kND; ++d) o[t][d] = mfma_bf16(vf[d], pf[t], o[t][d]);
+      for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf, o[d]);
     }
     arrived<0>();  // no transfer into LDS outlives the segment
-  }
-#pragma unroll
-  for (int t = 0; t < NRT; ++t) {
-    const int r = r0 + 16 * t + fr;
-    l[t] += __shfl_xor(l[t], 16, 64);
-    l[t] += __shfl_xor(l[t], 32, 64);
-    if (r >= R) continue;
-    const size_t row = size_t(q.slot) * (16 * NRT) + 16 * t + fr;
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (r >= R) return;
+    const size_t row = size_t(q.slot) * (16 * kW) + 16 * wave + fr;
     if (fq == 0) {
-      part_m[row] = m[t];
-      part_l[row] = l[t];
+      part_m[row] = m;
+      part_l[row] = l;
     }
 #pragma unroll
-    for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[t][d];
-  }
+    for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[d];
   });
 }
 
@@ -550,11 +543,11 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
     float* __restrict__ lse) {
   constexpr int kE = DH >= 64 ? DH / 64 : 1;
   typedef float vec_t __attribute__((ext_vector_type(kE)));
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t rows = int64_t(sh.n_q) * sh.Hq, row = kWaves == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
-  const int first = kWaves == 1 ? 0 : wave;
-  const int tok = int(row / sh.Hq), h = int(row % sh.Hq), G = sh.G;
-  if (row >= rows || tok >= cu_q[sh.B]) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int first = kWaves == 1 ? 0 : wave, G = sh.G;
+  const int tok = blockIdx.x, h = kWaves == 1 ? int(blockIdx.y) * 4 + wave : int(blockIdx.y);
+  if (h >= sh.Hq || tok >= cu_q[sh.B]) return;
+  const size_t row = size_t(tok) * sh.Hq + h;
   // the row's sequence, item and segments
   TreeBatch<kChunk> t;
   const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
@@ -843,23 +836,29 @@ __global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ 
 
 // ------------------------------------------------------------------ plan and workspace
 
-// How a call is cut: items of item_rows rows, at most `items` of them a (sequence, KV head), their chunks shared by
-// `wgs` workgroups.
+// How a call is cut: items of 2^item_shift rows, 16 a wave (fp32: 16 a workgroup), at most `items` of them a
+// (sequence, KV head), their chunks shared by `wgs` workgroups.
 struct TreePlan {
+  int waves;  // of a matrix-core workgroup
   int item_shift, items, wgs;
   bool stored;  // the scores are kept for the account
 };
+// Waves that share a ring: as many as have a transfer of each part (two at a head size of 32).
+constexpr int tree_waves(int dh) { return dh == 32 ? 2 : 4; }
+// LDS of tree_attn_mfma_kernel: the ring, and the rows of Q of several waves.
+inline int tree_lds(int dh, int waves) { return 320 * dh + (waves > 1 ? waves * 32 * dh : 0); }
 inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
   const int64_t rows = int64_t(max_q) * (Hq / Hkv);
   TreePlan p;
-  p.item_shift = dtype == ESTP_F32 || rows <= 16 ? 4 : 5;
+  p.waves = dtype == ESTP_F32 || rows <= 16 ? 1 : tree_waves(dh);
+  p.item_shift = p.waves == 1 ? 4 : p.waves == 2 ? 5 : 6;
   p.items = int((rows + (1 << p.item_shift) - 1) >> p.item_shift);
-  // one grid fills the chip: what 160 KB of LDS hold of the rings (fp32: two workgroups of 4 waves) on 256 units
-  const int64_t fill = dtype == ESTP_F32 ? 512 : 1024 * (128 / dh);
+  // one grid fills the chip: what 160 KB of LDS hold of the rings, or registers of the waves, on 256 units
+  const int64_t fill = dtype == ESTP_F32 ? 512 : p.waves == 1 ? 1024 * (128 / dh) : 512 * std::min(128 / dh, 4);
   const int64_t shares = (int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) + 3) / 4;  // at most
   p.wgs = int((std::min(fill, shares) + 7) / 8 * 8);
   // Scores: 8 bytes a row and key, written and read, against 2 dh for forming them again.
-  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.item_shift == 4 && rows * 4 <= dh;
+  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.waves == 1 && rows * 8 <= dh;
   return p;
 }
 
@@ -941,26 +940,25 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
   const dim3 grid{unsigned(p.wgs)};
   constexpr int kChunk = sizeof(T) == 2 ? 32 : kTKeys;
   if constexpr (sizeof(T) == 2) {
-    auto kernel = p.item_shift == 5 ? tree_attn_mfma_kernel<DH, 2, false>
-                  : scores          ? tree_attn_mfma_kernel<DH, 1, true>
-                                    : tree_attn_mfma_kernel<DH, 1, false>;
-    kernel<<<grid, dim3(64), 320 * DH, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
+    auto kernel = p.waves > 1 ? tree_attn_mfma_kernel<DH, tree_waves(DH), false>
+                  : scores    ? tree_attn_mfma_kernel<DH, 1, true>
+                              : tree_attn_mfma_kernel<DH, 1, false>;
+    kernel<<<grid, dim3(64 * p.waves), tree_lds(DH, p.waves), s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
   } else {
     tree_attn_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
   }
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
-  const size_t rows = size_t(sh.n_q) * sh.Hq;
-  auto join = [&](auto kernel, size_t wgs, int threads) {
-    kernel<<<dim3(unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
+  auto join = [&](auto kernel, int wgs, int threads) {  // wgs: of a token
+    kernel<<<dim3(unsigned(sh.n_q), unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
   };
   // segments of an item, about: waves of a row
   const int64_t segs = std::min<int64_t>(int64_t(p.wgs) / (int64_t(sh.B) * sh.Hkv * p.items), sh.max_kv / 128) + 2;
-  if (segs <= 16)
-    join(tree_join_kernel<T, DH, 1, kChunk>, (rows + 3) / 4, 256);
+  if (segs <= 24)
+    join(tree_join_kernel<T, DH, 1, kChunk>, (sh.Hq + 3) / 4, 256);
   else if (segs <= 64)
-    join(tree_join_kernel<T, DH, 4, kChunk>, rows, 256);
+    join(tree_join_kernel<T, DH, 4, kChunk>, sh.Hq, 256);
   else
-    join(tree_join_kernel<T, DH, 16, kChunk>, rows, 1024);
+    join(tree_join_kernel<T, DH, 16, kChunk>, sh.Hq, 1024);
   ESTP_CHECK_LAUNCH("tree_join_kernel");
   return ESTP_OK;
 }
