@@ -533,22 +533,51 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
   });
 }
 
-// Joins the partial results of each row's segments.  kWaves waves share a row and take every kWaves-th segment; a
-// lane fetches the state of one segment, 64 at a time, and DH / 64 (at least one) columns of those that hold
-// something.  Rows past the last sequence's are left as they are.
+// Where the partial results of an item lie: those of its n_seg segments, item_rows rows apart, the first's at row0.
+struct TreeParts {
+  int n_seg;
+  size_t row0;
+};
+// of part `part` of KV head g of the sequence in lane j of t, whose chunks start `off` chunks into the line
+template <int kChunk>
+__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, const TreeBatch<kChunk>& t, int j, uint32_t off,
+                                                uint32_t share, int g, int part) {
+  const uint32_t n = TreeBatch<kChunk>::chunks(int(lane_of(uint32_t(t.keys), j)));
+  const uint32_t items = TreeBatch<kChunk>::items(sh, int(lane_of(uint32_t(t.T), j)));
+  off += lane_of(t.upto, j) - lane_of(t.w, j) + (uint32_t(g) * items + uint32_t(part)) * n;
+  const uint32_t wg0 = off / share;
+  return {n > 0 ? int((off + n - 1) / share - wg0) + 1 : 0,
+          (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) << sh.item_shift};
+}
+// Running (maximum, sum) of a row over 64 segments of its item, first, first + step, ... < n_seg, one a lane; returns
+// the weight of the lane's segment against the new maximum.  The row's states start at part_m, part_l + row0.
+__device__ __forceinline__ float tree_fold(const float* part_m, const float* part_l, size_t row0, int item_shift,
+                                           int n_seg, int first, int step, float& M, float& l, float& down) {
+  const int p = first + step * int(threadIdx.x & 63);
+  const size_t at = row0 + (size_t(min(p, n_seg - 1)) << item_shift);
+  const float ms = part_m[at], ls = part_l[at];
+  const float lp = p < n_seg ? ls : 0.f, mp = lp == 0.f ? -INFINITY : ms;  // 0: the segment holds nothing the row sees
+  const float top = fmaxf(M, wave_max(mp)), ref = top == -INFINITY ? 0.f : top;
+  down = fast_exp2(M - ref);
+  const float f = lp == 0.f ? 0.f : fast_exp2(mp - ref);
+  M = top;
+  l = l * down + wave_sum(f * lp);
+  return f;
+}
+
+// Joins the partial results of the segments of row (token tok, head h).  kWaves waves share a row and take every
+// kWaves-th segment; a lane fetches the state of one segment, 64 at a time, and DH / 64 (at least one) columns of
+// each.  Rows past the last sequence's are left as they are.
 template <typename T, int DH, int kWaves, int kChunk>
-__global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_kernel(
-    const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
-    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
-    float* __restrict__ lse) {
+__device__ __forceinline__ void tree_join(const float* __restrict__ part_m, const float* __restrict__ part_l,
+                                          const float* __restrict__ part_o, const int* __restrict__ lens,
+                                          const int* __restrict__ cu_q, const TreeShape& sh, int wgs, int tok, int h,
+                                          T* __restrict__ O, float* __restrict__ lse) {
   constexpr int kE = DH >= 64 ? DH / 64 : 1;
   typedef float vec_t __attribute__((ext_vector_type(kE)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int first = kWaves == 1 ? 0 : wave, G = sh.G;
-  const int tok = blockIdx.x, h = kWaves == 1 ? int(blockIdx.y) * 4 + wave : int(blockIdx.y);
+  const int first = kWaves == 1 ? 0 : wave;
   if (h >= sh.Hq || tok >= cu_q[sh.B]) return;
-  const size_t row = size_t(tok) * sh.Hq + h;
-  // the row's sequence, item and segments
   TreeBatch<kChunk> t;
   const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
   uint32_t off = 0;
@@ -558,45 +587,36 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
     t.fetch(sh, lens, cu_q, t.b0 + 64);
   }
   if (!here) return;  // counts out of range (invalid input)
-  const int j = __builtin_ctzll(here);
-  off += lane_of(t.upto, j) - lane_of(t.w, j);
-  const int r = (tok - int(lane_of(uint32_t(t.q0), j))) * G + h - sh.token(h) * G, part = r >> sh.item_shift, g = sh.token(h);
-  const uint32_t n = TreeBatch<kChunk>::chunks(int(lane_of(uint32_t(t.keys), j)));
-  const uint32_t items = TreeBatch<kChunk>::items(sh, int(lane_of(uint32_t(t.T), j)));
-  off += (uint32_t(g) * items + uint32_t(part)) * n;
-  const uint32_t wg0 = off / share;
-  const int n_seg = n > 0 ? int((off + n - 1) / share - wg0) + 1 : 0;
-  const size_t row0 = (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) * sh.item_rows() +
-                      (r & (sh.item_rows() - 1));
+  const int j = __builtin_ctzll(here), g = sh.token(h);
+  const int r = (tok - int(lane_of(uint32_t(t.q0), j))) * sh.G + h - g * sh.G;
+  const TreeParts parts = tree_parts(sh, t, j, off, share, g, r >> sh.item_shift);
+  const size_t row0 = parts.row0 + (r & (sh.item_rows() - 1));
   const bool mine = kE * lane < DH;
   float M = -INFINITY, l = 0.f;
   vec_t o = 0.f;
-  for (int p0 = first; p0 < n_seg; p0 += 64 * kWaves) {
-    const int p = p0 + kWaves * lane;
-    const size_t at = row0 + (size_t(p) << sh.item_shift);
-    const float lp = p < n_seg ? part_l[at] : 0.f;
-    const float mp = lp == 0.f ? -INFINITY : part_m[at];  // 0: the segment holds nothing the row sees
-    const float top = fmaxf(M, wave_max(mp));
-    const float ref = top == -INFINITY ? 0.f : top, down = fast_exp2(M - ref);
-    const float f = lp == 0.f ? 0.f : fast_exp2(mp - ref);
-    M = top;
-    l = l * down + wave_sum(f * lp);
-    o *= down;
-    uint64_t left = __ballot(lp != 0.f);
-    while (left) {
-      vec_t v[4];
-      float w[4];
+  for (int p0 = first; p0 < parts.n_seg; p0 += 64 * kWaves) {
+    const int n = min(64, (parts.n_seg - p0 + kWaves - 1) / kWaves);
+    auto columns = [&](vec_t(&v)[4], int x) {  // of four segments
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {  // four segments' columns in flight
-        const int x = left ? __builtin_ctzll(left) : -1;
-        left &= left - 1;
-        w[u] = x < 0 ? 0.f : __shfl(f, x, 64);
+      for (int u = 0; u < 4; ++u) {
         v[u] = 0.f;
-        if (x >= 0 && mine)
-          v[u] = *reinterpret_cast<const vec_t*>(part_o + (row0 + (size_t(p0 + kWaves * x) << sh.item_shift)) * DH + kE * lane);
+        if (x + u < n && mine)
+          v[u] = *reinterpret_cast<const vec_t*>(
+              part_o + (row0 + (size_t(p0 + kWaves * (x + u)) << sh.item_shift)) * DH + kE * lane);
       }
+    };
+    vec_t v[4], next[4];
+    columns(v, 0);  // on their way before the states have come
+    float down;
+    const float f = tree_fold(part_m, part_l, row0, sh.item_shift, parts.n_seg, p0, kWaves, M, l, down);
+    o *= down;
+    for (int x = 0; x < n; x += 4) {
+      columns(next, x + 4);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) o += w[u] * v[u];
+      for (int u = 0; u < 4; ++u) {
+        o += __uint_as_float(lane_of(__float_as_uint(f), min(x + u, 63))) * v[u];
+        v[u] = next[u];
+      }
     }
   }
   if constexpr (kWaves > 1) {
@@ -625,36 +645,76 @@ __global__ __launch_bounds__(kWaves == 1 ? 256 : 64 * kWaves) void tree_join_ker
   const float inv = l == 0.f ? 0.f : 1.f / l;
   if (mine)
 #pragma unroll
-    for (int e = 0; e < kE; ++e) store1(O + row * DH + kE * lane + e, o[e] * inv);
+    for (int e = 0; e < kE; ++e) store1(O + (size_t(tok) * sh.Hq + h) * DH + kE * lane + e, o[e] * inv);
   if (lane == 0) lse[size_t(h) * sh.n_q + tok] = l == 0.f ? -INFINITY : kLn2 * (M + fast_log2(l));
 }
+constexpr int tree_join_threads(int waves) { return waves == 1 ? 256 : 64 * waves; }
+// One workgroup a row, or four rows of a token (one wave a row).
+template <typename T, int DH, int kWaves, int kChunk>
+__global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_join_kernel(
+    const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
+    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
+    float* __restrict__ lse) {
+  const int h = kWaves == 1 ? int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int(blockIdx.y);
+  tree_join<T, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, blockIdx.x, h, O, lse);
+}
 
-// acc[b][g][key] += sum over the rows of exp(s - lse), from the scores (base 2) the attention kernel has stored: a
-// thread per 4 keys.
-__global__ __launch_bounds__(256) void tree_weight_stored_kernel(const float* __restrict__ scores, int pitch,
-                                                                 const float* __restrict__ lse,
-                                                                 const int* __restrict__ lens,
-                                                                 const int* __restrict__ cu_q, TreeShape sh,
-                                                                 float* __restrict__ acc) {
-  const int bg = blockIdx.y, b = bg / sh.Hkv, g = bg % sh.Hkv, G = sh.Hq / sh.Hkv;
-  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
-  const int R = q.T * G, k = 4 * (blockIdx.x * 256 + threadIdx.x);
-  if (k >= q.keys || R == 0) return;
+// The join, and beside it acc[b][g][key] += sum over the rows of exp(s - lse) from the scores (base 2) that the
+// attention kernel has stored.  Workgroups n_join and on take 4 keys a thread of a (sequence, KV head), whose few rows'
+// normalisers they form for themselves: so neither waits for the other's launch.
+template <int DH, int kWaves, int kChunk>
+__global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
+    const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
+    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, uint16_t* __restrict__ O,
+    float* __restrict__ lse, int n_join, const float* __restrict__ scores, int pitch, float* __restrict__ acc) {
+  constexpr int kThreads = tree_join_threads(kWaves);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (int(blockIdx.x) < n_join) {
+    const uint32_t per = kWaves == 1 ? uint32_t(sh.Hq + 3) / 4 : uint32_t(sh.Hq);  // workgroups of a token
+    const uint32_t tok = blockIdx.x / per, y = blockIdx.x - tok * per;
+    tree_join<uint16_t, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, int(tok),
+                                            kWaves == 1 ? int(4 * y) + wave : int(y), O, lse);
+    return;
+  }
+  __shared__ float lse2[16];
+  const uint32_t id = blockIdx.x - n_join, bg = id % uint32_t(sh.B * sh.Hkv), k0 = id / uint32_t(sh.B * sh.Hkv) * (4 * kThreads);
+  const int b = int(bg / uint32_t(sh.Hkv)), g = int(bg) - b * sh.Hkv;
+  TreeBatch<kChunk> t;
+  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  uint32_t off = 0;
+  while (t.b0 + 64 <= b) {
+    off += t.all();
+    t.fetch(sh, lens, cu_q, t.b0 + 64);
+  }
+  const int j = b - t.b0, keys = int(lane_of(uint32_t(t.keys), j)), R = int(lane_of(uint32_t(t.T), j)) * sh.G;
+  if (int(k0) >= keys || R == 0) return;
+  const TreeParts parts = tree_parts(sh, t, j, off, share, g, 0);
+  const int k = int(k0) + 4 * int(threadIdx.x);
+  const float* s = scores + size_t(bg) * 16 * pitch + k;
+  f32x4_t first{0.f, 0.f, 0.f, 0.f};  // the first row's, on their way
+  if (k < keys) first = *reinterpret_cast<const f32x4_t*>(s);
+  for (int r = wave; r < R; r += kThreads / 64) {
+    float M = -INFINITY, l = 0.f, down;
+    for (int p0 = 0; p0 < parts.n_seg; p0 += 64)
+      tree_fold(part_m, part_l, parts.row0 + r, sh.item_shift, parts.n_seg, p0, 1, M, l, down);
+    if ((threadIdx.x & 63) == 0) lse2[r] = l == 0.f ? INFINITY : M + fast_log2(l);  // (infinite: adds nothing)
+  }
+  __syncthreads();
+  if (k >= keys) return;
   f32x4_t sum{0.f, 0.f, 0.f, 0.f};
   for (int r = 0; r < R; ++r) {
-    const float l = lse[size_t(g * G + r % G) * sh.n_q + q.q0 + r / G];
-    if (l == -INFINITY) continue;
-    const f32x4_t s = *reinterpret_cast<const f32x4_t*>(scores + (size_t(bg) * 16 + r) * pitch + k);
+    const f32x4_t x = r == 0 ? first : *reinterpret_cast<const f32x4_t*>(s + size_t(r) * pitch);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(fmaf(-l, kLog2e, s[e]));
+    for (int e = 0; e < 4; ++e) sum[e] += fast_exp2(x[e] - lse2[r]);
   }
   float* a = acc + size_t(bg) * sh.cap + k;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (k + e < q.keys) a[e] += sum[e];
+    if (k + e < keys) a[e] += sum[e];
 }
 
-// The same with the scores formed again on the matrix cores (bf16).  An item's rows wait in LDS, 128 at a time, with
+// acc[b][g][key] += sum over the rows of w exp(s - lse) with the scores formed again on the matrix cores (bf16).  An
+// item's rows wait in LDS, 128 at a time, with
 // their weights, normalisers and masks; a workgroup's share of 32-key tiles goes to its four waves in turn, a tile's
 // K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's columns are rows: their
 // sums join at the end of a tile, each exchange halving the values a lane still holds.
@@ -933,34 +993,46 @@ int debug_check_tree(const char* fn, const int32_t* lens, const int32_t* cu_q, i
   return ESTP_OK;
 }
 
+// acc: with stored scores, else null
 template <typename T, int DH>
 int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* cu_q, const int64_t* mask,
-                const TreeShape& sh, const TreePlan& p, bool scores, float scale, T* O, float* lse,
+                const TreeShape& sh, const TreePlan& p, float scale, T* O, float* lse, float* acc,
                 const TreeBuffers& t, hipStream_t s) {
   const dim3 grid{unsigned(p.wgs)};
   constexpr int kChunk = sizeof(T) == 2 ? 32 : kTKeys;
   if constexpr (sizeof(T) == 2) {
     auto kernel = p.waves > 1 ? tree_attn_mfma_kernel<DH, tree_waves(DH), false>
-                  : scores    ? tree_attn_mfma_kernel<DH, 1, true>
+                  : acc       ? tree_attn_mfma_kernel<DH, 1, true>
                               : tree_attn_mfma_kernel<DH, 1, false>;
-    kernel<<<grid, dim3(64 * p.waves), tree_lds(DH, p.waves), s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
+    kernel<<<grid, dim3(64 * p.waves), tree_lds(DH, p.waves), s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e,
+                                                                   t.scores, t.pitch, t.m, t.l, t.o);
   } else {
     tree_attn_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
   }
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
-  auto join = [&](auto kernel, int wgs, int threads) {  // wgs: of a token
-    kernel<<<dim3(unsigned(sh.n_q), unsigned(wgs)), dim3(threads), 0, s>>>(t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
-  };
   // segments of an item, about: waves of a row
   const int64_t segs = std::min<int64_t>(int64_t(p.wgs) / (int64_t(sh.B) * sh.Hkv * p.items), sh.max_kv / 128) + 2;
-  if (segs <= 24)
-    join(tree_join_kernel<T, DH, 1, kChunk>, (sh.Hq + 3) / 4, 256);
-  else if (segs <= 64)
-    join(tree_join_kernel<T, DH, 4, kChunk>, sh.Hq, 256);
-  else
-    join(tree_join_kernel<T, DH, 16, kChunk>, sh.Hq, 1024);
-  ESTP_CHECK_LAUNCH("tree_join_kernel");
-  return ESTP_OK;
+  auto join = [&](auto waves) -> int {
+    constexpr int kWaves = decltype(waves)::value, kThreads = tree_join_threads(kWaves);
+    const int per = kWaves == 1 ? (sh.Hq + 3) / 4 : sh.Hq;  // workgroups of a token
+    if constexpr (sizeof(T) == 2) {
+      if (acc) {
+        const unsigned n_join = unsigned(sh.n_q) * unsigned(per);
+        const unsigned n_keys = unsigned((sh.max_kv + 4 * kThreads - 1) / (4 * kThreads)) * unsigned(sh.B * sh.Hkv);
+        tree_finish_kernel<DH, kWaves, kChunk><<<dim3(n_join + n_keys), dim3(kThreads), 0, s>>>(
+            t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse, int(n_join), t.scores, t.pitch, acc);
+        ESTP_CHECK_LAUNCH("tree_finish_kernel");
+        return ESTP_OK;
+      }
+    }
+    tree_join_kernel<T, DH, kWaves, kChunk><<<dim3(unsigned(sh.n_q), unsigned(per)), dim3(kThreads), 0, s>>>(
+        t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
+    ESTP_CHECK_LAUNCH("tree_join_kernel");
+    return ESTP_OK;
+  };
+  if (segs <= 24) return join(std::integral_constant<int, 1>{});
+  if (segs <= 64) return join(std::integral_constant<int, 4>{});
+  return join(std::integral_constant<int, 16>{});
 }
 template <typename T, int DH>
 int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, const int* cu_q, const int64_t* mask,
@@ -1025,7 +1097,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
   const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
-  ESTP_REQUIRE(fits_launch(size_t(n_q) * Hq, 1024) &&
+  ESTP_REQUIRE(fits_launch(2 * size_t(n_q) * Hq, 1024) &&
                    int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
   const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, p.item_shift, p.items);
@@ -1034,19 +1106,13 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, s);
   if (checked != ESTP_OK) return checked;
   float* row_lse = lse ? lse : t.lse;
-  const bool stored = acc && p.stored;
   return tree_dispatch(dtype, dh, [&](auto element, auto size) -> int {
     using T = decltype(element);
     constexpr int DH = decltype(size)::value;
     const int rc = launch_tree<T, DH>(static_cast<const T*>(Q), static_cast<const T*>(K), static_cast<const T*>(V),
-                                      lens, cu_q, tree_mask, sh, p, stored, scale, static_cast<T*>(O), row_lse, t, s);
-    if (rc != ESTP_OK || !acc) return rc;
-    if (stored) {
-      tree_weight_stored_kernel<<<dim3(unsigned((max_kv + 1023) / 1024), unsigned(B * Hkv)), dim3(256), 0, s>>>(
-          t.scores, t.pitch, row_lse, lens, cu_q, sh, acc);
-      ESTP_CHECK_LAUNCH("tree_weight_stored_kernel");
-      return ESTP_OK;
-    }
+                                      lens, cu_q, tree_mask, sh, p, scale, static_cast<T*>(O), row_lse,
+                                      p.stored ? acc : nullptr, t, s);
+    if (rc != ESTP_OK || !acc || p.stored) return rc;
     return launch_weight<T, DH>(static_cast<const T*>(Q), static_cast<const T*>(K), row_lse, lens, cu_q, tree_mask,
                                 nullptr, sh, scale, acc, s);
   });
