@@ -130,12 +130,15 @@ __device__ __forceinline__ uint32_t tree_sees4(uint64_t bits, int rel) {
   return uint32_t(rel >= 0 ? drafted : rel > -4 ? both : ~uint64_t(0)) & 15u;
 }
 // Calls f with the segments of this workgroup's share, a multiple of kRound chunks, in turn; all values are uniform.
+// Neighbouring shares, whose items have keys in common, go to one XCD, and all XCDs (every 8th workgroup of the grid, a
+// multiple of 8) get as many of the shares there are: with shares rounded up there can be far fewer than workgroups.
 template <int kChunk, int kRound = 1, typename F>
-__device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, const int* cu_q, int wg, int wgs,
-                                          F&& f) {
+__device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, const int* cu_q, F&& f) {
   TreeBatch<kChunk> t;
-  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk, kRound>(total, wgs);
-  if (uint64_t(wg) * share >= total) return;
+  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk, kRound>(total, gridDim.x);
+  const uint32_t shares = (total + share - 1) / share, of_xcd = (shares + 7) / 8;
+  const int wg = int((blockIdx.x & 7) * of_xcd + (blockIdx.x >> 3));
+  if ((blockIdx.x >> 3) >= of_xcd || uint32_t(wg) >= shares) return;
   uint32_t at = uint32_t(wg) * share;
   const uint32_t end = min(total, at + share);
   uint32_t off = 0;  // of the batch, then of the sequence
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q,
   constexpr int P = DH + 4, PP = kTKeys + 4, NC = DH / 16;
   __shared__ __attribute__((aligned(16))) float qs[kTRows * P], ks[kTKeys * P], vs[kTKeys * P], ps[kTRows * PP];
   const int G = sh.Hq / sh.Hkv, tid = threadIdx.x, rr = tid >> 4, c = tid & 15;
-  tree_walk<kTKeys>(sh, lens, cu_q, blockIdx.x, gridDim.x, [&](const TreeSegment& q) {
+  tree_walk<kTKeys>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int R = q.T * G, r = q.r0 + rr;
     const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
     const size_t rows = size_t(q.b * sh.Hkv + q.g) * sh.cap;
@@ -349,9 +352,7 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
                                               ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
   };
   auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
-  // neighbouring shares, whose items have keys in common, on one XCD (the grid is a multiple of 8)
-  const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  tree_walk<kC>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
+  tree_walk<kC>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int bg = q.b * sh.Hkv + q.g, r0 = q.r0 + 16 * wave, R = q.T * G, r = r0 + fr;
     const char* Kb = reinterpret_cast<const char*>(K) + size_t(bg) * sh.cap * kRow;
     const char* Vb = reinterpret_cast<const char*>(V) + size_t(bg) * sh.cap * kRow;
@@ -742,8 +743,7 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
   int place = 0;
   const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.G;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  tree_walk<kWKeys, 4>(sh, lens, cu_q, wg, gridDim.x, [&](const TreeSegment& q) {
+  tree_walk<kWKeys, 4>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int R = q.T * G;
     const size_t at = size_t(q.b * sh.Hkv + q.g) * sh.cap;
     auto load_k = [&](bf16x8_t(&kf)[2][kNK], int k) {
