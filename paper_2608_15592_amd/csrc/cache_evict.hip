@@ -441,14 +441,17 @@ extern "C" int estp_cache_evict(void* K, void* V, const float* acc, const int32_
   }
   const int row16 = dh * (dtype == ESTP_F32 ? 4 : 2) / 16;
   const int64_t most = std::min<int64_t>(keep, cap - keep) * row16;  // 16-byte pieces that can move, of K or V
-  // Rows move in the selecting kernel where there are few: a kernel of their own costs its launch, but spreads the
-  // rows of the longest sequences over the chip.  Not in place of lens, which workgroups of the same sequence still
-  // read.
-  const bool here = std::min<int64_t>(keep, cap - keep) <= kMovesHere && most <= 2048 && lens_out != lens;
+  // Rows move in the selecting kernel where there can be few: a kernel of their own costs its launch, but spreads the
+  // rows over the chip (B Hkv = 64, 1152 slots cut to 1024, head size 128: here 10.9 us, apart 13.5; 1280 slots, fp32:
+  // 14.2 against 16.0; B Hkv = 256: 25.6 against 29.7).  Not in place of lens, which workgroups of the same sequence
+  // still read.
+  const bool here = std::min<int64_t>(keep, cap - keep) <= kMovesHere && lens_out != lens;
   EvictArgs g{acc, pos, lens, seen, Hkv, int(cap), keep, recent, sink, acc_out, pos_out, idx, e.moves, e.n_moves,
               here ? static_cast<piece_t*>(K) : nullptr, static_cast<piece_t*>(V), row16, lens_out};
-  auto select = cap <= kEThreads        ? evict_select_kernel<1>
-                : cap <= 4 * kEThreads  ? evict_select_kernel<4>
+  // Rounds in registers: the fewest that hold the capacity, as all are gone through.  64 groups, us: 4096 slots 12.5 in
+  // 4 rounds, 15.8 in 16; 10000 slots 35.4 in 16, 38.4 in 32; 32768 slots 87 in 32, 114 in 64; 65536 slots 210 in 64,
+  // 291 from memory.
+  auto select = cap <= 4 * kEThreads    ? evict_select_kernel<4>
                 : cap <= 16 * kEThreads ? evict_select_kernel<16>
                 : cap <= 32 * kEThreads ? evict_select_kernel<32>
                 : cap <= 64 * kEThreads ? evict_select_kernel<64>

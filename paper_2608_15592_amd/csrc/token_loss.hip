@@ -45,24 +45,41 @@ __device__ __forceinline__ float dot8(const float* a, const float* b, float s) {
   return s;
 }
 
-// loss_i = lse_i - x_i . W[t_i], one wave per token.  A sum of probabilities is at most 1, so a
-// difference below 0 is rounding and is returned as 0.
-template <typename T>
+// loss_i = lse_i - x_i . W[t_i], one wave per token, lse_i given or from `states` partial (maximum, sum) states in base
+// 2, state p of token i at p n_tok + i: then it is written too.  A sum of probabilities is at most 1, so a difference
+// below 0 is rounding and is returned as 0.  (In a launch of their own the states take 7 us after a pass of 226 us over
+// 61 tokens, d 4096, V 128256.)
+template <typename T, bool kStates>
 __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X, const T* __restrict__ W,
                                                         const int32_t* __restrict__ targets, int n_tok, int d, int V,
-                                                        const float* __restrict__ lse, float* __restrict__ loss) {
+                                                        const float* __restrict__ part_m,
+                                                        const float* __restrict__ part_s, int states,
+                                                        float* __restrict__ lse, float* __restrict__ loss) {
   const int tok = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (tok >= n_tok) return;
   const int t = targets[tok];
-  if (t < 0 || t >= V) {
-    if (lane == 0) loss[tok] = 0.f;
-    return;
+  const bool live = t >= 0 && t < V;
+  float z = 0.f;
+  if (live)
+    for (int k = 8 * lane; k < d; k += 512) z = dot8(X + size_t(tok) * d + k, W + size_t(t) * d + k, z);
+  z = wave_sum(z);
+  float l;
+  if constexpr (kStates) {
+    float M = -INFINITY, s = 0.f;
+    for (int p = lane; p < states; p += 64) {
+      const float m = part_m[size_t(p) * n_tok + tok], ps = part_s[size_t(p) * n_tok + tok];
+      const float top = fmaxf(M, m), ref = fmaxf(top, -0x1p127f);
+      s = s * fast_exp2(fmaxf(M - ref, kExp2Floor)) + ps * fast_exp2(fmaxf(m - ref, kExp2Floor));
+      M = top;
+    }
+    const float top = wave_max(M);
+    s = wave_sum(s * fast_exp2(fmaxf(M - fmaxf(top, -0x1p127f), kExp2Floor)));
+    l = kLn2 * (top + fast_log2(s));
+    if (lane == 0) lse[tok] = l;
+  } else {
+    l = lse[tok];
   }
-  float s = 0.f;
-  for (int k = 8 * lane; k < d; k += 512) s = dot8(X + size_t(tok) * d + k, W + size_t(t) * d + k, s);
-  s = wave_sum(s);
-  const float l = lse[tok] - s;
-  if (lane == 0) loss[tok] = l < 0.f ? 0.f : l;
+  if (lane == 0) loss[tok] = !live ? 0.f : l - z < 0.f ? 0.f : l - z;
 }
 
 // The live tokens in ascending order: row[slot] = token, slot[token] = slot or -1, n_live[0].  One
@@ -312,32 +329,6 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
       part_s[o] = s;
     }
   }
-}
-
-// lse of every token from its n partial states: 16 lanes a token take every 16th.
-__global__ __launch_bounds__(256) void loss_lse_merge_kernel(const float* __restrict__ part_m,
-                                                             const float* __restrict__ part_s, int n_tok, int n,
-                                                             float* __restrict__ lse) {
-  __shared__ float sh_m[16][17], sh_s[16][17];
-  const int t = threadIdx.x & 15, q = threadIdx.x >> 4, tok = blockIdx.x * 16 + t;
-  float M = -INFINITY, s = 0.f;
-  if (tok < n_tok)
-#pragma unroll 4
-    for (int p = q; p < n; p += 16) {
-      const float m = part_m[size_t(p) * n_tok + tok], l = part_s[size_t(p) * n_tok + tok];
-      const float top = fmaxf(M, m), ref = fmaxf(top, -0x1p127f);
-      s = s * fast_exp2(fmaxf(M - ref, kExp2Floor)) + l * fast_exp2(fmaxf(m - ref, kExp2Floor));
-      M = top;
-    }
-  sh_m[q][t] = M;
-  sh_s[q][t] = s;
-  __syncthreads();
-  if (q != 0 || tok >= n_tok) return;
-  for (int p = 1; p < 16; ++p) M = fmaxf(M, sh_m[p][t]);
-  const float ref = fmaxf(M, -0x1p127f);
-  s = 0.f;
-  for (int p = 0; p < 16; ++p) s += sh_s[p][t] * fast_exp2(fmaxf(sh_m[p][t] - ref, kExp2Floor));
-  lse[tok] = kLn2 * (M + fast_log2(s));
 }
 
 // G[slot][v] of vocabulary rows v0 .. v0 + Vc (columns past V: 0), pitch Vc.  M side: vocabulary rows.
@@ -722,7 +713,7 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
   LossPlan p;
   p.Vc = int(vc);
-  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : n_tok <= 128 ? 128 : 256;
+  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : n_tok <= 384 ? 128 : 256;
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -835,7 +826,7 @@ struct LsePlan {
 LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
   LsePlan p;
   const bool f32 = dtype == ESTP_F32;
-  p.tile = f32 ? f32_tile_toks(n_tok) : n_tok <= 128 ? 128 : 256;
+  p.tile = f32 ? f32_tile_toks(n_tok) : n_tok <= 384 ? 128 : 256;
   const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows, n_tt = (n_tok + p.tile - 1) / p.tile;
   const int64_t fill = f32 ? std::max<int64_t>(4, (p.tile < kFT ? 1024 : 512) / n_tt) : std::max<int64_t>(1, 256 / n_tt);
   p.slices = int(std::min(n_vt, fill));
@@ -874,6 +865,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
                "%s: n_tok = %lld needs more workgroups than one launch holds", fn, (long long)n_tok);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
+  const dim3 grid(unsigned((n_tok + 3) / 4)), block(256);
   if (own_lse(n_tok, dtype) && !H && !vocab_argmax) {
     // maximum and sum alone.  The entropy kernels' sums keep one order for any number of tokens, which leaves part of
     // the chip idle for few of them (1021 tokens, d 2048: 735 us, here 435), and run on the vector units for fp32.
@@ -898,19 +890,24 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
                                                                      p.slices, pm, ps);
     }
     ESTP_CHECK_LAUNCH("loss_lse_kernel");
-    loss_lse_merge_kernel<<<dim3(unsigned((n_tok + 15) / 16)), dim3(256), 0, s>>>(pm, ps, n, p.states, lse);
-    ESTP_CHECK_LAUNCH("loss_lse_merge_kernel");
+    if (dtype == ESTP_F32)
+      loss_pick_kernel<float, true><<<grid, block, 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W),
+                                                           targets, n, d, V, pm, ps, p.states, lse, loss);
+    else
+      loss_pick_kernel<__bf16, true><<<grid, block, 0, s>>>(static_cast<const __bf16*>(X),
+                                                            static_cast<const __bf16*>(W), targets, n, d, V, pm, ps,
+                                                            p.states, lse, loss);
   } else {
     const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
     if (rc != ESTP_OK) return rc;
+    if (dtype == ESTP_F32)
+      loss_pick_kernel<float, false><<<grid, block, 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W),
+                                                            targets, n, d, V, nullptr, nullptr, 0, lse, loss);
+    else
+      loss_pick_kernel<__bf16, false><<<grid, block, 0, s>>>(static_cast<const __bf16*>(X),
+                                                             static_cast<const __bf16*>(W), targets, n, d, V, nullptr,
+                                                             nullptr, 0, lse, loss);
   }
-  const dim3 grid(unsigned((n_tok + 3) / 4)), block(256);
-  if (dtype == ESTP_F32)
-    loss_pick_kernel<float><<<grid, block, 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), targets,
-                                                   n, d, V, lse, loss);
-  else
-    loss_pick_kernel<__bf16><<<grid, block, 0, s>>>(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W),
-                                                    targets, n, d, V, lse, loss);
   ESTP_CHECK_LAUNCH("loss_pick_kernel");
   return ESTP_OK;
 }
