@@ -82,10 +82,10 @@ __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X,
   if (lane == 0) loss[tok] = !live ? 0.f : l - z < 0.f ? 0.f : l - z;
 }
 
-// The live tokens in ascending order: row[slot] = token, slot[token] = slot or -1, n_live[0].  One
-// workgroup; each thread counts a contiguous run of tokens.
+// The live tokens in ascending order: row[slot] = token, slot[token] = slot or -1, n_live[0] of them, n_live[1] =
+// parts n_live[0] rows of G.  One workgroup; each thread counts a contiguous run of tokens.
 __global__ __launch_bounds__(1024) void loss_list_kernel(const int32_t* __restrict__ targets, int n_tok, int V,
-                                                         int* __restrict__ row, int* __restrict__ slot,
+                                                         int parts, int* __restrict__ row, int* __restrict__ slot,
                                                          int* __restrict__ n_live) {
   __shared__ int wave_total[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -109,19 +109,23 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(const int32_t* __restri
     base += total;
     __syncthreads();
   }
-  if (tid == 0) n_live[0] = base;
+  if (tid == 0) {
+    n_live[0] = base;
+    n_live[1] = parts * base;
+  }
 }
 
-// Rows, targets, normalisers and weights of the live tokens, next to each other.  16-byte pieces of rows.
+// Rows, targets, normalisers and weights of the live tokens, next to each other, and all of them once more where G has
+// two parts.  16-byte pieces of rows.
 __global__ __launch_bounds__(256) void loss_gather_kernel(const uint4* __restrict__ X, const int* __restrict__ row,
                                                           const int* __restrict__ n_live, int row16,
                                                           const int32_t* __restrict__ targets,
                                                           const float* __restrict__ lse, const float* __restrict__ grad,
                                                           uint4* __restrict__ Xc, int32_t* __restrict__ tc,
                                                           float* __restrict__ lc, float* __restrict__ gc) {
-  const int s = blockIdx.x;
-  if (s >= n_live[0]) return;
-  const int tok = row[s];
+  const int s = blockIdx.x, n = n_live[0];
+  if (s >= n_live[1]) return;
+  const int tok = row[s < n ? s : s - n];
   for (int k = threadIdx.x; k < row16; k += 256) Xc[size_t(s) * row16 + k] = X[size_t(tok) * row16 + k];
   if (threadIdx.x == 0) {
     tc[s] = targets[tok];
@@ -152,13 +156,15 @@ template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ slot,
                                                       const int* __restrict__ n_live, int d, int Vc, int tile_toks,
                                                       int wgs, size_t room, T* __restrict__ dX) {
-  const int tok = blockIdx.x, s = slot[tok], n = n_live[0];
+  const int tok = blockIdx.x, s = slot[tok], n = n_live[1], n_tokens = n_live[0];
   const Shares sh = dx_shares(n, d, Vc, tile_toks, wgs, room);
   const size_t each = size_t(n) * d;
   for (int k = 4 * threadIdx.x; k < d; k += 1024) {
     f32x4_t v{0.f, 0.f, 0.f, 0.f};
     if (s >= 0)
-      for (int p = 0; p < sh.n; ++p) v += *reinterpret_cast<const f32x4_t*>(acc + p * each + size_t(s) * d + k);
+      for (int p = 0; p < sh.n; ++p)
+        for (int r = s; r < n; r += n_tokens)  // both parts
+          v += *reinterpret_cast<const f32x4_t*>(acc + p * each + size_t(r) * d + k);
     T* o = dX + size_t(tok) * d + k;
 #pragma unroll
     for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
@@ -173,6 +179,7 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
 // gives row lane % 32 at one of two k; any order of the k will do if both sides keep it: of 8 k, step i takes k = i and
 // 4 + i, so that a lane's four values are one 16-byte read where k is contiguous.
 constexpr int kFT = 128, kFK = 32, kFPart = kFT * kFK * 4;
+constexpr int kFSum = 128;
 
 template <bool kAK, bool kBK, int kTN>
 struct F32Tile {
@@ -248,7 +255,30 @@ struct F32Tile {
     lds_barrier();  // the last tile's stages are read
     stage(k0, 0);
     int buf = 0;
+    Acc part_sum;
+    auto clear = [&]() {
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNJ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) part_sum[i][j][r] = 0.f;
+    };
+    auto add = [&]() {
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNJ; ++j) acc[i][j] += part_sum[i][j];
+    };
+    clear();
+    int left_in_sum = kFSum;
     for (int k = k0; k < k1; k += kFK, buf ^= 1) {
+      if (left_in_sum == 0) {
+        add();
+        clear();
+        left_in_sum = kFSum;
+      }
+      left_in_sum -= kFK;
       arrived<0>();
       lds_barrier();  // every wave's transfers of the stage have landed, and its reads of the other are done
       if (k + kFK < k1) stage(k + kFK, buf ^ 1);
@@ -265,9 +295,10 @@ struct F32Tile {
 #pragma unroll
           for (int i = 0; i < kMI; ++i)
 #pragma unroll
-            for (int j = 0; j < kNJ; ++j) acc[i][j] = mfma32_f32(a[i][q], b[j][q], acc[i][j]);
+            for (int j = 0; j < kNJ; ++j) part_sum[i][j] = mfma32_f32(a[i][q], b[j][q], part_sum[i][j]);
       }
     }
+    add();
   }
 };
 
@@ -341,7 +372,7 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
                                                                const float* __restrict__ gc, float* __restrict__ G) {
   using Run = F32Tile<true, true, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
-  const int n = n_live[0], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
+  const int n = n_live[1], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   if (n0 >= n || m0 >= rows) return;
   const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, rows};
@@ -381,7 +412,7 @@ __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __rest
                                                              float* __restrict__ sums) {
   using Run = F32Tile<false, true, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
-  const int n = n_live[0], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
+  const int n = n_live[1], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
   const Shares sh = dx_shares(n, d, Vc, kTN, wgs, room);
   if (n0 >= n) return;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
@@ -414,7 +445,7 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
                                                              int Vc, float* __restrict__ dW) {
   using Run = F32Tile<false, false, kFT>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
-  const int n = n_live[0], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kFT;
+  const int n = n_live[1], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kFT;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   if (n0 >= rows) return;
   const gemm::Operand A{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, d};
@@ -541,7 +572,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
                                                                 const float* __restrict__ gc, __bf16* __restrict__ G) {
   using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 4 * kNBN>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
-  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]), n_tokens = __builtin_amdgcn_readfirstlane(n_live[0]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
   const int n_m = (rows + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
   const gemm::TileOrder order(n_m, n_n);
@@ -594,6 +625,13 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
 #pragma unroll
               for (int e = 0; e < 8; ++e) p[q][e] = c0 + 32 * q + e < rows ? p[q][e] : 0.f;
           }
+          if (kNBN == 4 && n > n_tokens) {  // two parts: the second is what the rounding of the first leaves
+            const bool second = n0 + sl >= n_tokens;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) p[q][e] -= second ? float(__bf16(p[q][e])) : 0.f;
+          }
 #pragma unroll
           for (int q = 0; q < 4; ++q)
             buf_store16(out, uint32_t(sl) * uint32_t(Vc) * 2u + uint32_t(c0 + 32 * q) * 2u,
@@ -613,7 +651,7 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
                                                               float* __restrict__ out) {
   using Run = gemm::Tiles<false, true, false, kNBN, false, 8 * kNBN < 48 ? 8 * kNBN : 48>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
-  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
   const int n_m = (d + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
   const gemm::TileOrder order(n_m, n_n);
@@ -661,7 +699,7 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
                                                               int Vc, __bf16* __restrict__ dW) {
   using Run = gemm::Tiles<false, false, true, 8, false, 32>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
-  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
   const int n_m = (d + 255) / 256, n_n = (rows + 255) / 256;
   const gemm::TileOrder order(n_m, n_n);
@@ -694,9 +732,13 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
 
 // ------------------------------------------------------------------ plan and workspace
 
+// bf16 rows of G of a token: of few tokens, whose products would leave half of a tile's columns empty, what the
+// rounding of G leaves is a row of its own, so that dX and dW are rounded once.
+inline int g_parts(int64_t n_tok, int dtype) { return dtype == ESTP_BF16 && n_tok <= 64 ? 2 : 1; }
 // How a backward call is cut: Vc vocabulary rows a piece (a multiple of 256), n_split sums of dX in the workspace,
 // products of tile_toks tokens.
 struct LossPlan {
+  int parts;  // of G
   int Vc;
   int n_split;
   int tile_toks;
@@ -712,6 +754,7 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   int64_t vc = int64_t((size_t(256) << 20) / (es * size_t(tok_pad))) / 256 * 256;
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
   LossPlan p;
+  p.parts = g_parts(n_tok, dtype);
   p.Vc = int(vc);
   p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : n_tok <= 384 ? 128 : 256;
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
@@ -734,13 +777,14 @@ inline LossBuffers carve_loss(const LossPlan& p, int64_t n_tok, int d, int dtype
   LossBuffers b;
   b.row = c.take<int>(size_t(n_tok));
   b.slot = c.take<int>(size_t(n_tok));
-  b.n_live = c.take<int>(1);
-  b.tc = c.take<int32_t>(size_t(n_tok));
-  b.lc = c.take<float>(size_t(n_tok));
-  b.gc = c.take<float>(size_t(n_tok));
-  b.Xc = c.take<char>(size_t(n_tok) * d * es);
-  b.G = c.take<char>(size_t(n_tok) * p.Vc * es);
-  b.room = size_t(p.n_split) * size_t(n_tok) * d;
+  b.n_live = c.take<int>(2);
+  const size_t n_rows = size_t(p.parts) * size_t(n_tok);
+  b.tc = c.take<int32_t>(n_rows);
+  b.lc = c.take<float>(n_rows);
+  b.gc = c.take<float>(n_rows);
+  b.Xc = c.take<char>(n_rows * d * es);
+  b.G = c.take<char>(n_rows * p.Vc * es);
+  b.room = size_t(p.n_split) * n_rows * d;
   b.acc = c.take<float>(b.room);
   b.bytes = c.bytes();
   return b;
@@ -754,8 +798,8 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
   constexpr int kWgs = 256;  // of the persistent kernels: one on each compute unit
   const T *Wt = static_cast<const T*>(W), *Xc = reinterpret_cast<const T*>(b.Xc);
   T* G = reinterpret_cast<T*>(b.G);
-  loss_list_kernel<<<dim3(1), dim3(1024), 0, s>>>(targets, n, V, b.row, b.slot, b.n_live);
-  loss_gather_kernel<<<dim3(n), dim3(256), 0, s>>>(static_cast<const uint4*>(X), b.row, b.n_live,
+  loss_list_kernel<<<dim3(1), dim3(1024), 0, s>>>(targets, n, V, p.parts, b.row, b.slot, b.n_live);
+  loss_gather_kernel<<<dim3(unsigned(p.parts * n)), dim3(256), 0, s>>>(static_cast<const uint4*>(X), b.row, b.n_live,
                                                    int(size_t(d) * sizeof(T) / 16), targets, lse, grad,
                                                    reinterpret_cast<uint4*>(b.Xc), b.tc, b.lc, b.gc);
   ESTP_CHECK_LAUNCH("loss_gather_kernel");
