@@ -353,8 +353,10 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  *   dX [n_tok, d]    output (dtype), or NULL; rows of ignored tokens are 0
  *   dW [V, d]        output (dtype), or NULL; 16-byte aligned both, not both NULL
  * Rows of X, lse and grad of ignored tokens are not used (they may hold
- * anything).  G is formed a piece of the vocabulary at a time, in dtype; sums
- * are fp32 and each output element is rounded once.  Bitwise repeatable.
+ * anything).  G is formed a piece of the vocabulary at a time, in dtype (for up
+ * to 64 tokens of ESTP_BF16 in two parts, the second what the rounding of the
+ * first leaves); sums are fp32 and each output element is rounded once.
+ * Bitwise repeatable.
  * n_tok > 4194304, d > 1048576 or n_tok d > 2^36 returns ESTP_ERR_UNSUPPORTED.  The workspace
  * holds one piece of G (about 256 MiB, more past 8192 tokens of fp32 or 16384 of bf16), the live
  * rows of X and fp32 sums of dX.
@@ -400,8 +402,8 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  *   lse [Hq, n_q]           float32 output, natural log, or NULL
  *   acc [B, Hkv, cap]       float32, added to in place, or NULL
  * Query head h reads KV head h / (Hq / Hkv).  dh in {32, 64, 128}.  Weights
- * and sums are fp32; for ESTP_BF16 the weights are rounded to bf16 where the
- * matrix cores multiply them by V.  Bitwise repeatable.
+ * and sums are fp32; for ESTP_BF16 the matrix cores multiply the weights by V
+ * in two bf16 parts, so that O is rounded once.  Bitwise repeatable.
  *
  * estp_tree_importance: the account alone, from the rows' normalisers, with a
  * weight for each row: 1 for the drafted rows that were accepted, 0 for the

@@ -23,6 +23,11 @@ def _rounding(dtype: str) -> float:
     return 2.0 ** -8 if dtype == "bf16" else U
 
 
+def _two_parts(dtype: str) -> float:
+    """Largest relative error of a number as the sum of two of the type (bf16), or as one (fp32)."""
+    return 2.0 ** -16 if dtype == "bf16" else U
+
+
 def token_loss(X, W, targets):
     """(loss [n], lse [n]): lse_i = log sum_v exp(W_v . x_i), loss_i = lse_i - W_t . x_i; 0 where the
     target lies outside [0, V)."""
@@ -53,8 +58,9 @@ def lse_bound(X, W, lse):
 
 
 def token_loss_grads(X, W, targets, grad, dtype: str, lse=None):
-    """(dX, dW, bound_dX, bound_dW) of sum_i grad_i loss_i.  Bounds: G rounded to the type once, its p_iv off by
-    the relative error of its exponent and of exp2 (2 units), fp32 sums of V or n terms, one rounding at the end."""
+    """(dX, dW, bound_dX, bound_dW) of sum_i grad_i loss_i.  Bounds: G rounded to the type once (in two parts of up
+    to 64 tokens), its p_iv off by the relative error of its exponent and of exp2 (2 units), fp32 sums of V or n terms
+    a part, one rounding at the end."""
     dX_in, W64, t = widen(X), widen(W), np.asarray(targets)
     n, d = dX_in.shape
     V = W64.shape[0]
@@ -69,17 +75,18 @@ def token_loss_grads(X, W, targets, grad, dtype: str, lse=None):
     G[np.arange(len(live)), t[live]] -= 1.0
     G *= g[:, None]
     r = _rounding(dtype)
+    rg = _two_parts(dtype) if n <= 64 else r
     eps = np.zeros(len(live))
     if len(live):
         # exponent: the logit, the given lse, and the roundings of (z - lse) log2 e
         eps = 1.01 * (logit_bound(x, W64) + lse_bound(x, W64, l64) + 8 * U * (np.abs(z).max(axis=1) + np.abs(l64)))
         eps += 4 * U
-    dG = np.abs(G) * r * 1.01 + np.abs(g)[:, None] * (P * eps[:, None] + 2 * U * P + 2 * U)* (1.0 + r)
+    dG = np.abs(G) * rg * 1.01 + np.abs(g)[:, None] * (P * eps[:, None] + 2 * U * P + 2 * U)* (1.0 + r)
     dX[live] = G @ W64
     aW, ax = np.abs(W64), np.abs(x)
-    bX[live] = (dG + gamma(V + 8) * np.abs(G)) @ aW * (1.0 + r) + r * np.abs(dX[live])
+    bX[live] = (dG + gamma(2 * V + 8) * np.abs(G)) @ aW * (1.0 + r) + r * np.abs(dX[live])
     dW = G.T @ x
-    bW = (dG + gamma(len(live) + 8) * np.abs(G)).T @ ax * (1.0 + r) + r * np.abs(dW)
+    bW = (dG + gamma(2 * len(live) + 8) * np.abs(G)).T @ ax * (1.0 + r) + r * np.abs(dW)
     return dX, dW, bX, bW
 
 
@@ -122,9 +129,9 @@ def tree_attention(Q, K, V, lens, cu_q, tree_mask=None, scale=None, dtype: str =
                 out["lse"][h, i] = lse
                 out["lse_bound"][h, i] = dl
                 rel = 1.01 * (ds + dl + 4 * U * (np.abs(s) + abs(lse) + 1.0))
-                # weights rounded to the type, fp32 sums, one rounding of the result
-                out["O_bound"][i, h] = ((p * (rel + r * 1.01 + gamma(len(keys) + 64))) @ np.abs(v)) * (1 + r) \
-                    + r * np.abs(out["O"][i, h])
+                # weights in two parts, fp32 sums, one rounding of the result
+                dp = p * (rel + 1.01 * _two_parts(dtype) + gamma(2 * len(keys) + 64))
+                out["O_bound"][i, h] = (dp @ np.abs(v)) * (1 + r) + r * np.abs(out["O"][i, h])
                 if w != 0.0:
                     out["got"][b, h // G, keys] += w * p
                     out["got_bound"][b, h // G, keys] += abs(w) * p * (rel + gamma(2 * T * G + 8))
