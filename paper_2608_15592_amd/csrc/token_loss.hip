@@ -46,7 +46,7 @@ __device__ __forceinline__ float dot8(const float* a, const float* b, float s) {
 }
 
 // loss_i = lse_i - x_i . W[t_i], one wave per token, lse_i given or from `states` partial (maximum, sum) states in base
-// 2, state p of token i at p n_tok + i: then it is written too.  A sum of probabilities is at most 1, so a difference
+// 2, state p of token i at i states + p: then it is written too.  A sum of probabilities is at most 1, so a difference
 // below 0 is rounding and is returned as 0.  (In a launch of their own the states take 7 us after a pass of 226 us over
 // 61 tokens, d 4096, V 128256.)
 template <typename T, bool kStates>
@@ -65,11 +65,27 @@ __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X,
   z = wave_sum(z);
   float l;
   if constexpr (kStates) {
+    constexpr int kAhead = 8;  // states of a lane on their way together
     float M = -INFINITY, s = 0.f;
-    for (int p = lane; p < states; p += 64) {
-      const float m = part_m[size_t(p) * n_tok + tok], ps = part_s[size_t(p) * n_tok + tok];
-      const float top = fmaxf(M, m), ref = fmaxf(top, -0x1p127f);
-      s = s * fast_exp2(fmaxf(M - ref, kExp2Floor)) + ps * fast_exp2(fmaxf(m - ref, kExp2Floor));
+    for (int p0 = lane; p0 < states; p0 += 64 * kAhead) {
+      float m[kAhead], ps[kAhead], top = M;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const size_t at = size_t(tok) * states + min(p0 + 64 * u, states - 1);
+        m[u] = part_m[at];
+        ps[u] = part_s[at];
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const bool in = p0 + 64 * u < states;
+        m[u] = in ? m[u] : -INFINITY;
+        ps[u] = in ? ps[u] : 0.f;
+        top = fmaxf(top, m[u]);
+      }
+      const float ref = fmaxf(top, -0x1p127f);
+      s *= fast_exp2(fmaxf(M - ref, kExp2Floor));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) s = fmaf(ps[u], fast_exp2(fmaxf(m[u] - ref, kExp2Floor)), s);
       M = top;
     }
     const float top = wave_max(M);
@@ -151,24 +167,36 @@ __device__ __forceinline__ Shares dx_shares(int n_live, int d, int Vc, int tile_
   return {(Vc + rows - 1) / rows, rows};
 }
 
-// dX of every token from the partial sums of its slot, rounded once; 0 for ignored tokens.
+// dX of every token from the partial sums of its slot (and of the second part's), rounded once; 0 for ignored tokens.
+// Four columns a thread.  It reads what the products wrote: memory bounds it (684 live of 1021 tokens, d 2048, 10
+// shares: FIGDX).
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ slot,
                                                       const int* __restrict__ n_live, int d, int Vc, int tile_toks,
                                                       int wgs, size_t room, T* __restrict__ dX) {
-  const int tok = blockIdx.x, s = slot[tok], n = n_live[1], n_tokens = n_live[0];
+  const int tok = blockIdx.x, k = 4 * (blockIdx.y * 256 + threadIdx.x), s = slot[tok];
+  const int n = n_live[1], n_tokens = n_live[0];
+  if (k >= d) return;
   const Shares sh = dx_shares(n, d, Vc, tile_toks, wgs, room);
   const size_t each = size_t(n) * d;
-  for (int k = 4 * threadIdx.x; k < d; k += 1024) {
-    f32x4_t v{0.f, 0.f, 0.f, 0.f};
-    if (s >= 0)
-      for (int p = 0; p < sh.n; ++p)
-        for (int r = s; r < n; r += n_tokens)  // both parts
-          v += *reinterpret_cast<const f32x4_t*>(acc + p * each + size_t(r) * d + k);
-    T* o = dX + size_t(tok) * d + k;
+  f32x4_t v{0.f, 0.f, 0.f, 0.f};
+  if (s >= 0)
+    for (int r = s; r < n; r += n_tokens) {
+      const float* from = acc + size_t(r) * d + k;
+      constexpr int kAhead = 8;
+      for (int p = 0; p < sh.n; p += kAhead) {
+        f32x4_t x[kAhead];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
-  }
+        for (int u = 0; u < kAhead; ++u)
+          x[u] = *reinterpret_cast<const f32x4_t*>(from + size_t(min(p + u, sh.n - 1)) * each);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+          if (p + u < sh.n) v += x[u];
+      }
+    }
+  T* o = dX + size_t(tok) * d + k;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
 }
 
 // ------------------------------------------------------------------ matrix-core products (fp32)
@@ -304,7 +332,7 @@ struct F32Tile {
 
 // Running (maximum, sum) in base 2 of every token's logits over a slice of the vocabulary tiles: slice s of n_slices
 // takes tiles s, s + n_slices, ...; each wave's rows of a tile have a state of their own.  Partial states
-// [kWM n_slices, n_tok].
+// [n_tok, kWM n_slices].
 template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __restrict__ X, const float* __restrict__ W,
                                                               int n_tok, int d, int V, int n_slices,
@@ -355,7 +383,7 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
     const float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor)) + lo * fast_exp2(fmaxf(mo - ref, kExp2Floor));
     const int tok = at.n + 32 * j;
     if ((threadIdx.x & 32) == 0 && tok < n_tok) {
-      const size_t o = size_t(Run::kWM * slice + at.wm) * n_tok + tok;
+      const size_t o = size_t(tok) * (Run::kWM * n_slices) + Run::kWM * slice + at.wm;
       part_m[o] = M;
       part_s[o] = s;
     }
@@ -483,7 +511,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
 // first tile's maximum is the reference; later tiles add to the sum with one FMA, exponential and addition a logit,
-// and move the reference only where a sum would pass 2^64.  Partial states [2 n_slices, n_tok], a wave's 128 rows each.
+// and move the reference only where a sum would pass 2^64.  Partial states [n_tok, 2 n_slices], a wave's 128 rows each.
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __restrict__ X,
                                                                const __bf16* __restrict__ W, int n_tok, int d, int V,
@@ -554,7 +582,7 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
     }
     const int tok = Run::kBN * tt + 16 * kNBN * wn + 16 * j + (lane & 15);
     if (lane < 16 && tok < n_tok) {
-      const size_t o = size_t(2 * slice + wm) * n_tok + tok;
+      const size_t o = size_t(tok) * (2 * n_slices) + 2 * slice + wm;
       part_m[o] = m[j];
       part_s[o] = l[j];
     }
@@ -846,7 +874,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
     }
   }
   if (dX) {
-    loss_dx_kernel<T><<<dim3(n), block, 0, s>>>(b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room,
+    loss_dx_kernel<T><<<dim3(n, unsigned((d + 1023) / 1024)), block, 0, s>>>(b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room,
                                                 static_cast<T*>(dX));
     ESTP_CHECK_LAUNCH("loss_dx_kernel");
   }
