@@ -10,7 +10,9 @@
 //
 // Waves, ring, barriers and the spacing of reads and transfers between the MFMAs are entropy_gemm_kernel's: 4
 // waves of 128 x kBN / 2, one per SIMD, five 32 KB slots that hold A and B parts of the stages in turn, one barrier a
-// stage, transfers issued two and a half stages ahead and across tile boundaries.
+// stage, transfers issued two and a half stages ahead and across tile boundaries.  The matrix cores bound it: 256 x 256
+// tiles at a depth of 4096 reach 1.25 to 1.3 PFLOP/s with what follows a tile (library products of these shapes 1.15 to
+// 1.48); at a depth of 704, 11 stages, 0.8.
 #pragma once
 
 #include <type_traits>
@@ -57,7 +59,11 @@ struct TileOrder {
   Divisor per, tail;  // tiles of a group; columns of the last, smaller group
   uint32_t n_group;  // tiles of one whole group
   __device__ __forceinline__ TileOrder(int n_m, int n_n_)
-      : n_n(n_n_), full(n_n_ & ~7), per(uint32_t(8 * n_m)), tail(uint32_t(max(1, n_n_ & 7))), n_group(uint32_t(8 * n_m)) {}
+      : n_n(n_n_),
+        full(n_n_ & ~7),
+        per(uint32_t(8 * n_m)),
+        tail(uint32_t(max(1, n_n_ & 7))),
+        n_group(uint32_t(8 * n_m)) {}
   __device__ __forceinline__ TileAt operator()(int id) const {
     const uint32_t g = per.div(uint32_t(id)), rem = uint32_t(id) - g * n_group;
     const bool whole = int(8 * g) < full;
@@ -81,12 +87,11 @@ __device__ __forceinline__ int fresh_lane() {
 // First tile id of a workgroup; it goes on in steps of the grid (a multiple of 8).
 __device__ __forceinline__ int first_tile(int wg, int grid) { return (wg & 7) * (grid >> 3) + (wg >> 3); }
 
-// kAK, kBK: k contiguous (else strided).  kPairA: block i of a wave holds rows 32 (i / 2) + 4 (i % 2) + 8 (m / 4) + m % 4,
-// so that the results of a block pair in a lane are 8 consecutive m (a strided A then has 2-way bank conflicts, which
-// its reads have room for).
-// kNBN: 16-row blocks of a wave, N side.  kOdd: the depth may be an odd multiple of 32 (both k contiguous).  kStores:
-// vector-memory operations that done() leaves in flight at least (it ends with so many stores, always): the stage after
-// it need not wait for them.
+// kAK, kBK: k contiguous (else strided).  kPairA: block i of a wave holds rows 32 (i / 2) + 4 (i % 2) + 8 (m / 4) + m
+// % 4, so that the results of a block pair in a lane are 8 consecutive m (a strided A then has 2-way bank conflicts,
+// which its reads have room for). kNBN: 16-row blocks of a wave, N side.  kOdd: the depth may be an odd multiple of
+// 32 (both k contiguous).  kStores: vector-memory operations that done() leaves in flight at least (it ends with so
+// many stores, always): the stage after it need not wait for them.
 template <bool kAK, bool kBK, bool kPairA, int kNBN, bool kOdd, int kStores>
 struct Tiles {
   static constexpr int kBN = 32 * kNBN;

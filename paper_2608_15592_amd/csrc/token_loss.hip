@@ -4,19 +4,23 @@
 //   z_i = W x_i,  lse_i = log sum_v exp z_i[v],  loss_i = lse_i - z_i[t_i]
 //   G_iv = g_i (exp(z_i[v] - lse_i) - [v = t_i]),  dX = G W,  dW = G^T X
 //
-// Forward: lse comes from the entropy kernels (entropy.hip), whose running
-// maximum and sum it is; loss_pick_kernel forms z_i[t_i] from one row of each
-// operand.  A token whose target lies outside [0, V) is ignored: loss 0, no
-// gradient, and its row of X (padding may hold anything) is never multiplied.
+// Forward: lse comes from a pass over the vocabulary that keeps a maximum and a sum per token: of kernels of this file
+// (bf16 up to 2048 tokens, fp32), or the entropy kernels' (entropy.hip) for more tokens, and where H or the most
+// probable token are asked for too.  loss_pick_kernel forms z_i[t_i] from one row of each operand.  A token whose
+// target lies outside [0, V) is ignored: loss 0, no gradient, and its row of X (padding may hold anything) is never
+// multiplied into a gradient.
 //
-// Backward: the live tokens' rows are first gathered next to each other
-// (loss_list_kernel, loss_gather_kernel), so that ignored tokens cost nothing
-// and cannot put a NaN into dW.  Then, for one piece of the vocabulary after
-// the other, three products: the piece's logits again, turned into G in their
-// epilogue; dX += G W_piece in fp32; dW_piece = G^T X, written once.  G is held
-// in the inputs' type (bf16: one rounding of each entry, 2^-8 relative, the
-// type in which the matrix cores take it; the sums over it are fp32).  Last,
-// loss_dx_kernel rounds dX once and puts it into the tokens' places.
+// Backward: the live tokens' rows are first gathered next to each other (loss_list_kernel, loss_gather_kernel), so that
+// ignored tokens cost nothing and cannot put a NaN into dW.  Then, for one piece of the vocabulary after the other,
+// three products: the piece's logits again, turned into G in their epilogue; dX += G W_piece in fp32; dW_piece = G^T X,
+// written once.  G is held in the inputs' type (bf16: one rounding of each entry, 2^-8 relative, the type in which the
+// matrix cores take it; of up to 64 tokens in two parts; the sums over it are fp32).  Last, loss_dx_kernel rounds dX
+// once and puts it into the tokens' places.
+//
+// Few tokens are bounded by one pass over W for each product, many by the matrix cores: 2 n V d operations for the
+// logits of the forward, and three times as many for the backward, which forms them again instead of keeping n V of
+// them.  4096 tokens, d 4096, V 128256: 13.0 ms, 1.33 PFLOP/s over all of it (a library product of these logits alone
+// runs at 1.48).
 #include <algorithm>
 
 #include "estp_common.h"
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X,
 }
 
 // The live tokens in ascending order: row[slot] = token, slot[token] = slot or -1, n_live[0] of them, n_live[1] =
-// parts n_live[0] rows of G.  One workgroup; each thread counts a contiguous run of tokens.
+// parts n_live[0] rows of G.  One workgroup takes 1024 tokens a round: latency, 5 us for up to 4096.
 __global__ __launch_bounds__(1024) void loss_list_kernel(const int32_t* __restrict__ targets, int n_tok, int V,
                                                          int parts, int* __restrict__ row, int* __restrict__ slot,
                                                          int* __restrict__ n_live) {
@@ -132,7 +136,7 @@ __global__ __launch_bounds__(1024) void loss_list_kernel(const int32_t* __restri
 }
 
 // Rows, targets, normalisers and weights of the live tokens, next to each other, and all of them once more where G has
-// two parts.  16-byte pieces of rows.
+// two parts.  16-byte pieces of rows.  A copy (4096 tokens of 8 KB: 13 us, 5.1 TB/s).
 __global__ __launch_bounds__(256) void loss_gather_kernel(const uint4* __restrict__ X, const int* __restrict__ row,
                                                           const int* __restrict__ n_live, int row16,
                                                           const int32_t* __restrict__ targets,
@@ -169,7 +173,7 @@ __device__ __forceinline__ Shares dx_shares(int n_live, int d, int Vc, int tile_
 
 // dX of every token from the partial sums of its slot (and of the second part's), rounded once; 0 for ignored tokens.
 // Four columns a thread.  It reads what the products wrote: memory bounds it (684 live of 1021 tokens, d 2048, 10
-// shares: FIGDX).
+// shares: 20.8 us, 2.8 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ slot,
                                                       const int* __restrict__ n_live, int d, int Vc, int tile_toks,
@@ -202,10 +206,17 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
 // ------------------------------------------------------------------ matrix-core products (fp32)
 //
 // C[m][n] = sum_k A(m, k) B(n, k) over 128 x kTN tiles on v_mfma_f32_32x32x2_f32 (without packed instructions the
-// vector units reach half its rate), 4 waves of 64 x 64, or of 32 x kTN for the 64 and 32 columns of few tokens.  Operands lie in memory with k contiguous or strided and
-// reach LDS as they lie, 32 k a stage, two stages of at most 32 KB, so two or more workgroups share a compute unit.  A lane of a step
-// gives row lane % 32 at one of two k; any order of the k will do if both sides keep it: of 8 k, step i takes k = i and
-// 4 + i, so that a lane's four values are one 16-byte read where k is contiguous.
+// vector units reach half its rate), 4 waves of 64 x 64, or of 32 x kTN for the 64 and 32 columns of few tokens.
+// Operands lie in memory with k contiguous or strided and reach LDS as they lie, 32 k a stage, two stages of at most 32
+// KB, so two or more workgroups share a compute unit.  A lane of a step gives row lane % 32 at one of two k; any order
+// of the k will do if both sides keep it: of 8 k, step i takes k = i and 4 + i, so that a lane's four values are one
+// 16-byte read where k is contiguous.  kFSum terms at a time are summed before they enter the total, which keeps the
+// rounding of long sums small (3 tokens, d 2048: dW off by 2e-7, by 2e-6 with one chain of sums) for 64 additions in
+// 256 products.
+//
+// 400 tokens, d 2048, V 128256 (a product of 210 GFLOP, 153 TFLOP/s at most, a fifth of it on columns that no token
+// has): logits 2.15 ms, dX 2.14, dW 1.80 (117 TFLOP/s).  16 tokens, which one pass over the 1.05 GB of W or dW bounds:
+// logits 244 us (4.3 TB/s), dX 222, dW 354.
 constexpr int kFT = 128, kFK = 32, kFPart = kFT * kFK * 4;
 constexpr int kFSum = 128;
 
@@ -512,6 +523,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
 // first tile's maximum is the reference; later tiles add to the sum with one FMA, exponential and addition a logit,
 // and move the reference only where a sum would pass 2^64.  Partial states [n_tok, 2 n_slices], a wave's 128 rows each.
+// 61 tokens, d 4096, V 128256: 217 us, 4.8 TB/s of W; 1021 tokens, d 2048: 450 us, 1.19 PFLOP/s.
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __restrict__ X,
                                                                const __bf16* __restrict__ W, int n_tok, int d, int V,
@@ -590,7 +602,9 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
 }
 
 // G of a piece: products of W's rows (M side) and the live tokens (N side), turned into G as they leave the matrix
-// cores.  A lane holds 8 consecutive vocabulary rows of a token: one 16-byte store.
+// cores.  A lane holds 8 consecutive vocabulary rows of a token: one 16-byte store.  Bound by the matrix cores, with
+// the exponentials between two tiles (4096 tokens, d 4096, 32768 vocabulary rows, 1.1 TFLOP: 830 us, 1.32 PFLOP/s;
+// 684 live tokens, d 2048, all of 128256: 353 us, 1.02 PFLOP/s, a ninth of it on columns that no token has).
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __restrict__ Xc,
                                                                 const __bf16* __restrict__ W,
@@ -670,7 +684,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
 }
 
 // out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W (transposed reads), N
-// side: slots.
+// side: slots.  The matrix cores bound it (the sizes above: 870 us, 1.26 PFLOP/s, and 388 us, 0.93 PFLOP/s).
 template <int kNBN>
 __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __restrict__ G,
                                                               const __bf16* __restrict__ W,
@@ -720,7 +734,8 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
 }
 
 // dW of a piece: G^T Xc.  M side: columns k of Xc, N side: vocabulary rows; both transposed reads, the tokens are
-// the depth.
+// the depth.  The matrix cores bound it where there are many (the sizes above: 870 us, 1.26 PFLOP/s); of 684, which are
+// 11 stages a tile, its first stage and its stores are a good part (443 us, 0.81 PFLOP/s).
 __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __restrict__ G,
                                                               const __bf16* __restrict__ Xc,
                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
@@ -747,7 +762,7 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const uint32_t row = uint32_t(128 * wn + 16 * j + fr) * uint32_t(d);
-          const int c0 = m0 + 128 * wm + 8 * fq;  // 8 columns of every 32: d is a multiple of 32, all 8 are live or none
+          const int c0 = m0 + 128 * wm + 8 * fq;  // (of every 32: d is a multiple of 32, all 8 are live or none)
 #pragma unroll
           for (int i = 0; i < 8; i += 2)
             buf_store16(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
@@ -760,8 +775,10 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
 
 // ------------------------------------------------------------------ plan and workspace
 
-// bf16 rows of G of a token: of few tokens, whose products would leave half of a tile's columns empty, what the
-// rounding of G leaves is a row of its own, so that dX and dW are rounded once.
+// Rows of G of a token: of few tokens of bf16, whose products would leave half of a tile's columns empty, what the
+// rounding of G leaves is a row of its own, so that dX and dW are rounded once: their error is that of one rounding,
+// and 1.4 times that (of one token up to 1.7 times) otherwise.  d 2048, V 128256: 30 tokens 428 us with one part, 477
+// with two; 64 tokens 453 and 521.
 inline int g_parts(int64_t n_tok, int dtype) { return dtype == ESTP_BF16 && n_tok <= 64 ? 2 : 1; }
 // How a backward call is cut: Vc vocabulary rows a piece (a multiple of 256), n_split sums of dX in the workspace,
 // products of tile_toks tokens.
@@ -772,7 +789,13 @@ struct LossPlan {
   int tile_toks;
 };
 
-// Tokens of a fp32 tile.
+// Tokens of a bf16 tile: 256 read LDS less often, 128 leave fewer columns empty.  d 2048, V 128256, forward and
+// backward in us, 128 against 256: 64 tokens 135 and 451, 163 and 497; 200 tokens 148 and 569, 154 and 582; 384
+// tokens 203 and 725, 234 and 771; 512 tokens 260 and 889, 242 and 838; 1021 tokens 490 and 1581, 455 and 1438.
+inline int bf16_tile_toks(int64_t n_tok) { return n_tok <= 384 ? 128 : 256; }
+// Tokens of a fp32 tile: the narrowest that takes them all, up to 128.  d 2048, V 128256, forward and backward in us:
+// 16 tokens 253 and 771 with 32, 379 and 941 with 64, 518 and 1322 with 128; 50 tokens 360 and 1072 with 64, 504 and
+// 1434 with 128; 100 tokens 508 and 1676 with 128, 738 and 1780 with 64.
 inline int f32_tile_toks(int64_t n_tok) { return n_tok <= 32 ? 32 : n_tok <= 64 ? 64 : kFT; }
 
 inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
@@ -781,10 +804,12 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   const int64_t v_pad = (int64_t(V) + 255) / 256 * 256;
   int64_t vc = int64_t((size_t(256) << 20) / (es * size_t(tok_pad))) / 256 * 256;
   vc = std::min(std::max<int64_t>(vc, 8192), v_pad);
+  // G of 256 MiB or 8192 rows.  4096 tokens: d 4096 the same for 128 to 512 MiB and 1 % slower for 64; d 2048 5.40 ms,
+  // 5.33 for 64 and 5.39 for 512.
   LossPlan p;
   p.parts = g_parts(n_tok, dtype);
   p.Vc = int(vc);
-  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : n_tok <= 384 ? 128 : 256;
+  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : bf16_tile_toks(n_tok);
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -835,8 +860,9 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
   for (int64_t v0 = 0; v0 < V; v0 += p.Vc) {
     if constexpr (sizeof(T) == 2) {
       const dim3 grid(kWgs);
-      auto grad_kernel = p.tile_toks == 128 ? (d % 64 ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
-                                            : (d % 64 ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
+      const bool odd = d % 64 != 0;
+      auto grad_kernel = p.tile_toks == 128 ? (odd ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
+                                            : (odd ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
       grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
       ESTP_CHECK_LAUNCH("loss_grad_mfma_kernel");
       if (dX) {
@@ -874,8 +900,8 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
     }
   }
   if (dX) {
-    loss_dx_kernel<T><<<dim3(n, unsigned((d + 1023) / 1024)), block, 0, s>>>(b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room,
-                                                static_cast<T*>(dX));
+    loss_dx_kernel<T><<<dim3(n, unsigned((d + 1023) / 1024)), block, 0, s>>>(
+        b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room, static_cast<T*>(dX));
     ESTP_CHECK_LAUNCH("loss_dx_kernel");
   }
   return ESTP_OK;
@@ -894,18 +920,22 @@ namespace {
 struct LsePlan {
   int tile, slices, states;
 };
-// bf16: a workgroup on every compute unit.  fp32: two workgroups for every compute unit (four of the smaller ones).
+// bf16: a workgroup on every compute unit, tiles as in the backward.  fp32: two workgroups for every compute unit (four
+// of the smaller ones).
 LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
   LsePlan p;
   const bool f32 = dtype == ESTP_F32;
-  p.tile = f32 ? f32_tile_toks(n_tok) : n_tok <= 384 ? 128 : 256;
+  p.tile = f32 ? f32_tile_toks(n_tok) : bf16_tile_toks(n_tok);
   const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows, n_tt = (n_tok + p.tile - 1) / p.tile;
-  const int64_t fill = f32 ? std::max<int64_t>(4, (p.tile < kFT ? 1024 : 512) / n_tt) : std::max<int64_t>(1, 256 / n_tt);
-  p.slices = int(std::min(n_vt, fill));
+  const int64_t fill = !f32 ? 256 : p.tile < kFT ? 1024 : 512;
+  p.slices = int(std::min(n_vt, std::max<int64_t>(f32 ? 4 : 1, fill / n_tt)));
   p.states = p.slices * (f32 && p.tile < kFT ? 4 : 2);
   return p;
 }
-// bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.
+// bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.  d 2048, V 128256, here against
+// there: 128 tokens 137 and 154 us, 1021 tokens 451 and 626, 2048 tokens 870 and 1220, 2500 tokens 1077 and 991, 4096
+// tokens 1735 and 1544.  (Its sums keep one order for any number of tokens, and it forms H and the mode too.)  fp32:
+// the entropy kernel runs on the vector units.
 bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 2048; }
 
 }  // namespace
@@ -939,8 +969,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
   const int n = int(n_tok);
   const dim3 grid(unsigned((n_tok + 3) / 4)), block(256);
   if (own_lse(n_tok, dtype) && !H && !vocab_argmax) {
-    // maximum and sum alone.  The entropy kernels' sums keep one order for any number of tokens, which leaves part of
-    // the chip idle for few of them (1021 tokens, d 2048: 735 us, here 435), and run on the vector units for fp32.
+    // maximum and sum alone
     const LsePlan p = plan_lse(n_tok, V, dtype);
     Carver c(workspace);
     float* pm = c.take<float>(size_t(p.states) * size_t(n_tok));
@@ -1013,6 +1042,6 @@ extern "C" int estp_token_loss_backward(const void* X, const void* W, const int3
                "%s: workspace must be non-null and 256-byte aligned", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
-  return dtype == ESTP_F32 ? launch_loss_backward<float>(X, W, targets, lse, grad, n, d, V, dtype, dX, dW, workspace, s)
-                           : launch_loss_backward<__bf16>(X, W, targets, lse, grad, n, d, V, dtype, dX, dW, workspace, s);
+  auto launch = dtype == ESTP_F32 ? launch_loss_backward<float> : launch_loss_backward<__bf16>;
+  return launch(X, W, targets, lse, grad, n, d, V, dtype, dX, dW, workspace, s);
 }

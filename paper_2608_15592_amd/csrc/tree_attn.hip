@@ -13,12 +13,15 @@
 //
 // A row that sees nothing has lse -inf and O 0, and adds nothing.
 //
-// An item is one (sequence, KV head) and up to 16, 32 rows of it; its keys come in chunks.  All chunks of all items
-// form one line, cut into equal shares, one for each workgroup of a grid that fills the chip once: lengths may differ
-// as they like, and no workgroup is empty.  A share's piece of an item is a segment, worked off in one pass with the
-// running maximum and sum of the softmax (base 2); tree_join_kernel joins an item's segments.  The account takes the
-// rows' normalisers, so it comes last: from scores that the first kernel kept where the rows are few, else from
-// scores formed again.  No atomics: bitwise reproducible.
+// An item is one (sequence, KV head) and up to 16, 32 or 64 rows of it; its keys come in chunks.  All chunks of all
+// items form one line, cut into equal shares, one for each workgroup of a grid that fills the chip once: lengths may
+// differ as they like, and no workgroup is empty.  A share's piece of an item is a segment, worked off in one pass with
+// the running maximum and sum of the softmax (base 2); tree_join joins an item's segments.  The account takes the rows'
+// normalisers, so it comes last: from scores that the first kernel kept where the rows are few (in the launch of the
+// join), else from scores formed again.  No atomics: bitwise reproducible.
+//
+// The cache is read once; that bounds calls of few rows (a copy moves 4.9 TB/s on this card).  Calls of many rows spend
+// their time on the exponentials and what goes with them, each score twice.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -31,8 +34,6 @@ namespace estp {
 namespace detail {
 
 constexpr int kMaxTree = 64;  // drafted tokens of a sequence: the bits of a mask
-constexpr int kTRows = 16;    // rows of a workgroup
-constexpr int kTKeys = 64;    // keys of a tile
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
 struct TreeShape {
@@ -178,165 +179,74 @@ __device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, 
   }
 }
 
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&v)[4]);
-template <>
-__device__ __forceinline__ void load4<float>(const float* p, float (&v)[4]) {
-  const f32x4_t x = *reinterpret_cast<const f32x4_t*>(p);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = x[j];
-}
-template <>
-__device__ __forceinline__ void load4<uint16_t>(const uint16_t* p, float (&v)[4]) {
-  const uint2 x = *reinterpret_cast<const uint2*>(p);
-  v[0] = __uint_as_float(x.x << 16);
-  v[1] = __uint_as_float(x.x & 0xffff0000u);
-  v[2] = __uint_as_float(x.y << 16);
-  v[3] = __uint_as_float(x.y & 0xffff0000u);
-}
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(uint16_t* p, float v) {
   *p = __builtin_bit_cast(uint16_t, __bf16(v));  // round to nearest even
 }
 
-// n rows of DH elements (contiguous) into LDS rows of pitch P, as floats; rows at or past `live` become 0.
-template <typename T, int DH, int P>
-__device__ __forceinline__ void stage_rows(const T* src, int n, int live, float* lds) {
-  for (int i = threadIdx.x; i < n * (DH / 4); i += 256) {
-    const int r = i / (DH / 4), c = 4 * (i % (DH / 4));
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < live) load4<T>(src + size_t(r) * DH + c, v);
-    *reinterpret_cast<f32x4_t*>(lds + r * P + c) = f32x4_t{v[0], v[1], v[2], v[3]};
+// What differs between the types.  16 bytes of a row, a fragment, are 8 bf16 or 4 fp32 values; a 16-key block's scores
+// of 16 rows take one v_mfma_f32_16x16x32_bf16 for every 64 bytes of a row, or four v_mfma_f32_16x16x4_f32 (its k:
+// value j of the four lanes' fragments, the same in both operands).  Chunks of keys are equally large in bytes.
+template <typename T>
+struct TreeMath;
+template <>
+struct TreeMath<uint16_t> {
+  typedef bf16x8_t Frag;
+  static constexpr int kC = 32;  // keys of a chunk
+  __device__ static __forceinline__ f32x4_t scores(const Frag& k, const Frag& q, const f32x4_t& s) {
+    return mfma_bf16(k, q, s);
   }
-}
-// the 16 query rows from r0 of a KV head's T G rows
-template <typename T, int DH, int P>
-__device__ __forceinline__ void stage_queries(const T* Q, const TreeShape& sh, const TreeSegment& q, int R,
-                                              float* lds) {
-  const int G = sh.Hq / sh.Hkv;
-  for (int i = threadIdx.x; i < kTRows * (DH / 4); i += 256) {
-    const int r = q.r0 + i / (DH / 4), c = 4 * (i % (DH / 4));
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < R) load4<T>(Q + (size_t(q.q0 + r / G) * sh.Hq + q.g * G + r % G) * DH + c, v);
-    *reinterpret_cast<f32x4_t*>(lds + (i / (DH / 4)) * P + c) = f32x4_t{v[0], v[1], v[2], v[3]};
+};
+template <>
+struct TreeMath<float> {
+  typedef f32x4_t Frag;
+  static constexpr int kC = 16;
+  __device__ static __forceinline__ f32x4_t scores(const Frag& k, const Frag& q, f32x4_t s) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], q[j], s, 0, 0, 0);
+    return s;
   }
-}
-// s[j] = q row rr . key 16 j + c
-template <int DH, int P>
-__device__ __forceinline__ void scores4(const float* qs, const float* ks, int rr, int c, float (&s)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) s[j] = 0.f;
-  for (int d = 0; d < DH; d += 4) {
-    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(qs + rr * P + d);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4_t k = *reinterpret_cast<const f32x4_t*>(ks + (16 * j + c) * P + d);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[j] = fmaf(a[e], k[e], s[j]);
-    }
-  }
-}
+};
 
-// Vector-unit kernel (fp32).  Thread (rr, c) = (tid / 16, tid % 16) forms row rr's scores of keys c, 16 + c, 32 + c,
-// 48 + c of a tile and its output columns c DH / 16 ...
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void tree_attn_kernel(const T* __restrict__ Q, const T* __restrict__ K,
-                                                        const T* __restrict__ V, const int* __restrict__ lens,
-                                                        const int* __restrict__ cu_q,
-                                                        const int64_t* __restrict__ mask, TreeShape sh, float c2,
-                                                        float* __restrict__ part_m, float* __restrict__ part_l,
-                                                        float* __restrict__ part_o) {
-  constexpr int P = DH + 4, PP = kTKeys + 4, NC = DH / 16;
-  __shared__ __attribute__((aligned(16))) float qs[kTRows * P], ks[kTKeys * P], vs[kTKeys * P], ps[kTRows * PP];
-  const int G = sh.Hq / sh.Hkv, tid = threadIdx.x, rr = tid >> 4, c = tid & 15;
-  tree_walk<kTKeys>(sh, lens, cu_q, [&](const TreeSegment& q) {
-    const int R = q.T * G, r = q.r0 + rr;
-    const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
-    const size_t rows = size_t(q.b * sh.Hkv + q.g) * sh.cap;
-    const T *Kb = K + rows * DH, *Vb = V + rows * DH;
-    __syncthreads();  // the last segment's rows are read
-    stage_queries<T, DH, P>(Q, sh, q, R, qs);
-    float m = -INFINITY, l = 0.f, o[NC];
-#pragma unroll
-    for (int e = 0; e < NC; ++e) o[e] = 0.f;
-    for (int k = q.k0; k < q.k1; k += kTKeys) {
-      __syncthreads();
-      stage_rows<T, DH, P>(Kb + size_t(k) * DH, kTKeys, q.k1 - k, ks);
-      stage_rows<T, DH, P>(Vb + size_t(k) * DH, kTKeys, q.k1 - k, vs);
-      __syncthreads();
-      float s[4], mx = m;
-      scores4<DH, P>(qs, ks, rr, c, s);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int key = k + 16 * j + c;
-        s[j] = key < q.k1 && tree_sees(bits, key - q.len) ? s[j] * c2 : -INFINITY;
-        mx = fmaxf(mx, s[j]);
-      }
-#pragma unroll
-      for (int x = 1; x < 16; x <<= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-      const float ref = mx == -INFINITY ? 0.f : mx;  // nothing seen yet: all weights are 0
-      const float f = fast_exp2(m - ref);
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = fast_exp2(s[j] - ref);
-        ps[rr * PP + 16 * j + c] = p;
-        sum += p;
-      }
-#pragma unroll
-      for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x, 64);
-      l = l * f + sum;
-      m = mx;
-#pragma unroll
-      for (int e = 0; e < NC; ++e) o[e] *= f;
-      __syncthreads();
-      const int n = min(kTKeys, q.k1 - k), rel = k - q.len;
-      for (int j = 0; j < n; ++j) {
-        // a drafted token the row does not see adds nothing, whatever its values are
-        if (rel + j >= 0 && !tree_sees(bits, rel + j)) continue;
-        const float p = ps[rr * PP + j];
-#pragma unroll
-        for (int e = 0; e < NC; ++e) o[e] = fmaf(p, vs[j * P + c * NC + e], o[e]);
-      }
-    }
-    if (r >= R) return;
-    const size_t row = size_t(q.slot) * kTRows + rr;
-    if (c == 0) {
-      part_m[row] = m;
-      part_l[row] = l;
-    }
-#pragma unroll
-    for (int e = 0; e < NC; ++e) part_o[row * DH + c * NC + e] = o[e];
-  });
-}
-
-// Matrix-core kernel (bf16): items of 16 rows a wave, chunks of 32 keys.
+// Items of 16 rows a wave, chunks of 32 keys (fp32: 16).
 //
-// S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of the chunk's two 16-key blocks, keys
-// 4 fq .. 4 fq + 3 each (fq = lane / 16).  These 8 weights are at once the lane's part of the second product's
-// operand, O^T = V^T P^T over 32 keys, if V's part holds the same keys for one of its columns: two transposing reads.
-// So scores never leave the registers.  The reference of a row's exponentials follows its maximum only when a score
-// passes it by 2^16 (sums and weights stay far from overflow): most chunks neither exchange maxima between lanes nor
-// rescale O.
+// S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of each of the chunk's 16-key blocks, keys
+// 4 fq .. 4 fq + 3 (fq = lane / 16).  These weights are at once the lane's part of the second product's operand,
+// O^T = V^T P^T, if V's part holds the same keys for one of its columns: two transposing reads for 32 keys of bf16; for
+// fp32, where a product takes one key of each fq, 16-byte reads along a row of V, the lane's columns then being
+// neighbours.  So scores never leave the registers.  The reference of a row's exponentials follows its maximum only
+// when a score passes it by 2^16 (sums and weights stay far from overflow): most chunks neither exchange maxima
+// between lanes nor rescale O.
 //
 // The chunks' K and V parts go straight from memory into a ring of five parts.  Up to 16 rows: one wave that uses the
 // ring alone, without barriers, and counts its own transfers, two and a half chunks ahead; memory bounds it.  More
 // rows: kW waves of 16 rows each share the ring, so that the keys are fetched once for all of them, and there are more
 // waves on a compute unit to hide one another's waits.  16-byte pieces are swizzled so that the 16 rows of a K read
 // and the 8 of a transposing V read lie in distinct banks.
-template <int DH, int kW, bool kScores>
-__global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
-    const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
+//
+// Measured: one row of 32 heads on 8 KV heads of 128, one sequence of 32767: 26.2 us, 5.1 TB/s; 32 sequences of 500 to
+// 4000: 52 us, 4.4 TB/s.  31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 26.7 us, of which
+// 5 us pass before the first chunk and after the last; its exponentials alone are 4 us of the chip's.  fp32, the first
+// of these: 46 us, 5.8 TB/s; 31 drafted tokens at 8 sequences of 4500: 95 us, bf16 27.
+template <typename T, int DH, int kW, bool kScores>
+__global__ __launch_bounds__(64 * kW, 2) void tree_attn_kernel(
+    const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
     const int* __restrict__ lens, const int* __restrict__ cu_q, const int64_t* __restrict__ mask, TreeShape sh,
     float c2, float* __restrict__ scores, int pitch, float* __restrict__ part_m, float* __restrict__ part_l,
     float* __restrict__ part_o) {
-  constexpr int kC = 32, kRow = DH * 2, kPart = kC * kRow, kSlots = 5, kL = kPart / 1024;
-  constexpr int kPieces = DH / 8, kNK = DH / 32, kND = DH / 16;
-  constexpr int kWindow = 16 / kPieces;  // rows in 256 bytes
-  constexpr int kLw = kL / kW;           // transfers of a wave for a part
+  using Math = TreeMath<T>;
+  using Frag = typename Math::Frag;
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kC = Math::kC, kB = kC / 16, kRow = DH * int(sizeof(T)), kPart = kC * kRow, kSlots = 5;
+  constexpr int kL = kPart / 1024, kLw = kL / kW;  // transfers for a part; of a wave
+  constexpr int kPieces = kRow / 16, kNF = kPieces / 4, kND = DH / 16;
+  constexpr int kWindow = kPieces >= 16 ? 1 : 16 / kPieces;  // rows in 256 bytes
+  constexpr int kVW = kND < 4 ? kND : 4;                     // fp32: neighbouring columns of a lane
+  typedef float cols_t __attribute__((ext_vector_type(kVW)));
   static_assert(kL % kW == 0, "waves share a part's transfers equally");
-  // The ring, and 16 rows of Q for each of several waves: tree_lds(DH, kW) bytes.  (Dynamic: of a size it knows, the
-  // compiler takes one wave a SIMD for granted at a head size of 128, and copies sums between two register files.)
+  // The ring, and 16 rows of Q for each of several waves: tree_lds(DH, kW, sizeof(T)) bytes.  (Dynamic: of a size it
+  // knows, the compiler takes one wave a SIMD for granted at a head size of 128, and copies sums between two register
+  // files.)
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4, G = sh.G;
   const int wave = kW == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -345,11 +255,14 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
   for (int i = 0; i < kLw; ++i) {
     const int piece = 64 * (kW * i + wave) + lane, row = piece / kPieces, c = piece % kPieces;
     off_k[i] = uint32_t(row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16);
-    off_v[i] = uint32_t(row * kRow + (c ^ (2 * (row / kWindow & (kPieces / 2 - 1)))) * 16);
+    off_v[i] = uint32_t(row * kRow + (kBf16 ? c ^ (2 * (row / kWindow & (kPieces / 2 - 1))) : c) * 16);
   }
-  auto read_k = [&](const char* part, int row, int c) {  // dims 32 c + 8 fq .. + 7 of a row of a K part
-    return *reinterpret_cast<const bf16x8_t*>(part + row * kRow +
-                                              ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
+  auto read_k = [&](const char* part, int row, int c) {  // fragment 4 c + fq of a row of a K part
+    return *reinterpret_cast<const Frag*>(part + row * kRow + ((4 * c + fq) ^ (row / kWindow & (kPieces - 1))) * 16);
+  };
+  // column of O in o[d][z]
+  auto column = [&](int d, int z) {
+    return kBf16 ? 16 * d + 4 * fq + z : 16 * kVW * (d / kVW) + kVW * (4 * fq + z) + d % kVW;
   };
   auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
   tree_walk<kC>(sh, lens, cu_q, [&](const TreeSegment& q) {
@@ -372,7 +285,7 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
     const u32x4_t rq = rsrc_words(reinterpret_cast<const char*>(Q) + size_t(q.q0) * sh.Hq * kRow,
                                   uint32_t(q.T) * uint32_t(sh.Hq) * uint32_t(kRow));
 #pragma unroll
-    for (int i = 0; i < kL / 2; ++i) {
+    for (int i = 0; i < kRow / 64; ++i) {
       const int at = (64 * i + lane) / kPieces, row = r0 + at;
       const uint32_t piece = uint32_t((64 * i + lane) % kPieces ^ (at / kWindow & (kPieces - 1))) * 16u;
       const uint32_t tok = uint32_t(sh.token(row)), head = uint32_t(q.g * G + row) - tok * uint32_t(G);
@@ -385,9 +298,9 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
     issue(Vb, off_v);
     pf_key += kC;
     arrived<4 * kLw>();
-    bf16x8_t qf[kNK];
+    Frag qf[kNF];
 #pragma unroll
-    for (int c = 0; c < kNK; ++c) qf[c] = read_k(own, fr, c);
+    for (int c = 0; c < kNF; ++c) qf[c] = read_k(own, fr, c);
     lds_read_done();
     if (kW == 1) issue(Kb, off_k);
     float m = -INFINITY, l = 0.f;
@@ -407,27 +320,27 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
       // ---- scores
       part_landed();
       if (kW > 1) issue(Kb, off_k);
-      bf16x8_t kf[2][kNK];
+      Frag kf[kB][kNF];
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+      for (int a = 0; a < kB; ++a)
 #pragma unroll
-        for (int c = 0; c < kNK; ++c) kf[a][c] = read_k(lds + slot * kPart, 16 * a + fr, c);
+        for (int c = 0; c < kNF; ++c) kf[a][c] = read_k(lds + slot * kPart, 16 * a + fr, c);
       lds_read_done();
       if (kW == 1) {
         issue(Vb, off_v);
         pf_key += kC;
       }
       slot = slot + 1 == kSlots ? 0 : slot + 1;
-      f32x4_t s[2];
+      f32x4_t s[kB];
 #pragma unroll
-      for (int a = 0; a < 2; ++a) {
+      for (int a = 0; a < kB; ++a) {
         s[a] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < kNK; ++c) s[a] = mfma_bf16(kf[a][c], qf[c], s[a]);
+        for (int c = 0; c < kNF; ++c) s[a] = Math::scores(kf[a][c], qf[c], s[a]);
       }
       if (edge) {
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < kB; ++a) {
           const uint32_t sees = tree_sees4(bits, k + 16 * a + 4 * fq - q.len);
 #pragma unroll
           for (int z = 0; z < 4; ++z) s[a][z] = (sees >> z) & 1 ? s[a][z] : -INFINITY;
@@ -435,12 +348,12 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
+      for (int e = 0; e < 4 * kB; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
       mx *= c2;
       if (kScores && r < R) {
         float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
-        *reinterpret_cast<f32x4_t*>(w) = s[0] * c2;
-        *reinterpret_cast<f32x4_t*>(w + 16) = s[1] * c2;
+#pragma unroll
+        for (int a = 0; a < kB; ++a) *reinterpret_cast<f32x4_t*>(w + 16 * a) = s[a] * c2;
       }
       if (__any(mx > m + 16.f)) {
         mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
@@ -453,17 +366,19 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
         for (int d = 0; d < kND; ++d) o[d] *= f;
       }
       const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: all weights are 0
-      // The matrix cores take the weights as two bf16 numbers, the second what the rounding of the first leaves: O is
-      // rounded once, where it is written (with the first alone its error is 1.4 times that, at the same speed where
-      // memory bounds it).
-      float p[8];
+      // For bf16 the matrix cores take the weights as two numbers, the second what the rounding of the first leaves:
+      // O is rounded once, where it is written (with the first alone its error is 1.4 times that, at the same speed
+      // where memory bounds it).
+      float p[4 * kB];
       bf16x8_t pf, pf_lo;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4 * kB; ++e) {
         p[e] = fast_exp2(fmaf(s[e / 4][e % 4], c2, -ref));
         l += p[e];
-        pf[e] = __bf16(p[e]);
-        pf_lo[e] = __bf16(p[e] - float(pf[e]));
+        if constexpr (kBf16) {
+          pf[e] = __bf16(p[e]);
+          pf_lo[e] = __bf16(p[e] - float(pf[e]));
+        }
       }
       // ---- output
       part_landed();
@@ -472,48 +387,84 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
         pf_key += kC;
       }
       const char* vs = lds + slot * kPart;
-      bf16x8_t vf[kND];
+      bf16x8_t vf[kBf16 ? kND : 1];
+      cols_t vc[kBf16 ? 1 : 4][kBf16 ? 1 : kND / kVW];  // fp32: of keys 4 fq + i
+      if constexpr (kBf16) {
 #pragma unroll
-      for (int d = 0; d < kND; ++d) {
-        const int row = 4 * fq + (fr >> 2);  // and 16 further on: the swizzle is the same
-        const char* w = vs + row * kRow + (d ^ unit_of(row)) * 32 + (fr & 3) * 8;
-        vf[d] = join_tr(read_tr(w), read_tr(w + 16 * kRow));
+        for (int d = 0; d < kND; ++d) {
+          const int row = 4 * fq + (fr >> 2);  // and 16 further on: the swizzle is the same
+          const char* w = vs + row * kRow + (d ^ unit_of(row)) * 32 + (fr & 3) * 8;
+          vf[d] = join_tr(read_tr(w), read_tr(w + 16 * kRow));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int u = 0; u < kND / kVW; ++u)
+            vc[i][u] = *reinterpret_cast<const cols_t*>(vs + (4 * fq + i) * kRow + (16 * u + fr) * (4 * kVW));
       }
       lds_read_done();
       if (edge) {
         // A drafted token that a row does not see has weight 0 there, which a non-finite value must not meet: such
         // values leave the product and are added, one by one, to the rows that see them.
-        u16x2_t top{0, 0};  // the largest exponent
-#pragma unroll
-        for (int d = 0; d < kND; ++d) {
-          const u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, v[e] & 0x7f807f80u));
-        }
-        if (__any(top[0] == 0x7f80 || top[1] == 0x7f80)) {
+        bool bad = false;
+        if constexpr (kBf16) {
+          u16x2_t top{0, 0};  // the largest exponent
 #pragma unroll
           for (int d = 0; d < kND; ++d) {
-            s16x8_t v = __builtin_bit_cast(s16x8_t, vf[d]);
+            const u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (v[e] & 0x7f80) == 0x7f80 ? short(0) : v[e];
-            vf[d] = __builtin_bit_cast(bf16x8_t, v);
+            for (int e = 0; e < 4; ++e)
+              top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, v[e] & 0x7f807f80u));
+          }
+          bad = top[0] == 0x7f80 || top[1] == 0x7f80;
+        } else {
+          uint32_t top = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int d = 0; d < kND; ++d)
+              top = max(top, __float_as_uint(vc[i][d / kVW][d % kVW]) & 0x7f800000u);
+          bad = top == 0x7f800000u;
+        }
+        if (__any(bad)) {
+          if constexpr (kBf16) {
+#pragma unroll
+            for (int d = 0; d < kND; ++d) {
+              s16x8_t v = __builtin_bit_cast(s16x8_t, vf[d]);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = (v[e] & 0x7f80) == 0x7f80 ? short(0) : v[e];
+              vf[d] = __builtin_bit_cast(bf16x8_t, v);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int d = 0; d < kND; ++d) {
+                const float v = vc[i][d / kVW][d % kVW];
+                vc[i][d / kVW][d % kVW] = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.f : v;
+              }
           }
           for (int j = 0; j < kC && k + j < q.keys; ++j) {
             const int from = fr + 16 * (j % 16 / 4), e = j / 16 * 4 + j % 4;
             float mine = 0.f;
 #pragma unroll
-            for (int z = 0; z < 8; ++z) mine = z == e ? p[z] : mine;
+            for (int z = 0; z < 4 * kB; ++z) mine = z == e ? p[z] : mine;
             const float w = __shfl(mine, from, 64);
             if (!tree_sees(bits, k + j - q.len)) continue;
 #pragma unroll
             for (int d = 0; d < kND; ++d)
 #pragma unroll
               for (int z = 0; z < 4; ++z) {
-                const int at_d = 16 * d + 4 * fq + z;
-                const uint16_t v = *reinterpret_cast<const uint16_t*>(
-                    vs + j * kRow + ((at_d / 16) ^ unit_of(j)) * 32 + (at_d % 16) * 2);
-                if ((v & 0x7f80) == 0x7f80) o[d][z] += w * bf16_to_f32(v);
+                const int at = column(d, z);
+                if constexpr (kBf16) {
+                  const uint16_t v = *reinterpret_cast<const uint16_t*>(
+                      vs + j * kRow + ((at / 16) ^ unit_of(j)) * 32 + (at % 16) * 2);
+                  if ((v & 0x7f80) == 0x7f80) o[d][z] += w * bf16_to_f32(v);
+                } else {
+                  const float v = *reinterpret_cast<const float*>(vs + j * kRow + at * 4);
+                  if ((__float_as_uint(v) & 0x7f800000u) == 0x7f800000u) o[d][z] += w * v;
+                }
               }
           }
           lds_read_done();
@@ -521,10 +472,18 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
       }
       if (kW == 1) issue(Kb, off_k);
       slot = slot + 1 == kSlots ? 0 : slot + 1;
+      if constexpr (kBf16) {
 #pragma unroll
-      for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf, o[d]);
+        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf, o[d]);
 #pragma unroll
-      for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf_lo, o[d]);
+        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf_lo, o[d]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int d = 0; d < kND; ++d)
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vc[i][d / kVW][d % kVW], p[i], o[d], 0, 0, 0);
+      }
     }
     arrived<0>();  // no transfer into LDS outlives the segment
     l += __shfl_xor(l, 16, 64);
@@ -535,8 +494,20 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_mfma_kernel(
       part_m[row] = m;
       part_l[row] = l;
     }
+    if constexpr (kBf16) {
 #pragma unroll
-    for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + 16 * d + 4 * fq) = o[d];
+      for (int d = 0; d < kND; ++d) *reinterpret_cast<f32x4_t*>(part_o + row * DH + column(d, 0)) = o[d];
+    } else {
+#pragma unroll
+      for (int u = 0; u < kND / kVW; ++u)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          cols_t v;
+#pragma unroll
+          for (int e = 0; e < kVW; ++e) v[e] = o[kVW * u + e][z];
+          *reinterpret_cast<cols_t*>(part_o + row * DH + column(kVW * u, z)) = v;
+        }
+    }
   });
 }
 
@@ -574,7 +545,8 @@ __device__ __forceinline__ float tree_fold(const float* part_m, const float* par
 
 // Joins the partial results of the segments of row (token tok, head h).  kWaves waves share a row and take every
 // kWaves-th segment; a lane fetches the state of one segment, 64 at a time, and DH / 64 (at least one) columns of
-// each.  Rows past the last sequence's are left as they are.
+// each.  Rows past the last sequence's are left as they are.  Latency bounds it, a chain of four loads: 6 us for a few
+// rows, 8.0 us for 31 tokens of 32 heads in 8 sequences (34 MB of partial results).
 template <typename T, int DH, int kWaves, int kChunk>
 __device__ __forceinline__ void tree_join(const float* __restrict__ part_m, const float* __restrict__ part_l,
                                           const float* __restrict__ part_o, const int* __restrict__ lens,
@@ -668,23 +640,25 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_join_kernel(
 
 // The join, and beside it acc[b][g][key] += sum over the rows of exp(s - lse) from the scores (base 2) that the
 // attention kernel has stored.  Workgroups n_join and on take 4 keys a thread of a (sequence, KV head), whose few rows'
-// normalisers they form for themselves: so neither waits for the other's launch.
-template <int DH, int kWaves, int kChunk>
+// normalisers they form for themselves: so neither waits for the other's launch (6.7 us for one token at 32767, 7.3 us
+// for 32 sequences of 500 to 4000; in two launches 11.5 and 13 us).
+template <typename T, int DH, int kWaves, int kChunk>
 __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
     const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
-    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, uint16_t* __restrict__ O,
+    const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
     float* __restrict__ lse, int n_join, const float* __restrict__ scores, int pitch, float* __restrict__ acc) {
   constexpr int kThreads = tree_join_threads(kWaves);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (int(blockIdx.x) < n_join) {
     const uint32_t per = kWaves == 1 ? uint32_t(sh.Hq + 3) / 4 : uint32_t(sh.Hq);  // workgroups of a token
     const uint32_t tok = blockIdx.x / per, y = blockIdx.x - tok * per;
-    tree_join<uint16_t, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, int(tok),
+    tree_join<T, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, int(tok),
                                             kWaves == 1 ? int(4 * y) + wave : int(y), O, lse);
     return;
   }
   __shared__ float lse2[16];
-  const uint32_t id = blockIdx.x - n_join, bg = id % uint32_t(sh.B * sh.Hkv), k0 = id / uint32_t(sh.B * sh.Hkv) * (4 * kThreads);
+  const uint32_t id = blockIdx.x - n_join, groups = uint32_t(sh.B * sh.Hkv);
+  const uint32_t bg = id % groups, k0 = id / groups * (4 * kThreads);
   const int b = int(bg / uint32_t(sh.Hkv)), g = int(bg) - b * sh.Hkv;
   TreeBatch<kChunk> t;
   const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
@@ -720,23 +694,27 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
     if (k + e < keys) a[e] += sum[e];
 }
 
-// acc[b][g][key] += sum over the rows of w exp(s - lse) with the scores formed again on the matrix cores (bf16).  An
-// item's rows wait in LDS, 128 at a time, with
-// their weights, normalisers and masks; a workgroup's share of 32-key tiles goes to its four waves in turn, a tile's
-// K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's columns are rows: their
-// sums join at the end of a tile, each exchange halving the values a lane still holds.
+// acc[b][g][key] += sum over the rows of w exp(s - lse) with the scores formed again.  An item's rows wait in LDS,
+// 128 at a time, with their weights, normalisers and masks; a workgroup's share of 32-key tiles goes to its four
+// waves in turn, a tile's K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's
+// columns are rows: their sums join at the end of a tile, each exchange halving the values a lane still holds.  Every
+// score costs an exponential and two FMAs, which bound it (16 rows and 32 keys: 300 cycles of a SIMD) after some 6 us
+// until the first tile is done: 31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 18.2 us;
+// 23 tokens, heads of 128, 16 of 700 to 6000, a part of the rows accepted: 21.6 us, 4.3 TB/s.  fp32, the first at 8
+// of 4500: 64 us.
 constexpr int kWRows = 128;  // rows in LDS
 constexpr int kWKeys = 32;   // keys of a tile
-template <int DH>
-__global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kernel(const uint16_t* __restrict__ Q,
-                                                                  const uint16_t* __restrict__ K,
-                                                                  const float* __restrict__ lse,
-                                                                  const int* __restrict__ lens,
-                                                                  const int* __restrict__ cu_q,
-                                                                  const int64_t* __restrict__ mask,
-                                                                  const float* __restrict__ row_weight, TreeShape sh,
-                                                                  float c2, float* __restrict__ acc) {
-  constexpr int kNK = DH / 32, kRow = DH * 2, kPieces = DH / 8, kWindow = 16 / kPieces;
+// Workgroups of a compute unit: what its registers hold.
+constexpr int tree_weight_wgs(int row_bytes) { return row_bytes >= 512 ? 2 : row_bytes >= 256 ? 3 : 4; }
+template <typename T, int DH>
+__global__ __launch_bounds__(256, tree_weight_wgs(DH * int(sizeof(T)))) void tree_weight_kernel(
+    const T* __restrict__ Q, const T* __restrict__ K, const float* __restrict__ lse, const int* __restrict__ lens,
+    const int* __restrict__ cu_q, const int64_t* __restrict__ mask, const float* __restrict__ row_weight, TreeShape sh,
+    float c2, float* __restrict__ acc) {
+  using Math = TreeMath<T>;
+  using Frag = typename Math::Frag;
+  constexpr int kRow = DH * int(sizeof(T)), kPieces = kRow / 16, kNF = kPieces / 4;
+  constexpr int kWindow = kPieces >= 16 ? 1 : 16 / kPieces;
   struct RowInfo {  // of weight 0: not used
     float w, l2;
     uint64_t bits;
@@ -752,179 +730,140 @@ __global__ __launch_bounds__(256, DH == 128 ? 3 : 4) void tree_weight_mfma_kerne
   tree_walk<kWKeys, 4>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int R = q.T * G;
     const size_t at = size_t(q.b * sh.Hkv + q.g) * sh.cap;
-    auto load_k = [&](bf16x8_t(&kf)[2][kNK], int k) {
+    auto load_k = [&](Frag(&kf)[2][kNF], int k) {
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
         const size_t key = at + size_t(min(k + 16 * a + fr, q.keys - 1));
 #pragma unroll
-        for (int c = 0; c < kNK; ++c)
-          kf[a][c] = *reinterpret_cast<const bf16x8_t*>(K + key * DH + 32 * c + 8 * fq);
+        for (int c = 0; c < kNF; ++c)
+          kf[a][c] = reinterpret_cast<const Frag*>(K + key * DH)[4 * c + fq];
       }
     };
     for (int r0 = 0; r0 < R; r0 += kWRows) {
-    bf16x8_t kf[2][kNK], kn[2][kNK];
-    const int first = q.k0 + kWKeys * wave;
-    if (first < q.k1) load_k(kf, first);
-    int n_rows = min(kWRows, R - r0);
-    __syncthreads();  // the last rows are read
-    // the rows that count, next to each other (of a tree often few: the accepted ones); the rest of the last 16 are the
-    // last of them again, with weight 0 and an infinite normaliser
-    if (tid < kWRows) {
-      RowInfo x{0.f, 0.f, 0, 0};
-      if (tid < n_rows) {
-        const int r = r0 + tid, t = sh.token(r), tok = q.q0 + t;
-        const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r - t * G) * sh.n_q + tok];
-        const uint64_t bits = tree_bits(mask, q, t);
-        if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, bits, tok * sh.Hq + q.g * G + r - t * G};
+      Frag kf[2][kNF], kn[2][kNF];
+      const int first = q.k0 + kWKeys * wave;
+      if (first < q.k1) load_k(kf, first);
+      int n_rows = min(kWRows, R - r0);
+      __syncthreads();  // the last rows are read
+      // the rows that count, next to each other (of a tree often few: the accepted ones); the rest of the last 16 are
+      // the last of them again, with weight 0 and an infinite normaliser
+      if (tid < kWRows) {
+        RowInfo x{0.f, 0.f, 0, 0};
+        if (tid < n_rows) {
+          const int r = r0 + tid, t = sh.token(r), tok = q.q0 + t;
+          const float w = row_weight ? row_weight[tok] : 1.f, l = lse[size_t(q.g * G + r - t * G) * sh.n_q + tok];
+          const uint64_t bits = tree_bits(mask, q, t);
+          if (w != 0.f && l != -INFINITY) x = RowInfo{w, l * kLog2e, bits, tok * sh.Hq + q.g * G + r - t * G};
+        }
+        const uint64_t counts = __ballot(x.w != 0.f);
+        if (lane == 0) live[wave] = int(__popcll(counts));
+        info[tid] = RowInfo{0.f, INFINITY, 0, 0};
+        mine = x;
+        place = int(__popcll(counts & ((uint64_t(1) << lane) - 1)));
       }
-      const uint64_t counts = __ballot(x.w != 0.f);
-      if (lane == 0) live[wave] = int(__popcll(counts));
-      info[tid] = RowInfo{0.f, INFINITY, 0, 0};
-      mine = x;
-      place = int(__popcll(counts & ((uint64_t(1) << lane) - 1)));
-    }
-    __syncthreads();
-    if (tid < kWRows && mine.w != 0.f) info[place + (wave == 1 ? live[0] : 0)] = mine;
-    n_rows = live[0] + live[1];
-    __syncthreads();
-    for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
-      const int row = i / kPieces, c = i % kPieces, r = info[min(row, n_rows - 1)].r;
-      *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) =
-          reinterpret_cast<const uint4*>(Q)[size_t(r) * kPieces + c];
-    }
-    __syncthreads();
-    for (int k = first; k < q.k1; k += 4 * kWKeys) {
-      const bool edge = k + kWKeys > q.len;
-      const int key = k + 16 * ((fr >> 2) & 1) + 4 * fq + (fr & 3);  // whose sum ends up in this lane (fr < 8)
-      const bool writes = fr < 8 && key < q.keys && n_rows > 0;
-      float was = 0.f;
-      if (writes) was = acc[at + key];
-      if (k + 4 * kWKeys < q.k1) load_k(kn, k + 4 * kWKeys);
-      float sum[8];
+      __syncthreads();
+      if (tid < kWRows && mine.w != 0.f) info[place + (wave == 1 ? live[0] : 0)] = mine;
+      n_rows = live[0] + live[1];
+      __syncthreads();
+      for (int i = tid; i < (n_rows + 15) / 16 * 16 * kPieces; i += 256) {
+        const int row = i / kPieces, c = i % kPieces, r = info[min(row, n_rows - 1)].r;
+        *reinterpret_cast<uint4*>(qs + row * kRow + (c ^ (row / kWindow & (kPieces - 1))) * 16) =
+            reinterpret_cast<const uint4*>(Q)[size_t(r) * kPieces + c];
+      }
+      __syncthreads();
+      for (int k = first; k < q.k1; k += 4 * kWKeys) {
+        const bool edge = k + kWKeys > q.len;
+        const int key = k + 16 * ((fr >> 2) & 1) + 4 * fq + (fr & 3);  // whose sum ends up in this lane (fr < 8)
+        const bool writes = fr < 8 && key < q.keys && n_rows > 0;
+        float was = 0.f;
+        if (writes) was = acc[at + key];
+        if (k + 4 * kWKeys < q.k1) load_k(kn, k + 4 * kWKeys);
+        float sum[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-      auto add_rows = [&](auto at_edge) {
-        for (int r = 0; r < n_rows; r += 16) {
-          const float w = info[r + fr].w, l2 = info[r + fr].l2;
-          const uint64_t bits = decltype(at_edge)::value ? info[r + fr].bits : 0;
-          bf16x8_t qf[kNK];
+        for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+        auto add_rows = [&](auto at_edge) {
+          for (int r = 0; r < n_rows; r += 16) {
+            const float w = info[r + fr].w, l2 = info[r + fr].l2;
+            const uint64_t bits = decltype(at_edge)::value ? info[r + fr].bits : 0;
+            Frag qf[kNF];
 #pragma unroll
-          for (int c = 0; c < kNK; ++c)
-            qf[c] = *reinterpret_cast<const bf16x8_t*>(qs + (r + fr) * kRow +
-                                                       ((4 * c + fq) ^ ((r + fr) / kWindow & (kPieces - 1))) * 16);
+            for (int c = 0; c < kNF; ++c)
+              qf[c] = *reinterpret_cast<const Frag*>(qs + (r + fr) * kRow +
+                                                         ((4 * c + fq) ^ ((r + fr) / kWindow & (kPieces - 1))) * 16);
 #pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const uint32_t sees = decltype(at_edge)::value ? tree_sees4(bits, k + 16 * a + 4 * fq - q.len) : 15u;
-            f32x4_t s{0.f, 0.f, 0.f, 0.f};
+            for (int a = 0; a < 2; ++a) {
+              const uint32_t sees = decltype(at_edge)::value ? tree_sees4(bits, k + 16 * a + 4 * fq - q.len) : 15u;
+              f32x4_t s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < kNK; ++c) s = mfma_bf16(kf[a][c], qf[c], s);
+              for (int c = 0; c < kNF; ++c) s = Math::scores(kf[a][c], qf[c], s);
 #pragma unroll
-            for (int z = 0; z < 4; ++z) {
-              // (cached keys are seen by every row; one behind the last adds 0 exp2(score - infinity), NaN only where
-              // the last row's is)
-              const float p = fast_exp2(fmaf(s[z], c2, -l2));
-              if constexpr (decltype(at_edge)::value)
-                sum[4 * a + z] = (sees >> z) & 1 ? fmaf(w, p, sum[4 * a + z]) : sum[4 * a + z];
-              else
-                sum[4 * a + z] = fmaf(w, p, sum[4 * a + z]);
+              for (int z = 0; z < 4; ++z) {
+                // (cached keys are seen by every row; one behind the last adds 0 exp2(score - infinity), NaN only where
+                // the last row's is)
+                const float p = fast_exp2(fmaf(s[z], c2, -l2));
+                if constexpr (decltype(at_edge)::value)
+                  sum[4 * a + z] = (sees >> z) & 1 ? fmaf(w, p, sum[4 * a + z]) : sum[4 * a + z];
+                else
+                  sum[4 * a + z] = fmaf(w, p, sum[4 * a + z]);
+              }
             }
           }
-        }
-      };
-      if (edge)
-        add_rows(std::true_type{});
-      else
-        add_rows(std::false_type{});
+        };
+        if (edge)
+          add_rows(std::true_type{});
+        else
+          add_rows(std::false_type{});
 #pragma unroll
-      for (int half = 4; half >= 1; half >>= 1) {
-        const bool upper = (fr & half) != 0;
+        for (int half = 4; half >= 1; half >>= 1) {
+          const bool upper = (fr & half) != 0;
 #pragma unroll
-        for (int e = 0; e < half; ++e) {
-          const float keep = upper ? sum[e + half] : sum[e], give = upper ? sum[e] : sum[e + half];
-          sum[e] = keep + __shfl_xor(give, half, 64);
+          for (int e = 0; e < half; ++e) {
+            const float keep = upper ? sum[e + half] : sum[e], give = upper ? sum[e] : sum[e + half];
+            sum[e] = keep + __shfl_xor(give, half, 64);
+          }
         }
+        sum[0] += __shfl_xor(sum[0], 8, 64);
+        if (writes) acc[at + key] = was + sum[0];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int c = 0; c < kNF; ++c) kf[a][c] = kn[a][c];
       }
-      sum[0] += __shfl_xor(sum[0], 8, 64);
-      if (writes) acc[at + key] = was + sum[0];
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int c = 0; c < kNK; ++c) kf[a][c] = kn[a][c];
-    }
     }
   });
 }
 
-// acc[b][g][key] += sum over the rows of w exp(s - lse): one workgroup per 64 keys of a (sequence, KV head).
-template <typename T, int DH>
-__global__ __launch_bounds__(256) void tree_weight_kernel(const T* __restrict__ Q, const T* __restrict__ K,
-                                                          const float* __restrict__ lse, const int* __restrict__ lens,
-                                                          const int* __restrict__ cu_q,
-                                                          const int64_t* __restrict__ mask,
-                                                          const float* __restrict__ row_weight, TreeShape sh, float c2,
-                                                          float* __restrict__ acc) {
-  constexpr int P = DH + 4, PP = kTKeys + 4;
-  __shared__ __attribute__((aligned(16))) float qs[kTRows * P], ks[kTKeys * P], ps[kTRows * PP];
-  const int bg = blockIdx.x % (sh.B * sh.Hkv), b = bg / sh.Hkv, g = bg % sh.Hkv;
-  const int k = blockIdx.x / (sh.B * sh.Hkv) * kTKeys;
-  const int G = sh.Hq / sh.Hkv;
-  const TreeSeq q = tree_seq(sh, lens, cu_q, b);
-  const int R = q.T * G, tid = threadIdx.x, rr = tid >> 4, c = tid & 15;
-  if (k >= q.keys || R == 0) return;
-  stage_rows<T, DH, P>(K + (size_t(bg) * sh.cap + k) * DH, kTKeys, q.keys - k, ks);
-  float sum = 0.f;
-  for (int r0 = 0; r0 < R; r0 += kTRows) {
-    __syncthreads();
-    TreeSegment seg{};
-    seg.g = g;
-    seg.r0 = r0;
-    seg.q0 = q.q0;
-    stage_queries<T, DH, P>(Q, sh, seg, R, qs);
-    __syncthreads();
-    const int r = r0 + rr;
-    const uint64_t bits = r < R ? tree_bits(mask, q.q0, r / G) : 0;
-    const float l = r < R ? lse[size_t(g * G + r % G) * sh.n_q + q.q0 + r / G] : -INFINITY;
-    const float w = r >= R ? 0.f : row_weight ? row_weight[q.q0 + r / G] : 1.f;
-    float s[4];
-    scores4<DH, P>(qs, ks, rr, c, s);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const bool sees = w != 0.f && l != -INFINITY && tree_sees(bits, k + 16 * j + c - q.len);
-      ps[rr * PP + 16 * j + c] = sees ? w * fast_exp2(fmaf(s[j], c2, -l * kLog2e)) : 0.f;
-    }
-    __syncthreads();
-    if (tid < kTKeys)
-#pragma unroll
-      for (int i = 0; i < kTRows; ++i) sum += ps[i * PP + tid];
-  }
-  if (tid < kTKeys && k + tid < q.keys) acc[size_t(bg) * sh.cap + k + tid] += sum;
-}
-
 // ------------------------------------------------------------------ plan and workspace
 
-// How a call is cut: items of 2^item_shift rows, 16 a wave (fp32: 16 a workgroup), at most `items` of them a
+// How a call is cut: items of 2^item_shift rows, 16 a wave, at most `items` of them a
 // (sequence, KV head), their chunks shared by `wgs` workgroups.
 struct TreePlan {
-  int waves;  // of a matrix-core workgroup
+  int waves;  // of a workgroup
   int item_shift, items, wgs;
   bool stored;  // the scores are kept for the account
 };
 // Waves that share a ring: as many as have a transfer of each part (two at a head size of 32).
 constexpr int tree_waves(int dh) { return dh == 32 ? 2 : 4; }
-// LDS of tree_attn_mfma_kernel: the ring, and the rows of Q of several waves.
-inline int tree_lds(int dh, int waves) { return 320 * dh + (waves > 1 ? waves * 32 * dh : 0); }
+// LDS of tree_attn_kernel: the ring, and the rows of Q of several waves.
+inline int tree_lds(int dh, int waves, int es) { return 320 * dh + (waves > 1 ? waves * 16 * dh * es : 0); }
 inline TreePlan plan_tree(int B, int max_q, int max_kv, int Hq, int Hkv, int dh, int dtype) {
   const int64_t rows = int64_t(max_q) * (Hq / Hkv);
   TreePlan p;
-  p.waves = dtype == ESTP_F32 || rows <= 16 ? 1 : tree_waves(dh);
+  // One wave's rows up to 16: with 8 sequences of 4096, heads of 128, 12 rows take 41.7 us so and 50.5 us with three
+  // waves idle.  More rows: 20 rows 36.2 us with four waves of 16 rows, 38.2 us with a wave of 32; 64 rows 41.6 and
+  // 59.9; 92 rows at 16 sequences of 3000 63.3 and 113.6.
+  p.waves = rows <= 16 ? 1 : tree_waves(dh);
   p.item_shift = p.waves == 1 ? 4 : p.waves == 2 ? 5 : 6;
   p.items = int((rows + (1 << p.item_shift) - 1) >> p.item_shift);
   // one grid fills the chip: what 160 KB of LDS hold of the rings, or registers of the waves, on 256 units
-  const int64_t fill = dtype == ESTP_F32 ? 512 : p.waves == 1 ? 1024 * (128 / dh) : 512 * std::min(128 / dh, 4);
+  const int64_t fill = p.waves == 1 ? 1024 * (128 / dh) : 512 * std::min(128 / dh, 4);
   const int64_t shares = (int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) + 3) / 4;  // at most
   p.wgs = int((std::min(fill, shares) + 7) / 8 * 8);
-  // Scores: 8 bytes a row and key, written and read, against 2 dh for forming them again.
-  p.stored = dtype == ESTP_BF16 && p.items == 1 && p.waves == 1 && rows * 8 <= dh;
+  // Scores: 8 bytes a row and key, written and read, against 2 dh for forming them again.  8 sequences of 4096 or 8192,
+  // attention with account, kept against formed again: dh 128, 4 rows 42 and 49 us, 16 rows 50.5 and 50.8; dh 64, 4
+  // rows 27.3 and 32.8, 8 rows 47.9 and 50.1, 16 rows 53.8 and 51.6; dh 32, 4 rows 29.4 and 33.0, 8 rows 34.6 and
+  // 34.5.
+  p.stored = p.waves == 1 && rows * 16 <= dh * (dtype == ESTP_F32 ? 4 : 2);
   return p;
 }
 
@@ -966,19 +905,21 @@ int check_tree_args(const char* fn, const void* Q, const void* K, const int32_t*
   ESTP_REQUIRE(aligned(lens, 4) && aligned(cu_q, 4), ESTP_ERR_INVALID_ARG, "%s: lens and cu_q must be 4-byte aligned",
                fn);
   ESTP_REQUIRE(dh == 32 || dh == 64 || dh == 128, ESTP_ERR_UNSUPPORTED, "%s: head_dim %d not in {32, 64, 128}", fn, dh);
-  ESTP_REQUIRE(max_q <= kMaxTree, ESTP_ERR_UNSUPPORTED, "%s: max_q = %d, at most %d drafted tokens", fn, max_q, kMaxTree);
+  ESTP_REQUIRE(max_q <= kMaxTree, ESTP_ERR_UNSUPPORTED, "%s: max_q = %d, at most %d drafted tokens", fn, max_q,
+               kMaxTree);
   ESTP_REQUIRE(int64_t(max_q) * (Hq / Hkv) <= 65535 && Hq / Hkv <= 32768 && Hq <= 65535, ESTP_ERR_UNSUPPORTED,
                "%s: %d query heads, %d sharing a KV head", fn, Hq, Hq / Hkv);
   ESTP_REQUIRE(int64_t(B) * Hkv <= 65535 && n_q * Hq <= INT32_MAX / 64, ESTP_ERR_UNSUPPORTED,
-               "%s: B Hkv = %lld (at most 65535) or n_q Hq = %lld too large", fn, (long long)B * Hkv, (long long)n_q * Hq);
-  const size_t tiles = size_t(max_kv + kTKeys - 1) / kTKeys;
+               "%s: B Hkv = %lld (at most 65535) or n_q Hq = %lld too large", fn, (long long)B * Hkv,
+               (long long)n_q * Hq);
+  const size_t tiles = (size_t(max_kv) + 63) / 64;
   ESTP_REQUIRE(fits_launch(tiles * size_t(B) * Hkv, 256), ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv too large", fn);
   return ESTP_OK;
 }
 
 // ESTP_DEBUG_CHECKS=1: lens and cu_q against what the header asks of them, before any kernel reads them
-int debug_check_tree(const char* fn, const int32_t* lens, const int32_t* cu_q, int B, int max_q, int64_t n_q, int max_kv,
-                     hipStream_t s) {
+int debug_check_tree(const char* fn, const int32_t* lens, const int32_t* cu_q, int B, int max_q, int64_t n_q,
+                     int max_kv, hipStream_t s) {
   if (!debug_checks_enabled()) return ESTP_OK;
   std::vector<int> l, cu;
   int st = debug_copy(fn, "lens", lens, size_t(B), s, &l);
@@ -988,8 +929,8 @@ int debug_check_tree(const char* fn, const int32_t* lens, const int32_t* cu_q, i
   for (int b = 0; b < B; ++b) {
     const int64_t T = int64_t(cu[b + 1]) - cu[b];
     ESTP_REQUIRE(T >= 0 && T <= max_q, ESTP_ERR_INVALID_ARG,
-                 "%s: debug check: sequence %d has %lld drafted tokens, must be in [0, max_q = %d]", fn, b, (long long)T,
-                 max_q);
+                 "%s: debug check: sequence %d has %lld drafted tokens, must be in [0, max_q = %d]", fn, b,
+                 (long long)T, max_q);
     ESTP_REQUIRE(l[b] >= 0 && l[b] + T <= max_kv, ESTP_ERR_INVALID_ARG,
                  "%s: debug check: sequence %d has %d cached and %lld drafted tokens, max_kv = %d", fn, b, l[b],
                  (long long)T, max_kv);
@@ -1005,31 +946,27 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
                 const TreeShape& sh, const TreePlan& p, float scale, T* O, float* lse, float* acc,
                 const TreeBuffers& t, hipStream_t s) {
   const dim3 grid{unsigned(p.wgs)};
-  constexpr int kChunk = sizeof(T) == 2 ? 32 : kTKeys;
-  if constexpr (sizeof(T) == 2) {
-    auto kernel = p.waves > 1 ? tree_attn_mfma_kernel<DH, tree_waves(DH), false>
-                  : acc       ? tree_attn_mfma_kernel<DH, 1, true>
-                              : tree_attn_mfma_kernel<DH, 1, false>;
-    kernel<<<grid, dim3(64 * p.waves), tree_lds(DH, p.waves), s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e,
-                                                                   t.scores, t.pitch, t.m, t.l, t.o);
-  } else {
-    tree_attn_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.m, t.l, t.o);
-  }
+  constexpr int kChunk = TreeMath<T>::kC;
+  auto kernel = p.waves > 1 ? tree_attn_kernel<T, DH, tree_waves(DH), false>
+                : acc       ? tree_attn_kernel<T, DH, 1, true>
+                            : tree_attn_kernel<T, DH, 1, false>;
+  kernel<<<grid, dim3(64 * p.waves), tree_lds(DH, p.waves, int(sizeof(T))), s>>>(
+      Q, K, V, lens, cu_q, mask, sh, scale * kLog2e, t.scores, t.pitch, t.m, t.l, t.o);
   ESTP_CHECK_LAUNCH("tree_attn_kernel");
-  // segments of an item, about: waves of a row
+  // Segments of an item, about, and by them the waves of a row.  18 segments (8 sequences of 4096, 64 rows of 64): one
+  // wave 27.1 us with the attention, four 30.1; 34 segments (the same, 16 rows): 24.9 and 23.5; 66 (2 of 16000, 4
+  // rows of 128): four 33.3, sixteen 32.8; 130 (one of 32767): one 47.4, four 35.8, sixteen 33.4.
   const int64_t segs = std::min<int64_t>(int64_t(p.wgs) / (int64_t(sh.B) * sh.Hkv * p.items), sh.max_kv / 128) + 2;
   auto join = [&](auto waves) -> int {
     constexpr int kWaves = decltype(waves)::value, kThreads = tree_join_threads(kWaves);
     const int per = kWaves == 1 ? (sh.Hq + 3) / 4 : sh.Hq;  // workgroups of a token
-    if constexpr (sizeof(T) == 2) {
-      if (acc) {
-        const unsigned n_join = unsigned(sh.n_q) * unsigned(per);
-        const unsigned n_keys = unsigned((sh.max_kv + 4 * kThreads - 1) / (4 * kThreads)) * unsigned(sh.B * sh.Hkv);
-        tree_finish_kernel<DH, kWaves, kChunk><<<dim3(n_join + n_keys), dim3(kThreads), 0, s>>>(
-            t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse, int(n_join), t.scores, t.pitch, acc);
-        ESTP_CHECK_LAUNCH("tree_finish_kernel");
-        return ESTP_OK;
-      }
+    if (acc) {
+      const unsigned n_join = unsigned(sh.n_q) * unsigned(per);
+      const unsigned n_keys = unsigned((sh.max_kv + 4 * kThreads - 1) / (4 * kThreads)) * unsigned(sh.B * sh.Hkv);
+      tree_finish_kernel<T, DH, kWaves, kChunk><<<dim3(n_join + n_keys), dim3(kThreads), 0, s>>>(
+          t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse, int(n_join), t.scores, t.pitch, acc);
+      ESTP_CHECK_LAUNCH("tree_finish_kernel");
+      return ESTP_OK;
     }
     tree_join_kernel<T, DH, kWaves, kChunk><<<dim3(unsigned(sh.n_q), unsigned(per)), dim3(kThreads), 0, s>>>(
         t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
@@ -1043,17 +980,11 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
 template <typename T, int DH>
 int launch_weight(const T* Q, const T* K, const float* lse, const int* lens, const int* cu_q, const int64_t* mask,
                   const float* row_weight, TreeShape sh, float scale, float* acc, hipStream_t s) {
-  const unsigned tiles = unsigned((sh.max_kv + kTKeys - 1) / kTKeys);
-  const unsigned wgs = tiles * unsigned(sh.B * sh.Hkv);
-  if constexpr (sizeof(T) == 2) {
-    sh.item_shift = 16;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
-    const dim3 grid(std::min(DH == 128 ? 768u : 1024u, (wgs + 7) / 8 * 8));  // (a share is 128 keys or more)
-    tree_weight_mfma_kernel<DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
-                                                           acc);
-  } else {
-    tree_weight_kernel<T, DH><<<dim3(wgs), dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh,
-                                                              scale * kLog2e, acc);
-  }
+  sh.item_shift = 16;  // all rows of a (sequence, KV head) in one item: one workgroup adds to a slot
+  const size_t shares = (size_t(sh.max_kv) + 127) / 128 * size_t(sh.B) * sh.Hkv;  // of 128 keys or more: at most
+  const dim3 grid(unsigned(std::min<size_t>(256 * tree_weight_wgs(DH * int(sizeof(T))), (shares + 7) / 8 * 8)));
+  tree_weight_kernel<T, DH><<<grid, dim3(256), 0, s>>>(Q, K, lse, lens, cu_q, mask, row_weight, sh, scale * kLog2e,
+                                                       acc);
   ESTP_CHECK_LAUNCH("tree_weight_kernel");
   return ESTP_OK;
 }
@@ -1104,7 +1035,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
                "%s: workspace must be non-null and 256-byte aligned", fn);
   const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
   ESTP_REQUIRE(fits_launch(2 * size_t(n_q) * Hq, 1024) &&
-                   int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX,
+                   int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX / 2,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
   const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, p.item_shift, p.items);
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
