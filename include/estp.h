@@ -448,7 +448,7 @@ ESTP_API int estp_tree_importance(const void* Q, const void* K, const float* lse
  * Requires 1 <= keep <= cap, recent + sink <= keep, dh in {32, 64, 128}; B Hkv > 65535
  * returns ESTP_ERR_UNSUPPORTED.  Exact: copies and whole numbers only.
  * ------------------------------------------------------------------------ */
-ESTP_API size_t estp_cache_evict_workspace_size(int32_t B, int32_t Hkv, int32_t keep);
+ESTP_API size_t estp_cache_evict_workspace_size(int32_t B, int32_t Hkv, int64_t cap, int32_t keep);
 ESTP_API int estp_cache_evict(void* K, void* V, const float* acc, const int32_t* pos, const int32_t* lens,
                      const int32_t* seen, int32_t B, int32_t Hkv, int64_t cap, int32_t dh, int dtype, int32_t keep,
                      int32_t recent, int32_t sink, float* acc_out, int32_t* pos_out, int32_t* lens_out, int32_t* idx,

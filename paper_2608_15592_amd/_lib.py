@@ -130,7 +130,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.estp_tree_importance.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I32, _I32, _I64, _I32, _I32, _I64, _I32, _I32,
                                          _F, _INT, _P, _P]
     lib.estp_cache_evict_workspace_size.restype = _SZ
-    lib.estp_cache_evict_workspace_size.argtypes = [_I32, _I32, _I32]
+    lib.estp_cache_evict_workspace_size.argtypes = [_I32, _I32, _I64, _I32]
     lib.estp_cache_evict.restype = _INT
     lib.estp_cache_evict.argtypes = [_P, _P, _P, _P, _P, _P, _I32, _I32, _I64, _I32, _INT, _I32, _I32, _I32, _P, _P,
                                      _P, _P, _P, _SZ, _P]
@@ -673,7 +673,7 @@ def cache_evict(K: torch.Tensor, V: torch.Tensor, acc: torch.Tensor, pos: torch.
             idx = torch.empty(B, Hkv, max(keep, 0), dtype=i32, device=dev)
         else:
             _all_sized(dev.index, dev, (idx, "idx", B * Hkv * max(keep, 0), i32))
-        workspace, wsb = _workspace(lib.estp_cache_evict_workspace_size(B, Hkv, keep), dev, workspace)
+        workspace, wsb = _workspace(lib.estp_cache_evict_workspace_size(B, Hkv, cap, keep), dev, workspace)
         _check(lib.estp_cache_evict(_ptr(K), _ptr(V), _ptr(acc), _ptr(pos), _ptr(lens), _ptr(seen), B, Hkv, cap, dh,
                                     dt, keep, int(recent), int(sink), _ptr(acc_out), _ptr(pos_out),
                                     _ptr(lens_out), _ptr(idx), _ptr(workspace), wsb, st), "estp_cache_evict")

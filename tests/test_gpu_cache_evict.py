@@ -79,7 +79,10 @@ def test_eviction_is_exact(lens, Hkv, dh, cap, keep, recent, sink, values, in_pl
 
 
 LONG = [
-    # lens, Hkv, dh, cap, keep, recent, sink: slots held in registers up to 16384, 32768 and 65536 of a cache
+    # lens, Hkv, dh, cap, keep, recent, sink: about where slots no longer stay in registers, and past it
+    ([16384, 16385, 9000], 2, 64, 16385, 16384, 64, 4),
+    ([20000, 100, 0, 16385, 17000], 2, 32, 20000, 17000, 64, 4),
+    ([17000, 16000], 1, 32, 17000, 17000, 64, 4),
     ([16000, 16384, 4096, 4097], 1, 32, 16384, 4096, 64, 4),
     ([20000, 5000, 32768], 2, 32, 32768, 5000, 64, 4),
     ([32769, 65536, 40000], 2, 32, 65536, 32768, 64, 4),
@@ -92,6 +95,50 @@ LONG = [
 @pytest.mark.parametrize("values", ["heavy", "ties", "odd"])
 def test_eviction_from_long_caches(lens, Hkv, dh, cap, keep, recent, sink, values):
     _check(*_case(len(lens) + cap, lens, Hkv, dh, cap, "bf16", values), keep, recent, sink, values != "ties")
+
+
+def test_long_caches_of_many_groups():
+    # few segments a group
+    g = np.random.default_rng(9)
+    lens = np.concatenate([[16400, 0, 3000], g.integers(2500, 16401, 17)])
+    _check(*_case(9, lens.tolist(), 8, 32, 16400, "bf16"), 3000, 64, 4, True)
+
+
+@pytest.mark.parametrize("values", ["heavy", "ties", "equal"])
+def test_more_guarded_slots_than_kept_in_a_long_cache(values):
+    K, V, acc, pos, lens, seen = _case(12, [30000, 20000], 2, 32, 30000, "bf16", values)
+    pos[:] = np.where(np.arange(30000) % 2, 0, pos)
+    _check(K, V, acc, pos, lens, seen, 9000, 10, 5, False)
+
+
+def test_long_cache_replayed_in_a_graph_on_a_stale_workspace():
+    K, V, acc, pos, lens, seen = _case(13, [40000, 500], 2, 32, 40000, "bf16")
+    t = [dev(a) for a in (K, V, acc, pos, lens, seen)]
+    need = estp.load().estp_cache_evict_workspace_size(2, 2, 40000, 1000)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    idx = torch.empty(2, 2, 1000, dtype=torch.int32, device="cuda")
+    call = lambda: estp.cache_evict(*t, 1000, 64, 4, lens_out=t[4], idx=idx, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    want, new = OP.cache_evict(acc, pos, lens, seen, 1000, 64, 4)
+    for rep in range(3):
+        for a, b in zip(t, (K, V, acc, pos, lens, seen)):
+            a.copy_(dev(b))
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(host(idx), want)
+        np.testing.assert_array_equal(host(t[4]), new)
+        moved = OP.evicted(acc, want, lens, 0.0)
+        np.testing.assert_array_equal(host(t[2]).view(np.int32), moved.view(np.int32))
 
 
 def test_more_guarded_slots_than_kept():
@@ -139,7 +186,8 @@ def test_counts_out_of_range_stay_in_bounds():
 
 def test_repeats_and_streams():
     K, V, acc, pos, lens, seen = _case(5, [3000, 100, 2500], 8, 128, 3000, "bf16", "ties")
-    ws = torch.full((estp.load().estp_cache_evict_workspace_size(3, 8, 1000),), 255, dtype=torch.uint8, device="cuda")
+    need = estp.load().estp_cache_evict_workspace_size(3, 8, 3000, 1000)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
     outs = []
     side = torch.cuda.Stream()
     for kw in ({}, {"workspace": ws, "stream": side}):
@@ -154,7 +202,7 @@ def test_repeats_and_streams():
 def test_replayed_in_a_graph():
     K, V, acc, pos, lens, seen = _case(6, [300, 50], 2, 64, 300, "bf16")
     Kd, Vd, ad, pd, ld, sd = (dev(a) for a in (K, V, acc, pos, lens, seen))
-    ws = torch.empty(estp.load().estp_cache_evict_workspace_size(2, 2, 100), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(estp.load().estp_cache_evict_workspace_size(2, 2, 300, 100), dtype=torch.uint8, device="cuda")
     idx = torch.empty(2, 2, 100, dtype=torch.int32, device="cuda")
 
     def step():

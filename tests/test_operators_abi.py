@@ -113,8 +113,10 @@ def test_tree_importance_validation():
 
 def test_cache_evict_validation():
     lib = estp.load()
-    ws = lib.estp_cache_evict_workspace_size(2, 4, 50)
-    assert ws > 0 and lib.estp_cache_evict_workspace_size(0, 4, 50) == 0
+    ws = lib.estp_cache_evict_workspace_size(2, 4, 100, 50)
+    assert ws > 0 and lib.estp_cache_evict_workspace_size(0, 4, 100, 50) == 0
+    assert lib.estp_cache_evict_workspace_size(2, 4, 49, 50) == lib.estp_cache_evict_workspace_size(2, 4, 1 << 31, 50) == 0
+    assert lib.estp_cache_evict_workspace_size(2, 4, 1 << 20, 50) > ws
     names = "K V acc pos lens seen B Hkv cap dh dtype keep recent sink acc_out pos_out lens_out idx ws wsb stream".split()
     call = _caller(lib.estp_cache_evict, names, (FAKE, OTHER, FAKE, FAKE, FAKE, FAKE, 2, 4, 100, 64, 0, 50, 8, 4, FAKE,
                                                  FAKE, FAKE, FAKE, WS, ws, None))
