@@ -178,29 +178,30 @@ template <typename T>
 __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ acc, const int* __restrict__ slot,
                                                       const int* __restrict__ n_live, int d, int Vc, int tile_toks,
                                                       int wgs, size_t room, T* __restrict__ dX) {
-  const int tok = blockIdx.x, k = 4 * (blockIdx.y * 256 + threadIdx.x), s = slot[tok];
-  const int n = n_live[1], n_tokens = n_live[0];
-  if (k >= d) return;
+  const int tok = blockIdx.x, s = slot[tok], n = n_live[1], n_tokens = n_live[0];
   const Shares sh = dx_shares(n, d, Vc, tile_toks, wgs, room);
   const size_t each = size_t(n) * d;
-  f32x4_t v{0.f, 0.f, 0.f, 0.f};
-  if (s >= 0)
-    for (int r = s; r < n; r += n_tokens) {
-      const float* from = acc + size_t(r) * d + k;
-      constexpr int kAhead = 8;
-      for (int p = 0; p < sh.n; p += kAhead) {
-        f32x4_t x[kAhead];
+  for (int k = 4 * (blockIdx.y * 256 + threadIdx.x); k < d; k += 1024 * gridDim.y) {
+    f32x4_t v{0.f, 0.f, 0.f, 0.f};
+    if (s >= 0)
+      for (int r = s; r < n; r += n_tokens) {
+        const float* from = acc + size_t(r) * d + k;
+        constexpr int kAhead = 8;  // shares on their way together
+        for (int p = 0; p < sh.n; p += kAhead) {
+          f32x4_t x[kAhead];
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          x[u] = *reinterpret_cast<const f32x4_t*>(from + size_t(min(p + u, sh.n - 1)) * each);
+          for (int u = 0; u < kAhead; ++u) {
+            x[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            if (p + u < sh.n) x[u] = *reinterpret_cast<const f32x4_t*>(from + size_t(p + u) * each);
+          }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          if (p + u < sh.n) v += x[u];
+          for (int u = 0; u < kAhead; ++u) v += x[u];
+        }
       }
-    }
-  T* o = dX + size_t(tok) * d + k;
+    T* o = dX + size_t(tok) * d + k;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
+    for (int q = 0; q < 4; ++q) o[q] = T(v[q]);
+  }
 }
 
 // ------------------------------------------------------------------ matrix-core products (fp32)
@@ -900,7 +901,8 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
     }
   }
   if (dX) {
-    loss_dx_kernel<T><<<dim3(n, unsigned((d + 1023) / 1024)), block, 0, s>>>(
+    const unsigned of_token = unsigned(std::min((d + 1023) / 1024, std::max(1, 2048 / n)));  // few tokens: workgroups
+    loss_dx_kernel<T><<<dim3(n, of_token), block, 0, s>>>(
         b.acc, b.slot, b.n_live, d, p.Vc, p.tile_toks, kWgs, b.room, static_cast<T*>(dX));
     ESTP_CHECK_LAUNCH("loss_dx_kernel");
   }
