@@ -341,7 +341,8 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  *                    what estp_token_loss_backward takes
  *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL (lse can come from
  *                    other sums with them than without: its last bits then differ)
- * Other arguments and requirements are those of estp_token_entropy.
+ * Other arguments and requirements are those of estp_token_entropy; V > 2^31 - 65537 returns
+ * ESTP_ERR_UNSUPPORTED.
  *
  * estp_token_loss_backward: with grad_i the gradient of the objective with
  * respect to loss_i,
@@ -357,8 +358,8 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  * to 64 tokens of ESTP_BF16 in two parts, the second what the rounding of the
  * first leaves); sums are fp32 and each output element is rounded once.
  * Bitwise repeatable.
- * n_tok > 4194304, d > 1048576 or n_tok d > 2^36 returns ESTP_ERR_UNSUPPORTED.  The workspace
- * holds one piece of G (about 256 MiB, more past 8192 tokens of fp32 or 16384 of bf16), the live
+ * n_tok > 4194304, d > 1048576, n_tok d > 2^36 or V as above returns ESTP_ERR_UNSUPPORTED.  The
+ * workspace holds one piece of G (about 256 MiB, more past 8192 tokens of fp32 or 16384 of bf16), the live
  * rows of X and fp32 sums of dX.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);

@@ -958,6 +958,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
   ESTP_REQUIRE(targets && loss && lse, ESTP_ERR_INVALID_ARG, "%s: targets, loss and lse must be non-null", fn);
   ESTP_REQUIRE(aligned(targets, 4) && aligned(loss, 4) && aligned(lse, 4) && aligned(H, 4) && aligned(vocab_argmax, 4),
                ESTP_ERR_INVALID_ARG, "%s: targets and the outputs must be 4-byte aligned", fn);
+  ESTP_REQUIRE(V <= INT32_MAX - 65536, ESTP_ERR_UNSUPPORTED, "%s: V = %d, at most 2^31 - 65537", fn, V);
   const int st = check_lm_head_args(fn, X, W, n_tok, d, V, dtype);
   if (st != ESTP_OK) return st;
   const size_t need = estp_token_loss_workspace_size(n_tok, d, V, dtype);
@@ -1030,6 +1031,7 @@ extern "C" int estp_token_loss_backward(const void* X, const void* W, const int3
   ESTP_REQUIRE(aligned(targets, 4) && aligned(lse, 4) && aligned(grad, 4), ESTP_ERR_INVALID_ARG,
                "%s: targets, lse and grad must be 4-byte aligned", fn);
   ESTP_REQUIRE(aligned(dX, 16) && aligned(dW, 16), ESTP_ERR_INVALID_ARG, "%s: dX and dW must be 16-byte aligned", fn);
+  ESTP_REQUIRE(V <= INT32_MAX - 65536, ESTP_ERR_UNSUPPORTED, "%s: V = %d, at most 2^31 - 65537", fn, V);
   const int st = check_lm_head_args(fn, X, W, n_tok, d, V, dtype);
   if (st != ESTP_OK) return st;
   ESTP_REQUIRE(n_tok <= (int64_t(1) << 22), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %lld, at most 4194304", fn,

@@ -41,6 +41,7 @@ def test_token_loss_validation():
     assert call(d=40, dtype=1, wsb=0) == 3
     assert call(wsb=ws - 1) == 3
     assert lib.estp_token_loss_workspace_size(0, 64, 1000, 0) == 0
+    assert call(V=(1 << 31) - 65536, wsb=1 << 62) == 2
     # more tokens than one launch holds: refused before any kernel, with room enough
     for dtype in (0, 1):
         assert call(n=(1 << 26) + 1, V=3, dtype=dtype, wsb=1 << 62) == 2
@@ -61,6 +62,7 @@ def test_token_loss_backward_validation():
     assert call(n=0) == call(V=0) == call(d=60) == call(dtype=2) == 1
     assert call(d=40) == call(n=(1 << 22) + 1) == 2
     assert call(d=1 << 15, n=(1 << 21) + 1, dtype=1, wsb=1 << 62) == 2
+    assert call(V=(1 << 31) - 65536, wsb=1 << 62) == 2
     assert call(wsb=ws - 1) == 3
     for bad in ((0, 64, 1000), (100, 0, 1000), (100, 64, 0)):
         assert lib.estp_token_loss_backward_workspace_size(*bad, 0) == 0
