@@ -75,8 +75,16 @@ __device__ __forceinline__ bool tree_sees(uint64_t bits, int rel) {
 
 // ------------------------------------------------------------------ the line of chunks
 
-// 64 sequences, one a lane: counts, and how many chunks of kChunk keys their items have in all.
-template <int kChunk>
+// How the line is cut: chunks of kChunk keys; kStart units that an item counts for besides its chunks, so that a share
+// in which one starts, which begins a segment more, has less to do; shares of a multiple of kRound units.  (Attention,
+// kStart 4 against none: 8 sequences of 4096, 64 rows of 128 40.2 and 43.0 us; 26 others 13 % less to 2 % more.  Account,
+// 8 against none: one sequence of 16000, 256 rows of 128 25 and 35 us; 9 others 12 % less to 14 % more.)
+template <int kChunk_, int kStart_, int kRound_>
+struct TreeCut {
+  static constexpr int kChunk = kChunk_, kStart = kStart_, kRound = kRound_;
+};
+// 64 sequences, one a lane: counts, and how many units their items have in all.
+template <typename Cut>
 struct TreeBatch {
   int b0, q0, T, len, keys;
   uint32_t w, upto;  // chunks of the lane's sequence; of the batch's up to and with it
@@ -89,28 +97,30 @@ struct TreeBatch {
     T = q.T;
     len = q.len;
     keys = q.keys;
-    w = uint32_t(sh.Hkv) * items(sh, q.T) * chunks(q.keys);
+    w = uint32_t(sh.Hkv) * items(sh, q.T) * units(q.keys);
     upto = wave_prefix(w);
   }
   __device__ static __forceinline__ uint32_t items(const TreeShape& sh, int T) {  // of a KV head
     return uint32_t(T * sh.G + sh.item_rows() - 1) >> sh.item_shift;
   }
-  __device__ static __forceinline__ uint32_t chunks(int keys) { return uint32_t(keys + kChunk - 1) / kChunk; }
+  __device__ static __forceinline__ uint32_t units(int keys) {
+    return keys > 0 ? uint32_t(keys + Cut::kChunk - 1) / Cut::kChunk + Cut::kStart : 0;
+  }
   __device__ __forceinline__ uint32_t all() const { return lane_of(upto, 63); }
 };
 // Chunks of one share: at least 128 keys, so that joins stay few.
-template <int kChunk, int kRound = 1>
+template <typename Cut>
 __device__ __forceinline__ uint32_t tree_share(uint32_t total, int wgs) {
-  const uint32_t share = max(uint32_t(128 / kChunk), (total + uint32_t(wgs) - 1) / uint32_t(wgs));
-  return (share + kRound - 1) / kRound * kRound;
+  const uint32_t share = max(uint32_t(128 / Cut::kChunk), (total + uint32_t(wgs) - 1) / uint32_t(wgs));
+  return (share + Cut::kRound - 1) / Cut::kRound * Cut::kRound;
 }
-template <int kChunk>
+template <typename Cut>
 __device__ __forceinline__ uint32_t tree_total(const TreeShape& sh, const int* lens, const int* cu_q,
-                                               TreeBatch<kChunk>& first) {
+                                               TreeBatch<Cut>& first) {
   first.fetch(sh, lens, cu_q, 0);
   uint32_t total = first.all();
   for (int b0 = 64; b0 < sh.B; b0 += 64) {
-    TreeBatch<kChunk> t;
+    TreeBatch<Cut> t;
     t.fetch(sh, lens, cu_q, b0);
     total += t.all();
   }
@@ -133,10 +143,10 @@ __device__ __forceinline__ uint32_t tree_sees4(uint64_t bits, int rel) {
 // Calls f with the segments of this workgroup's share, a multiple of kRound chunks, in turn; all values are uniform.
 // Neighbouring shares, whose items have keys in common, go to one XCD, and all XCDs (every 8th workgroup of the grid, a
 // multiple of 8) get as many of the shares there are: with shares rounded up there can be far fewer than workgroups.
-template <int kChunk, int kRound = 1, typename F>
+template <typename Cut, typename F>
 __device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, const int* cu_q, F&& f) {
-  TreeBatch<kChunk> t;
-  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk, kRound>(total, gridDim.x);
+  TreeBatch<Cut> t;
+  const uint32_t total = tree_total<Cut>(sh, lens, cu_q, t), share = tree_share<Cut>(total, gridDim.x);
   const uint32_t shares = (total + share - 1) / share, of_xcd = (shares + 7) / 8;
   const int wg = int((blockIdx.x & 7) * of_xcd + (blockIdx.x >> 3));
   if ((blockIdx.x >> 3) >= of_xcd || uint32_t(wg) >= shares) return;
@@ -156,15 +166,15 @@ __device__ __forceinline__ void tree_walk(const TreeShape& sh, const int* lens, 
     s.T = int(lane_of(uint32_t(t.T), j));
     s.len = int(lane_of(uint32_t(t.len), j));
     s.keys = int(lane_of(uint32_t(t.keys), j));
-    const uint32_t n = TreeBatch<kChunk>::chunks(s.keys), items = TreeBatch<kChunk>::items(sh, s.T);
+    const uint32_t n = TreeBatch<Cut>::units(s.keys), items = TreeBatch<Cut>::items(sh, s.T);
     const uint32_t item = (at - off) / n, c0 = at - off - item * n, c1 = min(n, c0 + (end - at));
     s.g = __builtin_amdgcn_readfirstlane(int(item / items));
     const int part = __builtin_amdgcn_readfirstlane(int(item % items));
     s.r0 = part << sh.item_shift;
-    s.k0 = __builtin_amdgcn_readfirstlane(int(c0) * kChunk);
-    s.k1 = __builtin_amdgcn_readfirstlane(min(s.keys, int(c1) * kChunk));
+    s.k0 = __builtin_amdgcn_readfirstlane(max(0, int(c0) - Cut::kStart) * Cut::kChunk);
+    s.k1 = __builtin_amdgcn_readfirstlane(min(s.keys, max(0, int(c1) - Cut::kStart) * Cut::kChunk));
     s.slot = wg + (s.b * sh.Hkv + s.g) * sh.items + part;  // grows from segment to segment
-    f(s);
+    if (Cut::kStart == 0 || s.k0 < s.k1) f(s);
     at += c1 - c0;
     if (at >= end) return;
     if (at - off >= lane_of(t.w, j)) {
@@ -208,6 +218,9 @@ struct TreeMath<float> {
   }
 };
 
+template <typename T>
+using AttnCut = TreeCut<TreeMath<T>::kC, 4, 1>;
+
 // Items of 16 rows a wave, chunks of 32 keys (fp32: 16).
 //
 // S^T = K Q^T: a lane holds one row (column lane % 16 of the products) and, of each of the chunk's 16-key blocks, keys
@@ -225,7 +238,7 @@ struct TreeMath<float> {
 // and the 8 of a transposing V read lie in distinct banks.
 //
 // Measured: one row of 32 heads on 8 KV heads of 128, one sequence of 32767: 26.2 us, 5.1 TB/s; 32 sequences of 500 to
-// 4000: 52 us, 4.4 TB/s.  31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 26.7 us, of which
+// 4000: 52 us, 4.4 TB/s.  31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 25.8 us, of which
 // 5 us pass before the first chunk and after the last; its exponentials alone are 4 us of the chip's.  fp32, the first
 // of these: 46 us, 5.8 TB/s; 31 drafted tokens at 8 sequences of 4500: 95 us, bf16 27.
 template <typename T, int DH, int kW, bool kScores>
@@ -265,7 +278,7 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_kernel(
     return kBf16 ? 16 * d + 4 * fq + z : 16 * kVW * (d / kVW) + kVW * (4 * fq + z) + d % kVW;
   };
   auto unit_of = [](int row) { return row / kWindow & (kPieces / 2 - 1); };  // swizzle of a V part, in 32 bytes
-  tree_walk<kC>(sh, lens, cu_q, [&](const TreeSegment& q) {
+  tree_walk<AttnCut<T>>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int bg = q.b * sh.Hkv + q.g, r0 = q.r0 + 16 * wave, R = q.T * G, r = r0 + fr;
     const char* Kb = reinterpret_cast<const char*>(K) + size_t(bg) * sh.cap * kRow;
     const char* Vb = reinterpret_cast<const char*>(V) + size_t(bg) * sh.cap * kRow;
@@ -517,13 +530,13 @@ struct TreeParts {
   size_t row0;
 };
 // of part `part` of KV head g of the sequence in lane j of t, whose chunks start `off` chunks into the line
-template <int kChunk>
-__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, const TreeBatch<kChunk>& t, int j, uint32_t off,
+template <typename Cut>
+__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, const TreeBatch<Cut>& t, int j, uint32_t off,
                                                 uint32_t share, int g, int part) {
-  const uint32_t n = TreeBatch<kChunk>::chunks(int(lane_of(uint32_t(t.keys), j)));
-  const uint32_t items = TreeBatch<kChunk>::items(sh, int(lane_of(uint32_t(t.T), j)));
+  const uint32_t n = TreeBatch<Cut>::units(int(lane_of(uint32_t(t.keys), j)));
+  const uint32_t items = TreeBatch<Cut>::items(sh, int(lane_of(uint32_t(t.T), j)));
   off += lane_of(t.upto, j) - lane_of(t.w, j) + (uint32_t(g) * items + uint32_t(part)) * n;
-  const uint32_t wg0 = off / share;
+  const uint32_t wg0 = (off + Cut::kStart) / share;  // the first with a chunk of it
   return {n > 0 ? int((off + n - 1) / share - wg0) + 1 : 0,
           (size_t(wg0) + size_t((t.b0 + j) * sh.Hkv + g) * sh.items + part) << sh.item_shift};
 }
@@ -547,7 +560,7 @@ __device__ __forceinline__ float tree_fold(const float* part_m, const float* par
 // kWaves-th segment; a lane fetches the state of one segment, 64 at a time, and DH / 64 (at least one) columns of
 // each.  Rows past the last sequence's are left as they are.  Latency bounds it, a chain of four loads: 6 us for a few
 // rows, 8.0 us for 31 tokens of 32 heads in 8 sequences (34 MB of partial results).
-template <typename T, int DH, int kWaves, int kChunk>
+template <typename T, int DH, int kWaves>
 __device__ __forceinline__ void tree_join(const float* __restrict__ part_m, const float* __restrict__ part_l,
                                           const float* __restrict__ part_o, const int* __restrict__ lens,
                                           const int* __restrict__ cu_q, const TreeShape& sh, int wgs, int tok, int h,
@@ -557,8 +570,9 @@ __device__ __forceinline__ void tree_join(const float* __restrict__ part_m, cons
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int first = kWaves == 1 ? 0 : wave;
   if (h >= sh.Hq || tok >= cu_q[sh.B]) return;
-  TreeBatch<kChunk> t;
-  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  using Cut = AttnCut<T>;
+  TreeBatch<Cut> t;
+  const uint32_t total = tree_total<Cut>(sh, lens, cu_q, t), share = tree_share<Cut>(total, wgs);
   uint32_t off = 0;
   uint64_t here;
   while (!(here = __ballot(tok >= t.q0 && tok < t.q0 + t.T)) && t.b0 + 64 < sh.B) {
@@ -629,20 +643,20 @@ __device__ __forceinline__ void tree_join(const float* __restrict__ part_m, cons
 }
 constexpr int tree_join_threads(int waves) { return waves == 1 ? 256 : 64 * waves; }
 // One workgroup a row, or four rows of a token (one wave a row).
-template <typename T, int DH, int kWaves, int kChunk>
+template <typename T, int DH, int kWaves>
 __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_join_kernel(
     const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
     const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
     float* __restrict__ lse) {
   const int h = kWaves == 1 ? int(blockIdx.y) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : int(blockIdx.y);
-  tree_join<T, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, blockIdx.x, h, O, lse);
+  tree_join<T, DH, kWaves>(part_m, part_l, part_o, lens, cu_q, sh, wgs, blockIdx.x, h, O, lse);
 }
 
 // The join, and beside it acc[b][g][key] += sum over the rows of exp(s - lse) from the scores (base 2) that the
 // attention kernel has stored.  Workgroups n_join and on take 4 keys a thread of a (sequence, KV head), whose few rows'
 // normalisers they form for themselves: so neither waits for the other's launch (6.7 us for one token at 32767, 7.3 us
 // for 32 sequences of 500 to 4000; in two launches 11.5 and 13 us).
-template <typename T, int DH, int kWaves, int kChunk>
+template <typename T, int DH, int kWaves>
 __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
     const float* __restrict__ part_m, const float* __restrict__ part_l, const float* __restrict__ part_o,
     const int* __restrict__ lens, const int* __restrict__ cu_q, TreeShape sh, int wgs, T* __restrict__ O,
@@ -652,7 +666,7 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
   if (int(blockIdx.x) < n_join) {
     const uint32_t per = kWaves == 1 ? uint32_t(sh.Hq + 3) / 4 : uint32_t(sh.Hq);  // workgroups of a token
     const uint32_t tok = blockIdx.x / per, y = blockIdx.x - tok * per;
-    tree_join<T, DH, kWaves, kChunk>(part_m, part_l, part_o, lens, cu_q, sh, wgs, int(tok),
+    tree_join<T, DH, kWaves>(part_m, part_l, part_o, lens, cu_q, sh, wgs, int(tok),
                                             kWaves == 1 ? int(4 * y) + wave : int(y), O, lse);
     return;
   }
@@ -660,8 +674,9 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
   const uint32_t id = blockIdx.x - n_join, groups = uint32_t(sh.B * sh.Hkv);
   const uint32_t bg = id % groups, k0 = id / groups * (4 * kThreads);
   const int b = int(bg / uint32_t(sh.Hkv)), g = int(bg) - b * sh.Hkv;
-  TreeBatch<kChunk> t;
-  const uint32_t total = tree_total<kChunk>(sh, lens, cu_q, t), share = tree_share<kChunk>(total, wgs);
+  using Cut = AttnCut<T>;
+  TreeBatch<Cut> t;
+  const uint32_t total = tree_total<Cut>(sh, lens, cu_q, t), share = tree_share<Cut>(total, wgs);
   uint32_t off = 0;
   while (t.b0 + 64 <= b) {
     off += t.all();
@@ -699,8 +714,8 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
 // waves in turn, a tile's K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's
 // columns are rows: their sums join at the end of a tile, each exchange halving the values a lane still holds.  Every
 // score costs an exponential and two FMAs, which bound it (16 rows and 32 keys: 300 cycles of a SIMD) after some 6 us
-// until the first tile is done: 31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 18.2 us;
-// 23 tokens, heads of 128, 16 of 700 to 6000, a part of the rows accepted: 21.6 us, 4.3 TB/s.  fp32, the first at 8
+// until the first tile is done: 31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 14.6 us;
+// 23 tokens, heads of 128, 16 of 700 to 6000, a part of the rows accepted: 19.2 us, 4.8 TB/s.  fp32, the first at 8
 // of 4500: 64 us.
 constexpr int kWRows = 128;  // rows in LDS
 constexpr int kWKeys = 32;   // keys of a tile
@@ -727,7 +742,7 @@ __global__ __launch_bounds__(256, tree_weight_wgs(DH * int(sizeof(T)))) void tre
   int place = 0;
   const int tid = threadIdx.x, lane = tid & 63, fr = lane & 15, fq = lane >> 4, G = sh.G;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  tree_walk<kWKeys, 4>(sh, lens, cu_q, [&](const TreeSegment& q) {
+  tree_walk<TreeCut<kWKeys, 8, 4>>(sh, lens, cu_q, [&](const TreeSegment& q) {
     const int R = q.T * G;
     const size_t at = size_t(q.b * sh.Hkv + q.g) * sh.cap;
     auto load_k = [&](Frag(&kf)[2][kNF], int k) {
@@ -946,7 +961,6 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
                 const TreeShape& sh, const TreePlan& p, float scale, T* O, float* lse, float* acc,
                 const TreeBuffers& t, hipStream_t s) {
   const dim3 grid{unsigned(p.wgs)};
-  constexpr int kChunk = TreeMath<T>::kC;
   auto kernel = p.waves > 1 ? tree_attn_kernel<T, DH, tree_waves(DH), false>
                 : acc       ? tree_attn_kernel<T, DH, 1, true>
                             : tree_attn_kernel<T, DH, 1, false>;
@@ -963,12 +977,12 @@ int launch_tree(const T* Q, const T* K, const T* V, const int* lens, const int* 
     if (acc) {
       const unsigned n_join = unsigned(sh.n_q) * unsigned(per);
       const unsigned n_keys = unsigned((sh.max_kv + 4 * kThreads - 1) / (4 * kThreads)) * unsigned(sh.B * sh.Hkv);
-      tree_finish_kernel<T, DH, kWaves, kChunk><<<dim3(n_join + n_keys), dim3(kThreads), 0, s>>>(
+      tree_finish_kernel<T, DH, kWaves><<<dim3(n_join + n_keys), dim3(kThreads), 0, s>>>(
           t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse, int(n_join), t.scores, t.pitch, acc);
       ESTP_CHECK_LAUNCH("tree_finish_kernel");
       return ESTP_OK;
     }
-    tree_join_kernel<T, DH, kWaves, kChunk><<<dim3(unsigned(sh.n_q), unsigned(per)), dim3(kThreads), 0, s>>>(
+    tree_join_kernel<T, DH, kWaves><<<dim3(unsigned(sh.n_q), unsigned(per)), dim3(kThreads), 0, s>>>(
         t.m, t.l, t.o, lens, cu_q, sh, p.wgs, O, lse);
     ESTP_CHECK_LAUNCH("tree_join_kernel");
     return ESTP_OK;
@@ -1035,7 +1049,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
                "%s: workspace must be non-null and 256-byte aligned", fn);
   const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
   ESTP_REQUIRE(fits_launch(2 * size_t(n_q) * Hq, 1024) &&
-                   int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 31) / 32) <= INT32_MAX / 2,
+                   int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 15) / 16 + 4) <= INT32_MAX,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
   const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, p.item_shift, p.items);
   const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
