@@ -515,10 +515,6 @@ __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v)
   __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, 0);
 #endif
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, bf16x2_t{__bf16(lo), __bf16(hi)});
-}
 
 // Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The

@@ -383,16 +383,19 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_kernel(
       // O is rounded once, where it is written (with the first alone its error is 1.4 times that, at the same speed
       // where memory bounds it).
       float p[4 * kB];
-      bf16x8_t pf, pf_lo;
+      u32x4_t pf, pf_lo;
 #pragma unroll
       for (int e = 0; e < 4 * kB; ++e) {
         p[e] = fast_exp2(fmaf(s[e / 4][e % 4], c2, -ref));
         l += p[e];
-        if constexpr (kBf16) {
-          pf[e] = __bf16(p[e]);
-          pf_lo[e] = __bf16(p[e] - float(pf[e]));
-        }
       }
+      if constexpr (kBf16)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // two at a time
+          pf[e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+          pf_lo[e] = pack_bf16(p[2 * e] - __uint_as_float(pf[e] << 16),
+                               p[2 * e + 1] - __uint_as_float(pf[e] & 0xffff0000u));
+        }
       // ---- output
       part_landed();
       if (kW > 1) {
@@ -487,9 +490,9 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_kernel(
       slot = slot + 1 == kSlots ? 0 : slot + 1;
       if constexpr (kBf16) {
 #pragma unroll
-        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf, o[d]);
+        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pf), o[d]);
 #pragma unroll
-        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], pf_lo, o[d]);
+        for (int d = 0; d < kND; ++d) o[d] = mfma_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pf_lo), o[d]);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
