@@ -94,7 +94,11 @@ __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X,
     }
     const float top = wave_max(M);
     s = wave_sum(s * fast_exp2(fmaxf(M - fmaxf(top, -0x1p127f), kExp2Floor)));
-    l = kLn2 * (top + fast_log2(s));
+    // in natural units with one rounding (ln 2 in two parts): weights exp(z - lse) near 1, whose distance from 1 is the
+    // gradient, have the error of lse
+    constexpr float kLn2Rest = -1.904654299957768e-9f;
+    const float t2 = fast_log2(s);
+    l = top == -INFINITY ? top + t2 : fmaf(top, kLn2, fmaf(top, kLn2Rest, kLn2 * t2));  // (a NaN in s stays one)
     if (lane == 0) lse[tok] = l;
   } else {
     l = lse[tok];
@@ -223,7 +227,6 @@ constexpr int kFSum = 128;
 
 template <bool kAK, bool kBK, int kTN>
 struct F32Tile {
-  static_assert(kTN == kFT || kBK, "few columns: k contiguous");
   static constexpr int kWM = kTN == kFT ? 2 : 4;            // waves along the rows
   static constexpr int kMI = kFT / 32 / kWM, kNJ = kTN == kFT ? 2 : kTN / 32;  // 32 x 32 blocks of a wave
   static constexpr int kPartB = kTN * kFK * 4, kStage = kFPart + kPartB, kLds = 2 * kStage, kLB = kTN / 32;
@@ -236,8 +239,9 @@ struct F32Tile {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % kWM;
     return {m0 + 32 * kMI * wm + 4 * (lane >> 5), n0 + 32 * kNJ * (wave / kWM) + (lane & 31), wm};
   }
-  // byte offset in the source of what lane `lane` of transfer i of 4 brings; *kc: its first k where k is contiguous
-  template <bool kK>
+  // byte offset in the source of what lane `lane` of transfer i brings of a part of kRows rows; *kc: its first k where
+  // k is contiguous
+  template <bool kK, int kRows>
   __device__ static __forceinline__ uint32_t source(int i, int wave, int lane, uint32_t ld, int* kc) {
     const int at = 64 * (4 * i + wave) + lane;
     if (kK) {
@@ -246,15 +250,16 @@ struct F32Tile {
       return uint32_t(row) * ld + uint32_t(c) * 16u;
     }
     *kc = 0;
-    return uint32_t(at / 32) * ld + uint32_t(at % 32) * 16u;
+    return uint32_t(at / (kRows / 4)) * ld + uint32_t(at % (kRows / 4)) * 16u;
   }
   // rows 32 block + lane % 32 at k = 8 g + 4 (lane / 32) .. + 3 of a part in LDS
-  template <bool kK>
+  template <bool kK, int kRows>
   __device__ static __forceinline__ f32x4_t read(const char* part, int row, int g, int half) {
     if (kK) return *reinterpret_cast<const f32x4_t*>(part + row * 128 + ((2 * g + half) ^ (row & 7)) * 16);
     f32x4_t v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const float*>(part + (8 * g + 4 * half + i) * 512 + row * 4);
+    for (int i = 0; i < 4; ++i)
+      v[i] = *reinterpret_cast<const float*>(part + ((8 * g + 4 * half + i) * kRows + row) * 4);
     return v;
   }
   // acc[i][j] = the product over k in [k0, k1) of the wave's 32 x 32 blocks (mfma32_f32's layout)
@@ -272,9 +277,9 @@ struct F32Tile {
     uint32_t off_a[4], off_b[kLB];
     int kc_a[4], kc_b[kLB];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) off_a[i] = source<kAK>(i, wave, lane, A.ld, &kc_a[i]);
+    for (int i = 0; i < 4; ++i) off_a[i] = source<kAK, kFT>(i, wave, lane, A.ld, &kc_a[i]);
 #pragma unroll
-    for (int i = 0; i < kLB; ++i) off_b[i] = source<kBK>(i, wave, lane, B.ld, &kc_b[i]);
+    for (int i = 0; i < kLB; ++i) off_b[i] = source<kBK, kTN>(i, wave, lane, B.ld, &kc_b[i]);
     auto part = [&](auto contig, auto n_parts, const gemm::Operand& o, int r0, int rows, int k, const uint32_t* off,
                     const int* kc, char* dst) {
       constexpr bool kContig = decltype(contig)::value;
@@ -327,9 +332,9 @@ struct F32Tile {
       for (int g = 0; g < kFK / 8; ++g) {
         f32x4_t a[kMI], b[kNJ];
 #pragma unroll
-        for (int i = 0; i < kMI; ++i) a[i] = read<kAK>(pa, 32 * (kMI * wm + i) + row, g, half);
+        for (int i = 0; i < kMI; ++i) a[i] = read<kAK, kFT>(pa, 32 * (kMI * wm + i) + row, g, half);
 #pragma unroll
-        for (int j = 0; j < kNJ; ++j) b[j] = read<kBK>(pb, 32 * (kNJ * wn + j) + row, g, half);
+        for (int j = 0; j < kNJ; ++j) b[j] = read<kBK, kTN>(pb, 32 * (kNJ * wn + j) + row, g, half);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -480,23 +485,24 @@ __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __rest
 }
 
 // dW[v0 + v][k] = sum over the live tokens of G[s][v] Xc[s][k].  M side: columns k of Xc, N side: vocabulary rows.
+template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __restrict__ G, const float* __restrict__ Xc,
                                                              const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                              int Vc, float* __restrict__ dW) {
-  using Run = F32Tile<false, false, kFT>;
+  using Run = F32Tile<false, false, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
-  const int n = n_live[1], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kFT;
+  const int n = n_live[1], m0 = blockIdx.x * kFT, n0 = blockIdx.y * kTN;
   const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
   if (n0 >= rows) return;
   const gemm::Operand A{reinterpret_cast<const char*>(Xc), uint32_t(d) * 4u, d};
   const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, Vc};
-  Run::Acc acc;
+  typename Run::Acc acc;
   Run::run(lds, A, B, m0, n0, 0, n, acc);
   const auto at = Run::place(m0, n0);
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
+  for (int j = 0; j < Run::kNJ; ++j)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < Run::kMI; ++i)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int v = at.n + 32 * j, k = at.m + 32 * i + 8 * q;
@@ -793,7 +799,15 @@ inline int bf16_tile_toks(int64_t n_tok) { return n_tok <= 384 ? 128 : 256; }
 // Tokens of a fp32 tile: the narrowest that takes them all, up to 128.  d 2048, V 128256, forward and backward in us:
 // 16 tokens 253 and 771 with 32, 379 and 941 with 64, 518 and 1322 with 128; 50 tokens 360 and 1072 with 64, 504 and
 // 1434 with 128; 100 tokens 508 and 1676 with 128, 738 and 1780 with 64.
-inline int f32_tile_toks(int64_t n_tok) { return n_tok <= 32 ? 32 : n_tok <= 64 ? 64 : kFT; }
+// Where 128-wide tiles are fewer than kFewTiles, which leaves compute units idle, 32-wide ones share the work out (of
+// dW, whose columns are vocabulary rows, by its own tiles).  Forward and backward in us with 32 against 128: 128
+// tokens, d 64, V 1000 (8 tiles) 11.7 and 24.6, 11.9 and 38.5; 128 tokens, d 1024, V 16384 (128) 49 and 144, 75 and
+// 176; 400 tokens, d 2048, V 5000 (160) 122 and 315, 141 and 326, V 8000 (252) 161 and 430, 142 and 400.
+constexpr size_t kFewTiles = 192;
+inline int f32_tile_toks(int64_t n_tok, int V) {
+  const size_t tiles = size_t((n_tok + kFT - 1) / kFT) * ((size_t(V) + kFT - 1) / kFT);
+  return n_tok <= 32 || tiles < kFewTiles ? 32 : n_tok <= 64 ? 64 : kFT;
+}
 
 inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   const size_t es = dtype == ESTP_F32 ? 4 : 2;
@@ -806,7 +820,7 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   LossPlan p;
   p.parts = g_parts(n_tok, dtype);
   p.Vc = int(vc);
-  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok) : bf16_tile_toks(n_tok);
+  p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok, V) : bf16_tile_toks(n_tok);
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -891,7 +905,10 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
-        loss_dw_f32_kernel<<<dim3(n_dt, n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
+        const bool few = size_t(n_dt) * n_vt < kFewTiles;
+        auto dw_kernel = few ? loss_dw_f32_kernel<32> : loss_dw_f32_kernel<kFT>;
+        dw_kernel<<<dim3(n_dt, few ? unsigned(p.Vc / 32) : n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc,
+                                                                                 static_cast<T*>(dW));
         ESTP_CHECK_LAUNCH("loss_dw_f32_kernel");
       }
     }
@@ -923,7 +940,7 @@ struct LsePlan {
 LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
   LsePlan p;
   const bool f32 = dtype == ESTP_F32;
-  p.tile = f32 ? f32_tile_toks(n_tok) : bf16_tile_toks(n_tok);
+  p.tile = f32 ? f32_tile_toks(n_tok, V) : bf16_tile_toks(n_tok);
   const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows, n_tt = (n_tok + p.tile - 1) / p.tile;
   const int64_t fill = !f32 ? 256 : p.tile < kFT ? 1024 : 512;
   p.slices = int(std::min(n_vt, std::max<int64_t>(f32 ? 4 : 1, fill / n_tt)));
