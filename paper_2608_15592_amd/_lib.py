@@ -504,11 +504,15 @@ def head_train_step(pooled: torch.Tensor, y: torch.Tensor, edges: torch.Tensor, 
 
 def _head_shapes(X, W, targets):
     _need(X, "X", ndim=2)
-    _need(W, "W", device=X.device, dtype=X.dtype, ndim=2)
-    if W.shape[1] != X.shape[1]:
+    dev = X.device
+    if W.get_device() != dev.index or W.dtype is not X.dtype or W.dim() != 2 or not W.is_contiguous():
+        _need(W, "W", device=dev, dtype=X.dtype, ndim=2)
+    n_tok, d = X.shape
+    V, dw = W.shape
+    if dw != d:
         raise ValueError("X and W disagree on d")
-    _sized(targets, "targets", X.shape[0], device=X.device, dtype=torch.int32)
-    return X.shape[0], X.shape[1], W.shape[0]
+    _all_sized(dev.index, dev, (targets, "targets", n_tok, torch.int32))
+    return n_tok, d, V, dev
 
 
 def token_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None,
@@ -521,18 +525,18 @@ def token_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, loss: Op
     tensors) receive what ``token_entropy`` gives, from the same pass.
     """
     lib = load()
-    n_tok, d, V = _head_shapes(X, W, targets)
+    n_tok, d, V, dev = _head_shapes(X, W, targets)
     dt = _dtype_code(X)
     for t, name, dtype in ((loss, "loss", torch.float32), (lse, "lse", torch.float32), (H, "H", torch.float32),
                            (vocab_argmax, "vocab_argmax", torch.int32)):
         if t is not None:
-            _sized(t, name, n_tok, device=X.device, dtype=dtype)
-    with _on(stream, X.device) as st:
+            _all_sized(dev.index, dev, (t, name, n_tok, dtype))
+    with _on(stream, dev) as st:
         if loss is None:
-            loss = torch.empty(n_tok, dtype=torch.float32, device=X.device)
+            loss = torch.empty(n_tok, dtype=torch.float32, device=dev)
         if lse is None:
-            lse = torch.empty(n_tok, dtype=torch.float32, device=X.device)
-        workspace, wsb = _workspace(lib.estp_token_loss_workspace_size(n_tok, d, V, dt), X.device, workspace)
+            lse = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        workspace, wsb = _workspace(lib.estp_token_loss_workspace_size(n_tok, d, V, dt), dev, workspace)
         _check(lib.estp_token_loss(_ptr(X), _ptr(W), _ptr(targets), n_tok, d, V, dt, _ptr(loss), _ptr(lse), _ptr(H),
                                    _ptr(vocab_argmax), _ptr(workspace), wsb, st), "estp_token_loss")
     return loss, lse
@@ -547,20 +551,18 @@ def token_loss_backward(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
     ``lse`` is ``token_loss``'s; ``grad`` (float32 [n_tok], default all 1) the gradient with respect to the losses.
     """
     lib = load()
-    n_tok, d, V = _head_shapes(X, W, targets)
+    n_tok, d, V, dev = _head_shapes(X, W, targets)
     dt = _dtype_code(X)
-    _sized(lse, "lse", n_tok, device=X.device, dtype=torch.float32)
-    if grad is not None:
-        _sized(grad, "grad", n_tok, device=X.device, dtype=torch.float32)
-    with _on(stream, X.device) as st:
+    for t, name, n, dtype in ((lse, "lse", n_tok, torch.float32), (grad, "grad", n_tok, torch.float32),
+                              (dX, "dX", n_tok * d, X.dtype), (dW, "dW", V * d, X.dtype)):
+        if t is not None:
+            _all_sized(dev.index, dev, (t, name, n, dtype))
+    with _on(stream, dev) as st:
         if dX is None and want_dX:
             dX = torch.empty_like(X)
         if dW is None and want_dW:
             dW = torch.empty_like(W)
-        for t, name, like in ((dX, "dX", X), (dW, "dW", W)):
-            if t is not None:
-                _sized(t, name, like.numel(), device=X.device, dtype=X.dtype)
-        workspace, wsb = _workspace(lib.estp_token_loss_backward_workspace_size(n_tok, d, V, dt), X.device, workspace)
+        workspace, wsb = _workspace(lib.estp_token_loss_backward_workspace_size(n_tok, d, V, dt), dev, workspace)
         _check(lib.estp_token_loss_backward(_ptr(X), _ptr(W), _ptr(targets), _ptr(lse), _ptr(grad), n_tok, d, V, dt,
                                             _ptr(dX), _ptr(dW), _ptr(workspace), wsb, st),
                "estp_token_loss_backward")
