@@ -230,7 +230,7 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
     if (s >= 0)
       for (int r = s; r < n; r += n_tokens) {
         const float* from = acc + size_t(r) * d + k;
-        constexpr int kAhead = 8;  // shares on their way together
+        constexpr int kAhead = 16;  // shares on their way together
         for (int p = 0; p < sh.n; p += kAhead) {
           f32x4_t x[kAhead];
 #pragma unroll
@@ -555,10 +555,12 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
 // Stores of 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
+constexpr int kNonTemporal = 2;  // the cache policy of data that is not read again soon
+template <int kAux = 0>
 __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, 0);
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, kAux);
 #endif
 }
 
@@ -779,6 +781,13 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
 // dW of a piece: G^T Xc.  M side: columns k of Xc, N side: vocabulary rows; both transposed reads, the tokens are
 // the depth.  The matrix cores bound it where there are many (the sizes above: 870 us, 1.26 PFLOP/s); of 684, which are
 // 11 stages a tile, its first stage and its stores are a good part (443 us, 0.81 PFLOP/s).
+//
+// kStream: dW of few tokens is bound by its stores, and one that the last cache does not hold drives W out of it, which
+// the other products of the step read.  It is stored with the non-temporal policy: loss and gradient of 8, 64 and 128
+// tokens at d 2048, V 128256 take 493, 578 and 589 us so against 539, 592 and 603, of 16 at d 4096 894 against 958.
+// With more tokens the stores are spread over the products (256: 736 against 720, 512: 1086 against 1072), and a dW
+// that the cache holds is read from there by whoever uses it (16 at d 1024, V 32000: 106 against 101).
+template <bool kStream>
 __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __restrict__ G,
                                                               const __bf16* __restrict__ Xc,
                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
@@ -808,7 +817,7 @@ __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __re
           const int c0 = m0 + 128 * wm + 8 * fq;  // (of every 32: d is a multiple of 32, all 8 are live or none)
 #pragma unroll
           for (int i = 0; i < 8; i += 2)
-            buf_store16(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
+            buf_store16<kStream ? kNonTemporal : 0>(o, c0 + 16 * i < d ? (row + uint32_t(c0 + 16 * i)) * 2u : kPastEnd,
                         uint4{pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]),
                               pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]),
                               pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3])});
@@ -839,6 +848,12 @@ inline int bf16_tile_toks(int64_t n_tok) { return n_tok <= 384 ? 128 : 256; }
 // Tokens of a fp32 tile: the narrowest that takes them all, up to 128.  d 2048, V 128256, forward and backward in us:
 // 16 tokens 253 and 771 with 32, 379 and 941 with 64, 518 and 1322 with 128; 50 tokens 360 and 1072 with 64, 504 and
 // 1434 with 128; 100 tokens 508 and 1676 with 128, 738 and 1780 with 64.
+// The rule of loss_dw_mfma_kernel's kStream.
+inline bool stream_dw(int64_t n_tok, int d, int V) {
+  constexpr size_t kLastCache = size_t(256) << 20;  // bytes
+  return n_tok <= 128 && size_t(V) * d * 2 > kLastCache;
+}
+
 // Where 128-wide tiles are fewer than kFewTiles, which leaves compute units idle, 32-wide ones share the work out (of
 // dW, whose columns are vocabulary rows, by its own tiles).  Forward and backward in us with 32 against 128: 128
 // tokens, d 64, V 1000 (8 tiles) 11.7 and 24.6, 11.9 and 38.5; 128 tokens, d 1024, V 16384 (128) 49 and 144, 75 and
@@ -924,7 +939,8 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_mfma_kernel");
       }
       if (dW) {
-        loss_dw_mfma_kernel<<<grid, block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
+        auto dw_kernel = stream_dw(n, d, V) ? loss_dw_mfma_kernel<true> : loss_dw_mfma_kernel<false>;
+        dw_kernel<<<grid, block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
         ESTP_CHECK_LAUNCH("loss_dw_mfma_kernel");
       }
     } else {

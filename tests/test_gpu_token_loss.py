@@ -79,6 +79,13 @@ def test_several_vocabulary_pieces(dtype):
     _check_backward(X, W, t, g, dtype, _check_forward(X, W, t, dtype))
 
 
+@pytest.mark.parametrize("n", [5, 128, 129])
+def test_weights_larger_than_the_last_cache(n):
+    # 270 MB of W and dW
+    X, W, t, g = _inputs(n, n, 4096, 33001, "bf16", ignored=0.1)
+    _check_backward(X, W, t, g, "bf16", _check_forward(X, W, t, "bf16"))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_default_weights_and_single_outputs(dtype):
     X, W, t, g = _inputs(6, 90, 64, 700, dtype, ignored=0.3)
