@@ -72,7 +72,7 @@ struct TileOrder {
     return {int(m), int(8 * g + c)};
   }
 };
-// A tile: its first row on either side, its depth [k0, k1), and what the caller adds.
+// A tile: its first row on either side, its depth [k0, k1), [0, 0) if it is empty, and what the caller adds.
 struct Place {
   int m0, n0, k0, k1, tag;
 };

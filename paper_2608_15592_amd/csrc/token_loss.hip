@@ -25,6 +25,7 @@
 
 #include "estp_common.h"
 #include "lm_head.h"
+#include "loss_shares.h"
 #include "mfma_gemm.h"
 
 namespace estp {
@@ -196,23 +197,6 @@ __global__ __launch_bounds__(256) void loss_gather_kernel(const uint4* __restric
     lc[s] = lse[tok];
     gc[s] = grad ? grad[tok] : 1.f;
   }
-}
-
-// Shares of a piece's vocabulary rows whose products add up to its part of dX: as many as give a workgroup each to
-// the chip, while the fp32 sums of all shares (n live rows each) fit into `room` floats.  The same on every piece
-// and for every kernel of a call.
-struct Shares {
-  int n;     // shares
-  int rows;  // vocabulary rows of a share, a multiple of 64
-};
-__device__ __forceinline__ Shares dx_shares(int n_live, int d, int Vc, int tile_toks, int wgs, size_t room) {
-  const int tiles = (n_live + tile_toks - 1) / tile_toks * ((d + 255) / 256);
-  int s = tiles > 0 ? max(1, wgs / tiles) : 1;
-  s = min(s, (Vc + 63) / 64);
-  const size_t each = size_t(max(1, n_live)) * d;
-  s = int(min(size_t(s), max(size_t(1), room / each)));
-  const int rows = ((Vc + s - 1) / s + 63) / 64 * 64;
-  return {(Vc + rows - 1) / rows, rows};
 }
 
 // dX of every token from the partial sums of its slot (and of the second part's), rounded once; 0 for ignored tokens.
@@ -504,8 +488,9 @@ __global__ __launch_bounds__(256, 2) void loss_dx_f32_kernel(const float* __rest
   const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 4u, d};
   const gemm::Operand B{reinterpret_cast<const char*>(G), uint32_t(Vc) * 4u, n};
   for (int share = blockIdx.z; share < sh.n; share += gridDim.z) {
+    const Depth k = sh.depth(share, rows);
     typename Run::Acc acc;
-    Run::run(lds, A, B, m0, n0, min(rows, share * sh.rows), min(rows, (share + 1) * sh.rows), acc);
+    Run::run(lds, A, B, m0, n0, k.k0, k.k1, acc);
     float* out = sums + size_t(share) * size_t(n) * d;
     const auto at = Run::place(m0, n0);
 #pragma unroll
@@ -753,8 +738,8 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
       [&](int id) {
         const int share = int(share_tiles.div(uint32_t(id)));
         const gemm::TileAt t = order(id - share * tiles);
-        return gemm::Place{256 * t.m, Run::kBN * t.n, min(rows, share * sh.rows), min(rows, (share + 1) * sh.rows),
-                           share};
+        const Depth k = sh.depth(share, rows);
+        return gemm::Place{256 * t.m, Run::kBN * t.n, k.k0, k.k1, share};
       },
       [&](const gemm::Place& at, const f32x4_t(&acc)[8][kNBN]) {
         const int m0 = at.m0, n0 = at.n0, lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
