@@ -447,7 +447,8 @@ ESTP_API int estp_tree_importance(const void* Q, const void* K, const float* lse
  *   idx [B, Hkv, keep]      int32 output: the slot that slot i's content came from, -1 from
  *                           lens_out[b] on
  * Requires 1 <= keep <= cap, recent + sink <= keep, dh in {32, 64, 128}; B Hkv > 65535
- * returns ESTP_ERR_UNSUPPORTED.  Exact: copies and whole numbers only.
+ * returns ESTP_ERR_UNSUPPORTED.  Exact: copies and whole numbers only.  A
+ * workspace of a call serves every call with no larger B Hkv, cap and keep.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_cache_evict_workspace_size(int32_t B, int32_t Hkv, int64_t cap, int32_t keep);
 ESTP_API int estp_cache_evict(void* K, void* V, const float* acc, const int32_t* pos, const int32_t* lens,

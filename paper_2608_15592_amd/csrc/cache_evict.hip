@@ -337,14 +337,20 @@ __global__ __launch_bounds__(256) void evict_move_kernel(piece_t* __restrict__ K
 constexpr int kMostHeld = 16 * kEThreads;
 constexpr int kBins = 2048;       // of a digit
 constexpr int kSegments = 16;     // of a group at most, and one more for the cut at `keep`
+constexpr int64_t kAllSegments = 512;  // of all groups, about; every group has one and one more
 struct EvictCut {
   int seg, low, n;  // slots of a segment; segments of [0, keep); of the capacity
 };
 inline EvictCut evict_cut(int64_t groups, int64_t cap, int keep) {
-  const int64_t most = std::min<int64_t>(kSegments, std::max<int64_t>(1, 512 / groups - 1));
+  const int64_t most = std::min<int64_t>(kSegments, std::max<int64_t>(1, kAllSegments / groups - 1));
   const int64_t seg = std::max<int64_t>(4096, (cap + most - 1) / most + kEThreads - 1) / kEThreads * kEThreads;
   const int64_t low = (keep + seg - 1) / seg;
   return {int(seg), int(low), int(low + (cap - keep + seg - 1) / seg)};
+}
+// At least as many as evict_cut makes of so many groups or fewer, whatever the capacity and `keep`: a workspace of a
+// larger call serves a smaller one, whose groups may be cut into more.
+inline size_t evict_segments_room(size_t groups) {
+  return std::min<size_t>((kSegments + 1) * groups, std::max<size_t>(kAllSegments, 2 * groups));
 }
 struct EvictLong {
   EvictArgs g;
@@ -659,7 +665,7 @@ inline EvictBuffers carve_evict(size_t groups, int64_t cap, int keep, void* ws) 
   b.n_moves = c.take<int>(groups);
   if (cap > kMostHeld) {
     b.e.cut = evict_cut(int64_t(groups), cap, keep);
-    const size_t segments = groups * size_t(b.e.cut.n);
+    const size_t segments = evict_segments_room(groups);
     b.e.hist[0] = c.take<uint32_t>(segments * 2 * kBins);
     b.e.hist[1] = c.take<uint32_t>(segments * kBins);
     b.e.counted = c.take<uint32_t>(segments * 4);

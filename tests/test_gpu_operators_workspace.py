@@ -1,0 +1,39 @@
+"""Small calls of the loss, tree-attention and eviction operators on workspaces of larger ones, between guard bytes."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_15592_amd as estp
+from oracle import operators as OP
+from tests._util import dev, host
+from tests.test_gpu_cache_evict import _case
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 4096
+
+
+class Guarded:
+    """A workspace of n bytes between guard bytes, NaN in all of it."""
+
+    def __init__(self, n):
+        self.all = torch.full((n + 2 * GUARD,), 255, dtype=torch.uint8, device="cuda")
+        self.ws = self.all[GUARD:GUARD + n]
+
+    def check(self):
+        assert (self.all[:GUARD] == 255).all() and (self.all[GUARD + len(self.ws):] == 255).all()
+
+
+@pytest.mark.parametrize("groups,keep,larger", [(170, 2000, (171, 20000, 2000)), (2, 4095, (2, 20000, 4096)),
+                                                (2, 2000, (2, 20100, 2000)), (5, 300, (300, 18000, 300))])
+def test_eviction_on_a_larger_calls_workspace(groups, keep, larger):
+    cap = 20000 if groups != 5 else 17000
+    lens = np.random.default_rng(1).integers(keep, cap + 1, groups)
+    K, V, acc, pos, lens, seen = _case(groups, lens.tolist(), 1, 32, cap, "bf16")
+    g = Guarded(estp.load().estp_cache_evict_workspace_size(larger[0], 1, larger[1], larger[2]))
+    got_lens, got = estp.cache_evict(dev(K), dev(V), dev(acc), dev(pos), dev(lens), dev(seen), keep, 64, 4,
+                                     workspace=g.ws)
+    idx, new = OP.cache_evict(acc, pos, lens, seen, keep, 64, 4)
+    np.testing.assert_array_equal(host(got), idx)
+    np.testing.assert_array_equal(host(got_lens), new)
+    g.check()

@@ -1,0 +1,37 @@
+"""Workspaces of the loss, tree-attention and eviction calls: one that is sized for a program's largest call serves its
+smaller ones."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_15592_amd as estp
+
+FAKE = ctypes.c_void_p(1 << 20)
+OTHER = ctypes.c_void_p(1 << 21)
+WS = ctypes.c_void_p(1 << 24)
+
+
+def _never_less(size, values):
+    """size(x) over ascending x."""
+    sizes = np.array([size(x) for x in values])
+    assert (sizes > 0).all()
+    falls = np.flatnonzero(np.diff(sizes) < 0)
+    assert len(falls) == 0, [(values[i], sizes[i], values[i + 1], sizes[i + 1]) for i in falls[:3]]
+
+
+@pytest.mark.parametrize("cap", [4096, 16384, 16400, 20000, 65536, 131072, 1 << 20])
+def test_eviction_workspaces_grow_with_the_call(cap):
+    size = estp.load().estp_cache_evict_workspace_size
+    for keep in (1, 2048, cap):
+        _never_less(lambda b: size(b, 1, cap, min(keep, cap)), range(1, 700))
+        _never_less(lambda h: size(3, h, cap, min(keep, cap)), range(1, 200))
+    for groups in (1, 16, 30, 31, 170, 171, 256, 300):
+        _never_less(lambda k: size(groups, 1, cap, k), sorted({*range(1, cap + 1, cap // 300 + 1), 4095, 4096} & {*range(cap + 1)}))
+
+
+def test_eviction_workspaces_grow_with_the_capacity():
+    size = estp.load().estp_cache_evict_workspace_size
+    for groups in (1, 16, 170, 300):
+        _never_less(lambda c: size(groups, 1, c, 1024), [*range(1024, 20000, 61), *range(20000, 200000, 997)])
