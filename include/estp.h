@@ -342,7 +342,7 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL (lse can come from
  *                    other sums with them than without: its last bits then differ)
  * Other arguments and requirements are those of estp_token_entropy; V > 2^31 - 65537 returns
- * ESTP_ERR_UNSUPPORTED.
+ * ESTP_ERR_UNSUPPORTED.  A workspace of a call serves every call of no more tokens on the same W.
  *
  * estp_token_loss_backward: with grad_i the gradient of the objective with
  * respect to loss_i,

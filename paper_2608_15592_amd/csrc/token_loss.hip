@@ -990,6 +990,14 @@ LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
   p.states = p.slices * (f32 && p.tile < kFT ? 4 : 2);
   return p;
 }
+// At least the partial states of every call of n_tok tokens or fewer (plan_lse gives few tokens more slices): a workspace
+// of a larger call serves a smaller one.  slices n_tok is at most fill tile, or 4 n_tok, or n_vt n_tok.
+size_t lse_room(int64_t n_tok, int V, int dtype) {
+  const bool f32 = dtype == ESTP_F32;
+  const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows;
+  if (f32) return size_t(4 * std::min(n_vt * n_tok, std::max<int64_t>(4 * n_tok, 1024 * 64)));
+  return size_t(2 * std::min<int64_t>(n_vt * n_tok, 256 * 256));
+}
 // bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.  d 2048, V 128256, here against
 // there: 128 tokens 137 and 154 us, 1021 tokens 451 and 626, 2048 tokens 870 and 1220, 2500 tokens 1077 and 991, 4096
 // tokens 1735 and 1544.  (Its sums keep one order for any number of tokens, and it forms H and the mode too.)  fp32:
@@ -1000,9 +1008,9 @@ bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 20
 
 extern "C" size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   const size_t entropy = estp_token_entropy_workspace_size(n_tok, d, V, dtype);
-  if (entropy == 0 || !own_lse(n_tok, dtype)) return entropy;
+  if (entropy == 0) return 0;
   Carver c(nullptr);
-  for (int i = 0; i < 2; ++i) c.take<float>(size_t(plan_lse(n_tok, V, dtype).states) * size_t(n_tok));
+  for (int i = 0; i < 2; ++i) c.take<float>(lse_room(n_tok, V, dtype));
   return std::max(entropy, c.bytes());
 }
 

@@ -7,6 +7,7 @@ import paper_2608_15592_amd as estp
 from oracle import operators as OP
 from tests._util import dev, host
 from tests.test_gpu_cache_evict import _case
+from tests.test_gpu_token_loss import _inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -36,4 +37,16 @@ def test_eviction_on_a_larger_calls_workspace(groups, keep, larger):
     idx, new = OP.cache_evict(acc, pos, lens, seen, keep, 64, 4)
     np.testing.assert_array_equal(host(got), idx)
     np.testing.assert_array_equal(host(got_lens), new)
+    g.check()
+
+
+@pytest.mark.parametrize("dtype,n,larger", [("f32", 64, 65), ("f32", 65, 400), ("bf16", 128, 129), ("bf16", 385, 2049)])
+def test_loss_on_a_larger_calls_workspace(dtype, n, larger):
+    d, V = 32, 128256
+    X, W, t, _ = _inputs(n, n, d, V, dtype)
+    Xd, Wd, td = dev(X), dev(W), dev(t)
+    want = estp.token_loss(Xd, Wd, td)
+    g = Guarded(estp.load().estp_token_loss_workspace_size(larger, d, V, 0 if dtype == "bf16" else 1))
+    got = estp.token_loss(Xd, Wd, td, workspace=g.ws)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     g.check()

@@ -35,3 +35,13 @@ def test_eviction_workspaces_grow_with_the_capacity():
     size = estp.load().estp_cache_evict_workspace_size
     for groups in (1, 16, 170, 300):
         _never_less(lambda c: size(groups, 1, c, 1024), [*range(1024, 20000, 61), *range(20000, 200000, 997)])
+
+
+TOKENS = [*range(1, 2200), 2500, 4095, 4096, 4097, 8191, 8192, 8193, 16384, 16385, 65536, 100000, 1 << 20, 1 << 22]
+HEADS = [(2048, 128256), (4096, 128256), (1536, 151936), (1024, 16384), (96, 5000), (64, 1000), (32, 24449), (32, 1)]
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("d,V", HEADS)
+def test_loss_workspaces_grow_with_the_tokens(d, V, dtype):
+    _never_less(lambda n: estp.load().estp_token_loss_workspace_size(n, d, V, dtype), TOKENS)
