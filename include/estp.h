@@ -360,7 +360,7 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  * Bitwise repeatable.
  * n_tok > 4194304, d > 1048576, n_tok d > 2^36 or V as above returns ESTP_ERR_UNSUPPORTED.  The
  * workspace holds one piece of G (about 256 MiB, more past 8192 tokens of fp32 or 16384 of bf16), the live
- * rows of X and fp32 sums of dX.
+ * rows of X and fp32 sums of dX; that of a call serves every call of no more tokens on the same W.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
 ESTP_API int estp_token_loss(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,

@@ -866,6 +866,28 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   return p;
 }
 
+// Rows of G, its elements and the floats of dX's sums.
+struct LossRoom {
+  size_t rows, G, sums;
+};
+inline LossRoom loss_need(const LossPlan& p, int64_t n_tok, int d) {
+  const size_t rows = size_t(p.parts) * size_t(n_tok);
+  return {rows, rows * size_t(p.Vc), size_t(p.n_split) * rows * size_t(d)};
+}
+// At least what every call of n_tok tokens or fewer needs, which can be more than this one: parts, pieces and shares
+// follow the token count in steps.  A workspace of a larger call so serves a smaller one.
+inline LossRoom loss_room(int64_t n_tok, int d, int V, int dtype) {
+  const size_t n = size_t(n_tok), es = dtype == ESTP_F32 ? 4 : 2, v_pad = (size_t(V) + 255) / 256 * 256;
+  LossRoom r;
+  r.rows = dtype == ESTP_F32 ? n : n <= 64 ? 2 * n : std::max<size_t>(n, 2 * 64);
+  // a piece is all of the vocabulary, or 256 MiB of G, or 8192 rows
+  r.G = std::min(r.rows * v_pad, std::max((size_t(256) << 20) / es, 8192 * r.rows));
+  // t tiles of tokens have at most wide / t shares, and of at least 64 rows each
+  const size_t wide = std::max<size_t>(1, 256 / ((size_t(d) + 255) / 256)), tile = dtype == ESTP_F32 ? kFT : 256;
+  r.sums = std::max(r.rows, std::min(r.rows * std::min(wide, v_pad / 64), tile * wide)) * size_t(d);
+  return r;
+}
+
 struct LossBuffers {
   int *row, *slot, *n_live;
   int32_t* tc;
@@ -875,20 +897,19 @@ struct LossBuffers {
   size_t bytes;
 };
 
-inline LossBuffers carve_loss(const LossPlan& p, int64_t n_tok, int d, int dtype, void* ws) {
+inline LossBuffers carve_loss(const LossRoom& r, int64_t n_tok, int d, int dtype, void* ws) {
   const size_t es = dtype == ESTP_F32 ? 4 : 2;
   Carver c(ws);
   LossBuffers b;
   b.row = c.take<int>(size_t(n_tok));
   b.slot = c.take<int>(size_t(n_tok));
   b.n_live = c.take<int>(2);
-  const size_t n_rows = size_t(p.parts) * size_t(n_tok);
-  b.tc = c.take<int32_t>(n_rows);
-  b.lc = c.take<float>(n_rows);
-  b.gc = c.take<float>(n_rows);
-  b.Xc = c.take<char>(n_rows * d * es);
-  b.G = c.take<char>(n_rows * p.Vc * es);
-  b.room = size_t(p.n_split) * n_rows * d;
+  b.tc = c.take<int32_t>(r.rows);
+  b.lc = c.take<float>(r.rows);
+  b.gc = c.take<float>(r.rows);
+  b.Xc = c.take<char>(r.rows * d * es);
+  b.G = c.take<char>(r.G * es);
+  b.room = r.sums;
   b.acc = c.take<float>(b.room);
   b.bytes = c.bytes();
   return b;
@@ -898,7 +919,7 @@ template <typename T>
 int launch_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
                          int n, int d, int V, int dtype, void* dX, void* dW, void* workspace, hipStream_t s) {
   const LossPlan p = plan_loss(n, d, V, dtype);
-  const LossBuffers b = carve_loss(p, n, d, dtype, workspace);
+  const LossBuffers b = carve_loss(loss_need(p, n, d), n, d, dtype, workspace);
   constexpr int kWgs = 256;  // of the persistent kernels: one on each compute unit
   const T *Wt = static_cast<const T*>(W), *Xc = reinterpret_cast<const T*>(b.Xc);
   T* G = reinterpret_cast<T*>(b.G);
@@ -1082,7 +1103,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
 
 extern "C" size_t estp_token_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1) return 0;
-  return carve_loss(plan_loss(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
+  return carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
 }
 
 extern "C" int estp_token_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse,

@@ -50,3 +50,18 @@ def test_loss_on_a_larger_calls_workspace(dtype, n, larger):
     got = estp.token_loss(Xd, Wd, td, workspace=g.ws)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     g.check()
+
+
+@pytest.mark.parametrize("dtype,n,larger", [("bf16", 64, 65), ("bf16", 256, 257), ("bf16", 1024, 1025), ("f32", 32, 33),
+                                            ("f32", 128, 129), ("f32", 512, 513), ("bf16", 64, 64), ("f32", 200, 200),
+                                            ("bf16", 1, 4096)])
+@pytest.mark.parametrize("d,V", [(32, 128256), (288, 3000)])
+def test_gradient_on_a_larger_calls_workspace(dtype, n, larger, d, V):
+    X, W, t, g = _inputs(n, n, d, V, dtype, ignored=0.1)
+    Xd, Wd, td, gd = dev(X), dev(W), dev(t), dev(g)
+    lse = estp.token_loss(Xd, Wd, td)[1]
+    want = estp.token_loss_backward(Xd, Wd, td, lse, gd)
+    ws = Guarded(estp.load().estp_token_loss_backward_workspace_size(larger, d, V, 0 if dtype == "bf16" else 1))
+    got = estp.token_loss_backward(Xd, Wd, td, lse, gd, workspace=ws.ws)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    ws.check()

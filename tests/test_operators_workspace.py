@@ -45,3 +45,9 @@ HEADS = [(2048, 128256), (4096, 128256), (1536, 151936), (1024, 16384), (96, 500
 @pytest.mark.parametrize("d,V", HEADS)
 def test_loss_workspaces_grow_with_the_tokens(d, V, dtype):
     _never_less(lambda n: estp.load().estp_token_loss_workspace_size(n, d, V, dtype), TOKENS)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("d,V", HEADS)
+def test_gradient_workspaces_grow_with_the_tokens(d, V, dtype):
+    _never_less(lambda n: estp.load().estp_token_loss_backward_workspace_size(n, d, V, dtype), TOKENS)
