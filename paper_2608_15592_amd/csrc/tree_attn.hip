@@ -42,6 +42,7 @@ struct TreeShape {
   int G;                  // Hq / Hkv, at most 32768
   uint32_t over_G;        // ceil(2^31 / G)
   __device__ __forceinline__ int item_rows() const { return 1 << item_shift; }
+  __device__ __forceinline__ int most_rows() const { return max_q * G; }  // of a (sequence, KV head)
   // r / G for a row number (below 65536): r (G over_G - 2^31) stays below 2^31
   __device__ __forceinline__ int token(int r) const { return int(__umulhi(uint32_t(2 * r), over_G)); }
 };
@@ -364,7 +365,7 @@ __global__ __launch_bounds__(64 * kW, 2) void tree_attn_kernel(
       for (int e = 0; e < 4 * kB; ++e) mx = fmaxf(mx, s[e / 4][e % 4]);
       mx *= c2;
       if (kScores && r < R) {
-        float* w = scores + (size_t(bg) * 16 + fr) * pitch + k + 4 * fq;
+        float* w = scores + (size_t(bg) * sh.most_rows() + fr) * pitch + k + 4 * fq;
 #pragma unroll
         for (int a = 0; a < kB; ++a) *reinterpret_cast<f32x4_t*>(w + 16 * a) = s[a] * c2;
       }
@@ -689,7 +690,7 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
   if (int(k0) >= keys || R == 0) return;
   const TreeParts parts = tree_parts(sh, t, j, off, share, g, 0);
   const int k = int(k0) + 4 * int(threadIdx.x);
-  const float* s = scores + size_t(bg) * 16 * pitch + k;
+  const float* s = scores + size_t(bg) * sh.most_rows() * pitch + k;
   f32x4_t first{0.f, 0.f, 0.f, 0.f};  // the first row's, on their way
   if (k < keys) first = *reinterpret_cast<const f32x4_t*>(s);
   for (int r = wave; r < R; r += kThreads / 64) {
@@ -890,7 +891,8 @@ struct TreeBuffers {
   int pitch;
   size_t bytes;
 };
-inline TreeBuffers carve_tree(const TreePlan& p, int B, int64_t n_q, int Hq, int Hkv, int max_kv, int dh, void* ws) {
+inline TreeBuffers carve_tree(const TreePlan& p, int B, int max_q, int64_t n_q, int Hq, int Hkv, int max_kv, int dh,
+                              void* ws) {
   // a segment more than the last for every workgroup and for every item
   const size_t rows = (size_t(p.wgs) + size_t(B) * Hkv * p.items) << p.item_shift;
   Carver c(ws);
@@ -900,7 +902,7 @@ inline TreeBuffers carve_tree(const TreePlan& p, int B, int64_t n_q, int Hq, int
   t.o = c.take<float>(rows * dh);
   t.lse = c.take<float>(size_t(n_q) * Hq);
   t.pitch = (max_kv + 31) / 32 * 32;
-  t.scores = c.take<float>(p.stored ? size_t(B) * Hkv * 16 * t.pitch : 0);
+  t.scores = c.take<float>(p.stored ? size_t(B) * max_q * Hq * t.pitch : 0);
   t.bytes = c.bytes();
   return t;
 }
@@ -1030,7 +1032,8 @@ extern "C" size_t estp_tree_attention_workspace_size(int32_t B, int32_t max_q, i
   if (B < 1 || max_q < 1 || n_q < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_kv < 1 || dh < 1 ||
       max_kv > INT32_MAX - 256)
     return 0;
-  return carve_tree(plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype), B, n_q, Hq, Hkv, max_kv, dh, nullptr).bytes;
+  return carve_tree(plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype), B, max_q, n_q, Hq, Hkv, max_kv, dh, nullptr)
+      .bytes;
 }
 
 extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, const int32_t* lens,
@@ -1055,7 +1058,7 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
                    int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 15) / 16 + 4) <= INT32_MAX,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);
   const TreeShape sh = tree_shape(B, max_q, n_q, Hq, Hkv, cap, max_kv, p.item_shift, p.items);
-  const TreeBuffers t = carve_tree(p, B, n_q, Hq, Hkv, max_kv, dh, workspace);
+  const TreeBuffers t = carve_tree(p, B, max_q, n_q, Hq, Hkv, max_kv, dh, workspace);
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int checked = debug_check_tree(fn, lens, cu_q, B, max_q, n_q, max_kv, s);
   if (checked != ESTP_OK) return checked;

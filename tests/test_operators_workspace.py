@@ -51,3 +51,12 @@ def test_loss_workspaces_grow_with_the_tokens(d, V, dtype):
 @pytest.mark.parametrize("d,V", HEADS)
 def test_gradient_workspaces_grow_with_the_tokens(d, V, dtype):
     _never_less(lambda n: estp.load().estp_token_loss_backward_workspace_size(n, d, V, dtype), TOKENS)
+
+
+@pytest.mark.parametrize("B,max_q,Hq,Hkv,max_kv,dh", [(32, 1, 32, 8, 32768, 128), (8, 1, 32, 8, 131072, 128),
+                                                      (8, 4, 32, 8, 131072, 128), (1, 16, 8, 8, 100_003, 128)])
+def test_kept_scores_take_the_room_of_the_rows_there_are(B, max_q, Hq, Hkv, max_kv, dh):
+    # fp32 scores of every row; besides them 25 MB at most: the partial results of 1024 + B Hkv segments of 16 rows
+    size = estp.load().estp_tree_attention_workspace_size(B, max_q, B * max_q, Hq, Hkv, max_kv, dh, 0)
+    scores = 4 * B * max_q * Hq * (-(-max_kv // 32) * 32)
+    assert scores < size < scores + 25e6
