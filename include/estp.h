@@ -406,6 +406,13 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  * and sums are fp32; for ESTP_BF16 the matrix cores multiply the weights by V
  * in two bf16 parts, so that O is rounded once.  Bitwise repeatable.
  *
+ * Workspace: where the rows of a KV head are few, the size returned has room for
+ * their scores, 4 B max_q Hq max_kv bytes, which the account then reads.  So it
+ * does not grow with max_q throughout; but a workspace of a call serves every
+ * call with no larger B, max_q, n_q and max_kv on the same heads: one without
+ * room for the scores is taken too, and they are formed again (the account's
+ * last bits can then differ).  Without acc they are never kept.
+ *
  * estp_tree_importance: the account alone, from the rows' normalisers, with a
  * weight for each row: 1 for the drafted rows that were accepted, 0 for the
  * others (then call estp_tree_attention with acc = NULL).

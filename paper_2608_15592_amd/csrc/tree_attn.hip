@@ -859,7 +859,7 @@ __global__ __launch_bounds__(256, tree_weight_wgs(DH * int(sizeof(T)))) void tre
 struct TreePlan {
   int waves;  // of a workgroup
   int item_shift, items, wgs;
-  bool stored;  // the scores are kept for the account
+  bool stored;  // the scores are kept for the account, if there is one and the workspace holds them
 };
 // Waves that share a ring: as many as have a transfer of each part (two at a head size of 32).
 constexpr int tree_waves(int dh) { return dh == 32 ? 2 : 4; }
@@ -1048,12 +1048,16 @@ extern "C" int estp_tree_attention(const void* Q, const void* K, const void* V, 
   ESTP_REQUIRE(V && O, ESTP_ERR_INVALID_ARG, "%s: V and O must be non-null", fn);
   ESTP_REQUIRE(aligned(V, 16) && aligned(O, 16) && aligned(tree_mask, 8) && aligned(lse, 4) && aligned(acc, 4),
                ESTP_ERR_INVALID_ARG, "%s: V and O must be 16-byte, tree_mask 8-byte, lse and acc 4-byte aligned", fn);
-  const size_t need = estp_tree_attention_workspace_size(B, max_q, n_q, Hq, Hkv, max_kv, dh, dtype);
+  // A workspace without room for the scores serves too, as that of a larger max_q, whose scores are formed again: they
+  // are formed again here, too.
+  TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
+  p.stored = p.stored && acc &&
+             workspace_bytes >= estp_tree_attention_workspace_size(B, max_q, n_q, Hq, Hkv, max_kv, dh, dtype);
+  const size_t need = carve_tree(p, B, max_q, n_q, Hq, Hkv, max_kv, dh, nullptr).bytes;
   ESTP_REQUIRE(workspace_bytes >= need, ESTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn,
                workspace_bytes, need);
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
-  const TreePlan p = plan_tree(B, max_q, max_kv, Hq, Hkv, dh, dtype);
   ESTP_REQUIRE(fits_launch(2 * size_t(n_q) * Hq, 1024) &&
                    int64_t(B) * Hkv * p.items * ((int64_t(max_kv) + 15) / 16 + 4) <= INT32_MAX,
                ESTP_ERR_UNSUPPORTED, "%s: B Hkv max_kv max_q Hq too large", fn);

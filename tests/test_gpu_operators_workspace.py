@@ -8,6 +8,7 @@ from oracle import operators as OP
 from tests._util import dev, host
 from tests.test_gpu_cache_evict import _case
 from tests.test_gpu_token_loss import _inputs
+from tests.test_gpu_tree_attention import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,26 @@ def test_gradient_on_a_larger_calls_workspace(dtype, n, larger, d, V):
     got = estp.token_loss_backward(Xd, Wd, td, lse, gd, workspace=ws.ws)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     ws.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("larger", [1, 2, 9, 64])
+def test_a_decode_step_on_a_larger_trees_workspace(dtype, dh, larger):
+    # 2 heads on a KV head: one token's scores are kept, a tree's are not
+    c = Case(41, [3000, 700, 0], [1, 1, 1], 8, 4, dh, dtype, cap=3100)
+    size = lambda q: estp.load().estp_tree_attention_workspace_size(3, q, 3 * q, 8, 4, 3001, dh,  # noqa: E731
+                                                                    0 if dtype == "bf16" else 1)
+    g, acc = Guarded(size(larger)), dev(c.acc)
+    O, lse = c.attend(acc=acc, workspace=g.ws)
+    g.check()
+    c.check(O, lse, acc)
+    g = Guarded(size(larger))
+    O2, lse2 = c.attend(workspace=g.ws)  # without the account
+    g.check()
+    assert torch.equal(O, O2) and torch.equal(lse, lse2)
+    first = dev(c.acc)
+    want = c.attend(acc=first)
+    assert torch.equal(O, want[0]) and torch.equal(lse, want[1])
+    if larger <= 2:  # room for the scores: the same account, bit for bit
+        assert torch.equal(acc, first)

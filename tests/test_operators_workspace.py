@@ -60,3 +60,41 @@ def test_kept_scores_take_the_room_of_the_rows_there_are(B, max_q, Hq, Hkv, max_
     size = estp.load().estp_tree_attention_workspace_size(B, max_q, B * max_q, Hq, Hkv, max_kv, dh, 0)
     scores = 4 * B * max_q * Hq * (-(-max_kv // 32) * 32)
     assert scores < size < scores + 25e6
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="fake pointers")
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("dh", [32, 64, 128])
+@pytest.mark.parametrize("G", [1, 4, 6])
+@pytest.mark.parametrize("acc", [FAKE, None])
+def test_a_tree_workspace_serves_every_smaller_call(dh, G, dtype, acc):
+    lib = estp.load()
+
+    def size(B, max_q, max_kv):
+        return lib.estp_tree_attention_workspace_size(B, max_q, B * max_q, 8 * G, 8, max_kv, dh, dtype)
+
+    def taken(wsb, B, max_q, max_kv):  # whatever follows the checks fails without a GPU
+        status = lib.estp_tree_attention(FAKE, FAKE, OTHER, FAKE, FAKE, None, B, max_q, B * max_q, 8 * G, 8, 1 << 18,
+                                         max_kv, dh, 0.125, dtype, FAKE, FAKE, acc, WS, wsb, None)
+        assert status in (3, 4)
+        return status != 3
+
+    largest = [(B, q, kv) for B in (1, 8, 40) for q in (1, 2, 3, 5, 9, 16, 17, 40, 64) for kv in (70, 5000, 131072)]
+    for call in largest:
+        for larger in largest:
+            if all(a <= b for a, b in zip(call, larger)):
+                assert taken(size(*larger), *call), (call, larger)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="fake pointers")
+def test_scores_are_asked_for_where_they_are_kept():
+    # without the account, or of a call that keeps no scores, the least a call takes is the partial results
+    lib = estp.load()
+    full = lib.estp_tree_attention_workspace_size(8, 1, 8, 32, 8, 131072, 128, 0)
+    wide = lib.estp_tree_attention_workspace_size(8, 16, 128, 32, 8, 131072, 128, 0)
+    assert wide < full // 4
+    for acc in (FAKE, None):
+        for wsb, ok in ((full, True), (wide, True), (full - 1, True), (4096, False)):
+            status = lib.estp_tree_attention(FAKE, FAKE, OTHER, FAKE, FAKE, None, 8, 1, 8, 32, 8, 131072, 131072, 128,
+                                             0.125, 0, FAKE, FAKE, acc, WS, wsb, None)
+            assert status == (4 if ok else 3)
