@@ -339,8 +339,10 @@ ESTP_API int estp_head_train_step(const float* pooled, const float* y, int32_t B
  *   loss [n_tok]     float32 output, at least 0
  *   lse  [n_tok]     float32 output, natural log, of every token (ignored ones too):
  *                    what estp_token_loss_backward takes
- *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL (lse can come from
- *                    other sums with them than without: its last bits then differ)
+ *   H [n_tok], vocab_argmax [n_tok]  outputs as estp_token_entropy's, or NULL
+ * The last bits of lse and loss are those of the kernels that a call runs, which follow n_tok, V
+ * and whether H or vocab_argmax are asked for: the same token can differ by a rounding
+ * between calls that differ in these.  (H and vocab_argmax are bitwise estp_token_entropy's.)
  * Other arguments and requirements are those of estp_token_entropy; V > 2^31 - 65537 returns
  * ESTP_ERR_UNSUPPORTED.  A workspace of a call serves every call of no more tokens on the same W.
  *
@@ -387,9 +389,14 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  *
  * A row that sees nothing has O = 0 and lse = -inf and adds nothing.  A
  * drafted token that a row does not see does not enter it, whatever its K and
- * V hold.  The account acc keeps growing over calls: the decode-time
- * counterpart of estp_attn_importance, whose N_b S_j (Hq / Hkv) is a prompt's
- * starting account for each KV head, and what estp_cache_evict evicts by.
+ * V hold.  A non-finite V in a slot that a row sees makes that column of its O
+ * infinite or NaN.  The account acc keeps growing over calls: the decode-time
+ * counterpart of estp_attn_importance, and what estp_cache_evict evicts by.
+ * One layer's N_b S_j (Hq / Hkv) can start a prompt's account; S averages over all
+ * heads, so it is the same for every KV head, and an eviction right after the
+ * prefill keeps the same slots in all of them.  For accounts of each head's own,
+ * call estp_attn_importance for one KV head at a time (Hq / Hkv query heads, one
+ * KV head).
  *
  *   Q  [n_q, Hq, dh]        rows of all sequences, packed (dtype), 16-byte aligned
  *   K, V [B, Hkv, cap, dh]  (dtype), 16-byte aligned
