@@ -17,8 +17,9 @@
 // few, else in evict_move_kernel.  Everything is exact: whole numbers and copies.
 //
 // 6 groups of 1029 slots cut to 1024: 8.7 us.  256 groups of 700 to 4096 slots cut to 1024, heads of 128: selection
-// 11.2 us, then 22 us for the rows, 100 MB read and written at 4.5 TB/s.  64 groups of 16384 slots: selection 35 us,
-// bound by the vector instructions of a group's one compute unit.
+// 11.5 us, then 22 us for the rows, 100 MB read and written at 4.5 TB/s.  64 groups of 16384 slots: selection 35 us on a
+// compute unit a group, where vector instructions are in flight some two fifths of the cycles and waves wait 54 % of
+// theirs, for barriers and LDS.
 #include <algorithm>
 #include <vector>
 

@@ -19,7 +19,7 @@
 //
 // Few tokens are bounded by one pass over W for each product, many by the matrix cores: 2 n V d operations for the
 // logits of the forward, and three times as many for the backward, which forms them again instead of keeping n V of
-// them.  4096 tokens, d 4096, V 128256: 13.0 ms, 1.33 PFLOP/s over all of it (a library product of these logits alone
+// them.  4096 tokens, d 4096, V 128256: 13.1 ms, 1.31 PFLOP/s over all of it (a library product of these logits alone
 // runs at 1.48).
 #include <algorithm>
 
@@ -540,11 +540,9 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
 // Stores of 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
-constexpr int kNonTemporal = 2;  // the cache policy of data that is not read again soon
 template <int kAux = 0>
 __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
   __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, kAux);
 #endif
 }
@@ -768,10 +766,12 @@ __global__ __launch_bounds__(256, 1) void loss_dx_mfma_kernel(const __bf16* __re
 // 11 stages a tile, its first stage and its stores are a good part (443 us, 0.81 PFLOP/s).
 //
 // kStream: dW of few tokens is bound by its stores, and one that the last cache does not hold drives W out of it, which
-// the other products of the step read.  It is stored with the non-temporal policy: loss and gradient of 8, 64 and 128
-// tokens at d 2048, V 128256 take 493, 578 and 589 us so against 539, 592 and 603, of 16 at d 4096 894 against 958.
-// With more tokens the stores are spread over the products (256: 736 against 720, 512: 1086 against 1072), and a dW
-// that the cache holds is read from there by whoever uses it (16 at d 1024, V 32000: 106 against 101).
+// the next loss of the same W reads first.  It is stored with the non-temporal policy: loss and gradient of 8, 64 and 128
+// tokens at d 2048, V 128256, over and over, take 495, 581 and 586 us so against 538, 595 and 599, of 16 at d 4096 891
+// against 955; with an update of W from dW after each 785, 870 and 867 against 807, 869 and 868, and 1440 against 1484.
+// (The kernel itself is slower so: 211 us of 128 tokens against 178, and 700 MB leave L2 for a dW of 525.)  With more
+// tokens the stores are spread over the products (256: 736 against 720, 512: 1086 against 1072), and a dW that the cache
+// holds is read from there by whoever uses it (16 at d 1024, V 32000: 106 against 101).
 template <bool kStream>
 __global__ __launch_bounds__(256, 1) void loss_dw_mfma_kernel(const __bf16* __restrict__ G,
                                                               const __bf16* __restrict__ Xc,
@@ -830,15 +830,16 @@ struct LossPlan {
 // backward in us, 128 against 256: 64 tokens 135 and 451, 163 and 497; 200 tokens 148 and 569, 154 and 582; 384
 // tokens 203 and 725, 234 and 771; 512 tokens 260 and 889, 242 and 838; 1021 tokens 490 and 1581, 455 and 1438.
 inline int bf16_tile_toks(int64_t n_tok) { return n_tok <= 384 ? 128 : 256; }
-// Tokens of a fp32 tile: the narrowest that takes them all, up to 128.  d 2048, V 128256, forward and backward in us:
-// 16 tokens 253 and 771 with 32, 379 and 941 with 64, 518 and 1322 with 128; 50 tokens 360 and 1072 with 64, 504 and
-// 1434 with 128; 100 tokens 508 and 1676 with 128, 738 and 1780 with 64.
 // The rule of loss_dw_mfma_kernel's kStream.
 inline bool stream_dw(int64_t n_tok, int d, int V) {
   constexpr size_t kLastCache = size_t(256) << 20;  // bytes
   return n_tok <= 128 && size_t(V) * d * 2 > kLastCache;
 }
 
+// Tokens of a fp32 tile: the narrowest that takes them all, up to 128.  d 2048, V 128256, forward and backward in us:
+// 16 tokens 253 and 771 with 32, 379 and 941 with 64, 518 and 1322 with 128; 50 tokens 360 and 1072 with 64, 504 and
+// 1434 with 128; 100 tokens 508 and 1676 with 128, 738 and 1780 with 64.
+//
 // Where 128-wide tiles are fewer than kFewTiles, which leaves compute units idle, 32-wide ones share the work out (of
 // dW, whose columns are vocabulary rows, by its own tiles).  Forward and backward in us with 32 against 128: 128
 // tokens, d 64, V 1000 (8 tiles) 11.7 and 24.6, 11.9 and 38.5; 128 tokens, d 1024, V 16384 (128) 49 and 144, 75 and

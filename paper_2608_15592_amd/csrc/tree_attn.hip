@@ -20,8 +20,9 @@
 // normalisers, so it comes last: from scores that the first kernel kept where the rows are few (in the launch of the
 // join), else from scores formed again.  No atomics: bitwise reproducible.
 //
-// The cache is read once; that bounds calls of few rows (a copy moves 4.9 TB/s on this card).  Calls of many rows spend
-// their time on the exponentials and what goes with them, each score twice.
+// The cache is read once; that bounds calls of few rows (4.4 to 4.9 TB/s by the counters; a copy moves 4.9 on this card).
+// Calls of many rows spend their time on the exponentials and what goes with them, each score twice (256 rows of 64, 8
+// sequences of 8000, bf16: vector instructions in flight 55 % of the attention's cycles, matrix ones 28 %).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -717,10 +718,11 @@ __global__ __launch_bounds__(tree_join_threads(kWaves)) void tree_finish_kernel(
 // 128 at a time, with their weights, normalisers and masks; a workgroup's share of 32-key tiles goes to its four
 // waves in turn, a tile's K in registers (the next tile's under way) while the rows pass, 16 at a time.  A product's
 // columns are rows: their sums join at the end of a tile, each exchange halving the values a lane still holds.  Every
-// score costs an exponential and two FMAs, which bound it (16 rows and 32 keys: 300 cycles of a SIMD) after some 6 us
-// until the first tile is done: 31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 14.6 us;
-// 23 tokens, heads of 128, 16 of 700 to 6000, a part of the rows accepted: 19.2 us, 4.8 TB/s.  fp32, the first at 8
-// of 4500: 64 us.
+// score costs an exponential and two FMAs (16 rows and 32 keys: 300 cycles of a SIMD); vector instructions are in flight
+// 40 to 46 % of the cycles of long calls, and waits for K and LDS are the rest.  Short calls are bound by their ends, some
+// 6 us until the first tile is done: 31 drafted tokens, 4 heads of 64 on a KV head, 8 sequences of 900 to 8100: 14.5 us
+// (28 %); 23 tokens, heads of 128, 16 of 700 to 6000, a part of the rows accepted: 19.4 us, 4.6 TB/s.  fp32, the first at
+// 8 of 4500: 64 us.
 constexpr int kWRows = 128;  // rows in LDS
 constexpr int kWKeys = 32;   // keys of a tile
 // Workgroups of a compute unit: what its registers hold.
