@@ -828,7 +828,10 @@ struct LossPlan {
 
 // Tokens of a bf16 tile: 256 read LDS less often, 128 leave fewer columns empty.  d 2048, V 128256, forward and
 // backward in us, 128 against 256: 64 tokens 135 and 451, 163 and 497; 200 tokens 148 and 569, 154 and 582; 384
-// tokens 203 and 725, 234 and 771; 512 tokens 260 and 889, 242 and 838; 1021 tokens 490 and 1581, 455 and 1438.
+// tokens 203 and 725, 234 and 771; 512 tokens 260 and 889, 242 and 838; 1021 tokens 490 and 1581, 455 and 1438.  The
+// sides change at 384 tokens, three tiles of 128, at other shapes too: 384 and 385 tokens, d 4096, V 128256, 387 and
+// 1350, 419 and 1420, then 463 and 1548, 420 and 1454; d 1536, V 151936, 186 and 649, 210 and 676, then 225 and 750, 210
+// and 695.
 inline int bf16_tile_toks(int64_t n_tok) { return n_tok <= 384 ? 128 : 256; }
 // The rule of loss_dw_mfma_kernel's kStream.
 inline bool stream_dw(int64_t n_tok, int d, int V) {
@@ -1022,7 +1025,8 @@ size_t lse_room(int64_t n_tok, int V, int dtype) {
 }
 // bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.  d 2048, V 128256, here against
 // there: 128 tokens 137 and 154 us, 1021 tokens 451 and 626, 2048 tokens 870 and 1220, 2500 tokens 1077 and 991, 4096
-// tokens 1735 and 1544.  (Its sums keep one order for any number of tokens, and it forms H and the mode too.)  fp32:
+// tokens 1735 and 1544; d 4096 2048 tokens 1568 and 2304, 2304 tokens 1767 and 1629; d 1536, V 151936, 782 and 1149, 888
+// and 802.  (Its sums keep one order for any number of tokens, and it forms H and the mode too.)  fp32:
 // the entropy kernel runs on the vector units.
 bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 2048; }
 
