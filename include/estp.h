@@ -79,8 +79,8 @@ typedef enum estp_act { ESTP_ACT_RELU = 0, ESTP_ACT_GELU_TANH = 1 } estp_act;
  * ESTP_VERSION; a library whose estp_version() differs has other signatures.
  * 0.2.0 added the vocab_argmax argument of estp_token_entropy; 0.3.0 the calls
  * estp_token_loss(_backward), estp_tree_attention, estp_tree_importance and
- * estp_cache_evict. */
-#define ESTP_VERSION 300
+ * estp_cache_evict; 0.4.0 estp_token_logprobs and estp_distill_loss(_backward). */
+#define ESTP_VERSION 400
 ESTP_API int estp_version(void);
 
 /* Static text for a status code. */
@@ -372,6 +372,86 @@ ESTP_API size_t estp_token_loss_backward_workspace_size(int64_t n_tok, int32_t d
 ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse,
                              const float* grad, int64_t n_tok, int32_t d, int32_t V, int dtype, void* dX, void* dW,
                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Log-probabilities of given tokens, with entropy and top alternatives.
+ *
+ *   z_i = W x_i,  s_i = z_i / temperature,  lse_i = log sum_v exp s_i[v]
+ *   logprob_i = s_i[t_i] - lse_i,  H_i = lse_i - sum_v exp(s_i[v] - lse_i) s_i[v]
+ *   top_id_i: the k tokens of the largest z_i[v], descending, the lowest index first among equals
+ *   top_logprob_ij = s_i[top_id_ij] - lse_i
+ *
+ * What a server returns beside its tokens, and what a teacher leaves for
+ * estp_distill_loss (its temperature here, its top_id and top_logprob there).
+ * The logits of up to 8192 tokens at a time are kept for a piece of the
+ * vocabulary at most.
+ *
+ *   targets [n_tok]  int32, or NULL (then logprob is NULL too); a token whose target is outside
+ *                    [0, V) (-100, say) is ignored: its logprob is 0
+ *   k                alternatives, 0 to 128, at most V
+ *   temperature      in [0.001, 1000]
+ *   logprob [n_tok]  float32 output, nats; a target among the alternatives has their value, bit for bit
+ *   lse [n_tok], H [n_tok]  float32 outputs, natural log and nats, or NULL: of every token, ignored ones too
+ *   top_id [n_tok, k], top_logprob [n_tok, k]  int32 and float32 outputs; not used where k = 0
+ * The order is that of the logits as computed here (fp32 accumulation); a NaN ranks below all
+ * others.  Rows with a NaN logit have NaN values; their top_id are indices in [0, V) all the same.
+ * X, W, d and dtype are those of estp_token_entropy.  V > 2^24 returns ESTP_ERR_UNSUPPORTED.
+ * Bitwise repeatable.  A workspace of a call serves every call of no more tokens and no larger k
+ * on the same W.
+ * ------------------------------------------------------------------------ */
+ESTP_API size_t estp_token_logprobs_workspace_size(int64_t n_tok, int32_t d, int32_t V, int32_t k, int dtype);
+ESTP_API int estp_token_logprobs(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,
+                        int32_t k, float temperature, int dtype, float* logprob, float* lse, float* H,
+                        int32_t* top_id, float* top_logprob, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Distillation from a teacher's top tokens, and its gradient.
+ *
+ *   s_i = W x_i / temperature,  lse_i = log sum_v exp s_i[v],  logq_ik = s_i[id_ik] - lse_i
+ *   p_ik = exp(logp_ik), or with renormalise exp(logp_ik) / sum_k' exp(logp_ik')
+ *   loss_i = sum_k p_ik (log p_ik - logq_ik)
+ *
+ * the divergence of the student's distribution over the whole vocabulary from
+ * the teacher's over K tokens.  The logits never reach memory.
+ *
+ *   ids [n_tok, K]   int32 tokens, in any order; an entry outside [0, V) is not held and its logp not
+ *                    used.  Entries that name the same token count each for themselves
+ *   logp [n_tok, K]  float32 natural log-probabilities of the teacher's distribution at this temperature,
+ *                    as estp_token_logprobs returns them; with renormalise any constant may be added to a
+ *                    row (logits over the temperature, say).  -inf: no weight
+ *   K                1 to 128;  temperature in [0.001, 1000], of the student's logits alone
+ *   renormalise      0: the rest of the teacher's mass is left out (the loss can then be below 0); not 0:
+ *                    the held tokens take it, in proportion
+ *   loss [n_tok]     float32 output
+ *   lse  [n_tok]     float32 output, natural log, of every token
+ *   logq [n_tok, K]  float32 output, the student's log-probabilities; 0 of entries that are not held
+ * A row without an entry of weight (a prompt's, say) is ignored: its loss is 0.  X, W, d, dtype and V
+ * are those of estp_token_loss; n_tok > 4194304 returns ESTP_ERR_UNSUPPORTED.  A workspace of a call
+ * serves every call of no more tokens on the same W.  The last bits of the outputs are those of the
+ * kernels that a call runs, which follow n_tok and V.
+ *
+ * estp_distill_loss_backward: with grad_i the gradient of the objective with
+ * respect to loss_i (temperature^2 / n, say),
+ *
+ *   G_iv = grad_i / temperature (P_i exp(s_i[v] - lse_i) - sum_{k: id_ik = v} p_ik),  P_i = sum_k p_ik
+ *   dX = G W,  dW = G^T X
+ *
+ *   lse, logq        of estp_distill_loss on the same X, W, ids, logp, temperature and renormalise
+ *   grad [n_tok]     float32, or NULL (all 1)
+ *   dX, dW           as estp_token_loss_backward's, rows of ignored tokens of dX 0
+ * Rows of X, lse, logq and grad of ignored tokens are not used (they may hold anything).  G, its
+ * roundings, the sums, the sizes that are refused and the workspace are estp_token_loss_backward's.
+ * Bitwise repeatable.
+ * ------------------------------------------------------------------------ */
+ESTP_API size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
+ESTP_API int estp_distill_loss(const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok, int32_t d,
+                      int32_t V, int32_t K, float temperature, int renormalise, int dtype, float* loss, float* lse,
+                      float* logq, void* workspace, size_t workspace_bytes, void* stream);
+ESTP_API size_t estp_distill_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);
+ESTP_API int estp_distill_loss_backward(const void* X, const void* W, const int32_t* ids, const float* logp,
+                               const float* lse, const float* logq, const float* grad, int64_t n_tok, int32_t d,
+                               int32_t V, int32_t K, float temperature, int renormalise, int dtype, void* dX,
+                               void* dW, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
  * Attention of drafted tokens over a cache, with the weight each cached token

@@ -13,6 +13,8 @@ Python face of libestp.so: the four calls of the ESTP path (arXiv 2608.15592)
 * ``head_train_step`` - one Eq. 6-8 / AdamW training step of the K-bin head
 * ``token_loss``, ``token_loss_backward`` - LM-head cross entropy of given next tokens and its gradients,
   without the logits
+* ``token_logprobs``  - log-probabilities of given tokens, with entropy and the most probable alternatives
+* ``distill_loss``, ``distill_loss_backward`` - divergence from a teacher's top tokens and its gradients
 * ``tree_attention``  - attention of drafted tokens (one, a chain, a tree) over a cache, adding up the weight
   each slot receives; ``tree_importance`` - that account for the accepted rows
 * ``cache_evict``     - the cache cut to its most attended slots, in place
@@ -30,6 +32,8 @@ from ._lib import (  # noqa: F401
     attn_importance_ex,
     cache_evict,
     combine_pool,
+    distill_loss,
+    distill_loss_backward,
     load,
     predict,
     head_param_views,
@@ -39,6 +43,7 @@ from ._lib import (  # noqa: F401
     token_entropy,
     token_entropy_noalloc,
     token_entropy_workspace_size,
+    token_logprobs,
     token_loss,
     token_loss_backward,
     tree_attention,

@@ -40,6 +40,9 @@ EXPORTS = (
     "estp_head_train_step_workspace_size", "estp_head_train_step",
     "estp_token_loss_workspace_size", "estp_token_loss",
     "estp_token_loss_backward_workspace_size", "estp_token_loss_backward",
+    "estp_token_logprobs_workspace_size", "estp_token_logprobs",
+    "estp_distill_loss_workspace_size", "estp_distill_loss",
+    "estp_distill_loss_backward_workspace_size", "estp_distill_loss_backward",
     "estp_tree_attention_workspace_size", "estp_tree_attention", "estp_tree_importance",
     "estp_cache_evict_workspace_size", "estp_cache_evict",
     "estp_misalignment", "estp_sjf_padding",
@@ -121,6 +124,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.estp_token_loss_backward_workspace_size.argtypes = [_I64, _I32, _I32, _INT]
     lib.estp_token_loss_backward.restype = _INT
     lib.estp_token_loss_backward.argtypes = [_P, _P, _P, _P, _P, _I64, _I32, _I32, _INT, _P, _P, _P, _SZ, _P]
+    lib.estp_token_logprobs_workspace_size.restype = _SZ
+    lib.estp_token_logprobs_workspace_size.argtypes = [_I64, _I32, _I32, _I32, _INT]
+    lib.estp_token_logprobs.restype = _INT
+    lib.estp_token_logprobs.argtypes = [_P, _P, _P, _I64, _I32, _I32, _I32, _F, _INT, _P, _P, _P, _P, _P, _P, _SZ, _P]
+    lib.estp_distill_loss_workspace_size.restype = _SZ
+    lib.estp_distill_loss_workspace_size.argtypes = [_I64, _I32, _I32, _INT]
+    lib.estp_distill_loss.restype = _INT
+    lib.estp_distill_loss.argtypes = [_P, _P, _P, _P, _I64, _I32, _I32, _I32, _F, _INT, _INT, _P, _P, _P, _P, _SZ, _P]
+    lib.estp_distill_loss_backward_workspace_size.restype = _SZ
+    lib.estp_distill_loss_backward_workspace_size.argtypes = [_I64, _I32, _I32, _INT]
+    lib.estp_distill_loss_backward.restype = _INT
+    lib.estp_distill_loss_backward.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _F, _INT, _INT, _P,
+                                               _P, _P, _SZ, _P]
     lib.estp_tree_attention_workspace_size.restype = _SZ
     lib.estp_tree_attention_workspace_size.argtypes = [_I32, _I32, _I64, _I32, _I32, _I32, _I32, _INT]
     lib.estp_tree_attention.restype = _INT
@@ -511,7 +527,8 @@ def _head_shapes(X, W, targets):
     V, dw = W.shape
     if dw != d:
         raise ValueError("X and W disagree on d")
-    _all_sized(dev.index, dev, (targets, "targets", n_tok, torch.int32))
+    if targets is not None:
+        _all_sized(dev.index, dev, (targets, "targets", n_tok, torch.int32))
     return n_tok, d, V, dev
 
 
@@ -566,6 +583,115 @@ def token_loss_backward(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
         _check(lib.estp_token_loss_backward(_ptr(X), _ptr(W), _ptr(targets), _ptr(lse), _ptr(grad), n_tok, d, V, dt,
                                             _ptr(dX), _ptr(dW), _ptr(workspace), wsb, st),
                "estp_token_loss_backward")
+    return dX, dW
+
+
+def token_logprobs(X: torch.Tensor, W: torch.Tensor, targets: Optional[torch.Tensor], k: int = 0,
+                   temperature: float = 1.0, logprob: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None,
+                   top_id: Optional[torch.Tensor] = None, top_logprob: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None, stream=None):
+    """Log-probabilities (nats) under softmax(W @ X[i] / temperature): returns ``(logprob [n_tok] of the given tokens,
+    lse [n_tok], entropy H [n_tok], top_id [n_tok, k], top_logprob [n_tok, k])``, the alternatives descending.
+
+    Tokens whose target lies outside [0, V) have logprob 0.  ``targets`` None: no logprob (None is returned).
+    """
+    lib = load()
+    n_tok, d, V, dev = _head_shapes(X, W, targets)
+    dt = _dtype_code(X)
+    k = int(k)
+    if targets is None and logprob is not None:
+        raise ValueError("logprob needs targets")
+    for t, name, n, dtype in ((logprob, "logprob", n_tok, torch.float32), (lse, "lse", n_tok, torch.float32),
+                              (H, "H", n_tok, torch.float32), (top_id, "top_id", n_tok * k, torch.int32),
+                              (top_logprob, "top_logprob", n_tok * k, torch.float32)):
+        if t is not None:
+            _all_sized(dev.index, dev, (t, name, n, dtype))
+    with _on(stream, dev) as st:
+        if targets is not None and logprob is None:
+            logprob = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        if lse is None:
+            lse = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        if H is None:
+            H = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        if top_id is None:
+            top_id = torch.empty(n_tok, max(k, 0), dtype=torch.int32, device=dev)
+        if top_logprob is None:
+            top_logprob = torch.empty(n_tok, max(k, 0), dtype=torch.float32, device=dev)
+        workspace, wsb = _workspace(lib.estp_token_logprobs_workspace_size(n_tok, d, V, k, dt), dev, workspace)
+        _check(lib.estp_token_logprobs(_ptr(X), _ptr(W), _ptr(targets), n_tok, d, V, k, float(temperature), dt,
+                                       _ptr(logprob), _ptr(lse), _ptr(H), _ptr(top_id), _ptr(top_logprob),
+                                       _ptr(workspace), wsb, st), "estp_token_logprobs")
+    return logprob, lse, H, top_id, top_logprob
+
+
+def _distill_shapes(X, W, ids, logp):
+    n_tok, d, V, dev = _head_shapes(X, W, None)
+    _need(ids, "ids", device=dev, dtype=torch.int32, ndim=2)
+    if ids.shape[0] != n_tok:
+        raise ValueError(f"ids must have {n_tok} rows")
+    K = ids.shape[1]
+    _all_sized(dev.index, dev, (logp, "logp", n_tok * K, torch.float32))
+    return n_tok, d, V, K, dev
+
+
+def distill_loss(X: torch.Tensor, W: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, temperature: float = 1.0,
+                 renormalise: bool = True, loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 logq: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Divergence (nats) of softmax(W @ X[i] / temperature) from a teacher's top tokens: returns ``(loss [n_tok],
+    lse [n_tok], logq [n_tok, K])`` with loss = sum_k p_k (log p_k - logq_k).
+
+    ``ids`` (int32 [n_tok, K]) and ``logp`` (float32 [n_tok, K]) are the teacher's, as ``token_logprobs`` returns them
+    at this temperature; ids outside [0, V) are not held.  ``renormalise``: the held tokens' probabilities add up to 1.
+    """
+    lib = load()
+    n_tok, d, V, K, dev = _distill_shapes(X, W, ids, logp)
+    dt = _dtype_code(X)
+    for t, name, n in ((loss, "loss", n_tok), (lse, "lse", n_tok), (logq, "logq", n_tok * K)):
+        if t is not None:
+            _all_sized(dev.index, dev, (t, name, n, torch.float32))
+    with _on(stream, dev) as st:
+        if loss is None:
+            loss = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        if lse is None:
+            lse = torch.empty(n_tok, dtype=torch.float32, device=dev)
+        if logq is None:
+            logq = torch.empty(n_tok, K, dtype=torch.float32, device=dev)
+        workspace, wsb = _workspace(lib.estp_distill_loss_workspace_size(n_tok, d, V, dt), dev, workspace)
+        _check(lib.estp_distill_loss(_ptr(X), _ptr(W), _ptr(ids), _ptr(logp), n_tok, d, V, K, float(temperature),
+                                     int(bool(renormalise)), dt, _ptr(loss), _ptr(lse), _ptr(logq), _ptr(workspace),
+                                     wsb, st), "estp_distill_loss")
+    return loss, lse, logq
+
+
+def distill_loss_backward(X: torch.Tensor, W: torch.Tensor, ids: torch.Tensor, logp: torch.Tensor, lse: torch.Tensor,
+                          logq: torch.Tensor, grad: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                          renormalise: bool = True, dX: Optional[torch.Tensor] = None,
+                          dW: Optional[torch.Tensor] = None, want_dX: bool = True, want_dW: bool = True,
+                          workspace: Optional[torch.Tensor] = None, stream=None):
+    """Gradients ``(dX [n_tok, d] or None, dW [V, d] or None)`` of sum_i grad[i] loss[i], in the inputs' type.
+
+    ``lse`` and ``logq`` are ``distill_loss``'s of the same arguments; ``grad`` (float32 [n_tok], default all 1) the
+    gradient with respect to the losses.
+    """
+    lib = load()
+    n_tok, d, V, K, dev = _distill_shapes(X, W, ids, logp)
+    dt = _dtype_code(X)
+    for t, name, n, dtype in ((lse, "lse", n_tok, torch.float32), (logq, "logq", n_tok * K, torch.float32),
+                              (grad, "grad", n_tok, torch.float32), (dX, "dX", n_tok * d, X.dtype),
+                              (dW, "dW", V * d, X.dtype)):
+        if t is not None:
+            _all_sized(dev.index, dev, (t, name, n, dtype))
+    with _on(stream, dev) as st:
+        if dX is None and want_dX:
+            dX = torch.empty_like(X)
+        if dW is None and want_dW:
+            dW = torch.empty_like(W)
+        workspace, wsb = _workspace(lib.estp_distill_loss_backward_workspace_size(n_tok, d, V, dt), dev, workspace)
+        _check(lib.estp_distill_loss_backward(_ptr(X), _ptr(W), _ptr(ids), _ptr(logp), _ptr(lse), _ptr(logq),
+                                              _ptr(grad), n_tok, d, V, K, float(temperature), int(bool(renormalise)),
+                                              dt, _ptr(dX), _ptr(dW), _ptr(workspace), wsb, st),
+               "estp_distill_loss_backward")
     return dX, dW
 
 

@@ -1,0 +1,299 @@
+// Distillation over the LM head: a student held to a teacher's top tokens, and its gradient, without the n_tok x V
+// logits.
+//
+//   s_i = W x_i / temperature,  lse_i = log sum_v exp s_i[v],  logq_ik = s_i[id_ik] - lse_i
+//   p_ik = exp(logp_ik), or the softmax of logp_i over the row's held entries
+//   loss_i = sum_k p_ik (log p_ik - logq_ik)
+//   G_iv = grad_i / temperature (P_i exp(s_i[v] - lse_i) - sum_{k: id_ik = v} p_ik),  P_i = sum_k p_ik
+//   dX = G W,  dW = G^T X
+//
+// Forward: one pass over the vocabulary keeps a maximum and a sum per token (token_loss.hip), and distill_pick_kernel
+// forms the logits of the teacher's tokens from a row of W each.
+//
+// Backward: the gradient of the LM-head loss (token_loss.hip) with weight grad_i P_i / temperature gives G but for the
+// teacher's entries.  distill_entries_kernel writes those over it, n_tok K of n_tok V, from logq, before the products
+// read G: each is formed in fp32 from the whole of its terms, whatever entries of the row name the same token, and is
+// rounded as the others are.
+//
+// A row without a held entry (an id outside [0, V), or a logp of -inf) is ignored: loss 0, no gradient, and its row
+// of X is never multiplied into one.
+#include <algorithm>
+
+#include "estp_common.h"
+#include "lm_head.h"
+#include "lse_states.h"
+
+namespace estp {
+namespace detail {
+
+constexpr int kMaxTeacher = 128;  // entries of a row: two a lane
+
+// The teacher's row of token tok, by one wave: entries lane and lane + 64.
+struct TeacherRow {
+  int id[2];      // -1: not held
+  float p[2];     // 0 where not held
+  float logp[2];  // -inf where not held
+  float mass;     // sum of p
+  bool live;      // some entry has weight
+};
+__device__ __forceinline__ TeacherRow teacher_row(const int32_t* __restrict__ ids, const float* __restrict__ logp,
+                                                  int tok, int K, int V, int renormalise, int lane) {
+  TeacherRow r;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int k = lane + 64 * u;
+    const int id = k < K ? ids[size_t(tok) * K + k] : -1;
+    const float lp = k < K ? logp[size_t(tok) * K + k] : 0.f;
+    const bool held = id >= 0 && id < V;
+    r.id[u] = held ? id : -1;
+    r.logp[u] = held ? lp : -INFINITY;
+  }
+  r.live = __any(r.logp[0] != -INFINITY || r.logp[1] != -INFINITY);  // (a NaN is weight: it reaches the loss)
+  if (renormalise) {
+    const float ref = fmaxf(wave_max(fmaxf(r.logp[0], r.logp[1])), -0x1p127f);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) r.p[u] = fast_exp2((r.logp[u] - ref) * kLog2e);
+    const float sum = r.live ? wave_sum(r.p[0] + r.p[1]) : 1.f, log_sum = kLn2 * fast_log2(sum);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      r.p[u] = r.p[u] / sum;
+      r.logp[u] = r.logp[u] - ref - log_sum;
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) r.p[u] = fast_exp2(r.logp[u] * kLog2e);
+  }
+  r.mass = wave_sum(r.p[0] + r.p[1]);
+  return r;
+}
+
+// lse, logq and loss of a token, one workgroup each.  Its waves share the K products of a row of W with the token's row
+// of X, four at a time, whose rows are far apart: the bytes of n K rows bound it where tokens are many, the latency of
+// one wave's rows where they are few.
+template <typename T, int kThreads>
+__global__ __launch_bounds__(kThreads) void distill_pick_kernel(
+    const T* __restrict__ X, const T* __restrict__ W, const int32_t* __restrict__ ids, const float* __restrict__ logp,
+    int d, int V, int K, int renormalise, float inv_t, const float* __restrict__ part_m,
+    const float* __restrict__ part_s, int states, float* __restrict__ lse, float* __restrict__ loss,
+    float* __restrict__ logq) {
+  constexpr int kWaves = kThreads / 64, kRows = 4;
+  __shared__ float z[kMaxTeacher];
+  const int tok = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const T* x = X + size_t(tok) * d;
+  for (int k0 = wave; k0 < K; k0 += kWaves * kRows) {
+    const T* w[kRows];
+    float sum[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {  // (an entry that is not held takes row 0, and its product is not used)
+      const int id = k0 + kWaves * u < K ? ids[size_t(tok) * K + k0 + kWaves * u] : -1;
+      w[u] = W + size_t(id >= 0 && id < V ? id : 0) * d;
+      sum[u] = 0.f;
+    }
+    for (int k = 8 * lane; k < d; k += 512)
+#pragma unroll
+      for (int u = 0; u < kRows; ++u) sum[u] = dot8(x + k, w[u] + k, sum[u]);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      sum[u] = wave_sum(sum[u]);
+      if (lane == 0 && k0 + kWaves * u < K) z[k0 + kWaves * u] = sum[u];
+    }
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const float l = lse_of_states(part_m, part_s, tok, states, lane);
+  const TeacherRow r = teacher_row(ids, logp, tok, K, V, renormalise, lane);
+  float term = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int k = lane + 64 * u;
+    const float q = r.id[u] >= 0 ? fmaf(z[k & (kMaxTeacher - 1)], inv_t, -l) : 0.f;
+    if (k < K) logq[size_t(tok) * K + k] = q;
+    term += r.p[u] == 0.f ? 0.f : r.p[u] * (r.logp[u] - q);
+  }
+  term = wave_sum(term);
+  if (lane == 0) {
+    lse[tok] = l;
+    loss[tok] = r.live ? term : 0.f;
+  }
+}
+
+// What the gradient of the LM-head loss takes for a row: a target to leave out (some token of the teacher's, whose entry
+// is written over anyway; -1 for an ignored row) and the weight of the softmax.  One wave per token.
+__global__ __launch_bounds__(256) void distill_rows_kernel(const int32_t* __restrict__ ids,
+                                                           const float* __restrict__ logp,
+                                                           const float* __restrict__ grad, int n_tok, int V, int K,
+                                                           int renormalise, float inv_t, int32_t* __restrict__ target,
+                                                           float* __restrict__ weight) {
+  const int tok = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (tok >= n_tok) return;
+  const TeacherRow r = teacher_row(ids, logp, tok, K, V, renormalise, lane);
+  int some = max(r.id[0], r.id[1]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) some = max(some, __shfl_xor(some, o, 64));
+  if (lane == 0) {
+    target[tok] = r.live ? some : -1;
+    weight[tok] = (grad ? grad[tok] : 1.f) * inv_t * r.mass;
+  }
+}
+
+// The entries of G that belong to the teacher's tokens, in vocabulary rows v0 .. v0 + Vc.  One wave per token; entries of
+// a row that name the same token write the same number.  Where G has two parts, the second holds what rounding the
+// first leaves.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_entries_kernel(
+    const int32_t* __restrict__ ids, const float* __restrict__ logp, const float* __restrict__ logq,
+    const float* __restrict__ grad, int n_tok, int V, int K, int renormalise, float inv_t,
+    const int* __restrict__ slot, const int* __restrict__ n_live, int64_t v0, int Vc, T* __restrict__ G) {
+  const int tok = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (tok >= n_tok) return;
+  const int s = slot[tok];
+  if (s < 0) return;
+  const TeacherRow r = teacher_row(ids, logp, tok, K, V, renormalise, lane);
+  float same[2] = {0.f, 0.f};  // weight of all entries that name this one's token
+  for (int k = 0; k < K; ++k) {
+    const int u = k >> 6;
+    const int id = __builtin_amdgcn_readlane(u ? r.id[1] : r.id[0], k & 63);
+    const float p = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u ? r.p[1] : r.p[0]), k & 63));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) same[e] += r.id[e] == id ? p : 0.f;
+  }
+  const float g = (grad ? grad[tok] : 1.f) * inv_t;
+  const int n_tokens = n_live[0];
+  const bool two = n_live[1] > n_tokens;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int64_t v = int64_t(r.id[e]) - v0;
+    if (r.id[e] < 0 || v < 0 || v >= Vc) continue;
+    const float q = fast_exp2(logq[size_t(tok) * K + lane + 64 * e] * kLog2e);
+    const float value = g * fmaf(r.mass, q, -same[e]);
+    const T first = T(value);
+    G[size_t(s) * Vc + v] = first;
+    if (two) G[size_t(s + n_tokens) * Vc + v] = T(value - float(first));
+  }
+}
+
+int launch_teacher_entries(const Distillation& t, int n, int V, int dtype, const int* slot, const int* n_live,
+                           int64_t v0, int Vc, void* G, hipStream_t s) {
+  const dim3 grid(unsigned((n + 3) / 4)), block(256);
+  const float inv_t = inverse_temperature(t.temperature);
+  if (dtype == ESTP_F32)
+    distill_entries_kernel<float><<<grid, block, 0, s>>>(t.ids, t.logp, t.logq, t.grad, n, V, t.K, t.renormalise, inv_t,
+                                                         slot, n_live, v0, Vc, static_cast<float*>(G));
+  else
+    distill_entries_kernel<__bf16><<<grid, block, 0, s>>>(t.ids, t.logp, t.logq, t.grad, n, V, t.K, t.renormalise,
+                                                          inv_t, slot, n_live, v0, Vc, static_cast<__bf16*>(G));
+  ESTP_CHECK_LAUNCH("distill_entries_kernel");
+  return ESTP_OK;
+}
+
+}  // namespace detail
+}  // namespace estp
+
+using namespace estp;
+using namespace estp::detail;
+
+namespace {
+
+int check_distill(const char* fn, const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok,
+                  int32_t d, int32_t V, int32_t K, float temperature, int dtype) {
+  ESTP_REQUIRE(ids && logp, ESTP_ERR_INVALID_ARG, "%s: ids and logp must be non-null", fn);
+  ESTP_REQUIRE(aligned(ids, 4) && aligned(logp, 4), ESTP_ERR_INVALID_ARG, "%s: ids and logp must be 4-byte aligned", fn);
+  ESTP_REQUIRE(K >= 1 && K <= kMaxTeacher, ESTP_ERR_INVALID_ARG, "%s: K must be in [1, %d], got %d", fn, kMaxTeacher, K);
+  ESTP_REQUIRE(temperature >= 1e-3f && temperature <= 1e3f, ESTP_ERR_INVALID_ARG,
+               "%s: temperature must be in [0.001, 1000], got %g", fn, double(temperature));
+  ESTP_REQUIRE(V <= INT32_MAX - 65536, ESTP_ERR_UNSUPPORTED, "%s: V = %d, at most 2^31 - 65537", fn, V);
+  const int st = check_lm_head_args(fn, X, W, n_tok, d, V, dtype);
+  if (st != ESTP_OK) return st;
+  ESTP_REQUIRE(n_tok <= (int64_t(1) << 22), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %lld, at most 4194304", fn,
+               (long long)n_tok);
+  return ESTP_OK;
+}
+
+}  // namespace
+
+extern "C" size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
+  if (n_tok < 1 || d < 1 || V < 1) return 0;
+  return lse_states_bytes(n_tok, V, dtype, false);
+}
+
+extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok,
+                                 int32_t d, int32_t V, int32_t K, float temperature, int renormalise, int dtype,
+                                 float* loss, float* lse, float* logq, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  clear_error();
+  const char* fn = "estp_distill_loss";
+  ESTP_REQUIRE(loss && lse && logq, ESTP_ERR_INVALID_ARG, "%s: loss, lse and logq must be non-null", fn);
+  ESTP_REQUIRE(aligned(loss, 4) && aligned(lse, 4) && aligned(logq, 4), ESTP_ERR_INVALID_ARG,
+               "%s: loss, lse and logq must be 4-byte aligned", fn);
+  const int st = check_distill(fn, X, W, ids, logp, n_tok, d, V, K, temperature, dtype);
+  if (st != ESTP_OK) return st;
+  const size_t need = estp_distill_loss_workspace_size(n_tok, d, V, dtype);
+  ESTP_REQUIRE(workspace_bytes >= need, ESTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn,
+               workspace_bytes, need);
+  ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
+               "%s: workspace must be non-null and 256-byte aligned", fn);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int n = int(n_tok);
+  LseStates p;
+  const int rc = launch_lse_states(fn, X, W, n, d, V, dtype, base2_of_logit(temperature), workspace, s, &p);
+  if (rc != ESTP_OK) return rc;
+  const float inv_t = inverse_temperature(temperature);
+  auto go = [&](auto kernel, int threads, auto* x, auto* w) {
+    kernel<<<dim3(unsigned(n)), dim3(unsigned(threads)), 0, s>>>(x, w, ids, logp, d, V, K, renormalise != 0, inv_t, p.m,
+                                                                 p.s, p.states, lse, loss, logq);
+  };
+  const bool few = n <= 256;
+  if (dtype == ESTP_F32) {
+    const float *x = static_cast<const float*>(X), *w = static_cast<const float*>(W);
+    few ? go(distill_pick_kernel<float, 1024>, 1024, x, w) : go(distill_pick_kernel<float, 256>, 256, x, w);
+  } else {
+    const __bf16 *x = static_cast<const __bf16*>(X), *w = static_cast<const __bf16*>(W);
+    few ? go(distill_pick_kernel<__bf16, 1024>, 1024, x, w) : go(distill_pick_kernel<__bf16, 256>, 256, x, w);
+  }
+  ESTP_CHECK_LAUNCH("distill_pick_kernel");
+  return ESTP_OK;
+}
+
+extern "C" size_t estp_distill_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
+  if (n_tok < 1 || d < 1 || V < 1) return 0;
+  Carver c(nullptr);
+  c.take<int32_t>(size_t(n_tok));
+  c.take<float>(size_t(n_tok));
+  return c.bytes() + lm_head_backward_bytes(n_tok, d, V, dtype);
+}
+
+extern "C" int estp_distill_loss_backward(const void* X, const void* W, const int32_t* ids, const float* logp,
+                                          const float* lse, const float* logq, const float* grad, int64_t n_tok,
+                                          int32_t d, int32_t V, int32_t K, float temperature, int renormalise,
+                                          int dtype, void* dX, void* dW, void* workspace, size_t workspace_bytes,
+                                          void* stream) {
+  clear_error();
+  const char* fn = "estp_distill_loss_backward";
+  ESTP_REQUIRE(lse && logq, ESTP_ERR_INVALID_ARG, "%s: lse and logq must be non-null", fn);
+  ESTP_REQUIRE(dX || dW, ESTP_ERR_INVALID_ARG, "%s: dX and dW are both null", fn);
+  ESTP_REQUIRE(aligned(lse, 4) && aligned(logq, 4) && aligned(grad, 4), ESTP_ERR_INVALID_ARG,
+               "%s: lse, logq and grad must be 4-byte aligned", fn);
+  ESTP_REQUIRE(aligned(dX, 16) && aligned(dW, 16), ESTP_ERR_INVALID_ARG, "%s: dX and dW must be 16-byte aligned", fn);
+  const int st = check_distill(fn, X, W, ids, logp, n_tok, d, V, K, temperature, dtype);
+  if (st != ESTP_OK) return st;
+  ESTP_REQUIRE(d <= (1 << 20), ESTP_ERR_UNSUPPORTED, "%s: d = %d, at most 1048576", fn, d);
+  ESTP_REQUIRE(n_tok * d <= (int64_t(1) << 36), ESTP_ERR_UNSUPPORTED, "%s: n_tok d = %lld, at most 2^36", fn,
+               (long long)n_tok * d);
+  const size_t need = estp_distill_loss_backward_workspace_size(n_tok, d, V, dtype);
+  ESTP_REQUIRE(workspace_bytes >= need, ESTP_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", fn,
+               workspace_bytes, need);
+  ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
+               "%s: workspace must be non-null and 256-byte aligned", fn);
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int n = int(n_tok);
+  Carver c(workspace);
+  int32_t* target = c.take<int32_t>(size_t(n));
+  float* weight = c.take<float>(size_t(n));
+  distill_rows_kernel<<<dim3(unsigned((n + 3) / 4)), dim3(256), 0, s>>>(
+      ids, logp, grad, n, V, K, renormalise != 0, inverse_temperature(temperature), target, weight);
+  ESTP_CHECK_LAUNCH("distill_rows_kernel");
+  const Distillation t{ids, logp, logq, grad, K, renormalise != 0, temperature};
+  return launch_lm_head_backward(X, W, target, lse, weight, n, d, V, dtype, &t, dX, dW,
+                                 static_cast<char*>(workspace) + c.bytes(), s);
+}

@@ -22,6 +22,14 @@
 
 namespace estp {
 namespace detail {
+// Stores of 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
+template <int kAux = 0>
+__device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, kAux);
+#endif
+}
+
 namespace gemm {
 
 constexpr int kWaves = 4;
@@ -83,6 +91,20 @@ __device__ __forceinline__ int fresh_lane() {
   asm volatile("" : "+v"(lane));
 #endif
   return lane;
+}
+// Token tile and vocabulary slice of workgroup id `wg` of n_tt x n_slices, in groups of 8 token tiles: the 32 consecutive
+// ids that one XCD works on at a time stream 4 slices of W past 8 tiles of tokens.  slice >= n_slices: none.
+struct SliceAt {
+  int tile, slice;
+};
+__device__ __forceinline__ SliceAt slice_of(int wg, int n_tt, int n_slices) {
+  const int whole = n_tt & ~7, cols = n_tt & 7;
+  if (wg < whole * n_slices) {
+    const int group = wg / (8 * n_slices), r = wg - group * 8 * n_slices;
+    return {8 * group + (r & 7), r >> 3};
+  }
+  const int r = wg - whole * n_slices;
+  return cols ? SliceAt{whole + r % cols, r / cols} : SliceAt{0, n_slices};
 }
 // First tile id of a workgroup; it goes on in steps of the grid (a multiple of 8).
 __device__ __forceinline__ int first_tile(int wg, int grid) { return (wg & 7) * (grid >> 3) + (wg >> 3); }

@@ -24,31 +24,16 @@
 #include <algorithm>
 
 #include "estp_common.h"
+#include "f32_gemm.h"
 #include "lm_head.h"
 #include "loss_shares.h"
+#include "lse_states.h"
 #include "mfma_gemm.h"
 
 namespace estp {
 namespace detail {
 
 // ------------------------------------------------------------------ elementwise parts
-
-// sum over 8 consecutive elements of a[k] b[k]
-__device__ __forceinline__ float dot8(const __bf16* a, const __bf16* b, float s) {
-  const bf16x8_t x = *reinterpret_cast<const bf16x8_t*>(a), y = *reinterpret_cast<const bf16x8_t*>(b);
-#pragma unroll
-  for (int k = 0; k < 8; ++k) s = fmaf(float(x[k]), float(y[k]), s);
-  return s;
-}
-__device__ __forceinline__ float dot8(const float* a, const float* b, float s) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const f32x4_t x = *reinterpret_cast<const f32x4_t*>(a + 4 * h), y = *reinterpret_cast<const f32x4_t*>(b + 4 * h);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) s = fmaf(x[k], y[k], s);
-  }
-  return s;
-}
 
 // loss_i = lse_i - x_i . W[t_i], one wave per token, lse_i given or from `states` partial (maximum, sum) states in base
 // 2, state p of token i at i states + p: then it is written too.  A sum of probabilities is at most 1, so a difference
@@ -70,36 +55,7 @@ __global__ __launch_bounds__(256) void loss_pick_kernel(const T* __restrict__ X,
   z = wave_sum(z);
   float l;
   if constexpr (kStates) {
-    constexpr int kAhead = 8;  // states of a lane on their way together
-    float M = -INFINITY, s = 0.f;
-    for (int p0 = lane; p0 < states; p0 += 64 * kAhead) {
-      float m[kAhead], ps[kAhead], top = M;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const size_t at = size_t(tok) * states + min(p0 + 64 * u, states - 1);
-        m[u] = part_m[at];
-        ps[u] = part_s[at];
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const bool in = p0 + 64 * u < states;
-        m[u] = in ? m[u] : -INFINITY;
-        ps[u] = in ? ps[u] : 0.f;
-        top = fmaxf(top, m[u]);
-      }
-      const float ref = fmaxf(top, -0x1p127f);
-      s *= fast_exp2(fmaxf(M - ref, kExp2Floor));
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) s = fmaf(ps[u], fast_exp2(fmaxf(m[u] - ref, kExp2Floor)), s);
-      M = top;
-    }
-    const float top = wave_max(M);
-    s = wave_sum(s * fast_exp2(fmaxf(M - fmaxf(top, -0x1p127f), kExp2Floor)));
-    // in natural units with one rounding (ln 2 in two parts): weights exp(z - lse) near 1, whose distance from 1 is the
-    // gradient, have the error of lse
-    constexpr float kLn2Rest = -1.904654299957768e-9f;
-    const float t2 = fast_log2(s);
-    l = top == -INFINITY ? top + t2 : fmaf(top, kLn2, fmaf(top, kLn2Rest, kLn2 * t2));  // (a NaN in s stays one)
+    l = lse_of_states(part_m, part_s, tok, states, lane);
     if (lane == 0) lse[tok] = l;
   } else {
     l = lse[tok];
@@ -233,150 +189,13 @@ __global__ __launch_bounds__(256) void loss_dx_kernel(const float* __restrict__ 
 }
 
 // ------------------------------------------------------------------ matrix-core products (fp32)
-//
-// C[m][n] = sum_k A(m, k) B(n, k) over 128 x kTN tiles on v_mfma_f32_32x32x2_f32 (without packed instructions the
-// vector units reach half its rate), 4 waves of 64 x 64, or of 32 x kTN for the 64 and 32 columns of few tokens.
-// Operands lie in memory with k contiguous or strided and reach LDS as they lie, 32 k a stage, two stages of at most 32
-// KB, so two or more workgroups share a compute unit.  A lane of a step gives row lane % 32 at one of two k; any order
-// of the k will do if both sides keep it: of 8 k, step i takes k = i and 4 + i, so that a lane's four values are one
-// 16-byte read where k is contiguous.  kFSum terms at a time are summed before they enter the total, which keeps the
-// rounding of long sums small (3 tokens, d 2048: dW off by 2e-7, by 2e-6 with one chain of sums) for 64 additions in
-// 256 products.
-//
-// 400 tokens, d 2048, V 128256 (a product of 210 GFLOP, 153 TFLOP/s at most, a fifth of it on columns that no token
-// has): logits 2.15 ms, dX 2.14, dW 1.80 (117 TFLOP/s).  16 tokens, which one pass over the 1.05 GB of W or dW bounds:
-// logits 244 us (4.3 TB/s), dX 222, dW 354.
-constexpr int kFT = 128, kFK = 32, kFPart = kFT * kFK * 4;
-constexpr int kFSum = 128;
-
-template <bool kAK, bool kBK, int kTN>
-struct F32Tile {
-  static constexpr int kWM = kTN == kFT ? 2 : 4;            // waves along the rows
-  static constexpr int kMI = kFT / 32 / kWM, kNJ = kTN == kFT ? 2 : kTN / 32;  // 32 x 32 blocks of a wave
-  static constexpr int kPartB = kTN * kFK * 4, kStage = kFPart + kPartB, kLds = 2 * kStage, kLB = kTN / 32;
-  using Acc = f32x16_t[kMI][kNJ];
-  // What a lane holds: columns n + 32 j, and of each 32 rows from m + 32 i the four runs of four at 8 q.
-  struct At {
-    int m, n, wm;
-  };
-  __device__ static __forceinline__ At place(int m0, int n0) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % kWM;
-    return {m0 + 32 * kMI * wm + 4 * (lane >> 5), n0 + 32 * kNJ * (wave / kWM) + (lane & 31), wm};
-  }
-  // byte offset in the source of what lane `lane` of transfer i brings of a part of kRows rows; *kc: its first k where
-  // k is contiguous
-  template <bool kK, int kRows>
-  __device__ static __forceinline__ uint32_t source(int i, int wave, int lane, uint32_t ld, int* kc) {
-    const int at = 64 * (4 * i + wave) + lane;
-    if (kK) {
-      const int row = at / 8, c = (at % 8) ^ (row & 7);
-      *kc = 4 * c;
-      return uint32_t(row) * ld + uint32_t(c) * 16u;
-    }
-    *kc = 0;
-    return uint32_t(at / (kRows / 4)) * ld + uint32_t(at % (kRows / 4)) * 16u;
-  }
-  // rows 32 block + lane % 32 at k = 8 g + 4 (lane / 32) .. + 3 of a part in LDS
-  template <bool kK, int kRows>
-  __device__ static __forceinline__ f32x4_t read(const char* part, int row, int g, int half) {
-    if (kK) return *reinterpret_cast<const f32x4_t*>(part + row * 128 + ((2 * g + half) ^ (row & 7)) * 16);
-    f32x4_t v;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[i] = *reinterpret_cast<const float*>(part + ((8 * g + 4 * half + i) * kRows + row) * 4);
-    return v;
-  }
-  // acc[i][j] = the product over k in [k0, k1) of the wave's 32 x 32 blocks (mfma32_f32's layout)
-  __device__ static __forceinline__ void run(char* lds, const gemm::Operand& A, const gemm::Operand& B, int m0, int n0,
-                                             int k0, int k1, Acc& acc) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = wave % kWM, wn = wave / kWM, half = lane >> 5, row = lane & 31;
-#pragma unroll
-    for (int i = 0; i < kMI; ++i)
-#pragma unroll
-      for (int j = 0; j < kNJ; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-    if (k0 >= k1) return;
-    uint32_t off_a[4], off_b[kLB];
-    int kc_a[4], kc_b[kLB];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) off_a[i] = source<kAK, kFT>(i, wave, lane, A.ld, &kc_a[i]);
-#pragma unroll
-    for (int i = 0; i < kLB; ++i) off_b[i] = source<kBK, kTN>(i, wave, lane, B.ld, &kc_b[i]);
-    auto part = [&](auto contig, auto n_parts, const gemm::Operand& o, int r0, int rows, int k, const uint32_t* off,
-                    const int* kc, char* dst) {
-      constexpr bool kContig = decltype(contig)::value;
-      const int left = k1 - k;
-      const u32x4_t r = kContig ? rsrc_words(o.base + size_t(r0) * o.ld, uint32_t(min(rows, o.rows - r0)) * o.ld)
-                                : rsrc_words(o.base + size_t(k) * o.ld + size_t(r0) * 4,
-                                             uint32_t(min(kFK, left)) * o.ld - uint32_t(r0) * 4u);
-      const uint32_t soff = kContig ? uint32_t(k) * 4u : 0u;
-#pragma unroll
-      for (int i = 0; i < decltype(n_parts)::value; ++i)
-        dma16(r, kContig && kc[i] >= left ? kPastEnd : off[i], soff, dst + 1024 * (4 * i + wave));
-    };
-    auto stage = [&](int k, int buf) {
-      part(std::bool_constant<kAK>{}, std::integral_constant<int, 4>{}, A, m0, kFT, k, off_a, kc_a, lds + buf * kStage);
-      part(std::bool_constant<kBK>{}, std::integral_constant<int, kLB>{}, B, n0, kTN, k, off_b, kc_b,
-           lds + buf * kStage + kFPart);
-    };
-    lds_barrier();  // the last tile's stages are read
-    stage(k0, 0);
-    int buf = 0;
-    Acc part_sum;
-    auto clear = [&]() {
-#pragma unroll
-      for (int i = 0; i < kMI; ++i)
-#pragma unroll
-        for (int j = 0; j < kNJ; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) part_sum[i][j][r] = 0.f;
-    };
-    auto add = [&]() {
-#pragma unroll
-      for (int i = 0; i < kMI; ++i)
-#pragma unroll
-        for (int j = 0; j < kNJ; ++j) acc[i][j] += part_sum[i][j];
-    };
-    clear();
-    int left_in_sum = kFSum;
-    for (int k = k0; k < k1; k += kFK, buf ^= 1) {
-      if (left_in_sum == 0) {
-        add();
-        clear();
-        left_in_sum = kFSum;
-      }
-      left_in_sum -= kFK;
-      arrived<0>();
-      lds_barrier();  // every wave's transfers of the stage have landed, and its reads of the other are done
-      if (k + kFK < k1) stage(k + kFK, buf ^ 1);
-      const char *pa = lds + buf * kStage, *pb = pa + kFPart;
-#pragma unroll
-      for (int g = 0; g < kFK / 8; ++g) {
-        f32x4_t a[kMI], b[kNJ];
-#pragma unroll
-        for (int i = 0; i < kMI; ++i) a[i] = read<kAK, kFT>(pa, 32 * (kMI * wm + i) + row, g, half);
-#pragma unroll
-        for (int j = 0; j < kNJ; ++j) b[j] = read<kBK, kTN>(pb, 32 * (kNJ * wn + j) + row, g, half);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int i = 0; i < kMI; ++i)
-#pragma unroll
-            for (int j = 0; j < kNJ; ++j) part_sum[i][j] = mfma32_f32(a[i][q], b[j][q], part_sum[i][j]);
-      }
-    }
-    add();
-  }
-};
 
 // Running (maximum, sum) in base 2 of every token's logits over a slice of the vocabulary tiles: slice s of n_slices
 // takes tiles s, s + n_slices, ...; each wave's rows of a tile have a state of their own.  Partial states
 // [n_tok, kWM n_slices].
 template <int kTN>
 __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __restrict__ X, const float* __restrict__ W,
-                                                              int n_tok, int d, int V, int n_slices,
+                                                              int n_tok, int d, int V, float c2, int n_slices,
                                                               float* __restrict__ part_m, float* __restrict__ part_s) {
   using Run = F32Tile<true, true, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
@@ -401,7 +220,7 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
-          mx = fmaxf(mx, live ? acc[i][j][r] * kLog2e : -INFINITY);
+          mx = fmaxf(mx, live ? acc[i][j][r] * c2 : -INFINITY);
         }
       const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
       float sum = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
@@ -410,7 +229,7 @@ __global__ __launch_bounds__(256, 2) void loss_lse_f32_kernel(const float* __res
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const bool live = at.m + 32 * i + 8 * (r >> 2) + (r & 3) < V;
-          sum += live ? fast_exp2(fmaf(acc[i][j][r], kLog2e, -ref)) : 0.f;
+          sum += live ? fast_exp2(fmaf(acc[i][j][r], c2, -ref)) : 0.f;
         }
       m[j] = mx;
       l[j] = sum;
@@ -438,7 +257,8 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
                                                                const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                                int Vc, const int32_t* __restrict__ tc,
                                                                const float* __restrict__ lc,
-                                                               const float* __restrict__ gc, float* __restrict__ G) {
+                                                               const float* __restrict__ gc, float inv_t,
+                                                               float* __restrict__ G) {
   using Run = F32Tile<true, true, kTN>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
   const int n = n_live[1], n0 = blockIdx.y * kTN, m0 = blockIdx.x * kFT;
@@ -463,8 +283,8 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
         f32x4_t out;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          // (z - lse first: near 0 for the weights that matter, so its product is exact to its own rounding)
-          const float p = fast_exp2((acc[i][j][4 * q + e] - l) * kLog2e) - (v + e == t ? 1.f : 0.f);
+          // (z / temperature - lse first: near 0 for the weights that matter, so its product is exact to its own rounding)
+          const float p = fast_exp2(fmaf(acc[i][j][4 * q + e], inv_t, -l) * kLog2e) - (v + e == t ? 1.f : 0.f);
           out[e] = v + e < rows ? g * p : 0.f;
         }
         *reinterpret_cast<f32x4_t*>(G + size_t(s) * Vc + v) = out;
@@ -539,14 +359,6 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
 
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
-// Stores of 16 bytes at a byte offset of a buffer resource; past its end nothing is written.
-template <int kAux = 0>
-__device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_raw_buffer_store_b128(u32x4_t{v.x, v.y, v.z, v.w}, r, off, 0, kAux);
-#endif
-}
-
 // Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
 // first tile's maximum is the reference; later tiles add to the sum with one FMA, exponential and addition a logit,
@@ -555,12 +367,13 @@ __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v)
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __restrict__ X,
                                                                const __bf16* __restrict__ W, int n_tok, int d, int V,
-                                                               int n_tt, int n_slices, float* __restrict__ part_m,
+                                                               float c2, int n_tt, int n_slices,
+                                                               float* __restrict__ part_m,
                                                                float* __restrict__ part_s) {
   using Run = gemm::Tiles<true, true, false, kNBN, kOdd, 0>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
-  // token tiles of a slice, which stream the same rows of W, next to each other on one XCD
-  const int wg = gemm::first_tile(blockIdx.x, gridDim.x), tt = wg % n_tt, slice = wg / n_tt;
+  const gemm::SliceAt at_slice = gemm::slice_of(gemm::first_tile(blockIdx.x, gridDim.x), n_tt, n_slices);
+  const int tt = at_slice.tile, slice = at_slice.slice;
   if (slice >= n_slices) return;
   const gemm::Operand A{reinterpret_cast<const char*>(W), uint32_t(d) * 2u, V};
   const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 2u, n_tok};
@@ -587,7 +400,7 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s += fast_exp2(fmaf(acc[i][j][r], kLog2e, -m[j]));
+              for (int r = 0; r < 4; ++r) s += fast_exp2(fmaf(acc[i][j][r], c2, -m[j]));
             exact = !(s <= 0x1p64f);  // (a NaN takes the exact path and stays one)
             l[j] = exact ? l[j] : s;
           }
@@ -596,14 +409,14 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * kLog2e : -INFINITY);
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * c2 : -INFINITY);
             const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
             float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                s += 16 * i + r < lim ? fast_exp2(fmaf(acc[i][j][r], kLog2e, -ref)) : 0.f;
+                s += 16 * i + r < lim ? fast_exp2(fmaf(acc[i][j][r], c2, -ref)) : 0.f;
             m[j] = mx;
             l[j] = s;
           }
@@ -639,7 +452,8 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
                                                                 const int* __restrict__ n_live, int d, int V,
                                                                 int64_t v0, int Vc, const int32_t* __restrict__ tc,
                                                                 const float* __restrict__ lc,
-                                                                const float* __restrict__ gc, __bf16* __restrict__ G) {
+                                                                const float* __restrict__ gc, float c2,
+                                                                __bf16* __restrict__ G) {
   using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 4 * kNBN>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
   const int n = __builtin_amdgcn_readfirstlane(n_live[1]), n_tokens = __builtin_amdgcn_readfirstlane(n_live[0]);
@@ -682,7 +496,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
           for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              p[i / 2][4 * (i % 2) + r] = g * fast_exp2(fmaf(acc[i][j][r], kLog2e, -l2));
+              p[i / 2][4 * (i % 2) + r] = g * fast_exp2(fmaf(acc[i][j][r], c2, -l2));
           if (__any(rel >= 0 && rel < 128 && (rel & 31) < 8)) {  // seldom: one tile in V / 256 holds a token's target
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -921,12 +735,15 @@ inline LossBuffers carve_loss(const LossRoom& r, int64_t n_tok, int d, int dtype
 
 template <typename T>
 int launch_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
-                         int n, int d, int V, int dtype, void* dX, void* dW, void* workspace, hipStream_t s) {
+                         int n, int d, int V, int dtype, const Distillation* teacher, void* dX, void* dW,
+                         void* workspace, hipStream_t s) {
   const LossPlan p = plan_loss(n, d, V, dtype);
   const LossBuffers b = carve_loss(loss_need(p, n, d), n, d, dtype, workspace);
   constexpr int kWgs = 256;  // of the persistent kernels: one on each compute unit
   const T *Wt = static_cast<const T*>(W), *Xc = reinterpret_cast<const T*>(b.Xc);
   T* G = reinterpret_cast<T*>(b.G);
+  const float inv_t = teacher ? inverse_temperature(teacher->temperature) : 1.f;
+  const float c2 = teacher ? base2_of_logit(teacher->temperature) : kLog2e;
   if (n > 1024)
     loss_list_kernel<<<dim3(1), dim3(1024), 0, s>>>(targets, n, V, p.parts, b.row, b.slot, b.n_live);
   auto gather = n > 1024 ? loss_gather_kernel<false> : loss_gather_kernel<true>;
@@ -941,8 +758,12 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
       const bool odd = d % 64 != 0;
       auto grad_kernel = p.tile_toks == 128 ? (odd ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
                                             : (odd ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
-      grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, c2, G);
       ESTP_CHECK_LAUNCH("loss_grad_mfma_kernel");
+      if (teacher) {
+        const int rc = launch_teacher_entries(*teacher, n, V, dtype, b.slot, b.n_live, v0, p.Vc, G, s);
+        if (rc != ESTP_OK) return rc;
+      }
       if (dX) {
         auto dx_kernel = p.tile_toks == 128 ? loss_dx_mfma_kernel<4> : loss_dx_mfma_kernel<8>;
         dx_kernel<<<grid, block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, b.room, v0 == 0, b.acc);
@@ -959,8 +780,12 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
       auto grad_kernel = p.tile_toks == 32   ? loss_grad_f32_kernel<32>
                          : p.tile_toks == 64 ? loss_grad_f32_kernel<64>
                                              : loss_grad_f32_kernel<kFT>;
-      grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, G);
+      grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, inv_t, G);
       ESTP_CHECK_LAUNCH("loss_grad_f32_kernel");
+      if (teacher) {
+        const int rc = launch_teacher_entries(*teacher, n, V, dtype, b.slot, b.n_live, v0, p.Vc, G, s);
+        if (rc != ESTP_OK) return rc;
+      }
       if (dX) {
         // (a workgroup for every share there could be, up to a million in all: past that, a loop over the shares)
         const int64_t most = std::max<int64_t>(1, (int64_t(1) << 20) / (int64_t(n_dt) * n_tt));
@@ -990,13 +815,16 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
   return ESTP_OK;
 }
 
-}  // namespace detail
-}  // namespace estp
+size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype) {
+  return carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
+}
 
-using namespace estp;
-using namespace estp::detail;
-
-namespace {
+int launch_lm_head_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
+                            int n, int d, int V, int dtype, const Distillation* teacher, void* dX, void* dW,
+                            void* workspace, hipStream_t s) {
+  auto launch = dtype == ESTP_F32 ? launch_loss_backward<float> : launch_loss_backward<__bf16>;
+  return launch(X, W, targets, lse, grad, n, d, V, dtype, teacher, dX, dW, workspace, s);
+}
 
 // How a call that wants no more than lse is cut: tiles of `tile` tokens, the vocabulary tiles in `slices`, `states`
 // partial states a token.
@@ -1005,24 +833,82 @@ struct LsePlan {
 };
 // bf16: a workgroup on every compute unit, tiles as in the backward.  fp32: two workgroups for every compute unit (four
 // of the smaller ones).
-LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
+//
+// bf16 calls of more than 8 tiles, whose number does not divide 256, would so leave compute units idle (5 tiles of 52
+// at 13 tiles): they take up to four rounds of workgroups, as many slices as make the longest sum of a compute unit's
+// tiles shortest, with half a tile for a workgroup's first transfers.
+static LsePlan plan_lse(int64_t n_tok, int V, int dtype) {
   LsePlan p;
   const bool f32 = dtype == ESTP_F32;
   p.tile = f32 ? f32_tile_toks(n_tok, V) : bf16_tile_toks(n_tok);
   const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows, n_tt = (n_tok + p.tile - 1) / p.tile;
   const int64_t fill = !f32 ? 256 : p.tile < kFT ? 1024 : 512;
   p.slices = int(std::min(n_vt, std::max<int64_t>(f32 ? 4 : 1, fill / n_tt)));
+  if (!f32 && n_tt > 8) {
+    int64_t best = INT64_MAX;
+    for (int64_t c = p.slices; c <= std::min(n_vt, std::max<int64_t>(p.slices, 1024 / n_tt)); ++c) {
+      const int64_t cost = (n_tt * c + 255) / 256 * (2 * ((n_vt + c - 1) / c) + 1);
+      if (cost < best) {
+        best = cost;
+        p.slices = int(c);
+      }
+    }
+  }
   p.states = p.slices * (f32 && p.tile < kFT ? 4 : 2);
   return p;
 }
-// At least the partial states of every call of n_tok tokens or fewer (plan_lse gives few tokens more slices): a workspace
-// of a larger call serves a smaller one.  slices n_tok is at most fill tile, or 4 n_tok, or n_vt n_tok.
-size_t lse_room(int64_t n_tok, int V, int dtype) {
+// At least the partial states of every call of n_tok tokens or fewer, up to `most` (plan_lse gives few tokens more
+// slices): a workspace of a larger call serves a smaller one.  slices n_tok is at most fill tile (four times that of
+// more than 8 tiles), or 4 n_tok, or n_vt n_tok.
+static size_t lse_room(int64_t n_tok, int V, int dtype, bool few) {
   const bool f32 = dtype == ESTP_F32;
   const int64_t rows = f32 ? kFT : 256, n_vt = (int64_t(V) + rows - 1) / rows;
   if (f32) return size_t(4 * std::min(n_vt * n_tok, std::max<int64_t>(4 * n_tok, 1024 * 64)));
-  return size_t(2 * std::min<int64_t>(n_vt * n_tok, 256 * 256));
+  if (few) return size_t(2 * std::min<int64_t>(n_vt * n_tok, 256 * 256));
+  return size_t(2 * std::min<int64_t>(n_vt * n_tok, std::max<int64_t>(n_tok, 1024 * 256)));
 }
+
+size_t lse_states_bytes(int64_t n_tok, int V, int dtype, bool few) {
+  Carver c(nullptr);
+  for (int i = 0; i < 2; ++i) c.take<float>(lse_room(n_tok, V, dtype, few));
+  return c.bytes();
+}
+
+int launch_lse_states(const char* fn, const void* X, const void* W, int n, int d, int V, int dtype, float c2,
+                      void* workspace, hipStream_t s, LseStates* out) {
+  const LsePlan p = plan_lse(n, V, dtype);
+  Carver c(workspace);
+  out->m = c.take<float>(size_t(p.states) * size_t(n));
+  out->s = c.take<float>(size_t(p.states) * size_t(n));
+  out->states = p.states;
+  const int n_tt = int((int64_t(n) + p.tile - 1) / p.tile);
+  const size_t wgs = size_t(n_tt) * size_t(p.slices);
+  ESTP_REQUIRE(fits_launch(wgs + 7, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
+  if (dtype == ESTP_F32) {
+    auto kernel = p.tile == 32   ? loss_lse_f32_kernel<32>
+                  : p.tile == 64 ? loss_lse_f32_kernel<64>
+                                 : loss_lse_f32_kernel<kFT>;
+    kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), n, d,
+                                                     V, c2, p.slices, out->m, out->s);
+  } else {
+    auto kernel = p.tile == 128 ? (d % 64 ? loss_lse_mfma_kernel<4, true> : loss_lse_mfma_kernel<4, false>)
+                                : (d % 64 ? loss_lse_mfma_kernel<8, true> : loss_lse_mfma_kernel<8, false>);
+    kernel<<<dim3(unsigned((wgs + 7) / 8 * 8)), dim3(256), 0, s>>>(static_cast<const __bf16*>(X),
+                                                                   static_cast<const __bf16*>(W), n, d, V, c2, n_tt,
+                                                                   p.slices, out->m, out->s);
+  }
+  ESTP_CHECK_LAUNCH("loss_lse_kernel");
+  return ESTP_OK;
+}
+
+}  // namespace detail
+}  // namespace estp
+
+using namespace estp;
+using namespace estp::detail;
+
+namespace {
+
 // bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.  d 2048, V 128256, here against
 // there: 128 tokens 137 and 154 us, 1021 tokens 451 and 626, 2048 tokens 870 and 1220, 2500 tokens 1077 and 991, 4096
 // tokens 1735 and 1544; d 4096 2048 tokens 1568 and 2304, 2304 tokens 1767 and 1629; d 1536, V 151936, 782 and 1149, 888
@@ -1035,9 +921,7 @@ bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 20
 extern "C" size_t estp_token_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   const size_t entropy = estp_token_entropy_workspace_size(n_tok, d, V, dtype);
   if (entropy == 0) return 0;
-  Carver c(nullptr);
-  for (int i = 0; i < 2; ++i) c.take<float>(lse_room(n_tok, V, dtype));
-  return std::max(entropy, c.bytes());
+  return std::max(entropy, lse_states_bytes(n_tok, V, dtype, true));
 }
 
 extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d,
@@ -1063,33 +947,15 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
   const dim3 grid(unsigned((n_tok + 3) / 4)), block(256);
   if (own_lse(n_tok, dtype) && !H && !vocab_argmax) {
     // maximum and sum alone
-    const LsePlan p = plan_lse(n_tok, V, dtype);
-    Carver c(workspace);
-    float* pm = c.take<float>(size_t(p.states) * size_t(n_tok));
-    float* ps = c.take<float>(size_t(p.states) * size_t(n_tok));
-    const int n_tt = int((n_tok + p.tile - 1) / p.tile);
-    const size_t wgs = size_t(n_tt) * size_t(p.slices);
-    ESTP_REQUIRE(fits_launch(wgs + 7, 256), ESTP_ERR_UNSUPPORTED, "%s: n_tok = %d needs %zu workgroups", fn, n, wgs);
-    if (dtype == ESTP_F32) {
-      auto kernel = p.tile == 32   ? loss_lse_f32_kernel<32>
-                    : p.tile == 64 ? loss_lse_f32_kernel<64>
-                                   : loss_lse_f32_kernel<kFT>;
-      kernel<<<dim3(unsigned(wgs)), dim3(256), 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W), n, d,
-                                                       V, p.slices, pm, ps);
-    } else {
-      auto kernel = p.tile == 128 ? (d % 64 ? loss_lse_mfma_kernel<4, true> : loss_lse_mfma_kernel<4, false>)
-                                  : (d % 64 ? loss_lse_mfma_kernel<8, true> : loss_lse_mfma_kernel<8, false>);
-      kernel<<<dim3(unsigned((wgs + 7) / 8 * 8)), dim3(256), 0, s>>>(static_cast<const __bf16*>(X),
-                                                                     static_cast<const __bf16*>(W), n, d, V, n_tt,
-                                                                     p.slices, pm, ps);
-    }
-    ESTP_CHECK_LAUNCH("loss_lse_kernel");
+    LseStates p;
+    const int rc = launch_lse_states(fn, X, W, n, d, V, dtype, kLog2e, workspace, s, &p);
+    if (rc != ESTP_OK) return rc;
     if (dtype == ESTP_F32)
       loss_pick_kernel<float, true><<<grid, block, 0, s>>>(static_cast<const float*>(X), static_cast<const float*>(W),
-                                                           targets, n, d, V, pm, ps, p.states, lse, loss);
+                                                           targets, n, d, V, p.m, p.s, p.states, lse, loss);
     else
       loss_pick_kernel<__bf16, true><<<grid, block, 0, s>>>(static_cast<const __bf16*>(X),
-                                                            static_cast<const __bf16*>(W), targets, n, d, V, pm, ps,
+                                                            static_cast<const __bf16*>(W), targets, n, d, V, p.m, p.s,
                                                             p.states, lse, loss);
   } else {
     const int rc = launch_token_entropy(X, W, n, d, V, dtype, H, vocab_argmax, lse, workspace, s);
@@ -1108,7 +974,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
 
 extern "C" size_t estp_token_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1) return 0;
-  return carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
+  return lm_head_backward_bytes(n_tok, d, V, dtype);
 }
 
 extern "C" int estp_token_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse,
@@ -1135,7 +1001,5 @@ extern "C" int estp_token_loss_backward(const void* X, const void* W, const int3
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int n = int(n_tok);
-  auto launch = dtype == ESTP_F32 ? launch_loss_backward<float> : launch_loss_backward<__bf16>;
-  return launch(X, W, targets, lse, grad, n, d, V, dtype, dX, dW, workspace, s);
+  return launch_lm_head_backward(X, W, targets, lse, grad, int(n_tok), d, V, dtype, nullptr, dX, dW, workspace, s);
 }

@@ -1,0 +1,229 @@
+"""Log-probabilities, entropies and alternatives on the GPU against the fp64 oracle (oracle/head.py), at the bounds it
+derives; alternatives under the margin rule, and exactly where the logits are exact."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_15592_amd as estp
+from oracle import head as HD
+from oracle import operators as OP
+from tests._util import dev, host
+from tests.test_gpu_token_loss import _bits, _inputs, _wide
+
+pytestmark = pytest.mark.gpu
+
+
+def _check(X, W, t, k, temperature=1.0, **kw):
+    got = estp.token_logprobs(dev(X), dev(W), None if t is None else dev(t), k, temperature=temperature, **kw)
+    ref = HD.token_logprobs(X, W, t, k, temperature)
+    for name, a in zip(("logprob", "lse", "H"), got):
+        if a is not None:
+            over = np.abs(_wide(a) - ref[name]) - ref[name + "_bound"]
+            assert (over <= 0).all(), f"{name}: {over.max()} over the bound at row {over.argmax()}"
+    ids, top = host(got[3]), _wide(got[4])
+    assert ids.shape == top.shape == (len(X), k)
+    if k:
+        assert (ids >= 0).all() and (ids < len(W)).all()
+        assert all(len(set(r)) == k for r in ids.tolist())
+        # the j-th largest as computed is no further from the j-th largest than a logit's error, nor from its own
+        at, best = np.take_along_axis(ref["s"], ids, 1), np.take_along_axis(ref["s"], ref["top_id"], 1)
+        assert (np.abs(at - best) <= ref["margin"][:, None]).all()
+        over = np.abs(top - (at - ref["lse"][:, None])) - ref["logprob_bound"][:, None]
+        assert (over <= 0).all()
+        assert (np.diff(host(got[4]), axis=1) <= 0).all()
+    if t is not None:
+        assert (host(got[0])[(t < 0) | (t >= len(W))] == 0).all()
+    return got
+
+
+SHAPES = [(1, 32, 1, 1), (1, 64, 7, 7), (3, 32, 257, 20), (64, 96, 1000, 1), (65, 64, 256, 128), (127, 160, 4099, 5),
+          (257, 128, 8193, 33), (385, 64, 16640, 8), (1030, 64, 3001, 64)]
+
+
+@pytest.mark.parametrize("n,d,V,k", SHAPES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_and_alternatives(n, d, V, k, dtype):
+    X, W, t, _ = _inputs(n + V, n, d, V, dtype, ignored=0.2 if n > 3 else 0.0)
+    _check(X, W, t, k)
+
+
+@pytest.mark.parametrize("temperature", [0.1, 0.7, 2.0, 100.0])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_temperatures(temperature, dtype):
+    X, W, t, _ = _inputs(3, 140, 128, 3000, dtype)
+    _check(X, W, t, 12, temperature)
+
+
+@pytest.mark.parametrize("n,d,V", [(5, 8, 30), (70, 40, 300), (130, 72, 1003)])
+def test_f32_widths(n, d, V):
+    X, W, t, _ = _inputs(n, n, d, V, "f32")
+    _check(X, W, t, 9)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_without_targets_or_alternatives(dtype):
+    X, W, t, _ = _inputs(6, 90, 64, 700, dtype)
+    full = _check(X, W, t, 4)
+    bare = _check(X, W, None, 0)
+    assert bare[0] is None and torch.equal(bare[1], full[1]) and torch.equal(bare[2], full[2])
+    some = _check(X, W, None, 4)
+    assert torch.equal(some[3], full[3]) and torch.equal(some[4], full[4])
+
+
+def _exact_inputs(seed, n, d, V, dtype):
+    """Logits that are whole multiples of 2^-9 and exact in 32 bits in any order of summation: ties are frequent."""
+    g = np.random.default_rng(seed)
+    X, W = g.integers(-8, 9, (n, d)) / 8.0, g.integers(-12, 13, (V, d)) / 64.0
+    return _bits(X, dtype), _bits(W, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,d,V,k", [(1, 32, 300, 128), (33, 32, 20000, 128), (300, 64, 9000, 20), (2100, 32, 8700, 50)])
+def test_ties_go_to_the_lowest_index(n, d, V, k, dtype):
+    X, W = _exact_inputs(n, n, d, V, dtype)
+    ids, top = estp.token_logprobs(dev(X), dev(W), None, k)[3:]
+    z = OP.widen(X) @ OP.widen(W).T
+    np.testing.assert_array_equal(host(ids), np.argsort(-z, axis=1, kind="stable")[:, :k])
+    tied = np.diff(np.sort(z, axis=1)[:, ::-1][:, :k], axis=1) == 0
+    assert tied.any() and (np.diff(host(top), axis=1)[tied] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [2, 2300])
+def test_equal_logits(dtype, n):
+    # rows of zeros, as a padded batch has them: every token equally probable
+    V, k = 30000, 128
+    X, W = _bits(np.zeros((n, 32)), dtype), _bits(np.random.default_rng(1).standard_normal((V, 32)), dtype)
+    logprob, lse, H, ids, top = estp.token_logprobs(dev(X), dev(W), dev(np.full(n, 7, np.int32)), k)
+    assert torch.equal(ids, torch.arange(k, dtype=torch.int32, device="cuda").expand(n, k))
+    for a in (-logprob, lse, H, -top):
+        assert (np.abs(_wide(a) - np.log(V)) <= 64 * OP.U * np.log(V)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 700, 4200])
+@pytest.mark.parametrize("order", [1, -1])
+def test_a_vocabulary_in_order_of_its_logits(dtype, n, order):
+    # every next row of W is more (or less) probable than all before it
+    V, k = 16000, 100
+    X, W = np.zeros((n, 32)), np.zeros((V, 32))
+    X[:, 0], X[:, 1] = 1.0, 1.0 / 128
+    W[:, 0], W[:, 1] = np.arange(V) // 128 / 64.0, np.arange(V) % 128 / 64.0  # logit: v / 8192
+    ids = estp.token_logprobs(dev(_bits(X, dtype)), dev(_bits(W[::order], dtype)), None, k)[3]
+    want = np.arange(k) if order < 0 else V - 1 - np.arange(k)
+    assert (host(ids) == want).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [4, 2300])
+def test_non_finite_logits(dtype, n):
+    # a NaN row of W and one of -inf and +inf logits: NaN ranks last, its values are NaN
+    V, k = 9001, 16
+    X, W = _exact_inputs(n, n, 32, V, dtype)
+    Xd, Wd = dev(X), dev(W)
+    Xd[1:, 0] = 1.0
+    Xd[0, 0] = 0.0
+    Wd[:, 0] = 0.0
+    Wd[8500, 0] = float("-inf")
+    Xd[0] = float("nan")
+    logprob, lse, H, ids, top = estp.token_logprobs(Xd, Wd, dev(np.full(n, 5, np.int32)), k)
+    assert torch.isnan(lse[0]) and torch.isnan(logprob[0]) and torch.isnan(H[0]) and torch.isnan(top[0]).all()
+    assert torch.equal(ids[0], torch.arange(k, dtype=torch.int32, device="cuda"))
+    z = OP.widen(host(Xd.float())[1:]) @ OP.widen(np.where(np.isinf(host(Wd.float())), 0, host(Wd.float()))).T
+    z[:, 8500] = -np.inf
+    np.testing.assert_array_equal(host(ids)[1:], np.argsort(-z, axis=1, kind="stable")[:, :k])
+    for a in (logprob, lse, H, top):
+        assert torch.isfinite(a[1:]).all()
+    Wd[8500, 0], Wd[3, 0] = 0.0, float("inf")
+    ids, top = estp.token_logprobs(Xd, Wd, None, k)[3:]
+    assert (ids[1:, 0] == 3).all() and not torch.isfinite(top[1:, 0]).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [3, 200, 2500])
+def test_a_given_alternative_has_one_value(dtype, n):
+    X, W, t, _ = _inputs(17, n, 96, 5000, dtype, lean=12.0)
+    logprob, _, _, ids, top = estp.token_logprobs(dev(X), dev(W), dev(t), 30)
+    hit = ids == dev(t)[:, None]
+    assert hit.any() and torch.equal(top[hit], logprob[hit.any(dim=1)])
+
+
+def test_tokens_in_blocks_and_the_same_bits_twice():
+    # more tokens than one block; a row's values do not depend on its neighbours within a block of one size
+    n, d, V, k = 17000, 32, 2500, 10
+    X, W, t, _ = _inputs(18, n, d, V, "bf16", ignored=0.1)
+    first = _check(X, W, t, k)
+    again = estp.token_logprobs(dev(X), dev(W), dev(t), k)
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+def test_on_another_stream_with_given_outputs():
+    n, d, V, k = 300, 64, 9000, 7
+    X, W, t, _ = _inputs(19, n, d, V, "bf16")
+    want = _check(X, W, t, k)
+    out = {"logprob": torch.empty(n, device="cuda"), "lse": torch.empty(n, device="cuda"),
+           "H": torch.empty(n, device="cuda"), "top_id": torch.empty(n, k, dtype=torch.int32, device="cuda"),
+           "top_logprob": torch.empty(n, k, device="cuda")}
+    ws = torch.full((estp.load().estp_token_logprobs_workspace_size(n, d, V, k, 0),), 255, dtype=torch.uint8,
+                    device="cuda")
+    Xd, Wd, td = dev(X), dev(W), dev(t)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = estp.token_logprobs(Xd, Wd, td, k, workspace=ws, stream=side, **out)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b, c in zip(got, want, out.values()):
+        assert a is c and torch.equal(a, b)
+
+
+def test_replayed_in_a_graph():
+    n, d, V, k = 300, 64, 9000, 7
+    X, W, t, _ = _inputs(20, n, d, V, "bf16")
+    Xd, Wd, td = dev(X), dev(W), dev(t)
+    ws = torch.empty(estp.load().estp_token_logprobs_workspace_size(n, d, V, k, 0), dtype=torch.uint8, device="cuda")
+    out = estp.token_logprobs(Xd, Wd, td, k)
+    names = ("logprob", "lse", "H", "top_id", "top_logprob")
+
+    def step():
+        estp.token_logprobs(Xd, Wd, td, k, workspace=ws, **dict(zip(names, out)))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(3):
+        if rep:
+            Xd.copy_(dev(_inputs(20 + rep, n, d, V, "bf16")[0]))
+        want = estp.token_logprobs(Xd, Wd, td, k)
+        for a in out:
+            a.fill_(-1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
+
+
+def test_binding_refuses_mis_sized_tensors():
+    X, W = torch.zeros(4, 64, device="cuda"), torch.zeros(9, 64, device="cuda")
+    t, f = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    with pytest.raises(ValueError, match="targets must hold 4"):
+        estp.token_logprobs(X, W, t[:3], 2)
+    with pytest.raises(ValueError, match="disagree on d"):
+        estp.token_logprobs(X, W[:, :32].contiguous(), t, 2)
+    for name in ("logprob", "lse", "H", "top_id", "top_logprob"):
+        with pytest.raises((ValueError, TypeError), match=name):
+            estp.token_logprobs(X, W, t, 2, **{name: f[:3]})
+    with pytest.raises(ValueError, match="logprob needs targets"):
+        estp.token_logprobs(X, W, None, 2, logprob=f)
+    for k in (10, 129, -1):
+        with pytest.raises(estp.EstpError, match="k"):
+            estp.token_logprobs(X, W, t, k)
+    for temperature in (0.0, -1.0, float("nan"), float("inf")):
+        with pytest.raises(estp.EstpError, match="temperature"):
+            estp.token_logprobs(X, W, t, 2, temperature=temperature)
+    with pytest.raises(estp.EstpError, match="workspace"):
+        estp.token_logprobs(X, W, t, 2, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
