@@ -37,16 +37,26 @@ __device__ __forceinline__ u32x4_t rsrc_words(const void* base, uint32_t bytes) 
   const uint64_t a = uint64_t(base);
   return u32x4_t{uint32_t(a), uint32_t(a >> 32) & 0xffffu, bytes, 0x00020000u};
 }
+template <bool kStream = false>
 __device__ __forceinline__ void dma16(u32x4_t r, uint32_t voffset, uint32_t soffset, char* dst_wave_base) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const uint32_t m0 = uint32_t(uintptr_t((__attribute__((address_space(3))) char*)(dst_wave_base)));
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
-      "buffer_load_dwordx4 %1, %2, %3 offen lds"
-      :
-      : "s"(m0), "v"(voffset), "s"(r), "s"(soffset)
-      : "memory", "m0");
+  if constexpr (kStream)  // non-temporal: a line used once
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, %3 offen nt lds"
+        :
+        : "s"(m0), "v"(voffset), "s"(r), "s"(soffset)
+        : "memory", "m0");
+  else
+    asm volatile(
+        "s_mov_b32 m0, %0\n\t"
+        "s_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, %3 offen lds"
+        :
+        : "s"(m0), "v"(voffset), "s"(r), "s"(soffset)
+        : "memory", "m0");
 #endif
 }
 

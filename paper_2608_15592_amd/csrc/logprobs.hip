@@ -8,12 +8,6 @@
 // The logits of a block of tokens over a piece of the vocabulary are formed by the matrix cores and kept in fp32
 // (logits_mfma_kernel, logits_f32_kernel); logprob_select_kernel makes of each chunk of a row a partial state and its k
 // largest logits; logprob_merge_kernel joins a row's chunks.
-//
-// Selection: a workgroup's threads hold E logits each.  The k largest of them lie in the k threads whose own largest
-// are the largest (if a logit lay in another, k threads would hold a larger one), so the k-th largest of the threads'
-// maxima bounds them from below.  What reaches the bound, k E logits at most and few more than k as a rule, is listed
-// and ranked by comparing all pairs.  Logits are ordered by one whole number each: the logit's bits made ascending, NaN
-// below all, then the lowest index first; no two are equal, so the order in which the list is filled changes nothing.
 #include <algorithm>
 
 #include "estp_common.h"
@@ -21,23 +15,10 @@
 #include "lm_head.h"
 #include "lse_states.h"
 #include "mfma_gemm.h"
+#include "top_k.h"
 
 namespace estp {
 namespace detail {
-
-constexpr int kMaxTop = 128;
-
-// Ascending as the logits are, lower indices above higher ones; 0 is below every key.
-__device__ __forceinline__ uint64_t key_of(float z, int id) {
-  const uint32_t u = __float_as_uint(z + 0.f);  // (-0 is 0)
-  const uint32_t up = z != z ? 1u : u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
-  return uint64_t(up) << 32 | uint32_t(~id);
-}
-__device__ __forceinline__ float logit_of(uint64_t key) {
-  const uint32_t up = uint32_t(key >> 32);
-  return up == 1u ? __uint_as_float(0x7fc00000u) : __uint_as_float(up & 0x80000000u ? up ^ 0x80000000u : ~up);
-}
-__device__ __forceinline__ int id_of(uint64_t key) { return int(~uint32_t(key)); }
 
 // ------------------------------------------------------------------ logits
 
@@ -47,7 +28,7 @@ template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __restrict__ X,
                                                              const __bf16* __restrict__ W, int n, int d, int V,
                                                              int64_t v0, int Vc, float* __restrict__ Z) {
-  using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 8 * kNBN < 48 ? 8 * kNBN : 48>;
+  using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 8 * kNBN < 48 ? 8 * kNBN : 48, kNBN == 4>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
   const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
   const int n_m = (rows + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
@@ -106,46 +87,6 @@ __global__ __launch_bounds__(256, 2) void logits_f32_kernel(const float* __restr
 
 // ------------------------------------------------------------------ selection
 
-// The k largest of the workgroup's 256 kE keys (0: none), and rank 0 the largest: put(rank, key) by some thread for
-// each rank below k that has a key.  All threads call it; its LDS may be used again after a barrier.
-template <int kE>
-struct TopOf {
-  uint64_t thread_max[256], list[kMaxTop * kE];
-  uint64_t bound;
-  int count;
-
-  template <typename Put>
-  __device__ __forceinline__ void run(const uint64_t (&key)[kE], int k, Put&& put) {
-    const int tid = threadIdx.x;
-    uint64_t mine = key[0];
-#pragma unroll
-    for (int e = 1; e < kE; ++e) mine = key[e] > mine ? key[e] : mine;
-    thread_max[tid] = mine;
-    if (tid == 0) count = 0;
-    __syncthreads();
-    int rank = 0;  // among the threads; threads without a key follow in their order
-#pragma unroll 8
-    for (int t = 0; t < 256; ++t) {
-      const uint64_t other = thread_max[t];
-      rank += other > mine || (other == mine && t < tid);
-    }
-    if (rank == k - 1) bound = mine;
-    __syncthreads();
-    const uint64_t from = bound;
-#pragma unroll
-    for (int e = 0; e < kE; ++e)
-      if (key[e] != 0 && key[e] >= from) list[atomicAdd(&count, 1)] = key[e];
-    __syncthreads();
-    const int n = count;
-    for (int at = tid; at < n; at += 256) {
-      const uint64_t own = list[at];
-      int r = 0;
-      for (int t = 0; t < n; ++t) r += list[t] > own;
-      if (r < k) put(r, own);
-    }
-  }
-};
-
 __device__ __forceinline__ float exp2_arg_floor(float x) { return x < kExp2Floor ? kExp2Floor : x; }  // (NaN stays)
 
 // Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.
@@ -154,31 +95,26 @@ template <int kE>
 __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int Vc, int live, int64_t v0,
                                                              float c2, int k, int piece_chunks, int chunk0, int chunks,
                                                              float* __restrict__ part, uint64_t* __restrict__ top) {
-  __shared__ TopOf<kE> pick;
+  __shared__ TopK<kMaxTop * kE> pick;
   __shared__ float wave_m[4], wave_s[4], wave_t[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tok = blockIdx.x / piece_chunks, c = blockIdx.x % piece_chunks;
   const float* row = Z + size_t(tok) * Vc;
+  const int first = 256 * kE * c + 4 * tid;  // columns first + 1024 u + e, ascending in 4 u + e
   f32x4_t z[kE / 4];
 #pragma unroll
-  for (int u = 0; u < kE / 4; ++u) {
-    const int v = 256 * kE * c + 1024 * u + 4 * tid;
-    z[u] = v < Vc ? *reinterpret_cast<const f32x4_t*>(row + v) : f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  uint64_t key[kE];
+  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + first + 1024 * u);
   float m = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kE / 4; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int v = 256 * kE * c + 1024 * u + 4 * tid + e;
-      const bool in = v < live;
-      key[4 * u + e] = in ? key_of(z[u][e], int(v0 + v)) : 0;
-      z[u][e] = in ? z[u][e] : -INFINITY;
+      z[u][e] = first + 1024 * u + e < live ? z[u][e] : -INFINITY;
       m = fmaxf(m, z[u][e]);
     }
   m = wave_max(m);
   if (lane == 0) wave_m[wave] = m;
+  if (tid == 0) pick.count = 0;
   __syncthreads();
   m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3])) * c2;
   const float ref = fmaxf(m, -0x1p127f);
@@ -205,10 +141,26 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
     part[3 * at + 2] = wave_t[0] + wave_t[1] + wave_t[2] + wave_t[3];
   }
   if (k == 0) return;
+  uint32_t up[kE], most = 0;
+#pragma unroll
+  for (int e = 0; e < kE; ++e) {
+    up[e] = first + 1024 * (e / 4) + e % 4 < live ? ascending(z[e / 4][e % 4]) : 0;
+    most = max(most, up[e]);
+  }
+  int which = 0;
+#pragma unroll
+  for (int e = kE - 1; e >= 0; --e) which = up[e] == most ? e : which;  // the lowest
+  auto id = [&](int e) { return int(v0) + first + 1024 * (e / 4) + e % 4; };
+  const uint64_t from = pick.bound_of(most ? key_of(most, id(which)) : 0, k);
+#pragma unroll
+  for (int e = 0; e < kE; ++e)
+    if (up[e] >= uint32_t(from >> 32) && key_of(up[e], id(e)) >= from && up[e])
+      pick.list[atomicAdd(&pick.count, 1)] = key_of(up[e], id(e));
+  __syncthreads();
   uint64_t* out = top + at * k;
-  const int have = min(live - 256 * kE * c, 256 * kE);
-  if (tid >= have && tid < k) out[tid] = 0;  // (fewer columns than k)
-  pick.run(key, k, [&](int r, uint64_t v) { out[r] = v; });
+  const int n = pick.count;
+  if (tid >= n && tid < k) out[tid] = 0;  // (fewer columns than k)
+  pick.rank(n, k, [&](int r, uint64_t v) { out[r] = v; });
 }
 
 // A token's outputs from its chunks.  One workgroup each.
@@ -220,9 +172,8 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
                                                             float* __restrict__ logprob, float* __restrict__ lse,
                                                             float* __restrict__ H, int32_t* __restrict__ top_id,
                                                             float* __restrict__ top_logprob) {
-  constexpr int kE = 8;
-  __shared__ TopOf<kE> pick;
-  __shared__ uint64_t best[2][kMaxTop];
+  __shared__ TopK<2048> pick;
+  __shared__ uint64_t best[kMaxTop];
   __shared__ float wave_z[4];
   __shared__ Ent2 wave_state[4];
   __shared__ bool among;  // the given token is an alternative
@@ -252,27 +203,22 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
   z = wave_z[0] + wave_z[1] + wave_z[2] + wave_z[3];
   a = ent2_merge(ent2_merge(wave_state[0], wave_state[1]), ent2_merge(wave_state[2], wave_state[3]));
   const float l = natural_lse(a.m, a.s);
-  // the k largest of the chunks' largest, 256 kE at a time with those so far
-  int have = 0, now = 0;
-  const size_t total = size_t(chunks) * k;
-  for (size_t from = 0; from < total;) {
-    uint64_t key[kE];
-#pragma unroll
-    for (int e = 0; e < kE; ++e) {
-      const int i = 256 * e + tid;
-      const size_t at = from + size_t(i - have);
-      key[e] = i < have ? best[now][i] : at < total ? top[size_t(tok) * total + at] : 0;
-    }
-    if (tid < k) best[now ^ 1][tid] = 0;
+  // the k largest of the chunks' largest, as many at a time as the list takes with those so far
+  if (tid < k) best[tid] = 0;
+  const uint64_t* from = top + size_t(tok) * chunks * k;
+  int have = 0;
+  for (size_t at = 0, total = size_t(chunks) * k; at < total;) {
+    const int now = int(min(total - at, size_t(2048 - have)));
+    if (tid < have) pick.list[tid] = best[tid];
+    for (int i = tid; i < now; i += 256) pick.list[have + i] = from[at + i];
     __syncthreads();
-    pick.run(key, k, [&](int r, uint64_t v) { best[now ^ 1][r] = v; });
+    pick.rank(have + now, k, [&](int r, uint64_t v) { best[r] = v; });
     __syncthreads();
-    from += size_t(256 * kE - have);
-    now ^= 1;
+    at += now;
     have = k;
   }
   if (tid < k) {
-    const uint64_t key = best[now][tid];
+    const uint64_t key = best[tid];
     const float zk = logit_of(key);
     top_id[size_t(tok) * k + tid] = id_of(key);
     top_logprob[size_t(tok) * k + tid] = fmaf(zk, inv_t, -l);

@@ -114,7 +114,7 @@ __device__ __forceinline__ int first_tile(int wg, int grid) { return (wg & 7) * 
 // which its reads have room for). kNBN: 16-row blocks of a wave, N side.  kOdd: the depth may be an odd multiple of
 // 32 (both k contiguous).  kStores: vector-memory operations that done() leaves in flight at least (it ends with so
 // many stores, always): the stage after it need not wait for them.
-template <bool kAK, bool kBK, bool kPairA, int kNBN, bool kOdd, int kStores>
+template <bool kAK, bool kBK, bool kPairA, int kNBN, bool kOdd, int kStores, bool kStreamA = false>
 struct Tiles {
   static constexpr int kBN = 32 * kNBN;
   static constexpr int kLA = 8;              // transfers of a wave per part
@@ -219,7 +219,7 @@ struct Tiles {
     };
     auto dma_a = [&](const Part& p, int i) {
       const uint32_t o = kOdd && kAK && 8 * kc_a[i] >= p.depth ? kPastEnd : off_a[i];
-      dma16(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
+      dma16<kStreamA>(p.rsrc, o, p.soff, p.dst + 1024 * kWaves * i);
     };
     auto dma_b = [&](const Part& p, int i) {
       const uint32_t o = kOdd && kBK && 8 * kc_b[i] >= p.depth ? kPastEnd : off_b[i];

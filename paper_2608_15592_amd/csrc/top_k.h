@@ -1,0 +1,108 @@
+// The k largest of many logits, ties to the lowest index, by a workgroup of 256 threads (logprobs.hip).
+//
+// Every thread's largest key is known first.  The k largest keys of all lie in the k threads whose own largest are the
+// largest (if one lay in another, k threads would hold a larger one), so the k-th largest of the 256 maxima bounds them
+// from below, and at most k times a thread's keys reach the bound; a few more than k, as a rule.
+//
+// A logit is ordered by one whole number, its key: the logit's bits made ascending, NaN below all, then the lowest index
+// first.  No two keys are equal, so the order in which lists are filled changes nothing.
+#pragma once
+
+#include "estp_common.h"
+
+namespace estp {
+namespace detail {
+
+constexpr int kMaxTop = 128;
+
+// Ascending as the logits are, never 0.
+__device__ __forceinline__ uint32_t ascending(float z) {
+  const uint32_t u = __float_as_uint(z + 0.f);  // (-0 is 0)
+  return z != z ? 1u : u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint64_t key_of(uint32_t up, int id) { return uint64_t(up) << 32 | uint32_t(~id); }
+__device__ __forceinline__ float logit_of(uint64_t key) {
+  const uint32_t up = uint32_t(key >> 32);
+  return up == 1u ? __uint_as_float(0x7fc00000u) : __uint_as_float(up & 0x80000000u ? up ^ 0x80000000u : ~up);
+}
+__device__ __forceinline__ int id_of(uint64_t key) { return int(~uint32_t(key)); }
+
+// Key 0 is none.  kCap: keys of the list.
+template <int kCap>
+struct TopK {
+  uint64_t list[kCap], maxima[256], bound;
+  int count;
+
+  // The k-th largest of the threads' keys, k <= 256, or 1 where fewer threads have one.  One wave, four keys a lane,
+  // finds it bit by bit, and what lies below the logit's bits only where equal logits need it.
+  __device__ __forceinline__ uint64_t bound_of(uint64_t mine, int k) {
+    const int tid = threadIdx.x;
+    maxima[tid] = mine;
+    __syncthreads();
+    if (tid < 64) {
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint64_t v = maxima[64 * u + tid];
+        hi[u] = uint32_t(v >> 32);
+        lo[u] = uint32_t(v);
+      }
+      auto number = [&](auto&& holds) {
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) n += __popcll(__ballot(holds(u)));
+        return n;
+      };
+      uint32_t top = 0, low = 0;
+      for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+        const uint32_t c = top | bit;
+        if (number([&](int u) { return hi[u] >= c; }) >= k) top = c;
+      }
+      const int left = k - number([&](int u) { return hi[u] > top; });
+      if (top && number([&](int u) { return hi[u] == top; }) > left)
+        for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+          const uint32_t c = low | bit;
+          if (number([&](int u) { return hi[u] == top && lo[u] >= c; }) >= left) low = c;
+        }
+      if (tid == 0) bound = top ? uint64_t(top) << 32 | low : 1;
+    }
+    __syncthreads();
+    return bound;
+  }
+
+  // put(rank, key) by some thread for the k largest of the n keys listed, n <= kCap <= 4096, the largest first.  All
+  // threads call it, after a barrier; the list may be used again after one.
+  template <typename Put>
+  __device__ __forceinline__ void rank(int n, int k, Put&& put) {
+    static_assert(kCap <= 4096, "keys of a thread");
+    const int tid = threadIdx.x;
+    while (n > 256) {  // (at most k of every n / 256 stay)
+      constexpr int kE = (kCap + 255) / 256;
+      uint64_t own[kE], mine = 0;
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        own[e] = 256 * e + tid < n ? list[256 * e + tid] : 0;
+        mine = own[e] > mine ? own[e] : mine;
+      }
+      const uint64_t from = bound_of(mine, k);
+      if (tid == 0) count = 0;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < kE; ++e)
+        if (own[e] >= from) list[atomicAdd(&count, 1)] = own[e];
+      __syncthreads();
+      n = count;
+      __syncthreads();
+    }
+    if (tid < n) {
+      const uint64_t own = list[tid];
+      int r = 0;
+#pragma unroll 4
+      for (int t = 0; t < n; ++t) r += list[t] > own;
+      if (r < k) put(r, own);
+    }
+  }
+};
+
+}  // namespace detail
+}  // namespace estp
