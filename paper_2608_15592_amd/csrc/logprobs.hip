@@ -10,9 +10,11 @@
 // largest logits; logprob_merge_kernel joins a row's chunks.
 #include <algorithm>
 
+#include "ent_fold.h"
 #include "estp_common.h"
 #include "f32_gemm.h"
 #include "lm_head.h"
+#include "logprob_plan.h"
 #include "lse_states.h"
 #include "mfma_gemm.h"
 #include "top_k.h"
@@ -22,31 +24,31 @@ namespace detail {
 
 // ------------------------------------------------------------------ logits
 
-// Z[token][v] of vocabulary rows v0 .. v0 + Vc (columns past V: 0), pitch Vc.  M side: vocabulary rows.  A lane holds 8
-// consecutive vocabulary rows of a token: two 16-byte stores.
+// Z[token][v] of n_m vocabulary tiles, every `step`-th from row v0 (rows past V: 0), pitch Vc.  M side: vocabulary rows.
+// A lane holds 8 consecutive vocabulary rows of a token: two 16-byte stores.
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __restrict__ X,
                                                              const __bf16* __restrict__ W, int n, int d, int V,
-                                                             int64_t v0, int Vc, float* __restrict__ Z) {
+                                                             int64_t v0, int n_m, int step, int Vc,
+                                                             float* __restrict__ Z) {
   using Run = gemm::Tiles<true, true, true, kNBN, kOdd, 8 * kNBN < 48 ? 8 * kNBN : 48, kNBN == 4>;
   __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
-  const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
-  const int n_m = (rows + 255) / 256, n_n = (n + Run::kBN - 1) / Run::kBN;
+  const int n_n = (n + Run::kBN - 1) / Run::kBN;
   const gemm::TileOrder order(n_m, n_n);
-  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 2u, rows};
+  const gemm::Operand A{reinterpret_cast<const char*>(W + size_t(v0) * d), uint32_t(d) * 2u, int(V - v0)};
   const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 2u, n};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
   Run::run(
       lds, A, B, gemm::first_tile(blockIdx.x, gridDim.x), gridDim.x, n_m * n_n,
       [&](int id) {
         const gemm::TileAt t = order(id);
-        return gemm::Place{256 * t.m, Run::kBN * t.n, 0, d, 0};
+        return gemm::Place{256 * step * t.m, Run::kBN * t.n, 0, d, 256 * t.m};
       },
       [&](const gemm::Place& at, const f32x4_t(&acc)[8][kNBN]) {
         const int lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
         const int live = min(Run::kBN, n - at.n0);
         const buf_rsrc_t out = make_rsrc(Z + size_t(at.n0) * Vc, uint32_t(live) * uint32_t(Vc) * 4u);
-        const int c0 = at.m0 + 128 * wm + 8 * fq;
+        const int c0 = at.tag + 128 * wm + 8 * fq;
 #pragma unroll
         for (int j = 0; j < kNBN; ++j) {
           const uint32_t row = uint32_t(16 * kNBN * wn + 16 * j + fr) * uint32_t(Vc);
@@ -85,15 +87,159 @@ __global__ __launch_bounds__(256, 2) void logits_f32_kernel(const float* __restr
   }
 }
 
+// ------------------------------------------------------------------ many tokens: what may be among the largest
+//
+// With a bound of each token's k-th largest logit from a sample of the vocabulary's tiles, the products of the other
+// tiles leave behind only the logits that reach it, a quad of four rows at a time: some k V / sample of each token's V.
+// They go where all would go, and a bit says of each quad whether it was written, so there is room for any number of
+// them, nothing is counted across lanes, and no order depends on which workgroup runs first.
+
+// The next fp32 number above x (of the largest, infinity; of infinity, a NaN).
+__device__ __forceinline__ float next_up(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return __uint_as_float(u >> 31 ? u - 1 : u + 1);
+}
+
+// Workgroup (token tile, slice) takes the vocabulary tiles slice, slice + n_slices, ... of those that are not in the
+// sample (every `step`-th; step 0: no sample).  Partial states 2 slice + wave row of the last 2 n_slices of `states` a token.
+// kTop: quads that reach the logit of bounds[token k + k - 1], and their bits.
+//
+// What follows a tile's products is a branch only where a state is refolded: a quad that is not wanted is stored past the
+// end of the resource.  (With a branch and a list for each, sums were moved to memory and back: 125 us a tile of d 4096,
+// V 128256, and 93 without.)
+template <bool kOdd, bool kTop>
+__global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __restrict__ X,
+                                                              const __bf16* __restrict__ W, int n, int d, int V,
+                                                              float c2, int n_tt, int n_slices, int step, int n_main,
+                                                              int k, const uint64_t* __restrict__ bounds, int states,
+                                                              float* __restrict__ part, Quads quads) {
+  using Run = gemm::Tiles<true, true, false, 8, kOdd, kTop ? 48 : 0>;
+  __shared__ __attribute__((aligned(16))) char lds[gemm::kSlots * gemm::kSlotBytes];
+  const gemm::SliceAt wg = gemm::slice_of(gemm::first_tile(blockIdx.x, gridDim.x), n_tt, n_slices);
+  const int tt = wg.tile, slice = wg.slice;
+  if (slice >= n_slices) return;
+  const gemm::Operand A{reinterpret_cast<const char*>(W), uint32_t(d) * 2u, V};
+  const gemm::Operand B{reinterpret_cast<const char*>(X), uint32_t(d) * 2u, n};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+  const int n_mine = (n_main - slice + n_slices - 1) / n_slices;
+  const gemm::Divisor between(uint32_t(max(1, step - 1)));  // tiles between two of the sample
+  Ent2 st[8];
+  float from[8];  // what a logit has to reach
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    st[j] = Ent2{-INFINITY, 0.f, 0.f};
+    const int tok = 256 * tt + 128 * wn + 16 * j + (threadIdx.x & 15);
+    from[j] = __uint_as_float(0x7fc00000u);
+    if (kTop && tok < n) {
+      // a bound from the first tile, below all of these, has to be exceeded; one of NaN keeps whatever is not NaN out
+      const uint64_t key = bounds[size_t(tok) * k + k - 1];
+      const float z = logit_of(key);
+      from[j] = z != z ? -INFINITY : id_of(key) < 256 ? next_up(z) : z;
+    }
+  }
+  Run::run(
+      lds, A, B, 0, 1, n_mine,
+      [&](int i) {
+        const int at = slice + i * n_slices, vt = step ? at + 1 + int(between.div(uint32_t(at))) : at;
+        return gemm::Place{256 * vt, 256 * tt, 0, d, i};
+      },
+      [&](const gemm::Place& at, const f32x4_t(&acc)[8][8]) {
+        const int lane = gemm::fresh_lane(), fr = lane & 15, fq = lane >> 4;
+        const bool ragged = at.m0 + 256 > V;
+        const int lim = V - (at.m0 + 128 * wm + 4 * fq);  // live rows: 16 i + r < lim
+        const int place = slice + at.tag * n_slices;
+        const buf_rsrc_t out = make_rsrc(quads.z + (size_t(tt) * n_main + place) * kQuadTile, kTop ? kQuadTile * 4 : 0);
+        uint32_t bits[2] = {0, 0};  // byte j % 4 of bits[j / 4]: bit i
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (kTop) {
+            const uint32_t row = uint32_t(128 * wn + 16 * j + fr) * 1024u + uint32_t(128 * wm + 4 * fq) * 4u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const f32x4_t z = acc[i][j];
+              const bool hit = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) >= from[j];
+              bits[j / 4] |= hit ? 1u << (8 * (j % 4) + i) : 0u;
+              buf_store16(out, (hit ? row : 0x80000000u) + 64u * i, __builtin_bit_cast(uint4, z));
+            }
+          }
+          Ent2 e = st[j];
+          bool exact = ragged || at.tag == 0;
+          if (!exact) {
+            float s = e.s, t = e.t;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float dd = fmaf(acc[i][j][r], c2, -e.m), p = fast_exp2(dd);
+                s += p;
+                t = fmaf(p, dd, t);
+              }
+            exact = !(s <= 0x1p64f);  // (a NaN takes the exact path and stays one)
+            e.s = exact ? e.s : s;
+            e.t = exact ? e.t : t;
+          }
+          if (exact) {
+            float mx = e.m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * c2 : -INFINITY);
+            const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
+            const float dl = fmaxf(e.m - ref, kExp2Floor), sc = fast_exp2(dl);
+            float s = sc * e.s, t = sc * fmaf(e.s, dl, e.t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float dd = exp2_arg(fmaf(16 * i + r < lim ? acc[i][j][r] : -INFINITY, c2, -ref)), p = fast_exp2(dd);
+                s += p;
+                t = fmaf(p, dd, t);
+              }
+            e = Ent2{mx, s, t};
+          }
+          st[j] = e;
+        }
+        if constexpr (kTop) {
+          // lane (fq, fr) takes tokens 2 fq and 2 fq + 1 of the eight blocks: a word of each, byte q from lane (q, fr)
+          uint32_t word[2] = {0, 0};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t lo = __shfl(bits[0], 16 * q + fr, 64), hi = __shfl(bits[1], 16 * q + fr, 64);
+            const uint32_t both = (fq & 2 ? hi : lo) >> (16 * (fq & 1));
+            word[0] |= (both & 0xffu) << (8 * q);
+            word[1] |= (both >> 8 & 0xffu) << (8 * q);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const size_t tok = size_t(256) * tt + 128 * wn + 16 * (2 * fq + e) + fr;  // (whole tiles have room)
+            quads.bits[tok * (2 * n_main) + 2 * place + wm] = word[e];
+          }
+        }
+      });
+  const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int tok = 256 * tt + 128 * wn + 16 * j + fr;
+    // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same tokens
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1)
+      st[j] = ent2_merge(st[j], Ent2{__shfl_xor(st[j].m, o, 64), __shfl_xor(st[j].s, o, 64), __shfl_xor(st[j].t, o, 64)});
+    if (fq == 0 && tok < n) {
+      float* p = part + 3 * (size_t(tok) * states + states - 2 * n_slices + 2 * slice + wm);
+      p[0] = st[j].m;
+      p[1] = st[j].s;
+      p[2] = st[j].t;
+    }
+  }
+}
+
 // ------------------------------------------------------------------ selection
 
-__device__ __forceinline__ float exp2_arg_floor(float x) { return x < kExp2Floor ? kExp2Floor : x; }  // (NaN stays)
-
-// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.
-// One workgroup each.
+// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  Column
+// c is vocabulary row v0 + c, or of every `step`-th tile of 256.  One workgroup each.
 template <int kE>
 __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int Vc, int live, int64_t v0,
-                                                             float c2, int k, int piece_chunks, int chunk0, int chunks,
+                                                             int step, float c2, int k, int piece_chunks, int chunk0, int states, int chunks,
                                                              float* __restrict__ part, uint64_t* __restrict__ top) {
   __shared__ TopK<kMaxTop * kE> pick;
   __shared__ float wave_m[4], wave_s[4], wave_t[4];
@@ -123,7 +269,7 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
   for (int u = 0; u < kE / 4; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float dd = exp2_arg_floor(fmaf(z[u][e], c2, -ref)), p = fast_exp2(dd);
+      const float dd = exp2_arg(fmaf(z[u][e], c2, -ref)), p = fast_exp2(dd);
       s += p;
       t = fmaf(p, dd, t);
     }
@@ -134,11 +280,11 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
     wave_t[wave] = t;
   }
   __syncthreads();
-  const size_t at = size_t(tok) * chunks + chunk0 + c;
   if (tid == 0) {
-    part[3 * at] = m;
-    part[3 * at + 1] = wave_s[0] + wave_s[1] + wave_s[2] + wave_s[3];
-    part[3 * at + 2] = wave_t[0] + wave_t[1] + wave_t[2] + wave_t[3];
+    float* p = part + 3 * (size_t(tok) * states + chunk0 + c);
+    p[0] = m;
+    p[1] = wave_s[0] + wave_s[1] + wave_s[2] + wave_s[3];
+    p[2] = wave_t[0] + wave_t[1] + wave_t[2] + wave_t[3];
   }
   if (k == 0) return;
   uint32_t up[kE], most = 0;
@@ -150,29 +296,35 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
   int which = 0;
 #pragma unroll
   for (int e = kE - 1; e >= 0; --e) which = up[e] == most ? e : which;  // the lowest
-  auto id = [&](int e) { return int(v0) + first + 1024 * (e / 4) + e % 4; };
+  auto id = [&](int e) {
+    const int col = first + 1024 * (e / 4) + e % 4;
+    return int(v0) + (col >> 8) * 256 * step + (col & 255);
+  };
   const uint64_t from = pick.bound_of(most ? key_of(most, id(which)) : 0, k);
 #pragma unroll
   for (int e = 0; e < kE; ++e)
     if (up[e] >= uint32_t(from >> 32) && key_of(up[e], id(e)) >= from && up[e])
       pick.list[atomicAdd(&pick.count, 1)] = key_of(up[e], id(e));
   __syncthreads();
-  uint64_t* out = top + at * k;
+  uint64_t* out = top + (size_t(tok) * chunks + chunk0 + c) * k;
   const int n = pick.count;
   if (tid >= n && tid < k) out[tid] = 0;  // (fewer columns than k)
   pick.rank(n, k, [&](int r, uint64_t v) { out[r] = v; });
 }
 
-// A token's outputs from its chunks.  One workgroup each.
-template <typename T>
+// A token's outputs from its `states` partial states and from the k largest of each of its `chunks` chunks, or (kQuads)
+// from the k largest of the sample and the quads that reach them.  One workgroup each.
+template <typename T, bool kQuads>
 __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict__ X, const T* __restrict__ W,
                                                             const int32_t* __restrict__ targets, int d, int V, int k,
-                                                            float inv_t, int chunks, const float* __restrict__ part,
-                                                            const uint64_t* __restrict__ top,
+                                                            float inv_t, int states, const float* __restrict__ part,
+                                                            int chunks, const uint64_t* __restrict__ top, Quads quads,
+                                                            int n_main, int step,
                                                             float* __restrict__ logprob, float* __restrict__ lse,
                                                             float* __restrict__ H, int32_t* __restrict__ top_id,
                                                             float* __restrict__ top_logprob) {
-  __shared__ TopK<2048> pick;
+  constexpr int kCap = kQuads ? 4096 : 2048;
+  __shared__ TopK<kCap> pick;
   __shared__ uint64_t best[kMaxTop];
   __shared__ float wave_z[4];
   __shared__ Ent2 wave_state[4];
@@ -185,10 +337,9 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
   if (live)
     for (int i = 8 * tid; i < d; i += 2048) z = dot8(X + size_t(tok) * d + i, W + size_t(t) * d + i, z);
   z = wave_sum(z);
-  // the chunks' states
   Ent2 a{-INFINITY, 0.f, 0.f};
-  for (int c = tid; c < chunks; c += 256) {
-    const float* p = part + 3 * (size_t(tok) * chunks + c);
+  for (int c = tid; c < states; c += 256) {
+    const float* p = part + 3 * (size_t(tok) * states + c);
     a = ent2_merge(a, Ent2{p[0], p[1], p[2]});
   }
 #pragma unroll
@@ -203,19 +354,72 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
   z = wave_z[0] + wave_z[1] + wave_z[2] + wave_z[3];
   a = ent2_merge(ent2_merge(wave_state[0], wave_state[1]), ent2_merge(wave_state[2], wave_state[3]));
   const float l = natural_lse(a.m, a.s);
-  // the k largest of the chunks' largest, as many at a time as the list takes with those so far
   if (tid < k) best[tid] = 0;
   const uint64_t* from = top + size_t(tok) * chunks * k;
-  int have = 0;
-  for (size_t at = 0, total = size_t(chunks) * k; at < total;) {
-    const int now = int(min(total - at, size_t(2048 - have)));
-    if (tid < have) pick.list[tid] = best[tid];
-    for (int i = tid; i < now; i += 256) pick.list[have + i] = from[at + i];
+  if constexpr (kQuads) {
+    // three quads a thread and round; what exceeds the bound joins the list, which is cut to its k largest where the
+    // next round could pass its end
+    constexpr int kAhead = 3;
+    if (tid < k) pick.list[tid] = from[tid];
+    if (tid == 0) pick.count = k;
+    uint64_t bound = k > 0 ? from[k - 1] : 0;
+    const int words = k > 0 ? 2 * n_main : 0;
+    const uint32_t* bits = quads.bits + size_t(tok) * words;
+    const float* zt = quads.z + size_t(tok / 256) * n_main * kQuadTile + tok % 256 * 256;
+    int at = tid;
+    uint32_t left = at < words ? bits[at] : 0;
+    for (;;) {
+      f32x4_t z[kAhead];
+      int row[kAhead];  // its first vocabulary row, -1: none
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        while (left == 0 && at < words) {
+          at += 256;
+          left = at < words ? bits[at] : 0;
+        }
+        row[u] = -1;
+        if (left) {
+          const int b = __ffs(left) - 1, place = at >> 1, vt = place + 1 + place / (step - 1);
+          const int col = 128 * (at & 1) + 16 * (b & 7) + 4 * (b >> 3);
+          z[u] = *reinterpret_cast<const f32x4_t*>(zt + size_t(place) * kQuadTile + col);
+          row[u] = 256 * vt + col;
+          left &= left - 1;
+        }
+      }
+      if (!__syncthreads_or(row[0] >= 0)) break;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (row[u] >= 0 && row[u] + e < V) {
+            const uint64_t key = key_of(ascending(z[u][e]), row[u] + e);
+            if (key > bound) pick.list[atomicAdd(&pick.count, 1)] = key;
+          }
+      __syncthreads();
+      if (pick.count > kCap - 256 * 4 * kAhead) {
+        pick.rank(pick.count, k, [&](int r, uint64_t v) { best[r] = v; });
+        __syncthreads();
+        if (tid < k) pick.list[tid] = best[tid];
+        if (tid == 0) pick.count = k;
+        bound = best[k - 1];
+      }
+    }
     __syncthreads();
-    pick.rank(have + now, k, [&](int r, uint64_t v) { best[r] = v; });
+    if (k > 0) pick.rank(pick.count, k, [&](int r, uint64_t v) { best[r] = v; });
     __syncthreads();
-    at += now;
-    have = k;
+  } else {
+    // as many at a time as the list takes with those so far
+    int have = 0;
+    for (size_t at = 0, total = size_t(chunks) * k; at < total;) {
+      const int now = int(min(total - at, size_t(kCap - have)));
+      if (tid < have) pick.list[tid] = best[tid];
+      for (int i = tid; i < now; i += 256) pick.list[have + i] = from[at + i];
+      __syncthreads();
+      pick.rank(have + now, k, [&](int r, uint64_t v) { best[r] = v; });
+      __syncthreads();
+      at += now;
+      have = k;
+    }
   }
   if (tid < k) {
     const uint64_t key = best[tid];
@@ -235,48 +439,15 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
   }
 }
 
-// ------------------------------------------------------------------ plan and workspace
-
-// A call takes its tokens in blocks of up to kBlockToks, and a block the vocabulary in pieces of Vc rows (a multiple of
-// 8192), whose logits fit `room` floats.
-constexpr int kBlockToks = 8192;
-constexpr size_t kRoom = size_t(64) << 20;
-constexpr int kChunk = 8192;  // columns of a selecting workgroup
-constexpr int64_t kMaxPiece = int64_t(1) << 21;  // offsets of a tile's 256 tokens fit 32 bits
-
-struct LogprobPlan {
-  int Vc, chunks;
-};
-inline LogprobPlan plan_logprobs(int n, int V) {
-  const int64_t v_pad = (int64_t(V) + kChunk - 1) / kChunk * kChunk;
-  LogprobPlan p;
-  p.Vc = int(std::min({v_pad, int64_t(kRoom / size_t(n)) / kChunk * kChunk, kMaxPiece}));
-  p.chunks = int(v_pad / kChunk);
-  return p;
-}
-struct LogprobBuffers {
-  float *Z, *part;
-  uint64_t* top;
-  size_t bytes;
-};
-// At least what a call of n tokens or fewer, and of k alternatives or fewer, needs.
-inline LogprobBuffers carve_logprobs(int64_t n_tok, int V, int k, void* ws) {
-  const size_t n = size_t(std::min<int64_t>(n_tok, kBlockToks));
-  const size_t chunks = (size_t(V) + kChunk - 1) / kChunk;
-  Carver c(ws);
-  LogprobBuffers b;
-  b.Z = c.take<float>(std::min(n * chunks * kChunk, kRoom));
-  b.part = c.take<float>(3 * n * chunks);
-  b.top = c.take<uint64_t>(n * chunks * size_t(k));
-  b.bytes = c.bytes();
-  return b;
-}
+// ------------------------------------------------------------------ launches
 
 template <typename T>
-int launch_logprobs(const T* X, const T* W, const int32_t* targets, int n, int d, int V, int k, float temperature,
-                    const LogprobBuffers& b, float* logprob, float* lse, float* H, int32_t* top_id,
-                    float* top_logprob, hipStream_t s) {
-  const LogprobPlan p = plan_logprobs(n, V);
+int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, int V, int k, float temperature,
+                  void* workspace, float* logprob, float* lse, float* H, int32_t* top_id, float* top_logprob,
+                  hipStream_t s) {
+  const PiecePlan p = plan_pieces(n, V);
+  LogprobBuffers b;
+  carve_logprobs(piece_room(n, V, k), workspace, &b);
   const float c2 = base2_of_logit(temperature), inv_t = inverse_temperature(temperature);
   const dim3 block(256);
   for (int64_t v0 = 0; v0 < V; v0 += p.Vc) {
@@ -285,7 +456,7 @@ int launch_logprobs(const T* X, const T* W, const int32_t* targets, int n, int d
       const bool odd = d % 64 != 0, narrow = n <= 384;
       auto kernel = narrow ? (odd ? logits_mfma_kernel<4, true> : logits_mfma_kernel<4, false>)
                            : (odd ? logits_mfma_kernel<8, true> : logits_mfma_kernel<8, false>);
-      kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, v0, p.Vc, b.Z);
+      kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, v0, (rows + 255) / 256, 1, p.Vc, b.Z);
     } else {
       const int tile = n <= 32 ? 32 : n <= 64 ? 64 : kFT;
       auto kernel = tile == 32 ? logits_f32_kernel<32> : tile == 64 ? logits_f32_kernel<64> : logits_f32_kernel<kFT>;
@@ -295,11 +466,43 @@ int launch_logprobs(const T* X, const T* W, const int32_t* targets, int n, int d
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int in_piece = (rows + kChunk - 1) / kChunk;
     logprob_select_kernel<kChunk / 256><<<dim3(unsigned(n) * unsigned(in_piece)), block, 0, s>>>(
-        b.Z, p.Vc, rows, v0, c2, k, in_piece, int(v0 / kChunk), p.chunks, b.part, b.top);
+        b.Z, p.Vc, rows, v0, 1, c2, k, in_piece, int(v0 / kChunk), p.chunks, p.chunks, b.part, b.top);
     ESTP_CHECK_LAUNCH("logprob_select_kernel");
   }
-  logprob_merge_kernel<T><<<dim3(unsigned(n)), block, 0, s>>>(X, W, targets, d, V, k, inv_t, p.chunks, b.part, b.top,
-                                                              logprob, lse, H, top_id, top_logprob);
+  logprob_merge_kernel<T, false><<<dim3(unsigned(n)), block, 0, s>>>(X, W, targets, d, V, k, inv_t, p.chunks, b.part,
+                                                                     p.chunks, b.top, b.quads, 0, 0, logprob, lse, H,
+                                                                     top_id, top_logprob);
+  ESTP_CHECK_LAUNCH("logprob_merge_kernel");
+  return ESTP_OK;
+}
+
+int launch_quads(const __bf16* X, const __bf16* W, const int32_t* targets, int n, int d, int V, int k,
+                 float temperature, void* workspace, float* logprob, float* lse, float* H, int32_t* top_id,
+                 float* top_logprob, hipStream_t s) {
+  const QuadPlan p = plan_quads(n, V, k);
+  LogprobBuffers b;
+  carve_logprobs(quad_room(n, p, k), workspace, &b);
+  const float c2 = base2_of_logit(temperature), inv_t = inverse_temperature(temperature);
+  const bool odd = d % 64 != 0;
+  const dim3 block(256);
+  const int states = (k > 0) + 2 * p.slices, n_tt = (n + 255) / 256;
+  if (k > 0) {
+    auto kernel = odd ? logits_mfma_kernel<8, true> : logits_mfma_kernel<8, false>;
+    kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, 0, p.sample, p.step, 256 * kSampleTiles, b.Z);
+    ESTP_CHECK_LAUNCH("logits_kernel");
+    const int live = 256 * (p.sample - 1) + std::min(256, V - 256 * p.step * (p.sample - 1));
+    logprob_select_kernel<kSampleTiles><<<dim3(unsigned(n)), block, 0, s>>>(b.Z, 256 * kSampleTiles, live, 0, p.step, c2,
+                                                                            k, 1, 0, states, 1, b.part, b.top);
+    ESTP_CHECK_LAUNCH("logprob_select_kernel");
+  }
+  auto main = k > 0 ? (odd ? logprob_main_kernel<true, true> : logprob_main_kernel<false, true>)
+                    : (odd ? logprob_main_kernel<true, false> : logprob_main_kernel<false, false>);
+  main<<<dim3(unsigned((n_tt * p.slices + 7) / 8 * 8)), block, 0, s>>>(X, W, n, d, V, c2, n_tt, p.slices, p.step,
+                                                                       p.n_main, k, b.top, states, b.part, b.quads);
+  ESTP_CHECK_LAUNCH("logprob_main_kernel");
+  logprob_merge_kernel<__bf16, true><<<dim3(unsigned(n)), block, 0, s>>>(X, W, targets, d, V, k, inv_t, states, b.part,
+                                                                         1, b.top, b.quads, p.n_main, p.step, logprob, lse,
+                                                                         H, top_id, top_logprob);
   ESTP_CHECK_LAUNCH("logprob_merge_kernel");
   return ESTP_OK;
 }
@@ -311,9 +514,8 @@ using namespace estp;
 using namespace estp::detail;
 
 extern "C" size_t estp_token_logprobs_workspace_size(int64_t n_tok, int32_t d, int32_t V, int32_t k, int dtype) {
-  (void)dtype;
   if (n_tok < 1 || d < 1 || V < 1 || V > (1 << 24) || k < 0 || k > kMaxTop) return 0;
-  return carve_logprobs(n_tok, V, k, nullptr).bytes;
+  return logprob_bytes(n_tok, V, k, dtype);
 }
 
 extern "C" int estp_token_logprobs(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d,
@@ -343,16 +545,21 @@ extern "C" int estp_token_logprobs(const void* X, const void* W, const int32_t* 
   ESTP_REQUIRE(workspace && aligned(workspace, 256), ESTP_ERR_INVALID_ARG,
                "%s: workspace must be non-null and 256-byte aligned", fn);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const LogprobBuffers b = carve_logprobs(n_tok, V, k, workspace);
-  for (int64_t at = 0; at < n_tok; at += kBlockToks) {
-    const int n = int(std::min<int64_t>(kBlockToks, n_tok - at));
-    auto go = [&](auto* x, auto* w) {
-      return launch_logprobs(x + size_t(at) * d, w, targets ? targets + at : nullptr, n, d, V, k, temperature, b,
-                             logprob ? logprob + at : nullptr, lse ? lse + at : nullptr, H ? H + at : nullptr,
-                             top_id ? top_id + at * k : nullptr, top_logprob ? top_logprob + at * k : nullptr, s);
+  const bool quads = use_quads(n_tok, V, dtype);
+  // blocks of the same size, in whole tiles
+  const int64_t most = quads ? kQuadToks : kBlockToks, blocks = (n_tok + most - 1) / most;
+  const int64_t each = std::min(most, ((n_tok + blocks - 1) / blocks + 255) / 256 * 256);
+  for (int64_t at = 0; at < n_tok; at += each) {
+    const int n = int(std::min(each, n_tok - at));
+    auto go = [&](auto launch, auto* x, auto* w) {
+      return launch(x + size_t(at) * d, w, targets ? targets + at : nullptr, n, d, V, k, temperature, workspace,
+                    logprob ? logprob + at : nullptr, lse ? lse + at : nullptr, H ? H + at : nullptr,
+                    top_id ? top_id + at * k : nullptr, top_logprob ? top_logprob + at * k : nullptr, s);
     };
-    const int rc = dtype == ESTP_F32 ? go(static_cast<const float*>(X), static_cast<const float*>(W))
-                                     : go(static_cast<const __bf16*>(X), static_cast<const __bf16*>(W));
+    const __bf16 *x = static_cast<const __bf16*>(X), *w = static_cast<const __bf16*>(W);
+    const int rc = quads                ? go(launch_quads, x, w)
+                   : dtype == ESTP_BF16 ? go(launch_pieces<__bf16>, x, w)
+                                        : go(launch_pieces<float>, static_cast<const float*>(X), static_cast<const float*>(W));
     if (rc != ESTP_OK) return rc;
   }
   return ESTP_OK;

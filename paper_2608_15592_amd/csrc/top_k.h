@@ -70,11 +70,10 @@ struct TopK {
     return bound;
   }
 
-  // put(rank, key) by some thread for the k largest of the n keys listed, n <= kCap <= 4096, the largest first.  All
+  // put(rank, key) by some thread for the k largest of the n keys listed, n <= kCap, the largest first.  All
   // threads call it, after a barrier; the list may be used again after one.
   template <typename Put>
   __device__ __forceinline__ void rank(int n, int k, Put&& put) {
-    static_assert(kCap <= 4096, "keys of a thread");
     const int tid = threadIdx.x;
     while (n > 256) {  // (at most k of every n / 256 stay)
       constexpr int kE = (kCap + 255) / 256;

@@ -8,6 +8,7 @@ import paper_2608_15592_amd as estp
 from oracle import head as HD
 from oracle import operators as OP
 from tests._util import dev, host
+from tests.test_gpu_operators_workspace import Guarded
 from tests.test_gpu_token_loss import _bits, _inputs, _wide
 
 pytestmark = pytest.mark.gpu
@@ -101,17 +102,70 @@ def test_equal_logits(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n", [3, 700, 4200])
+@pytest.mark.parametrize("n,V", [(3, 16000), (700, 16000), (385, 40001), (2305, 33000)])
 @pytest.mark.parametrize("order", [1, -1])
-def test_a_vocabulary_in_order_of_its_logits(dtype, n, order):
-    # every next row of W is more (or less) probable than all before it
-    V, k = 16000, 100
-    X, W = np.zeros((n, 32)), np.zeros((V, 32))
-    X[:, 0], X[:, 1] = 1.0, 1.0 / 128
-    W[:, 0], W[:, 1] = np.arange(V) // 128 / 64.0, np.arange(V) % 128 / 64.0  # logit: v / 8192
+def test_a_vocabulary_in_order_of_its_logits(dtype, n, V, order):
+    # every next row of W is more (or less) probable than all before it: no bound from a sample keeps any out for long
+    k = 100
+    X, W, v = np.zeros((n, 32)), np.zeros((V, 32)), np.arange(V)
+    X[:, 0], X[:, 1], X[:, 2] = 1.0, 1.0 / 128, 1.0 / 16384
+    W[:, 0], W[:, 1], W[:, 2] = v >> 14, v >> 7 & 127, v & 127  # logit: v / 16384
     ids = estp.token_logprobs(dev(_bits(X, dtype)), dev(_bits(W[::order], dtype)), None, k)[3]
     want = np.arange(k) if order < 0 else V - 1 - np.arange(k)
     assert (host(ids) == want).all()
+
+
+# many tokens of bf16 and a large vocabulary: bounds from a sample of its tiles, the last of them short or whole
+LARGE = [(385, 32, 33000, 20), (400, 96, 32768, 1), (1500, 64, 33001, 128), (2048, 32, 40000, 64), (2300, 64, 36097, 5),
+         (500, 32, 70000, 33), (513, 64, 33000, 0)]
+
+
+@pytest.mark.parametrize("n,d,V,k", LARGE)
+def test_large_vocabularies(n, d, V, k):
+    X, W, t, _ = _inputs(n + V, n, d, V, "bf16", ignored=0.2)
+    ws = Guarded(estp.load().estp_token_logprobs_workspace_size(n, d, V, k, 0))
+    got = _check(X, W, t, k, 1.3, workspace=ws.ws)
+    ws.check()
+    again = estp.token_logprobs(dev(X), dev(W), dev(t), k, 1.3)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("n,larger", [(385, 2048), (1, 2500), (384, 385), (700, 20000), (2049, 4000)])
+def test_on_a_larger_calls_workspace(n, larger):
+    d, V, k = 32, 33000, 30
+    X, W, t, _ = _inputs(n, n, d, V, "bf16")
+    want = estp.token_logprobs(dev(X), dev(W), dev(t), k)
+    ws = Guarded(estp.load().estp_token_logprobs_workspace_size(larger, d, V, 40, 0))
+    got = estp.token_logprobs(dev(X), dev(W), dev(t), k, workspace=ws.ws)
+    ws.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("n,V,k", [(600, 33000, 128), (2100, 33000, 20), (400, 60000, 1)])
+def test_ties_of_large_vocabularies(n, V, k):
+    X, W = _exact_inputs(n, n, 32, V, "bf16")
+    X[5] = 0
+    ids = estp.token_logprobs(dev(X), dev(W), None, k)[3]
+    z = OP.widen(X) @ OP.widen(W).T
+    np.testing.assert_array_equal(host(ids), np.argsort(-z, axis=1, kind="stable")[:, :k])
+
+
+def test_non_finite_logits_of_large_vocabularies():
+    # infinities and NaN within and outside of the sample, one row NaN throughout
+    n, V, k = 500, 33000, 16
+    X, W = _exact_inputs(n, n, 32, V, "bf16")
+    Xd, Wd = dev(X), dev(W)
+    Xd[:, 0], Wd[:, 0] = 1.0, 0.0
+    low, nan = [0, 300, 20000, 32999], [5, 700, 32998]
+    Wd[low, 0], Wd[nan, 0] = float("-inf"), float("nan")
+    Xd[7] = float("nan")
+    _, lse, _, ids, _ = estp.token_logprobs(Xd, Wd, None, k)
+    assert torch.isnan(lse).all() and torch.equal(ids[7], torch.arange(k, dtype=torch.int32, device="cuda"))
+    z = OP.widen(host(Xd.float())) @ OP.widen(np.nan_to_num(host(Wd.float()), nan=0.0, neginf=0.0)).T
+    z[:, low + nan] = -np.inf
+    want = np.argsort(-z, axis=1, kind="stable")[:, :k]
+    keep = np.arange(n) != 7
+    np.testing.assert_array_equal(host(ids)[keep], want[keep])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

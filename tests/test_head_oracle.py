@@ -1,6 +1,7 @@
 """The fp64 oracle of the log-probability calls pinned against hand-computed values, differences and its own symmetries;
 their refusals on the host; their workspaces."""
-import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -9,6 +10,7 @@ import torch
 import paper_2608_15592_amd as estp
 from oracle import head as HD
 from oracle import operators as OP
+from paper_2608_15592_amd import build
 from tests.test_operators_abi import FAKE, HALF, ODD, WS, _caller
 from tests.test_operators_workspace import HEADS, TOKENS, _never_less
 
@@ -140,3 +142,14 @@ def test_workspaces_grow_with_the_tokens(d, V, dtype):
         _never_less(lambda n: lib.estp_token_logprobs_workspace_size(n, d, V, k, dtype), TOKENS)
     for n in (1, 100, 5000):
         _never_less(lambda k: lib.estp_token_logprobs_workspace_size(n, d, V, k, dtype), range(129))
+
+
+def test_plans_of_log_probability_calls(tmp_path):
+    exe = str(tmp_path / "logprob_plan")
+    here = os.path.dirname(os.path.abspath(__file__))
+    cmd = [build.hipcc(), f"--offload-arch={build.ARCH}", "-O1", "-std=c++17", f"-I{build.INCLUDE}", f"-I{build.CSRC}",
+           os.path.join(here, "host", "logprob_plan.hip"), "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stdout + r.stderr
