@@ -100,6 +100,24 @@ __device__ __forceinline__ float next_up(float x) {
   return __uint_as_float(u >> 31 ? u - 1 : u + 1);
 }
 
+// The largest of four sums (a NaN only of four).
+__device__ __forceinline__ float largest(const float (&z)[4]) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  float m;  // (fmaxf would make each operand canonical first)
+  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max_f32 %0, %0, %4" : "=&v"(m) : "v"(z[0]), "v"(z[1]), "v"(z[2]), "v"(z[3]));
+  return m;
+#else
+  return z[0];
+#endif
+}
+// A number formed by now: what it is made of is not kept for later.
+__device__ __forceinline__ uint32_t settled(uint32_t v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#endif
+  return v;
+}
+
 // Workgroup (token tile, slice) takes the vocabulary tiles slice, slice + n_slices, ... of those that are not in the
 // sample (every `step`-th; step 0: no sample).  Partial states 2 slice + wave row of the last 2 n_slices of `states` a token.
 // kTop: quads that reach the logit of bounds[token k + k - 1], and their bits.
@@ -150,17 +168,25 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
         const int place = slice + at.tag * n_slices;
         const buf_rsrc_t out = make_rsrc(quads.z + (size_t(tt) * n_main + place) * kQuadTile, kTop ? kQuadTile * 4 : 0);
         uint32_t bits[2] = {0, 0};  // byte j % 4 of bits[j / 4]: bit i
+        gemm::sums_ready();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
+          float z[8][4];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[i][r] = gemm::read_sum(acc[i][j][r]);
           if constexpr (kTop) {
             const uint32_t row = uint32_t(128 * wn + 16 * j + fr) * 1024u + uint32_t(128 * wm + 4 * fq) * 4u;
+            uint32_t mine = bits[j / 4];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-              const f32x4_t z = acc[i][j];
-              const bool hit = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])) >= from[j];
-              bits[j / 4] |= hit ? 1u << (8 * (j % 4) + i) : 0u;
-              buf_store16(out, (hit ? row : 0x80000000u) + 64u * i, __builtin_bit_cast(uint4, z));
+              const bool hit = largest(z[i]) >= from[j];
+              mine |= hit ? 1u << (8 * (j % 4) + i) : 0u;
+              buf_store16(out, (hit ? row : 0x80000000u) + 64u * i,
+                          __builtin_bit_cast(uint4, f32x4_t{z[i][0], z[i][1], z[i][2], z[i][3]}));
             }
+            bits[j / 4] = settled(mine);
           }
           Ent2 e = st[j];
           bool exact = ragged || at.tag == 0;
@@ -170,7 +196,7 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
             for (int i = 0; i < 8; ++i)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float dd = fmaf(acc[i][j][r], c2, -e.m), p = fast_exp2(dd);
+                const float dd = fmaf(z[i][r], c2, -e.m), p = fast_exp2(dd);
                 s += p;
                 t = fmaf(p, dd, t);
               }
@@ -183,7 +209,7 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * c2 : -INFINITY);
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? z[i][r] * c2 : -INFINITY);
             const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
             const float dl = fmaxf(e.m - ref, kExp2Floor), sc = fast_exp2(dl);
             float s = sc * e.s, t = sc * fmaf(e.s, dl, e.t);
@@ -191,7 +217,7 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
             for (int i = 0; i < 8; ++i)
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                const float dd = exp2_arg(fmaf(16 * i + r < lim ? acc[i][j][r] : -INFINITY, c2, -ref)), p = fast_exp2(dd);
+                const float dd = exp2_arg(fmaf(16 * i + r < lim ? z[i][r] : -INFINITY, c2, -ref)), p = fast_exp2(dd);
                 s += p;
                 t = fmaf(p, dd, t);
               }

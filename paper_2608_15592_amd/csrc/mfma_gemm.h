@@ -84,6 +84,24 @@ struct TileOrder {
 struct Place {
   int m0, n0, k0, k1, tag;
 };
+// A sum where the matrix cores left it, copied to a register that the vector units read: here, and not before.  (Left to
+// the compiler, all 256 sums of a lane are copied at the end of the products, and what has no room goes to memory.)  The
+// first of them follows sums_ready().
+__device__ __forceinline__ float read_sum(float a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  float v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(a));
+  return v;
+#else
+  return a;
+#endif
+}
+// The last products are done: 18 wait states, which the compiler does not count for reads it cannot see.
+__device__ __forceinline__ void sums_ready() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+#endif
+}
 // This lane's number, formed anew: what done() derives from it is not kept in registers through the products.
 __device__ __forceinline__ int fresh_lane() {
   int lane = threadIdx.x & 63;
