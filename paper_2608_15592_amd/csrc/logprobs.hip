@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
                                                             float* __restrict__ logprob, float* __restrict__ lse,
                                                             float* __restrict__ H, int32_t* __restrict__ top_id,
                                                             float* __restrict__ top_logprob) {
-  constexpr int kCap = kQuads ? 4096 : 2048;
+  constexpr int kCap = kQuads ? 3072 : 2048;
   __shared__ TopK<kCap> pick;
   __shared__ uint64_t best[kMaxTop];
   __shared__ float wave_z[4];
@@ -383,51 +383,85 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
   if (tid < k) best[tid] = 0;
   const uint64_t* from = top + size_t(tok) * chunks * k;
   if constexpr (kQuads) {
-    // three quads a thread and round; what exceeds the bound joins the list, which is cut to its k largest where the
-    // next round could pass its end
-    constexpr int kAhead = 3;
+    // A thread reads the bits of up to kWords half tiles, and lists their quads; then the threads share these out,
+    // kAhead each and round.  What exceeds the bound joins the keys, which are cut to the k largest where the next round
+    // could pass their end.  (Quads that do not fit their list are taken by the thread that read their bits.)
+    constexpr int kWords = 4, kAhead = 2, kCodes = 1536;
+    __shared__ uint32_t code[kCodes];
+    __shared__ int codes;
     if (tid < k) pick.list[tid] = from[tid];
     if (tid == 0) pick.count = k;
     uint64_t bound = k > 0 ? from[k - 1] : 0;
     const int words = k > 0 ? 2 * n_main : 0;
     const uint32_t* bits = quads.bits + size_t(tok) * words;
     const float* zt = quads.z + size_t(tok / 256) * n_main * kQuadTile + tok % 256 * 256;
-    int at = tid;
-    uint32_t left = at < words ? bits[at] : 0;
-    for (;;) {
-      f32x4_t z[kAhead];
-      int row[kAhead];  // its first vocabulary row, -1: none
+    for (int w0 = 0; w0 < words; w0 += 256 * kWords) {
+      uint32_t left[kWords];
+      int n = 0;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        while (left == 0 && at < words) {
-          at += 256;
-          left = at < words ? bits[at] : 0;
-        }
-        row[u] = -1;
-        if (left) {
-          const int b = __ffs(left) - 1, place = at >> 1, vt = place + 1 + place / (step - 1);
-          const int col = 128 * (at & 1) + 16 * (b & 7) + 4 * (b >> 3);
-          z[u] = *reinterpret_cast<const f32x4_t*>(zt + size_t(place) * kQuadTile + col);
-          row[u] = 256 * vt + col;
-          left &= left - 1;
-        }
+      for (int u = 0; u < kWords; ++u) {
+        left[u] = w0 + 256 * u + tid < words ? bits[w0 + 256 * u + tid] : 0;
+        n += __popc(left[u]);
       }
-      if (!__syncthreads_or(row[0] >= 0)) break;
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (row[u] >= 0 && row[u] + e < V) {
-            const uint64_t key = key_of(ascending(z[u][e]), row[u] + e);
-            if (key > bound) pick.list[atomicAdd(&pick.count, 1)] = key;
-          }
+      if (tid == 0) codes = 0;
       __syncthreads();
-      if (pick.count > kCap - 256 * 4 * kAhead) {
-        pick.rank(pick.count, k, [&](int r, uint64_t v) { best[r] = v; });
+      int at = n > 0 ? atomicAdd(&codes, n) : 0;
+#pragma unroll
+      for (int u = 0; u < kWords; ++u)
+        for (; left[u] && at < kCodes; ++at) {
+          const uint32_t b = __ffs(left[u]) - 1;
+          code[at] = uint32_t(256 * u + tid) << 5 | b;
+          left[u] &= left[u] - 1;
+        }
+      __syncthreads();
+      const int listed = min(codes, kCodes);
+      bool more = false;
+#pragma unroll
+      for (int u = 0; u < kWords; ++u) more |= left[u] != 0;
+      for (int c0 = 0; __syncthreads_or(c0 < listed || more); c0 += 256 * kAhead) {
+        f32x4_t z[kAhead];
+        int row[kAhead];  // its first vocabulary row, -1: none
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int c = c0 + 256 * u + tid;
+          uint32_t own = 0xffffffffu;
+          if (c < listed) {
+            own = code[c];
+          } else if (c0 >= listed && more) {
+            more = false;
+#pragma unroll
+            for (int w = kWords - 1; w >= 0; --w)
+              if (left[w]) own = uint32_t(256 * w + tid) << 5 | uint32_t(__ffs(left[w]) - 1);
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) {
+              if (int(own >> 5) == 256 * w + tid) left[w] &= left[w] - 1;
+              more |= left[w] != 0;
+            }
+          }
+          row[u] = -1;
+          if (own != 0xffffffffu) {
+            const int word = w0 + int(own >> 5), b = int(own & 31u), place = word >> 1;
+            const int col = 128 * (word & 1) + 16 * (b & 7) + 4 * (b >> 3);
+            z[u] = *reinterpret_cast<const f32x4_t*>(zt + size_t(place) * kQuadTile + col);
+            row[u] = 256 * (place + 1 + place / (step - 1)) + col;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (row[u] >= 0 && row[u] + e < V) {
+              const uint64_t key = key_of(ascending(z[u][e]), row[u] + e);
+              if (key > bound) pick.list[atomicAdd(&pick.count, 1)] = key;
+            }
         __syncthreads();
-        if (tid < k) pick.list[tid] = best[tid];
-        if (tid == 0) pick.count = k;
-        bound = best[k - 1];
+        if (pick.count > kCap - 256 * 4 * kAhead) {
+          pick.rank(pick.count, k, [&](int r, uint64_t v) { best[r] = v; });
+          __syncthreads();
+          if (tid < k) pick.list[tid] = best[tid];
+          if (tid == 0) pick.count = k;
+          bound = best[k - 1];
+        }
       }
     }
     __syncthreads();

@@ -392,15 +392,21 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
         const int fq = gemm::fresh_lane() >> 4;
         const int lim = V - (at.m0 + 128 * wm + 4 * fq);  // live rows: 16 i + r < lim
         const bool ragged = at.m0 + 256 > V;
+        gemm::sums_ready();
 #pragma unroll
         for (int j = 0; j < kNBN; ++j) {
+          float z[8][4];
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z[i][r] = gemm::read_sum(acc[i][j][r]);
           bool exact = ragged || at.tag == 0;
           if (!exact) {
             float s = l[j];
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) s += fast_exp2(fmaf(acc[i][j][r], c2, -m[j]));
+              for (int r = 0; r < 4; ++r) s += fast_exp2(fmaf(z[i][r], c2, -m[j]));
             exact = !(s <= 0x1p64f);  // (a NaN takes the exact path and stays one)
             l[j] = exact ? l[j] : s;
           }
@@ -409,14 +415,14 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][j][r] * c2 : -INFINITY);
+              for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? z[i][r] * c2 : -INFINITY);
             const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
             float s = l[j] * fast_exp2(fmaxf(m[j] - ref, kExp2Floor));
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                s += 16 * i + r < lim ? fast_exp2(fmaf(acc[i][j][r], c2, -ref)) : 0.f;
+                s += 16 * i + r < lim ? fast_exp2(fmaf(z[i][r], c2, -ref)) : 0.f;
             m[j] = mx;
             l[j] = s;
           }
