@@ -9,10 +9,12 @@
 // (logits_mfma_kernel, logits_f32_kernel); logprob_select_kernel makes of each chunk of a row a partial state and its k
 // largest logits; logprob_merge_kernel joins a row's chunks.
 #include <algorithm>
+#include <type_traits>
 
 #include "ent_fold.h"
 #include "estp_common.h"
 #include "f32_gemm.h"
+#include "few_tokens.h"
 #include "lm_head.h"
 #include "logprob_plan.h"
 #include "lse_states.h"
@@ -58,6 +60,20 @@ __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __res
                         __builtin_bit_cast(uint4, acc[i][j]));
         }
       });
+}
+
+// Z[token][v] of few tokens and all of the vocabulary.
+template <int kSteps, int kNB>
+__global__ __launch_bounds__(64 * few::kWaves, 2) void logits_few_kernel(const __bf16* __restrict__ X,
+                                                                         const __bf16* __restrict__ W, int n, int d,
+                                                                         int V, int Vc, float* __restrict__ Z) {
+  __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
+  const int tok = threadIdx.x / 64 * 16 + (threadIdx.x & 15);
+  const buf_rsrc_t out = make_rsrc(Z, uint32_t(n) * uint32_t(Vc) * 4u);
+  const uint32_t base = uint32_t(tok) * uint32_t(Vc) * 4u;
+  few::run<kSteps, kNB, 1>(X, W, n, d, V, lds, [&](int64_t row, f32x4_t z) {
+    buf_store16(out, tok < n ? base + uint32_t(row) * 4u : kPastEnd, __builtin_bit_cast(uint4, z));
+  });
 }
 
 template <int kTN>
@@ -513,10 +529,17 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
   for (int64_t v0 = 0; v0 < V; v0 += p.Vc) {
     const int rows = int(std::min<int64_t>(V - v0, p.Vc));
     if constexpr (sizeof(T) == 2) {
-      const bool odd = d % 64 != 0, narrow = n <= 384;
-      auto kernel = narrow ? (odd ? logits_mfma_kernel<4, true> : logits_mfma_kernel<4, false>)
-                           : (odd ? logits_mfma_kernel<8, true> : logits_mfma_kernel<8, false>);
-      kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, v0, (rows + 255) / 256, 1, p.Vc, b.Z);
+      if (p.Vc >= V && few::takes(n, d, ESTP_BF16)) {
+        few::choose(n, d, [&](auto steps, auto nb) {
+          logits_few_kernel<decltype(steps)::value, decltype(nb)::value>
+              <<<dim3(few::workgroups(V)), dim3(64 * few::kWaves), 0, s>>>(X, W, n, d, V, p.Vc, b.Z);
+        });
+      } else {
+        const bool odd = d % 64 != 0, narrow = n <= 384;
+        auto kernel = narrow ? (odd ? logits_mfma_kernel<4, true> : logits_mfma_kernel<4, false>)
+                             : (odd ? logits_mfma_kernel<8, true> : logits_mfma_kernel<8, false>);
+        kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, v0, (rows + 255) / 256, 1, p.Vc, b.Z);
+      }
     } else {
       const int tile = n <= 32 ? 32 : n <= 64 ? 64 : kFT;
       auto kernel = tile == 32 ? logits_f32_kernel<32> : tile == 64 ? logits_f32_kernel<64> : logits_f32_kernel<kFT>;

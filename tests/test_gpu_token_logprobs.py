@@ -115,6 +115,44 @@ def test_a_vocabulary_in_order_of_its_logits(dtype, n, V, order):
     assert (host(ids) == want).all()
 
 
+# few tokens, whose part of the depth stays in registers; vocabularies that end within a tile of 16 rows, fewer tiles than
+# compute units, and several rounds of them
+FEW = [(1, 1024, 5000), (16, 1024, 9001), (17, 1024, 77), (64, 1024, 4100), (5, 1536, 8197), (33, 1536, 4097),
+       (64, 1536, 12300), (2, 2048, 16400), (31, 2048, 5003), (50, 2048, 4099), (9, 2560, 4500), (32, 2560, 4500),
+       (40, 2560, 4500), (16, 3584, 4111), (20, 3584, 5000), (1, 4096, 4600), (16, 4096, 8200), (32, 4096, 4097),
+       (33, 4096, 4097), (12, 512, 3000), (12, 4352, 3000)]
+
+
+@pytest.mark.parametrize("n,d,V", FEW)
+def test_few_tokens(n, d, V):
+    X, W, t, _ = _inputs(n + d, n, d, V, "bf16", lean=3.0)
+    ws = Guarded(estp.load().estp_token_logprobs_workspace_size(n, d, V, 6, 0))
+    got = _check(X, W, t, 6, 0.9, workspace=ws.ws)
+    ws.check()
+    again = estp.token_logprobs(dev(X), dev(W), dev(t), 6, 0.9)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+@pytest.mark.parametrize("n", [1, 20, 60])
+def test_a_non_finite_row_of_weights_stays_in_its_row(n):
+    d, V = 2048, 5000
+    X, W, _, _ = _inputs(n, n, d, V, "bf16")
+    want = estp.token_logprobs(dev(X), dev(W), None, 5)
+    low = np.argmin(OP.widen(X) @ OP.widen(W).T, axis=1)[0]  # not an alternative of any row's, or of few
+    Wd = dev(W)
+    for at in (0, 1, d // 8, d - 1):  # in each wave's eighth
+        Wd[low] = dev(W)[low]
+        Wd[low, at] = -float("inf")
+        Xd = dev(X)
+        Xd[:, at] = 1.0
+        ids = estp.token_logprobs(Xd, Wd, None, 5)[3]
+        z = OP.widen(host(Xd.float())) @ OP.widen(W).T
+        z[:, low] = -np.inf
+        best, margin = np.sort(z, axis=1)[:, ::-1][:, :5], 2 * OP.logit_bound(host(Xd.float()), W)
+        assert (np.abs(np.take_along_axis(z, host(ids), 1) - best) <= margin[:, None]).all()
+    assert want[3].shape == (n, 5)
+
+
 # many tokens of bf16 and a large vocabulary: bounds from a sample of its tiles, the last of them short or whole
 LARGE = [(385, 32, 33000, 20), (400, 96, 32768, 1), (1500, 64, 33001, 128), (2048, 32, 40000, 64), (2300, 64, 36097, 5),
          (500, 32, 70000, 33), (513, 64, 33000, 0)]
