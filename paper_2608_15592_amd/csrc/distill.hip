@@ -20,6 +20,7 @@
 #include <algorithm>
 
 #include "estp_common.h"
+#include "few_tokens.h"
 #include "lm_head.h"
 #include "lse_states.h"
 
@@ -65,6 +66,42 @@ __device__ __forceinline__ TeacherRow teacher_row(const int32_t* __restrict__ id
   }
   r.mass = wave_sum(r.p[0] + r.p[1]);
   return r;
+}
+
+// Partial (maximum, sum) states in base 2 of few tokens' logits times c2, one of each workgroup.
+template <int kSteps, int kNB>
+__global__ __launch_bounds__(64 * few::kWaves, 2) void distill_lse_few_kernel(const __bf16* __restrict__ X,
+                                                                              const __bf16* __restrict__ W, int n,
+                                                                              int d, int V, float c2,
+                                                                              float* __restrict__ part_m,
+                                                                              float* __restrict__ part_s) {
+  __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
+  float m = -INFINITY, s = 0.f;
+  few::run<kSteps, kNB, 0>(X, W, n, d, V, lds, [&](int64_t row, f32x4_t z) {
+    float mx = m, zc[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      zc[r] = row + r < V ? z[r] * c2 : -INFINITY;
+      mx = fmaxf(mx, zc[r]);
+    }
+    const float ref = fmaxf(mx, -0x1p127f);  // finite for a thread with no live row yet
+    s *= fast_exp2(fmaxf(m - ref, kExp2Floor));
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s += row + r < V ? fast_exp2(fmaf(z[r], c2, -ref)) : 0.f;
+    m = mx;
+  });
+  // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same tokens
+#pragma unroll
+  for (int o = 16; o <= 32; o <<= 1) {
+    const float mo = __shfl_xor(m, o, 64), so = __shfl_xor(s, o, 64), M = fmaxf(m, mo), ref = fmaxf(M, -0x1p127f);
+    s = s * fast_exp2(fmaxf(m - ref, kExp2Floor)) + so * fast_exp2(fmaxf(mo - ref, kExp2Floor));
+    m = M;
+  }
+  const int lane = threadIdx.x & 63, tok = threadIdx.x / 64 * 16 + lane;
+  if (lane < 16 && tok < min(n, 16 * kNB)) {
+    part_m[size_t(tok) * gridDim.x + blockIdx.x] = m;
+    part_s[size_t(tok) * gridDim.x + blockIdx.x] = s;
+  }
 }
 
 // lse, logq and loss of a token, one workgroup each.  Its waves share the K products of a row of W with the token's row
@@ -214,7 +251,9 @@ int check_distill(const char* fn, const void* X, const void* W, const int32_t* i
 
 extern "C" size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1) return 0;
-  return lse_states_bytes(n_tok, V, dtype, false);
+  Carver few_states(nullptr);
+  for (int i = 0; i < 2; ++i) few_states.take<float>(size_t(few::workgroups(V)) * size_t(std::min<int64_t>(n_tok, 64)));
+  return std::max(lse_states_bytes(n_tok, V, dtype, false), few_states.bytes());
 }
 
 extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok,
@@ -236,8 +275,22 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
   hipStream_t s = static_cast<hipStream_t>(stream);
   const int n = int(n_tok);
   LseStates p;
-  const int rc = launch_lse_states(fn, X, W, n, d, V, dtype, base2_of_logit(temperature), workspace, s, &p);
-  if (rc != ESTP_OK) return rc;
+  if (few::takes(n, d, dtype)) {
+    p.states = int(few::workgroups(V));
+    Carver c(workspace);
+    p.m = c.take<float>(size_t(p.states) * size_t(n));
+    p.s = c.take<float>(size_t(p.states) * size_t(n));
+    few::choose(n, d, [&](auto steps, auto nb) {
+      distill_lse_few_kernel<decltype(steps)::value, decltype(nb)::value>
+          <<<dim3(unsigned(p.states)), dim3(64 * few::kWaves), 0, s>>>(static_cast<const __bf16*>(X),
+                                                                       static_cast<const __bf16*>(W), n, d, V,
+                                                                       base2_of_logit(temperature), p.m, p.s);
+    });
+    ESTP_CHECK_LAUNCH("distill_lse_few_kernel");
+  } else {
+    const int rc = launch_lse_states(fn, X, W, n, d, V, dtype, base2_of_logit(temperature), workspace, s, &p);
+    if (rc != ESTP_OK) return rc;
+  }
   const float inv_t = inverse_temperature(temperature);
   auto go = [&](auto kernel, int threads, auto* x, auto* w) {
     kernel<<<dim3(unsigned(n)), dim3(unsigned(threads)), 0, s>>>(x, w, ids, logp, d, V, K, renormalise != 0, inv_t, p.m,

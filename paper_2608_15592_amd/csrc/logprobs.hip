@@ -62,17 +62,17 @@ __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __res
       });
 }
 
-// Z[token][v] of few tokens and all of the vocabulary.
+// Z[v / 16][token][v % 16] of few tokens and all of the vocabulary: a tile's logits lie together.  (With a row for each
+// token, 64 bytes of each at distances of a power of 2, 32 tokens of d 1536, V 151936 take 86 us instead of 71.)
 template <int kSteps, int kNB>
 __global__ __launch_bounds__(64 * few::kWaves, 2) void logits_few_kernel(const __bf16* __restrict__ X,
                                                                          const __bf16* __restrict__ W, int n, int d,
-                                                                         int V, int Vc, float* __restrict__ Z) {
+                                                                         int V, float* __restrict__ Z) {
   __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
   const int tok = threadIdx.x / 64 * 16 + (threadIdx.x & 15);
-  const buf_rsrc_t out = make_rsrc(Z, uint32_t(n) * uint32_t(Vc) * 4u);
-  const uint32_t base = uint32_t(tok) * uint32_t(Vc) * 4u;
   few::run<kSteps, kNB, 1>(X, W, n, d, V, lds, [&](int64_t row, f32x4_t z) {
-    buf_store16(out, tok < n ? base + uint32_t(row) * 4u : kPastEnd, __builtin_bit_cast(uint4, z));
+    const buf_rsrc_t out = make_rsrc(Z + size_t(row & ~int64_t(15)) * n, uint32_t(n) * 64u);
+    buf_store16(out, uint32_t(tok) * 64u + uint32_t(row & 15) * 4u, __builtin_bit_cast(uint4, z));
   });
 }
 
@@ -277,21 +277,22 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
 
 // ------------------------------------------------------------------ selection
 
-// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  Column
-// c is vocabulary row v0 + c, or of every `step`-th tile of 256.  One workgroup each.
+// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  16
+// columns lie together, those of a token `of_tok` apart, and the next of the same token `of_16` on.  Column c is vocabulary
+// row v0 + c, or of every `step`-th tile of 256.  One workgroup each.
 template <int kE>
-__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int Vc, int live, int64_t v0,
+__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_16, int live, int64_t v0,
                                                              int step, float c2, int k, int piece_chunks, int chunk0, int states, int chunks,
                                                              float* __restrict__ part, uint64_t* __restrict__ top) {
   __shared__ TopK<kMaxTop * kE> pick;
   __shared__ float wave_m[4], wave_s[4], wave_t[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tok = blockIdx.x / piece_chunks, c = blockIdx.x % piece_chunks;
-  const float* row = Z + size_t(tok) * Vc;
+  const float* row = Z + size_t(tok) * of_tok;
   const int first = 256 * kE * c + 4 * tid;  // columns first + 1024 u + e, ascending in 4 u + e
   f32x4_t z[kE / 4];
 #pragma unroll
-  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + first + 1024 * u);
+  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + size_t((first + 1024 * u) >> 4) * of_16 + (first & 15));
   float m = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kE / 4; ++u)
@@ -526,13 +527,15 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
   carve_logprobs(piece_room(n, V, k), workspace, &b);
   const float c2 = base2_of_logit(temperature), inv_t = inverse_temperature(temperature);
   const dim3 block(256);
+  bool tiled = false;
   for (int64_t v0 = 0; v0 < V; v0 += p.Vc) {
     const int rows = int(std::min<int64_t>(V - v0, p.Vc));
     if constexpr (sizeof(T) == 2) {
-      if (p.Vc >= V && few::takes(n, d, ESTP_BF16)) {
+      tiled = p.Vc >= V && few::takes(n, d, ESTP_BF16);
+      if (tiled) {
         few::choose(n, d, [&](auto steps, auto nb) {
           logits_few_kernel<decltype(steps)::value, decltype(nb)::value>
-              <<<dim3(few::workgroups(V)), dim3(64 * few::kWaves), 0, s>>>(X, W, n, d, V, p.Vc, b.Z);
+              <<<dim3(few::workgroups(V)), dim3(64 * few::kWaves), 0, s>>>(X, W, n, d, V, b.Z);
         });
       } else {
         const bool odd = d % 64 != 0, narrow = n <= 384;
@@ -549,7 +552,7 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int in_piece = (rows + kChunk - 1) / kChunk;
     logprob_select_kernel<kChunk / 256><<<dim3(unsigned(n) * unsigned(in_piece)), block, 0, s>>>(
-        b.Z, p.Vc, rows, v0, 1, c2, k, in_piece, int(v0 / kChunk), p.chunks, p.chunks, b.part, b.top);
+        b.Z, tiled ? 16 : p.Vc, tiled ? 16 * n : 16, rows, v0, 1, c2, k, in_piece, int(v0 / kChunk), p.chunks, p.chunks, b.part, b.top);
     ESTP_CHECK_LAUNCH("logprob_select_kernel");
   }
   logprob_merge_kernel<T, false><<<dim3(unsigned(n)), block, 0, s>>>(X, W, targets, d, V, k, inv_t, p.chunks, b.part,
@@ -574,7 +577,7 @@ int launch_quads(const __bf16* X, const __bf16* W, const int32_t* targets, int n
     kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, 0, p.sample, p.step, 256 * kSampleTiles, b.Z);
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int live = 256 * (p.sample - 1) + std::min(256, V - 256 * p.step * (p.sample - 1));
-    logprob_select_kernel<kSampleTiles><<<dim3(unsigned(n)), block, 0, s>>>(b.Z, 256 * kSampleTiles, live, 0, p.step, c2,
+    logprob_select_kernel<kSampleTiles><<<dim3(unsigned(n)), block, 0, s>>>(b.Z, 256 * kSampleTiles, 16, live, 0, p.step, c2,
                                                                             k, 1, 0, states, 1, b.part, b.top);
     ESTP_CHECK_LAUNCH("logprob_select_kernel");
   }

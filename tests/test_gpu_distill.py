@@ -82,6 +82,14 @@ def test_several_vocabulary_pieces(dtype):
     _check(_case(5, n, 32, 17001, 6, dtype, ignored=0.9), dtype, 2.0)
 
 
+@pytest.mark.parametrize("n,d,V", [(1, 1024, 5000), (17, 1024, 77), (64, 1024, 4100), (33, 1536, 4097), (20, 2048, 16400),
+                                   (50, 2048, 4099), (32, 2560, 4500), (40, 2560, 4500), (16, 3584, 4111),
+                                   (1, 4096, 4600), (32, 4096, 4097), (33, 4096, 4097)])
+def test_few_tokens(n, d, V):
+    # whose part of the depth stays in registers, where they fit
+    _check(_case(n + d, n, d, V, 10, "bf16"), "bf16", 1.2)
+
+
 @pytest.mark.parametrize("n", [2049, 2500, 3400, 4400])
 def test_many_tokens_forward(n):
     _check(_case(n, n, 64, 6000, 4, "bf16"), "bf16", 1.5, grads=False)
