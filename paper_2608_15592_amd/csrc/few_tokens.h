@@ -36,8 +36,9 @@ inline unsigned workgroups(int V) { return unsigned(std::min(kWgs, (V + kRows - 
 template <int kSteps, int kNB>
 struct Rows {
   static constexpr int kTile = 1024 * kSteps;                 // bytes of a wave's part of a tile
-  static constexpr int kSlots = kSteps > 8 ? 1 : 16 / kSteps;  // of the ring of a wave
-  static constexpr int kRound = kNB < 2 ? kNB : 2;             // blocks of tokens whose sums meet at a barrier
+  static constexpr bool kWide = kNB == 4 && kSteps < 8;         // room for the sums of all four blocks
+  static constexpr int kSlots = kSteps > 8 ? 1 : (kWide ? 12 : 16) / kSteps;  // of the ring of a wave
+  static constexpr int kRound = kWide ? 4 : kNB < 2 ? kNB : 2;  // blocks of tokens whose sums meet at a barrier
   static constexpr int kRing = kWaves * kSlots * kTile;
   static constexpr int kLds = kRing + 2 * kWaves * kRound * 1024;
   static constexpr int kPer = 4 * kSteps;  // 16-byte chunks of a row's eighth

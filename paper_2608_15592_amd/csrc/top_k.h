@@ -33,8 +33,9 @@ struct TopK {
   uint64_t list[kCap], maxima[256], bound;
   int count;
 
-  // The k-th largest of the threads' keys, k <= 256, or 1 where fewer threads have one.  One wave, four keys a lane,
-  // finds it bit by bit, and what lies below the logit's bits only where equal logits need it.
+  // A key that k of the threads' keys reach, and kMaxTop at most, or 1 where fewer than k threads have one.  One wave, four
+  // keys a lane, forms it bit by bit, until few enough reach it, and what lies below the logit's bits only where equal
+  // logits need it.
   __device__ __forceinline__ uint64_t bound_of(uint64_t mine, int k) {
     const int tid = threadIdx.x;
     maxima[tid] = mine;
@@ -54,12 +55,18 @@ struct TopK {
         return n;
       };
       uint32_t top = 0, low = 0;
-      for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+      int reach = 256;
+      const int enough = min(k + 32, kMaxTop);
+      for (uint32_t bit = 0x80000000u; bit && reach > enough; bit >>= 1) {
         const uint32_t c = top | bit;
-        if (number([&](int u) { return hi[u] >= c; }) >= k) top = c;
+        const int n = number([&](int u) { return hi[u] >= c; });
+        if (n >= k) {
+          top = c;
+          reach = n;
+        }
       }
       const int left = k - number([&](int u) { return hi[u] > top; });
-      if (top && number([&](int u) { return hi[u] == top; }) > left)
+      if (top && reach > enough)
         for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
           const uint32_t c = low | bit;
           if (number([&](int u) { return hi[u] == top && lo[u] >= c; }) >= left) low = c;
