@@ -492,6 +492,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
           t_of[j] = tc[s];
         }
         __builtin_amdgcn_sched_barrier(0);
+        gemm::sums_ready();
 #pragma unroll
         for (int j = 0; j < kNBN; ++j) {
           const int sl = 16 * kNBN * wn + 16 * j + fr;
@@ -502,7 +503,7 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
           for (int i = 0; i < 8; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              p[i / 2][4 * (i % 2) + r] = g * fast_exp2(fmaf(acc[i][j][r], c2, -l2));
+              p[i / 2][4 * (i % 2) + r] = g * fast_exp2(fmaf(gemm::read_sum(acc[i][j][r]), c2, -l2));
           if (__any(rel >= 0 && rel < 128 && (rel & 31) < 8)) {  // seldom: one tile in V / 256 holds a token's target
 #pragma unroll
             for (int q = 0; q < 4; ++q)
