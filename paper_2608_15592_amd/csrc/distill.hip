@@ -20,9 +20,11 @@
 #include <algorithm>
 
 #include "estp_common.h"
+#include "f32_split.h"
 #include "few_tokens.h"
 #include "lm_head.h"
 #include "lse_states.h"
+#include "mfma_gemm.h"
 
 namespace estp {
 namespace detail {
@@ -101,6 +103,65 @@ __global__ __launch_bounds__(64 * few::kWaves, 2) void distill_lse_few_kernel(co
   if (lane < 16 && tok < min(n, 16 * kNB)) {
     part_m[size_t(tok) * gridDim.x + blockIdx.x] = m;
     part_s[size_t(tok) * gridDim.x + blockIdx.x] = s;
+  }
+}
+
+// The same of fp32 logits by the bf16 matrix cores: workgroup (token tile, slice) takes the vocabulary tiles slice, slice +
+// n_slices, ..., and has a state for each of its waves.
+template <int kNB, bool kStream>
+__global__ __launch_bounds__(64 * split::kWaves, 2) void distill_lse_split_kernel(
+    const float* __restrict__ X, const __bf16* __restrict__ parts, const float* __restrict__ W, int n, int d, int V,
+    float c2, int n_tt, int n_slices, float* __restrict__ part_m, float* __restrict__ part_s) {
+  using Run = split::Tile<kNB, kStream>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const gemm::SliceAt wg = gemm::slice_of(gemm::first_tile(blockIdx.x, gridDim.x), n_tt, n_slices);
+  if (wg.slice >= n_slices) return;
+  const int n_vt = (V + split::kRows - 1) / split::kRows, n0 = wg.tile * Run::kTN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float m[kNB], s[kNB];
+#pragma unroll
+  for (int b = 0; b < kNB; ++b) {
+    m[b] = -INFINITY;
+    s[b] = 0.f;
+  }
+  Run::run(
+      lds, W, V, X, parts, n, n, d, (n_vt - wg.slice + n_slices - 1) / n_slices,
+      [&](int i) { return typename Run::Place{(wg.slice + i * n_slices) * split::kRows, n0}; },
+      [&](const typename Run::Place& at, const typename Run::Acc& acc) {
+        const int lim = V - (at.m0 + 32 * wave + 4 * (lane >> 4));  // live rows: 16 i + r < lim
+#pragma unroll
+        for (int b = 0; b < kNB; ++b) {
+          float mx = m[b];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) mx = fmaxf(mx, 16 * i + r < lim ? acc[i][b][r] * c2 : -INFINITY);
+          const float ref = fmaxf(mx, -0x1p127f);  // finite for a lane with no live row yet
+          float sum = s[b] * fast_exp2(fmaxf(m[b] - ref, kExp2Floor));
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += 16 * i + r < lim ? fast_exp2(fmaf(acc[i][b][r], c2, -ref)) : 0.f;
+          m[b] = mx;
+          s[b] = sum;
+        }
+      });
+#pragma unroll
+  for (int b = 0; b < kNB; ++b) {
+    // lanes l, l ^ 16, l ^ 32, l ^ 48 hold the same tokens
+#pragma unroll
+    for (int o = 16; o <= 32; o <<= 1) {
+      const float mo = __shfl_xor(m[b], o, 64), so = __shfl_xor(s[b], o, 64), M = fmaxf(m[b], mo);
+      const float ref = fmaxf(M, -0x1p127f);
+      s[b] = s[b] * fast_exp2(fmaxf(m[b] - ref, kExp2Floor)) + so * fast_exp2(fmaxf(mo - ref, kExp2Floor));
+      m[b] = M;
+    }
+    const int tok = n0 + 16 * b + lane;
+    if (lane < 16 && tok < n) {
+      const size_t o = size_t(tok) * (split::kWaves * n_slices) + split::kWaves * wg.slice + wave;
+      part_m[o] = m[b];
+      part_s[o] = s[b];
+    }
   }
 }
 
@@ -232,6 +293,28 @@ using namespace estp::detail;
 
 namespace {
 
+// Token tiles of a call by the bf16 matrix cores, and slices of the vocabulary's: up to two rounds of workgroups, as many
+// as make the longest sum of a compute unit's tiles shortest, with half a tile for a workgroup's first transfers.
+struct SplitStates {
+  int tiles, slices;
+};
+SplitStates split_states(int64_t n, int d, int V) {
+  (void)d;
+  const int tile = 16 * split::blocks_of(n);
+  const int64_t n_tt = (n + tile - 1) / tile, n_vt = (int64_t(V) + split::kRows - 1) / split::kRows;
+  SplitStates r{int(n_tt), 1};
+  int64_t least = INT64_MAX;
+  for (int64_t c = std::min(n_vt, std::max<int64_t>(1, 256 / n_tt)); c <= std::min(n_vt, std::max<int64_t>(1, 512 / n_tt));
+       ++c) {
+    const int64_t cost = (n_tt * c + 255) / 256 * (2 * ((n_vt + c - 1) / c) + 1);
+    if (cost < least) {
+      least = cost;
+      r.slices = int(c);
+    }
+  }
+  return r;
+}
+
 int check_distill(const char* fn, const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok,
                   int32_t d, int32_t V, int32_t K, float temperature, int dtype) {
   ESTP_REQUIRE(ids && logp, ESTP_ERR_INVALID_ARG, "%s: ids and logp must be non-null", fn);
@@ -251,9 +334,16 @@ int check_distill(const char* fn, const void* X, const void* W, const int32_t* i
 
 extern "C" size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1) return 0;
-  Carver few_states(nullptr);
-  for (int i = 0; i < 2; ++i) few_states.take<float>(size_t(few::workgroups(V)) * size_t(std::min<int64_t>(n_tok, 64)));
-  return std::max(lse_states_bytes(n_tok, V, dtype, false), few_states.bytes());
+  Carver own(nullptr);
+  if (dtype == ESTP_F32) {
+    // slices n_tok is at most 512 tiles' worth, or n_tok
+    for (int i = 0; i < 2; ++i)
+      own.take<float>(split::kWaves * std::max<size_t>(size_t(n_tok), 512 * 96));
+    own.take<__bf16>(split::parts_bytes(size_t(n_tok), d) / 2);
+  } else {
+    for (int i = 0; i < 2; ++i) own.take<float>(size_t(few::workgroups(V)) * size_t(std::min<int64_t>(n_tok, 64)));
+  }
+  return std::max(lse_states_bytes(n_tok, V, dtype, false), own.bytes());
 }
 
 extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* ids, const float* logp, int64_t n_tok,
@@ -287,6 +377,21 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
                                                                        base2_of_logit(temperature), p.m, p.s);
     });
     ESTP_CHECK_LAUNCH("distill_lse_few_kernel");
+  } else if (dtype == ESTP_F32 && split::takes(n, d, V)) {
+    const float *x = static_cast<const float*>(X), *w = static_cast<const float*>(W);
+    const SplitStates r = split_states(n, d, V);
+    p.states = split::kWaves * r.slices;
+    Carver c(workspace);
+    p.m = c.take<float>(size_t(p.states) * size_t(n));
+    p.s = c.take<float>(size_t(p.states) * size_t(n));
+    __bf16* parts = c.take<__bf16>(split::parts_bytes(size_t(n), d) / 2);
+    split::split_rows_kernel<<<dim3(unsigned(n)), dim3(256), 0, s>>>(x, n, nullptr, d, parts);
+    split::choose(n, [&](auto nb, auto stream) {
+      distill_lse_split_kernel<decltype(nb)::value, decltype(stream)::value>
+          <<<dim3(unsigned((r.tiles * r.slices + 7) / 8 * 8)), dim3(64 * split::kWaves), 0, s>>>(
+              x, parts, w, n, d, V, base2_of_logit(temperature), r.tiles, r.slices, p.m, p.s);
+    });
+    ESTP_CHECK_LAUNCH("distill_lse_split_kernel");
   } else {
     const int rc = launch_lse_states(fn, X, W, n, d, V, dtype, base2_of_logit(temperature), workspace, s, &p);
     if (rc != ESTP_OK) return rc;
@@ -313,7 +418,7 @@ extern "C" size_t estp_distill_loss_backward_workspace_size(int64_t n_tok, int32
   Carver c(nullptr);
   c.take<int32_t>(size_t(n_tok));
   c.take<float>(size_t(n_tok));
-  return c.bytes() + lm_head_backward_bytes(n_tok, d, V, dtype);
+  return c.bytes() + lm_head_backward_bytes(n_tok, d, V, dtype, true);
 }
 
 extern "C" int estp_distill_loss_backward(const void* X, const void* W, const int32_t* ids, const float* logp,

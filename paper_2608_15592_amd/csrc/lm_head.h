@@ -44,7 +44,7 @@ int launch_teacher_entries(const Distillation& t, int n, int V, int dtype, const
 
 // The gradient's kernels on checked arguments: G_iv = grad_i (exp(z_i[v] - lse_i) - [v = t_i]), or with a teacher
 // grad_i exp(z_i[v] / temperature - lse_i) except where launch_teacher_entries has written.
-size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype);
+size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype, bool teacher);
 int launch_lm_head_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
                             int n, int d, int V, int dtype, const Distillation* teacher, void* dX, void* dW,
                             void* workspace, hipStream_t s);

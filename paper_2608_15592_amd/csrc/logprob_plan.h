@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "estp_common.h"
+#include "f32_split.h"
 
 namespace estp {
 namespace detail {
@@ -71,41 +72,44 @@ inline bool use_quads(int64_t n_tok, int V, int dtype) {
 struct LogprobBuffers {
   float *Z, *part;
   uint64_t* top;
+  __bf16* parts;  // of fp32 tokens
   Quads quads;
 };
 // Room of one form: logits, partial states, keys, words of bits and tiles of quads.
 struct LogprobRoom {
-  size_t Z, states, keys, words, tiles;
+  size_t Z, states, keys, words, tiles, parts;
 };
 inline size_t carve_logprobs(const LogprobRoom& r, void* ws, LogprobBuffers* b) {
   Carver c(ws);
   b->Z = c.take<float>(r.Z);
   b->part = c.take<float>(3 * r.states);
   b->top = c.take<uint64_t>(r.keys);
+  b->parts = c.take<__bf16>(r.parts / 2);
   b->quads.bits = c.take<uint32_t>(r.words);
   b->quads.z = c.take<float>(r.tiles * kQuadTile);
   return c.bytes();
 }
-inline LogprobRoom piece_room(int64_t n, int V, int k) {
+inline LogprobRoom piece_room(int64_t n, int d, int V, int k, int dtype) {
   const size_t toks = size_t(n), chunks = (size_t(V) + kChunk - 1) / kChunk;
-  return {std::min(toks * chunks * kChunk, kRoom), toks * chunks, toks * chunks * size_t(k), 0, 0};
+  return {std::min(toks * chunks * kChunk, kRoom), toks * chunks, toks * chunks * size_t(k), 0, 0,
+          dtype == ESTP_F32 ? split::parts_bytes(toks, d) : 0};
 }
 inline LogprobRoom quad_room(int n, const QuadPlan& p, int k) {
   const size_t toks = size_t(n), n_tt = (toks + 255) / 256, main = k > 0 ? size_t(p.n_main) : 0;
   return {k > 0 ? toks * 256 * kSampleTiles : 0, toks * size_t((k > 0) + 2 * p.slices), toks * size_t(k),
-          n_tt * 256 * 2 * main, n_tt * main};
+          n_tt * 256 * 2 * main, n_tt * main, 0};
 }
 // The most that a block of up to n tokens takes, in either form.
-inline size_t logprob_bytes(int64_t n_tok, int V, int k, int dtype) {
+inline size_t logprob_bytes(int64_t n_tok, int d, int V, int k, int dtype) {
   LogprobBuffers b;
-  size_t most = carve_logprobs(piece_room(std::min<int64_t>(use_quads(n_tok, V, dtype) ? 384 : n_tok, kBlockToks), V, k),
-                               nullptr, &b);
+  const int64_t listed = std::min<int64_t>(use_quads(n_tok, V, dtype) ? 384 : n_tok, kBlockToks);
+  size_t most = carve_logprobs(piece_room(listed, d, V, k, dtype), nullptr, &b);
   if (use_quads(n_tok, V, dtype)) {
     // slices: up to 512 tiles of workgroups
     const size_t toks = size_t(std::min<int64_t>(n_tok, kQuadToks)), n_tt = (toks + 255) / 256;
     const size_t main = k > 0 ? (size_t(V) + 255) / 256 : 0;
     most = std::max(most, carve_logprobs({toks * 256 * kSampleTiles, toks + 2 * 512 * 256, toks * size_t(k),
-                                          n_tt * 256 * 2 * main, n_tt * main}, nullptr, &b));
+                                          n_tt * 256 * 2 * main, n_tt * main, 0}, nullptr, &b));
   }
   return most;
 }

@@ -14,6 +14,7 @@
 #include "ent_fold.h"
 #include "estp_common.h"
 #include "f32_gemm.h"
+#include "f32_split.h"
 #include "few_tokens.h"
 #include "lm_head.h"
 #include "logprob_plan.h"
@@ -101,6 +102,37 @@ __global__ __launch_bounds__(256, 2) void logits_f32_kernel(const float* __restr
         *reinterpret_cast<f32x4_t*>(Z + size_t(s) * Vc + at.m + 32 * i + 8 * q) =
             f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
   }
+}
+
+// The same of vocabulary rows v0 .. v0 + Vc by the bf16 matrix cores.
+template <int kNB, bool kStream>
+__global__ __launch_bounds__(64 * split::kWaves, 2) void logits_split_kernel(const float* __restrict__ X,
+                                                                             const __bf16* __restrict__ parts,
+                                                                             const float* __restrict__ W, int n, int d,
+                                                                             int V, int64_t v0, int Vc,
+                                                                             float* __restrict__ Z) {
+  using Run = split::Tile<kNB, kStream>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
+  const int n_vt = (rows + split::kRows - 1) / split::kRows, n_tt = (n + Run::kTN - 1) / Run::kTN;
+  // (the token tiles of a vocabulary tile next to each other on one XCD)
+  const int first = gemm::first_tile(blockIdx.x, gridDim.x), total = n_vt * n_tt;
+  Run::run(
+      lds, W + size_t(v0) * d, rows, X, parts, n, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
+      [&](int i) {
+        const int id = first + i * int(gridDim.x);
+        return typename Run::Place{id / n_tt * split::kRows, id % n_tt * Run::kTN};
+      },
+      [&](const typename Run::Place& at, const typename Run::Acc& acc) {
+        const int lane = threadIdx.x & 63, row = at.m0 + 32 * int(threadIdx.x >> 6) + 4 * (lane >> 4);
+#pragma unroll
+        for (int b = 0; b < kNB; ++b) {
+          const int tok = at.n0 + 16 * b + (lane & 15);
+          if (tok >= n) continue;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) *reinterpret_cast<f32x4_t*>(Z + size_t(tok) * Vc + row + 16 * i) = acc[i][b];
+        }
+      });
 }
 
 // ------------------------------------------------------------------ many tokens: what may be among the largest
@@ -524,7 +556,7 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
                   hipStream_t s) {
   const PiecePlan p = plan_pieces(n, V);
   LogprobBuffers b;
-  carve_logprobs(piece_room(n, V, k), workspace, &b);
+  carve_logprobs(piece_room(n, d, V, k, sizeof(T) == 4 ? ESTP_F32 : ESTP_BF16), workspace, &b);
   const float c2 = base2_of_logit(temperature), inv_t = inverse_temperature(temperature);
   const dim3 block(256);
   bool tiled = false;
@@ -544,10 +576,19 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
         kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, v0, (rows + 255) / 256, 1, p.Vc, b.Z);
       }
     } else {
-      const int tile = n <= 32 ? 32 : n <= 64 ? 64 : kFT;
-      auto kernel = tile == 32 ? logits_f32_kernel<32> : tile == 64 ? logits_f32_kernel<64> : logits_f32_kernel<kFT>;
-      kernel<<<dim3(unsigned((rows + kFT - 1) / kFT), unsigned((n + tile - 1) / tile)), block, 0, s>>>(X, W, n, d, V, v0,
-                                                                                                      p.Vc, b.Z);
+      if (split::takes(n, d, V)) {
+        if (v0 == 0)
+          split::split_rows_kernel<<<dim3(unsigned(n)), block, 0, s>>>(X, n, nullptr, d, b.parts);
+        split::choose(n, [&](auto nb, auto stream) {
+          logits_split_kernel<decltype(nb)::value, decltype(stream)::value>
+              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(X, b.parts, W, n, d, V, v0, p.Vc, b.Z);
+        });
+      } else {
+        const int tile = n <= 32 ? 32 : n <= 64 ? 64 : kFT;
+        auto kernel = tile == 32 ? logits_f32_kernel<32> : tile == 64 ? logits_f32_kernel<64> : logits_f32_kernel<kFT>;
+        kernel<<<dim3(unsigned((rows + kFT - 1) / kFT), unsigned((n + tile - 1) / tile)), block, 0, s>>>(
+            X, W, n, d, V, v0, p.Vc, b.Z);
+      }
     }
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int in_piece = (rows + kChunk - 1) / kChunk;
@@ -601,7 +642,7 @@ using namespace estp::detail;
 
 extern "C" size_t estp_token_logprobs_workspace_size(int64_t n_tok, int32_t d, int32_t V, int32_t k, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1 || V > (1 << 24) || k < 0 || k > kMaxTop) return 0;
-  return logprob_bytes(n_tok, V, k, dtype);
+  return logprob_bytes(n_tok, d, V, k, dtype);
 }
 
 extern "C" int estp_token_logprobs(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d,

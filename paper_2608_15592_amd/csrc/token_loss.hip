@@ -25,6 +25,7 @@
 
 #include "estp_common.h"
 #include "f32_gemm.h"
+#include "f32_split.h"
 #include "lm_head.h"
 #include "loss_shares.h"
 #include "lse_states.h"
@@ -290,6 +291,45 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
         *reinterpret_cast<f32x4_t*>(G + size_t(s) * Vc + v) = out;
       }
   }
+}
+
+// G of a distillation by the bf16 matrix cores: loss_grad_f32_kernel's, from the parts of the live rows.
+template <int kNB, bool kStream>
+__global__ __launch_bounds__(64 * split::kWaves, 2) void loss_grad_split_kernel(
+    const float* __restrict__ Xc, const __bf16* __restrict__ parts, int n_max, const float* __restrict__ W,
+    const int* __restrict__ n_live, int d, int V, int64_t v0, int Vc, const float* __restrict__ lc,
+    const float* __restrict__ gc, float inv_t, float* __restrict__ G) {
+  using Run = split::Tile<kNB, kStream>;
+  __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
+  const int n_vt = (rows + split::kRows - 1) / split::kRows, n_tt = (n + Run::kTN - 1) / Run::kTN;
+  // (the token tiles of a vocabulary tile next to each other on one XCD)
+  const int first = gemm::first_tile(blockIdx.x, gridDim.x), total = n_vt * n_tt;
+  Run::run(
+      lds, W + size_t(v0) * d, rows, Xc, parts, n_max, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
+      [&](int i) {
+        const int id = first + i * int(gridDim.x);
+        return typename Run::Place{id / n_tt * split::kRows, id % n_tt * Run::kTN};
+      },
+      [&](const typename Run::Place& at, const typename Run::Acc& acc) {
+        const int lane = threadIdx.x & 63, v0_of = at.m0 + 32 * int(threadIdx.x >> 6) + 4 * (lane >> 4);
+#pragma unroll
+        for (int b = 0; b < kNB; ++b) {
+          const int s = at.n0 + 16 * b + (lane & 15);
+          if (s >= n) continue;
+          const float l = lc[s], g = gc[s];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int v = v0_of + 16 * i;
+            f32x4_t out;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              out[e] = v + e < rows ? g * fast_exp2(fmaf(acc[i][b][e], inv_t, -l) * kLog2e) : 0.f;
+            *reinterpret_cast<f32x4_t*>(G + size_t(s) * Vc + v) = out;
+          }
+        }
+      });
 }
 
 // out[share][slot][k] (+)= G W_piece over the share's vocabulary rows, shares blockIdx.z, + gridDim.z, ...  M side:
@@ -674,7 +714,7 @@ inline int f32_tile_toks(int64_t n_tok, int V) {
   return n_tok <= 32 || tiles < kFewTiles ? 32 : n_tok <= 64 ? 64 : kFT;
 }
 
-inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
+inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype, bool teacher) {
   const size_t es = dtype == ESTP_F32 ? 4 : 2;
   const int64_t tok_pad = (n_tok + 255) / 256 * 256;
   const int64_t v_pad = (int64_t(V) + 255) / 256 * 256;
@@ -686,6 +726,9 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype) {
   p.parts = g_parts(n_tok, dtype);
   p.Vc = int(vc);
   p.tile_toks = dtype == ESTP_F32 ? f32_tile_toks(n_tok, V) : bf16_tile_toks(n_tok);
+  // (dX of a distillation, 90 tokens, d 1536, V 151936: 96 columns 372 us, 128 481)
+  if (teacher && dtype == ESTP_F32 && p.tile_toks == kFT && (n_tok + 95) / 96 * 96 < (n_tok + kFT - 1) / kFT * kFT)
+    p.tile_toks = 96;
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -744,11 +787,13 @@ template <typename T>
 int launch_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
                          int n, int d, int V, int dtype, const Distillation* teacher, void* dX, void* dW,
                          void* workspace, hipStream_t s) {
-  const LossPlan p = plan_loss(n, d, V, dtype);
+  const LossPlan p = plan_loss(n, d, V, dtype, teacher != nullptr);
   const LossBuffers b = carve_loss(loss_need(p, n, d), n, d, dtype, workspace);
   constexpr int kWgs = 256;  // of the persistent kernels: one on each compute unit
   const T *Wt = static_cast<const T*>(W), *Xc = reinterpret_cast<const T*>(b.Xc);
   T* G = reinterpret_cast<T*>(b.G);
+  const bool by_parts = sizeof(T) == 4 && teacher && split::takes(n, d, V);
+  __bf16* parts = reinterpret_cast<__bf16*>(static_cast<char*>(workspace) + b.bytes);
   const float inv_t = teacher ? inverse_temperature(teacher->temperature) : 1.f;
   const float c2 = teacher ? base2_of_logit(teacher->temperature) : kLog2e;
   if (n > 1024)
@@ -784,10 +829,20 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
     } else {
       const unsigned n_tt = unsigned((n + p.tile_toks - 1) / p.tile_toks), n_dt = unsigned((d + kFT - 1) / kFT);
       const unsigned n_vt = unsigned((p.Vc + kFT - 1) / kFT);
-      auto grad_kernel = p.tile_toks == 32   ? loss_grad_f32_kernel<32>
-                         : p.tile_toks == 64 ? loss_grad_f32_kernel<64>
-                                             : loss_grad_f32_kernel<kFT>;
-      grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, inv_t, G);
+      if (by_parts) {
+        if (v0 == 0) split::split_rows_kernel<<<dim3(unsigned(n)), block, 0, s>>>(Xc, n, b.n_live, d, parts);
+        split::choose(n, [&](auto nb, auto stream) {
+          loss_grad_split_kernel<decltype(nb)::value, decltype(stream)::value>
+              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(Xc, parts, n, Wt, b.n_live, d, V, v0, p.Vc, b.lc,
+                                                                      b.gc, inv_t, G);
+        });
+      } else {
+        auto grad_kernel = p.tile_toks == 32   ? loss_grad_f32_kernel<32>
+                           : p.tile_toks == 64 ? loss_grad_f32_kernel<64>
+                           : p.tile_toks == 96 ? loss_grad_f32_kernel<96>
+                                               : loss_grad_f32_kernel<kFT>;
+        grad_kernel<<<dim3(n_vt, n_tt), block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, inv_t, G);
+      }
       ESTP_CHECK_LAUNCH("loss_grad_f32_kernel");
       if (teacher) {
         const int rc = launch_teacher_entries(*teacher, n, V, dtype, b.slot, b.n_live, v0, p.Vc, G, s);
@@ -799,6 +854,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         const unsigned shares = unsigned(std::min({int64_t(kWgs), int64_t((p.Vc + 63) / 64), most}));
         auto dx_kernel = p.tile_toks == 32   ? loss_dx_f32_kernel<32>
                          : p.tile_toks == 64 ? loss_dx_f32_kernel<64>
+                         : p.tile_toks == 96 ? loss_dx_f32_kernel<96>
                                              : loss_dx_f32_kernel<kFT>;
         dx_kernel<<<dim3(n_dt, n_tt, shares), block, 0, s>>>(G, Wt, b.n_live, d, V, v0, p.Vc, kWgs, b.room, v0 == 0,
                                                              b.acc);
@@ -822,8 +878,9 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
   return ESTP_OK;
 }
 
-size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype) {
-  return carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
+size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype, bool teacher) {
+  const size_t loss = carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
+  return loss + (teacher && dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) : 0);
 }
 
 int launch_lm_head_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
@@ -981,7 +1038,7 @@ extern "C" int estp_token_loss(const void* X, const void* W, const int32_t* targ
 
 extern "C" size_t estp_token_loss_backward_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype) {
   if (n_tok < 1 || d < 1 || V < 1) return 0;
-  return lm_head_backward_bytes(n_tok, d, V, dtype);
+  return lm_head_backward_bytes(n_tok, d, V, dtype, false);
 }
 
 extern "C" int estp_token_loss_backward(const void* X, const void* W, const int32_t* targets, const float* lse,

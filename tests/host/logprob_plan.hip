@@ -20,15 +20,15 @@ int main() {
         LogprobBuffers b;
         const PiecePlan p = plan_pieces(n, V);
         check(p.Vc >= kChunk && p.Vc % kChunk == 0 && int64_t(p.Vc) * 256 * 4 <= int64_t(1) << 32 &&
-                  size_t(n) * size_t(p.Vc) <= piece_room(n, V, k).Z && int64_t(p.chunks) * kChunk >= V,
+                  size_t(n) * size_t(p.Vc) <= piece_room(n, 64, V, k, 0).Z && int64_t(p.chunks) * kChunk >= V,
               "pieces", n, V, k);
         if (!use_quads(385, V, 0)) {
-          check(carve_logprobs(piece_room(n, V, k), nullptr, &b) <= logprob_bytes(n, V, k, 0), "room", n, V, k);
+          check(carve_logprobs(piece_room(n, 64, V, k, 0), nullptr, &b) <= logprob_bytes(n, 64, V, k, 0), "room", n, V, k);
           continue;
         }
         if (n <= 384) {
-          check(carve_logprobs(piece_room(n, V, k), nullptr, &b) <= logprob_bytes(n, V, k, 0), "room", n, V, k);
-          check(logprob_bytes(n, V, k, 0) <= logprob_bytes(385, V, k, 0), "grows", n, V, k);
+          check(carve_logprobs(piece_room(n, 64, V, k, 0), nullptr, &b) <= logprob_bytes(n, 64, V, k, 0), "room", n, V, k);
+          check(logprob_bytes(n, 64, V, k, 0) <= logprob_bytes(385, 64, V, k, 0), "grows", n, V, k);
         }
         if (n > kQuadToks) continue;
         // (the last block of a call of many tokens may be of any size)
@@ -48,8 +48,8 @@ int main() {
           check(other == 0 && at == q.n_main, "tiles", n, V, k);
         }
         const size_t need = carve_logprobs(quad_room(n, q, k), nullptr, &b);
-        check(need <= logprob_bytes(std::max(n, 385), V, k, 0), "room for quads", n, V, k);
-        check(need <= logprob_bytes(100000, V, k, 0), "room for a last block", n, V, k);
+        check(need <= logprob_bytes(std::max(n, 385), 64, V, k, 0), "room for quads", n, V, k);
+        check(need <= logprob_bytes(100000, 64, V, k, 0), "room for a last block", n, V, k);
       }
     }
   printf("%d plans with quads, %d wrong\n", listed, bad);

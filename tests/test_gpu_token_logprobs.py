@@ -133,10 +133,43 @@ def test_few_tokens(n, d, V):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
-@pytest.mark.parametrize("n", [1, 20, 60])
-def test_a_non_finite_row_of_weights_stays_in_its_row(n):
-    d, V = 2048, 5000
-    X, W, _, _ = _inputs(n, n, d, V, "bf16")
+# fp32 calls whose products are formed from parts in bf16: widths of a stage and others, tokens of each tile's width
+SPLIT = [(16, 1024, 65000, 9), (30, 520, 66000, 9), (37, 1000, 28000, 20), (64, 264, 61000, 5), (90, 256, 45000, 20),
+         (100, 72, 140001, 3), (200, 512, 10003, 128), (500, 256, 8300, 9)]
+
+
+@pytest.mark.parametrize("n,d,V,k", SPLIT)
+def test_f32_from_parts(n, d, V, k):
+    X, W, t, _ = _inputs(n + d, n, d, V, "f32", ignored=0.1)
+    ws = Guarded(estp.load().estp_token_logprobs_workspace_size(n, d, V, k, 1))
+    got = _check(X, W, t, k, 1.1, workspace=ws.ws)
+    ws.check()
+    again = estp.token_logprobs(dev(X), dev(W), dev(t), k, 1.1)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_f32_logits_are_as_exact_as_fp32_sums():
+    # numbers of 24 significant bits and of very different sizes, logits that cancel: off by less than d roundings of
+    # the largest partial sum (a chain of fp32 FMAs is off by up to d)
+    n, d, V = 64, 512, 40000
+    g = np.random.default_rng(5)
+    X = (g.standard_normal((n, d)) * 2.0 ** g.integers(-6, 7, (n, d))).astype(np.float32)
+    W = (g.standard_normal((V, d)) * 2.0 ** g.integers(-9, 3, (V, d))).astype(np.float32)
+    top = estp.token_logprobs(dev(X), dev(W), None, 128, temperature=64.0)
+    z = X.astype(np.float64) @ W.astype(np.float64).T
+    size = np.abs(X).astype(np.float64) @ np.abs(W).astype(np.float64).T
+    ids = host(top[3])
+    got = (_wide(top[4]) + _wide(top[1])[:, None]) * 64.0
+    at, of = np.take_along_axis(z, ids, 1), np.take_along_axis(size, ids, 1)
+    # (the log-probability itself is rounded, at most twice at its own size and that of lse)
+    room = 4 * OP.U * (np.abs(at) + 64.0 * np.abs(_wide(top[1])[:, None]))
+    assert (np.abs(got - at) <= 8 * OP.U * of + room).all()
+
+
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 1, 5000), ("bf16", 20, 5000), ("bf16", 60, 5000), ("f32", 60, 9000)])
+def test_a_non_finite_row_of_weights_stays_in_its_row(dtype, n, V):
+    d = 2048
+    X, W, _, _ = _inputs(n, n, d, V, dtype)
     want = estp.token_logprobs(dev(X), dev(W), None, 5)
     low = np.argmin(OP.widen(X) @ OP.widen(W).T, axis=1)[0]  # not an alternative of any row's, or of few
     Wd = dev(W)
