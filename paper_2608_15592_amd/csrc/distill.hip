@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * few::kWaves, 2) void distill_lse_few_kernel(co
                                                                               float* __restrict__ part_s) {
   __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
   float m = -INFINITY, s = 0.f;
-  few::run<kSteps, kNB, 0>(X, W, n, d, V, lds, [&](int64_t row, f32x4_t z) {
+  few::run<kSteps, kNB, 0>(X, W, n, d, V, few::tiles_of(V), lds, [&](int64_t row, f32x4_t z) {
     float mx = m, zc[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -341,7 +341,7 @@ extern "C" size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int
       own.take<float>(split::kWaves * std::max<size_t>(size_t(n_tok), 512 * 96));
     own.take<__bf16>(split::parts_bytes(size_t(n_tok), d) / 2);
   } else {
-    for (int i = 0; i < 2; ++i) own.take<float>(size_t(few::workgroups(V)) * size_t(std::min<int64_t>(n_tok, 64)));
+    for (int i = 0; i < 2; ++i) own.take<float>(size_t(few::workgroups(few::tiles_of(V))) * size_t(std::min<int64_t>(n_tok, 64)));
   }
   return std::max(lse_states_bytes(n_tok, V, dtype, false), own.bytes());
 }
@@ -366,7 +366,7 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
   const int n = int(n_tok);
   LseStates p;
   if (few::takes(n, d, dtype)) {
-    p.states = int(few::workgroups(V));
+    p.states = int(few::workgroups(few::tiles_of(V)));
     Carver c(workspace);
     p.m = c.take<float>(size_t(p.states) * size_t(n));
     p.s = c.take<float>(size_t(p.states) * size_t(n));

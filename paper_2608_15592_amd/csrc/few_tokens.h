@@ -31,7 +31,8 @@ inline bool takes(int64_t n_tok, int d, int dtype) {
   const int steps = d / (32 * kWaves);
   return steps == 4 || steps == 6 || steps == 8 || ((steps == 10 || steps == 14 || steps == 16) && blocks_of(n_tok) <= 2);
 }
-inline unsigned workgroups(int V) { return unsigned(std::min(kWgs, (V + kRows - 1) / kRows)); }
+__host__ __device__ __forceinline__ int tiles_of(int V) { return (V + kRows - 1) / kRows; }
+inline unsigned workgroups(int tiles) { return unsigned(std::min(kWgs, (tiles + 1) / 2)); }
 
 template <int kSteps, int kNB>
 struct Rows {
@@ -48,12 +49,12 @@ struct Rows {
   }
 };
 
-// take(row, z): 4 consecutive vocabulary rows' logits (rows past V: 0) of token 16 b + lane % 16, where waves 0 .. kNB - 1
+// Tiles 0 .. tiles - 1 of W's V rows.  take(row, z): 4 consecutive vocabulary rows' logits (rows past V: 0) of token 16 b + lane % 16, where waves 0 .. kNB - 1
 // take block b = wave; by the same thread for all rows that are equal modulo 16.  It ends with kStores vector-memory
 // operations, always.
 template <int kSteps, int kNB, int kStores, typename Take>
 __device__ __forceinline__ void run(const __bf16* __restrict__ X, const __bf16* __restrict__ W, int n, int d, int V,
-                                    char* lds, Take&& take) {
+                                    int tiles, char* lds, Take&& take) {
   using R = Rows<kSteps, kNB>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t ld = uint32_t(d) * 2u, part = ld / kWaves;  // bytes of a row, and of its eighth
@@ -78,7 +79,6 @@ __device__ __forceinline__ void run(const __bf16* __restrict__ X, const __bf16* 
   for (int s = 0; s < kSteps; ++s) at[s] = uint32_t(fr * R::kPer + R::swz(fr, 4 * s + fq)) * 16u;
   char* ring = lds + wave * (R::kSlots * R::kTile);
   f32x4_t* sums = reinterpret_cast<f32x4_t*>(lds + R::kRing);
-  const int tiles = (V + kRows - 1) / kRows;
   auto fetch = [&](int64_t tile, int slot) {  // past the last tile an empty resource: no access
     const int64_t row = tile * kRows;
     const int rows = __builtin_amdgcn_readfirstlane(int(max(int64_t(0), min(int64_t(kRows), V - row))));
@@ -86,12 +86,18 @@ __device__ __forceinline__ void run(const __bf16* __restrict__ X, const __bf16* 
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) dma16<true>(r, src[s], 0, ring + slot * R::kTile + 1024 * s);
   };
+  // two neighbours a workgroup in turn, where more than one is on its way (12 tokens, d 2048, V 128256: 84 us one by one, 80;
+  // one token, d 4096: 155, and 167 with two)
+  auto tile_of = [&](int i) {
+    constexpr int kPair = R::kSlots > 1 ? 1 : 0;
+    return ((int64_t(blockIdx.x) + int64_t(i >> kPair) * gridDim.x) << kPair) + (i & kPair);
+  };
   wait_vm<0>();  // (the waits below count transfers alone)
 #pragma unroll
-  for (int i = 0; i < R::kSlots; ++i) fetch(int64_t(blockIdx.x) + int64_t(i) * gridDim.x, i);
+  for (int i = 0; i < R::kSlots; ++i) fetch(tile_of(i), i);
   const bool takes = wave < kNB;
   int slot = 0, buf = 0, nth = 0;
-  for (int64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++nth) {
+  for (int64_t tile = tile_of(0); tile < tiles; tile = tile_of(++nth)) {
     // the tile has landed: what may be on its way is later tiles' transfers, and what take() has left since
     constexpr int kLater = (R::kSlots - 1) * kSteps;
     __builtin_amdgcn_sched_barrier(0);
@@ -105,7 +111,7 @@ __device__ __forceinline__ void run(const __bf16* __restrict__ X, const __bf16* 
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) w[s] = *reinterpret_cast<const bf16x8_t*>(ring + slot * R::kTile + at[s]);
     lds_read_done();
-    fetch(tile + int64_t(R::kSlots) * gridDim.x, slot);
+    fetch(tile_of(nth + R::kSlots), slot);
     slot = slot + 1 == R::kSlots ? 0 : slot + 1;
     __builtin_amdgcn_sched_barrier(0);
     f32x4_t acc[kNB];

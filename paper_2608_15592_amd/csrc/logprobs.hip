@@ -63,17 +63,16 @@ __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __res
       });
 }
 
-// Z[v / 16][token][v % 16] of few tokens and all of the vocabulary: a tile's logits lie together.  (With a row for each
-// token, 64 bytes of each at distances of a power of 2, 32 tokens of d 1536, V 151936 take 86 us instead of 71.)
+// Z[v / 32][token][v % 32] of few tokens and all of the vocabulary: the logits of two tiles, a workgroup's, lie together.
 template <int kSteps, int kNB>
 __global__ __launch_bounds__(64 * few::kWaves, 2) void logits_few_kernel(const __bf16* __restrict__ X,
                                                                          const __bf16* __restrict__ W, int n, int d,
                                                                          int V, float* __restrict__ Z) {
   __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
   const int tok = threadIdx.x / 64 * 16 + (threadIdx.x & 15);
-  few::run<kSteps, kNB, 1>(X, W, n, d, V, lds, [&](int64_t row, f32x4_t z) {
-    const buf_rsrc_t out = make_rsrc(Z + size_t(row & ~int64_t(15)) * n, uint32_t(n) * 64u);
-    buf_store16(out, uint32_t(tok) * 64u + uint32_t(row & 15) * 4u, __builtin_bit_cast(uint4, z));
+  few::run<kSteps, kNB, 1>(X, W, n, d, V, few::tiles_of(V), lds, [&](int64_t row, f32x4_t z) {
+    const buf_rsrc_t out = make_rsrc(Z + size_t(row & ~int64_t(31)) * n, uint32_t(n) * 128u);
+    buf_store16(out, uint32_t(tok) * 128u + uint32_t(row & 31) * 4u, __builtin_bit_cast(uint4, z));
   });
 }
 
@@ -309,11 +308,11 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
 
 // ------------------------------------------------------------------ selection
 
-// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  16
-// columns lie together, those of a token `of_tok` apart, and the next of the same token `of_16` on.  Column c is vocabulary
+// Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  32
+// columns lie together, those of a token `of_tok` apart, and the next of the same token `of_32` on.  Column c is vocabulary
 // row v0 + c, or of every `step`-th tile of 256.  One workgroup each.
 template <int kE>
-__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_16, int live, int64_t v0,
+__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_32, int live, int64_t v0,
                                                              int step, float c2, int k, int piece_chunks, int chunk0, int states, int chunks,
                                                              float* __restrict__ part, uint64_t* __restrict__ top) {
   __shared__ TopK<kMaxTop * kE> pick;
@@ -324,7 +323,7 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
   const int first = 256 * kE * c + 4 * tid;  // columns first + 1024 u + e, ascending in 4 u + e
   f32x4_t z[kE / 4];
 #pragma unroll
-  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + size_t((first + 1024 * u) >> 4) * of_16 + (first & 15));
+  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + size_t((first + 1024 * u) >> 5) * of_32 + (first & 31));
   float m = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kE / 4; ++u)
@@ -333,6 +332,7 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
       z[u][e] = first + 1024 * u + e < live ? z[u][e] : -INFINITY;
       m = fmaxf(m, z[u][e]);
     }
+  const float mine = m;
   m = wave_max(m);
   if (lane == 0) wave_m[wave] = m;
   if (tid == 0) pick.count = 0;
@@ -355,31 +355,40 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
     wave_t[wave] = t;
   }
   __syncthreads();
+  s = wave_s[0] + wave_s[1] + wave_s[2] + wave_s[3];
   if (tid == 0) {
     float* p = part + 3 * (size_t(tok) * states + chunk0 + c);
     p[0] = m;
-    p[1] = wave_s[0] + wave_s[1] + wave_s[2] + wave_s[3];
+    p[1] = s;
     p[2] = wave_t[0] + wave_t[1] + wave_t[2] + wave_t[3];
   }
   if (k == 0) return;
-  uint32_t up[kE], most = 0;
-#pragma unroll
-  for (int e = 0; e < kE; ++e) {
-    up[e] = first + 1024 * (e / 4) + e % 4 < live ? ascending(z[e / 4][e % 4]) : 0;
-    most = max(most, up[e]);
-  }
-  int which = 0;
-#pragma unroll
-  for (int e = kE - 1; e >= 0; --e) which = up[e] == most ? e : which;  // the lowest
   auto id = [&](int e) {
     const int col = first + 1024 * (e / 4) + e % 4;
     return int(v0) + (col >> 8) * 256 * step + (col & 255);
   };
-  const uint64_t from = pick.bound_of(most ? key_of(most, id(which)) : 0, k);
+  const float reach = pick.bound_of(first < live ? ascending(mine) : 0u, k);
+  if (reach == reach && s == s) {  // as a rule: numbers, and different ones where it matters
 #pragma unroll
-  for (int e = 0; e < kE; ++e)
-    if (up[e] >= uint32_t(from >> 32) && key_of(up[e], id(e)) >= from && up[e])
-      pick.list[atomicAdd(&pick.count, 1)] = key_of(up[e], id(e));
+    for (int e = 0; e < kE; ++e)
+      if (z[e / 4][e % 4] >= reach)
+        pick.list[atomicAdd(&pick.count, 1)] = key_of(ascending(z[e / 4][e % 4]), id(e));
+  } else {
+    uint32_t up[kE], most = 0;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) {
+      up[e] = first + 1024 * (e / 4) + e % 4 < live ? ascending(z[e / 4][e % 4]) : 0;
+      most = max(most, up[e]);
+    }
+    int which = 0;
+#pragma unroll
+    for (int e = kE - 1; e >= 0; --e) which = up[e] == most ? e : which;  // the lowest
+    const uint64_t from = pick.bound_of(most ? key_of(most, id(which)) : uint64_t(0), k);
+#pragma unroll
+    for (int e = 0; e < kE; ++e)
+      if (up[e] >= uint32_t(from >> 32) && key_of(up[e], id(e)) >= from && up[e])
+        pick.list[atomicAdd(&pick.count, 1)] = key_of(up[e], id(e));
+  }
   __syncthreads();
   uint64_t* out = top + (size_t(tok) * chunks + chunk0 + c) * k;
   const int n = pick.count;
@@ -567,7 +576,7 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
       if (tiled) {
         few::choose(n, d, [&](auto steps, auto nb) {
           logits_few_kernel<decltype(steps)::value, decltype(nb)::value>
-              <<<dim3(few::workgroups(V)), dim3(64 * few::kWaves), 0, s>>>(X, W, n, d, V, b.Z);
+              <<<dim3(few::workgroups(few::tiles_of(V))), dim3(64 * few::kWaves), 0, s>>>(X, W, n, d, V, b.Z);
         });
       } else {
         const bool odd = d % 64 != 0, narrow = n <= 384;
@@ -593,7 +602,7 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int in_piece = (rows + kChunk - 1) / kChunk;
     logprob_select_kernel<kChunk / 256><<<dim3(unsigned(n) * unsigned(in_piece)), block, 0, s>>>(
-        b.Z, tiled ? 16 : p.Vc, tiled ? 16 * n : 16, rows, v0, 1, c2, k, in_piece, int(v0 / kChunk), p.chunks, p.chunks, b.part, b.top);
+        b.Z, tiled ? 32 : p.Vc, tiled ? 32 * n : 32, rows, v0, 1, c2, k, in_piece, int(v0 / kChunk), p.chunks, p.chunks, b.part, b.top);
     ESTP_CHECK_LAUNCH("logprob_select_kernel");
   }
   logprob_merge_kernel<T, false><<<dim3(unsigned(n)), block, 0, s>>>(X, W, targets, d, V, k, inv_t, p.chunks, b.part,
@@ -618,7 +627,7 @@ int launch_quads(const __bf16* X, const __bf16* W, const int32_t* targets, int n
     kernel<<<dim3(256), block, 0, s>>>(X, W, n, d, V, 0, p.sample, p.step, 256 * kSampleTiles, b.Z);
     ESTP_CHECK_LAUNCH("logits_kernel");
     const int live = 256 * (p.sample - 1) + std::min(256, V - 256 * p.step * (p.sample - 1));
-    logprob_select_kernel<kSampleTiles><<<dim3(unsigned(n)), block, 0, s>>>(b.Z, 256 * kSampleTiles, 16, live, 0, p.step, c2,
+    logprob_select_kernel<kSampleTiles><<<dim3(unsigned(n)), block, 0, s>>>(b.Z, 256 * kSampleTiles, 32, live, 0, p.step, c2,
                                                                             k, 1, 0, states, 1, b.part, b.top);
     ESTP_CHECK_LAUNCH("logprob_select_kernel");
   }

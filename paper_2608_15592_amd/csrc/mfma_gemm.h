@@ -30,6 +30,14 @@ __device__ __forceinline__ void buf_store16(buf_rsrc_t r, uint32_t off, uint4 v)
 #endif
 }
 
+template <int kAux = 0>
+__device__ __forceinline__ void buf_store8(buf_rsrc_t r, uint32_t off, uint32_t lo, uint32_t hi) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+  __builtin_amdgcn_raw_buffer_store_b64(u32x2_t{lo, hi}, r, off, 0, kAux);
+#endif
+}
+
 namespace gemm {
 
 constexpr int kWaves = 4;

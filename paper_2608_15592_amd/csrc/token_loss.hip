@@ -26,6 +26,7 @@
 #include "estp_common.h"
 #include "f32_gemm.h"
 #include "f32_split.h"
+#include "few_tokens.h"
 #include "lm_head.h"
 #include "loss_shares.h"
 #include "lse_states.h"
@@ -572,6 +573,41 @@ __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __
       });
 }
 
+// G of a distillation of few tokens, with W in whole runs (few_tokens.h); the same numbers as above.
+template <int kSteps, int kNB>
+__global__ __launch_bounds__(64 * few::kWaves, 2) void loss_grad_few_kernel(const __bf16* __restrict__ Xc,
+                                                                            const __bf16* __restrict__ W,
+                                                                            const int* __restrict__ n_live, int d,
+                                                                            int V, int64_t v0, int Vc,
+                                                                            const float* __restrict__ lc,
+                                                                            const float* __restrict__ gc, float c2,
+                                                                            __bf16* __restrict__ G) {
+  __shared__ __attribute__((aligned(16))) char lds[few::Rows<kSteps, kNB>::kLds];
+  const int n = __builtin_amdgcn_readfirstlane(n_live[0]);  // of two parts each
+  const int rows = __builtin_amdgcn_readfirstlane(int(min(int64_t(V) - v0, int64_t(Vc))));
+  const int s = threadIdx.x / 64 * 16 + (threadIdx.x & 15);
+  const bool live = s < n;
+  const float l2 = live ? lc[s] * kLog2e : 0.f, g = live ? gc[s] : 0.f;
+  const buf_rsrc_t out = make_rsrc(G, uint32_t(2 * n) * uint32_t(Vc) * 2u);
+  const uint32_t base = uint32_t(s) * uint32_t(Vc) * 2u, part = uint32_t(n) * uint32_t(Vc) * 2u;
+  // (whole tiles of 256: what follows reads columns past the last row, where G is 0)
+  few::run<kSteps, kNB, 2>(Xc, W + size_t(v0) * d, n, d, rows, (rows + 255) / 256 * 16, lds,
+                           [&](int64_t row, f32x4_t z) {
+    float p[4];
+    uint32_t q[2], left[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = row + e < rows ? g * fast_exp2(fmaf(z[e], c2, -l2)) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      q[e] = pack_bf16(p[2 * e], p[2 * e + 1]);
+      left[e] = pack_bf16(p[2 * e] - __uint_as_float(q[e] << 16), p[2 * e + 1] - __uint_as_float(q[e] & 0xffff0000u));
+    }
+    const uint32_t off = base + uint32_t(row) * 2u;
+    buf_store8(out, live ? off : kPastEnd, q[0], q[1]);
+    buf_store8(out, live ? off + part : kPastEnd, left[0], left[1]);
+  });
+}
+
 // out[share][slot][k] (+)= G W_piece over the share's vocabulary rows.  M side: columns k of W (transposed reads), N
 // side: slots.  The matrix cores bound it (the sizes above: 870 us, 1.26 PFLOP/s, and 388 us, 0.93 PFLOP/s).
 template <int kNBN>
@@ -810,7 +846,14 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
       const bool odd = d % 64 != 0;
       auto grad_kernel = p.tile_toks == 128 ? (odd ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
                                             : (odd ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
-      grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, c2, G);
+      if (teacher && p.parts == 2 && few::takes(n, d, dtype) && size_t(p.Vc) * 256 < (size_t(1) << 32))
+        few::choose(n, d, [&](auto steps, auto nb) {
+          loss_grad_few_kernel<decltype(steps)::value, decltype(nb)::value>
+              <<<dim3(few::workgroups(p.Vc / 16)), dim3(64 * few::kWaves), 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.lc,
+                                                                                   b.gc, c2, G);
+        });
+      else
+        grad_kernel<<<grid, block, 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.tc, b.lc, b.gc, c2, G);
       ESTP_CHECK_LAUNCH("loss_grad_mfma_kernel");
       if (teacher) {
         const int rc = launch_teacher_entries(*teacher, n, V, dtype, b.slot, b.n_live, v0, p.Vc, G, s);

@@ -33,6 +33,29 @@ struct TopK {
   uint64_t list[kCap], maxima[256], bound;
   int count;
 
+  // Keys of a wave's 256 that hold.
+  template <typename Holds>
+  __device__ static __forceinline__ int number(Holds&& holds) {
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) n += __popcll(__ballot(holds(u)));
+    return n;
+  }
+  __device__ static __forceinline__ int enough(int k) { return min(k + 32, kMaxTop); }
+  __device__ static __forceinline__ uint32_t top_of(const uint32_t (&hi)[4], int k, int* reach) {
+    uint32_t top = 0;
+    *reach = 256;
+    for (uint32_t bit = 0x80000000u; bit && *reach > enough(k); bit >>= 1) {
+      const uint32_t c = top | bit;
+      const int n = number([&](int u) { return hi[u] >= c; });
+      if (n >= k) {
+        top = c;
+        *reach = n;
+      }
+    }
+    return top;
+  }
+
   // A key that k of the threads' keys reach, and kMaxTop at most, or 1 where fewer than k threads have one.  One wave, four
   // keys a lane, forms it bit by bit, until few enough reach it, and what lies below the logit's bits only where equal
   // logits need it.
@@ -48,25 +71,11 @@ struct TopK {
         hi[u] = uint32_t(v >> 32);
         lo[u] = uint32_t(v);
       }
-      auto number = [&](auto&& holds) {
-        int n = 0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) n += __popcll(__ballot(holds(u)));
-        return n;
-      };
-      uint32_t top = 0, low = 0;
-      int reach = 256;
-      const int enough = min(k + 32, kMaxTop);
-      for (uint32_t bit = 0x80000000u; bit && reach > enough; bit >>= 1) {
-        const uint32_t c = top | bit;
-        const int n = number([&](int u) { return hi[u] >= c; });
-        if (n >= k) {
-          top = c;
-          reach = n;
-        }
-      }
+      uint32_t low = 0;
+      int reach;
+      const uint32_t top = top_of(hi, k, &reach);
       const int left = k - number([&](int u) { return hi[u] > top; });
-      if (top && reach > enough)
+      if (top && reach > enough(k))
         for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
           const uint32_t c = low | bit;
           if (number([&](int u) { return hi[u] == top && lo[u] >= c; }) >= left) low = c;
@@ -75,6 +84,25 @@ struct TopK {
     }
     __syncthreads();
     return bound;
+  }
+  // The same of the logits' bits alone: a logit that k of the threads' largest reach, and kMaxTop at most; a NaN where
+  // equal, infinite or too few ones allow none.
+  __device__ __forceinline__ float bound_of(uint32_t mine, int k) {
+    const int tid = threadIdx.x;
+    uint32_t* of = reinterpret_cast<uint32_t*>(maxima);
+    of[tid] = mine;
+    __syncthreads();
+    if (tid < 64) {
+      uint32_t hi[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) hi[u] = of[64 * u + tid];
+      int reach;
+      const uint32_t top = top_of(hi, k, &reach);
+      constexpr uint32_t kLowest = 0x00800000u;  // of the largest negative number
+      if (tid == 0) bound = reach > enough(k) || top < kLowest ? 1u : top;
+    }
+    __syncthreads();
+    return logit_of(bound << 32);
   }
 
   // put(rank, key) by some thread for the k largest of the n keys listed, n <= kCap, the largest first.  All
