@@ -383,8 +383,9 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  *
  * What a server returns beside its tokens, and what a teacher leaves for
  * estp_distill_loss (its temperature here, its top_id and top_logprob there).
- * The logits of up to 8192 tokens at a time are kept for a piece of the
- * vocabulary at most.
+ * Few tokens' logits are kept in the workspace (up to 64 Mi numbers at a time);
+ * of more than 384 tokens of ESTP_BF16, 2048 at a time and V >= 32768, those
+ * that reach the k-th largest of a sample of the vocabulary.
  *
  *   targets [n_tok]  int32, or NULL (then logprob is NULL too); a token whose target is outside
  *                    [0, V) (-100, say) is ignored: its logprob is 0
@@ -395,9 +396,12 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  *   top_id [n_tok, k], top_logprob [n_tok, k]  int32 and float32 outputs; not used where k = 0
  * The order is that of the logits as computed here (fp32 accumulation); a NaN ranks below all
  * others.  Rows with a NaN logit have NaN values; their top_id are indices in [0, V) all the same.
- * X, W, d and dtype are those of estp_token_entropy.  V > 2^24 returns ESTP_ERR_UNSUPPORTED.
- * Bitwise repeatable.  A workspace of a call serves every call of no more tokens and no larger k
- * on the same W.
+ * X, W, d and dtype are those of estp_token_entropy.  fp32 logits of larger calls are formed by
+ * the bf16 matrix cores, each number as the sum of three bf16 ones, and are as exact as fp32 sums.
+ * V > 2^24 returns ESTP_ERR_UNSUPPORTED.  Bitwise repeatable; the last bits are those of the
+ * kernels that a call runs, which follow n_tok, d and V.  A workspace of a call serves every call
+ * of no more tokens and no larger k on the same W; it is largest for 2048 tokens of ESTP_BF16 and
+ * more (room for each of their logits, 4 bytes, once: 1.1 GB at V 128256).
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_logprobs_workspace_size(int64_t n_tok, int32_t d, int32_t V, int32_t k, int dtype);
 ESTP_API int estp_token_logprobs(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,
@@ -428,7 +432,7 @@ ESTP_API int estp_token_logprobs(const void* X, const void* W, const int32_t* ta
  * A row without an entry of weight (a prompt's, say) is ignored: its loss is 0.  X, W, d, dtype and V
  * are those of estp_token_loss; n_tok > 4194304 returns ESTP_ERR_UNSUPPORTED.  A workspace of a call
  * serves every call of no more tokens on the same W.  The last bits of the outputs are those of the
- * kernels that a call runs, which follow n_tok and V.
+ * kernels that a call runs, which follow n_tok, d and V.  (fp32 logits as estp_token_logprobs'.)
  *
  * estp_distill_loss_backward: with grad_i the gradient of the objective with
  * respect to loss_i (temperature^2 / n, say),

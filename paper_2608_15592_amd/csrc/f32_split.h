@@ -290,7 +290,8 @@ void choose(int64_t n, Go&& go) {
   }
 }
 // Calls whose products are worth splitting the tokens for: the launch costs as much as 1 GFLOP of the fp32 kernels.
-inline bool takes(int64_t n, int d, int V) { return double(n) * d * V >= 1e9; }
+// (and 256 rows of W whose offsets fit 32 bits)
+inline bool takes(int64_t n, int d, int V) { return d <= (1 << 20) && double(n) * d * V >= 1e9; }
 
 }  // namespace split
 }  // namespace detail
