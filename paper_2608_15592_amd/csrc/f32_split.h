@@ -289,9 +289,15 @@ void choose(int64_t n, Go&& go) {
     default: return with(std::integral_constant<int, 6>{});
   }
 }
-// Calls whose products are worth splitting the tokens for: the launch costs as much as 1 GFLOP of the fp32 kernels.
-// (and 256 rows of W whose offsets fit 32 bits)
-inline bool takes(int64_t n, int d, int V) { return d <= (1 << 20) && double(n) * d * V >= 1e9; }
+// Calls that the fp32 instructions do no faster: tiles for most compute units, of few tokens, which one pass over W bounds,
+// for all of them more than once.  Log-sum-exps in us here and there: 33 tokens, d 2048, V 128256 (501 tiles) 229 and 323;
+// 30 tokens, d 2048, V 50000 (196) 92 and 107; 200 tokens, d 2048, V 33000 (387) 237 and 506; 300 tokens, d 256, V 16384
+// (256) 36 and 43; 400 tokens, d 512, V 5000 (100) 44 and 39; 100 tokens, d 2048, V 5000 (40) 94 and 61; one token, d 512,
+// V 128256 51 and 56; 8 tokens, d 1024, V 65536 (256) 68 and 54.  (And 256 rows of W whose offsets fit 32 bits.)
+inline bool takes(int64_t n, int d, int V) {
+  const int64_t cols = 16 * blocks_of(n), tiles = ((int64_t(V) + kRows - 1) / kRows) * ((n + cols - 1) / cols);
+  return d >= 64 && d <= (1 << 20) && tiles >= (n <= 16 ? 384 : 192);
+}
 
 }  // namespace split
 }  // namespace detail

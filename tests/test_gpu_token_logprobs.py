@@ -134,8 +134,8 @@ def test_few_tokens(n, d, V):
 
 
 # fp32 calls whose products are formed from parts in bf16: widths of a stage and others, tokens of each tile's width
-SPLIT = [(16, 1024, 65000, 9), (30, 520, 66000, 9), (37, 1000, 28000, 20), (64, 264, 61000, 5), (90, 256, 45000, 20),
-         (100, 72, 140001, 3), (200, 512, 10003, 128), (500, 256, 8300, 9)]
+SPLIT = [(1, 128, 98400, 2), (16, 264, 98500, 9), (30, 520, 50000, 9), (37, 1000, 49200, 20), (64, 264, 61000, 5),
+         (90, 256, 50000, 20), (100, 72, 140001, 3), (200, 512, 17003, 128), (500, 256, 8300, 9)]
 
 
 @pytest.mark.parametrize("n,d,V,k", SPLIT)
@@ -151,7 +151,7 @@ def test_f32_from_parts(n, d, V, k):
 def test_f32_logits_are_as_exact_as_fp32_sums():
     # numbers of 24 significant bits and of very different sizes, logits that cancel: off by less than d roundings of
     # the largest partial sum (a chain of fp32 FMAs is off by up to d)
-    n, d, V = 64, 512, 40000
+    n, d, V = 64, 512, 50000
     g = np.random.default_rng(5)
     X = (g.standard_normal((n, d)) * 2.0 ** g.integers(-6, 7, (n, d))).astype(np.float32)
     W = (g.standard_normal((V, d)) * 2.0 ** g.integers(-9, 3, (V, d))).astype(np.float32)
@@ -166,7 +166,7 @@ def test_f32_logits_are_as_exact_as_fp32_sums():
     assert (np.abs(got - at) <= 8 * OP.U * of + room).all()
 
 
-@pytest.mark.parametrize("dtype,n,V", [("bf16", 1, 5000), ("bf16", 20, 5000), ("bf16", 60, 5000), ("f32", 60, 9000)])
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 1, 5000), ("bf16", 20, 5000), ("bf16", 60, 5000), ("f32", 60, 49300)])
 def test_a_non_finite_row_of_weights_stays_in_its_row(dtype, n, V):
     d = 2048
     X, W, _, _ = _inputs(n, n, d, V, dtype)
