@@ -79,8 +79,34 @@ static __device__ __attribute__((noinline)) float plain(const float* __restrict_
   return z;
 }
 
+// The same of up to 96 rows as the matrix cores take them where the rows are the depth: of 16 columns, a part and 32 rows
+// 1 KB, lane (column lane % 16) the rows 8 (lane / 16) .. + 7; zeros past the live rows.  One workgroup a block of columns.
+constexpr int kDeepRows = 96;
+static __global__ __launch_bounds__(192) void split_columns_kernel(const float* __restrict__ X,
+                                                                   const int* __restrict__ n_live, int d, int steps,
+                                                                   __bf16* __restrict__ parts) {
+  const int lane = threadIdx.x & 63, step = threadIdx.x >> 6, col = 16 * blockIdx.x + (lane & 15), n = *n_live;
+  if (step >= steps) return;
+  uint32_t q[3][4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int row = 32 * step + 8 * (lane >> 4) + 2 * e;
+    const float a = row < n && col < d ? X[size_t(row) * d + col] : 0.f;
+    const float b = row + 1 < n && col < d ? X[size_t(row + 1) * d + col] : 0.f;
+    const Parts p = parts_of(a, b);
+    q[0][e] = p.p1;
+    q[1][e] = p.p2;
+    q[2][e] = p.p3;
+  }
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    *reinterpret_cast<uint4*>(parts + ((size_t(blockIdx.x) * 3 + p) * steps + step) * 512 + 8 * lane) =
+        uint4{q[p][0], q[p][1], q[p][2], q[p][3]};
+}
+
 // Bytes of the parts of n rows.
 inline size_t parts_bytes(size_t n, int d) { return 3 * n * size_t(padded(d)) * 2; }
+inline size_t column_bytes(int d) { return size_t((d + 15) / 16) * 3 * (kDeepRows / 32) * 1024; }
 
 // 256 vocabulary rows x 16 kNB tokens by 8 waves, tile after tile.  Three stages of 32 k in LDS: two are on their way, 64 KB
 // of W, while one is multiplied, across tile boundaries too.  kStream: each row of W is read once in the call.

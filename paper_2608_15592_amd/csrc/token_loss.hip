@@ -398,6 +398,92 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
       }
 }
 
+// A number of dW by fp32 FMAs.  It ends where it has become NaN, which it then stays.
+static __device__ __attribute__((noinline)) float dw_plain(const float* __restrict__ g, int Vc,
+                                                           const float* __restrict__ x, int d, int n) {
+  float z = 0.f;
+  for (int i = 0; i < n && z == z; ++i) z = fmaf(g[size_t(i) * Vc], x[size_t(i) * d], z);
+  return z;
+}
+
+// dW of up to 96 rows of a distillation by the bf16 matrix cores: G^T X of numbers in three parts each, six products, as
+// the logits of f32_split.h and as exact.  A wave holds the parts of G's 64 columns v, all rows deep, in registers, and
+// goes along X's columns, 16 at a time, whose parts split_columns_kernel laid out in the order of the operands; the next
+// ones are on their way meanwhile.  No LDS, no barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a
+// quarter of the columns: G is split once more for each share.  90 tokens, d 1536, V 151936 (933 MB of dW): 326 us, 495
+// with the fp32 instructions' tiles; 471 without the loads ahead, 376 with ordinary stores in place of non-temporal ones.
+// Its 270 GF of bf16 products (190 us) and its stores (190 us at the rate of a copy) overlap in part.
+template <int kSteps>
+__global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __restrict__ G,
+                                                               const float* __restrict__ X,
+                                                               const __bf16* __restrict__ columns,
+                                                               const int* __restrict__ n_live, int d, int V,
+                                                               int64_t v0, int Vc, float* __restrict__ dW) {
+  const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc))), v = 256 * blockIdx.x + 64 * int(threadIdx.x >> 6) + fr;
+  if (v - fr >= rows) return;
+  const buf_rsrc_t rg = make_rsrc(G, uint32_t(n) * uint32_t(Vc) * 4u);  // (rows past the live ones read 0)
+  bf16x8_t g[4][kSteps][3];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      uint32_t q[3][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t at = uint32_t(32 * s + 8 * fq + 2 * e) * uint32_t(Vc) + uint32_t(min(v + 16 * j, Vc - 1));
+        const split::Parts p = split::parts_of(buf_load1(rg, 4u * at), buf_load1(rg, 4u * (at + uint32_t(Vc))));
+        q[0][e] = p.p1;
+        q[1][e] = p.p2;
+        q[2][e] = p.p3;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) g[j][s][p] = __builtin_bit_cast(bf16x8_t, uint4{q[p][0], q[p][1], q[p][2], q[p][3]});
+    }
+  const int blocks = (d + 15) / 16, per = (blocks + int(gridDim.y) - 1) / int(gridDim.y), first = per * int(blockIdx.y);
+  const int last = min(blocks, first + per);
+  bf16x8_t x[kSteps][3], ahead[kSteps][3];
+  const auto load = [&](int c) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+        ahead[s][p] = *reinterpret_cast<const bf16x8_t*>(columns + ((size_t(c) * 3 + p) * kSteps + s) * 512 + 8 * lane);
+  };
+  load(min(first, blocks - 1));
+  for (int c = first; c < last; ++c) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) x[s][p] = ahead[s][p];
+    load(min(c + 1, blocks - 1));
+    f32x4_t acc[4], low[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = low[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    constexpr int kX[6] = {2, 0, 1, 0, 1, 0}, kG[6] = {0, 2, 1, 1, 0, 0};
+#pragma unroll
+    for (int t = 0; t < 6; ++t)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f32x4_t& sum = t == 5 ? acc[j] : low[j];
+          sum = mfma_bf16(x[s][kX[t]], g[j][s][kG[t]], sum);
+        }
+    const int k = 16 * c + 4 * fq;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (v + 16 * j < rows && k < d) {  // (d is a multiple of 8)
+        f32x4_t out = acc[j] + low[j];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!(fabsf(out[r]) < INFINITY)) out[r] = dw_plain(G + v + 16 * j, Vc, X + k + r, d, n);
+        __builtin_nontemporal_store(out, reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + 16 * j) * d + k));
+      }
+  }
+}
+
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
 // Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
@@ -904,6 +990,21 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
+        if (by_parts && n <= split::kDeepRows && size_t(p.Vc) * split::kDeepRows < (size_t(1) << 30)) {
+          const int steps = (n + 31) / 32;
+          __bf16* columns = parts + split::parts_bytes(size_t(n), d) / 2;
+          if (v0 == 0)
+            split::split_columns_kernel<<<dim3(unsigned((d + 15) / 16)), dim3(192), 0, s>>>(Xc, b.n_live, d, steps,
+                                                                                           columns);
+          auto kernel = steps == 1   ? loss_dw_split_kernel<1>
+                        : steps == 2 ? loss_dw_split_kernel<2>
+                                     : loss_dw_split_kernel<3>;
+          const unsigned along = unsigned(std::max(1, std::min(4, d / 128)));  // of the columns: shares of 128 at least
+          kernel<<<dim3(unsigned((p.Vc + 255) / 256), along), block, 0, s>>>(G, Xc, columns, b.n_live, d, V, v0, p.Vc,
+                                                                             static_cast<T*>(dW));
+          ESTP_CHECK_LAUNCH("loss_dw_split_kernel");
+          continue;
+        }
         const bool few = size_t(n_dt) * n_vt < kFewTiles;
         auto dw_kernel = few ? loss_dw_f32_kernel<32> : loss_dw_f32_kernel<kFT>;
         dw_kernel<<<dim3(n_dt, few ? unsigned(p.Vc / 32) : n_vt), block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc,
@@ -923,7 +1024,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
 
 size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype, bool teacher) {
   const size_t loss = carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
-  return loss + (teacher && dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) : 0);
+  return loss + (teacher && dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) + split::column_bytes(d) : 0);
 }
 
 int launch_lm_head_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,

@@ -91,7 +91,7 @@ def test_few_tokens(n, d, V):
 
 
 @pytest.mark.parametrize("n,d,V,K", [(1, 128, 98400, 2), (16, 264, 98500, 9), (30, 520, 50000, 9), (64, 264, 61000, 5),
-                                     (90, 256, 50000, 20), (100, 72, 140001, 3), (200, 512, 17003, 128),
+                                     (65, 72, 50001, 7), (90, 256, 50000, 20), (96, 136, 49153, 4), (100, 72, 140001, 3), (200, 512, 17003, 128),
                                      (500, 256, 8300, 9), (9000, 64, 8200, 4)])
 def test_f32_from_parts(n, d, V, K):
     # products formed from parts in bf16
@@ -173,6 +173,26 @@ def test_non_finite_values_stay_in_their_row():
     bad[5] = bad[9] = True
     assert torch.isnan(loss[bad]).all() and torch.isnan(dX[bad]).all()
     assert torch.isfinite(loss[~bad]).all() and torch.isfinite(dX[~bad]).all()
+
+
+def test_f32_from_parts_with_infinite_numbers():
+    # one live row of X holds an infinite number, two gradients are infinite: dW is infinite or NaN in what they reach, as
+    # products of 64 bits are, and the rest is as it was without them
+    n, d, V = 70, 64, 50000
+    X, W, ids, logp, g = _case(21, n, d, V, 6, "f32")
+    clean = _check((X, W, ids, logp, g), "f32")
+    args = [dev(a) for a in (W, ids, logp)] + [clean["lse"], clean["logq"]]
+    Xd, gd = dev(X), dev(g)
+    live = (((ids >= 0) & (ids < V)) & (logp > -np.inf)).any(axis=1).nonzero()[0]
+    gd[int(live[3])] = float("inf")
+    got = estp.distill_loss_backward(Xd, *args, gd, want_dX=False)[1]
+    # that row's factor (p sum_w - w) is nowhere 0 here, so that every number of dW has a product of infinity in it
+    assert not torch.isfinite(got).any()
+    x = Xd[int(live[3])]
+    rows = torch.randperm(V, generator=torch.Generator().manual_seed(3))[:500].cuda()
+    others = sorted(set(range(V)) - set(ids[int(live[3])].tolist()))
+    rows = rows[torch.isin(rows, torch.tensor(others, device="cuda"))]
+    assert torch.equal(got[rows], torch.sign(x).expand(len(rows), d) * float("inf"))
 
 
 @pytest.mark.parametrize("renormalise", [True, False])
