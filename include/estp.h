@@ -384,8 +384,8 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  * What a server returns beside its tokens, and what a teacher leaves for
  * estp_distill_loss (its temperature here, its top_id and top_logprob there).
  * Few tokens' logits are kept in the workspace (up to 64 Mi numbers at a time);
- * of more than 384 tokens of ESTP_BF16, 2048 at a time and V >= 32768, those
- * that reach the k-th largest of a sample of the vocabulary.
+ * of more than 384 tokens of ESTP_BF16, 2048 at a time and V from 32768 to 2^20,
+ * those that reach the k-th largest of a sample of the vocabulary.
  *
  *   targets [n_tok]  int32, or NULL (then logprob is NULL too); a token whose target is outside
  *                    [0, V) (-100, say) is ignored: its logprob is 0
@@ -401,7 +401,7 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  * V > 2^24 returns ESTP_ERR_UNSUPPORTED.  Bitwise repeatable; the last bits are those of the
  * kernels that a call runs, which follow n_tok, d and V.  A workspace of a call serves every call
  * of no more tokens and no larger k on the same W; it is largest for 2048 tokens of ESTP_BF16 and
- * more (room for each of their logits, 4 bytes, once: 1.1 GB at V 128256).
+ * more (room for each of their logits, 4 bytes, once: 1.1 GB at V 128256, 8.7 GB at 2^20).
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_token_logprobs_workspace_size(int64_t n_tok, int32_t d, int32_t V, int32_t k, int dtype);
 ESTP_API int estp_token_logprobs(const void* X, const void* W, const int32_t* targets, int64_t n_tok, int32_t d, int32_t V,

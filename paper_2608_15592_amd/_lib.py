@@ -600,6 +600,8 @@ def token_logprobs(X: torch.Tensor, W: torch.Tensor, targets: Optional[torch.Ten
     n_tok, d, V, dev = _head_shapes(X, W, targets)
     dt = _dtype_code(X)
     k = int(k)
+    if not -2 ** 31 <= k < 2 ** 31:
+        raise ValueError(f"k must be in [0, 128], got {k}")
     if targets is None and logprob is not None:
         raise ValueError("logprob needs targets")
     for t, name, n, dtype in ((logprob, "logprob", n_tok, torch.float32), (lse, "lse", n_tok, torch.float32),
@@ -615,9 +617,9 @@ def token_logprobs(X: torch.Tensor, W: torch.Tensor, targets: Optional[torch.Ten
         if H is None:
             H = torch.empty(n_tok, dtype=torch.float32, device=dev)
         if top_id is None:
-            top_id = torch.empty(n_tok, max(k, 0), dtype=torch.int32, device=dev)
+            top_id = torch.empty(n_tok, min(max(k, 0), 128), dtype=torch.int32, device=dev)
         if top_logprob is None:
-            top_logprob = torch.empty(n_tok, max(k, 0), dtype=torch.float32, device=dev)
+            top_logprob = torch.empty(n_tok, min(max(k, 0), 128), dtype=torch.float32, device=dev)
         workspace, wsb = _workspace(lib.estp_token_logprobs_workspace_size(n_tok, d, V, k, dt), dev, workspace)
         _check(lib.estp_token_logprobs(_ptr(X), _ptr(W), _ptr(targets), n_tok, d, V, k, float(temperature), dt,
                                        _ptr(logprob), _ptr(lse), _ptr(H), _ptr(top_id), _ptr(top_logprob),

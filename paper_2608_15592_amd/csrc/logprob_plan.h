@@ -67,9 +67,10 @@ inline QuadPlan plan_quads(int n, int V, int k) {
 }
 // By quads and by pieces, us, 20 alternatives: d 2048, V 128256, 256 tokens 247 and 236, 385 tokens 312 and 311, 500 tokens
 // 321 and 367, with 128 alternatives 407 and 397, 1000 tokens of 128 604 and 894; d 1024, V 33000, 400 tokens 96 and 86, 800
-// tokens 132 and 132, 2000 tokens 208 and 273.  (A smaller vocabulary has no sample of its own size to leave out.)
+// tokens 132 and 132, 2000 tokens 208 and 273.  (A smaller vocabulary has no sample of its own size to leave out; of a
+// larger one the room for 2048 tokens' logits would pass 8.6 GB.)
 inline bool use_quads(int64_t n_tok, int V, int dtype) {
-  return dtype == ESTP_BF16 && n_tok > 384 && V >= 256 * 128;
+  return dtype == ESTP_BF16 && n_tok > 384 && V >= 256 * 128 && V <= (1 << 20);
 }
 
 struct LogprobBuffers {

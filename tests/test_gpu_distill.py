@@ -91,7 +91,7 @@ def test_few_tokens(n, d, V):
 
 
 @pytest.mark.parametrize("n,d,V,K", [(1, 128, 98400, 2), (16, 264, 98500, 9), (30, 520, 50000, 9), (64, 264, 61000, 5),
-                                     (65, 72, 50001, 7), (90, 256, 50000, 20), (96, 136, 49153, 4), (100, 72, 140001, 3), (200, 512, 17003, 128),
+                                     (65, 72, 50001, 7), (90, 256, 50000, 20), (96, 136, 49153, 4), (100, 72, 140001, 3), (90, 64, 270001, 5), (200, 512, 17003, 128),
                                      (500, 256, 8300, 9), (9000, 64, 8200, 4)])
 def test_f32_from_parts(n, d, V, K):
     # products formed from parts in bf16
@@ -369,3 +369,44 @@ def test_binding_refuses_mis_sized_tensors():
         estp.distill_loss(X, W, torch.zeros(4, 129, dtype=torch.int32, device="cuda"), torch.zeros(4, 129, device="cuda"))
     with pytest.raises(estp.EstpError, match="temperature"):
         estp.distill_loss(X, W, ids, logp, temperature=0.0)
+
+
+@pytest.mark.parametrize("dtype,n,other,d,V", [("bf16", 40, 300, 1024, 9000), ("f32", 90, 33, 64, 50000),
+                                               ("f32", 20, 130, 64, 50000)])
+def test_two_graphs_on_the_same_workspaces(dtype, n, other, d, V):
+    # a step of loss and gradients each, of different forms and sizes; eager steps on those workspaces come between
+    lib, code, calls, graphs = estp.load(), 0 if dtype == "bf16" else 1, [], []
+    most = max(n, other)
+    wss = [torch.empty(f(most, d, V, code), dtype=torch.uint8, device="cuda")
+           for f in (lib.estp_distill_loss_workspace_size, lib.estp_distill_loss_backward_workspace_size)]
+    W = dev(_inputs(71, 1, d, V, dtype)[1])
+
+    def step(X, ids, logp, g, out=(None,) * 5, ws=(None, None)):
+        loss, lse, logq = estp.distill_loss(X, W, ids, logp, 1.5, loss=out[0], lse=out[1], logq=out[2], workspace=ws[0])
+        dX, dW = estp.distill_loss_backward(X, W, ids, logp, lse, logq, g, 1.5, dX=out[3], dW=out[4], workspace=ws[1])
+        return loss, lse, logq, dX, dW
+
+    for m in (n, other):
+        X, _, ids, logp, g = _case(70 + m, m, d, V, 9, dtype)
+        args = tuple(map(dev, (X, ids, logp, g)))
+        calls.append((args, step(*args, ws=wss)))
+    torch.cuda.synchronize()
+    for args, out in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(*args, out, wss)
+        graphs.append(graph)
+    for rep in range(3):
+        wants = []
+        for args, out in calls:
+            if rep:
+                args[0].copy_(args[0].roll(1, 0))
+                args[2].copy_(args[2].flip(1))
+            wants.append(step(*args))
+            for a in out:
+                a.fill_(-1)
+        for graph in graphs:
+            graph.replay()
+        step(*calls[1][0], ws=wss)
+        for (_, out), want in zip(calls, wants):
+            assert all(torch.equal(a, b) for a, b in zip(out, want)), rep

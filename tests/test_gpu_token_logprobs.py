@@ -344,11 +344,48 @@ def test_binding_refuses_mis_sized_tensors():
             estp.token_logprobs(X, W, t, 2, **{name: f[:3]})
     with pytest.raises(ValueError, match="logprob needs targets"):
         estp.token_logprobs(X, W, None, 2, logprob=f)
-    for k in (10, 129, -1):
+    for k in (10, 129, -1, 2 ** 31 - 1):
         with pytest.raises(estp.EstpError, match="k"):
             estp.token_logprobs(X, W, t, k)
+    with pytest.raises(ValueError, match="k must"):  # not one of 32 bits
+        estp.token_logprobs(X, W, t, 2 ** 32 + 1)
     for temperature in (0.0, -1.0, float("nan"), float("inf")):
         with pytest.raises(estp.EstpError, match="temperature"):
             estp.token_logprobs(X, W, t, 2, temperature=temperature)
     with pytest.raises(estp.EstpError, match="workspace"):
         estp.token_logprobs(X, W, t, 2, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,n,other,d,V", [("bf16", 12, 700, 1024, 33000), ("bf16", 500, 3, 64, 33000),
+                                               ("f32", 40, 17, 64, 50000), ("f32", 200, 9, 32, 9000)])
+def test_two_graphs_on_one_workspace(dtype, n, other, d, V):
+    # the calls of two graphs have different forms and sizes; eager calls on that workspace come between the replays
+    k, code = 11, 0 if dtype == "bf16" else 1
+    calls, graphs = [], []
+    size = estp.load().estp_token_logprobs_workspace_size(max(n, other), d, V, k, code)
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    W = dev(_inputs(61, 1, d, V, dtype)[1])
+    for m in (n, other):
+        X, _, t, _ = _inputs(60 + m, m, d, V, dtype)
+        X, t = dev(X), dev(t)
+        calls.append((X, t, estp.token_logprobs(X, W, t, k, workspace=ws)))
+    names = ("logprob", "lse", "H", "top_id", "top_logprob")
+    torch.cuda.synchronize()
+    for X, t, out in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            estp.token_logprobs(X, W, t, k, workspace=ws, **dict(zip(names, out)))
+        graphs.append(graph)
+    for rep in range(3):
+        wants = []
+        for X, t, out in calls:
+            if rep:
+                X.copy_(X.roll(1, 0) if rep == 1 else -X)
+            wants.append(estp.token_logprobs(X, W, t, k))
+            for a in out:
+                a.fill_(-1)
+        for graph in graphs:
+            graph.replay()
+        estp.token_logprobs(calls[0][0], W, None, k, workspace=ws)
+        for (_, _, out), want in zip(calls, wants):
+            assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
