@@ -15,6 +15,7 @@ namespace estp {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
@@ -52,13 +53,21 @@ __device__ __forceinline__ void lds_dma16_buf(buf_rsrc_t r, uint32_t voffset, ui
 #endif
 }
 
-// 16- and 4-byte loads at a byte offset of a buffer resource; kPastEnd is past the end of any resource here.
+// 16-, 8- and 4-byte loads at a byte offset of a buffer resource; kPastEnd is past the end of any resource here.
 constexpr uint32_t kPastEnd = 0xfffffff0u;
 __device__ __forceinline__ f32x4_t buf_load4(buf_rsrc_t r, uint32_t off) {
 #if defined(__HIP_DEVICE_COMPILE__)
   return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
 #else
   return f32x4_t{};
+#endif
+}
+template <int kPolicy = 0>
+__device__ __forceinline__ f32x2_t buf_load2(buf_rsrc_t r, uint32_t off) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_bit_cast(f32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kPolicy));
+#else
+  return f32x2_t{};
 #endif
 }
 __device__ __forceinline__ float buf_load1(buf_rsrc_t r, uint32_t off) {

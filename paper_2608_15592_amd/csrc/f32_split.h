@@ -51,6 +51,26 @@ __device__ __forceinline__ Parts parts_of(float a, float b) {
   return r;
 }
 
+// 8 numbers of a lane, as they are, and their parts, formed in 8 pieces.
+struct Raw {
+  float v[8];
+};
+struct Frag {
+  uint32_t q[3][4];
+  __device__ __forceinline__ bf16x8_t part(int p) const {
+    return __builtin_bit_cast(bf16x8_t, uint4{q[p][0], q[p][1], q[p][2], q[p][3]});
+  }
+  __device__ __forceinline__ void piece(Raw& r, int j) {
+    const int e = j / 2;
+    float &a = r.v[2 * e], &b = r.v[2 * e + 1];
+    const uint32_t pair = as_formed(pack_bf16(a, b));
+    a -= low_half(pair);
+    b -= top_half(pair);
+    q[j % 2][e] = pair;
+    if (j % 2) q[2][e] = pack_bf16(a, b);
+  }
+};
+
 // parts[p][row][padded(d)] of X's rows, below n (or *n_live).  Four numbers a thread.
 static __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ X, int n,
                                                                 const int* __restrict__ n_live, int d,
@@ -172,32 +192,12 @@ struct Tile {
         where = pf < count ? at(pf) : Place{0, 0};
       }
     };
-    // 8 numbers of 16 rows a lane, as they are, and their parts
-    struct Raw {
-      float v[8];
-    };
     auto read = [&](int slot, int i) {
       const int row = 32 * wave + 16 * i + fr, g = (row >> 1) & 7;
       const char* p = lds + slot * kStage + row * 128;
       const f32x4_t lo = *reinterpret_cast<const f32x4_t*>(p + ((2 * fq) ^ g) * 16);
       const f32x4_t hi = *reinterpret_cast<const f32x4_t*>(p + ((2 * fq + 1) ^ g) * 16);
       return Raw{{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}};
-    };
-    // parts of 8 numbers, formed in 8 pieces
-    struct Frag {
-      uint32_t q[3][4];
-      __device__ __forceinline__ bf16x8_t part(int p) const {
-        return __builtin_bit_cast(bf16x8_t, uint4{q[p][0], q[p][1], q[p][2], q[p][3]});
-      }
-      __device__ __forceinline__ void piece(Raw& r, int j) {
-        const int e = j / 2;
-        float &a = r.v[2 * e], &b = r.v[2 * e + 1];
-        const uint32_t pair = as_formed(pack_bf16(a, b));
-        a -= low_half(pair);
-        b -= top_half(pair);
-        q[j % 2][e] = pair;
-        if (j % 2) q[2][e] = pack_bf16(a, b);
-      }
     };
     wait_vm<0>();  // (the waits below count transfers alone)
     fetch();
@@ -300,6 +300,13 @@ inline int blocks_of(int64_t n) {
       best = nb;
     }
   }
+  return best;
+}
+// The same of a tile whose depth is the vocabulary (dX).
+inline int deep_blocks(int64_t n) {
+  int best = 6;
+  for (int nb : {4, 2})
+    if ((n + 16 * nb - 1) / (16 * nb) * (nb + 3) < (n + 16 * best - 1) / (16 * best) * (best + 3)) best = nb;
   return best;
 }
 // go(kNB, kStream) as integral constants.

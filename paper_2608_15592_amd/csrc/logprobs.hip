@@ -5,9 +5,16 @@
 //   H_i = lse_i - sum_v exp(s_i[v] - lse_i) s_i[v]
 //   top_i = the k largest z_i[v], descending, the lowest v first among equals
 //
-// The logits of a block of tokens over a piece of the vocabulary are formed by the matrix cores and kept in fp32
-// (logits_mfma_kernel, logits_f32_kernel); logprob_select_kernel makes of each chunk of a row a partial state and its k
+// Few tokens, and fp32 (launch_pieces): the logits of a block of tokens over a piece of the vocabulary are formed by the
+// matrix cores and kept in fp32 (logits_few_kernel, where one pass over W bounds the call; logits_mfma_kernel;
+// logits_split_kernel, logits_f32_kernel); logprob_select_kernel makes of each chunk of a row a partial state and its k
 // largest logits; logprob_merge_kernel joins a row's chunks.
+//
+// Many tokens of bf16 (launch_quads): to write and read again 4 bytes a logit would cost as much as half of the products.
+// So a sample of the vocabulary's tiles gives a lower bound of each token's k-th largest logit, by the two kernels above,
+// and the products of all other tiles end in the partial states and in the few logits that reach the bound
+// (logprob_main_kernel), which logprob_merge_kernel ranks.  8192 tokens, d 4096, V 128256, 64 alternatives: 6.4 to 6.7 ms,
+// 1.28 to 1.34 PFLOP/s over all of it; 5.9 ms is what a plain product of this size takes at the card's best rate.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,7 +35,9 @@ namespace detail {
 // ------------------------------------------------------------------ logits
 
 // Z[token][v] of n_m vocabulary tiles, every `step`-th from row v0 (rows past V: 0), pitch Vc.  M side: vocabulary rows.
-// A lane holds 8 consecutive vocabulary rows of a token: two 16-byte stores.
+// A lane holds 8 consecutive vocabulary rows of a token: two 16-byte stores.  Bound by the matrix cores and the stores: a
+// sample of 39 tiles, 2048 tokens, d 4096, 109 us, 1.54 PFLOP/s; of 1511 tokens, d 2048, which 240 workgroups of 256 share
+// a tile each, 69.
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __restrict__ X,
                                                              const __bf16* __restrict__ W, int n, int d, int V,
@@ -64,6 +73,8 @@ __global__ __launch_bounds__(256, 1) void logits_mfma_kernel(const __bf16* __res
 }
 
 // Z[v / 32][token][v % 32] of few tokens and all of the vocabulary: the logits of two tiles, a workgroup's, lie together.
+// Bound by the bytes of W: one token, d 4096, V 128256 155 us, 6.8 TB/s; 48 tokens, d 1536, V 151936 88 us, 5.3 TB/s, and
+// 29 MB of logits besides.
 template <int kSteps, int kNB>
 __global__ __launch_bounds__(64 * few::kWaves, 2) void logits_few_kernel(const __bf16* __restrict__ X,
                                                                          const __bf16* __restrict__ W, int n, int d,
@@ -103,7 +114,8 @@ __global__ __launch_bounds__(256, 2) void logits_f32_kernel(const float* __restr
   }
 }
 
-// The same of vocabulary rows v0 .. v0 + Vc by the bf16 matrix cores.
+// The same of vocabulary rows v0 .. v0 + Vc by the bf16 matrix cores.  37 tokens, d 2048, V 128256: 237 us, 4.4 TB/s of W
+// (323 by the fp32 instructions); 48 columns' products, 121 GF in bf16, and the splitting of W take about as long as W.
 template <int kNB, bool kStream>
 __global__ __launch_bounds__(64 * split::kWaves, 2) void logits_split_kernel(const float* __restrict__ X,
                                                                              const __bf16* __restrict__ parts,
@@ -171,7 +183,9 @@ __device__ __forceinline__ uint32_t settled(uint32_t v) {
 //
 // What follows a tile's products is a branch only where a state is refolded: a quad that is not wanted is stored past the
 // end of the resource.  (With a branch and a list for each, sums were moved to memory and back: 125 us a tile of d 4096,
-// V 128256, and 93 without.)
+// V 128256, and 93 without.)  Bound by the matrix cores: 2048 tokens, d 4096, the 462 tiles that are not in a sample of 39
+// of V 128256: 1410 us, 1.41 PFLOP/s, where the same products end in a log-sum-exp alone at 1.58; the rest is the entropy's
+// second sum, the comparisons and the stores.
 template <bool kOdd, bool kTop>
 __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __restrict__ X,
                                                               const __bf16* __restrict__ W, int n, int d, int V,
@@ -310,7 +324,9 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
 
 // Partial state (base 2) and the k largest logits of 256 kE columns of Z's row, chunk `chunk0 + c` of the token's.  32
 // columns lie together, those of a token `of_tok` apart, and the next of the same token `of_32` on.  Column c is vocabulary
-// row v0 + c, or of every `step`-th tile of 256.  One workgroup each.
+// row v0 + c, or of every `step`-th tile of 256.  One workgroup each, with its logits in registers: they are read once.
+// One token's 16 chunks of 8192: 6 us, latency; 48 tokens, 19 chunks: 13.5 (29 MB, from L2 or the last cache); 2048 tokens'
+// samples, 84 MB: 31, 2.7 TB/s, what the barriers of the bound and of the ranking leave.
 template <int kE>
 __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_32, int live, int64_t v0,
                                                              int step, float c2, int k, int piece_chunks, int chunk0, int states, int chunks,
@@ -397,7 +413,9 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
 }
 
 // A token's outputs from its `states` partial states and from the k largest of each of its `chunks` chunks, or (kQuads)
-// from the k largest of the sample and the quads that reach them.  One workgroup each.
+// from the k largest of the sample and the quads that reach them.  One workgroup each; latency: bits, then quads, then the
+// ranking, each behind the other.  One token 5 us; 1511 tokens with 5 alternatives 24; 2048 with 64, some 800 quads each,
+// 71 (16-byte reads far apart).
 template <typename T, bool kQuads>
 __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict__ X, const T* __restrict__ W,
                                                             const int32_t* __restrict__ targets, int d, int V, int k,

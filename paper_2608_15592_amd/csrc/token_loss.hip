@@ -294,7 +294,8 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
   }
 }
 
-// G of a distillation by the bf16 matrix cores: loss_grad_f32_kernel's, from the parts of the live rows.
+// G of a distillation by the bf16 matrix cores: loss_grad_f32_kernel's, from the parts of the live rows.  90 tokens, d
+// 1536, V 151936: 305 us; by the fp32 instructions 506.
 template <int kNB, bool kStream>
 __global__ __launch_bounds__(64 * split::kWaves, 2) void loss_grad_split_kernel(
     const float* __restrict__ Xc, const __bf16* __restrict__ parts, int n_max, const float* __restrict__ W,
@@ -398,12 +399,145 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
       }
 }
 
-// A number of dW by fp32 FMAs.  It ends where it has become NaN, which it then stays.
-static __device__ __attribute__((noinline)) float dw_plain(const float* __restrict__ g, int Vc,
-                                                           const float* __restrict__ x, int d, int n) {
+// The sum of n products, numbers `ld_a` and `ld_b` apart, by fp32 FMAs.  It ends where it has become NaN, which it then
+// stays.
+static __device__ __attribute__((noinline)) float plain_sum(const float* __restrict__ a, size_t ld_a,
+                                                            const float* __restrict__ b, size_t ld_b, int n) {
   float z = 0.f;
-  for (int i = 0; i < n && z == z; ++i) z = fmaf(g[size_t(i) * Vc], x[size_t(i) * d], z);
+  for (int i = 0; i < n && z == z; ++i) z = fmaf(a[i * ld_a], b[i * ld_b], z);
   return z;
+}
+
+// loss_dx_f32_kernel's sums of a distillation by the bf16 matrix cores, numbers in three parts each.  Workgroup (256
+// columns, 16 kNB tokens, share); a wave takes 32 columns and all of those tokens, 32 vocabulary rows a step.  W goes into
+// registers as it lies, 8 rows and 2 columns a lane, a step ahead, and is split between the products of the step before.
+// G's parts, which the waves share, are formed by a wave for each 16 tokens, and lie in LDS in the order of the operands,
+// two steps of them: one barrier a step.  M side: columns of W, N side: tokens.
+template <int kNB>
+__global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __restrict__ G, const float* __restrict__ W,
+                                                               const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                               int Vc, int n_cols, int n_tiles, int n_slices, int wgs,
+                                                               size_t room, bool first, float* __restrict__ sums) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * 3072 * kNB];
+  const gemm::SliceAt wg = gemm::slice_of(gemm::first_tile(blockIdx.x, gridDim.x), n_tiles, n_slices);
+  const int all = __builtin_amdgcn_readfirstlane(n_live[1]), n0 = wg.tile / n_cols * 16 * kNB, n = min(16 * kNB, all - n0);
+  if (wg.slice >= n_slices || n <= 0) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
+  const int c0 = 256 * (wg.tile % n_cols) + 32 * wave;
+  const Shares sh = dx_shares(all, d, Vc, 16 * kNB, wgs, room);
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc)));
+  G += size_t(n0) * Vc;
+  const buf_rsrc_t rg = make_rsrc(G, uint32_t(n) * uint32_t(Vc) * 4u);  // (rows past the live ones read 0)
+  uint32_t off[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) off[e] = (uint32_t(8 * fq + e) * uint32_t(d) + uint32_t(c0 + 2 * fr)) * 4u;
+  for (int share = wg.slice; share < sh.n; share += n_slices) {
+    const Depth depth = sh.depth(share, rows);
+    const int steps = (depth.k1 - depth.k0 + 63) / 64 * 2;  // (of rows past the share's nothing but zeros)
+    // (columns past d hold the next row's numbers, or 0; they are not stored)
+    auto load_w = [&](int t, split::Raw (&raw)[2]) {
+      const int at = depth.k0 + 32 * t, left = c0 < d ? max(0, min(32, depth.k1 - at)) : 0;
+      const buf_rsrc_t r = make_rsrc(W + size_t(v0 + (left > 0 ? at : 0)) * d, uint32_t(left) * uint32_t(d) * 4u);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const f32x2_t w = buf_load2<kNonTemporal>(r, off[e]);
+        raw[0].v[e] = w[0];
+        raw[1].v[e] = w[1];
+      }
+    };
+    f32x4_t g[2];
+    auto load_g = [&](int t) {
+      if (wave >= kNB || t >= steps) return;
+      const uint32_t o = (uint32_t(16 * wave + fr) * uint32_t(Vc) + uint32_t(depth.k0 + 32 * t + 8 * fq)) * 4u;
+      g[0] = buf_load4(rg, o);
+      g[1] = buf_load4(rg, o + 16u);
+    };
+    auto keep_g = [&](int t) {
+      if (wave >= kNB || t >= steps) return;
+      split::Raw r{{g[0][0], g[0][1], g[0][2], g[0][3], g[1][0], g[1][1], g[1][2], g[1][3]}};
+      const int left = depth.k1 - depth.k0 - 32 * t;
+      if (left < 32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = 8 * fq + e < left ? r.v[e] : 0.f;
+      }
+      split::Frag f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f.piece(r, j);
+#pragma unroll
+      for (int p = 0; p < 3; ++p)
+        *reinterpret_cast<bf16x8_t*>(lds + (t & 1) * 3072 * kNB + (3 * wave + p) * 1024 + 16 * lane) = f.part(p);
+    };
+    f32x4_t acc[2][kNB], low[2][kNB];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int b = 0; b < kNB; ++b) acc[i][b] = low[i][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    split::Raw even[2], odd[2];
+    split::Frag here[2], next[2];
+    load_g(0);
+    load_w(0, even);
+    load_w(1, odd);
+    keep_g(0);
+    load_g(1);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) here[i].piece(even[i], j);
+    lds_barrier();
+    // step t from `w`; `later` are the rows of step t + 1, and those of t + 2 come into `free`
+    auto step = [&](int t, const split::Frag (&w)[2], split::Frag (&then)[2], split::Raw (&later)[2],
+                    split::Raw (&free)[2]) {
+      load_w(t + 2, free);
+      keep_g(t + 1);
+      load_g(t + 2);
+      const char* from = lds + (t & 1) * 3072 * kNB + 16 * lane;
+      bf16x8_t x[2][3];
+      auto read = [&](int b) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) x[b & 1][p] = *reinterpret_cast<const bf16x8_t*>(from + (3 * b + p) * 1024);
+      };
+      read(0);
+      __builtin_amdgcn_sched_barrier(0);
+      constexpr int kEvery = 12 * kNB / 16;
+#pragma unroll
+      for (int m = 0; m < 12 * kNB; ++m) {
+        constexpr int kW[6] = {2, 0, 1, 0, 1, 0}, kX[6] = {0, 2, 1, 1, 0, 0};
+        const int b = m / 12, s = m % 12 / 2, i = m % 2;
+        if (m % 12 == 0 && b + 1 < kNB) read(b + 1);
+        f32x4_t& sum = s == 5 ? acc[i][b] : low[i][b];
+        sum = mfma_bf16(w[i].part(kW[s]), x[b & 1][kX[s]], sum);
+        if (m % kEvery == 0 && m / kEvery < 16) then[m / kEvery / 8].piece(later[m / kEvery / 8], m / kEvery % 8);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lds_barrier();
+    };
+    for (int t = 0; t < steps; t += 2) {
+      step(t, here, next, odd, even);
+      step(t + 1, next, here, even, odd);
+    }
+    float* out = sums + (size_t(share) * size_t(all) + n0) * d;
+    const int c = c0 + 8 * fq;
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      const int s = 16 * b + fr;
+      if (s >= n || c >= d) continue;  // (d is a multiple of 8)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4_t v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = 2 * h + q / 2, i = q % 2;
+          v[q] = acc[i][b][r] + low[i][b][r];
+          if (!(fabsf(v[q]) < INFINITY))
+            v[q] = plain_sum(G + size_t(s) * Vc + depth.k0, 1, W + size_t(v0 + depth.k0) * d + c + 4 * h + q, d,
+                             depth.k1 - depth.k0);
+        }
+        f32x4_t* o = reinterpret_cast<f32x4_t*>(out + size_t(s) * d + c + 4 * h);
+        if (!first) v += *o;
+        *o = v;
+      }
+    }
+  }
 }
 
 // dW of up to 96 rows of a distillation by the bf16 matrix cores: G^T X of numbers in three parts each, six products, as
@@ -478,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
         f32x4_t out = acc[j] + low[j];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (!(fabsf(out[r]) < INFINITY)) out[r] = dw_plain(G + v + 16 * j, Vc, X + k + r, d, n);
+          if (!(fabsf(out[r]) < INFINITY)) out[r] = plain_sum(G + v + 16 * j, Vc, X + k + r, d, n);
         __builtin_nontemporal_store(out, reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + 16 * j) * d + k));
       }
   }
@@ -490,7 +624,9 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
 // first tile's maximum is the reference; later tiles add to the sum with one FMA, exponential and addition a logit,
 // and move the reference only where a sum would pass 2^64.  Partial states [n_tok, 2 n_slices], a wave's 128 rows each.
-// 61 tokens, d 4096, V 128256: 217 us, 4.8 TB/s of W; 1021 tokens, d 2048: 450 us, 1.19 PFLOP/s.
+// 61 tokens, d 4096, V 128256: 217 us, 4.8 TB/s of W; 1021 tokens, d 2048: 404 us, 1.33 PFLOP/s; 4096 tokens, d 4096:
+// 2716 us, 1.58 PFLOP/s.  (The sums leave the matrix cores' registers column by column, read_sum: with all of them at once,
+// some went through memory, and the three took 217, 450 and 2820 us.)
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __restrict__ X,
                                                                const __bf16* __restrict__ W, int n_tok, int d, int V,
@@ -577,8 +713,9 @@ __global__ __launch_bounds__(256, 1) void loss_lse_mfma_kernel(const __bf16* __r
 
 // G of a piece: products of W's rows (M side) and the live tokens (N side), turned into G as they leave the matrix
 // cores.  A lane holds 8 consecutive vocabulary rows of a token: one 16-byte store.  Bound by the matrix cores, with
-// the exponentials between two tiles (4096 tokens, d 4096, 32768 vocabulary rows, 1.1 TFLOP: 830 us, 1.32 PFLOP/s;
-// 684 live tokens, d 2048, all of 128256: 353 us, 1.02 PFLOP/s, a ninth of it on columns that no token has).
+// the exponentials between two tiles (4096 tokens, d 4096, 32768 vocabulary rows, 1.1 TFLOP: 735 us, 1.50 PFLOP/s;
+// 684 live tokens, d 2048, all of 128256: 353 us, 1.02 PFLOP/s, a ninth of it on columns that no token has; 766 of 1021
+// live 417).
 template <int kNBN, bool kOdd>
 __global__ __launch_bounds__(256, 1) void loss_grad_mfma_kernel(const __bf16* __restrict__ Xc,
                                                                 const __bf16* __restrict__ W,
@@ -851,6 +988,7 @@ inline LossPlan plan_loss(int64_t n_tok, int d, int V, int dtype, bool teacher) 
   // (dX of a distillation, 90 tokens, d 1536, V 151936: 96 columns 372 us, 128 481)
   if (teacher && dtype == ESTP_F32 && p.tile_toks == kFT && (n_tok + 95) / 96 * 96 < (n_tok + kFT - 1) / kFT * kFT)
     p.tile_toks = 96;
+  if (teacher && dtype == ESTP_F32 && split::takes(n_tok, d, V)) p.tile_toks = 16 * split::deep_blocks(n_tok);
   const int64_t tiles = (n_tok + p.tile_toks - 1) / p.tile_toks * ((d + 255) / 256);
   p.n_split = int(std::min<int64_t>(std::max<int64_t>(1, 256 / tiles), (vc + 63) / 64));
   return p;
@@ -977,7 +1115,16 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         const int rc = launch_teacher_entries(*teacher, n, V, dtype, b.slot, b.n_live, v0, p.Vc, G, s);
         if (rc != ESTP_OK) return rc;
       }
-      if (dX) {
+      if (dX && by_parts) {
+        const int n_cols = (d + 255) / 256, n_tiles = n_cols * int(n_tt);
+        const int slices = int(std::min<int64_t>(std::max(1, kWgs / n_tiles), (p.Vc + 63) / 64));
+        auto kernel = p.tile_toks == 32   ? loss_dx_split_kernel<2>
+                      : p.tile_toks == 64 ? loss_dx_split_kernel<4>
+                                          : loss_dx_split_kernel<6>;
+        kernel<<<dim3(unsigned((int64_t(n_tiles) * slices + 7) / 8 * 8)), dim3(512), 0, s>>>(
+            G, Wt, b.n_live, d, V, v0, p.Vc, n_cols, n_tiles, slices, kWgs, b.room, v0 == 0, b.acc);
+        ESTP_CHECK_LAUNCH("loss_dx_split_kernel");
+      } else if (dX) {
         // (a workgroup for every share there could be, up to a million in all: past that, a loop over the shares)
         const int64_t most = std::max<int64_t>(1, (int64_t(1) << 20) / (int64_t(n_dt) * n_tt));
         const unsigned shares = unsigned(std::min({int64_t(kWgs), int64_t((p.Vc + 63) / 64), most}));
@@ -990,7 +1137,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
-        if (by_parts && n <= split::kDeepRows && size_t(p.Vc) * split::kDeepRows < (size_t(1) << 30)) {
+        if (by_parts && n <= split::kDeepRows) {
           const int steps = (n + 31) / 32;
           __bf16* columns = parts + split::parts_bytes(size_t(n), d) / 2;
           if (v0 == 0)
@@ -1120,8 +1267,9 @@ namespace {
 // bf16 calls of more tokens run the entropy kernel, whose 16 slices then fill the chip.  d 2048, V 128256, here against
 // there: 128 tokens 137 and 154 us, 1021 tokens 451 and 626, 2048 tokens 870 and 1220, 2500 tokens 1077 and 991, 4096
 // tokens 1735 and 1544; d 4096 2048 tokens 1568 and 2304, 2304 tokens 1767 and 1629; d 1536, V 151936, 782 and 1149, 888
-// and 802.  (Its sums keep one order for any number of tokens, and it forms H and the mode too.)  fp32:
-// the entropy kernel runs on the vector units.
+// and 802.  (Figures of a form of loss_lse_mfma_kernel that was a tenth slower; since then it is the faster one of 4096
+// tokens at d 4096 too, 2716 and 2882, but the entropy kernel's sums keep one order for any number of tokens, so losses
+// keep their last bits, and it forms H and the mode too.)  fp32: the entropy kernel runs on the vector units.
 bool own_lse(int64_t n_tok, int dtype) { return dtype == ESTP_F32 || n_tok <= 2048; }
 
 }  // namespace
