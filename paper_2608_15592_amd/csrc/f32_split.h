@@ -1,4 +1,5 @@
-// fp32 logits by the bf16 matrix cores, shared by logprobs.hip and distill.hip.
+// fp32 logits by the bf16 matrix cores, shared by logprobs.hip, distill.hip and token_loss.hip (whose dX and dW of a
+// distillation form their products of the same parts).
 //
 // A number of 24 bits is the sum of three bf16 numbers, each what rounding has left of it: x = x1 + x2 + x3.  Of the nine
 // products of two numbers' parts, six are formed: x1 w1, and apart from it, where rounding costs less, x1 w2, x2 w1, x2 w2,

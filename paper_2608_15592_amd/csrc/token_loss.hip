@@ -412,7 +412,9 @@ static __device__ __attribute__((noinline)) float plain_sum(const float* __restr
 // columns, 16 kNB tokens, share); a wave takes 32 columns and all of those tokens, 32 vocabulary rows a step.  W goes into
 // registers as it lies, 8 rows and 2 columns a lane, a step ahead, and is split between the products of the step before.
 // G's parts, which the waves share, are formed by a wave for each 16 tokens, and lie in LDS in the order of the operands,
-// two steps of them: one barrier a step.  M side: columns of W, N side: tokens.
+// two steps of them: one barrier a step.  M side: columns of W, N side: tokens.  By parts and by the fp32 instructions, us:
+// 12 tokens, d 2048, V 128256 173 and 195, 33 tokens 226 and 309, 200 827 and 1039, 400 1374 and 2075; 90 tokens, d 1536, V
+// 151936 250 and 394, 3.7 TB/s of W and 1.1 PFLOP/s: W and the matrix cores take about 133 and 190 of it each.
 template <int kNB>
 __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __restrict__ G, const float* __restrict__ W,
                                                                const int* __restrict__ n_live, int d, int V, int64_t v0,
@@ -543,10 +545,11 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
 // dW of up to 96 rows of a distillation by the bf16 matrix cores: G^T X of numbers in three parts each, six products, as
 // the logits of f32_split.h and as exact.  A wave holds the parts of G's 64 columns v, all rows deep, in registers, and
 // goes along X's columns, 16 at a time, whose parts split_columns_kernel laid out in the order of the operands; the next
-// ones are on their way meanwhile.  No LDS, no barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a
-// quarter of the columns: G is split once more for each share.  90 tokens, d 1536, V 151936 (933 MB of dW): 326 us, 495
-// with the fp32 instructions' tiles; 471 without the loads ahead, 376 with ordinary stores in place of non-temporal ones.
-// Its 270 GF of bf16 products (190 us) and its stores (190 us at the rate of a copy) overlap in part.
+// ones are on their way meanwhile.  No barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a quarter
+// of the columns: G is split once more for each share.  Results pass LDS, 64 columns at a time, so that 256 bytes of a row
+// leave together, non-temporal.  90 tokens, d 1536, V 151936 (933 MB of dW): 265 to 284 us on two cards of another pace, 495
+// with the fp32 instructions' tiles; 471 with ordinary 64-byte runs and no loads ahead, 376 with these, 326 non-temporal.
+// 12 and 33 tokens, d 2048, V 128256 (1.05 GB): 265 and 260, 442 and 465 in runs of 64 bytes; 4.0 TB/s of stores.
 template <int kSteps>
 __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __restrict__ G,
                                                                const float* __restrict__ X,
@@ -575,8 +578,12 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
 #pragma unroll
       for (int p = 0; p < 3; ++p) g[j][s][p] = __builtin_bit_cast(bf16x8_t, uint4{q[p][0], q[p][1], q[p][2], q[p][3]});
     }
-  const int blocks = (d + 15) / 16, per = (blocks + int(gridDim.y) - 1) / int(gridDim.y), first = per * int(blockIdx.y);
-  const int last = min(blocks, first + per);
+  // a wave's 64 rows of 64 columns, which leave it in whole runs of a row
+  constexpr int kPitch = 68;
+  __shared__ __attribute__((aligned(16))) float lds[4 * 64 * kPitch];
+  float* mine = lds + (threadIdx.x >> 6) * (64 * kPitch);
+  const int blocks = (d + 15) / 16, per = ((blocks + 3) / 4 + int(gridDim.y) - 1) / int(gridDim.y) * 4;
+  const int first = per * int(blockIdx.y), last = min(blocks, first + per);
   bf16x8_t x[kSteps][3], ahead[kSteps][3];
   const auto load = [&](int c) {
 #pragma unroll
@@ -613,8 +620,19 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
 #pragma unroll
         for (int r = 0; r < 4; ++r)
           if (!(fabsf(out[r]) < INFINITY)) out[r] = plain_sum(G + v + 16 * j, Vc, X + k + r, d, n);
-        __builtin_nontemporal_store(out, reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + 16 * j) * d + k));
+        *reinterpret_cast<f32x4_t*>(mine + (16 * j + fr) * kPitch + 16 * (c & 3) + 4 * fq) = out;
       }
+    if ((c & 3) != 3 && c + 1 < last) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int col = 16 * (c & ~3) + 4 * fr;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i)
+      if (v - fr + 4 * i + fq < rows && col < min(d, 16 * (c + 1)))
+        __builtin_nontemporal_store(*reinterpret_cast<const f32x4_t*>(mine + (4 * i + fq) * kPitch + 4 * fr),
+                                    reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v - fr + 4 * i + fq) * d + col));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
