@@ -546,10 +546,11 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
 // the logits of f32_split.h and as exact.  A wave holds the parts of G's 64 columns v, all rows deep, in registers, and
 // goes along X's columns, 16 at a time, whose parts split_columns_kernel laid out in the order of the operands; the next
 // ones are on their way meanwhile.  No barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a quarter
-// of the columns: G is split once more for each share.  Results pass LDS, 64 columns at a time, so that 256 bytes of a row
+// of the columns, so that what runs at a time writes all parts of a row; G is split once more for each share.  Results pass LDS, 64 columns at a time, so that 256 bytes of a row
 // leave together, non-temporal.  90 tokens, d 1536, V 151936 (933 MB of dW): 265 to 284 us on two cards of another pace, 495
 // with the fp32 instructions' tiles; 471 with ordinary 64-byte runs and no loads ahead, 376 with these, 326 non-temporal.
-// 12 and 33 tokens, d 2048, V 128256 (1.05 GB): 265 and 260, 442 and 465 in runs of 64 bytes; 4.0 TB/s of stores.
+// 12 tokens, d 2048, V 128256 (1.05 GB): 229, 4.6 TB/s of stores; 442 in runs of 64 bytes, 265 where the shares of a row are
+// far apart in the grid.
 template <int kSteps>
 __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __restrict__ G,
                                                                const float* __restrict__ X,
@@ -558,7 +559,7 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
                                                                int64_t v0, int Vc, float* __restrict__ dW) {
   const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
   const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
-  const int rows = int(min(int64_t(V) - v0, int64_t(Vc))), v = 256 * blockIdx.x + 64 * int(threadIdx.x >> 6) + fr;
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc))), v = 256 * blockIdx.y + 64 * int(threadIdx.x >> 6) + fr;
   if (v - fr >= rows) return;
   const buf_rsrc_t rg = make_rsrc(G, uint32_t(n) * uint32_t(Vc) * 4u);  // (rows past the live ones read 0)
   bf16x8_t g[4][kSteps][3];
@@ -582,8 +583,8 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
   constexpr int kPitch = 68;
   __shared__ __attribute__((aligned(16))) float lds[4 * 64 * kPitch];
   float* mine = lds + (threadIdx.x >> 6) * (64 * kPitch);
-  const int blocks = (d + 15) / 16, per = ((blocks + 3) / 4 + int(gridDim.y) - 1) / int(gridDim.y) * 4;
-  const int first = per * int(blockIdx.y), last = min(blocks, first + per);
+  const int blocks = (d + 15) / 16, per = ((blocks + 3) / 4 + int(gridDim.x) - 1) / int(gridDim.x) * 4;
+  const int first = per * int(blockIdx.x), last = min(blocks, first + per);
   bf16x8_t x[kSteps][3], ahead[kSteps][3];
   const auto load = [&](int c) {
 #pragma unroll
@@ -637,6 +638,92 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
 }
 
 // ------------------------------------------------------------------ matrix-core products (bf16)
+
+// Of 16 columns of Xc's live rows (at most 128) and 32 rows 1 KB, as the matrix cores take them where the rows are the
+// depth; zeros past the live rows.  One workgroup a block of columns.
+__global__ __launch_bounds__(256) void loss_columns_kernel(const __bf16* __restrict__ Xc, const int* __restrict__ n_live,
+                                                           int d, int steps, __bf16* __restrict__ columns) {
+  const int lane = threadIdx.x & 63, step = threadIdx.x >> 6, n = n_live[1];
+  if (step >= steps) return;
+  bf16x8_t x;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int row = 32 * step + 8 * (lane >> 4) + e;
+    x[e] = row < n ? Xc[size_t(row) * d + 16 * blockIdx.x + (lane & 15)] : __bf16(0.f);
+  }
+  *reinterpret_cast<bf16x8_t*>(columns + (size_t(blockIdx.x) * steps + step) * 512 + 8 * lane) = x;
+}
+
+// dW of up to 64 tokens of a distillation, whose G has two parts: at most 128 rows deep.  A wave holds G's 64 columns v,
+// four a lane, all rows deep, in registers, and goes along X's columns, 16 at a time, from loss_columns_kernel; the next
+// ones are on their way meanwhile.  No barrier.  M side: X's columns, N side: vocabulary rows.  Results pass LDS, 128
+// columns at a time, so that 256 bytes of a row leave together, non-temporal: its stores bound it.  12 tokens, d 2048, V
+// 128256 (525 MB): 105 us, 5.0 TB/s (with the tiles of larger calls 195; 163 where the shares of a row are far apart in the
+// grid, since what is written at a time then lies in one part of each row); 64 tokens, d 4096 238; 16 tokens, d 64, V 1000 4.
+template <int kSteps>
+__global__ __launch_bounds__(256, 2) void loss_dw_few_kernel(const __bf16* __restrict__ G,
+                                                             const __bf16* __restrict__ columns,
+                                                             const int* __restrict__ n_live, int d, int V, int64_t v0,
+                                                             int Vc, __bf16* __restrict__ dW) {
+  constexpr int kPitch = 132;  // (four rows on, eight banks on)
+  __shared__ __attribute__((aligned(16))) __bf16 lds[4 * 64 * kPitch];
+  const int lane = threadIdx.x & 63, fr = lane & 15, fq = lane >> 4;
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]);
+  const int rows = int(min(int64_t(V) - v0, int64_t(Vc))), v = 256 * blockIdx.y + 64 * int(threadIdx.x >> 6);
+  if (v >= rows) return;
+  __bf16* mine = lds + (threadIdx.x >> 6) * (64 * kPitch);
+  const buf_rsrc_t rg = make_rsrc(G, uint32_t(n) * uint32_t(Vc) * 2u);  // (rows past the live ones read 0)
+  bf16x8_t g[4][kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t at = uint32_t(32 * s + 8 * fq + e) * uint32_t(Vc) + uint32_t(v + 4 * fr);
+      const bf16x4_t four = __builtin_bit_cast(bf16x4_t, buf_load2(rg, 2u * at));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) g[j][s][e] = four[j];
+    }
+  const int blocks = d / 16, per = ((blocks + 7) / 8 + int(gridDim.x) - 1) / int(gridDim.x) * 8;  // (d a multiple of 32)
+  const int first = per * int(blockIdx.x), last = min(blocks, first + per);
+  bf16x8_t x[kSteps], ahead[kSteps];
+  const auto load = [&](int c) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+      ahead[s] = *reinterpret_cast<const bf16x8_t*>(columns + (size_t(c) * kSteps + s) * 512 + 8 * lane);
+  };
+  load(min(first, blocks - 1));
+  for (int c = first; c < last; ++c) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) x[s] = ahead[s];
+    load(min(c + 1, blocks - 1));
+    f32x4_t acc[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = mfma_bf16(x[s], g[j][s], acc[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint2*>(mine + (4 * fr + j) * kPitch + 16 * (c & 7) + 4 * fq) =
+          uint2{pack_bf16(acc[j][0], acc[j][1]), pack_bf16(acc[j][2], acc[j][3])};
+    if ((c & 7) != 7 && c + 1 < last) continue;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int col = 16 * (c & ~7) + 8 * fr;
+#pragma unroll 4
+    for (int i = 0; i < 16; ++i) {
+      const int row = 4 * i + fq;
+      const uint2* from = reinterpret_cast<const uint2*>(mine + row * kPitch + 8 * fr);
+      const uint2 lo = from[0], hi = from[1];
+      if (v + row < rows && col < 16 * (c + 1))
+        __builtin_nontemporal_store(u32x4_t{lo.x, lo.y, hi.x, hi.y},
+                                    reinterpret_cast<u32x4_t*>(dW + (size_t(v0) + v + row) * d + col));
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
 
 // Running (reference, sum) in base 2 of every token's logits, for calls of few tokens: workgroup (token tile, slice)
 // takes the vocabulary tiles slice, slice + n_slices, ..., so that any number of token tiles fills the chip.  The
@@ -1107,6 +1194,21 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_mfma_kernel");
       }
       if (dW) {
+        if (teacher && p.parts == 2) {
+          const int steps = (2 * n + 31) / 32;
+          __bf16* columns = parts;
+          if (v0 == 0)
+            loss_columns_kernel<<<dim3(unsigned(d / 16)), block, 0, s>>>(Xc, b.n_live, d, steps, columns);
+          auto kernel = steps == 1   ? loss_dw_few_kernel<1>
+                        : steps == 2 ? loss_dw_few_kernel<2>
+                        : steps == 3 ? loss_dw_few_kernel<3>
+                                     : loss_dw_few_kernel<4>;
+          const unsigned along = unsigned(std::max(1, std::min(4, d / 256)));  // of the columns: shares of 256 at least
+          kernel<<<dim3(along, unsigned((p.Vc + 255) / 256)), block, 0, s>>>(G, columns, b.n_live, d, V, v0, p.Vc,
+                                                                             static_cast<T*>(dW));
+          ESTP_CHECK_LAUNCH("loss_dw_few_kernel");
+          continue;
+        }
         auto dw_kernel = stream_dw(n, d, V) ? loss_dw_mfma_kernel<true> : loss_dw_mfma_kernel<false>;
         dw_kernel<<<grid, block, 0, s>>>(G, Xc, b.n_live, d, V, v0, p.Vc, static_cast<T*>(dW));
         ESTP_CHECK_LAUNCH("loss_dw_mfma_kernel");
@@ -1165,7 +1267,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
                         : steps == 2 ? loss_dw_split_kernel<2>
                                      : loss_dw_split_kernel<3>;
           const unsigned along = unsigned(std::max(1, std::min(4, d / 128)));  // of the columns: shares of 128 at least
-          kernel<<<dim3(unsigned((p.Vc + 255) / 256), along), block, 0, s>>>(G, Xc, columns, b.n_live, d, V, v0, p.Vc,
+          kernel<<<dim3(along, unsigned((p.Vc + 255) / 256)), block, 0, s>>>(G, Xc, columns, b.n_live, d, V, v0, p.Vc,
                                                                              static_cast<T*>(dW));
           ESTP_CHECK_LAUNCH("loss_dw_split_kernel");
           continue;
@@ -1189,7 +1291,10 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
 
 size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype, bool teacher) {
   const size_t loss = carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
-  return loss + (teacher && dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) + split::column_bytes(d) : 0);
+  if (!teacher) return loss;
+  // the parts of fp32 tokens, and columns as the operands of dW
+  return loss + (dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) + split::column_bytes(d)
+                                   : size_t(d / 16 + 1) * 4096);
 }
 
 int launch_lm_head_backward(const void* X, const void* W, const int32_t* targets, const float* lse, const float* grad,
