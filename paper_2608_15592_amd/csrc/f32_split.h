@@ -135,7 +135,7 @@ template <int kNB, bool kStream>
 struct Tile {
   static constexpr int kTN = 16 * kNB, kStages = 3;
   static constexpr int kLX = (3 * kNB + kWaves - 1) / kWaves;  // transfers of a wave of the tokens' parts
-  static constexpr int kStageW = kRows * kDepth * 4, kStage = kStageW + 3072 * kNB;
+  static constexpr int kStageW = kRows * kDepth * 4, kStage = kStageW + 3 * 1024 * kNB;
   static constexpr int kLds = kStages * kStage + 1024;  // and what transfers past the last block bring, zeros
   static_assert(kLds <= 163840, "LDS of a compute unit");
   using Acc = f32x4_t[2][kNB];

@@ -425,7 +425,7 @@ __global__ __launch_bounds__(256) void logprob_merge_kernel(const T* __restrict_
                                                             float* __restrict__ logprob, float* __restrict__ lse,
                                                             float* __restrict__ H, int32_t* __restrict__ top_id,
                                                             float* __restrict__ top_logprob) {
-  constexpr int kCap = kQuads ? 3072 : 2048;
+  constexpr int kCap = kQuads ? 12 * 256 : 2048;
   __shared__ TopK<kCap> pick;
   __shared__ uint64_t best[kMaxTop];
   __shared__ float wave_z[4];

@@ -420,7 +420,7 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
                                                                const int* __restrict__ n_live, int d, int V, int64_t v0,
                                                                int Vc, int n_cols, int n_tiles, int n_slices, int wgs,
                                                                size_t room, bool first, float* __restrict__ sums) {
-  __shared__ __attribute__((aligned(16))) char lds[2 * 3072 * kNB];
+  __shared__ __attribute__((aligned(16))) char lds[2 * 3 * 1024 * kNB];
   const gemm::SliceAt wg = gemm::slice_of(gemm::first_tile(blockIdx.x, gridDim.x), n_tiles, n_slices);
   const int all = __builtin_amdgcn_readfirstlane(n_live[1]), n0 = wg.tile / n_cols * 16 * kNB, n = min(16 * kNB, all - n0);
   if (wg.slice >= n_slices || n <= 0) return;
@@ -467,7 +467,7 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
       for (int j = 0; j < 8; ++j) f.piece(r, j);
 #pragma unroll
       for (int p = 0; p < 3; ++p)
-        *reinterpret_cast<bf16x8_t*>(lds + (t & 1) * 3072 * kNB + (3 * wave + p) * 1024 + 16 * lane) = f.part(p);
+        *reinterpret_cast<bf16x8_t*>(lds + (t & 1) * (3 * 1024 * kNB) + (3 * wave + p) * 1024 + 16 * lane) = f.part(p);
     };
     f32x4_t acc[2][kNB], low[2][kNB];
 #pragma unroll
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
       load_w(t + 2, free);
       keep_g(t + 1);
       load_g(t + 2);
-      const char* from = lds + (t & 1) * 3072 * kNB + 16 * lane;
+      const char* from = lds + (t & 1) * (3 * 1024 * kNB) + 16 * lane;
       bf16x8_t x[2][3];
       auto read = [&](int b) {
 #pragma unroll
