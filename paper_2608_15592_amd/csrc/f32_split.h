@@ -100,13 +100,14 @@ static __device__ __attribute__((noinline)) float plain(const float* __restrict_
   return z;
 }
 
-// The same of up to 96 rows as the matrix cores take them where the rows are the depth: of 16 columns, a part and 32 rows
-// 1 KB, lane (column lane % 16) the rows 8 (lane / 16) .. + 7; zeros past the live rows.  One workgroup a block of columns.
-constexpr int kDeepRows = 96;
+// The same as the matrix cores take them where the rows are the depth: of 16 columns, a part and 32 rows (of `steps`) 1 KB,
+// lane (column lane % 16) the rows 8 (lane / 16) .. + 7; zeros past the live rows.  A wave for 16 columns and 32 rows.
+constexpr int kDeepRows = 96;  // that a wave holds in registers (loss_dw_split_kernel)
 static __global__ __launch_bounds__(192) void split_columns_kernel(const float* __restrict__ X,
                                                                    const int* __restrict__ n_live, int d, int steps,
                                                                    __bf16* __restrict__ parts) {
-  const int lane = threadIdx.x & 63, step = threadIdx.x >> 6, col = 16 * blockIdx.x + (lane & 15), n = *n_live;
+  const int lane = threadIdx.x & 63, step = 3 * blockIdx.y + (threadIdx.x >> 6);
+  const int col = 16 * blockIdx.x + (lane & 15), n = *n_live;
   if (step >= steps) return;
   uint32_t q[3][4];
 #pragma unroll
@@ -127,7 +128,7 @@ static __global__ __launch_bounds__(192) void split_columns_kernel(const float* 
 
 // Bytes of the parts of n rows.
 inline size_t parts_bytes(size_t n, int d) { return 3 * n * size_t(padded(d)) * 2; }
-inline size_t column_bytes(int d) { return size_t((d + 15) / 16) * 3 * (kDeepRows / 32) * 1024; }
+inline size_t column_bytes(size_t n, int d) { return size_t((d + 15) / 16) * 3 * ((n + 31) / 32) * 1024; }
 
 // 256 vocabulary rows x 16 kNB tokens by 8 waves, tile after tile.  Three stages of 32 k in LDS: two are on their way, 64 KB
 // of W, while one is multiplied, across tile boundaries too.  kStream: each row of W is read once in the call.

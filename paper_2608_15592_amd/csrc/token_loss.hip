@@ -637,6 +637,114 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
   }
 }
 
+// The same of any number of rows.  Workgroup (256 vocabulary rows, 16 kNB columns of X); a wave takes 32 vocabulary rows and
+// all of those columns, 32 tokens a step.  As loss_dx_split_kernel, with G, whose columns are split on the way, in the place
+// of W, and X's parts as split_columns_kernel laid them out, through LDS, in the place of G's.  The column tiles of 256
+// vocabulary rows run next to each other on one XCD, whose L2 G's columns so leave memory for once.  M side: X's columns, N
+// side: vocabulary rows.
+template <int kNB>
+__global__ __launch_bounds__(512, 2) void loss_dw_split_many_kernel(const float* __restrict__ G,
+                                                                    const float* __restrict__ X,
+                                                                    const __bf16* __restrict__ columns, int all_steps,
+                                                                    const int* __restrict__ n_live, int d, int V,
+                                                                    int64_t v0, int Vc, int n_cols,
+                                                                    float* __restrict__ dW) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * 3 * 1024 * kNB];
+  const int id = gemm::first_tile(blockIdx.x, gridDim.x), rows = int(min(int64_t(V) - v0, int64_t(Vc)));
+  const int m0 = 256 * (id / n_cols), first = kNB * (id % n_cols);  // block of 16 columns
+  if (m0 >= rows) return;
+  const int n = __builtin_amdgcn_readfirstlane(n_live[1]), steps = (n + 63) / 64 * 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
+  const int v = m0 + 32 * wave + 2 * fr;
+  uint32_t off[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) off[e] = (uint32_t(8 * fq + e) * uint32_t(Vc) + uint32_t(v)) * 4u;
+  auto load_g = [&](int t, split::Raw (&raw)[2]) {
+    const int left = max(0, min(32, n - 32 * t));
+    const buf_rsrc_t r = make_rsrc(G + size_t(left > 0 ? 32 * t : 0) * Vc, uint32_t(left) * uint32_t(Vc) * 4u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const f32x2_t g = buf_load2(r, off[e]);
+      raw[0].v[e] = g[0];
+      raw[1].v[e] = g[1];
+    }
+  };
+  bf16x8_t x[3];
+  const bool brings = wave < kNB && 16 * (first + wave) < d;
+  auto load_x = [&](int t) {
+    if (!brings || t >= all_steps) return;
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+      x[p] = *reinterpret_cast<const bf16x8_t*>(columns + ((size_t(first + wave) * 3 + p) * all_steps + t) * 512 + 8 * lane);
+  };
+  auto keep_x = [&](int t) {
+    if (wave >= kNB || t >= steps) return;
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+      *reinterpret_cast<uint4*>(lds + (t & 1) * (3 * 1024 * kNB) + (3 * wave + p) * 1024 + 16 * lane) =
+          brings && t < all_steps ? __builtin_bit_cast(uint4, x[p]) : uint4{0, 0, 0, 0};
+  };
+  f32x4_t acc[2][kNB], low[2][kNB];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) acc[i][b] = low[i][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  split::Raw even[2], odd[2];
+  split::Frag here[2], next[2];
+  load_x(0);
+  load_g(0, even);
+  load_g(1, odd);
+  keep_x(0);
+  load_x(1);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) here[i].piece(even[i], j);
+  lds_barrier();
+  auto step = [&](int t, const split::Frag (&g)[2], split::Frag (&then)[2], split::Raw (&later)[2],
+                  split::Raw (&free)[2]) {
+    load_g(t + 2, free);
+    keep_x(t + 1);
+    load_x(t + 2);
+    const char* from = lds + (t & 1) * (3 * 1024 * kNB) + 16 * lane;
+    bf16x8_t xs[2][3];
+    auto read = [&](int b) {
+#pragma unroll
+      for (int p = 0; p < 3; ++p) xs[b & 1][p] = *reinterpret_cast<const bf16x8_t*>(from + (3 * b + p) * 1024);
+    };
+    read(0);
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kEvery = 12 * kNB / 16;
+#pragma unroll
+    for (int m = 0; m < 12 * kNB; ++m) {
+      constexpr int kG[6] = {2, 0, 1, 0, 1, 0}, kX[6] = {0, 2, 1, 1, 0, 0};
+      const int b = m / 12, s = m % 12 / 2, i = m % 2;
+      if (m % 12 == 0 && b + 1 < kNB) read(b + 1);
+      f32x4_t& sum = s == 5 ? acc[i][b] : low[i][b];
+      sum = mfma_bf16(xs[b & 1][kX[s]], g[i].part(kG[s]), sum);
+      if (m % kEvery == 0 && m / kEvery < 16) then[m / kEvery / 8].piece(later[m / kEvery / 8], m / kEvery % 8);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    lds_barrier();
+  };
+  for (int t = 0; t < steps; t += 2) {
+    step(t, here, next, odd, even);
+    step(t + 1, next, here, even, odd);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      const int k = 16 * (first + b) + 4 * fq;
+      if (v + i >= rows || k >= d) continue;  // (d is a multiple of 8)
+      f32x4_t out = acc[i][b] + low[i][b];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!(fabsf(out[r]) < INFINITY)) out[r] = plain_sum(G + v + i, Vc, X + k + r, d, n);
+      *reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + i) * d + k) = out;
+    }
+}
+
 // ------------------------------------------------------------------ matrix-core products (bf16)
 
 // Of 16 columns of Xc's live rows (at most 128) and 32 rows 1 KB, as the matrix cores take them where the rows are the
@@ -1257,12 +1365,22 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         ESTP_CHECK_LAUNCH("loss_dx_f32_kernel");
       }
       if (dW) {
-        if (by_parts && n <= split::kDeepRows) {
+        if (by_parts) {
           const int steps = (n + 31) / 32;
           __bf16* columns = parts + split::parts_bytes(size_t(n), d) / 2;
           if (v0 == 0)
-            split::split_columns_kernel<<<dim3(unsigned((d + 15) / 16)), dim3(192), 0, s>>>(Xc, b.n_live, d, steps,
-                                                                                           columns);
+            split::split_columns_kernel<<<dim3(unsigned((d + 15) / 16), unsigned((steps + 2) / 3)), dim3(192), 0, s>>>(
+                Xc, b.n_live, d, steps, columns);
+          if (n > split::kDeepRows) {
+            const int nb = split::deep_blocks(d), n_cols = (d + 16 * nb - 1) / (16 * nb);
+            auto kernel = nb == 2   ? loss_dw_split_many_kernel<2>
+                          : nb == 4 ? loss_dw_split_many_kernel<4>
+                                    : loss_dw_split_many_kernel<6>;
+            kernel<<<dim3(unsigned((int64_t((p.Vc + 255) / 256) * n_cols + 7) / 8 * 8)), dim3(512), 0, s>>>(
+                G, Xc, columns, steps, b.n_live, d, V, v0, p.Vc, n_cols, static_cast<T*>(dW));
+            ESTP_CHECK_LAUNCH("loss_dw_split_many_kernel");
+            continue;
+          }
           auto kernel = steps == 1   ? loss_dw_split_kernel<1>
                         : steps == 2 ? loss_dw_split_kernel<2>
                                      : loss_dw_split_kernel<3>;
@@ -1293,7 +1411,7 @@ size_t lm_head_backward_bytes(int64_t n_tok, int d, int V, int dtype, bool teach
   const size_t loss = carve_loss(loss_room(n_tok, d, V, dtype), n_tok, d, dtype, nullptr).bytes;
   if (!teacher) return loss;
   // the parts of fp32 tokens, and columns as the operands of dW
-  return loss + (dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) + split::column_bytes(d)
+  return loss + (dtype == ESTP_F32 ? split::parts_bytes(size_t(n_tok), d) + split::column_bytes(size_t(n_tok), d)
                                    : size_t(d / 16 + 1) * 4096);
 }
 
