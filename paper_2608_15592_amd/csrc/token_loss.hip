@@ -637,13 +637,15 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
   }
 }
 
-// The same of any number of rows.  Workgroup (256 vocabulary rows, 16 kNB columns of X); a wave takes 32 vocabulary rows and
+// The same of any number of rows.  Workgroup (128 vocabulary rows, 16 kNB columns of X); a wave takes 32 vocabulary rows and
 // all of those columns, 32 tokens a step.  As loss_dx_split_kernel, with G, whose columns are split on the way, in the place
-// of W, and X's parts as split_columns_kernel laid them out, through LDS, in the place of G's.  The column tiles of 256
-// vocabulary rows run next to each other on one XCD, whose L2 G's columns so leave memory for once.  M side: X's columns, N
-// side: vocabulary rows.
+// of W, and X's parts as split_columns_kernel laid them out, through LDS, in the place of G's.  The column tiles of 128
+// vocabulary rows run next to each other on one XCD, into whose L2 G's columns so come once.  M side: X's columns, N side:
+// vocabulary rows.  Two workgroups share a compute unit, so that one's first loads and stores lie beside the other's
+// products: with one of 8 waves 657, 974, 1603 and 788 us where it takes 574 (128 tokens, d 2048, V 128256), 848 (200), 1384
+// (400, 0.9 PFLOP/s of the parts) and 741 (1000, d 1024, V 65536); 711, 1082, 1981 and 1144 by the fp32 instructions.
 template <int kNB>
-__global__ __launch_bounds__(512, 2) void loss_dw_split_many_kernel(const float* __restrict__ G,
+__global__ __launch_bounds__(256, 2) void loss_dw_split_many_kernel(const float* __restrict__ G,
                                                                     const float* __restrict__ X,
                                                                     const __bf16* __restrict__ columns, int all_steps,
                                                                     const int* __restrict__ n_live, int d, int V,
@@ -651,7 +653,7 @@ __global__ __launch_bounds__(512, 2) void loss_dw_split_many_kernel(const float*
                                                                     float* __restrict__ dW) {
   __shared__ __attribute__((aligned(16))) char lds[2 * 3 * 1024 * kNB];
   const int id = gemm::first_tile(blockIdx.x, gridDim.x), rows = int(min(int64_t(V) - v0, int64_t(Vc)));
-  const int m0 = 256 * (id / n_cols), first = kNB * (id % n_cols);  // block of 16 columns
+  const int m0 = 128 * (id / n_cols), first = kNB * (id % n_cols);  // block of 16 columns
   if (m0 >= rows) return;
   const int n = __builtin_amdgcn_readfirstlane(n_live[1]), steps = (n + 63) / 64 * 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), fr = lane & 15, fq = lane >> 4;
@@ -669,20 +671,22 @@ __global__ __launch_bounds__(512, 2) void loss_dw_split_many_kernel(const float*
       raw[1].v[e] = g[1];
     }
   };
-  bf16x8_t x[3];
-  const bool brings = wave < kNB && 16 * (first + wave) < d;
+  constexpr int kBring = (3 * kNB + 3) / 4;  // pieces of 1 KB of a step that a wave brings
+  bf16x8_t x[kBring];
+  const int pieces = 3 * min(kNB, (d + 15) / 16 - first);
   auto load_x = [&](int t) {
-    if (!brings || t >= all_steps) return;
 #pragma unroll
-    for (int p = 0; p < 3; ++p)
-      x[p] = *reinterpret_cast<const bf16x8_t*>(columns + ((size_t(first + wave) * 3 + p) * all_steps + t) * 512 + 8 * lane);
+    for (int u = 0; u < kBring; ++u)
+      if (wave + 4 * u < pieces && t < all_steps)
+        x[u] = *reinterpret_cast<const bf16x8_t*>(columns + ((size_t(first) * 3 + wave + 4 * u) * all_steps + t) * 512 +
+                                                  8 * lane);
   };
   auto keep_x = [&](int t) {
-    if (wave >= kNB || t >= steps) return;
 #pragma unroll
-    for (int p = 0; p < 3; ++p)
-      *reinterpret_cast<uint4*>(lds + (t & 1) * (3 * 1024 * kNB) + (3 * wave + p) * 1024 + 16 * lane) =
-          brings && t < all_steps ? __builtin_bit_cast(uint4, x[p]) : uint4{0, 0, 0, 0};
+    for (int u = 0; u < kBring; ++u)
+      if (wave + 4 * u < 3 * kNB && t < steps)
+        *reinterpret_cast<uint4*>(lds + (t & 1) * (3 * 1024 * kNB) + (wave + 4 * u) * 1024 + 16 * lane) =
+            wave + 4 * u < pieces && t < all_steps ? __builtin_bit_cast(uint4, x[u]) : uint4{0, 0, 0, 0};
   };
   f32x4_t acc[2][kNB], low[2][kNB];
 #pragma unroll
@@ -1376,7 +1380,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
             auto kernel = nb == 2   ? loss_dw_split_many_kernel<2>
                           : nb == 4 ? loss_dw_split_many_kernel<4>
                                     : loss_dw_split_many_kernel<6>;
-            kernel<<<dim3(unsigned((int64_t((p.Vc + 255) / 256) * n_cols + 7) / 8 * 8)), dim3(512), 0, s>>>(
+            kernel<<<dim3(unsigned((int64_t(p.Vc / 128) * n_cols + 7) / 8 * 8)), block, 0, s>>>(
                 G, Xc, columns, steps, b.n_live, d, V, v0, p.Vc, n_cols, static_cast<T*>(dW));
             ESTP_CHECK_LAUNCH("loss_dw_split_many_kernel");
             continue;
