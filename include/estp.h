@@ -444,7 +444,8 @@ ESTP_API int estp_token_logprobs(const void* X, const void* W, const int32_t* ta
  *   grad [n_tok]     float32, or NULL (all 1)
  *   dX, dW           as estp_token_loss_backward's, rows of ignored tokens of dX 0
  * Rows of X, lse, logq and grad of ignored tokens are not used (they may hold anything).  G, its
- * roundings, the sums, the sizes that are refused and the workspace are estp_token_loss_backward's.
+ * roundings, the sums, the sizes that are refused and the workspace are estp_token_loss_backward's
+ * (of fp32 12 bytes more for each number of X).  fp32 products of larger calls as the logits'.
  * Bitwise repeatable.
  * ------------------------------------------------------------------------ */
 ESTP_API size_t estp_distill_loss_workspace_size(int64_t n_tok, int32_t d, int32_t V, int dtype);

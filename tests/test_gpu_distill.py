@@ -410,3 +410,21 @@ def test_two_graphs_on_the_same_workspaces(dtype, n, other, d, V):
         step(*calls[1][0], ws=wss)
         for (_, out), want in zip(calls, wants):
             assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
+
+
+@pytest.mark.parametrize("dtype,n,d,V", [("bf16", 7, 96, 4001), ("bf16", 64, 1056, 1003), ("f32", 30, 72, 50001),
+                                         ("f32", 96, 136, 49153), ("f32", 130, 104, 33001), ("f32", 9, 40, 515)])
+def test_outputs_end_where_their_arrays_end(dtype, n, d, V):
+    case = _case(n + V, n, d, V, 7, dtype)
+    X, W, ids, logp, g = map(dev, case)
+    of = {"bf16": (torch.bfloat16, 2), "f32": (torch.float32, 4)}[dtype]
+    guards = [Guarded(b) for b in (4 * n, 4 * n, 28 * n, of[1] * n * d, of[1] * V * d)]
+    loss, lse, logq = (a.ws.view(torch.float32) for a in guards[:3])
+    dX, dW = (a.ws.view(of[0]).view(-1, d) for a in guards[3:])
+    estp.distill_loss(X, W, ids, logp, loss=loss, lse=lse, logq=logq.view(n, 7))
+    estp.distill_loss_backward(X, W, ids, logp, lse, logq.view(n, 7), g, dX=dX, dW=dW)
+    for a in guards:
+        a.check()
+    ref = HD.distill(*case[:4], 1.0, True, case[4], dtype)
+    for name, a in (("loss", loss), ("lse", lse), ("logq", logq.view(n, 7)), ("dX", dX), ("dW", dW)):
+        assert (np.abs(_wide(a) - ref[name]) <= ref[name + "_bound"]).all(), name

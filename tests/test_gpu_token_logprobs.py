@@ -389,3 +389,17 @@ def test_two_graphs_on_one_workspace(dtype, n, other, d, V):
         estp.token_logprobs(calls[0][0], W, None, k, workspace=ws)
         for (_, _, out), want in zip(calls, wants):
             assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
+
+
+@pytest.mark.parametrize("dtype,n,d,V,k", [("bf16", 3, 1024, 4001, 5), ("bf16", 390, 32, 33001, 17), ("bf16", 100, 64, 999, 128),
+                                           ("f32", 33, 72, 50001, 3), ("f32", 5, 40, 515, 20)])
+def test_outputs_end_where_their_arrays_end(dtype, n, d, V, k):
+    X, W, t, _ = _inputs(n + V, n, d, V, dtype, ignored=0.2)
+    X, W, t = dev(X), dev(W), dev(t)
+    guards = [Guarded(4 * n * m) for m in (1, 1, 1, k, k)]
+    out = [a.ws.view(torch.int32 if i == 3 else torch.float32) for i, a in enumerate(guards)]
+    out[3:] = [a.view(n, k) for a in out[3:]]
+    estp.token_logprobs(X, W, t, k, **dict(zip(("logprob", "lse", "H", "top_id", "top_logprob"), out)))
+    for a in guards:
+        a.check()
+    assert all(torch.equal(a, b) for a, b in zip(out, estp.token_logprobs(X, W, t, k)))
