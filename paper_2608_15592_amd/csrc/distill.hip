@@ -114,7 +114,7 @@ __global__ __launch_bounds__(64 * few::kWaves, 2) void distill_lse_few_kernel(co
 // of its parts' products, whose splitting the vector units do meanwhile; 504 with the fp32 instructions.
 template <int kNB, bool kStream>
 __global__ __launch_bounds__(64 * split::kWaves, 2) void distill_lse_split_kernel(
-    const float* __restrict__ X, const __bf16* __restrict__ parts, const float* __restrict__ W, int n, int d, int V,
+    const __bf16* __restrict__ parts, const float* __restrict__ W, int n, int d, int V,
     float c2, int n_tt, int n_slices, float* __restrict__ part_m, float* __restrict__ part_s) {
   using Run = split::Tile<kNB, kStream>;
   __shared__ __attribute__((aligned(16))) char lds[Run::kLds];
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * split::kWaves, 2) void distill_lse_split_kerne
     s[b] = 0.f;
   }
   Run::run(
-      lds, W, V, X, parts, n, n, d, (n_vt - wg.slice + n_slices - 1) / n_slices,
+      lds, W, V, parts, n, n, d, (n_vt - wg.slice + n_slices - 1) / n_slices,
       [&](int i) { return typename Run::Place{(wg.slice + i * n_slices) * split::kRows, n0}; },
       [&](const typename Run::Place& at, const typename Run::Acc& acc) {
         const int lim = V - (at.m0 + 32 * wave + 4 * (lane >> 4));  // live rows: 16 i + r < lim
@@ -393,7 +393,7 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
     split::choose(n, [&](auto nb, auto stream) {
       distill_lse_split_kernel<decltype(nb)::value, decltype(stream)::value>
           <<<dim3(unsigned((r.tiles * r.slices + 7) / 8 * 8)), dim3(64 * split::kWaves), 0, s>>>(
-              x, parts, w, n, d, V, base2_of_logit(temperature), r.tiles, r.slices, p.m, p.s);
+              parts, w, n, d, V, base2_of_logit(temperature), r.tiles, r.slices, p.m, p.s);
     });
     ESTP_CHECK_LAUNCH("distill_lse_split_kernel");
   } else {

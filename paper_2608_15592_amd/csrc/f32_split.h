@@ -7,8 +7,9 @@
 // logit is as exact as a chain of fp32 FMAs, at a sixth of the bf16 rate, 2.6 times that of v_mfma_f32 instructions.
 //
 // The tokens are few beside the vocabulary: their parts are written once (split_rows_kernel).  W is read as it is, and 16
-// rows of a wave are split, 44 vector instructions, between the products of the 16 before them, 36 of 96 tokens.  A part of
-// an infinite number or of one above the largest of bf16 is NaN: a logit that is not finite is formed again by fp32 FMAs.
+// rows of a wave are split, 44 vector instructions, between the products of the 16 before them, 36 of 96 tokens.  The second
+// part of an infinite number is NaN, the first is the number itself (as of those within 2^-8 of the largest): where the sum
+// of x1 w1 is not finite, it is the result, infinite or NaN as products and sums of infinite numbers are.
 #pragma once
 
 #include <type_traits>
@@ -72,6 +73,12 @@ struct Frag {
   }
 };
 
+// A sum of products: that of x1 w1 and that of the others.
+__device__ __forceinline__ float joined(float sum, float low) { return fabsf(sum) < INFINITY ? sum + low : sum; }
+__device__ __forceinline__ f32x4_t joined(const f32x4_t& sum, const f32x4_t& low) {
+  return f32x4_t{joined(sum[0], low[0]), joined(sum[1], low[1]), joined(sum[2], low[2]), joined(sum[3], low[3])};
+}
+
 // parts[p][row][padded(d)] of X's rows, below n (or *n_live).  Four numbers a thread.
 static __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ X, int n,
                                                                 const int* __restrict__ n_live, int d,
@@ -87,17 +94,6 @@ static __global__ __launch_bounds__(256) void split_rows_kernel(const float* __r
     for (int p = 0; p < 3; ++p)
       *reinterpret_cast<uint2*>(parts + (size_t(p) * n + row) * dp + k) = uint2{at[p][0], at[p][1]};
   }
-}
-
-// A logit by fp32 FMAs.  It ends where it has become NaN, which it then stays.
-static __device__ __attribute__((noinline)) float plain(const float* __restrict__ w, const float* __restrict__ x, int d) {
-  float z = 0.f;
-  for (int k = 0; k < d && z == z; k += 4) {
-    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(w + k), b = *reinterpret_cast<const f32x4_t*>(x + k);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) z = fmaf(a[e], b[e], z);
-  }
-  return z;
 }
 
 // The same as the matrix cores take them where the rows are the depth: of 16 columns, a part and 32 rows (of `steps`) 1 KB,
@@ -149,8 +145,8 @@ struct Tile {
   // parts as split_rows_kernel's of X's n rows, of which `live` are given.
   template <typename At, typename Done>
   __device__ static __forceinline__ void run(char* lds, const float* __restrict__ W, int rows,
-                                             const float* __restrict__ X, const __bf16* __restrict__ parts, int n,
-                                             int live, int d, int count, At&& at, Done&& done) {
+                                             const __bf16* __restrict__ parts, int n, int live, int d, int count,
+                                             At&& at, Done&& done) {
     if (count <= 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int fr = lane & 15, fq = lane >> 4, dp = padded(d);
@@ -275,16 +271,7 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) {
-          acc[i][b] += low[i][b];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float z = acc[i][b][r];
-            const int row = p.m0 + 32 * wave + 16 * i + 4 * fq + r, tok = p.n0 + 16 * b + fr;
-            if (!(fabsf(z) < INFINITY) && row < rows && tok < live)
-              acc[i][b][r] = plain(W + size_t(row) * d, X + size_t(tok) * d, d);
-          }
-        }
+        for (int b = 0; b < kNB; ++b) acc[i][b] = joined(acc[i][b], low[i][b]);
       done(p, acc);
     }
     wait_vm<0>();  // no transfer into LDS outlives the workgroup

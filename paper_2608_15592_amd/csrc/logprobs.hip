@@ -117,8 +117,7 @@ __global__ __launch_bounds__(256, 2) void logits_f32_kernel(const float* __restr
 // The same of vocabulary rows v0 .. v0 + Vc by the bf16 matrix cores.  37 tokens, d 2048, V 128256: 237 us, 4.4 TB/s of W
 // (323 by the fp32 instructions); 48 columns' products, 121 GF in bf16, and the splitting of W take about as long as W.
 template <int kNB, bool kStream>
-__global__ __launch_bounds__(64 * split::kWaves, 2) void logits_split_kernel(const float* __restrict__ X,
-                                                                             const __bf16* __restrict__ parts,
+__global__ __launch_bounds__(64 * split::kWaves, 2) void logits_split_kernel(const __bf16* __restrict__ parts,
                                                                              const float* __restrict__ W, int n, int d,
                                                                              int V, int64_t v0, int Vc,
                                                                              float* __restrict__ Z) {
@@ -129,7 +128,7 @@ __global__ __launch_bounds__(64 * split::kWaves, 2) void logits_split_kernel(con
   // (the token tiles of a vocabulary tile next to each other on one XCD)
   const int first = gemm::first_tile(blockIdx.x, gridDim.x), total = n_vt * n_tt;
   Run::run(
-      lds, W + size_t(v0) * d, rows, X, parts, n, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
+      lds, W + size_t(v0) * d, rows, parts, n, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
       [&](int i) {
         const int id = first + i * int(gridDim.x);
         return typename Run::Place{id / n_tt * split::kRows, id % n_tt * Run::kTN};
@@ -608,7 +607,7 @@ int launch_pieces(const T* X, const T* W, const int32_t* targets, int n, int d, 
           split::split_rows_kernel<<<dim3(unsigned(n)), block, 0, s>>>(X, n, nullptr, d, b.parts);
         split::choose(n, [&](auto nb, auto stream) {
           logits_split_kernel<decltype(nb)::value, decltype(stream)::value>
-              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(X, b.parts, W, n, d, V, v0, p.Vc, b.Z);
+              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(b.parts, W, n, d, V, v0, p.Vc, b.Z);
         });
       } else {
         const int tile = n <= 32 ? 32 : n <= 64 ? 64 : kFT;

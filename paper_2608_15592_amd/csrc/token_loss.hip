@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256, 2) void loss_grad_f32_kernel(const float* __re
 // 1536, V 151936: 305 us; by the fp32 instructions 506.
 template <int kNB, bool kStream>
 __global__ __launch_bounds__(64 * split::kWaves, 2) void loss_grad_split_kernel(
-    const float* __restrict__ Xc, const __bf16* __restrict__ parts, int n_max, const float* __restrict__ W,
+    const __bf16* __restrict__ parts, int n_max, const float* __restrict__ W,
     const int* __restrict__ n_live, int d, int V, int64_t v0, int Vc, const float* __restrict__ lc,
     const float* __restrict__ gc, float inv_t, float* __restrict__ G) {
   using Run = split::Tile<kNB, kStream>;
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(64 * split::kWaves, 2) void loss_grad_split_kernel(
   // (the token tiles of a vocabulary tile next to each other on one XCD)
   const int first = gemm::first_tile(blockIdx.x, gridDim.x), total = n_vt * n_tt;
   Run::run(
-      lds, W + size_t(v0) * d, rows, Xc, parts, n_max, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
+      lds, W + size_t(v0) * d, rows, parts, n_max, n, d, first < total ? (total - first - 1) / int(gridDim.x) + 1 : 0,
       [&](int i) {
         const int id = first + i * int(gridDim.x);
         return typename Run::Place{id / n_tt * split::kRows, id % n_tt * Run::kTN};
@@ -397,15 +397,6 @@ __global__ __launch_bounds__(256, 2) void loss_dw_f32_kernel(const float* __rest
         *reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v) * d + k) =
             f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
       }
-}
-
-// The sum of n products, numbers `ld_a` and `ld_b` apart, by fp32 FMAs.  It ends where it has become NaN, which it then
-// stays.
-static __device__ __attribute__((noinline)) float plain_sum(const float* __restrict__ a, size_t ld_a,
-                                                            const float* __restrict__ b, size_t ld_b, int n) {
-  float z = 0.f;
-  for (int i = 0; i < n && z == z; ++i) z = fmaf(a[i * ld_a], b[i * ld_b], z);
-  return z;
 }
 
 // loss_dx_f32_kernel's sums of a distillation by the bf16 matrix cores, numbers in three parts each.  Workgroup (256
@@ -529,10 +520,7 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const int r = 2 * h + q / 2, i = q % 2;
-          v[q] = acc[i][b][r] + low[i][b][r];
-          if (!(fabsf(v[q]) < INFINITY))
-            v[q] = plain_sum(G + size_t(s) * Vc + depth.k0, 1, W + size_t(v0 + depth.k0) * d + c + 4 * h + q, d,
-                             depth.k1 - depth.k0);
+          v[q] = split::joined(acc[i][b][r], low[i][b][r]);
         }
         f32x4_t* o = reinterpret_cast<f32x4_t*>(out + size_t(s) * d + c + 4 * h);
         if (!first) v += *o;
@@ -553,7 +541,6 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
 // far apart in the grid.
 template <int kSteps>
 __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __restrict__ G,
-                                                               const float* __restrict__ X,
                                                                const __bf16* __restrict__ columns,
                                                                const int* __restrict__ n_live, int d, int V,
                                                                int64_t v0, int Vc, float* __restrict__ dW) {
@@ -613,16 +600,9 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
           f32x4_t& sum = t == 5 ? acc[j] : low[j];
           sum = mfma_bf16(x[s][kX[t]], g[j][s][kG[t]], sum);
         }
-    const int k = 16 * c + 4 * fq;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (v + 16 * j < rows && k < d) {  // (d is a multiple of 8)
-        f32x4_t out = acc[j] + low[j];
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (!(fabsf(out[r]) < INFINITY)) out[r] = plain_sum(G + v + 16 * j, Vc, X + k + r, d, n);
-        *reinterpret_cast<f32x4_t*>(mine + (16 * j + fr) * kPitch + 16 * (c & 3) + 4 * fq) = out;
-      }
+      *reinterpret_cast<f32x4_t*>(mine + (16 * j + fr) * kPitch + 16 * (c & 3) + 4 * fq) = split::joined(acc[j], low[j]);
     if ((c & 3) != 3 && c + 1 < last) continue;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -646,7 +626,6 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __re
 // (400, 0.9 PFLOP/s of the parts) and 741 (1000, d 1024, V 65536); 711, 1082, 1981 and 1144 by the fp32 instructions.
 template <int kNB>
 __global__ __launch_bounds__(256, 2) void loss_dw_split_many_kernel(const float* __restrict__ G,
-                                                                    const float* __restrict__ X,
                                                                     const __bf16* __restrict__ columns, int all_steps,
                                                                     const int* __restrict__ n_live, int d, int V,
                                                                     int64_t v0, int Vc, int n_cols,
@@ -741,11 +720,7 @@ __global__ __launch_bounds__(256, 2) void loss_dw_split_many_kernel(const float*
     for (int b = 0; b < kNB; ++b) {
       const int k = 16 * (first + b) + 4 * fq;
       if (v + i >= rows || k >= d) continue;  // (d is a multiple of 8)
-      f32x4_t out = acc[i][b] + low[i][b];
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (!(fabsf(out[r]) < INFINITY)) out[r] = plain_sum(G + v + i, Vc, X + k + r, d, n);
-      *reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + i) * d + k) = out;
+      *reinterpret_cast<f32x4_t*>(dW + (size_t(v0) + v + i) * d + k) = split::joined(acc[i][b], low[i][b]);
     }
 }
 
@@ -1332,7 +1307,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
         if (v0 == 0) split::split_rows_kernel<<<dim3(unsigned(n)), block, 0, s>>>(Xc, n, b.n_live, d, parts);
         split::choose(n, [&](auto nb, auto stream) {
           loss_grad_split_kernel<decltype(nb)::value, decltype(stream)::value>
-              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(Xc, parts, n, Wt, b.n_live, d, V, v0, p.Vc, b.lc,
+              <<<dim3(split::kWgs), dim3(64 * split::kWaves), 0, s>>>(parts, n, Wt, b.n_live, d, V, v0, p.Vc, b.lc,
                                                                       b.gc, inv_t, G);
         });
       } else {
@@ -1381,7 +1356,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
                           : nb == 4 ? loss_dw_split_many_kernel<4>
                                     : loss_dw_split_many_kernel<6>;
             kernel<<<dim3(unsigned((int64_t(p.Vc / 128) * n_cols + 7) / 8 * 8)), block, 0, s>>>(
-                G, Xc, columns, steps, b.n_live, d, V, v0, p.Vc, n_cols, static_cast<T*>(dW));
+                G, columns, steps, b.n_live, d, V, v0, p.Vc, n_cols, static_cast<T*>(dW));
             ESTP_CHECK_LAUNCH("loss_dw_split_many_kernel");
             continue;
           }
@@ -1389,7 +1364,7 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
                         : steps == 2 ? loss_dw_split_kernel<2>
                                      : loss_dw_split_kernel<3>;
           const unsigned along = unsigned(std::max(1, std::min(4, d / 128)));  // of the columns: shares of 128 at least
-          kernel<<<dim3(along, unsigned((p.Vc + 255) / 256)), block, 0, s>>>(G, Xc, columns, b.n_live, d, V, v0, p.Vc,
+          kernel<<<dim3(along, unsigned((p.Vc + 255) / 256)), block, 0, s>>>(G, columns, b.n_live, d, V, v0, p.Vc,
                                                                              static_cast<T*>(dW));
           ESTP_CHECK_LAUNCH("loss_dw_split_kernel");
           continue;
