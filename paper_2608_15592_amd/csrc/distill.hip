@@ -302,8 +302,7 @@ namespace {
 struct SplitStates {
   int tiles, slices;
 };
-SplitStates split_states(int64_t n, int d, int V) {
-  (void)d;
+SplitStates split_states(int64_t n, int V) {
   const int tile = 16 * split::blocks_of(n);
   const int64_t n_tt = (n + tile - 1) / tile, n_vt = (int64_t(V) + split::kRows - 1) / split::kRows;
   SplitStates r{int(n_tt), 1};
@@ -383,7 +382,7 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
     ESTP_CHECK_LAUNCH("distill_lse_few_kernel");
   } else if (dtype == ESTP_F32 && split::takes(n, d, V)) {
     const float *x = static_cast<const float*>(X), *w = static_cast<const float*>(W);
-    const SplitStates r = split_states(n, d, V);
+    const SplitStates r = split_states(n, V);
     p.states = split::kWaves * r.slices;
     Carver c(workspace);
     p.m = c.take<float>(size_t(p.states) * size_t(n));

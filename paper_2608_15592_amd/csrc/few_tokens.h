@@ -49,9 +49,9 @@ struct Rows {
   }
 };
 
-// Tiles 0 .. tiles - 1 of W's V rows.  take(row, z): 4 consecutive vocabulary rows' logits (rows past V: 0) of token 16 b + lane % 16, where waves 0 .. kNB - 1
-// take block b = wave; by the same thread for all rows that are equal modulo 16.  It ends with kStores vector-memory
-// operations, always.
+// Tiles 0 .. tiles - 1 of W's V rows.  take(row, z): 4 consecutive vocabulary rows' logits (rows past V: 0) of token 16 b +
+// lane % 16, where waves 0 .. kNB - 1 take block b = wave; by the same thread for all rows that are equal modulo 16.  It ends
+// with kStores vector-memory operations, always.
 template <int kSteps, int kNB, int kStores, typename Take>
 __device__ __forceinline__ void run(const __bf16* __restrict__ X, const __bf16* __restrict__ W, int n, int d, int V,
                                     int tiles, char* lds, Take&& take) {

@@ -327,8 +327,9 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
 // One token's 16 chunks of 8192: 6 us, latency; 48 tokens, 19 chunks: 13.5 (29 MB, from L2 or the last cache); 2048 tokens'
 // samples, 84 MB: 31, 2.7 TB/s, what the barriers of the bound and of the ranking leave.
 template <int kE>
-__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_32, int live, int64_t v0,
-                                                             int step, float c2, int k, int piece_chunks, int chunk0, int states, int chunks,
+__global__ __launch_bounds__(256) void logprob_select_kernel(const float* __restrict__ Z, int of_tok, int of_32,
+                                                             int live, int64_t v0, int step, float c2, int k,
+                                                             int piece_chunks, int chunk0, int states, int chunks,
                                                              float* __restrict__ part, uint64_t* __restrict__ top) {
   __shared__ TopK<kMaxTop * kE> pick;
   __shared__ float wave_m[4], wave_s[4], wave_t[4];
@@ -338,7 +339,8 @@ __global__ __launch_bounds__(256) void logprob_select_kernel(const float* __rest
   const int first = 256 * kE * c + 4 * tid;  // columns first + 1024 u + e, ascending in 4 u + e
   f32x4_t z[kE / 4];
 #pragma unroll
-  for (int u = 0; u < kE / 4; ++u) z[u] = *reinterpret_cast<const f32x4_t*>(row + size_t((first + 1024 * u) >> 5) * of_32 + (first & 31));
+  for (int u = 0; u < kE / 4; ++u)
+    z[u] = *reinterpret_cast<const f32x4_t*>(row + size_t((first + 1024 * u) >> 5) * of_32 + (first & 31));
   float m = -INFINITY;
 #pragma unroll
   for (int u = 0; u < kE / 4; ++u)

@@ -530,15 +530,15 @@ __global__ __launch_bounds__(512, 2) void loss_dx_split_kernel(const float* __re
   }
 }
 
-// dW of up to 96 rows of a distillation by the bf16 matrix cores: G^T X of numbers in three parts each, six products, as
-// the logits of f32_split.h and as exact.  A wave holds the parts of G's 64 columns v, all rows deep, in registers, and
-// goes along X's columns, 16 at a time, whose parts split_columns_kernel laid out in the order of the operands; the next
-// ones are on their way meanwhile.  No barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a quarter
-// of the columns, so that what runs at a time writes all parts of a row; G is split once more for each share.  Results pass LDS, 64 columns at a time, so that 256 bytes of a row
-// leave together, non-temporal.  90 tokens, d 1536, V 151936 (933 MB of dW): 265 to 284 us on two cards of another pace, 495
-// with the fp32 instructions' tiles; 471 with ordinary 64-byte runs and no loads ahead, 376 with these, 326 non-temporal.
-// 12 tokens, d 2048, V 128256 (1.05 GB): 229, 4.6 TB/s of stores; 442 in runs of 64 bytes, 265 where the shares of a row are
-// far apart in the grid.
+// dW of up to 96 rows of a distillation by the bf16 matrix cores: G^T X of numbers in three parts each, six products,
+// as the logits of f32_split.h and as exact.  A wave holds the parts of G's 64 columns v, all rows deep, in registers,
+// and goes along X's columns, 16 at a time, whose parts split_columns_kernel laid out in the order of the operands; the
+// next ones are on their way meanwhile.  No barrier.  M side: X's columns, N side: vocabulary rows.  A wave has up to a
+// quarter of the columns, so that what runs at a time writes all parts of a row; G is split once more for each share.
+// Results pass LDS, 64 columns at a time, so that 256 bytes of a row leave together, non-temporal.  90 tokens, d 1536,
+// V 151936 (933 MB of dW): about 250 us, 495 with the fp32 instructions' tiles; 471 with
+// ordinary 64-byte runs and no loads ahead, 376 with these, 326 non-temporal.  12 tokens, d 2048, V 128256 (1.05 GB):
+// 229, 4.6 TB/s of stores; 442 in runs of 64 bytes, 265 where the shares of a row are far apart in the grid.
 template <int kSteps>
 __global__ __launch_bounds__(256, 2) void loss_dw_split_kernel(const float* __restrict__ G,
                                                                const __bf16* __restrict__ columns,
