@@ -122,6 +122,16 @@ static __global__ __launch_bounds__(192) void split_columns_kernel(const float* 
         uint4{q[p][0], q[p][1], q[p][2], q[p][3]};
 }
 
+// What a stage's transfers may read of `rows` rows, and the offset along them that they add to every lane's.  Of no rows that
+// is 0 too: of a resource shorter than the scalar offset the hardware's range check, offset >= length - scalar offset, is not
+// known to hold.
+struct Window {
+  uint32_t bytes, offset;
+};
+__host__ __device__ __forceinline__ Window window(int rows, uint32_t pitch, uint32_t offset) {
+  return {rows > 0 ? uint32_t(rows) * pitch : 0u, rows > 0 ? offset : 0u};
+}
+
 // Bytes of the parts of n rows.
 inline size_t parts_bytes(size_t n, int d) { return 3 * n * size_t(padded(d)) * 2; }
 inline size_t column_bytes(size_t n, int d) { return size_t((d + 15) / 16) * 3 * ((n + 31) / 32) * 1024; }
@@ -168,19 +178,19 @@ struct Tile {
     auto fetch = [&]() {
       char* to = lds + pf_slot * kStage;
       const bool some = pf < count;
-      const u32x4_t rw = rsrc_words(W + size_t(where.m0) * d,
-                                    some ? uint32_t(min(kRows, rows - where.m0)) * uint32_t(d) * 4u : 0u);
+      const Window w = window(some ? min(kRows, rows - where.m0) : 0, uint32_t(d) * 4u, uint32_t(pf_k) * 4u);
+      const u32x4_t rw = rsrc_words(W + size_t(where.m0) * d, w.bytes);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        dma16<kStream>(rw, pf_k + kc[i] < d ? off_w[i] : kPastEnd, uint32_t(pf_k) * 4u,
-                       to + 1024 * (kWaves * i + wave));
+        dma16<kStream>(rw, pf_k + kc[i] < d ? off_w[i] : kPastEnd, w.offset, to + 1024 * (kWaves * i + wave));
 #pragma unroll
       for (int i = 0; i < kLX; ++i) {
         const int t = kWaves * i + wave, p = t / kNB, b = t % kNB;
         const int left = some && t < 3 * kNB ? min(16, live - where.n0 - 16 * b) : 0;
-        const u32x4_t r = rsrc_words(parts + (size_t(min(p, 2)) * n + (left > 0 ? where.n0 + 16 * b : 0)) * dp,
-                                     left > 0 ? uint32_t(left) * uint32_t(dp) * 2u : 0u);
-        dma16(r, off_x, uint32_t(pf_k) * 2u, t < 3 * kNB ? to + kStageW + 1024 * t : lds + kStages * kStage);
+        const Window x = window(left, uint32_t(dp) * 2u, uint32_t(pf_k) * 2u);
+        const u32x4_t r =
+            rsrc_words(parts + (size_t(min(p, 2)) * n + (left > 0 ? where.n0 + 16 * b : 0)) * dp, x.bytes);
+        dma16(r, off_x, x.offset, t < 3 * kNB ? to + kStageW + 1024 * t : lds + kStages * kStage);
       }
       pf_slot = pf_slot + 1 == kStages ? 0 : pf_slot + 1;
       pf_k += kDepth;
