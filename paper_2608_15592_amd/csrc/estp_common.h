@@ -42,6 +42,16 @@ __device__ __forceinline__ buf_rsrc_t make_rsrc(const void* base, uint32_t bytes
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, int(bytes), 0x00020000);
 }
 
+// What transfers along rows may read of `rows` rows, and the scalar offset that they add to every lane's.  Of no rows that
+// is 0 too: of a resource shorter than the scalar offset the hardware's range check, offset >= length - scalar offset, is
+// not known to hold.
+struct Window {
+  uint32_t bytes, offset;
+};
+__host__ __device__ __forceinline__ Window window(int rows, uint32_t pitch, uint32_t offset) {
+  return {rows > 0 ? uint32_t(rows) * pitch : 0u, rows > 0 ? offset : 0u};
+}
+
 // 16-byte buffer -> LDS transfer (buffer_load_dwordx4 ... lds): lane l reads
 // the 16 bytes at voffset(l) + soffset of the resource; they land in LDS at
 // dst_wave_base + 16 * l.  `soffset` and `dst_wave_base` must be uniform.

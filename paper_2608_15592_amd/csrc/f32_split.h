@@ -122,16 +122,6 @@ static __global__ __launch_bounds__(192) void split_columns_kernel(const float* 
         uint4{q[p][0], q[p][1], q[p][2], q[p][3]};
 }
 
-// What a stage's transfers may read of `rows` rows, and the offset along them that they add to every lane's.  Of no rows that
-// is 0 too: of a resource shorter than the scalar offset the hardware's range check, offset >= length - scalar offset, is not
-// known to hold.
-struct Window {
-  uint32_t bytes, offset;
-};
-__host__ __device__ __forceinline__ Window window(int rows, uint32_t pitch, uint32_t offset) {
-  return {rows > 0 ? uint32_t(rows) * pitch : 0u, rows > 0 ? offset : 0u};
-}
-
 // Bytes of the parts of n rows.
 inline size_t parts_bytes(size_t n, int d) { return 3 * n * size_t(padded(d)) * 2; }
 inline size_t column_bytes(size_t n, int d) { return size_t((d + 15) / 16) * 3 * ((n + 31) / 32) * 1024; }

@@ -1,5 +1,5 @@
-// What the stages of the fp32 products by parts may read, on the host: within the rows that there are, and of none of them
-// with an offset of 0.
+// What transfers along rows may read, on the host, at the sizes of the fp32 products by parts and of the entropy kernels:
+// within the rows that there are, and of none of them with an offset of 0.
 #include <stdio.h>
 
 #include "f32_split.h"
@@ -8,14 +8,14 @@ using namespace estp::detail;
 
 int main() {
   int empty = 0, bad = 0;
-  for (int d : {64, 72, 264, 1536, 4096, 1 << 20}) {
+  for (int d : {32, 64, 72, 264, 1536, 4096, 1 << 20}) {
     const uint32_t dp = uint32_t(split::padded(d));
     for (int rows : {-1000000, -17, -1, 0, 1, 15, 16, 255, 256})
       for (uint32_t k = 0; k < dp; k += split::kDepth)
         for (uint32_t size : {4u, 2u}) {  // W's rows of d numbers, the parts' of dp
           if (size == 2 && rows > 16) continue;
           const uint32_t pitch = size == 4 ? uint32_t(d) * 4u : dp * 2u;
-          const split::Window w = split::window(rows, pitch, k * size);
+          const estp::Window w = estp::window(rows, pitch, k * size);
           const bool ok = rows > 0 ? uint64_t(w.bytes) == uint64_t(rows) * pitch && w.offset == k * size && w.offset < w.bytes
                                    : w.bytes == 0 && w.offset == 0;
           empty += w.bytes == 0;
