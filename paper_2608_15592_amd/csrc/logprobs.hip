@@ -260,7 +260,8 @@ __global__ __launch_bounds__(256, 1) void logprob_main_kernel(const __bf16* __re
                 s += p;
                 t = fmaf(p, dd, t);
               }
-            exact = !(s <= 0x1p64f);  // (a NaN takes the exact path and stays one)
+            // (a logit of -inf makes t NaN, 0 times its exponent, which the exact path clamps; a NaN stays one there)
+            exact = !(s <= 0x1p64f && t == t);
             e.s = exact ? e.s : s;
             e.t = exact ? e.t : t;
           }
