@@ -12,6 +12,16 @@ __device__ __forceinline__ float exp2_arg(float x) { return x < kExp2Floor ? kEx
 
 constexpr int kFoldBlocks = 8;  // 16-row blocks of a lane's tile
 
+// The state relative to its log-sum-exp: m += log2 s, s = 1, t = t / s - log2 s.  (s >= 1 where a logit was seen: the
+// reference never exceeds the largest, in base 2.)
+__device__ __forceinline__ Ent2 rebased(Ent2 e) {
+  if (e.s > 0.f) {
+    const float dl = fast_log2(e.s);
+    e = Ent2{e.m + dl, 1.f, e.t / e.s - dl};
+  }
+  return e;
+}
+
 // Fold of a finished tile into one lane's running state of one token: the lane's 32 logits z(i, r) of
 // vocabulary rows 16 i + r past its first, live where 16 i + r < lim; times c2 they are in base 2.
 //
@@ -82,13 +92,7 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
       }
     e = Ent2{mnew, s, t};
   }
-  // rebase to the running log-sum-exp: m += log2 s, s = 1, t = t / s - log2 s
-  // (s >= 1 here: the reference never exceeds the largest logit seen, in base 2)
-  if (e.s > 0.f) {
-    const float dl = fast_log2(e.s);
-    e = Ent2{e.m + dl, 1.f, e.t / e.s - dl};
-  }
-  return e;
+  return rebased(e);
 }
 
 }  // namespace detail

@@ -427,3 +427,47 @@ def test_tokens_of_no_probability_leave_an_entropy(n, low, k):
     np.testing.assert_array_equal(host(ids), rest[ref["top_id"]])
     assert (np.abs(_wide(top) - ref["top_logprob"]) <= ref["logprob_bound"][:, None]).all()
     assert torch.isfinite(got[2]).all()
+
+
+def test_entropy_of_a_mode_far_above_the_first_tile():
+    # a background of zeros and, 55 to 62 units of ln 2 above it, two tokens that a lane folds together in one of its
+    # later tiles: all else weighs less than 2^-40.  What is left are roundings of the second weight's exponent (at most 6
+    # in base 2: 4 u), of two weights and their sums (2 u each), of a logarithm below 1 and of H and its change of base
+    n, V, first, u = 2048, 33000, 2300, OP.U
+    X, W, i = np.zeros((n, 96)), np.zeros((V, 96)), np.arange(n)
+    place = first + 472 * np.arange(64)  # of 118 rows of four each: every 16-row block and wave
+    which, height, gap = i % 64, 38.0 + (i % 19) * 0.25, (1 + i * 7 % 61) / 16.0
+    X[i, which], X[:, 64], X[:, 65] = height, gap, (i % 128) / 1024.0
+    W[place, np.arange(64)] = W[place + 1, np.arange(64)] = 1.0
+    W[place + 1, 64], W[place, 65], W[place + 1, 65] = -1.0, 1.0, 1.0
+    for k in (0, 3):
+        lse, H, ids = estp.token_logprobs(dev(_bits(X, "bf16")), dev(_bits(W, "bf16")), None, k)[1:4]
+        two = np.log1p(np.exp(-gap))
+        want = two + gap / (1.0 + np.exp(gap))
+        assert (np.abs(_wide(H) - want) <= 24 * u * (1.0 + want)).all()
+        assert (np.abs(_wide(lse) - (height + X[:, 65] + two)) <= 4 * u * 64).all()
+        if k:
+            np.testing.assert_array_equal(host(ids)[:, :2], place[which][:, None] + np.arange(2))
+
+
+@pytest.mark.parametrize("n", [400, 2000])
+def test_entropy_of_peaked_distributions(n):
+    # modes of 10 to 17 nats over logits of deviation 0.9, in any tile, at temperature 0.7.  A sum of weights is off by its
+    # chain, 512 u, by 40 u of merges and by the weights' own errors, 300 u: exponents of up to 60 in base 2 and three moves
+    # of a reference of up to 60.  So the mode's is off by 600 u, and the others' move H by 852 u p (|log p| + H) at most
+    d, V = 64, 128256
+    g = np.random.default_rng(n)
+    W = np.zeros((V, d))
+    W[:, :32] = g.integers(-8, 9, (V, 32)) / 32.0
+    X = np.zeros((n, d))
+    X[:, :32] = g.integers(-8, 9, (n, 32)) / 8.0
+    X[:, :32] *= 0.7 * 0.9 / np.sqrt((X[:, :32] ** 2).sum(axis=1, keepdims=True) * (W[:, :32] ** 2).mean())
+    X[:, :32] = np.round(X[:, :32] * 64) / 64
+    t = g.integers(0, V, n)
+    W[t[:31], 32 + np.arange(31)] = 1.0
+    X[np.arange(n), 32 + np.arange(n) % 31] = 0.7 * g.uniform(10.0, 17.0, n)
+    X, W = _bits(X, "bf16"), _bits(W, "bf16")
+    H = estp.token_logprobs(dev(X), dev(W), None, 5, 0.7)[2]
+    some = np.arange(0, n, n // 62)
+    ref = HD.token_logprobs(X[some], W, None, 5, 0.7)["H"]
+    assert (np.abs(_wide(H)[some] - ref) <= (600 + 1704 * ref) * OP.U).all() and ref.min() < 0.6
