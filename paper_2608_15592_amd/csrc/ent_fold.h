@@ -1,5 +1,6 @@
-// The running entropy state of a token's logits, shared by the matrix-core kernels that stream the LM head (entropy.hip,
-// logprobs.hip).
+// The running entropy state of a token's logits in the matrix-core kernels that stream the LM head: the exponent of a weight
+// and the rebased state are entropy.hip's and logprobs.hip's, the fold of a tile entropy.hip's.  (logprobs.hip has its own,
+// which looks for a maximum and rebases only where a sum has grown: its logits stay in registers, a column at a time.)
 #pragma once
 
 #include "estp_common.h"
@@ -23,7 +24,7 @@ __device__ __forceinline__ Ent2 rebased(Ent2 e) {
 }
 
 // Fold of a finished tile into one lane's running state of one token: the lane's 32 logits z(i, r) of
-// vocabulary rows 16 i + r past its first, live where 16 i + r < lim; times c2 they are in base 2.
+// vocabulary rows 16 i + r past its first, live where 16 i + r < lim.
 //
 // The state (m, s, t) is kept relative to a reference m that is the running
 // log-sum-exp after each tile (rebased so that s = 1).  Full tiles are then
@@ -36,7 +37,7 @@ __device__ __forceinline__ Ent2 rebased(Ent2 e) {
 // next-token mode kernel spilled 17 instead of 13 registers and took 1% longer
 // (8192 tokens, V 151936, d 1536).  test_few_tokens_change_no_bit holds the two equal.
 template <typename Z>
-__device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int lim, float c2, Z&& z) {
+__device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int lim, Z&& z) {
   bool exact = ragged;
   if (!ragged) {
     if (first) {  // first tile: the tile's own max is the reference
@@ -45,14 +46,14 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
       for (int i = 0; i < kFoldBlocks; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, z(i, r));
-      e = Ent2{mx * c2, 0.f, 0.f};
+      e = Ent2{mx * kLog2e, 0.f, 0.f};
     }
     float s = e.s, t = e.t;
 #pragma unroll
     for (int i = 0; i < kFoldBlocks; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float dd = fmaf(z(i, r), c2, -e.m);
+        const float dd = fmaf(z(i, r), kLog2e, -e.m);
         const float p = fast_exp2(dd);
         s += p;
         t = fmaf(p, dd, t);
@@ -73,7 +74,7 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
         const bool live = !ragged || i * 16 + r < lim;
         mx = live ? fmaxf(mx, z(i, r)) : mx;
       }
-    const float mnew = fmaxf(e.m, mx * c2);
+    const float mnew = fmaxf(e.m, mx * kLog2e);
     const float mref = fmaxf(mnew, -0x1p127f);  // finite for a lane with no live row yet
     const float dl = fmaxf(e.m - mnew, kExp2Floor);
     const float sc = fast_exp2(dl);
@@ -85,7 +86,7 @@ __device__ __forceinline__ Ent2 fold_tile(Ent2 e, bool first, bool ragged, int l
       for (int r = 0; r < 4; ++r) {
         // dead rows enter as -inf: dd clamps to the floor and adds 0 * floor
         const bool live = !ragged || i * 16 + r < lim;
-        const float dd = exp2_arg(fmaf(live ? z(i, r) : -INFINITY, c2, -mref));
+        const float dd = exp2_arg(fmaf(live ? z(i, r) : -INFINITY, kLog2e, -mref));
         const float p = fast_exp2(dd);
         s += p;
         t = fmaf(p, dd, t);

@@ -790,7 +790,7 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_few_kernel(
           const int vt = vs + tile * n_vsplit;
           const bool ragged = (vt + 1) * kBV > V;
           const int row0 = vt * kBV + wv * 128 + 4 * sq, lim = V - row0;
-          st = fold_tile(st, tile == 0, ragged, lim, kLog2e, [&](int i, int r) { return z[i][r]; });
+          st = fold_tile(st, tile == 0, ragged, lim, [&](int i, int r) { return z[i][r]; });
           if (kArg) {
             float tb = -INFINITY;  // the tile's largest live logit
 #pragma unroll
