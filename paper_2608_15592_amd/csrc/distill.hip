@@ -404,9 +404,7 @@ extern "C" int estp_distill_loss(const void* X, const void* W, const int32_t* id
     kernel<<<dim3(unsigned(n)), dim3(unsigned(threads)), 0, s>>>(x, w, ids, logp, d, V, K, renormalise != 0, inv_t, p.m,
                                                                  p.s, p.states, lse, loss, logq);
   };
-  // 16 waves a token or 4, d 2048, in us: 12 tokens of 16 entries 7.4 and 7.2, 200 of 16 12.5 and 14.2, 900 of 16 28 and 18,
-  // 202 of 100 27 and 68, 901 of 100 65 and 86; d 4096, 400 of 32 31 and 49
-  const bool wide = n <= 256 || K > 24;
+  const bool wide = pick_threads(size_t(n), K) == 1024;
   if (dtype == ESTP_F32) {
     const float *x = static_cast<const float*>(X), *w = static_cast<const float*>(W);
     wide ? go(distill_pick_kernel<float, 1024>, 1024, x, w) : go(distill_pick_kernel<float, 256>, 256, x, w);

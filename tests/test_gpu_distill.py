@@ -428,3 +428,21 @@ def test_outputs_end_where_their_arrays_end(dtype, n, d, V):
     ref = HD.distill(*case[:4], 1.0, True, case[4], dtype)
     for name, a in (("loss", loss), ("lse", lse), ("logq", logq.view(n, 7)), ("dX", dX), ("dW", dW)):
         assert (np.abs(_wide(a) - ref[name]) <= ref[name + "_bound"]).all(), name
+
+
+def test_the_most_tokens_that_a_call_takes():
+    # 2^22 tokens of 25 entries, of which a few rows are compared
+    n, d, V, K = 1 << 22, 32, 70, 25
+    Xs, W, _, _ = _inputs(81, 4096, d, V, "bf16")
+    g = torch.Generator(device="cuda").manual_seed(82)
+    X = dev(Xs).repeat(n // 4096, 1)
+    ids = torch.randint(0, V, (n, K), generator=g, device="cuda", dtype=torch.int32)
+    logp = torch.randn(n, K, generator=g, device="cuda")
+    grad = torch.rand(n, generator=g, device="cuda")
+    loss, lse, logq = estp.distill_loss(X, dev(W), ids, logp)
+    dX, _ = estp.distill_loss_backward(X, dev(W), ids, logp, lse, logq, grad, want_dW=False)
+    rows = np.concatenate([np.arange(0, 70), np.arange(n // 2 - 30, n // 2 + 30), np.arange(n - 70, n)])
+    some = [a[dev(rows)] for a in (ids, logp, grad)]
+    ref = HD.distill(Xs[rows % 4096], W, *(host(a) for a in some[:2]), 1.0, True, host(some[2]), "bf16")
+    for name, a in (("loss", loss), ("lse", lse), ("logq", logq), ("dX", dX)):
+        assert (np.abs(_wide(a[dev(rows)]) - ref[name]) <= ref[name + "_bound"]).all(), name

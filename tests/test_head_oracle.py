@@ -153,3 +153,14 @@ def test_plans_of_log_probability_calls(tmp_path):
     assert r.returncode == 0, r.stderr[-3000:]
     r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0, r.stdout + r.stderr
+
+
+def test_launches_of_a_teachers_entries(tmp_path):
+    exe = str(tmp_path / "pick_threads")
+    here = os.path.dirname(os.path.abspath(__file__))
+    cmd = [build.hipcc(), f"--offload-arch={build.ARCH}", "-O1", "-std=c++17", f"-I{build.INCLUDE}", f"-I{build.CSRC}",
+           os.path.join(here, "host", "pick_threads.hip"), "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0, r.stdout + r.stderr
