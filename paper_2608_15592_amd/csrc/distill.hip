@@ -54,7 +54,7 @@ __device__ __forceinline__ TeacherRow teacher_row(const int32_t* __restrict__ id
   }
   r.live = __any(r.logp[0] != -INFINITY || r.logp[1] != -INFINITY);  // (a NaN is weight: it reaches the loss)
   if (renormalise) {
-    const float ref = fmaxf(wave_max(fmaxf(r.logp[0], r.logp[1])), -0x1p127f);
+    const float most = wave_max(fmaxf(r.logp[0], r.logp[1])), ref = most == -INFINITY ? 0.f : most;
 #pragma unroll
     for (int u = 0; u < 2; ++u) r.p[u] = fast_exp2((r.logp[u] - ref) * kLog2e);
     const float sum = r.live ? wave_sum(r.p[0] + r.p[1]) : 1.f, log_sum = kLn2 * fast_log2(sum);

@@ -446,3 +446,28 @@ def test_the_most_tokens_that_a_call_takes():
     ref = HD.distill(Xs[rows % 4096], W, *(host(a) for a in some[:2]), 1.0, True, host(some[2]), "bf16")
     for name, a in (("loss", loss), ("lse", lse), ("logq", logq), ("dX", dX)):
         assert (np.abs(_wide(a[dev(rows)]) - ref[name]) <= ref[name + "_bound"]).all(), name
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_any_constant_may_be_added_to_a_renormalised_row(dtype):
+    # the type's lowest and highest numbers among them: as a row of zeros, bit for bit
+    n, V = 40, 300
+    X, W, ids, logp, g = map(dev, _case(91, n, 64, V, 7, dtype, ignored=0.0))
+    logp.zero_()
+    want = estp.distill_loss(X, W, ids, logp)
+    want += estp.distill_loss_backward(X, W, ids, logp, *want[1:], g)
+    big = torch.finfo(torch.float32).max
+    for i, c in enumerate((-big, big, -2.0 ** 127, -1.1 * 2.0 ** 127, 1e30, -1e30, -3.0)):
+        logp[i::7] = c
+    got = estp.distill_loss(X, W, ids, logp)
+    got += estp.distill_loss_backward(X, W, ids, logp, *got[1:], g)
+    assert torch.isfinite(got[0]).all() and all(torch.equal(a, b) for a, b in zip(got, want))
+    # beside other numbers the lowest has no weight
+    logp.zero_()
+    logp[:, ::2] = -float("inf")
+    want = estp.distill_loss(X, W, ids, logp)
+    logp[:, ::2] = -big
+    live = (((ids >= 0) & (ids < V))[:, 1::2]).any(dim=1)
+    assert live.any()
+    for a, b in zip(estp.distill_loss(X, W, ids, logp), want):
+        assert torch.equal(a[live], b[live])
