@@ -1262,7 +1262,8 @@ int launch_loss_backward(const void* X, const void* W, const int32_t* targets, c
       const bool odd = d % 64 != 0;
       auto grad_kernel = p.tile_toks == 128 ? (odd ? loss_grad_mfma_kernel<4, true> : loss_grad_mfma_kernel<4, false>)
                                             : (odd ? loss_grad_mfma_kernel<8, true> : loss_grad_mfma_kernel<8, false>);
-      if (teacher && p.parts == 2 && few::takes(n, d, dtype) && size_t(p.Vc) * 256 < (size_t(1) << 32))
+      // (its 32-bit offsets: 128 rows of a piece of 2^19 columns at most, 2^27 bytes)
+      if (teacher && p.parts == 2 && few::takes(n, d, dtype))
         few::choose(n, d, [&](auto steps, auto nb) {
           loss_grad_few_kernel<decltype(steps)::value, decltype(nb)::value>
               <<<dim3(few::workgroups(p.Vc / 16)), dim3(64 * few::kWaves), 0, s>>>(Xc, Wt, b.n_live, d, V, v0, p.Vc, b.lc,
