@@ -471,3 +471,37 @@ def test_any_constant_may_be_added_to_a_renormalised_row(dtype):
     assert live.any()
     for a, b in zip(estp.distill_loss(X, W, ids, logp), want):
         assert torch.equal(a[live], b[live])
+
+
+@pytest.mark.parametrize("n", [70, 130])
+def test_f32_from_parts_with_an_infinite_number_in_a_row_of_X(n):
+    # products and sums of infinite numbers are as they are without parts: of up to 96 tokens and of more
+    d, V, c = 64, 50000, 11
+    X, W, ids, logp, g = _case(23, n, d, V, 6, "f32")
+    clean = _check((X, W, ids, logp, g), "f32")
+    live = (((ids >= 0) & (ids < V)) & (logp > -np.inf)).any(axis=1).nonzero()[0]
+    r = int(live[5])
+    Xd, Wd, idd, lpd, gd = map(dev, (X, W, ids, logp, g))
+    bad = Xd.clone()
+    bad[r, c] = float("inf")
+    rest = torch.arange(n, device="cuda") != r
+    # its own row is lost, and with it dW; the other rows keep their bits
+    loss, lse, logq = estp.distill_loss(bad, Wd, idd, lpd)
+    dX, dW = estp.distill_loss_backward(bad, Wd, idd, lpd, lse, logq, gd)
+    held = dev((ids[r] >= 0) & (ids[r] < V))
+    assert not torch.isfinite(lse[r]) and not torch.isfinite(loss[r]) and not torch.isfinite(logq[r][held]).any()
+    assert not torch.isfinite(dX[r]).any() and not torch.isfinite(dW).any()
+    for name, a in (("loss", loss), ("lse", lse), ("logq", logq), ("dX", dX)):
+        assert torch.equal(a[rest], clean[name][rest]), name
+    # beside the log-sum-exps of finite rows its weights are infinite where W's number is above 0 and 0 where it is below
+    dX, dW = estp.distill_loss_backward(bad, Wd, idd, lpd, clean["lse"], clean["logq"], gd)
+    assert not torch.isfinite(dX[r]).any() and torch.equal(dX[rest], clean["dX"][rest])
+    other = torch.ones(V, dtype=torch.bool, device="cuda")
+    other[idd[r][held].long()] = False
+    up, down = other & (Wd[:, c] > 0), other & (Wd[:, c] < 0)
+    sign = torch.sign(gd[r] * bad[r])
+    assert torch.equal(dW[up], (sign * float("inf")).expand(int(up.sum()), d)) and torch.isnan(dW[down][:, c]).all()
+    gd[r] = 0.0
+    without = estp.distill_loss_backward(Xd, Wd, idd, lpd, clean["lse"], clean["logq"], gd)[1]
+    keep = torch.arange(d, device="cuda") != c
+    assert torch.equal(dW[down][:, keep], without[down][:, keep])

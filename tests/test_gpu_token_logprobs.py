@@ -471,3 +471,24 @@ def test_entropy_of_peaked_distributions(n):
     some = np.arange(0, n, n // 62)
     ref = HD.token_logprobs(X[some], W, None, 5, 0.7)["H"]
     assert (np.abs(_wide(H)[some] - ref) <= (600 + 1704 * ref) * OP.U).all() and ref.min() < 0.6
+
+
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 1, 5000), ("bf16", 20, 5000), ("bf16", 60, 5000), ("f32", 60, 49300)])
+def test_values_beside_a_row_of_weights_with_an_infinite_number(dtype, n, V):
+    # at places of the depth that different waves take: the values are those of the vocabulary without that row
+    d = 2048
+    X, W, _, _ = _inputs(n, n, d, V, dtype)
+    low = V // 3
+    rest = np.delete(np.arange(V), low)
+    for at in (0, d // 8 + 1, d // 2, d - 1):
+        Xd, Wd = dev(X), dev(W)
+        Xd[:, at], Wd[low, at] = 1.0, float("-inf")
+        _, lse, H, ids, top = estp.token_logprobs(Xd, Wd, None, 5)
+        ref = HD.token_logprobs(_bits(host(Xd.float()), dtype), W[rest], None, 5)
+        assert (np.abs(_wide(lse) - ref["lse"]) <= ref["lse_bound"]).all()
+        assert (np.abs(_wide(H) - ref["H"]) <= ref["H_bound"]).all()
+        assert (host(ids) != low).all()
+        where = np.searchsorted(rest, host(ids))
+        at_ids, best = (np.take_along_axis(ref["s"], i, 1) for i in (where, ref["top_id"]))
+        assert (np.abs(at_ids - best) <= ref["margin"][:, None]).all()
+        assert (np.abs(_wide(top) - (at_ids - ref["lse"][:, None])) <= ref["logprob_bound"][:, None]).all()
