@@ -398,7 +398,8 @@ ESTP_API int estp_token_loss_backward(const void* X, const void* W, const int32_
  * others.  Rows with a NaN logit have NaN values; their top_id are indices in [0, V) all the same.
  * X, W, d and dtype are those of estp_token_entropy.  fp32 logits of larger calls are formed by
  * the bf16 matrix cores, each number as the sum of three bf16 ones, and are as exact as fp32 sums
- * (there a number within 1/256 of the largest counts as infinite).
+ * (there a number within 1/256 of the largest counts as infinite, and what a number has below
+ * 2^-126 may be left out, of numbers below 2^-110 so some of their last bits).
  * V > 2^24 returns ESTP_ERR_UNSUPPORTED.  Bitwise repeatable; the last bits are those of the
  * kernels that a call runs, which follow n_tok, d and V.  A workspace of a call serves every call
  * of no more tokens and no larger k on the same W; it is largest for 2048 tokens of ESTP_BF16 and

@@ -4,7 +4,9 @@
 // A number of 24 bits is the sum of three bf16 numbers, each what rounding has left of it: x = x1 + x2 + x3.  Of the nine
 // products of two numbers' parts, six are formed: x1 w1, and apart from it, where rounding costs less, x1 w2, x2 w1, x2 w2,
 // x1 w3 and x3 w1.  The other three are below 2^-26 of |x w|, a quarter of what rounding the product to fp32 may take.  So a
-// logit is as exact as a chain of fp32 FMAs, at a sixth of the bf16 rate, 2.6 times that of v_mfma_f32 instructions.
+// logit is as exact as a chain of fp32 FMAs, at a sixth of the bf16 rate, 2.6 times that of v_mfma_f32 instructions.  (The
+// third part of a number below 2^-110 is below the smallest normal one, 2^-126, and such parts may be taken as 0: numbers
+// are held to 2^-24 of themselves or to 2^-126, whichever is more.)
 //
 // The tokens are few beside the vocabulary: their parts are written once (split_rows_kernel).  W is read as it is, and 16
 // rows of a wave are split, 44 vector instructions, between the products of the 16 before them, 36 of 96 tokens.  The second

@@ -505,3 +505,23 @@ def test_f32_from_parts_with_an_infinite_number_in_a_row_of_X(n):
     without = estp.distill_loss_backward(Xd, Wd, idd, lpd, clean["lse"], clean["logq"], gd)[1]
     keep = torch.arange(d, device="cuda") != c
     assert torch.equal(dW[down][:, keep], without[down][:, keep])
+
+
+@pytest.mark.parametrize("n", [70, 130])
+def test_f32_from_parts_of_very_small_numbers(n):
+    # tokens of 60 to 95 nats below the others: entries of G from 2^-90 to below the smallest number.  Parts, weights and
+    # products below 2^-126 may be taken as 0, which is all that dW is off by beside the bound of fp32 sums
+    d, V = 64, 50000
+    X, W, ids, logp, g = _case(25, n, d, V, 6, "f32")
+    X[:, 0] = 1.0
+    far = np.arange(3, V, 5)
+    W[far, 0] = -(60.0 + 35.0 * np.random.default_rng(26).uniform(size=len(far))).astype(np.float32)
+    Xd, Wd, idd, lpd, gd = map(dev, (X, W, ids, logp, g))
+    loss, lse, logq = estp.distill_loss(Xd, Wd, idd, lpd)
+    dX, dW = estp.distill_loss_backward(Xd, Wd, idd, lpd, lse, logq, gd)
+    ref = HD.distill(X, W, ids, logp, 1.0, True, g, "f32")
+    small = n * 2.0 ** -126 * (3 * np.abs(X).max() + 8)
+    for name, a, room in (("loss", loss, 0), ("lse", lse, 0), ("logq", logq, 0), ("dX", dX, 0), ("dW", dW, small)):
+        assert (np.abs(_wide(a) - ref[name]) <= ref[name + "_bound"] + room).all(), name
+    tiny = np.abs(ref["dW"][far]).max(axis=1)
+    assert (tiny < 2.0 ** -118).any() and (tiny > 2.0 ** -100).any()
