@@ -24,7 +24,8 @@ constexpr int kWaves = 8;
 constexpr int kRows = 16;  // of a tile
 constexpr int kWgs = 256;  // one on each compute unit
 
-// Products of 32 k of a wave, and blocks of 16 tokens: what both take of the registers sets which calls come here.
+// Products of 32 k of a wave, and blocks of 16 tokens: what both take of the registers sets which calls come here.  A slot of
+// the ring takes 8 KB for each of them: 16 and the sums' 32 KB fill the 160 KB of LDS.
 inline int blocks_of(int64_t n) { return n <= 16 ? 1 : n <= 32 ? 2 : 4; }
 inline bool takes(int64_t n_tok, int d, int dtype) {
   if (dtype != ESTP_BF16 || n_tok > 64 || d % (32 * kWaves) != 0) return false;
