@@ -287,15 +287,15 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_gemm_kernel(
     const bool live = pf_tile < n_my_tiles;
     Part p;
     p.dst = lds + pf_slot * G::kPartBytes + G::kRowsPerInst * wave * G::kRowBytes;
-    const Window w = window(live ? min(kBV, V - pf_vt * kBV) : 0, uint32_t(row_stride), uint32_t(pf_ks) * G::kRowBytes);
-    p.soff = w.offset;
+    p.soff = uint32_t(pf_ks) * G::kRowBytes;  // (0 past the last tile)
     if (op == 0) {
       // past the last tile pf_w points beyond W, but the empty resource never reads it
-      p.rsrc = make_rsrc(pf_w, w.bytes);
+      const uint32_t rows = live ? uint32_t(min(kBV, V - pf_vt * kBV)) : 0u;
+      p.rsrc = make_rsrc(pf_w, rows * uint32_t(row_stride));
     } else {
       p.rsrc = live ? rx : r_none;
       const bool wrap = pf_ks + 1 == nk;
-      pf_ks = wrap ? 0 : pf_ks + 1;
+      pf_ks = next_stage(pf_ks, nk, live);
       if (wrap) {
         ++pf_tile;
         pf_vt += n_vsplit;
@@ -680,11 +680,11 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_few_kernel(
     const bool live = pf_g < n_groups;
     const int64_t row0 = int64_t(vs + (live ? pf_g : 0) * kFewTiles * n_vsplit) * kBV;
     const int64_t rows = min(int64_t(V) - row0, int64_t((kFewTiles - 1) * n_vsplit + 1) * kBV);
-    const Window w = window(live ? int(rows) : 0, row_stride, uint32_t(pf_ks) * 128u);
-    const buf_rsrc_t rw = make_rsrc(reinterpret_cast<const char*>(W) + size_t(row0) * row_stride, w.bytes);
+    const buf_rsrc_t rw =
+        make_rsrc(reinterpret_cast<const char*>(W) + size_t(row0) * row_stride, live ? uint32_t(rows) * row_stride : 0u);
     const buf_rsrc_t rxx = live ? rx : make_rsrc(X, 0u);
     char* dst = lds + pf_slot * kStage + 1024 * wave;
-    const uint32_t soff = w.offset;
+    const uint32_t soff = uint32_t(pf_ks) * 128u;  // (0 past the last group)
 #pragma unroll
     for (int q = 0; q < LW; ++q)
       lds_dma16_buf<kStreamW ? kNonTemporal : 0>(rw, w_off[q], soff, dst + 1024 * kWaves * q);
@@ -692,7 +692,7 @@ __global__ __launch_bounds__(kWaves * 64, 1) void entropy_few_kernel(
     for (int q = 0; q < LX; ++q) lds_dma16_buf(rxx, x_off[q], soff, dst + kFewRows * 128 + 1024 * kWaves * q);
     pf_slot = pf_slot + 1 == kFewRing ? 0 : pf_slot + 1;
     const bool wrap = pf_ks + 1 == nk;
-    pf_ks = wrap ? 0 : pf_ks + 1;
+    pf_ks = next_stage(pf_ks, nk, live);
     pf_g += wrap;
   };
   const int fr = lane & 15, fq = lane >> 4;

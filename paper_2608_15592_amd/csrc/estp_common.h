@@ -51,6 +51,9 @@ struct Window {
 __host__ __device__ __forceinline__ Window window(int rows, uint32_t pitch, uint32_t offset) {
   return {rows > 0 ? uint32_t(rows) * pitch : 0u, rows > 0 ? offset : 0u};
 }
+// The stage after stage ks of nk along the depth of a tile.  Past the last tile (not live) it stays the first, so that the
+// empty resources there come with an offset of 0 by themselves.
+__host__ __device__ __forceinline__ int next_stage(int ks, int nk, bool live) { return ks + 1 == nk ? 0 : ks + int(live); }
 
 // 16-byte buffer -> LDS transfer (buffer_load_dwordx4 ... lds): lane l reads
 // the 16 bytes at voffset(l) + soffset of the resource; they land in LDS at

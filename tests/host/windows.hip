@@ -1,5 +1,5 @@
-// What transfers along rows may read, on the host, at the sizes of the fp32 products by parts and of the entropy kernels:
-// within the rows that there are, and of none of them with an offset of 0.
+// What transfers along rows may read, on the host: within the rows that there are, and of none of them with an offset of 0
+// (the fp32 products by parts); every stage of every tile once and then the first one alone (the entropy kernels).
 #include <stdio.h>
 
 #include "f32_split.h"
@@ -8,7 +8,7 @@ using namespace estp::detail;
 
 int main() {
   int empty = 0, bad = 0;
-  for (int d : {32, 64, 72, 264, 1536, 4096, 1 << 20}) {
+  for (int d : {64, 72, 264, 1536, 4096, 1 << 20}) {
     const uint32_t dp = uint32_t(split::padded(d));
     for (int rows : {-1000000, -17, -1, 0, 1, 15, 16, 255, 256})
       for (uint32_t k = 0; k < dp; k += split::kDepth)
@@ -22,6 +22,17 @@ int main() {
           if (!ok && bad++ < 5) printf("d %d, %d rows, k %u: %u bytes at %u\n", d, rows, k, w.bytes, w.offset);
         }
   }
+  for (int nk : {1, 2, 3, 7, 64})
+    for (int tiles : {0, 1, 2, 5}) {
+      int tile = 0, ks = 0;
+      for (int i = 0; i < (tiles + 3) * nk; ++i) {
+        const bool live = tile < tiles, wrap = ks + 1 == nk;
+        const bool ok = live ? tile == i / nk && ks == i % nk : ks == 0;
+        if (!ok && bad++ < 5) printf("%d tiles of %d stages: stage %d is %d\n", tiles, nk, i, ks);
+        ks = estp::next_stage(ks, nk, live);
+        tile += wrap;
+      }
+    }
   printf("%d empty windows, %d wrong\n", empty, bad);
   return bad != 0 || empty == 0;
 }
